@@ -358,6 +358,145 @@ DSM_API dsm_status dsm_test_stream(int32_t kind, float* dev_buf, int64_t n_elems
                                    uint32_t* dev_words, uint32_t pattern, void* stream);
 
 /*
+ * Language-model operators beside the optimizer path: the output layer's loss
+ * with its gradients, and updates that are orthogonalised instead of signed.
+ *
+ * They have no context: each call takes a problem (sizes and types), buffers
+ * and a workspace, enqueues its work on buffers->stream and returns.  The
+ * workspace holds nothing between calls; two calls that may overlap in time
+ * (on two streams) need one each.  Data pointers need the alignment of their
+ * elements, the workspace 256 bytes.  A problem with nothing to compute (no
+ * matrices, an empty matrix) succeeds and enqueues nothing.
+ */
+typedef enum dsm_dtype { DSM_F32 = 0, DSM_BF16 = 1 } dsm_dtype;
+
+/*
+ * Softmax cross entropy of a linear layer: logits z = h w^T of `tokens` rows
+ * over a vocabulary of `vocab`.
+ */
+typedef struct dsm_ce_problem {
+    int64_t tokens; /* T in [0, 2^20] */
+    int64_t dim;    /* D in [1, 2^16] */
+    int64_t vocab;  /* V in [1, 2^20] */
+    int32_t dtype;  /* dsm_dtype of h, w, dh and dw */
+    int32_t grads;  /* 1: dh and dw are wanted too */
+} dsm_ce_problem;
+
+typedef struct dsm_ce_buffers {
+    const void* h;         /* [T, D], rows h_stride elements apart (>= D) */
+    int64_t h_stride;
+    const void* w;         /* [V, D], rows w_stride elements apart */
+    int64_t w_stride;
+    const int64_t* target; /* [T]; a token whose target lies outside [0, V) is left
+                              out: no loss, no gradient, and not counted */
+    const float* weight;   /* [T] weight of each token's loss, or NULL for 1 */
+    float* total;          /* [1] */
+    float* loss;           /* [T] loss of each token, unweighted; 0 where left out */
+    float* lse;            /* [T] log of the sum of exp z, or NULL */
+    void* dh;              /* [T, D], rows dh_stride apart; NULL without gradients */
+    int64_t dh_stride;
+    void* dw;              /* [V, D], rows dw_stride apart; NULL without gradients */
+    int64_t dw_stride;
+    void* workspace;
+    int64_t workspace_bytes;
+    void* stream;
+} dsm_ce_buffers;
+
+/* dsm_ce_workspace - host only: the workspace of a problem in bytes.
+ * Errors: DSM_ERR_INVALID_ARG. */
+DSM_API dsm_status dsm_ce_workspace(const dsm_ce_problem* problem, int64_t* workspace_bytes);
+
+/*
+ * dsm_linear_ce - for every token t with its target y in [0, V):
+ *   lse_t = log sum_v exp z_tv;  loss_t = lse_t - z_ty
+ *   total = sum_t c_t loss_t,  c_t = weight_t, divided by the number of such
+ *           tokens (at least 1) when mean != 0
+ * and, where the problem asks for gradients, those of total:
+ *   G_tv = c_t (exp(z_tv - lse_t) - [v = y]);  dh = G w;  dw = G^T h
+ * dh is 0 for the tokens left out; dh and dw are written, not added to.  The
+ * vocabulary is taken in pieces and the logits are never in memory.  Products
+ * of bf16 buffers take bf16 operands, with G rounded to bf16; those of fp32
+ * buffers carry 22 bits.  Everything else is fp32.  Results do not depend on
+ * the order in which the GPU runs: reruns give the same bits.
+ * Non-finite values in h, w or weight reach every output that depends on them.
+ * dh may not overlap h, nor dw w.
+ * Errors: DSM_ERR_INVALID_ARG; DSM_ERR_HIP.
+ */
+DSM_API dsm_status dsm_linear_ce(const dsm_ce_problem* problem, const dsm_ce_buffers* buffers,
+                                 int32_t mean);
+
+/*
+ * A batch of matrices of one shape inside larger buffers: matrix i starts
+ * offsets[i] elements into every buffer of the call, its rows row_stride
+ * elements apart.  In an arena, offsets are those of dsm_layout; copy k of a
+ * contiguous per-worker buffer is k * d_pad elements further.
+ */
+typedef struct dsm_ortho_problem {
+    int64_t rows, cols;     /* each in [0, 2^20], the smaller one at most 2^14 */
+    int64_t row_stride;     /* >= cols */
+    const int64_t* offsets; /* host array [count]; matrices must not overlap */
+    int32_t count;          /* >= 0 */
+    int32_t dtype;          /* dsm_dtype; dsm_ortho_step takes DSM_F32 */
+    int32_t steps;          /* iterations, 1..32; 5 is customary */
+    float eps;              /* >= 0, added to the norm; 1e-7 is customary */
+    const float* coeffs;    /* host array [steps][3] of a, b, c, or NULL for
+                               3.4445, -4.7750, 2.0315 in every iteration */
+} dsm_ortho_problem;
+
+typedef struct dsm_ortho_buffers {
+    const void* in; /* the updates U (dsm_orthogonalize) or gradients g (dsm_ortho_step) */
+    void* out;      /* results; may be `in` itself */
+    float* m;       /* dsm_ortho_step: momentum, updated; NULL for none (u = g) */
+    float* x;       /* dsm_ortho_step: parameters, updated; NULL to write out instead */
+    void* workspace;
+    int64_t workspace_bytes;
+    void* stream;
+} dsm_ortho_buffers;
+
+typedef struct dsm_ortho_hparams {
+    float lr;           /* > 0 */
+    float mu;           /* momentum coefficient in [0, 1] */
+    float scale;        /* factor of the orthogonalised update, e.g. 0.2 sqrt(max(rows, cols)) */
+    float weight_decay; /* decoupled, >= 0 */
+    int32_t nesterov;
+} dsm_ortho_hparams;
+
+/* dsm_ortho_workspace - host only: the workspace of a problem in bytes (a
+ * bounded number of matrices is worked on at a time).  The offsets are not read.
+ * Errors: DSM_ERR_INVALID_ARG; DSM_ERR_UNSUPPORTED for coefficients whose
+ * iterates grow beyond 2^10. */
+DSM_API dsm_status dsm_ortho_workspace(const dsm_ortho_problem* problem, int64_t* workspace_bytes);
+
+/*
+ * dsm_orthogonalize - for every matrix U of the batch:
+ *   X = U / (||U||_F + eps);  `steps` times: A = X X^T, X <- a X + (b A + c A A) X
+ * on the shorter side (for rows > cols, of U^T, transposed back), and out = X:
+ * with the customary coefficients the singular values of U are brought near 1.
+ * A matrix of zeros gives zeros; one with a NaN or infinite entry gives NaN.
+ * fp32 matrices are iterated with 22-bit operands, bf16 ones with 11-bit
+ * operands; sums are fp32, norms fp64.
+ * Errors: DSM_ERR_INVALID_ARG; DSM_ERR_UNSUPPORTED (as dsm_ortho_workspace);
+ * DSM_ERR_HIP.
+ */
+DSM_API dsm_status dsm_orthogonalize(const dsm_ortho_problem* problem,
+                                     const dsm_ortho_buffers* buffers);
+
+/*
+ * dsm_ortho_step - the momentum step of an orthogonalised update, O as above:
+ *   m <- mu m + g;  u = g + mu m (nesterov) or m;  d = scale O(u)
+ *   x given:  x <- x - lr (d + weight_decay x)
+ *   x NULL:   out = d, for instance as the direction input g_rep of
+ *             dsm_local_step with DSM_BASE_SGD_MOMENTUM and beta1 = 0
+ *             (lr and weight_decay are then not used)
+ * The sums of m, u and x are fp32, one rounding per operation.
+ * Errors: DSM_ERR_INVALID_ARG (dtype other than DSM_F32, both or neither of x
+ * and out, hyperparameters); DSM_ERR_UNSUPPORTED (as dsm_ortho_workspace);
+ * DSM_ERR_HIP.
+ */
+DSM_API dsm_status dsm_ortho_step(const dsm_ortho_problem* problem, const dsm_ortho_buffers* buffers,
+                                  const dsm_ortho_hparams* hp);
+
+/*
  * dsm_destroy - synchronises the context's stream and frees the context's
  * host memory.  The caller's device buffers are untouched.  NULL is a no-op.
  */

@@ -9,6 +9,7 @@ import os
 import shutil
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -20,6 +21,9 @@ LIBPATH = os.path.join(LIBDIR, "libdsm.so")
 
 ARCH = "gfx950"
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
+
+KERNELS = ["dsm_kernels.hip", "ortho.hip", "linear_ce.hip"]
+HOST = ["dsm_runtime.cpp", "ops_runtime.cpp"]
 
 # Numerics: one IEEE fp32 rounding per written operation (no FMA contraction),
 # correctly rounded division and square root, denormals kept.  Packed fp32
@@ -60,14 +64,18 @@ def build(verbose=False, out=LIBPATH):
     objdir = os.path.join(OBJDIR, "default")
     os.makedirs(objdir, exist_ok=True)
     cc = hipcc()
-    k_obj = os.path.join(objdir, "dsm_kernels.o")
-    r_obj = os.path.join(objdir, "dsm_runtime.o")
-    _run([cc, "-x", "hip", *COMMON_FLAGS, *DEVICE_FLAGS, "-c",
-          os.path.join(CSRC, "dsm_kernels.hip"), "-o", k_obj], verbose)
-    _run([cc, "-x", "c++", "-D__HIP_PLATFORM_AMD__", f"-I{ROCM}/include", *COMMON_FLAGS,
-          "-c", os.path.join(CSRC, "dsm_runtime.cpp"), "-o", r_obj], verbose)
+    objs = [os.path.join(objdir, os.path.splitext(src)[0] + ".o") for src in KERNELS + HOST]
+
+    def compile_one(job):
+        src, obj = job
+        lang = (["-x", "hip", *COMMON_FLAGS, *DEVICE_FLAGS] if src in KERNELS else
+                ["-x", "c++", "-D__HIP_PLATFORM_AMD__", f"-I{ROCM}/include", *COMMON_FLAGS])
+        _run([cc, *lang, "-c", os.path.join(CSRC, src), "-o", obj], verbose)
+
+    with ThreadPoolExecutor(max_workers=len(objs)) as pool:
+        list(pool.map(compile_one, zip(KERNELS + HOST, objs)))
     tmp = out + ".tmp"
-    _run([cc, "-shared", f"--offload-arch={ARCH}", "-o", tmp, k_obj, r_obj,
+    _run([cc, "-shared", f"--offload-arch={ARCH}", "-o", tmp, *objs,
           "-Wl,--no-undefined", "-Wl,-soname,libdsm.so"], verbose)
     os.replace(tmp, out)
     return out

@@ -320,6 +320,12 @@ void end_round(dsm_ctx* ctx, bool broadcast, bool randomized) {
 
 }  // namespace
 
+namespace dsm {
+
+dsm_status set_thread_error(dsm_status st, const char* message) { return fail(nullptr, st, "%s", message); }
+
+}  // namespace dsm
+
 extern "C" {
 
 dsm_status dsm_layout(const dsm_problem* problem, int64_t* arena_elems, int64_t* tensor_offsets,

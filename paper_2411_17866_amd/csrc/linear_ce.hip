@@ -1,0 +1,491 @@
+// Softmax cross entropy of a linear layer over a large vocabulary on gfx950,
+// with the gradients of the layer's input and weight.
+//
+//   z = h w^T;  lse_t = log sum_v exp z_tv;  loss_t = lse_t - z_t,target
+//   G_tv = c_t (exp(z_tv - lse_t) - [v = target_t]);  dh = G w;  dw = G^T h
+//
+// The logits are never in memory.  A first pass over the vocabulary computes
+// them tile by tile and keeps of each row of a tile its largest logit and the
+// sum of exp(z - largest); joined over the tiles they give lse.  A second pass
+// takes the vocabulary in pieces: it computes a piece's logits again, writes G
+// for the piece (16 bits, or two halves), and multiplies it by w and by h.  So
+// with gradients the matrix cores do 8 T V D operations where keeping all
+// logits would need 6.
+//
+// Types.  bf16: the products take bf16 as it is, G rounds to bf16 once (its
+// sums have thousands of terms whose rounding errors are independent; they stay
+// below what rounding the gradients to bf16 costs).  fp32: h, w and G go as two
+// fp16 halves each (gemm_tile.h), scaled by powers of two so that the largest
+// finite entry lies just under fp16's largest number.  Logits, softmax statistics, losses and
+// sums are fp32.
+//
+// A token whose target lies outside [0, vocab) has no loss and no gradient, and
+// what its row of h holds, NaN included, reaches no output but its own zeros.
+#include <hip/hip_runtime.h>
+
+#include "gemm_tile.h"
+#include "ops_internal.h"
+
+#pragma clang fp contract(off)
+
+namespace dsm {
+namespace {
+
+using tile::f4;
+using tile::kContig;
+using tile::kStrided;
+using tile::Operand;
+
+typedef unsigned short u16;
+typedef u16 u16x4 __attribute__((ext_vector_type(4)));
+typedef u16 u16x8 __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ u16 float_to_bf16(float v) {
+    return __builtin_bit_cast(u16, static_cast<__bf16>(v));
+}
+__device__ __forceinline__ float half_to_float(u16 v) {
+    return static_cast<float>(__builtin_bit_cast(_Float16, v));
+}
+__device__ __forceinline__ u16 float_to_half(float v) {
+    return __builtin_bit_cast(u16, static_cast<_Float16>(v));
+}
+
+struct Scalars {
+    uint32_t h_max, w_max;  // bits of the largest finite |h| and |w| (fp32 buffers)
+    uint32_t c_max;         // bits of the largest finite |c_t|
+    int32_t valid;          // tokens whose target lies in the vocabulary
+};
+
+// The power of two that brings a largest magnitude into [2^14, 2^15).
+__device__ __forceinline__ int exponent_for(uint32_t bits) {
+    if (bits == 0) return 0;
+    int e;
+    frexpf(__builtin_bit_cast(float, bits), &e);
+    return min(15 - e, 120);
+}
+
+__device__ __forceinline__ bool is_valid(int64_t target, int vocab) { return target >= 0 && target < vocab; }
+
+__device__ __forceinline__ uint32_t finite_bits(float v) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, v) & 0x7fffffffu;
+    return b < 0x7f800000u ? b : 0u;
+}
+
+// c_t of every token, their largest magnitude and the number of valid targets.
+__global__ __launch_bounds__(1024) void k_coef(CePlan p, CeBuffers b) {
+    __shared__ int count;
+    __shared__ uint32_t c_max;
+    if (threadIdx.x == 0) {
+        count = 0;
+        c_max = 0;
+    }
+    __syncthreads();
+    int mine = 0;
+    for (int t = threadIdx.x; t < p.tokens; t += 1024) mine += is_valid(b.target[t], p.vocab);
+    for (int w = 32; w > 0; w >>= 1) mine += __shfl_xor(mine, w);
+    if ((threadIdx.x & 63) == 0) atomicAdd(&count, mine);
+    __syncthreads();
+    const float by = b.mean ? static_cast<float>(max(count, 1)) : 1.0f;
+    float* coef = reinterpret_cast<float*>(b.workspace + p.coef);
+    uint32_t top = 0;
+    for (int t = threadIdx.x; t < p.tokens; t += 1024) {
+        float c = 0.f;
+        if (is_valid(b.target[t], p.vocab)) c = (b.weight ? b.weight[t] : 1.0f) / by;
+        coef[t] = c;
+        top = max(top, finite_bits(c));
+    }
+    atomicMax(&c_max, top);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        Scalars* s = reinterpret_cast<Scalars*>(b.workspace + p.scalars);
+        s->h_max = 0;
+        s->w_max = 0;
+        s->c_max = c_max;
+        s->valid = count;
+    }
+}
+
+// The largest finite magnitude of h's valid rows (blockIdx.y = 0) and of w (1).
+__global__ __launch_bounds__(256) void k_largest(CePlan p, CeBuffers b) {
+    const bool of_w = blockIdx.y != 0;
+    const float* src = static_cast<const float*>(of_w ? b.w : b.h);
+    const int64_t stride = of_w ? b.w_stride : b.h_stride;
+    const int rows = of_w ? p.vocab : p.tokens;
+    uint32_t top = 0;
+    for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4) {
+        if (!of_w && !is_valid(b.target[r], p.vocab)) continue;
+        const float* row = src + r * stride;
+        for (int c = threadIdx.x & 63; c < p.dim; c += 64) top = max(top, finite_bits(row[c]));
+    }
+    for (int w = 32; w > 0; w >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), w)));
+    Scalars* s = reinterpret_cast<Scalars*>(b.workspace + p.scalars);
+    if ((threadIdx.x & 63) == 0 && top) atomicMax(of_w ? &s->w_max : &s->h_max, top);
+}
+
+// h (blockIdx.y = 0) and w (1) as the products take them: rows of a multiple of
+// 64 columns, zeros in the padding and in h's rows without a valid target.
+template <bool SPLIT>
+__global__ __launch_bounds__(256) void k_operands(CePlan p, CeBuffers b) {
+    const bool of_w = blockIdx.y != 0;
+    const int rows = of_w ? p.vocab : p.tokens;
+    const int64_t stride = of_w ? b.w_stride : b.h_stride;
+    const int64_t ld = of_w ? p.ld_w : p.ld_h;
+    const int cols = static_cast<int>(SPLIT ? ld / 2 : ld);
+    u16* dst = reinterpret_cast<u16*>(b.workspace + (of_w ? p.w : p.h));
+    int e = 0;
+    if constexpr (SPLIT) {
+        const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
+        e = exponent_for(of_w ? s->w_max : s->h_max);
+    }
+    for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4) {
+        const bool keep = of_w || is_valid(b.target[r], p.vocab);
+        u16* out = dst + r * ld;
+        for (int c = (threadIdx.x & 63) * 4; c < cols; c += 256) {
+            u16x4 hi, lo;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if constexpr (SPLIT) {
+                    float v = 0.f;
+                    if (keep && c + q < p.dim)
+                        v = ldexpf(static_cast<const float*>(of_w ? b.w : b.h)[r * stride + c + q], e);
+                    hi[q] = float_to_half(v);
+                    lo[q] = float_to_half(v - half_to_float(hi[q]));
+                } else {
+                    hi[q] = keep && c + q < p.dim
+                                ? static_cast<const u16*>(of_w ? b.w : b.h)[r * stride + c + q]
+                                : u16(0);
+                }
+            }
+            if constexpr (SPLIT) {
+                u16* at = out + ((c >> 5) << 6) + (c & 31);
+                *reinterpret_cast<u16x4*>(at) = hi;
+                *reinterpret_cast<u16x4*>(at + 32) = lo;
+            } else {
+                *reinterpret_cast<u16x4*>(out + c) = hi;
+            }
+        }
+    }
+}
+
+// Work-groups go to the XCDs in turn; every XCD gets one run of the tiles in
+// order, so that the tiles that share rows share an L2.
+__device__ __forceinline__ int xcd_run(int b, int total) {
+    const int x = b & 7, q = total >> 3, r = total & 7;
+    return x * q + min(x, r) + (b >> 3);
+}
+
+template <int S, int BM, int WM, int WN, tile::Kind KI, tile::Kind KJ>
+using CeTile = tile::Tile<S == 1, S, BM, BM, WM, WN, KI, KJ>;
+
+__device__ __forceinline__ Operand h_rows(const CePlan& p, const CeBuffers& b) {
+    return Operand{reinterpret_cast<const u16*>(b.workspace + p.h), p.ld_h, p.tokens,
+                   static_cast<int32_t>(p.ld_h)};
+}
+__device__ __forceinline__ Operand w_rows(const CePlan& p, const CeBuffers& b, int first) {
+    const u16* w = b.w_direct ? static_cast<const u16*>(b.w) : reinterpret_cast<const u16*>(b.workspace + p.w);
+    const int64_t ld = b.w_direct ? b.w_stride : p.ld_w;
+    return Operand{w + first * ld, ld, p.vocab - first, static_cast<int32_t>(p.ld_w)};
+}
+
+// What brings a tile's accumulators to logits.
+template <int S>
+__device__ __forceinline__ int logit_exponent(const CePlan& p, const CeBuffers& b) {
+    if constexpr (S == 1) return 0;
+    const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
+    return -(exponent_for(s->h_max) + exponent_for(s->w_max));
+}
+
+// First pass: each row's largest logit and sum of exp(z - largest) in a tile,
+// and the target's logit.
+template <int S, int BM, int WM, int WN>
+__global__ __launch_bounds__(WM* WN * 64) void k_stats(CePlan p, CeBuffers b) {
+    using T = CeTile<S, BM, WM, WN, kContig, kContig>;
+    __shared__ __align__(1024) char lds[T::kLdsBytes];
+    const int tiles_t = (p.tokens + BM - 1) / BM, tiles_v = (p.vocab + BM - 1) / BM;
+    const int id = xcd_run(blockIdx.x, tiles_t * tiles_v);
+    const int tv = id / tiles_t, tt = id - tv * tiles_t;
+    T t;
+    t.run(h_rows(p, b), w_rows(p, b, 0), tt * BM, tv * BM, 0, static_cast<int>(p.ld_h / S), (DSM_LDS char*)lds);
+    const int ex = logit_exponent<S>(p, b);
+    float* hit = reinterpret_cast<float*>(b.workspace + p.hit);
+    float2* part = reinterpret_cast<float2*>(lds);  // [WN][BM]
+#pragma unroll
+    for (int fi = 0; fi < T::FI; ++fi) {
+        const int token = tt * BM + t.row(fi);
+        const int64_t target = token < p.tokens ? b.target[token] : -1;
+        const int64_t rel = target - tv * BM;  // columns of the tile
+        float top = -__builtin_inff();
+#pragma unroll
+        for (int fj = 0; fj < T::FJ; ++fj)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int c = t.col(fj) + r;
+                float z = S == 1 ? t.acc[fi][fj][r] : ldexpf(t.acc[fi][fj][r], ex);
+                if (target >= 0 && rel == c && tv * BM + c < p.vocab) hit[token] = z;
+                if (tv * BM + c >= p.vocab) z = -__builtin_inff();
+                t.acc[fi][fj][r] = z;
+                top = fmaxf(top, z);
+            }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        float sum = 0.f;
+        if (top != -__builtin_inff()) {
+#pragma unroll
+            for (int fj = 0; fj < T::FJ; ++fj)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float d = t.acc[fi][fj][r] - top;
+                    sum += S == 1 ? __expf(d) : expf(d);
+                }
+        }
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if (t.lane < 16) part[t.wj * BM + t.row(fi)] = make_float2(top, sum);
+    }
+    __syncthreads();
+    float2* stats = reinterpret_cast<float2*>(b.workspace + p.stats) + static_cast<int64_t>(tv) * p.tokens;
+    for (int r = threadIdx.x; r < BM; r += T::kThreads) {
+        if (tt * BM + r >= p.tokens) break;
+        float2 a = part[r];
+#pragma unroll
+        for (int w = 1; w < WN; ++w) {
+            const float2 c = part[w * BM + r];
+            const float top = fmaxf(a.x, c.x);
+            const float sa = a.x == -__builtin_inff() ? a.y : a.y * expf(a.x - top);
+            const float sc = c.x == -__builtin_inff() ? c.y : c.y * expf(c.x - top);
+            a = make_float2(top, sa + sc);
+        }
+        stats[tt * BM + r] = a;
+    }
+}
+
+// lse and loss: a wave's lanes take the tiles of a token in turn.
+__global__ __launch_bounds__(256) void k_join(CePlan p, CeBuffers b, int tiles) {
+    const int token = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (token >= p.tokens) return;
+    const float2* stats = reinterpret_cast<const float2*>(b.workspace + p.stats);
+    float top = -__builtin_inff(), sum = 0.f;
+    for (int v = threadIdx.x & 63; v < tiles; v += 64) top = fmaxf(top, stats[static_cast<int64_t>(v) * p.tokens + token].x);
+    for (int w = 32; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
+    for (int v = threadIdx.x & 63; v < tiles; v += 64) {
+        const float2 s = stats[static_cast<int64_t>(v) * p.tokens + token];
+        sum += s.x == -__builtin_inff() ? s.y : s.y * expf(s.x - top);
+    }
+    for (int w = 32; w > 0; w >>= 1) sum += __shfl_xor(sum, w);
+    if ((threadIdx.x & 63) == 0) {
+        const float lse = top + logf(sum);
+        reinterpret_cast<float*>(b.workspace + p.lse)[token] = lse;
+        if (b.lse) b.lse[token] = lse;
+        float loss = 0.f;
+        if (is_valid(b.target[token], p.vocab))
+            loss = lse - reinterpret_cast<const float*>(b.workspace + p.hit)[token];
+        b.loss[token] = loss;
+    }
+}
+
+// The weighted total, in a fixed order.
+__global__ __launch_bounds__(1024) void k_total(CePlan p, CeBuffers b) {
+    __shared__ double s[1024];
+    const float* coef = reinterpret_cast<const float*>(b.workspace + p.coef);
+    double sum = 0.0;
+    for (int t = threadIdx.x; t < p.tokens; t += 1024)
+        if (is_valid(b.target[t], p.vocab)) sum += static_cast<double>(coef[t]) * b.loss[t];
+    s[threadIdx.x] = sum;
+    __syncthreads();
+    for (int w = 512; w > 0; w >>= 1) {
+        if (static_cast<int>(threadIdx.x) < w) s[threadIdx.x] += s[threadIdx.x + w];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) b.total[0] = static_cast<float>(s[0]);
+}
+
+// G of one piece of the vocabulary, [first, first + cols).
+template <int S, int BM, int WM, int WN>
+__global__ __launch_bounds__(WM* WN * 64) void k_piece(CePlan p, CeBuffers b, int first, int cols) {
+    using T = CeTile<S, BM, WM, WN, kContig, kContig>;
+    __shared__ __align__(1024) char lds[T::kLdsBytes];
+    const int rows_pad = (p.tokens + 63) / 64 * 64, cols_pad = (cols + 63) / 64 * 64;
+    const int tiles_t = (p.tokens + BM - 1) / BM, tiles_v = (cols + BM - 1) / BM;
+    const int id = xcd_run(blockIdx.x, tiles_t * tiles_v);
+    const int tv = id / tiles_t, tt = id - tv * tiles_t;
+    T t;
+    t.run(h_rows(p, b), w_rows(p, b, first), tt * BM, tv * BM, 0, static_cast<int>(p.ld_h / S), (DSM_LDS char*)lds);
+    const int ex = logit_exponent<S>(p, b);
+    const int eg = S == 1 ? 0 : exponent_for(reinterpret_cast<const Scalars*>(b.workspace + p.scalars)->c_max);
+    const float* lse = reinterpret_cast<const float*>(b.workspace + p.lse);
+    const float* coef = reinterpret_cast<const float*>(b.workspace + p.coef);
+    u16* g = reinterpret_cast<u16*>(b.workspace + p.p);
+#pragma unroll
+    for (int fi = 0; fi < T::FI; ++fi) {
+        const int token = tt * BM + t.row(fi);
+        if (token >= rows_pad) continue;
+        const bool in = token < p.tokens;
+        const int64_t target = in ? b.target[token] : -1;
+        const bool valid = is_valid(target, p.vocab);
+        const int64_t rel = valid ? target - first - tv * BM : -1;
+        const float l = in ? lse[token] : 0.f, c = in ? ldexpf(coef[token], eg) : 0.f;
+#pragma unroll
+        for (int fj = 0; fj < T::FJ; ++fj) {
+            const int col = t.col(fj);
+            if (tv * BM + col >= cols_pad) continue;
+            u16x4 hi, lo;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float z = S == 1 ? t.acc[fi][fj][r] : ldexpf(t.acc[fi][fj][r], ex);
+                float v = S == 1 ? __expf(z - l) : expf(z - l);
+                if (rel == col + r) v -= 1.0f;
+                v *= c;
+                if (!valid || tv * BM + col + r >= cols) v = 0.f;
+                if constexpr (S == 1) {
+                    hi[r] = float_to_bf16(v);
+                } else {
+                    hi[r] = float_to_half(v);
+                    lo[r] = float_to_half(v - half_to_float(hi[r]));
+                }
+            }
+            const int at = tv * BM + col;
+            u16* out = g + token * p.ld_p + (S == 1 ? at : ((at >> 5) << 6) + (at & 31));
+            *reinterpret_cast<u16x4*>(out) = hi;
+            if constexpr (S == 2) *reinterpret_cast<u16x4*>(out + 32) = lo;
+        }
+    }
+}
+
+// dh's sums over one piece, each of dh_splits parts into its own fp32 buffer.
+template <int S, int BM, int WM, int WN>
+__global__ __launch_bounds__(WM* WN * 64) void k_dh(CePlan p, CeBuffers b, int first, int cols) {
+    using T = CeTile<S, BM, WM, WN, kContig, kStrided>;
+    __shared__ __align__(1024) char lds[T::kLdsBytes];
+    const int tiles_t = (p.tokens + BM - 1) / BM, tiles_d = (p.dim + BM - 1) / BM;
+    int id = xcd_run(blockIdx.x, tiles_t * tiles_d * p.dh_splits);
+    const int part = id / (tiles_t * tiles_d);
+    id -= part * tiles_t * tiles_d;
+    const int tt = id / tiles_d, td = id - tt * tiles_d;
+    const int cols_pad = (cols + 63) / 64 * 64;
+    const int each = (cols_pad / 64 + p.dh_splits - 1) / p.dh_splits * 64;
+    const int k0 = min(part * each, cols_pad), k1 = min(k0 + each, cols_pad);
+    T t;
+    const Operand g{reinterpret_cast<const u16*>(b.workspace + p.p), p.ld_p, p.tokens, 0};
+    t.run(g, w_rows(p, b, first), tt * BM, td * BM, k0, k1, (DSM_LDS char*)lds);
+    float* out = reinterpret_cast<float*>(b.workspace + p.dh) + static_cast<int64_t>(part) * p.tokens * p.dim;
+#pragma unroll
+    for (int fi = 0; fi < T::FI; ++fi) {
+        const int token = tt * BM + t.row(fi);
+        if (token >= p.tokens) continue;
+#pragma unroll
+        for (int fj = 0; fj < T::FJ; ++fj)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int d = td * BM + t.col(fj) + r;
+                if (d >= p.dim) continue;
+                float* q = out + static_cast<int64_t>(token) * p.dim + d;
+                *q = first == 0 ? t.acc[fi][fj][r] : *q + t.acc[fi][fj][r];
+            }
+    }
+}
+
+template <int S>
+__device__ __forceinline__ void store_grad(void* base, int64_t at, float v) {
+    if constexpr (S == 1)
+        static_cast<u16*>(base)[at] = float_to_bf16(v);
+    else
+        static_cast<float*>(base)[at] = v;
+}
+
+template <int S>
+__global__ __launch_bounds__(256) void k_dh_join(CePlan p, CeBuffers b) {
+    int ex = 0;
+    if constexpr (S == 2) {
+        const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
+        ex = -(exponent_for(s->c_max) + exponent_for(s->w_max));
+    }
+    const int64_t total = static_cast<int64_t>(p.tokens) * p.dim;
+    const float* parts = reinterpret_cast<const float*>(b.workspace + p.dh);
+    for (int64_t e = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; e < total; e += static_cast<int64_t>(gridDim.x) * 256) {
+        float v = 0.f;
+        for (int s = 0; s < p.dh_splits; ++s) v += parts[s * total + e];
+        const int64_t r = e / p.dim;
+        store_grad<S>(b.dh, r * b.dh_stride + (e - r * p.dim), S == 1 ? v : ldexpf(v, ex));
+    }
+}
+
+// dw of one piece.
+template <int S, int BM, int WM, int WN>
+__global__ __launch_bounds__(WM* WN * 64) void k_dw(CePlan p, CeBuffers b, int first, int cols) {
+    using T = CeTile<S, BM, WM, WN, kStrided, kStrided>;
+    __shared__ __align__(1024) char lds[T::kLdsBytes];
+    const int tiles_v = (cols + BM - 1) / BM, tiles_d = (p.dim + BM - 1) / BM;
+    const int id = xcd_run(blockIdx.x, tiles_v * tiles_d);
+    const int tv = id / tiles_d, td = id - tv * tiles_d;
+    const int rows_pad = (p.tokens + 63) / 64 * 64;
+    T t;
+    const Operand g{reinterpret_cast<const u16*>(b.workspace + p.p), p.ld_p, rows_pad,
+                    static_cast<int32_t>(p.ld_p)};
+    t.run(g, h_rows(p, b), tv * BM, td * BM, 0, rows_pad, (DSM_LDS char*)lds);
+    int ex = 0;
+    if constexpr (S == 2) {
+        const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
+        ex = -(exponent_for(s->c_max) + exponent_for(s->h_max));
+    }
+#pragma unroll
+    for (int fi = 0; fi < T::FI; ++fi) {
+        const int v = tv * BM + t.row(fi);
+        if (v >= cols) continue;
+#pragma unroll
+        for (int fj = 0; fj < T::FJ; ++fj)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int d = td * BM + t.col(fj) + r;
+                if (d >= p.dim) continue;
+                const float x = t.acc[fi][fj][r];
+                store_grad<S>(b.dw, (first + v) * b.dw_stride + d, S == 1 ? x : ldexpf(x, ex));
+            }
+    }
+}
+
+template <int S, int BM, int WM, int WN>
+void products(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
+    constexpr int kThreads = WM * WN * 64;
+    const int tt = (p.tokens + BM - 1) / BM, tv = (p.vocab + BM - 1) / BM, td = (p.dim + BM - 1) / BM;
+    k_stats<S, BM, WM, WN><<<tt * tv, kThreads, 0, stream>>>(p, b);
+    k_join<<<(p.tokens + 3) / 4, 256, 0, stream>>>(p, b, tv);
+    k_total<<<1, 1024, 0, stream>>>(p, b);
+    if (!p.grads) return;
+    for (int first = 0; first < p.vocab; first += p.piece) {
+        const int cols = p.vocab - first < p.piece ? p.vocab - first : p.piece;
+        const int tp = (cols + BM - 1) / BM;
+        k_piece<S, BM, WM, WN><<<tt * tp, kThreads, 0, stream>>>(p, b, first, cols);
+        k_dh<S, BM, WM, WN><<<tt * td * p.dh_splits, kThreads, 0, stream>>>(p, b, first, cols);
+        k_dw<S, BM, WM, WN><<<tp * td, kThreads, 0, stream>>>(p, b, first, cols);
+    }
+    const int64_t total = static_cast<int64_t>(p.tokens) * p.dim;
+    k_dh_join<S><<<static_cast<unsigned>(total < 2048 * 256 ? (total + 255) / 256 : 2048), 256, 0, stream>>>(p, b);
+}
+
+}  // namespace
+
+hipError_t launch_linear_ce(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
+    k_coef<<<1, 1024, 0, stream>>>(p, b);
+    const int most = p.tokens > p.vocab ? p.tokens : p.vocab;
+    const unsigned rows = static_cast<unsigned>(most < 8192 ? (most + 3) / 4 : 2048);
+    if (p.split) {
+        k_largest<<<dim3(rows, 2), 256, 0, stream>>>(p, b);
+        k_operands<true><<<dim3(rows, 2), 256, 0, stream>>>(p, b);
+    } else {
+        k_operands<false><<<dim3(rows, b.w_direct ? 1 : 2), 256, 0, stream>>>(p, b);
+    }
+    if (p.tile == 256) {
+        if (p.split)
+            products<2, 256, 2, 4>(p, b, stream);
+        else
+            products<1, 256, 2, 4>(p, b, stream);
+    } else {
+        if (p.split)
+            products<2, 128, 2, 2>(p, b, stream);
+        else
+            products<1, 128, 2, 2>(p, b, stream);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace dsm

@@ -1,0 +1,85 @@
+// Shared by the host runtime (ops_runtime.cpp) and the kernels of the
+// language-model operators (ortho.hip, linear_ce.hip).
+#pragma once
+
+#include <hip/hip_runtime_api.h>
+#include <stdint.h>
+
+#include "dsm.h"
+
+namespace dsm {
+
+// ---- Orthogonalised updates (ortho.hip) ----
+
+constexpr int kOrthoGroup = 64;  // matrices that one set of launches takes
+
+struct OrthoOffsets {
+    int64_t at[kOrthoGroup];  // elements from the buffers' start to each matrix
+};
+
+// Power-of-two exponents of one iteration's stored operands: X * 2^x, A * 2^a,
+// B * 2^b, and X * 2^x_next after it.
+struct OrthoScales {
+    int x, a, b, x_next;
+};
+
+// One group of matrices, all of one shape.  The iteration works on the wide
+// orientation: m = min(rows, cols) rows of n = max columns.
+struct OrthoGroup {
+    int32_t count;
+    int32_t m, n;
+    int32_t tall;   // the matrix in memory is n x m
+    int32_t split;  // fp32 buffers, operands in two fp16 halves; else bf16 buffers, one fp16
+    int64_t row_stride;
+    OrthoOffsets off;
+    // Workspace (per matrix strides follow from m and n, see ortho.hip).
+    void* workspace;
+    // Buffers.  in: the update (orthogonalize) or the gradient (step).
+    const void* in;
+    void* out;    // orthogonalised update, or the scaled direction; NULL if x is updated
+    float* mom;   // momentum, updated; NULL without
+    float* x;     // parameters, updated; NULL if out is written
+    float mu, lr, scale, weight_decay, eps;
+    int32_t nesterov;
+};
+
+// Bytes of workspace that a group of `count` m x n matrices needs.
+int64_t ortho_group_bytes(int count, int m, int n, bool split);
+
+hipError_t launch_ortho(const OrthoGroup& g, const float* coeffs, const OrthoScales* scales, int steps,
+                        hipStream_t stream);
+
+// ---- Linear layer with softmax cross entropy (linear_ce.hip) ----
+
+// Where the parts of the workspace lie (bytes from its start), and how the
+// vocabulary is cut.
+struct CePlan {
+    int32_t tokens, dim, vocab;
+    int32_t split;       // fp32 buffers: operands in two fp16 halves; else bf16 as they are
+    int32_t grads;
+    int32_t tile;        // rows and columns of a work-group's tile
+    int32_t piece;       // columns of the vocabulary whose gradients are in memory at once
+    int32_t dh_splits;   // parts of a piece that dh is summed over side by side
+    int64_t scalars, coef, lse, hit, stats, h, w, p, dh, bytes;
+    int64_t ld_h, ld_w, ld_p;  // 16-bit elements of a row
+};
+
+struct CeBuffers {
+    const void* h;
+    const void* w;
+    const int64_t* target;
+    const float* weight;
+    float* total;
+    float* loss;
+    float* lse;
+    void* dh;
+    void* dw;
+    int64_t h_stride, w_stride, dh_stride, dw_stride;
+    char* workspace;
+    int32_t mean;
+    int32_t w_direct;  // bf16 w is read where it lies
+};
+
+hipError_t launch_linear_ce(const CePlan& plan, const CeBuffers& buf, hipStream_t stream);
+
+}  // namespace dsm

@@ -1,0 +1,347 @@
+// Host runtime of the language-model operators in include/dsm.h: argument
+// checks, workspace plans, the powers of two of the iteration's operands, and
+// launches.  The runtime owns no memory of any kind; nothing here throws.
+#include <algorithm>
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+
+#include "dsm.h"
+#include "dsm_internal.h"
+#include "ops_internal.h"
+
+namespace {
+
+constexpr int64_t kMaxTokens = int64_t(1) << 20, kMaxVocab = int64_t(1) << 20, kMaxDim = 1 << 16;
+constexpr int64_t kMaxSide = int64_t(1) << 20, kMaxShort = 1 << 14;
+constexpr int kMaxSteps = 32;
+
+dsm_status bad(dsm_status st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+dsm_status bad(dsm_status st, const char* fmt, ...) {
+    char msg[512];
+    va_list ap;
+    va_start(ap, fmt);
+    std::vsnprintf(msg, sizeof msg, fmt, ap);
+    va_end(ap);
+    return dsm::set_thread_error(st, msg);
+}
+
+dsm_status invalid(const char* what) { return bad(DSM_ERR_INVALID_ARG, "%s", what); }
+
+bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+dsm_status check_device() {
+    int n = 0;
+    if (hipGetDeviceCount(&n) != hipSuccess || n < 1) return bad(DSM_ERR_HIP, "no HIP device");
+    return DSM_OK;
+}
+
+dsm_status launched(const char* what, hipError_t e) {
+    if (e == hipSuccess) return DSM_OK;
+    return bad(DSM_ERR_HIP, "%s: %s (%d)", what, hipGetErrorString(e), static_cast<int>(e));
+}
+
+dsm_status check_workspace(const void* ws, int64_t bytes, int64_t need) {
+    if (!ws) return invalid("workspace is NULL");
+    if (!aligned(ws, 256)) return invalid("workspace is not 256-byte aligned");
+    if (bytes < need)
+        return bad(DSM_ERR_INVALID_ARG, "workspace_bytes %lld < %lld", static_cast<long long>(bytes),
+                   static_cast<long long>(need));
+    return DSM_OK;
+}
+
+// ---- Linear layer with softmax cross entropy ----
+
+// G of a piece takes at most this much memory.  A larger piece means fewer
+// launches and longer sums for dh.
+constexpr int64_t kPieceBytes = int64_t(256) << 20;
+
+dsm_status check_ce(const dsm_ce_problem* p) {
+    if (!p) return invalid("problem is NULL");
+    if (p->tokens < 0 || p->tokens > kMaxTokens) return invalid("tokens outside [0, 2^20]");
+    if (p->dim < 1 || p->dim > kMaxDim) return invalid("dim outside [1, 2^16]");
+    if (p->vocab < 1 || p->vocab > kMaxVocab) return invalid("vocab outside [1, 2^20]");
+    if (p->dtype != DSM_F32 && p->dtype != DSM_BF16) return bad(DSM_ERR_INVALID_ARG, "unknown dtype %d", p->dtype);
+    if (p->grads != 0 && p->grads != 1) return invalid("grads must be 0 or 1");
+    return DSM_OK;
+}
+
+dsm::CePlan make_plan(const dsm_ce_problem* p) {
+    dsm::CePlan q{};
+    q.tokens = static_cast<int32_t>(p->tokens);
+    q.dim = static_cast<int32_t>(p->dim);
+    q.vocab = static_cast<int32_t>(p->vocab);
+    q.split = p->dtype == DSM_F32;
+    q.grads = p->grads;
+    const int64_t T = p->tokens, V = p->vocab, width = q.split ? 2 : 1;
+    const int64_t tokens_pad = round_up(T, 64);
+    q.tile = T > 512 ? 256 : 128;
+    q.ld_h = q.ld_w = round_up(p->dim, 64) * width;
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const int64_t here = at;
+        at = round_up(at + bytes, 256);
+        return here;
+    };
+    q.scalars = take(64);
+    q.coef = take(T * 4);
+    q.lse = take(T * 4);
+    q.hit = take(T * 4);
+    q.stats = take((V + q.tile - 1) / q.tile * T * 8);
+    q.h = take(T * q.ld_h * 2);
+    q.w = take(V * q.ld_w * 2);
+    if (p->grads && T > 0) {
+        int64_t most = kPieceBytes / (tokens_pad * 2 * width) / q.tile * q.tile;
+        most = std::max<int64_t>(most, q.tile);
+        const int64_t pieces = (V + most - 1) / most;
+        q.piece = static_cast<int32_t>(round_up((V + pieces - 1) / pieces, q.tile));
+        q.ld_p = q.piece * width;
+        q.p = take(tokens_pad * q.ld_p * 2);
+        // As many parts as fill the 256 CUs: the share of them that the last
+        // turn leaves idle is what counts, and each part costs a pass over dh.
+        const int64_t tiles = ((T + q.tile - 1) / q.tile) * ((p->dim + q.tile - 1) / q.tile);
+        const int64_t per_cu = q.tile == 256 ? 1 : 2, slots = 256 * per_cu;
+        double best = 0.0;
+        for (int s = 1; s <= 16 && s * 64 * 4 <= q.piece; ++s) {
+            const int64_t n = tiles * s, turns = (n + slots - 1) / slots;
+            const double score = static_cast<double>(n) / static_cast<double>(turns * slots) - 0.01 * s;
+            if (q.dh_splits == 0 || score > best) {
+                best = score;
+                q.dh_splits = s;
+            }
+        }
+        if (q.dh_splits == 0) q.dh_splits = 1;
+        q.dh = take(static_cast<int64_t>(q.dh_splits) * T * p->dim * 4);
+    }
+    q.bytes = at;
+    return q;
+}
+
+// ---- Orthogonalised updates ----
+
+constexpr float kCoeffs[3] = {3.4445f, -4.7750f, 2.0315f};
+// The matrices that one set of launches takes have at most this much workspace
+// between them (one matrix may need more).
+constexpr int64_t kGroupBytes = int64_t(4) << 30;
+
+struct Iteration {
+    float coeffs[3 * kMaxSteps];
+    dsm::OrthoScales scales[kMaxSteps];
+};
+
+// The power of two that brings `bound` to at most 60000 (fp16 holds 65504).
+int exponent_under(double bound) {
+    int e = 0;
+    std::frexp(60000.0 / std::max(bound, 1e-6), &e);
+    return std::min(e - 1, 15);
+}
+
+// Bounds of |X|, |A| and |B| in each iteration from the singular values' range:
+// they start in [0, 1] (divided by the Frobenius norm), and go through
+// s -> |a s + b s^3 + c s^5|; A has s^2, B has b s^2 + c s^4.  1% covers rounding.
+dsm_status plan_iteration(const dsm_ortho_problem* p, Iteration* it) {
+    double r = 1.01;
+    for (int k = 0; k < p->steps; ++k) {
+        double f[3];
+        for (int j = 0; j < 3; ++j) {
+            const float v = p->coeffs ? p->coeffs[3 * k + j] : kCoeffs[j];
+            if (!std::isfinite(v)) return invalid("coeffs hold a number that is not finite");
+            it->coeffs[3 * k + j] = v;
+            f[j] = v;
+        }
+        const double a = f[0], b = f[1], c = f[2], l = r * r;
+        double top_b = std::fabs(b * l + c * l * l);
+        if (c != 0.0) {
+            const double z = -b / (2 * c);
+            if (z > 0 && z < l) top_b = std::max(top_b, std::fabs(b * z + c * z * z));
+        }
+        double next = std::fabs(a * r + b * r * l + c * r * l * l);
+        auto extremum = [&](double z) {  // of s -> a s + b s^3 + c s^5 at s^2 = z
+            if (z > 0 && z < l) next = std::max(next, std::fabs(std::sqrt(z) * (a + b * z + c * z * z)));
+        };
+        if (c != 0.0) {
+            const double disc = 9 * b * b - 20 * a * c;
+            if (disc >= 0) {
+                extremum((-3 * b + std::sqrt(disc)) / (10 * c));
+                extremum((-3 * b - std::sqrt(disc)) / (10 * c));
+            }
+        } else if (b != 0.0) {
+            extremum(-a / (3 * b));
+        }
+        next *= 1.01;
+        if (!(r <= 1024.0 && top_b <= 1048576.0 && next <= 1024.0))
+            return bad(DSM_ERR_UNSUPPORTED, "coeffs: the iterates of step %d grow beyond 2^10", k);
+        dsm::OrthoScales& s = it->scales[k];
+        s.x = exponent_under(r);
+        s.a = exponent_under(l);
+        s.b = exponent_under(top_b * 1.01);
+        if (k > 0) it->scales[k - 1].x_next = s.x;
+        s.x_next = 0;  // the last result as it is
+        r = next;
+    }
+    return DSM_OK;
+}
+
+dsm_status check_ortho(const dsm_ortho_problem* p, Iteration* it) {
+    if (!p) return invalid("problem is NULL");
+    if (p->rows < 0 || p->rows > kMaxSide || p->cols < 0 || p->cols > kMaxSide)
+        return invalid("rows or cols outside [0, 2^20]");
+    if (std::min(p->rows, p->cols) > kMaxShort) return invalid("the smaller of rows and cols exceeds 2^14");
+    if (p->row_stride < p->cols) return invalid("row_stride < cols");
+    if (p->count < 0) return invalid("count < 0");
+    if (p->dtype != DSM_F32 && p->dtype != DSM_BF16) return bad(DSM_ERR_INVALID_ARG, "unknown dtype %d", p->dtype);
+    if (p->steps < 1 || p->steps > kMaxSteps) return invalid("steps outside [1, 32]");
+    if (!std::isfinite(p->eps) || p->eps < 0) return invalid("eps must be finite and >= 0");
+    return plan_iteration(p, it);
+}
+
+bool is_empty(const dsm_ortho_problem* p) { return p->rows == 0 || p->cols == 0 || p->count == 0; }
+
+int group_size(const dsm_ortho_problem* p) {
+    const int m = static_cast<int>(std::min(p->rows, p->cols)), n = static_cast<int>(std::max(p->rows, p->cols));
+    const int64_t one = dsm::ortho_group_bytes(1, m, n, p->dtype == DSM_F32);
+    const int64_t fit = std::max<int64_t>(1, kGroupBytes / one);
+    return static_cast<int>(std::min<int64_t>(std::min<int64_t>(fit, p->count), dsm::kOrthoGroup));
+}
+
+int64_t ortho_bytes(const dsm_ortho_problem* p) {
+    if (is_empty(p)) return 0;
+    const int m = static_cast<int>(std::min(p->rows, p->cols)), n = static_cast<int>(std::max(p->rows, p->cols));
+    return dsm::ortho_group_bytes(group_size(p), m, n, p->dtype == DSM_F32);
+}
+
+dsm_status run_ortho(const dsm_ortho_problem* p, const dsm_ortho_buffers* b, const dsm_ortho_hparams* hp,
+                     const Iteration& it) {
+    if (!p->offsets) return invalid("offsets is NULL");
+    for (int i = 0; i < p->count; ++i)
+        if (p->offsets[i] < 0) return bad(DSM_ERR_INVALID_ARG, "offsets[%d] < 0", i);
+    if (dsm_status st = check_workspace(b->workspace, b->workspace_bytes, ortho_bytes(p))) return st;
+    if (dsm_status st = check_device()) return st;
+    const int group = group_size(p);
+    dsm::OrthoGroup g{};
+    g.m = static_cast<int32_t>(std::min(p->rows, p->cols));
+    g.n = static_cast<int32_t>(std::max(p->rows, p->cols));
+    g.tall = p->rows > p->cols;
+    g.split = p->dtype == DSM_F32;
+    g.row_stride = p->row_stride;
+    g.workspace = b->workspace;
+    g.in = b->in;
+    g.out = b->out;
+    g.eps = p->eps;
+    g.scale = 1.0f;
+    if (hp) {
+        g.mom = b->m;
+        g.x = b->x;
+        g.mu = hp->mu;
+        g.lr = hp->lr;
+        g.scale = hp->scale;
+        g.weight_decay = hp->weight_decay;
+        g.nesterov = hp->nesterov;
+    }
+    for (int first = 0; first < p->count; first += group) {
+        g.count = std::min(group, p->count - first);
+        for (int i = 0; i < g.count; ++i) g.off.at[i] = p->offsets[first + i];
+        const hipError_t e = dsm::launch_ortho(g, it.coeffs, it.scales, p->steps, static_cast<hipStream_t>(b->stream));
+        if (e != hipSuccess) return launched("launching the orthogonalisation", e);
+    }
+    return DSM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+dsm_status dsm_ce_workspace(const dsm_ce_problem* problem, int64_t* workspace_bytes) {
+    if (dsm_status st = check_ce(problem)) return st;
+    if (!workspace_bytes) return invalid("workspace_bytes is NULL");
+    *workspace_bytes = make_plan(problem).bytes;
+    return DSM_OK;
+}
+
+dsm_status dsm_linear_ce(const dsm_ce_problem* problem, const dsm_ce_buffers* buffers, int32_t mean) {
+    if (dsm_status st = check_ce(problem)) return st;
+    if (!buffers) return invalid("buffers is NULL");
+    const dsm_ce_problem& p = *problem;
+    const dsm_ce_buffers& b = *buffers;
+    const size_t elem = p.dtype == DSM_F32 ? 4 : 2;
+    if (!b.w || !b.total) return invalid("w or total is NULL");
+    if (p.tokens > 0 && (!b.h || !b.target || !b.loss)) return invalid("h, target or loss is NULL");
+    if (p.grads && (!b.dw || (p.tokens > 0 && !b.dh))) return invalid("dh or dw is NULL");
+    if (b.h_stride < p.dim || b.w_stride < p.dim) return invalid("h_stride or w_stride < dim");
+    if (p.grads && (b.dh_stride < p.dim || b.dw_stride < p.dim)) return invalid("dh_stride or dw_stride < dim");
+    if (!aligned(b.h, elem) || !aligned(b.w, elem) || !aligned(b.dh, elem) || !aligned(b.dw, elem))
+        return invalid("h, w, dh or dw is not aligned to its elements");
+    if (!aligned(b.target, 8) || !aligned(b.weight, 4) || !aligned(b.total, 4) || !aligned(b.loss, 4) ||
+        !aligned(b.lse, 4))
+        return invalid("target, weight, total, loss or lse is not aligned to its elements");
+    const dsm::CePlan plan = make_plan(problem);
+    if (dsm_status st = check_workspace(b.workspace, b.workspace_bytes, plan.bytes)) return st;
+    if (dsm_status st = check_device()) return st;
+    dsm::CeBuffers q{};
+    q.h = b.h;
+    q.w = b.w;
+    q.target = b.target;
+    q.weight = b.weight;
+    q.total = b.total;
+    q.loss = b.loss;
+    q.lse = b.lse;
+    q.dh = b.dh;
+    q.dw = b.dw;
+    q.h_stride = b.h_stride;
+    q.w_stride = b.w_stride;
+    q.dh_stride = b.dh_stride;
+    q.dw_stride = b.dw_stride;
+    q.workspace = static_cast<char*>(b.workspace);
+    q.mean = mean != 0;
+    // 16-byte loads of whole 64-column steps, with 32-bit offsets inside a tile.
+    q.w_direct = p.dtype == DSM_BF16 && p.dim % 64 == 0 && b.w_stride % 8 == 0 && aligned(b.w, 16) &&
+                 b.w_stride < (int64_t(1) << 22);
+    return launched("launching the cross entropy", dsm::launch_linear_ce(plan, q, static_cast<hipStream_t>(b.stream)));
+}
+
+dsm_status dsm_ortho_workspace(const dsm_ortho_problem* problem, int64_t* workspace_bytes) {
+    Iteration it;
+    if (dsm_status st = check_ortho(problem, &it)) return st;
+    if (!workspace_bytes) return invalid("workspace_bytes is NULL");
+    *workspace_bytes = ortho_bytes(problem);
+    return DSM_OK;
+}
+
+dsm_status dsm_orthogonalize(const dsm_ortho_problem* problem, const dsm_ortho_buffers* buffers) {
+    Iteration it;
+    if (dsm_status st = check_ortho(problem, &it)) return st;
+    if (!buffers) return invalid("buffers is NULL");
+    if (buffers->m || buffers->x) return invalid("m and x belong to dsm_ortho_step");
+    if (is_empty(problem)) return DSM_OK;
+    const size_t elem = problem->dtype == DSM_F32 ? 4 : 2;
+    if (!buffers->in || !buffers->out) return invalid("in or out is NULL");
+    if (!aligned(buffers->in, elem) || !aligned(buffers->out, elem))
+        return invalid("in or out is not aligned to its elements");
+    return run_ortho(problem, buffers, nullptr, it);
+}
+
+dsm_status dsm_ortho_step(const dsm_ortho_problem* problem, const dsm_ortho_buffers* buffers,
+                          const dsm_ortho_hparams* hp) {
+    Iteration it;
+    if (dsm_status st = check_ortho(problem, &it)) return st;
+    if (!buffers) return invalid("buffers is NULL");
+    if (!hp) return invalid("hparams is NULL");
+    if (problem->dtype != DSM_F32) return invalid("dsm_ortho_step takes fp32 buffers");
+    if (!std::isfinite(hp->mu) || hp->mu < 0 || hp->mu > 1) return invalid("mu outside [0, 1]");
+    if (!std::isfinite(hp->scale)) return invalid("scale is not finite");
+    if (is_empty(problem)) return DSM_OK;
+    if (!buffers->in) return invalid("in is NULL");
+    if ((buffers->x != nullptr) == (buffers->out != nullptr)) return invalid("exactly one of x and out is wanted");
+    if (buffers->x) {
+        if (!std::isfinite(hp->lr) || hp->lr <= 0) return invalid("lr must be finite and > 0");
+        if (!std::isfinite(hp->weight_decay) || hp->weight_decay < 0)
+            return invalid("weight_decay must be finite and >= 0");
+    }
+    if (!aligned(buffers->in, 4) || !aligned(buffers->out, 4) || !aligned(buffers->m, 4) || !aligned(buffers->x, 4))
+        return invalid("in, out, m or x is not aligned to its elements");
+    return run_ortho(problem, buffers, hp, it);
+}
+
+}  // extern "C"

@@ -1,0 +1,379 @@
+// Orthogonalised updates on gfx950: Newton-Schulz iteration on batches of
+// matrices, with the momentum before it and the parameter update after it.
+//
+//   X = U / (||U||_F + eps);  then for each step, with A = X X^T,
+//   B = b A + c A A,  X <- a X + B X
+//
+// on the wide orientation (m <= n), so A and B are m x m.  A step is three
+// matrix products, m^2 n + m^3 + 2 m^2 n operations with the symmetry of A and
+// of A A used: the two symmetric products compute the tiles on and below the
+// diagonal and store each tile below it a second time, transposed.
+//
+// Precision.  Products accumulate in fp32.  fp32 matrices go through the
+// products as two fp16 halves (gemm_tile.h: 22 bits, three matrix instructions),
+// which keeps the result as near to 64-bit arithmetic as fp32 products do.
+// bf16 matrices go through them as one fp16 (11 bits, against bf16's 8: the
+// iteration multiplies small singular values by up to 3.4445^5 = 485, and with
+// them what rounding X, A or B to 8 bits put there).  Two rules keep 11 bits
+// enough: A is rounded once and that same A enters b A and c A A, and the term
+// a X takes X from 22 bits (hi + lo), the products hi alone.  Against 64 bits
+// this gives 0.02-0.2% (a strong low rank over noise, and noise alone), below
+// the 0.17% that rounding the result to bf16 costs; all of it in bf16, 1-5%.
+//
+// Range.  ||X||_2 <= 1 at the start, and the polynomial bounds it after each
+// step, so the host picks for each stored operand the power of two that brings
+// its bound just under fp16's largest number; entries then keep their bits down
+// to 2^-40 of that bound.
+#include <hip/hip_runtime.h>
+
+#include "gemm_tile.h"
+#include "ops_internal.h"
+
+#pragma clang fp contract(off)
+
+namespace dsm {
+namespace {
+
+using tile::f4;
+using tile::kContig;
+using tile::kStrided;
+using tile::Operand;
+
+typedef unsigned short u16;
+typedef u16 u16x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kPad = 64;          // k of every operand is padded to this with zeros
+constexpr int kNormParts = 128;   // partial sums of squares of a matrix, at most
+constexpr int kPrepTile = 64;
+
+__host__ __device__ inline int pad(int v) { return (v + kPad - 1) / kPad * kPad; }
+__host__ __device__ inline int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
+
+// Workspace of one matrix: the partial sums, two X, A and B.  A split operand
+// keeps hi and lo interleaved in blocks of 32 columns (twice the columns); with
+// one half, X's lo lies apart, where only the epilogue reads it.
+struct Parts {
+    int64_t x[2], a, b, bytes;
+    int64_t lo;  // from an X to its lo half (one half only)
+    __host__ __device__ Parts(int m, int n, bool split) {
+        const int64_t xb = up256(static_cast<int64_t>(m) * pad(n) * 2) * 2;
+        const int64_t ab = up256(static_cast<int64_t>(m) * pad(m) * 2 * (split ? 2 : 1));
+        lo = xb / 2;
+        x[0] = up256(kNormParts * 8);
+        x[1] = x[0] + xb;
+        a = x[1] + xb;
+        b = a + ab;
+        bytes = b + ab;
+    }
+};
+
+__device__ __forceinline__ float from_bits(u16 v) {
+    return static_cast<float>(__builtin_bit_cast(_Float16, v));
+}
+__device__ __forceinline__ u16 to_bits(float v) {
+    return __builtin_bit_cast(u16, static_cast<_Float16>(v));
+}
+__device__ __forceinline__ float bf16_to_float(u16 v) {
+    return __builtin_bit_cast(float, static_cast<uint32_t>(v) << 16);
+}
+__device__ __forceinline__ u16 float_to_bf16(float v) {
+    return __builtin_bit_cast(u16, static_cast<__bf16>(v));
+}
+
+// Where element (i, j) of a stored operand lies; the lo half is 32 further.
+template <int S>
+__device__ __forceinline__ int64_t at(int64_t i, int j, int64_t ld) {
+    return S == 1 ? i * ld + j : i * ld + ((j >> 5) << 6) + (j & 31);
+}
+
+// The update u = g + mu m, m, or the matrix itself at element e; with `write`
+// the new momentum is stored, otherwise it has been.
+template <bool STEP, bool BF16>
+__device__ __forceinline__ float update_at(const OrthoGroup& g, int64_t e, bool write) {
+    if constexpr (STEP) {
+        const float grad = static_cast<const float*>(g.in)[e];
+        if (!g.mom) return grad;
+        float m = g.mom[e];
+        if (write) {
+            m = g.mu * m + grad;
+            g.mom[e] = m;
+        }
+        return g.nesterov ? grad + g.mu * m : m;
+    } else if constexpr (BF16) {
+        return bf16_to_float(static_cast<const u16*>(g.in)[e]);
+    } else {
+        return static_cast<const float*>(g.in)[e];
+    }
+}
+
+// Momentum and the partial sums of squares, in double so that no fp32 update
+// overflows or vanishes in its square; a fixed order, so reruns give the same bits.
+template <bool STEP, bool BF16>
+__global__ __launch_bounds__(256) void k_norm(OrthoGroup g, Parts parts, int n_parts) {
+    const int rows = g.tall ? g.n : g.m, cols = g.tall ? g.m : g.n;
+    const int64_t base = g.off.at[blockIdx.y];
+    const int64_t total = static_cast<int64_t>(rows) * cols;
+    double sum = 0.0;
+    const int64_t stride = static_cast<int64_t>(n_parts) * 256;
+    int64_t e = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    int64_t r = e / cols;
+    int64_t c = e - r * cols;
+    const int64_t dr = stride / cols, dc = stride - dr * cols;
+    for (; e < total; e += stride) {
+        const double v = update_at<STEP, BF16>(g, base + r * g.row_stride + c, true);
+        sum += v * v;
+        r += dr;
+        c += dc;
+        if (c >= cols) {
+            c -= cols;
+            ++r;
+        }
+    }
+    __shared__ double s[256];
+    s[threadIdx.x] = sum;
+    __syncthreads();
+    for (int w = 128; w > 0; w >>= 1) {
+        if (static_cast<int>(threadIdx.x) < w) s[threadIdx.x] += s[threadIdx.x + w];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0)
+        reinterpret_cast<double*>(static_cast<char*>(g.workspace) + blockIdx.y * parts.bytes)[blockIdx.x] = s[0];
+}
+
+// X_0 in the stored form, wide, its padding zero: 64 x 64 of it per work-group.
+template <int S, bool STEP, bool BF16>
+__global__ __launch_bounds__(256) void k_start(OrthoGroup g, Parts parts, int n_parts, int x_exp) {
+    __shared__ float t[kPrepTile][kPrepTile + 1];
+    __shared__ double s[kNormParts];
+    char* ws = static_cast<char*>(g.workspace) + blockIdx.z * parts.bytes;
+    const double* p = reinterpret_cast<const double*>(ws);
+    for (int q = threadIdx.x; q < kNormParts; q += 256) s[q] = q < n_parts ? p[q] : 0.0;
+    __syncthreads();
+    for (int w = kNormParts / 2; w > 0; w >>= 1) {
+        if (static_cast<int>(threadIdx.x) < w) s[threadIdx.x] += s[threadIdx.x + w];
+        __syncthreads();
+    }
+    const double inv = ldexp(1.0 / (sqrt(s[0]) + static_cast<double>(g.eps)), x_exp);
+    const int64_t base = g.off.at[blockIdx.z];
+    const int i0 = blockIdx.y * kPrepTile, j0 = blockIdx.x * kPrepTile;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int r = wave; r < kPrepTile; r += 4) {
+        // Rows of memory: i of the wide orientation, or j where the matrix is tall.
+        const int i = g.tall ? i0 + lane : i0 + r, j = g.tall ? j0 + r : j0 + lane;
+        float v = 0.f;
+        if (i < g.m && j < g.n) {
+            const int64_t e = base + (g.tall ? j * g.row_stride + i : i * g.row_stride + j);
+            v = static_cast<float>(update_at<STEP, BF16>(g, e, false) * inv);
+        }
+        if (g.tall)
+            t[lane][r] = v;
+        else
+            t[r][lane] = v;
+    }
+    __syncthreads();
+    const int np = pad(g.n);
+    u16* x = reinterpret_cast<u16*>(ws + parts.x[0]);
+    for (int r = wave; r < kPrepTile; r += 4) {
+        const int i = i0 + r, j = j0 + lane;
+        if (i >= g.m || j >= np) continue;
+        const float v = t[r][lane];
+        const u16 hi = to_bits(v);
+        const u16 lo = to_bits(v - from_bits(hi));
+        u16* q = x + at<S>(i, j, static_cast<int64_t>(np) * S);
+        q[0] = hi;
+        if constexpr (S == 2)
+            q[32] = lo;
+        else
+            q[parts.lo / 2] = lo;
+    }
+}
+
+enum Product { kGram, kPoly, kUpdate, kLast };
+
+// Work-groups go to the XCDs in turn; every XCD gets one run of the tiles in
+// order, so that the tiles that share rows share an L2.
+__device__ __forceinline__ int xcd_run(int b, int total) {
+    const int x = b & 7, q = total >> 3, r = total & 7;
+    return x * q + min(x, r) + (b >> 3);
+}
+
+template <int S, int BM, int WM, int WN, Product P>
+__global__ __launch_bounds__(WM* WN * 64) void k_product(OrthoGroup g, Parts parts, int from, float mul,
+                                                         float add, OrthoScales sc) {
+    using T = tile::Tile<false, S, BM, BM, WM, WN, kContig, P == kGram || P == kPoly ? kContig : kStrided>;
+    constexpr bool kSymmetric = P == kGram || P == kPoly;
+    __shared__ __align__(1024) char lds[T::kLdsBytes];
+    const int m = g.m, n = g.n, mp = pad(m), np = pad(n);
+    const int ti_n = (m + BM - 1) / BM, tj_n = ((kSymmetric ? m : n) + BM - 1) / BM;
+    const int each = kSymmetric ? ti_n * (ti_n + 1) / 2 : ti_n * tj_n;
+    const int id = xcd_run(blockIdx.x, each * g.count);
+    const int which = id / each;
+    int ti = 0, tj = id - which * each;
+    if (kSymmetric) {
+        while (tj > ti) tj -= ++ti;
+    } else {
+        // Down the columns of tiles: the next work-group takes the same columns of X.
+        ti = tj % ti_n;
+        tj /= ti_n;
+    }
+    char* ws = static_cast<char*>(g.workspace) + which * parts.bytes;
+    u16* X = reinterpret_cast<u16*>(ws + parts.x[from]);
+    u16* Y = reinterpret_cast<u16*>(ws + parts.x[from ^ 1]);
+    u16* A = reinterpret_cast<u16*>(ws + parts.a);
+    u16* B = reinterpret_cast<u16*>(ws + parts.b);
+    const int64_t ldx = static_cast<int64_t>(np) * S, lda = static_cast<int64_t>(mp) * S;
+    const Operand ox{X, ldx, m, np * S}, oa{A, lda, m, mp * S}, ob{B, lda, m, mp * S};
+    T t;
+    t.run(P == kGram ? ox : P == kPoly ? oa : ob, P == kPoly ? oa : ox, ti * BM, tj * BM, 0,
+          P == kGram ? np : mp, (DSM_LDS char*)lds);
+
+    // mul, add: powers of two and coefficients that bring the accumulator and
+    // the stored A or X to the stored result.
+#pragma unroll
+    for (int fi = 0; fi < T::FI; ++fi) {
+        const int i = ti * BM + t.row(fi);
+#pragma unroll
+        for (int fj = 0; fj < T::FJ; ++fj) {
+            const int j = tj * BM + t.col(fj);
+            f4 v = t.acc[fi][fj];
+            if constexpr (kSymmetric) {
+                if (i >= mp || j >= mp) continue;
+                const int64_t q = at<S>(i, j, lda);
+                u16* out = P == kGram ? A : B;
+                f4 old = {0.f, 0.f, 0.f, 0.f};
+                if (P == kPoly && i < m) {
+                    const u16x4 h = *reinterpret_cast<const u16x4*>(A + q);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) old[r] = from_bits(h[r]);
+                    if constexpr (S == 2) {
+                        const u16x4 l = *reinterpret_cast<const u16x4*>(A + q + 32);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) old[r] += from_bits(l[r]);
+                    }
+                }
+                u16x4 hi, lo;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    float w = v[r] * mul;
+                    if constexpr (P == kPoly) w = __builtin_fmaf(add, old[r], w);
+                    if (i >= m || j + r >= m) w = 0.f;  // the padding of k
+                    hi[r] = to_bits(w);
+                    lo[r] = to_bits(w - from_bits(hi[r]));
+                }
+                if (i < m) {
+                    *reinterpret_cast<u16x4*>(out + q) = hi;
+                    if constexpr (S == 2) *reinterpret_cast<u16x4*>(out + q + 32) = lo;
+                }
+                if (ti != tj) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        if (j + r >= m) continue;
+                        const int64_t w = at<S>(j + r, i, lda);
+                        out[w] = hi[r];
+                        if constexpr (S == 2) out[w + 32] = lo[r];
+                    }
+                }
+            } else {
+                if (i >= m || j >= np) continue;
+                const int64_t q = at<S>(i, j, ldx);
+                const u16x4 h = *reinterpret_cast<const u16x4*>(X + q);
+                const u16x4 l = *reinterpret_cast<const u16x4*>(X + q + (S == 2 ? 32 : parts.lo / 2));
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    v[r] = __builtin_fmaf(add, from_bits(h[r]) + from_bits(l[r]), v[r] * mul);
+                if constexpr (P == kUpdate) {
+                    u16x4 hi, lo;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        hi[r] = to_bits(v[r]);
+                        lo[r] = to_bits(v[r] - from_bits(hi[r]));
+                    }
+                    *reinterpret_cast<u16x4*>(Y + q) = hi;
+                    *reinterpret_cast<u16x4*>(Y + q + (S == 2 ? 32 : parts.lo / 2)) = lo;
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        if (j + r >= n) continue;
+                        const int64_t e = g.off.at[which] + (g.tall ? (j + r) * g.row_stride + i
+                                                                     : i * g.row_stride + j + r);
+                        if constexpr (S == 1) {
+                            static_cast<u16*>(g.out)[e] = float_to_bf16(v[r]);
+                        } else {
+                            const float d = g.scale * v[r];
+                            if (g.x) {
+                                const float x = g.x[e];
+                                g.x[e] = x - g.lr * (d + g.weight_decay * x);
+                            } else {
+                                static_cast<float*>(g.out)[e] = d;
+                            }
+                        }
+                    }
+                }
+            }
+        }
+    }
+}
+
+float pow2(int e) { return __builtin_ldexpf(1.0f, e); }
+
+template <int S, int BM, int WM, int WN>
+void iterate(const OrthoGroup& g, const Parts& parts, const float* coeffs, const OrthoScales* scales,
+             int steps, hipStream_t stream) {
+    const int ti = (g.m + BM - 1) / BM, tj = (g.n + BM - 1) / BM;
+    const unsigned sym = static_cast<unsigned>(ti * (ti + 1) / 2) * g.count;
+    const unsigned full = static_cast<unsigned>(ti) * tj * g.count;
+    constexpr int kThreads = WM * WN * 64;
+    for (int s = 0; s < steps; ++s) {
+        const OrthoScales sc = scales[s];
+        const float a = coeffs[3 * s], b = coeffs[3 * s + 1], c = coeffs[3 * s + 2];
+        k_product<S, BM, WM, WN, kGram><<<sym, kThreads, 0, stream>>>(g, parts, s & 1, pow2(sc.a - 2 * sc.x), 0.f, sc);
+        k_product<S, BM, WM, WN, kPoly><<<sym, kThreads, 0, stream>>>(
+            g, parts, s & 1, c * pow2(sc.b - 2 * sc.a), b * pow2(sc.b - sc.a), sc);
+        const float mul = pow2(sc.x_next - sc.b - sc.x), add = a * pow2(sc.x_next - sc.x);
+        if (s + 1 < steps)
+            k_product<S, BM, WM, WN, kUpdate><<<full, kThreads, 0, stream>>>(g, parts, s & 1, mul, add, sc);
+        else
+            k_product<S, BM, WM, WN, kLast><<<full, kThreads, 0, stream>>>(g, parts, s & 1, mul, add, sc);
+    }
+}
+
+template <int S, bool STEP, bool BF16>
+void start(const OrthoGroup& g, const Parts& parts, int x_exp, hipStream_t stream) {
+    const int64_t total = static_cast<int64_t>(g.m) * g.n;
+    const int n_parts = static_cast<int>(total < kNormParts * 1024 ? (total + 1023) / 1024 : kNormParts);
+    k_norm<STEP, BF16><<<dim3(n_parts, g.count), 256, 0, stream>>>(g, parts, n_parts);
+    const dim3 grid((pad(g.n) + kPrepTile - 1) / kPrepTile, (g.m + kPrepTile - 1) / kPrepTile, g.count);
+    k_start<S, STEP, BF16><<<grid, 256, 0, stream>>>(g, parts, n_parts, x_exp);
+}
+
+}  // namespace
+
+int64_t ortho_group_bytes(int count, int m, int n, bool split) {
+    return Parts(m, n, split).bytes * count;
+}
+
+hipError_t launch_ortho(const OrthoGroup& g, const float* coeffs, const OrthoScales* scales, int steps,
+                        hipStream_t stream) {
+    const Parts parts(g.m, g.n, g.split != 0);
+    if (!g.split)
+        start<1, false, true>(g, parts, scales[0].x, stream);
+    else if (g.mom || g.x)
+        start<2, true, false>(g, parts, scales[0].x, stream);
+    else
+        start<2, false, false>(g, parts, scales[0].x, stream);
+    const int64_t big = static_cast<int64_t>((g.m + 255) / 256) * ((g.n + 255) / 256) * g.count;
+    if (big >= 256) {
+        if (g.split)
+            iterate<2, 256, 2, 4>(g, parts, coeffs, scales, steps, stream);
+        else
+            iterate<1, 256, 2, 4>(g, parts, coeffs, scales, steps, stream);
+    } else {
+        if (g.split)
+            iterate<2, 128, 2, 2>(g, parts, coeffs, scales, steps, stream);
+        else
+            iterate<1, 128, 2, 2>(g, parts, coeffs, scales, steps, stream);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace dsm

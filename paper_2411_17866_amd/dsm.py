@@ -44,7 +44,10 @@ DSM_STREAM_READ, DSM_STREAM_WRITE = 0, 1
 EXPORTED = ("dsm_layout", "dsm_init", "dsm_init_static", "dsm_local_step", "dsm_global_step",
             "dsm_round_end", "dsm_sync",
             "dsm_read_bounds", "dsm_test_philox", "dsm_test_stream", "dsm_destroy",
-            "dsm_last_error")
+            "dsm_last_error", "dsm_ce_workspace", "dsm_linear_ce", "dsm_ortho_workspace",
+            "dsm_orthogonalize", "dsm_ortho_step")
+
+DSM_F32, DSM_BF16 = 0, 1
 
 
 class DsmError(RuntimeError):
@@ -81,6 +84,40 @@ class dsm_global_hparams(ctypes.Structure):
                 ("seed", ctypes.c_uint64), ("rule", ctypes.c_int32), ("eps", ctypes.c_float)]
 
 
+class dsm_ce_problem(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("dim", ctypes.c_int64), ("vocab", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("grads", ctypes.c_int32)]
+
+
+class dsm_ce_buffers(ctypes.Structure):
+    _fields_ = [("h", ctypes.c_void_p), ("h_stride", ctypes.c_int64),
+                ("w", ctypes.c_void_p), ("w_stride", ctypes.c_int64),
+                ("target", ctypes.c_void_p), ("weight", ctypes.c_void_p),
+                ("total", ctypes.c_void_p), ("loss", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+                ("dh", ctypes.c_void_p), ("dh_stride", ctypes.c_int64),
+                ("dw", ctypes.c_void_p), ("dw_stride", ctypes.c_int64),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64),
+                ("stream", ctypes.c_void_p)]
+
+
+class dsm_ortho_problem(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64), ("offsets", ctypes.POINTER(ctypes.c_int64)),
+                ("count", ctypes.c_int32), ("dtype", ctypes.c_int32), ("steps", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("coeffs", ctypes.POINTER(ctypes.c_float))]
+
+
+class dsm_ortho_buffers(ctypes.Structure):
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("x", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_int64), ("stream", ctypes.c_void_p)]
+
+
+class dsm_ortho_hparams(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_float), ("mu", ctypes.c_float), ("scale", ctypes.c_float),
+                ("weight_decay", ctypes.c_float), ("nesterov", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -114,6 +151,15 @@ def load_library(path=LIBPATH):
                                     ctypes.c_void_p]
     lib.dsm_test_stream.argtypes = [ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64,
                                     ctypes.c_void_p, ctypes.c_uint32, ctypes.c_void_p]
+    lib.dsm_ce_workspace.argtypes = [ctypes.POINTER(dsm_ce_problem), c_int64_p]
+    lib.dsm_linear_ce.argtypes = [ctypes.POINTER(dsm_ce_problem), ctypes.POINTER(dsm_ce_buffers),
+                                  ctypes.c_int32]
+    lib.dsm_ortho_workspace.argtypes = [ctypes.POINTER(dsm_ortho_problem), c_int64_p]
+    lib.dsm_orthogonalize.argtypes = [ctypes.POINTER(dsm_ortho_problem),
+                                      ctypes.POINTER(dsm_ortho_buffers)]
+    lib.dsm_ortho_step.argtypes = [ctypes.POINTER(dsm_ortho_problem),
+                                   ctypes.POINTER(dsm_ortho_buffers),
+                                   ctypes.POINTER(dsm_ortho_hparams)]
     lib.dsm_destroy.argtypes = [ctypes.c_void_p]
     lib.dsm_last_error.argtypes = [ctypes.c_void_p]
     lib.dsm_last_error.restype = ctypes.c_char_p
@@ -222,3 +268,50 @@ def dsm_test_stream(kind, dev_buf_ptr, n_elems, dev_words_ptr=None, pattern=0, s
 
 def dsm_destroy(ctx):
     _check(load_library().dsm_destroy(ctx))
+
+
+def dsm_ce_workspace(problem):
+    """Workspace of a dsm_ce_problem in bytes."""
+    ws = ctypes.c_int64()
+    _check(load_library().dsm_ce_workspace(ctypes.byref(problem), ctypes.byref(ws)))
+    return ws.value
+
+
+def dsm_linear_ce(problem, buffers, mean=True):
+    _check(load_library().dsm_linear_ce(ctypes.byref(problem), ctypes.byref(buffers),
+                                        1 if mean else 0))
+
+
+def make_ortho_problem(rows, cols, offsets, dtype=DSM_F32, row_stride=None, steps=5, eps=1e-7,
+                       coeffs=None):
+    """A dsm_ortho_problem plus the host arrays it points to (kept alive with it)."""
+    offs = np.ascontiguousarray(np.asarray(offsets, dtype=np.int64))
+    prob = dsm_ortho_problem(rows, cols, cols if row_stride is None else row_stride,
+                             offs.ctypes.data_as(ctypes.POINTER(ctypes.c_int64)), len(offs), dtype,
+                             steps, eps, None)
+    keep = [offs]
+    if coeffs is not None:
+        c = np.ascontiguousarray(np.asarray(coeffs, dtype=np.float32))
+        if c.shape != (steps, 3):
+            raise ValueError(f"coeffs must have the shape ({steps}, 3), got {c.shape}")
+        keep.append(c)
+        prob.coeffs = c.ctypes.data_as(ctypes.POINTER(ctypes.c_float))
+    prob._keep = keep
+    return prob
+
+
+def dsm_ortho_workspace(problem):
+    """Workspace of a dsm_ortho_problem in bytes."""
+    ws = ctypes.c_int64()
+    _check(load_library().dsm_ortho_workspace(ctypes.byref(problem), ctypes.byref(ws)))
+    return ws.value
+
+
+def dsm_orthogonalize(problem, buffers):
+    _check(load_library().dsm_orthogonalize(ctypes.byref(problem), ctypes.byref(buffers)))
+
+
+def dsm_ortho_step(problem, buffers, lr, mu, scale=1.0, weight_decay=0.0, nesterov=True):
+    hp = dsm_ortho_hparams(lr, mu, scale, weight_decay, 1 if nesterov else 0)
+    _check(load_library().dsm_ortho_step(ctypes.byref(problem), ctypes.byref(buffers),
+                                         ctypes.byref(hp)))
