@@ -153,8 +153,9 @@ struct Side {
 };
 
 // BM x BN tile by WM x WN waves.
-template <bool BF16, int S, int BM, int BN, int WM, int WN, Kind KI, Kind KJ>
+template <bool BF16, int S, int BM, int BN, int WM, int WN_, Kind KI, Kind KJ>
 struct Tile {
+    static constexpr int WN = WN_;
     static constexpr int kWaves = WM * WN;
     static constexpr int kThreads = kWaves * 64;
     static constexpr int FI = BM / WM / 16, FJ = BN / WN / 16;  // fragments of a wave
@@ -256,6 +257,249 @@ struct Tile {
     __device__ __forceinline__ int row(int fi) const { return (wi * FI + fi) * 16 + (lane & 15); }
     __device__ __forceinline__ int col(int fj) const { return (wj * FJ + fj) * 16 + (lane >> 4) * 4; }
 };
+
+// One side of a big tile (BigTile below): two half tiles of 128 rows (or
+// columns), each a buffer of its own in LDS.  Half h holds, of every wave's
+// 2 * HW rows, the HW from h * HW on.
+template <int HW, Kind KIND, int S>
+struct HalfSide {
+    static constexpr int kRows = 128;
+    static constexpr int kBytes = kRows * 128;
+    static constexpr int kWaves = 8;
+    static constexpr int kLoads = kBytes / 1024 / kWaves;
+    static constexpr int kSteps = S == 1 ? 64 : 32;
+    static constexpr int kRowBytes = kRows * 2 * S;  // k-strided: one k row
+
+    const char* base;
+    int64_t ld_bytes;
+    uint32_t off[2][kLoads];
+    int32_t k_rows, last_col;
+
+    static __device__ __forceinline__ int swz(int k) { return (k & 3) | ((k >> 1) & 4); }
+    // Row (or column) of the tile that row r of half h is.
+    static __device__ __forceinline__ int source(int r, int h) { return r / HW * (2 * HW) + h * HW + r % HW; }
+
+    __device__ __forceinline__ void init(const Operand& o, int64_t first, int lane, int wave) {
+        ld_bytes = o.ld * 2;
+        if constexpr (KIND == kContig) {
+            base = reinterpret_cast<const char*>(o.p) + first * ld_bytes;
+            const int last = static_cast<int>(o.rows - 1 - first);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int q = 0; q < kLoads; ++q) {
+                    const int r = (q * kWaves + wave) * 8 + (lane >> 3);
+                    const int chunk = (lane & 7) ^ (r & 7);
+                    off[h][q] = static_cast<uint32_t>(min(source(r, h), last)) * static_cast<uint32_t>(ld_bytes) +
+                                chunk * 16;
+                }
+        } else {
+            base = reinterpret_cast<const char*>(o.p) + first * 2 * S;
+            k_rows = o.rows;
+            last_col = (o.cols - static_cast<int>(first) * S - 8) * 2;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int q = 0; q < kLoads; ++q) off[h][q] = strided_off(h, q, lane, wave, 1 << 30);
+        }
+    }
+    __device__ __forceinline__ uint32_t strided_off(int h, int q, int lane, int wave, int k_max) const {
+        const int byte = (q * kWaves + wave) * 1024 + lane * 16;
+        const int k = byte / kRowBytes;
+        const int slot = (byte % kRowBytes) >> 4;
+        const int at = (((slot >> 1) ^ swz(k)) << 1) | (slot & 1);  // 16-byte column of the half tile
+        // 16-byte columns come in runs of HW columns of the tile.
+        constexpr int kRun = HW * S / 8;
+        const int col = (at / kRun * (2 * kRun) + h * kRun + at % kRun) * 16;
+        return static_cast<uint32_t>(min(k, k_max)) * static_cast<uint32_t>(ld_bytes) + min(col, last_col);
+    }
+    // Starts this wave's loads of half h of the stage at step k0.
+    template <int H>
+    __device__ __forceinline__ void issue(int k0, DSM_LDS char* lds, int lane, int wave) {
+        const char* b;
+        if constexpr (KIND == kContig) {
+            b = base + static_cast<int64_t>(k0 / kSteps) * 128;
+        } else {
+            b = base + static_cast<int64_t>(min(k0, k_rows - 1)) * ld_bytes;
+            if (k0 + kSteps > k_rows) {  // rows past the end read the last one
+                const int last_k = max(k_rows - 1 - k0, 0);
+#pragma unroll
+                for (int q = 0; q < kLoads; ++q) off[H][q] = strided_off(H, q, lane, wave, last_k);
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q)
+            __builtin_amdgcn_global_load_lds(
+                reinterpret_cast<const DSM_GLOBAL uint32_t*>(reinterpret_cast<uintptr_t>(b + off[H][q])),
+                reinterpret_cast<DSM_LDS uint32_t*>(lds + (q * kWaves + wave) * 1024), 16, 0, 0);
+    }
+    static __device__ __forceinline__ short8v fragment(const DSM_LDS char* lds, int f, int part, int lane) {
+        return Side<kRows, kWaves, KIND, S>::fragment(lds, f, part, lane);
+    }
+};
+
+// A 256 x 256 tile by 8 waves (2 x 4, each 128 x 64), two waves on each SIMD.
+//
+// The two waves of a SIMD take turns: while one feeds the matrix core the other
+// reads fragments from LDS and starts global loads, then they change over at a
+// barrier (waves 4-7 run one turn behind).  A stage of k has two such turns, one
+// for each half of the wave's rows:
+//
+//   turn  reads       multiplies      starts the loads of
+//   0     I0 J0 J1    I0 (J0 J1)      I1 one stage on
+//   1     I1          I1 (J0 J1)      I0 J0 J1 two stages on
+//
+// A turn's reads are waited for before the barrier that ends it, so the next
+// turn's loads may overwrite what was read, by the waves that run behind too.
+// Each load has two turns or more to arrive: before the barrier a wave waits
+// until at most 8 of its loads are in flight, which is all but those that the
+// next turn's reads need.
+template <bool BF16, int S, Kind KI, Kind KJ>
+struct BigTile {
+    static constexpr int kBM = 256, kThreads = 512;
+    static constexpr int WN = 4, FI = 8, FJ = 4;
+    using SideI = HalfSide<64, KI, S>;
+    using SideJ = HalfSide<32, KJ, S>;
+    static constexpr int kSteps = SideI::kSteps;
+    static constexpr int kHalf = SideI::kBytes;
+    static constexpr int kStageBytes = 4 * kHalf;  // J0, I0, J1, I1
+    static constexpr int kLdsBytes = 2 * kStageBytes;
+
+    f4 acc[FI][FJ];
+    int lane, wave, wi, wj;
+    short8v fi[4][2], fj[4][2];
+
+    static __device__ __forceinline__ void fence() {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("" ::: "memory");
+    }
+    // Until this wave's reads are done and at most N of its loads are in flight.
+    template <int N>
+    static __device__ __forceinline__ void wait() {
+        fence();
+        __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));
+        fence();
+    }
+    static __device__ __forceinline__ void turn_over() {
+        fence();
+        __builtin_amdgcn_s_barrier();
+        fence();
+    }
+    __device__ __forceinline__ void read_i(const DSM_LDS char* half) {
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+#pragma unroll
+            for (int f = 0; f < 4; ++f) fi[f][part] = SideI::fragment(half, wi * 4 + f, part, lane);
+    }
+    template <int H>
+    __device__ __forceinline__ void read_j(const DSM_LDS char* half) {
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+#pragma unroll
+            for (int f = 0; f < 2; ++f) fj[H * 2 + f][part] = SideJ::fragment(half, wj * 2 + f, part, lane);
+    }
+    template <int H>
+    __device__ __forceinline__ void multiply() {
+        fence();
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int t = 0; t < (S == 1 ? 2 : 3); ++t) {
+            // S = 2: lo hi, hi lo, hi hi.
+            const int pi = S == 1 ? t : t == 1, pj = S == 1 ? t : t == 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[H * 4 + i][j] = mfma<BF16>(fj[j][pj], fi[i][pi], acc[H * 4 + i][j]);
+        }
+        __builtin_amdgcn_s_setprio(0);
+        fence();
+    }
+
+    __device__ __forceinline__ void run(const Operand& oi, const Operand& oj, int64_t i0, int64_t j0,
+                                        int k_begin, int k_end, DSM_LDS char* lds) {
+        lane = threadIdx.x & 63;
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        wi = wave / WN;
+        wj = wave % WN;
+#pragma unroll
+        for (int i = 0; i < FI; ++i)
+#pragma unroll
+            for (int j = 0; j < FJ; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+        if (k_begin >= k_end) return;
+        SideI si;
+        SideJ sj;
+        si.init(oi, i0, lane, wave);
+        sj.init(oj, j0, lane, wave);
+        load_front(si, sj, k_begin, lds);
+        si.template issue<1>(k_begin, lds + 3 * kHalf, lane, wave);
+        if (k_begin + kSteps < k_end) {
+            load_front(si, sj, k_begin + kSteps, lds + kStageBytes);
+            wait<8>();  // the front of the first stage is there
+        } else {
+            wait<0>();
+        }
+        turn_over();
+        if (wave >= 4) turn_over();
+        for (int k = k_begin;;) {
+            stage<0>(si, sj, k, k_end, lds);
+            if ((k += kSteps) >= k_end) break;
+            stage<1>(si, sj, k, k_end, lds);
+            if ((k += kSteps) >= k_end) break;
+        }
+        if (wave < 4) turn_over();
+        turn_over();  // every wave is done with LDS
+    }
+    __device__ __forceinline__ void load_front(SideI& si, SideJ& sj, int k, DSM_LDS char* st) {
+        sj.template issue<0>(k, st, lane, wave);
+        si.template issue<0>(k, st + kHalf, lane, wave);
+        sj.template issue<1>(k, st + 2 * kHalf, lane, wave);
+    }
+    // The stage at step k, in buffer B.
+    template <int B>
+    __device__ __forceinline__ void stage(SideI& si, SideJ& sj, int k, int k_end, DSM_LDS char* lds) {
+        DSM_LDS char* st = lds + B * kStageBytes;
+        const bool next = k + kSteps < k_end, more = k + 2 * kSteps < k_end;
+        read_j<0>(st);
+        read_i(st + kHalf);
+        read_j<1>(st + 2 * kHalf);
+        if (next) {
+            si.template issue<1>(k + kSteps, lds + (B ^ 1) * kStageBytes + 3 * kHalf, lane, wave);
+            wait<8>();
+        } else {
+            wait<0>();
+        }
+        turn_over();
+        multiply<0>();
+        turn_over();
+        read_i(st + 3 * kHalf);
+        if (more) {
+            load_front(si, sj, k + 2 * kSteps, st);
+            wait<8>();
+        } else {
+            wait<0>();
+        }
+        turn_over();
+        multiply<1>();
+        turn_over();
+    }
+
+    // i and j of acc[fi][fj][r] inside the tile.
+    __device__ __forceinline__ int row(int f) const { return wi * 128 + f * 16 + (lane & 15); }
+    __device__ __forceinline__ int col(int f) const { return wj * 64 + f * 16 + (lane >> 4) * 4; }
+};
+
+template <bool BF16, int S, int BM, Kind KI, Kind KJ>
+struct Picked {
+    static_assert(BM == 128, "tiles are 128 or 256 square");
+    using T = Tile<BF16, S, 128, 128, 2, 2, KI, KJ>;
+};
+template <bool BF16, int S, Kind KI, Kind KJ>
+struct Picked<BF16, S, 256, KI, KJ> {
+    using T = BigTile<BF16, S, KI, KJ>;
+};
+// The tile of BM x BM by BM * 2 threads.
+template <bool BF16, int S, int BM, Kind KI, Kind KJ>
+using Pick = typename Picked<BF16, S, BM, KI, KJ>::T;
 
 }  // namespace tile
 }  // namespace dsm

@@ -12,12 +12,14 @@
 // with gradients the matrix cores do 8 T V D operations where keeping all
 // logits would need 6.
 //
-// Types.  bf16: the products take bf16 as it is, G rounds to bf16 once (its
-// sums have thousands of terms whose rounding errors are independent; they stay
-// below what rounding the gradients to bf16 costs).  fp32: h, w and G go as two
-// fp16 halves each (gemm_tile.h), scaled by powers of two so that the largest
-// finite entry lies just under fp16's largest number.  Logits, softmax statistics, losses and
-// sums are fp32.
+// Types.  With gradients every operand is fp16, scaled by a power of two so that
+// its largest finite entry lies just under fp16's largest number.  A bf16 number
+// then keeps all its bits down to 2^-32 of the largest one, and G keeps 11 bits
+// where bf16 would leave it 8: a row of G is mostly its target's entry, whose
+// rounding no sum averages out, and in bf16 it alone would cost the gradients
+// what their own rounding to bf16 does.  fp32 buffers go as two fp16 halves each
+// (gemm_tile.h).  The losses alone of bf16 buffers take bf16 operands as they
+// are.  Logits, softmax statistics, losses and sums are fp32.
 //
 // A token whose target lies outside [0, vocab) has no loss and no gradient, and
 // what its row of h holds, NaN included, reaches no output but its own zeros.
@@ -50,6 +52,13 @@ __device__ __forceinline__ u16 float_to_half(float v) {
     return __builtin_bit_cast(u16, static_cast<_Float16>(v));
 }
 
+__device__ __forceinline__ float bf16_to_float(u16 v) {
+    return __builtin_bit_cast(float, static_cast<uint32_t>(v) << 16);
+}
+
+// What the products take: bf16 as it is, scaled fp16, or two halves of it.
+enum Form { kBf16, kHalf, kHalves };
+
 struct Scalars {
     uint32_t h_max, w_max;  // bits of the largest finite |h| and |w| (fp32 buffers)
     uint32_t c_max;         // bits of the largest finite |c_t|
@@ -61,7 +70,7 @@ __device__ __forceinline__ int exponent_for(uint32_t bits) {
     if (bits == 0) return 0;
     int e;
     frexpf(__builtin_bit_cast(float, bits), &e);
-    return min(15 - e, 120);
+    return min(15 - e, 100);
 }
 
 __device__ __forceinline__ bool is_valid(int64_t target, int vocab) { return target >= 0 && target < vocab; }
@@ -105,58 +114,95 @@ __global__ __launch_bounds__(1024) void k_coef(CePlan p, CeBuffers b) {
     }
 }
 
+template <bool F32>
+__device__ __forceinline__ f4 load4(const void* base, int64_t at, int have, bool vec) {
+    f4 v = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (F32) {
+        const float* p = static_cast<const float*>(base) + at;
+        if (vec) return *reinterpret_cast<const f4*>(p);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (q < have) v[q] = p[q];
+    } else {
+        const u16* p = static_cast<const u16*>(base) + at;
+        if (vec) {
+            const u16x4 b = *reinterpret_cast<const u16x4*>(p);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = bf16_to_float(b[q]);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (q < have) v[q] = bf16_to_float(p[q]);
+        }
+    }
+    return v;
+}
+
 // The largest finite magnitude of h's valid rows (blockIdx.y = 0) and of w (1).
+template <bool F32>
 __global__ __launch_bounds__(256) void k_largest(CePlan p, CeBuffers b) {
     const bool of_w = blockIdx.y != 0;
-    const float* src = static_cast<const float*>(of_w ? b.w : b.h);
+    const void* src = of_w ? b.w : b.h;
+    const bool vec = of_w ? b.w_vector : b.h_vector;
     const int64_t stride = of_w ? b.w_stride : b.h_stride;
     const int rows = of_w ? p.vocab : p.tokens;
     uint32_t top = 0;
     for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4) {
         if (!of_w && !is_valid(b.target[r], p.vocab)) continue;
-        const float* row = src + r * stride;
-        for (int c = threadIdx.x & 63; c < p.dim; c += 64) top = max(top, finite_bits(row[c]));
+#pragma unroll 4
+        for (int c = (threadIdx.x & 63) * 4; c < p.dim; c += 256) {
+            const f4 v = load4<F32>(src, r * stride + c, p.dim - c, vec);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) top = max(top, finite_bits(v[q]));
+        }
     }
     for (int w = 32; w > 0; w >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), w)));
-    Scalars* s = reinterpret_cast<Scalars*>(b.workspace + p.scalars);
-    if ((threadIdx.x & 63) == 0 && top) atomicMax(of_w ? &s->w_max : &s->h_max, top);
+    __shared__ uint32_t tops[4];
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+        Scalars* s = reinterpret_cast<Scalars*>(b.workspace + p.scalars);
+        if (top) atomicMax(of_w ? &s->w_max : &s->h_max, top);
+    }
 }
 
 // h (blockIdx.y = 0) and w (1) as the products take them: rows of a multiple of
 // 64 columns, zeros in the padding and in h's rows without a valid target.
-template <bool SPLIT>
+template <Form FORM>
 __global__ __launch_bounds__(256) void k_operands(CePlan p, CeBuffers b) {
     const bool of_w = blockIdx.y != 0;
     const int rows = of_w ? p.vocab : p.tokens;
+    const void* src = of_w ? b.w : b.h;
+    const bool vec = of_w ? b.w_vector : b.h_vector;
     const int64_t stride = of_w ? b.w_stride : b.h_stride;
     const int64_t ld = of_w ? p.ld_w : p.ld_h;
-    const int cols = static_cast<int>(SPLIT ? ld / 2 : ld);
+    const int cols = static_cast<int>(FORM == kHalves ? ld / 2 : ld);
     u16* dst = reinterpret_cast<u16*>(b.workspace + (of_w ? p.w : p.h));
-    int e = 0;
-    if constexpr (SPLIT) {
+    float scale = 1.f;
+    if constexpr (FORM != kBf16) {
         const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
-        e = exponent_for(of_w ? s->w_max : s->h_max);
+        scale = ldexpf(1.f, exponent_for(of_w ? s->w_max : s->h_max));
     }
     for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4) {
         const bool keep = of_w || is_valid(b.target[r], p.vocab);
         u16* out = dst + r * ld;
+#pragma unroll 4
         for (int c = (threadIdx.x & 63) * 4; c < cols; c += 256) {
+            f4 v = {0.f, 0.f, 0.f, 0.f};
+            if (keep && c < p.dim) v = load4<FORM == kHalves>(src, r * stride + c, p.dim - c, vec);
             u16x4 hi, lo;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                if constexpr (SPLIT) {
-                    float v = 0.f;
-                    if (keep && c + q < p.dim)
-                        v = ldexpf(static_cast<const float*>(of_w ? b.w : b.h)[r * stride + c + q], e);
-                    hi[q] = float_to_half(v);
-                    lo[q] = float_to_half(v - half_to_float(hi[q]));
+                if constexpr (FORM == kBf16) {
+                    hi[q] = float_to_bf16(v[q]);
                 } else {
-                    hi[q] = keep && c + q < p.dim
-                                ? static_cast<const u16*>(of_w ? b.w : b.h)[r * stride + c + q]
-                                : u16(0);
+                    const float x = v[q] * scale;
+                    hi[q] = float_to_half(x);
+                    lo[q] = float_to_half(x - half_to_float(hi[q]));
                 }
             }
-            if constexpr (SPLIT) {
+            if constexpr (FORM == kHalves) {
                 u16* at = out + ((c >> 5) << 6) + (c & 31);
                 *reinterpret_cast<u16x4*>(at) = hi;
                 *reinterpret_cast<u16x4*>(at + 32) = lo;
@@ -174,8 +220,8 @@ __device__ __forceinline__ int xcd_run(int b, int total) {
     return x * q + min(x, r) + (b >> 3);
 }
 
-template <int S, int BM, int WM, int WN, tile::Kind KI, tile::Kind KJ>
-using CeTile = tile::Tile<S == 1, S, BM, BM, WM, WN, KI, KJ>;
+template <Form FORM, int BM, tile::Kind KI, tile::Kind KJ>
+using CeTile = tile::Pick<FORM == kBf16, FORM == kHalves ? 2 : 1, BM, KI, KJ>;
 
 __device__ __forceinline__ Operand h_rows(const CePlan& p, const CeBuffers& b) {
     return Operand{reinterpret_cast<const u16*>(b.workspace + p.h), p.ld_h, p.tokens,
@@ -188,40 +234,45 @@ __device__ __forceinline__ Operand w_rows(const CePlan& p, const CeBuffers& b, i
 }
 
 // What brings a tile's accumulators to logits.
-template <int S>
+template <Form FORM>
 __device__ __forceinline__ int logit_exponent(const CePlan& p, const CeBuffers& b) {
-    if constexpr (S == 1) return 0;
+    if constexpr (FORM == kBf16) return 0;
     const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
     return -(exponent_for(s->h_max) + exponent_for(s->w_max));
 }
 
 // First pass: each row's largest logit and sum of exp(z - largest) in a tile,
 // and the target's logit.
-template <int S, int BM, int WM, int WN>
-__global__ __launch_bounds__(WM* WN * 64) void k_stats(CePlan p, CeBuffers b) {
-    using T = CeTile<S, BM, WM, WN, kContig, kContig>;
+template <Form FORM, int BM>
+__global__ __launch_bounds__(BM * 2) void k_stats(CePlan p, CeBuffers b) {
+    using T = CeTile<FORM, BM, kContig, kContig>;
     __shared__ __align__(1024) char lds[T::kLdsBytes];
     const int tiles_t = (p.tokens + BM - 1) / BM, tiles_v = (p.vocab + BM - 1) / BM;
     const int id = xcd_run(blockIdx.x, tiles_t * tiles_v);
     const int tv = id / tiles_t, tt = id - tv * tiles_t;
     T t;
-    t.run(h_rows(p, b), w_rows(p, b, 0), tt * BM, tv * BM, 0, static_cast<int>(p.ld_h / S), (DSM_LDS char*)lds);
-    const int ex = logit_exponent<S>(p, b);
+    t.run(h_rows(p, b), w_rows(p, b, 0), tt * BM, tv * BM, 0, static_cast<int>(p.ld_h / (FORM == kHalves ? 2 : 1)), (DSM_LDS char*)lds);
+    const int ex = logit_exponent<FORM>(p, b);
     float* hit = reinterpret_cast<float*>(b.workspace + p.hit);
-    float2* part = reinterpret_cast<float2*>(lds);  // [WN][BM]
+    float2* part = reinterpret_cast<float2*>(lds);  // [T::WN][BM]
+    int rel[T::FI];  // the target's column in the tile, or -1
 #pragma unroll
     for (int fi = 0; fi < T::FI; ++fi) {
         const int token = tt * BM + t.row(fi);
-        const int64_t target = token < p.tokens ? b.target[token] : -1;
-        const int64_t rel = target - tv * BM;  // columns of the tile
+        const int64_t target = b.target[min(token, p.tokens - 1)];
+        rel[fi] = token < p.tokens && is_valid(target, p.vocab) ? static_cast<int>(target) - tv * BM : -1;
+    }
+#pragma unroll
+    for (int fi = 0; fi < T::FI; ++fi) {
+        const int token = tt * BM + t.row(fi);
         float top = -__builtin_inff();
 #pragma unroll
         for (int fj = 0; fj < T::FJ; ++fj)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int c = t.col(fj) + r;
-                float z = S == 1 ? t.acc[fi][fj][r] : ldexpf(t.acc[fi][fj][r], ex);
-                if (target >= 0 && rel == c && tv * BM + c < p.vocab) hit[token] = z;
+                float z = FORM == kBf16 ? t.acc[fi][fj][r] : ldexpf(t.acc[fi][fj][r], ex);
+                if (rel[fi] == c) hit[token] = z;
                 if (tv * BM + c >= p.vocab) z = -__builtin_inff();
                 t.acc[fi][fj][r] = z;
                 top = fmaxf(top, z);
@@ -235,7 +286,7 @@ __global__ __launch_bounds__(WM* WN * 64) void k_stats(CePlan p, CeBuffers b) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const float d = t.acc[fi][fj][r] - top;
-                    sum += S == 1 ? __expf(d) : expf(d);
+                    sum += FORM == kHalves ? expf(d) : __expf(d);
                 }
         }
         sum += __shfl_xor(sum, 16);
@@ -248,7 +299,7 @@ __global__ __launch_bounds__(WM* WN * 64) void k_stats(CePlan p, CeBuffers b) {
         if (tt * BM + r >= p.tokens) break;
         float2 a = part[r];
 #pragma unroll
-        for (int w = 1; w < WN; ++w) {
+        for (int w = 1; w < T::WN; ++w) {
             const float2 c = part[w * BM + r];
             const float top = fmaxf(a.x, c.x);
             const float sa = a.x == -__builtin_inff() ? a.y : a.y * expf(a.x - top);
@@ -300,30 +351,38 @@ __global__ __launch_bounds__(1024) void k_total(CePlan p, CeBuffers b) {
 }
 
 // G of one piece of the vocabulary, [first, first + cols).
-template <int S, int BM, int WM, int WN>
-__global__ __launch_bounds__(WM* WN * 64) void k_piece(CePlan p, CeBuffers b, int first, int cols) {
-    using T = CeTile<S, BM, WM, WN, kContig, kContig>;
+template <Form FORM, int BM>
+__global__ __launch_bounds__(BM * 2) void k_piece(CePlan p, CeBuffers b, int first, int cols) {
+    using T = CeTile<FORM, BM, kContig, kContig>;
     __shared__ __align__(1024) char lds[T::kLdsBytes];
     const int rows_pad = (p.tokens + 63) / 64 * 64, cols_pad = (cols + 63) / 64 * 64;
     const int tiles_t = (p.tokens + BM - 1) / BM, tiles_v = (cols + BM - 1) / BM;
     const int id = xcd_run(blockIdx.x, tiles_t * tiles_v);
     const int tv = id / tiles_t, tt = id - tv * tiles_t;
     T t;
-    t.run(h_rows(p, b), w_rows(p, b, first), tt * BM, tv * BM, 0, static_cast<int>(p.ld_h / S), (DSM_LDS char*)lds);
-    const int ex = logit_exponent<S>(p, b);
-    const int eg = S == 1 ? 0 : exponent_for(reinterpret_cast<const Scalars*>(b.workspace + p.scalars)->c_max);
+    t.run(h_rows(p, b), w_rows(p, b, first), tt * BM, tv * BM, 0, static_cast<int>(p.ld_h / (FORM == kHalves ? 2 : 1)), (DSM_LDS char*)lds);
+    const int ex = logit_exponent<FORM>(p, b);
+    const int eg = exponent_for(reinterpret_cast<const Scalars*>(b.workspace + p.scalars)->c_max);
     const float* lse = reinterpret_cast<const float*>(b.workspace + p.lse);
     const float* coef = reinterpret_cast<const float*>(b.workspace + p.coef);
     u16* g = reinterpret_cast<u16*>(b.workspace + p.p);
+    // What the rows need, all loaded before the first store.
+    int rel[T::FI];
+    bool valid[T::FI];
+    float l[T::FI], c[T::FI];
+#pragma unroll
+    for (int fi = 0; fi < T::FI; ++fi) {
+        const int token = tt * BM + t.row(fi), at = min(token, p.tokens - 1);
+        const int64_t target = b.target[at];
+        valid[fi] = token < p.tokens && is_valid(target, p.vocab);
+        rel[fi] = valid[fi] ? static_cast<int>(target) - first - tv * BM : -1;
+        l[fi] = lse[at];
+        c[fi] = ldexpf(coef[at], eg);
+    }
 #pragma unroll
     for (int fi = 0; fi < T::FI; ++fi) {
         const int token = tt * BM + t.row(fi);
         if (token >= rows_pad) continue;
-        const bool in = token < p.tokens;
-        const int64_t target = in ? b.target[token] : -1;
-        const bool valid = is_valid(target, p.vocab);
-        const int64_t rel = valid ? target - first - tv * BM : -1;
-        const float l = in ? lse[token] : 0.f, c = in ? ldexpf(coef[token], eg) : 0.f;
 #pragma unroll
         for (int fj = 0; fj < T::FJ; ++fj) {
             const int col = t.col(fj);
@@ -331,30 +390,26 @@ __global__ __launch_bounds__(WM* WN * 64) void k_piece(CePlan p, CeBuffers b, in
             u16x4 hi, lo;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const float z = S == 1 ? t.acc[fi][fj][r] : ldexpf(t.acc[fi][fj][r], ex);
-                float v = S == 1 ? __expf(z - l) : expf(z - l);
-                if (rel == col + r) v -= 1.0f;
-                v *= c;
-                if (!valid || tv * BM + col + r >= cols) v = 0.f;
-                if constexpr (S == 1) {
-                    hi[r] = float_to_bf16(v);
-                } else {
-                    hi[r] = float_to_half(v);
-                    lo[r] = float_to_half(v - half_to_float(hi[r]));
-                }
+                const float z = ldexpf(t.acc[fi][fj][r], ex) - l[fi];
+                float v = FORM == kHalves ? expf(z) : __expf(z);
+                if (rel[fi] == col + r) v -= 1.0f;
+                v *= c[fi];
+                if (!valid[fi] || tv * BM + col + r >= cols) v = 0.f;
+                hi[r] = float_to_half(v);
+                lo[r] = float_to_half(v - half_to_float(hi[r]));
             }
             const int at = tv * BM + col;
-            u16* out = g + token * p.ld_p + (S == 1 ? at : ((at >> 5) << 6) + (at & 31));
+            u16* out = g + token * p.ld_p + (FORM == kHalves ? ((at >> 5) << 6) + (at & 31) : at);
             *reinterpret_cast<u16x4*>(out) = hi;
-            if constexpr (S == 2) *reinterpret_cast<u16x4*>(out + 32) = lo;
+            if constexpr (FORM == kHalves) *reinterpret_cast<u16x4*>(out + 32) = lo;
         }
     }
 }
 
 // dh's sums over one piece, each of dh_splits parts into its own fp32 buffer.
-template <int S, int BM, int WM, int WN>
-__global__ __launch_bounds__(WM* WN * 64) void k_dh(CePlan p, CeBuffers b, int first, int cols) {
-    using T = CeTile<S, BM, WM, WN, kContig, kStrided>;
+template <Form FORM, int BM>
+__global__ __launch_bounds__(BM * 2) void k_dh(CePlan p, CeBuffers b, int first, int cols) {
+    using T = CeTile<FORM, BM, kContig, kStrided>;
     __shared__ __align__(1024) char lds[T::kLdsBytes];
     const int tiles_t = (p.tokens + BM - 1) / BM, tiles_d = (p.dim + BM - 1) / BM;
     int id = xcd_run(blockIdx.x, tiles_t * tiles_d * p.dh_splits);
@@ -367,52 +422,82 @@ __global__ __launch_bounds__(WM* WN * 64) void k_dh(CePlan p, CeBuffers b, int f
     T t;
     const Operand g{reinterpret_cast<const u16*>(b.workspace + p.p), p.ld_p, p.tokens, 0};
     t.run(g, w_rows(p, b, first), tt * BM, td * BM, k0, k1, (DSM_LDS char*)lds);
-    float* out = reinterpret_cast<float*>(b.workspace + p.dh) + static_cast<int64_t>(part) * p.tokens * p.dim;
+    float* out = reinterpret_cast<float*>(b.workspace + p.dh) + part * p.tokens * p.ld_dh;
+    const int ld = static_cast<int>(p.ld_dh);
+    constexpr int kBatch = 4;
 #pragma unroll
-    for (int fi = 0; fi < T::FI; ++fi) {
-        const int token = tt * BM + t.row(fi);
-        if (token >= p.tokens) continue;
+    for (int f0 = 0; f0 < T::FI; f0 += kBatch) {
+        f4 old[kBatch][T::FJ];
 #pragma unroll
-        for (int fj = 0; fj < T::FJ; ++fj)
+        for (int fi = 0; fi < kBatch; ++fi)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int d = td * BM + t.col(fj) + r;
-                if (d >= p.dim) continue;
-                float* q = out + static_cast<int64_t>(token) * p.dim + d;
-                *q = first == 0 ? t.acc[fi][fj][r] : *q + t.acc[fi][fj][r];
+            for (int fj = 0; fj < T::FJ; ++fj) {
+                const int64_t q = static_cast<int64_t>(min(tt * BM + t.row(f0 + fi), p.tokens - 1)) * ld +
+                                  min(td * BM + t.col(fj), ld - 4);
+                old[fi][fj] = first == 0 ? f4{0.f, 0.f, 0.f, 0.f} : *reinterpret_cast<const f4*>(out + q);
             }
+#pragma unroll
+        for (int fi = 0; fi < kBatch; ++fi) {
+            const int token = tt * BM + t.row(f0 + fi);
+#pragma unroll
+            for (int fj = 0; fj < T::FJ; ++fj) {
+                const int d = td * BM + t.col(fj);
+                if (token < p.tokens && d < ld)
+                    *reinterpret_cast<f4*>(out + static_cast<int64_t>(token) * ld + d) = old[fi][fj] + t.acc[f0 + fi][fj];
+            }
+        }
     }
 }
 
-template <int S>
-__device__ __forceinline__ void store_grad(void* base, int64_t at, float v) {
-    if constexpr (S == 1)
-        static_cast<u16*>(base)[at] = float_to_bf16(v);
-    else
-        static_cast<float*>(base)[at] = v;
+// Four entries of a gradient, of which `have` exist.
+template <bool F32>
+__device__ __forceinline__ void store_grad(void* base, int64_t at, f4 v, int have, bool vec) {
+    if constexpr (F32) {
+        float* p = static_cast<float*>(base) + at;
+        if (vec && have >= 4) {
+            *reinterpret_cast<f4*>(p) = v;
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (r < have) p[r] = v[r];
+        }
+    } else {
+        u16* p = static_cast<u16*>(base) + at;
+        u16x4 w;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) w[r] = float_to_bf16(v[r]);
+        if (vec && have >= 4) {
+            *reinterpret_cast<u16x4*>(p) = w;
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (r < have) p[r] = w[r];
+        }
+    }
 }
 
-template <int S>
+// dh from its parts, which are added in order; a wave takes a row.
+template <bool F32>
 __global__ __launch_bounds__(256) void k_dh_join(CePlan p, CeBuffers b) {
-    int ex = 0;
-    if constexpr (S == 2) {
-        const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
-        ex = -(exponent_for(s->c_max) + exponent_for(s->w_max));
-    }
-    const int64_t total = static_cast<int64_t>(p.tokens) * p.dim;
-    const float* parts = reinterpret_cast<const float*>(b.workspace + p.dh);
-    for (int64_t e = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; e < total; e += static_cast<int64_t>(gridDim.x) * 256) {
-        float v = 0.f;
-        for (int s = 0; s < p.dh_splits; ++s) v += parts[s * total + e];
-        const int64_t r = e / p.dim;
-        store_grad<S>(b.dh, r * b.dh_stride + (e - r * p.dim), S == 1 ? v : ldexpf(v, ex));
+    const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
+    const int ex = -(exponent_for(s->c_max) + exponent_for(s->w_max));
+    const int64_t each = p.tokens * p.ld_dh;
+    const int row = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= p.tokens) return;
+    const float* parts = reinterpret_cast<const float*>(b.workspace + p.dh) + row * p.ld_dh;
+    for (int d = (threadIdx.x & 63) * 4; d < p.dim; d += 256) {
+        f4 v = {0.f, 0.f, 0.f, 0.f};
+        for (int q = 0; q < p.dh_splits; ++q) v += *reinterpret_cast<const f4*>(parts + q * each + d);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = ldexpf(v[r], ex);
+        store_grad<F32>(b.dh, row * b.dh_stride + d, v, p.dim - d, b.dh_vector);
     }
 }
 
 // dw of one piece.
-template <int S, int BM, int WM, int WN>
-__global__ __launch_bounds__(WM* WN * 64) void k_dw(CePlan p, CeBuffers b, int first, int cols) {
-    using T = CeTile<S, BM, WM, WN, kStrided, kStrided>;
+template <Form FORM, int BM>
+__global__ __launch_bounds__(BM * 2) void k_dw(CePlan p, CeBuffers b, int first, int cols) {
+    using T = CeTile<FORM, BM, kStrided, kStrided>;
     __shared__ __align__(1024) char lds[T::kLdsBytes];
     const int tiles_v = (cols + BM - 1) / BM, tiles_d = (p.dim + BM - 1) / BM;
     const int id = xcd_run(blockIdx.x, tiles_v * tiles_d);
@@ -422,44 +507,56 @@ __global__ __launch_bounds__(WM* WN * 64) void k_dw(CePlan p, CeBuffers b, int f
     const Operand g{reinterpret_cast<const u16*>(b.workspace + p.p), p.ld_p, rows_pad,
                     static_cast<int32_t>(p.ld_p)};
     t.run(g, h_rows(p, b), tv * BM, td * BM, 0, rows_pad, (DSM_LDS char*)lds);
-    int ex = 0;
-    if constexpr (S == 2) {
-        const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
-        ex = -(exponent_for(s->c_max) + exponent_for(s->h_max));
-    }
+    const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
+    const int ex = -(exponent_for(s->c_max) + exponent_for(s->h_max));
 #pragma unroll
     for (int fi = 0; fi < T::FI; ++fi) {
         const int v = tv * BM + t.row(fi);
         if (v >= cols) continue;
 #pragma unroll
-        for (int fj = 0; fj < T::FJ; ++fj)
+        for (int fj = 0; fj < T::FJ; ++fj) {
+            const int d = td * BM + t.col(fj);
+            f4 x = t.acc[fi][fj];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int d = td * BM + t.col(fj) + r;
-                if (d >= p.dim) continue;
-                const float x = t.acc[fi][fj][r];
-                store_grad<S>(b.dw, (first + v) * b.dw_stride + d, S == 1 ? x : ldexpf(x, ex));
-            }
+            for (int r = 0; r < 4; ++r) x[r] = ldexpf(x[r], ex);
+            if (d < p.dim)
+                store_grad<FORM == kHalves>(b.dw, (first + v) * b.dw_stride + d, x, p.dim - d, b.dw_vector);
+        }
     }
 }
 
-template <int S, int BM, int WM, int WN>
-void products(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
-    constexpr int kThreads = WM * WN * 64;
-    const int tt = (p.tokens + BM - 1) / BM, tv = (p.vocab + BM - 1) / BM, td = (p.dim + BM - 1) / BM;
-    k_stats<S, BM, WM, WN><<<tt * tv, kThreads, 0, stream>>>(p, b);
+template <Form FORM, int BM>
+void losses(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
+    const int tt = (p.tokens + BM - 1) / BM, tv = (p.vocab + BM - 1) / BM;
+    k_stats<FORM, BM><<<tt * tv, BM * 2, 0, stream>>>(p, b);
     k_join<<<(p.tokens + 3) / 4, 256, 0, stream>>>(p, b, tv);
     k_total<<<1, 1024, 0, stream>>>(p, b);
-    if (!p.grads) return;
+}
+
+template <Form FORM, int BM>
+void gradients(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
+    const int tt = (p.tokens + BM - 1) / BM, td = (p.dim + BM - 1) / BM;
     for (int first = 0; first < p.vocab; first += p.piece) {
         const int cols = p.vocab - first < p.piece ? p.vocab - first : p.piece;
         const int tp = (cols + BM - 1) / BM;
-        k_piece<S, BM, WM, WN><<<tt * tp, kThreads, 0, stream>>>(p, b, first, cols);
-        k_dh<S, BM, WM, WN><<<tt * td * p.dh_splits, kThreads, 0, stream>>>(p, b, first, cols);
-        k_dw<S, BM, WM, WN><<<tp * td, kThreads, 0, stream>>>(p, b, first, cols);
+        k_piece<FORM, BM><<<tt * tp, BM * 2, 0, stream>>>(p, b, first, cols);
+        k_dh<FORM, BM><<<tt * td * p.dh_splits, BM * 2, 0, stream>>>(p, b, first, cols);
+        k_dw<FORM, BM><<<tp * td, BM * 2, 0, stream>>>(p, b, first, cols);
     }
-    const int64_t total = static_cast<int64_t>(p.tokens) * p.dim;
-    k_dh_join<S><<<static_cast<unsigned>(total < 2048 * 256 ? (total + 255) / 256 : 2048), 256, 0, stream>>>(p, b);
+    k_dh_join<FORM == kHalves><<<(p.tokens + 3) / 4, 256, 0, stream>>>(p, b);
+}
+
+template <int BM>
+void products(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
+    if (p.f32) {
+        losses<kHalves, BM>(p, b, stream);
+        if (p.grads) gradients<kHalves, BM>(p, b, stream);
+    } else if (p.grads) {
+        losses<kHalf, BM>(p, b, stream);
+        gradients<kHalf, BM>(p, b, stream);
+    } else {
+        losses<kBf16, BM>(p, b, stream);
+    }
 }
 
 }  // namespace
@@ -468,23 +565,19 @@ hipError_t launch_linear_ce(const CePlan& p, const CeBuffers& b, hipStream_t str
     k_coef<<<1, 1024, 0, stream>>>(p, b);
     const int most = p.tokens > p.vocab ? p.tokens : p.vocab;
     const unsigned rows = static_cast<unsigned>(most < 8192 ? (most + 3) / 4 : 2048);
-    if (p.split) {
-        k_largest<<<dim3(rows, 2), 256, 0, stream>>>(p, b);
-        k_operands<true><<<dim3(rows, 2), 256, 0, stream>>>(p, b);
+    if (p.f32) {
+        k_largest<true><<<dim3(rows, 2), 256, 0, stream>>>(p, b);
+        k_operands<kHalves><<<dim3(rows, 2), 256, 0, stream>>>(p, b);
+    } else if (p.grads) {
+        k_largest<false><<<dim3(rows, 2), 256, 0, stream>>>(p, b);
+        k_operands<kHalf><<<dim3(rows, 2), 256, 0, stream>>>(p, b);
     } else {
-        k_operands<false><<<dim3(rows, b.w_direct ? 1 : 2), 256, 0, stream>>>(p, b);
+        k_operands<kBf16><<<dim3(rows, b.w_direct ? 1 : 2), 256, 0, stream>>>(p, b);
     }
-    if (p.tile == 256) {
-        if (p.split)
-            products<2, 256, 2, 4>(p, b, stream);
-        else
-            products<1, 256, 2, 4>(p, b, stream);
-    } else {
-        if (p.split)
-            products<2, 128, 2, 2>(p, b, stream);
-        else
-            products<1, 128, 2, 2>(p, b, stream);
-    }
+    if (p.tile == 256)
+        products<256>(p, b, stream);
+    else
+        products<128>(p, b, stream);
     return hipGetLastError();
 }
 

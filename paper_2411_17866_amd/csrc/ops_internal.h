@@ -30,6 +30,8 @@ struct OrthoGroup {
     int32_t m, n;
     int32_t tall;   // the matrix in memory is n x m
     int32_t split;  // fp32 buffers, operands in two fp16 halves; else bf16 buffers, one fp16
+    int32_t vector;  // rows start where four elements can be moved at once (not for the
+                     // transposed stores of a tall matrix)
     int64_t row_stride;
     OrthoOffsets off;
     // Workspace (per matrix strides follow from m and n, see ortho.hip).
@@ -55,13 +57,14 @@ hipError_t launch_ortho(const OrthoGroup& g, const float* coeffs, const OrthoSca
 // vocabulary is cut.
 struct CePlan {
     int32_t tokens, dim, vocab;
-    int32_t split;       // fp32 buffers: operands in two fp16 halves; else bf16 as they are
+    int32_t f32;         // fp32 buffers, else bf16
     int32_t grads;
     int32_t tile;        // rows and columns of a work-group's tile
     int32_t piece;       // columns of the vocabulary whose gradients are in memory at once
     int32_t dh_splits;   // parts of a piece that dh is summed over side by side
     int64_t scalars, coef, lse, hit, stats, h, w, p, dh, bytes;
     int64_t ld_h, ld_w, ld_p;  // 16-bit elements of a row
+    int64_t ld_dh;             // floats of a row of dh's sums
 };
 
 struct CeBuffers {
@@ -78,6 +81,8 @@ struct CeBuffers {
     char* workspace;
     int32_t mean;
     int32_t w_direct;  // bf16 w is read where it lies
+    // Rows whose elements can be moved by four.
+    int32_t h_vector, w_vector, dh_vector, dw_vector;
 };
 
 hipError_t launch_linear_ce(const CePlan& plan, const CeBuffers& buf, hipStream_t stream);

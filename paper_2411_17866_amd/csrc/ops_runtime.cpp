@@ -73,9 +73,9 @@ dsm::CePlan make_plan(const dsm_ce_problem* p) {
     q.tokens = static_cast<int32_t>(p->tokens);
     q.dim = static_cast<int32_t>(p->dim);
     q.vocab = static_cast<int32_t>(p->vocab);
-    q.split = p->dtype == DSM_F32;
+    q.f32 = p->dtype == DSM_F32;
     q.grads = p->grads;
-    const int64_t T = p->tokens, V = p->vocab, width = q.split ? 2 : 1;
+    const int64_t T = p->tokens, V = p->vocab, width = q.f32 ? 2 : 1;
     const int64_t tokens_pad = round_up(T, 64);
     q.tile = T > 512 ? 256 : 128;
     q.ld_h = q.ld_w = round_up(p->dim, 64) * width;
@@ -113,7 +113,8 @@ dsm::CePlan make_plan(const dsm_ce_problem* p) {
             }
         }
         if (q.dh_splits == 0) q.dh_splits = 1;
-        q.dh = take(static_cast<int64_t>(q.dh_splits) * T * p->dim * 4);
+        q.ld_dh = round_up(p->dim, 4);
+        q.dh = take(q.dh_splits * T * q.ld_dh * 4);
     }
     q.bytes = at;
     return q;
@@ -240,6 +241,11 @@ dsm_status run_ortho(const dsm_ortho_problem* p, const dsm_ortho_buffers* b, con
         g.weight_decay = hp->weight_decay;
         g.nesterov = hp->nesterov;
     }
+    const size_t four = p->dtype == DSM_F32 ? 16 : 8;
+    bool vector = p->row_stride % 4 == 0 && aligned(g.in, four) && aligned(g.out, four) && aligned(g.mom, 16) &&
+                  aligned(g.x, 16);
+    for (int i = 0; i < p->count; ++i) vector = vector && p->offsets[i] % 4 == 0;
+    g.vector = vector;
     for (int first = 0; first < p->count; first += group) {
         g.count = std::min(group, p->count - first);
         for (int i = 0; i < g.count; ++i) g.off.at[i] = p->offsets[first + i];
@@ -296,8 +302,13 @@ dsm_status dsm_linear_ce(const dsm_ce_problem* problem, const dsm_ce_buffers* bu
     q.workspace = static_cast<char*>(b.workspace);
     q.mean = mean != 0;
     // 16-byte loads of whole 64-column steps, with 32-bit offsets inside a tile.
-    q.w_direct = p.dtype == DSM_BF16 && p.dim % 64 == 0 && b.w_stride % 8 == 0 && aligned(b.w, 16) &&
+    q.w_direct = p.dtype == DSM_BF16 && !p.grads && p.dim % 64 == 0 && b.w_stride % 8 == 0 && aligned(b.w, 16) &&
                  b.w_stride < (int64_t(1) << 22);
+    const size_t four = 4 * elem;
+    q.h_vector = p.dim % 4 == 0 && b.h_stride % 4 == 0 && aligned(b.h, four);
+    q.w_vector = p.dim % 4 == 0 && b.w_stride % 4 == 0 && aligned(b.w, four);
+    q.dh_vector = p.dim % 4 == 0 && b.dh_stride % 4 == 0 && aligned(b.dh, four);
+    q.dw_vector = p.dim % 4 == 0 && b.dw_stride % 4 == 0 && aligned(b.dw, four);
     return launched("launching the cross entropy", dsm::launch_linear_ce(plan, q, static_cast<hipStream_t>(b.stream)));
 }
 

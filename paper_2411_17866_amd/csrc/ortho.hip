@@ -43,7 +43,7 @@ typedef unsigned short u16;
 typedef u16 u16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kPad = 64;          // k of every operand is padded to this with zeros
-constexpr int kNormParts = 128;   // partial sums of squares of a matrix, at most
+constexpr int kNormParts = 256;   // partial sums of squares of a matrix, at most
 constexpr int kPrepTile = 64;
 
 __host__ __device__ inline int pad(int v) { return (v + kPad - 1) / kPad * kPad; }
@@ -86,48 +86,84 @@ __device__ __forceinline__ int64_t at(int64_t i, int j, int64_t ld) {
     return S == 1 ? i * ld + j : i * ld + ((j >> 5) << 6) + (j & 31);
 }
 
-// The update u = g + mu m, m, or the matrix itself at element e; with `write`
-// the new momentum is stored, otherwise it has been.
-template <bool STEP, bool BF16>
-__device__ __forceinline__ float update_at(const OrthoGroup& g, int64_t e, bool write) {
-    if constexpr (STEP) {
-        const float grad = static_cast<const float*>(g.in)[e];
-        if (!g.mom) return grad;
-        float m = g.mom[e];
-        if (write) {
-            m = g.mu * m + grad;
-            g.mom[e] = m;
+// The update u = g + mu m, m, or the matrix itself, at four elements from e on
+// (`have` of them exist); FIRST computes and stores the new momentum, which a
+// later call reads.
+template <bool STEP, bool BF16, bool FIRST>
+__device__ __forceinline__ f4 update_at(const OrthoGroup& g, int64_t e, int have) {
+    f4 v = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (BF16) {
+        const u16* in = static_cast<const u16*>(g.in) + e;
+        if (g.vector && have >= 4) {
+            const u16x4 b = *reinterpret_cast<const u16x4*>(in);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] = bf16_to_float(b[r]);
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (r < have) v[r] = bf16_to_float(in[r]);
         }
-        return g.nesterov ? grad + g.mu * m : m;
-    } else if constexpr (BF16) {
-        return bf16_to_float(static_cast<const u16*>(g.in)[e]);
-    } else {
-        return static_cast<const float*>(g.in)[e];
+        return v;
     }
+    const float* in = static_cast<const float*>(g.in) + e;
+    const bool vec = g.vector && have >= 4;
+    if (vec) {
+        v = *reinterpret_cast<const f4*>(in);
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (r < have) v[r] = in[r];
+    }
+    if constexpr (STEP) {
+        if (!g.mom) return v;
+        float* mom = g.mom + e;
+        f4 m = {0.f, 0.f, 0.f, 0.f};
+        if (vec) {
+            m = *reinterpret_cast<const f4*>(mom);
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (r < have) m[r] = mom[r];
+        }
+        if constexpr (FIRST) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) m[r] = g.mu * m[r] + v[r];
+            if (vec) {
+                *reinterpret_cast<f4*>(mom) = m;
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (r < have) mom[r] = m[r];
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = g.nesterov ? v[r] + g.mu * m[r] : m[r];
+    }
+    return v;
 }
 
 // Momentum and the partial sums of squares, in double so that no fp32 update
-// overflows or vanishes in its square; a fixed order, so reruns give the same bits.
+// overflows or vanishes in its square; a fixed order, so reruns give the same
+// bits.  A work-group takes every n_parts-th row of a matrix, or, where rows are
+// short, that run of them; four elements a lane.
 template <bool STEP, bool BF16>
 __global__ __launch_bounds__(256) void k_norm(OrthoGroup g, Parts parts, int n_parts) {
     const int rows = g.tall ? g.n : g.m, cols = g.tall ? g.m : g.n;
     const int64_t base = g.off.at[blockIdx.y];
-    const int64_t total = static_cast<int64_t>(rows) * cols;
+    const int quads = (cols + 3) / 4;
     double sum = 0.0;
-    const int64_t stride = static_cast<int64_t>(n_parts) * 256;
-    int64_t e = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    int64_t r = e / cols;
-    int64_t c = e - r * cols;
-    const int64_t dr = stride / cols, dc = stride - dr * cols;
-    for (; e < total; e += stride) {
-        const double v = update_at<STEP, BF16>(g, base + r * g.row_stride + c, true);
-        sum += v * v;
-        r += dr;
-        c += dc;
-        if (c >= cols) {
-            c -= cols;
-            ++r;
-        }
+    // Lanes over (row, quad) pairs: lanes of a row side by side, rows to fill 256.
+    const int per_row = quads < 256 ? quads : 256;
+    const int rows_at_once = 256 / per_row;
+    const int mine = threadIdx.x / per_row, q0 = threadIdx.x - mine * per_row;
+    if (mine < rows_at_once) {
+        for (int r = blockIdx.x * rows_at_once + mine; r < rows; r += n_parts * rows_at_once)
+#pragma unroll 4
+            for (int q = q0; q < quads; q += per_row) {
+                const f4 v = update_at<STEP, BF16, true>(g, base + r * g.row_stride + q * 4, cols - q * 4);
+                sum += static_cast<double>(v[0]) * v[0] + static_cast<double>(v[1]) * v[1] +
+                       (static_cast<double>(v[2]) * v[2] + static_cast<double>(v[3]) * v[3]);
+            }
     }
     __shared__ double s[256];
     s[threadIdx.x] = sum;
@@ -144,47 +180,59 @@ __global__ __launch_bounds__(256) void k_norm(OrthoGroup g, Parts parts, int n_p
 template <int S, bool STEP, bool BF16>
 __global__ __launch_bounds__(256) void k_start(OrthoGroup g, Parts parts, int n_parts, int x_exp) {
     __shared__ float t[kPrepTile][kPrepTile + 1];
-    __shared__ double s[kNormParts];
+    __shared__ double s[256];
     char* ws = static_cast<char*>(g.workspace) + blockIdx.z * parts.bytes;
     const double* p = reinterpret_cast<const double*>(ws);
-    for (int q = threadIdx.x; q < kNormParts; q += 256) s[q] = q < n_parts ? p[q] : 0.0;
+    s[threadIdx.x] = static_cast<int>(threadIdx.x) < n_parts ? p[threadIdx.x] : 0.0;
+    // Rows of memory: i of the wide orientation, or j where the matrix is tall.
+    const int64_t base = g.off.at[blockIdx.z];
+    const int i0 = blockIdx.y * kPrepTile, j0 = blockIdx.x * kPrepTile;
+    const int r0 = g.tall ? j0 : i0, c0 = g.tall ? i0 : j0;
+    const int rows = g.tall ? g.n : g.m, cols = g.tall ? g.m : g.n;
+    const int c = threadIdx.x & 15;
+    f4 v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int r = r0 + k * 16 + (threadIdx.x >> 4);
+        const int have = r < rows ? cols - (c0 + c * 4) : 0;
+        v[k] = have > 0 ? update_at<STEP, BF16, false>(g, base + r * g.row_stride + c0 + c * 4, have)
+                        : f4{0.f, 0.f, 0.f, 0.f};
+    }
     __syncthreads();
-    for (int w = kNormParts / 2; w > 0; w >>= 1) {
+    for (int w = 128; w > 0; w >>= 1) {
         if (static_cast<int>(threadIdx.x) < w) s[threadIdx.x] += s[threadIdx.x + w];
         __syncthreads();
     }
     const double inv = ldexp(1.0 / (sqrt(s[0]) + static_cast<double>(g.eps)), x_exp);
-    const int64_t base = g.off.at[blockIdx.z];
-    const int i0 = blockIdx.y * kPrepTile, j0 = blockIdx.x * kPrepTile;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int r = wave; r < kPrepTile; r += 4) {
-        // Rows of memory: i of the wide orientation, or j where the matrix is tall.
-        const int i = g.tall ? i0 + lane : i0 + r, j = g.tall ? j0 + r : j0 + lane;
-        float v = 0.f;
-        if (i < g.m && j < g.n) {
-            const int64_t e = base + (g.tall ? j * g.row_stride + i : i * g.row_stride + j);
-            v = static_cast<float>(update_at<STEP, BF16>(g, e, false) * inv);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int r = k * 16 + (threadIdx.x >> 4);
+            const float x = static_cast<float>(v[k][q] * inv);
+            if (g.tall)
+                t[c * 4 + q][r] = x;
+            else
+                t[r][c * 4 + q] = x;
         }
-        if (g.tall)
-            t[lane][r] = v;
-        else
-            t[r][lane] = v;
-    }
     __syncthreads();
     const int np = pad(g.n);
     u16* x = reinterpret_cast<u16*>(ws + parts.x[0]);
-    for (int r = wave; r < kPrepTile; r += 4) {
-        const int i = i0 + r, j = j0 + lane;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int r = k * 16 + (threadIdx.x >> 4);
+        const int i = i0 + r, j = j0 + c * 4;
         if (i >= g.m || j >= np) continue;
-        const float v = t[r][lane];
-        const u16 hi = to_bits(v);
-        const u16 lo = to_bits(v - from_bits(hi));
-        u16* q = x + at<S>(i, j, static_cast<int64_t>(np) * S);
-        q[0] = hi;
-        if constexpr (S == 2)
-            q[32] = lo;
-        else
-            q[parts.lo / 2] = lo;
+        u16x4 hi, lo;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float w = t[r][c * 4 + q];
+            hi[q] = to_bits(w);
+            lo[q] = to_bits(w - from_bits(hi[q]));
+        }
+        u16* to = x + at<S>(i, j, static_cast<int64_t>(np) * S);
+        *reinterpret_cast<u16x4*>(to) = hi;
+        *reinterpret_cast<u16x4*>(to + (S == 2 ? 32 : parts.lo / 2)) = lo;
     }
 }
 
@@ -197,10 +245,22 @@ __device__ __forceinline__ int xcd_run(int b, int total) {
     return x * q + min(x, r) + (b >> 3);
 }
 
-template <int S, int BM, int WM, int WN, Product P>
-__global__ __launch_bounds__(WM* WN * 64) void k_product(OrthoGroup g, Parts parts, int from, float mul,
+// Four parameters of row i, columns j .. j + 3 of the wide orientation (0 outside).
+__device__ __forceinline__ f4 load_old(const OrthoGroup& g, int which, int i, int j) {
+    f4 v = {0.f, 0.f, 0.f, 0.f};
+    if (i >= g.m) return v;
+    const float* x = g.x + g.off.at[which] + (g.tall ? j * g.row_stride + i : i * g.row_stride + j);
+    if (g.vector && !g.tall && j + 3 < g.n) return *reinterpret_cast<const f4*>(x);
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+        if (j + r < g.n) v[r] = x[g.tall ? r * g.row_stride : r];
+    return v;
+}
+
+template <int S, int BM, Product P>
+__global__ __launch_bounds__(BM * 2) void k_product(OrthoGroup g, Parts parts, int from, float mul,
                                                          float add, OrthoScales sc) {
-    using T = tile::Tile<false, S, BM, BM, WM, WN, kContig, P == kGram || P == kPoly ? kContig : kStrided>;
+    using T = tile::Pick<false, S, BM, kContig, P == kGram || P == kPoly ? kContig : kStrided>;
     constexpr bool kSymmetric = P == kGram || P == kPoly;
     __shared__ __align__(1024) char lds[T::kLdsBytes];
     const int m = g.m, n = g.n, mp = pad(m), np = pad(n);
@@ -228,85 +288,120 @@ __global__ __launch_bounds__(WM* WN * 64) void k_product(OrthoGroup g, Parts par
           P == kGram ? np : mp, (DSM_LDS char*)lds);
 
     // mul, add: powers of two and coefficients that bring the accumulator and
-    // the stored A or X to the stored result.
+    // the stored A or X to the stored result.  What a batch of fragments needs of
+    // them is loaded before the batch's first store, which the compiler must
+    // assume to overlap it: one wait a batch, not one a fragment.
+    constexpr int kBatch = 4;
+    constexpr int kLo = S == 2 ? 32 : 0;
+    const int64_t lo_at = S == 2 ? 32 : parts.lo / 2;  // of an X
+    const u16* old = P == kPoly ? A : X;
+    const int64_t ld_old = P == kPoly ? lda : ldx;
+    const int last_col = (P == kPoly ? mp : np) - 4;
 #pragma unroll
-    for (int fi = 0; fi < T::FI; ++fi) {
-        const int i = ti * BM + t.row(fi);
+    for (int f0 = 0; f0 < T::FI; f0 += kBatch) {
+        u16x4 oh[kBatch][T::FJ], ol[kBatch][T::FJ];
+        if constexpr (P != kGram) {
 #pragma unroll
-        for (int fj = 0; fj < T::FJ; ++fj) {
-            const int j = tj * BM + t.col(fj);
-            f4 v = t.acc[fi][fj];
-            if constexpr (kSymmetric) {
-                if (i >= mp || j >= mp) continue;
-                const int64_t q = at<S>(i, j, lda);
-                u16* out = P == kGram ? A : B;
-                f4 old = {0.f, 0.f, 0.f, 0.f};
-                if (P == kPoly && i < m) {
-                    const u16x4 h = *reinterpret_cast<const u16x4*>(A + q);
+            for (int fi = 0; fi < kBatch; ++fi)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) old[r] = from_bits(h[r]);
-                    if constexpr (S == 2) {
-                        const u16x4 l = *reinterpret_cast<const u16x4*>(A + q + 32);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) old[r] += from_bits(l[r]);
-                    }
+                for (int fj = 0; fj < T::FJ; ++fj) {
+                    const int64_t q = at<S>(min(ti * BM + t.row(f0 + fi), m - 1),
+                                            min(tj * BM + t.col(fj), last_col), ld_old);
+                    oh[fi][fj] = *reinterpret_cast<const u16x4*>(old + q);
+                    if constexpr (P != kPoly || S == 2)
+                        ol[fi][fj] = *reinterpret_cast<const u16x4*>(old + q + (P == kPoly ? kLo : lo_at));
                 }
-                u16x4 hi, lo;
+        }
+        f4 ox_[kBatch][T::FJ];
+        if constexpr (P == kLast && S == 2) {
+            if (g.x) {
+#pragma unroll
+                for (int fi = 0; fi < kBatch; ++fi)
+#pragma unroll
+                    for (int fj = 0; fj < T::FJ; ++fj)
+                        ox_[fi][fj] = load_old(g, which, ti * BM + t.row(f0 + fi), tj * BM + t.col(fj));
+            }
+        }
+#pragma unroll
+        for (int fi = 0; fi < kBatch; ++fi) {
+            const int i = ti * BM + t.row(f0 + fi);
+#pragma unroll
+            for (int fj = 0; fj < T::FJ; ++fj) {
+                const int j = tj * BM + t.col(fj);
+                f4 v = t.acc[f0 + fi][fj];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    float w = v[r] * mul;
-                    if constexpr (P == kPoly) w = __builtin_fmaf(add, old[r], w);
-                    if (i >= m || j + r >= m) w = 0.f;  // the padding of k
-                    hi[r] = to_bits(w);
-                    lo[r] = to_bits(w - from_bits(hi[r]));
-                }
-                if (i < m) {
-                    *reinterpret_cast<u16x4*>(out + q) = hi;
-                    if constexpr (S == 2) *reinterpret_cast<u16x4*>(out + q + 32) = lo;
-                }
-                if (ti != tj) {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        if (j + r >= m) continue;
-                        const int64_t w = at<S>(j + r, i, lda);
-                        out[w] = hi[r];
-                        if constexpr (S == 2) out[w + 32] = lo[r];
+                    v[r] *= mul;
+                    if constexpr (P != kGram) {
+                        float o = from_bits(oh[fi][fj][r]);
+                        if constexpr (P != kPoly || S == 2) o += from_bits(ol[fi][fj][r]);
+                        v[r] = __builtin_fmaf(add, o, v[r]);
                     }
                 }
-            } else {
-                if (i >= m || j >= np) continue;
-                const int64_t q = at<S>(i, j, ldx);
-                const u16x4 h = *reinterpret_cast<const u16x4*>(X + q);
-                const u16x4 l = *reinterpret_cast<const u16x4*>(X + q + (S == 2 ? 32 : parts.lo / 2));
+                if constexpr (kSymmetric) {
+                    if (i >= mp || j >= mp) continue;
+                    u16* out = P == kGram ? A : B;
+                    u16x4 hi, lo;
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    v[r] = __builtin_fmaf(add, from_bits(h[r]) + from_bits(l[r]), v[r] * mul);
-                if constexpr (P == kUpdate) {
+                    for (int r = 0; r < 4; ++r) {
+                        const float w = i >= m || j + r >= m ? 0.f : v[r];  // the padding of k
+                        hi[r] = to_bits(w);
+                        lo[r] = to_bits(w - from_bits(hi[r]));
+                    }
+                    if (i < m) {
+                        const int64_t q = at<S>(i, j, lda);
+                        *reinterpret_cast<u16x4*>(out + q) = hi;
+                        if constexpr (S == 2) *reinterpret_cast<u16x4*>(out + q + 32) = lo;
+                    }
+                    if (ti != tj) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            if (j + r >= m) continue;
+                            const int64_t w = at<S>(j + r, i, lda);
+                            out[w] = hi[r];
+                            if constexpr (S == 2) out[w + 32] = lo[r];
+                        }
+                    }
+                } else if constexpr (P == kUpdate) {
+                    if (i >= m || j >= np) continue;
                     u16x4 hi, lo;
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         hi[r] = to_bits(v[r]);
                         lo[r] = to_bits(v[r] - from_bits(hi[r]));
                     }
+                    const int64_t q = at<S>(i, j, ldx);
                     *reinterpret_cast<u16x4*>(Y + q) = hi;
-                    *reinterpret_cast<u16x4*>(Y + q + (S == 2 ? 32 : parts.lo / 2)) = lo;
+                    *reinterpret_cast<u16x4*>(Y + q + lo_at) = lo;
                 } else {
+                    if (i >= m || j >= n) continue;
+                    const int64_t e = g.off.at[which] + (g.tall ? j * g.row_stride + i : i * g.row_stride + j);
+                    if constexpr (S == 2) {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        if (j + r >= n) continue;
-                        const int64_t e = g.off.at[which] + (g.tall ? (j + r) * g.row_stride + i
-                                                                     : i * g.row_stride + j + r);
-                        if constexpr (S == 1) {
-                            static_cast<u16*>(g.out)[e] = float_to_bf16(v[r]);
-                        } else {
-                            const float d = g.scale * v[r];
-                            if (g.x) {
-                                const float x = g.x[e];
-                                g.x[e] = x - g.lr * (d + g.weight_decay * x);
-                            } else {
-                                static_cast<float*>(g.out)[e] = d;
-                            }
+                        for (int r = 0; r < 4; ++r) {
+                            v[r] *= g.scale;
+                            if (g.x) v[r] = ox_[fi][fj][r] - g.lr * (v[r] + g.weight_decay * ox_[fi][fj][r]);
                         }
+                        float* out = g.x ? g.x : static_cast<float*>(g.out);
+                        if (g.vector && !g.tall && j + 3 < n) {
+                            *reinterpret_cast<f4*>(out + e) = v;
+                            continue;
+                        }
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (j + r < n) out[e + (g.tall ? r * g.row_stride : r)] = v[r];
+                    } else {
+                        u16* out = static_cast<u16*>(g.out);
+                        u16x4 b;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) b[r] = float_to_bf16(v[r]);
+                        if (g.vector && !g.tall && j + 3 < n) {
+                            *reinterpret_cast<u16x4*>(out + e) = b;
+                            continue;
+                        }
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (j + r < n) out[e + (g.tall ? r * g.row_stride : r)] = b[r];
                     }
                 }
             }
@@ -316,31 +411,32 @@ __global__ __launch_bounds__(WM* WN * 64) void k_product(OrthoGroup g, Parts par
 
 float pow2(int e) { return __builtin_ldexpf(1.0f, e); }
 
-template <int S, int BM, int WM, int WN>
+template <int S, int BM>
 void iterate(const OrthoGroup& g, const Parts& parts, const float* coeffs, const OrthoScales* scales,
              int steps, hipStream_t stream) {
     const int ti = (g.m + BM - 1) / BM, tj = (g.n + BM - 1) / BM;
     const unsigned sym = static_cast<unsigned>(ti * (ti + 1) / 2) * g.count;
     const unsigned full = static_cast<unsigned>(ti) * tj * g.count;
-    constexpr int kThreads = WM * WN * 64;
+    constexpr int kThreads = BM * 2;
     for (int s = 0; s < steps; ++s) {
         const OrthoScales sc = scales[s];
         const float a = coeffs[3 * s], b = coeffs[3 * s + 1], c = coeffs[3 * s + 2];
-        k_product<S, BM, WM, WN, kGram><<<sym, kThreads, 0, stream>>>(g, parts, s & 1, pow2(sc.a - 2 * sc.x), 0.f, sc);
-        k_product<S, BM, WM, WN, kPoly><<<sym, kThreads, 0, stream>>>(
+        k_product<S, BM, kGram><<<sym, kThreads, 0, stream>>>(g, parts, s & 1, pow2(sc.a - 2 * sc.x), 0.f, sc);
+        k_product<S, BM, kPoly><<<sym, kThreads, 0, stream>>>(
             g, parts, s & 1, c * pow2(sc.b - 2 * sc.a), b * pow2(sc.b - sc.a), sc);
         const float mul = pow2(sc.x_next - sc.b - sc.x), add = a * pow2(sc.x_next - sc.x);
         if (s + 1 < steps)
-            k_product<S, BM, WM, WN, kUpdate><<<full, kThreads, 0, stream>>>(g, parts, s & 1, mul, add, sc);
+            k_product<S, BM, kUpdate><<<full, kThreads, 0, stream>>>(g, parts, s & 1, mul, add, sc);
         else
-            k_product<S, BM, WM, WN, kLast><<<full, kThreads, 0, stream>>>(g, parts, s & 1, mul, add, sc);
+            k_product<S, BM, kLast><<<full, kThreads, 0, stream>>>(g, parts, s & 1, mul, add, sc);
     }
 }
 
 template <int S, bool STEP, bool BF16>
 void start(const OrthoGroup& g, const Parts& parts, int x_exp, hipStream_t stream) {
+    // Some 4096 elements a work-group, and enough of them for all CUs.
     const int64_t total = static_cast<int64_t>(g.m) * g.n;
-    const int n_parts = static_cast<int>(total < kNormParts * 1024 ? (total + 1023) / 1024 : kNormParts);
+    const int n_parts = static_cast<int>(total < kNormParts * 4096 ? (total + 4095) / 4096 : kNormParts);
     k_norm<STEP, BF16><<<dim3(n_parts, g.count), 256, 0, stream>>>(g, parts, n_parts);
     const dim3 grid((pad(g.n) + kPrepTile - 1) / kPrepTile, (g.m + kPrepTile - 1) / kPrepTile, g.count);
     k_start<S, STEP, BF16><<<grid, 256, 0, stream>>>(g, parts, n_parts, x_exp);
@@ -364,14 +460,14 @@ hipError_t launch_ortho(const OrthoGroup& g, const float* coeffs, const OrthoSca
     const int64_t big = static_cast<int64_t>((g.m + 255) / 256) * ((g.n + 255) / 256) * g.count;
     if (big >= 256) {
         if (g.split)
-            iterate<2, 256, 2, 4>(g, parts, coeffs, scales, steps, stream);
+            iterate<2, 256>(g, parts, coeffs, scales, steps, stream);
         else
-            iterate<1, 256, 2, 4>(g, parts, coeffs, scales, steps, stream);
+            iterate<1, 256>(g, parts, coeffs, scales, steps, stream);
     } else {
         if (g.split)
-            iterate<2, 128, 2, 2>(g, parts, coeffs, scales, steps, stream);
+            iterate<2, 128>(g, parts, coeffs, scales, steps, stream);
         else
-            iterate<1, 128, 2, 2>(g, parts, coeffs, scales, steps, stream);
+            iterate<1, 128>(g, parts, coeffs, scales, steps, stream);
     }
     return hipGetLastError();
 }
