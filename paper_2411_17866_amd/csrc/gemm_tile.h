@@ -60,6 +60,30 @@ __device__ __forceinline__ f4 mfma(short8v a, short8v b, f4 c) {
                                                       __builtin_bit_cast(half8, b), c, 0, 0, 0);
 }
 
+// Eight consecutive columns of one row from two neighbouring fragments, of which
+// each lane holds four and four: the odd rows of 16 lanes of the first fragment
+// change places with the even ones of the second.  Lane l then holds columns
+// (l / 16 % 2) * 16 + l / 32 * 8 and the next seven of the two fragments' 32, so
+// that four lanes move 64 bytes of fp16 in a row at once.
+struct Eight {
+    float v[8];
+};
+__device__ __forceinline__ Eight join(const f4& a, const f4& b) {
+    Eight e;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        // Copies: a bit cast of a vector's element takes its first element.
+        const float x = a[r], y = b[r];
+        const auto s = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x),
+                                                        __builtin_bit_cast(unsigned, y), false, false);
+        const unsigned p = s[0], q = s[1];
+        e.v[r] = __builtin_bit_cast(float, p);
+        e.v[4 + r] = __builtin_bit_cast(float, q);
+    }
+    return e;
+}
+__device__ __forceinline__ int joined_col(int lane) { return ((lane >> 4) & 1) * 16 + (lane >> 5) * 8; }
+
 // One operand's loader and fragment reader: R rows (or columns) of the tile,
 // NW waves in the work-group.
 template <int R, int NW, Kind KIND, int S>
@@ -256,6 +280,9 @@ struct Tile {
     // i and j of acc[fi][fj][r] inside the tile.
     __device__ __forceinline__ int row(int fi) const { return (wi * FI + fi) * 16 + (lane & 15); }
     __device__ __forceinline__ int col(int fj) const { return (wj * FJ + fj) * 16 + (lane >> 4) * 4; }
+    // Fragments 2 p and 2 p + 1 of row(fi), and their first column.
+    __device__ __forceinline__ Eight eight(int fi, int p) const { return join(acc[fi][2 * p], acc[fi][2 * p + 1]); }
+    __device__ __forceinline__ int col8(int p) const { return (wj * FJ + 2 * p) * 16 + joined_col(lane); }
 };
 
 // One side of a big tile (BigTile below): two half tiles of 128 rows (or
@@ -486,6 +513,29 @@ struct BigTile {
     // i and j of acc[fi][fj][r] inside the tile.
     __device__ __forceinline__ int row(int f) const { return wi * 128 + f * 16 + (lane & 15); }
     __device__ __forceinline__ int col(int f) const { return wj * 64 + f * 16 + (lane >> 4) * 4; }
+    // Fragments 2 p and 2 p + 1 of row(fi), and their first column.
+    __device__ __forceinline__ Eight eight(int f, int p) const { return join(acc[f][2 * p], acc[f][2 * p + 1]); }
+    __device__ __forceinline__ int col8(int p) const { return wj * 64 + p * 32 + joined_col(lane); }
+};
+
+// A BM x BM tile of 16-bit values in LDS (rows of BM * 2 bytes, their 32-byte
+// columns exchanged as a k-strided operand's are), to be read transposed.
+template <int BM>
+struct Turned {
+    static __device__ __forceinline__ int at(int i, int j) {
+        return i * BM * 2 + (((j >> 4) ^ ((i & 3) | ((i >> 1) & 4))) << 5) + (j & 15) * 2;
+    }
+    static __device__ __forceinline__ void put(DSM_LDS char* lds, int i, int j8, short8v v) {
+        *reinterpret_cast<DSM_LDS short8v*>(lds + at(i, j8)) = v;
+    }
+    // Rows i .. i + 7 (i = i0 + lane / 16 * 8) of column j0 + lane % 16; i0 a
+    // multiple of 32, j0 of 16.
+    static __device__ __forceinline__ short8v get(DSM_LDS char* lds, int i0, int j0, int lane) {
+        const int i = i0 + (lane >> 4) * 8 + ((lane & 15) >> 2), j = j0 + (lane & 3) * 4;
+        short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<DSM_LDS short4v*>(lds + at(i, j)));
+        short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<DSM_LDS short4v*>(lds + at(i + 4, j)));
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
 };
 
 template <bool BF16, int S, int BM, Kind KI, Kind KJ>

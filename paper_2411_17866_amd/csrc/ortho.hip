@@ -34,6 +34,7 @@
 namespace dsm {
 namespace {
 
+using tile::Eight;
 using tile::f4;
 using tile::kContig;
 using tile::kStrided;
@@ -41,6 +42,7 @@ using tile::Operand;
 
 typedef unsigned short u16;
 typedef u16 u16x4 __attribute__((ext_vector_type(4)));
+typedef u16 u16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kPad = 64;          // k of every operand is padded to this with zeros
 constexpr int kNormParts = 256;   // partial sums of squares of a matrix, at most
@@ -245,16 +247,38 @@ __device__ __forceinline__ int xcd_run(int b, int total) {
     return x * q + min(x, r) + (b >> 3);
 }
 
-// Four parameters of row i, columns j .. j + 3 of the wide orientation (0 outside).
-__device__ __forceinline__ f4 load_old(const OrthoGroup& g, int which, int i, int j) {
-    f4 v = {0.f, 0.f, 0.f, 0.f};
-    if (i >= g.m) return v;
+// Eight parameters of row i, columns j .. j + 7 of the wide orientation (0 outside).
+__device__ __forceinline__ Eight load_old(const OrthoGroup& g, int which, int i, int j) {
+    Eight e = {};
+    if (i >= g.m) return e;
     const float* x = g.x + g.off.at[which] + (g.tall ? j * g.row_stride + i : i * g.row_stride + j);
-    if (g.vector && !g.tall && j + 3 < g.n) return *reinterpret_cast<const f4*>(x);
+    if (g.vector && !g.tall && j + 7 < g.n) {
+        const f4 a = *reinterpret_cast<const f4*>(x), b = *reinterpret_cast<const f4*>(x + 4);
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-        if (j + r < g.n) v[r] = x[g.tall ? r * g.row_stride : r];
-    return v;
+        for (int r = 0; r < 4; ++r) {
+            e.v[r] = a[r];
+            e.v[4 + r] = b[r];
+        }
+        return e;
+    }
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+        if (j + r < g.n) e.v[r] = x[g.tall ? r * g.row_stride : r];
+    return e;
+}
+
+// fp16 halves of eight numbers.
+__device__ __forceinline__ u16x8 upper(const Eight& e) {
+    u16x8 h;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) h[r] = to_bits(e.v[r]);
+    return h;
+}
+__device__ __forceinline__ u16x8 lower(const Eight& e) {
+    u16x8 l;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) l[r] = to_bits(e.v[r] - from_bits(to_bits(e.v[r])));
+    return l;
 }
 
 template <int S, int BM, Product P>
@@ -291,120 +315,135 @@ __global__ __launch_bounds__(BM * 2) void k_product(OrthoGroup g, Parts parts, i
     // the stored A or X to the stored result.  What a batch of fragments needs of
     // them is loaded before the batch's first store, which the compiler must
     // assume to overlap it: one wait a batch, not one a fragment.
-    constexpr int kBatch = 4;
-    constexpr int kLo = S == 2 ? 32 : 0;
+    constexpr int kBatch = 4, kPairs = T::FJ / 2;
     const int64_t lo_at = S == 2 ? 32 : parts.lo / 2;  // of an X
     const u16* old = P == kPoly ? A : X;
-    const int64_t ld_old = P == kPoly ? lda : ldx;
-    const int last_col = (P == kPoly ? mp : np) - 4;
+    const int64_t ld_old = P == kPoly ? lda : ldx, old_lo = P == kPoly ? 32 : lo_at;
+    const int last_col = (P == kPoly ? mp : np) - 8;
 #pragma unroll
     for (int f0 = 0; f0 < T::FI; f0 += kBatch) {
-        u16x4 oh[kBatch][T::FJ], ol[kBatch][T::FJ];
+        u16x8 oh[kBatch][kPairs], ol[kBatch][kPairs];
         if constexpr (P != kGram) {
 #pragma unroll
             for (int fi = 0; fi < kBatch; ++fi)
 #pragma unroll
-                for (int fj = 0; fj < T::FJ; ++fj) {
+                for (int p = 0; p < kPairs; ++p) {
                     const int64_t q = at<S>(min(ti * BM + t.row(f0 + fi), m - 1),
-                                            min(tj * BM + t.col(fj), last_col), ld_old);
-                    oh[fi][fj] = *reinterpret_cast<const u16x4*>(old + q);
+                                            min(tj * BM + t.col8(p), last_col), ld_old);
+                    oh[fi][p] = *reinterpret_cast<const u16x8*>(old + q);
                     if constexpr (P != kPoly || S == 2)
-                        ol[fi][fj] = *reinterpret_cast<const u16x4*>(old + q + (P == kPoly ? kLo : lo_at));
+                        ol[fi][p] = *reinterpret_cast<const u16x8*>(old + q + old_lo);
                 }
-        }
-        f4 ox_[kBatch][T::FJ];
-        if constexpr (P == kLast && S == 2) {
-            if (g.x) {
-#pragma unroll
-                for (int fi = 0; fi < kBatch; ++fi)
-#pragma unroll
-                    for (int fj = 0; fj < T::FJ; ++fj)
-                        ox_[fi][fj] = load_old(g, which, ti * BM + t.row(f0 + fi), tj * BM + t.col(fj));
-            }
         }
 #pragma unroll
         for (int fi = 0; fi < kBatch; ++fi) {
             const int i = ti * BM + t.row(f0 + fi);
+            Eight px[kPairs];
+            if constexpr (P == kLast && S == 2) {
+                if (g.x) {
 #pragma unroll
-            for (int fj = 0; fj < T::FJ; ++fj) {
-                const int j = tj * BM + t.col(fj);
-                f4 v = t.acc[f0 + fi][fj];
+                    for (int p = 0; p < kPairs; ++p) px[p] = load_old(g, which, i, tj * BM + t.col8(p));
+                }
+            }
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    v[r] *= mul;
+            for (int p = 0; p < kPairs; ++p) {
+                const int j = tj * BM + t.col8(p);
+                Eight v = t.eight(f0 + fi, p);
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    v.v[r] *= mul;
                     if constexpr (P != kGram) {
-                        float o = from_bits(oh[fi][fj][r]);
-                        if constexpr (P != kPoly || S == 2) o += from_bits(ol[fi][fj][r]);
-                        v[r] = __builtin_fmaf(add, o, v[r]);
+                        float o = from_bits(oh[fi][p][r]);
+                        if constexpr (P != kPoly || S == 2) o += from_bits(ol[fi][p][r]);
+                        v.v[r] = __builtin_fmaf(add, o, v.v[r]);
                     }
                 }
                 if constexpr (kSymmetric) {
-                    if (i >= mp || j >= mp) continue;
-                    u16* out = P == kGram ? A : B;
-                    u16x4 hi, lo;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float w = i >= m || j + r >= m ? 0.f : v[r];  // the padding of k
-                        hi[r] = to_bits(w);
-                        lo[r] = to_bits(w - from_bits(hi[r]));
-                    }
-                    if (i < m) {
-                        const int64_t q = at<S>(i, j, lda);
-                        *reinterpret_cast<u16x4*>(out + q) = hi;
-                        if constexpr (S == 2) *reinterpret_cast<u16x4*>(out + q + 32) = lo;
-                    }
-                    if (ti != tj) {
+                    for (int r = 0; r < 8; ++r)
+                        if (i >= m || j + r >= m) v.v[r] = 0.f;  // the padding of k
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            if (j + r >= m) continue;
-                            const int64_t w = at<S>(j + r, i, lda);
-                            out[w] = hi[r];
-                            if constexpr (S == 2) out[w + 32] = lo[r];
-                        }
+                    for (int r = 0; r < 4; ++r) {  // for the mirror image
+                        t.acc[f0 + fi][2 * p][r] = v.v[r];
+                        t.acc[f0 + fi][2 * p + 1][r] = v.v[4 + r];
                     }
+                    if (i >= m || j >= mp) continue;
+                    u16* out = (P == kGram ? A : B) + at<S>(i, j, lda);
+                    *reinterpret_cast<u16x8*>(out) = upper(v);
+                    if constexpr (S == 2) *reinterpret_cast<u16x8*>(out + 32) = lower(v);
                 } else if constexpr (P == kUpdate) {
                     if (i >= m || j >= np) continue;
-                    u16x4 hi, lo;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        hi[r] = to_bits(v[r]);
-                        lo[r] = to_bits(v[r] - from_bits(hi[r]));
-                    }
-                    const int64_t q = at<S>(i, j, ldx);
-                    *reinterpret_cast<u16x4*>(Y + q) = hi;
-                    *reinterpret_cast<u16x4*>(Y + q + lo_at) = lo;
+                    u16* out = Y + at<S>(i, j, ldx);
+                    *reinterpret_cast<u16x8*>(out) = upper(v);
+                    *reinterpret_cast<u16x8*>(out + lo_at) = lower(v);
                 } else {
                     if (i >= m || j >= n) continue;
                     const int64_t e = g.off.at[which] + (g.tall ? j * g.row_stride + i : i * g.row_stride + j);
+                    const bool whole = g.vector && !g.tall && j + 7 < n;
+                    const int64_t step = g.tall ? g.row_stride : 1;
                     if constexpr (S == 2) {
+                        float* out = (g.x ? g.x : static_cast<float*>(g.out)) + e;
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            v[r] *= g.scale;
-                            if (g.x) v[r] = ox_[fi][fj][r] - g.lr * (v[r] + g.weight_decay * ox_[fi][fj][r]);
+                        for (int r = 0; r < 8; ++r) {
+                            v.v[r] *= g.scale;
+                            if (g.x) v.v[r] = px[p].v[r] - g.lr * (v.v[r] + g.weight_decay * px[p].v[r]);
                         }
-                        float* out = g.x ? g.x : static_cast<float*>(g.out);
-                        if (g.vector && !g.tall && j + 3 < n) {
-                            *reinterpret_cast<f4*>(out + e) = v;
+                        if (whole) {
+                            *reinterpret_cast<f4*>(out) = f4{v.v[0], v.v[1], v.v[2], v.v[3]};
+                            *reinterpret_cast<f4*>(out + 4) = f4{v.v[4], v.v[5], v.v[6], v.v[7]};
                             continue;
                         }
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (j + r < n) out[e + (g.tall ? r * g.row_stride : r)] = v[r];
+                        for (int r = 0; r < 8; ++r)
+                            if (j + r < n) out[r * step] = v.v[r];
                     } else {
-                        u16* out = static_cast<u16*>(g.out);
-                        u16x4 b;
+                        u16* out = static_cast<u16*>(g.out) + e;
+                        u16x8 b;
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) b[r] = float_to_bf16(v[r]);
-                        if (g.vector && !g.tall && j + 3 < n) {
-                            *reinterpret_cast<u16x4*>(out + e) = b;
+                        for (int r = 0; r < 8; ++r) b[r] = float_to_bf16(v.v[r]);
+                        if (whole) {
+                            *reinterpret_cast<u16x4*>(out) = u16x4{b[0], b[1], b[2], b[3]};
+                            *reinterpret_cast<u16x4*>(out + 4) = u16x4{b[4], b[5], b[6], b[7]};
                             continue;
                         }
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (j + r < n) out[e + (g.tall ? r * g.row_stride : r)] = b[r];
+                        for (int r = 0; r < 8; ++r)
+                            if (j + r < n) out[r * step] = b[r];
                     }
                 }
             }
+        }
+    }
+    // The tile above the diagonal: the same values through LDS, read transposed.
+    if constexpr (kSymmetric) {
+        if (ti == tj) return;
+        using Turn = tile::Turned<BM>;
+        DSM_LDS char* turned = (DSM_LDS char*)lds;
+#pragma unroll
+        for (int half = 0; half < S; ++half) {
+#pragma unroll
+            for (int fi = 0; fi < T::FI; ++fi)
+#pragma unroll
+                for (int p = 0; p < kPairs; ++p) {
+                    Eight v;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        v.v[r] = t.acc[fi][2 * p][r];
+                        v.v[4 + r] = t.acc[fi][2 * p + 1][r];
+                    }
+                    Turn::put(turned, t.row(fi), t.col8(p),
+                              __builtin_bit_cast(tile::short8v, half == 0 ? upper(v) : lower(v)));
+                }
+            __syncthreads();
+            // 16 rows of the mirror image by 32 of its columns for each wave and turn.
+            for (int c = t.wave; c < BM / 16 * (BM / 32); c += BM * 2 / 64) {
+                const int j0 = c / (BM / 32) * 16, i0 = c % (BM / 32) * 32;
+                const int j = tj * BM + j0 + (t.lane & 15), i = ti * BM + i0 + (t.lane >> 4) * 8;
+                const tile::short8v v = Turn::get(turned, i0, j0, t.lane);
+                if (j < m && i < mp)
+                    *reinterpret_cast<tile::short8v*>((P == kGram ? A : B) + at<S>(j, i, lda) + half * 32) = v;
+            }
+            if (half + 1 < S) __syncthreads();
         }
     }
 }
