@@ -70,7 +70,7 @@ __device__ __forceinline__ int exponent_for(uint32_t bits) {
     if (bits == 0) return 0;
     int e;
     frexpf(__builtin_bit_cast(float, bits), &e);
-    return min(15 - e, 100);
+    return min(15 - e, 120);
 }
 
 __device__ __forceinline__ bool is_valid(int64_t target, int vocab) { return target >= 0 && target < vocab; }
@@ -233,12 +233,21 @@ __device__ __forceinline__ Operand w_rows(const CePlan& p, const CeBuffers& b, i
     return Operand{w + first * ld, ld, p.vocab - first, static_cast<int32_t>(p.ld_w)};
 }
 
-// What brings a tile's accumulators to logits.
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+
+// What brings a tile's accumulators to logits in units of log2.
 template <Form FORM>
-__device__ __forceinline__ int logit_exponent(const CePlan& p, const CeBuffers& b) {
-    if constexpr (FORM == kBf16) return 0;
+__device__ __forceinline__ float logit_unit(const CePlan& p, const CeBuffers& b) {
+    if constexpr (FORM == kBf16) return kLog2e;
     const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
-    return -(exponent_for(s->h_max) + exponent_for(s->w_max));
+    return ldexpf(kLog2e, -(exponent_for(s->h_max) + exponent_for(s->w_max)));
+}
+
+// Largest exponent and sum of exp2(z2 - largest) of two sets of logits.
+__device__ __forceinline__ float2 joined(float2 a, float2 c) {
+    const float top = fmaxf(a.x, c.x);
+    if (top == -__builtin_inff()) return make_float2(top, a.y + c.y);
+    return make_float2(top, a.y * __builtin_amdgcn_exp2f(a.x - top) + c.y * __builtin_amdgcn_exp2f(c.x - top));
 }
 
 // First pass: each row's largest logit and sum of exp(z - largest) in a tile,
@@ -252,7 +261,8 @@ __global__ __launch_bounds__(BM * 2) void k_stats(CePlan p, CeBuffers b) {
     const int tv = id / tiles_t, tt = id - tv * tiles_t;
     T t;
     t.run(h_rows(p, b), w_rows(p, b, 0), tt * BM, tv * BM, 0, static_cast<int>(p.ld_h / (FORM == kHalves ? 2 : 1)), (DSM_LDS char*)lds);
-    const int ex = logit_exponent<FORM>(p, b);
+    // In units of log2: z2 = acc * unit, exp(z) = exp2(z2).
+    const float unit = logit_unit<FORM>(p, b);
     float* hit = reinterpret_cast<float*>(b.workspace + p.hit);
     float2* part = reinterpret_cast<float2*>(lds);  // [T::WN][BM]
     int rel[T::FI];  // the target's column in the tile, or -1
@@ -262,32 +272,42 @@ __global__ __launch_bounds__(BM * 2) void k_stats(CePlan p, CeBuffers b) {
         const int64_t target = b.target[min(token, p.tokens - 1)];
         rel[fi] = token < p.tokens && is_valid(target, p.vocab) ? static_cast<int>(target) - tv * BM : -1;
     }
-#pragma unroll
-    for (int fi = 0; fi < T::FI; ++fi) {
-        const int token = tt * BM + t.row(fi);
-        float top = -__builtin_inff();
+    if (tv * BM + BM > p.vocab) {  // columns past the vocabulary
 #pragma unroll
         for (int fj = 0; fj < T::FJ; ++fj)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int c = t.col(fj) + r;
-                float z = FORM == kBf16 ? t.acc[fi][fj][r] : ldexpf(t.acc[fi][fj][r], ex);
-                if (rel[fi] == c) hit[token] = z;
-                if (tv * BM + c >= p.vocab) z = -__builtin_inff();
-                t.acc[fi][fj][r] = z;
-                top = fmaxf(top, z);
-            }
+            for (int r = 0; r < 4; ++r)
+                if (tv * BM + t.col(fj) + r >= p.vocab)
+#pragma unroll
+                    for (int fi = 0; fi < T::FI; ++fi) t.acc[fi][fj][r] = -__builtin_inff();
+    }
+    const int first_col = t.wj * T::FJ * 16;
+#pragma unroll
+    for (int fi = 0; fi < T::FI; ++fi) {
+        const int token = tt * BM + t.row(fi);
+        // Few waves hold a target's column.
+        if (__any(rel[fi] >= first_col && rel[fi] < first_col + T::FJ * 16)) {
+#pragma unroll
+            for (int fj = 0; fj < T::FJ; ++fj)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (rel[fi] == t.col(fj) + r) hit[token] = t.acc[fi][fj][r] * unit;
+        }
+        float top = t.acc[fi][0][0];
+#pragma unroll
+        for (int fj = 0; fj < T::FJ; ++fj)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) top = fmaxf(top, t.acc[fi][fj][r]);
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
+        top *= unit;
         float sum = 0.f;
         if (top != -__builtin_inff()) {
 #pragma unroll
             for (int fj = 0; fj < T::FJ; ++fj)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float d = t.acc[fi][fj][r] - top;
-                    sum += FORM == kHalves ? expf(d) : __expf(d);
-                }
+                for (int r = 0; r < 4; ++r)
+                    sum += __builtin_amdgcn_exp2f(__builtin_fmaf(t.acc[fi][fj][r], unit, -top));
         }
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
@@ -299,39 +319,32 @@ __global__ __launch_bounds__(BM * 2) void k_stats(CePlan p, CeBuffers b) {
         if (tt * BM + r >= p.tokens) break;
         float2 a = part[r];
 #pragma unroll
-        for (int w = 1; w < T::WN; ++w) {
-            const float2 c = part[w * BM + r];
-            const float top = fmaxf(a.x, c.x);
-            const float sa = a.x == -__builtin_inff() ? a.y : a.y * expf(a.x - top);
-            const float sc = c.x == -__builtin_inff() ? c.y : c.y * expf(c.x - top);
-            a = make_float2(top, sa + sc);
-        }
+        for (int w = 1; w < T::WN; ++w) a = joined(a, part[w * BM + r]);
         stats[tt * BM + r] = a;
     }
 }
 
-// lse and loss: a wave's lanes take the tiles of a token in turn.
-__global__ __launch_bounds__(256) void k_join(CePlan p, CeBuffers b, int tiles) {
-    const int token = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (token >= p.tokens) return;
-    const float2* stats = reinterpret_cast<const float2*>(b.workspace + p.stats);
-    float top = -__builtin_inff(), sum = 0.f;
-    for (int v = threadIdx.x & 63; v < tiles; v += 64) top = fmaxf(top, stats[static_cast<int64_t>(v) * p.tokens + token].x);
-    for (int w = 32; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
-    for (int v = threadIdx.x & 63; v < tiles; v += 64) {
-        const float2 s = stats[static_cast<int64_t>(v) * p.tokens + token];
-        sum += s.x == -__builtin_inff() ? s.y : s.y * expf(s.x - top);
-    }
-    for (int w = 32; w > 0; w >>= 1) sum += __shfl_xor(sum, w);
-    if ((threadIdx.x & 63) == 0) {
-        const float lse = top + logf(sum);
-        reinterpret_cast<float*>(b.workspace + p.lse)[token] = lse;
-        if (b.lse) b.lse[token] = lse;
-        float loss = 0.f;
-        if (is_valid(b.target[token], p.vocab))
-            loss = lse - reinterpret_cast<const float*>(b.workspace + p.hit)[token];
-        b.loss[token] = loss;
-    }
+// lse and loss of 64 tokens by a work-group: a lane a token, the waves share the
+// tiles.
+__global__ __launch_bounds__(1024) void k_join(CePlan p, CeBuffers b, int tiles) {
+    __shared__ float2 part[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int token = blockIdx.x * 64 + lane, at = min(token, p.tokens - 1);
+    const float2* stats = reinterpret_cast<const float2*>(b.workspace + p.stats) + at;
+    float2 a = make_float2(-__builtin_inff(), 0.f);
+#pragma unroll 4
+    for (int v = wave; v < tiles; v += 16) a = joined(a, stats[static_cast<int64_t>(v) * p.tokens]);
+    part[wave][lane] = a;
+    __syncthreads();
+    if (wave != 0 || token >= p.tokens) return;
+    for (int w = 1; w < 16; ++w) a = joined(a, part[w][lane]);
+    const float lse2 = a.x + __builtin_amdgcn_logf(a.y);  // v_log_f32: log2
+    reinterpret_cast<float*>(b.workspace + p.lse)[token] = lse2;
+    if (b.lse) b.lse[token] = lse2 * kLn2;
+    float loss = 0.f;
+    if (is_valid(b.target[token], p.vocab))
+        loss = (lse2 - reinterpret_cast<const float*>(b.workspace + p.hit)[token]) * kLn2;
+    b.loss[token] = loss;
 }
 
 // The weighted total, in a fixed order.
@@ -361,47 +374,57 @@ __global__ __launch_bounds__(BM * 2) void k_piece(CePlan p, CeBuffers b, int fir
     const int tv = id / tiles_t, tt = id - tv * tiles_t;
     T t;
     t.run(h_rows(p, b), w_rows(p, b, first), tt * BM, tv * BM, 0, static_cast<int>(p.ld_h / (FORM == kHalves ? 2 : 1)), (DSM_LDS char*)lds);
-    const int ex = logit_exponent<FORM>(p, b);
+    const float unit = logit_unit<FORM>(p, b);
     const int eg = exponent_for(reinterpret_cast<const Scalars*>(b.workspace + p.scalars)->c_max);
     const float* lse = reinterpret_cast<const float*>(b.workspace + p.lse);
     const float* coef = reinterpret_cast<const float*>(b.workspace + p.coef);
     u16* g = reinterpret_cast<u16*>(b.workspace + p.p);
-    // What the rows need, all loaded before the first store.
+    // What the rows need, all loaded before the first store.  A row without a
+    // valid target gets exp2(z2 - inf) = 0 throughout.
     int rel[T::FI];
-    bool valid[T::FI];
     float l[T::FI], c[T::FI];
 #pragma unroll
     for (int fi = 0; fi < T::FI; ++fi) {
         const int token = tt * BM + t.row(fi), at = min(token, p.tokens - 1);
         const int64_t target = b.target[at];
-        valid[fi] = token < p.tokens && is_valid(target, p.vocab);
-        rel[fi] = valid[fi] ? static_cast<int>(target) - first - tv * BM : -1;
-        l[fi] = lse[at];
-        c[fi] = ldexpf(coef[at], eg);
+        const bool valid = token < p.tokens && is_valid(target, p.vocab);
+        rel[fi] = valid ? static_cast<int>(target) - first - tv * BM : -1;
+        l[fi] = valid ? lse[at] : __builtin_inff();
+        c[fi] = valid ? ldexpf(coef[at], eg) : 0.f;
     }
+    const bool ragged = tv * BM + BM > cols;
+    const int first_col = t.wj * T::FJ * 16;
 #pragma unroll
     for (int fi = 0; fi < T::FI; ++fi) {
         const int token = tt * BM + t.row(fi);
+        // Few waves hold a target's column.
+        const bool hits = __any(rel[fi] >= first_col && rel[fi] < first_col + T::FJ * 16);
         if (token >= rows_pad) continue;
 #pragma unroll
-        for (int fj = 0; fj < T::FJ; ++fj) {
-            const int col = t.col(fj);
-            if (tv * BM + col >= cols_pad) continue;
-            u16x4 hi, lo;
+        for (int q = 0; q < T::FJ / 2; ++q) {
+            const int col = t.col8(q);
+            const tile::Eight z = t.eight(fi, q);
+            float v[8];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float z = ldexpf(t.acc[fi][fj][r], ex) - l[fi];
-                float v = FORM == kHalves ? expf(z) : __expf(z);
-                if (rel[fi] == col + r) v -= 1.0f;
-                v *= c[fi];
-                if (!valid[fi] || tv * BM + col + r >= cols) v = 0.f;
-                hi[r] = float_to_half(v);
-                lo[r] = float_to_half(v - half_to_float(hi[r]));
+            for (int r = 0; r < 8; ++r) v[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(z.v[r], unit, -l[fi]));
+            if (hits) {
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+                    if (rel[fi] == col + r) v[r] -= 1.0f;
+            }
+            u16x8 hi, lo;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                v[r] *= c[fi];
+                if (ragged && tv * BM + col + r >= cols) v[r] = 0.f;
+                hi[r] = float_to_half(v[r]);
+                lo[r] = float_to_half(v[r] - half_to_float(hi[r]));
             }
             const int at = tv * BM + col;
+            if (at >= cols_pad) continue;
             u16* out = g + token * p.ld_p + (FORM == kHalves ? ((at >> 5) << 6) + (at & 31) : at);
-            *reinterpret_cast<u16x4*>(out) = hi;
-            if constexpr (FORM == kHalves) *reinterpret_cast<u16x4*>(out + 32) = lo;
+            *reinterpret_cast<u16x8*>(out) = hi;
+            if constexpr (FORM == kHalves) *reinterpret_cast<u16x8*>(out + 32) = lo;
         }
     }
 }
@@ -514,13 +537,18 @@ __global__ __launch_bounds__(BM * 2) void k_dw(CePlan p, CeBuffers b, int first,
         const int v = tv * BM + t.row(fi);
         if (v >= cols) continue;
 #pragma unroll
-        for (int fj = 0; fj < T::FJ; ++fj) {
-            const int d = td * BM + t.col(fj);
-            f4 x = t.acc[fi][fj];
+        for (int q = 0; q < T::FJ / 2; ++q) {
+            const int d = td * BM + t.col8(q);
+            const tile::Eight x = t.eight(fi, q);
+            f4 lo, hi;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] = ldexpf(x[r], ex);
-            if (d < p.dim)
-                store_grad<FORM == kHalves>(b.dw, (first + v) * b.dw_stride + d, x, p.dim - d, b.dw_vector);
+            for (int r = 0; r < 4; ++r) {
+                lo[r] = ldexpf(x.v[r], ex);
+                hi[r] = ldexpf(x.v[4 + r], ex);
+            }
+            const int64_t at = (first + v) * b.dw_stride + d;
+            if (d < p.dim) store_grad<FORM == kHalves>(b.dw, at, lo, p.dim - d, b.dw_vector);
+            if (d + 4 < p.dim) store_grad<FORM == kHalves>(b.dw, at + 4, hi, p.dim - d - 4, b.dw_vector);
         }
     }
 }
@@ -529,7 +557,7 @@ template <Form FORM, int BM>
 void losses(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
     const int tt = (p.tokens + BM - 1) / BM, tv = (p.vocab + BM - 1) / BM;
     k_stats<FORM, BM><<<tt * tv, BM * 2, 0, stream>>>(p, b);
-    k_join<<<(p.tokens + 3) / 4, 256, 0, stream>>>(p, b, tv);
+    k_join<<<(p.tokens + 63) / 64, 1024, 0, stream>>>(p, b, tv);
     k_total<<<1, 1024, 0, stream>>>(p, b);
 }
 

@@ -54,9 +54,41 @@ dsm_status check_workspace(const void* ws, int64_t bytes, int64_t need) {
 
 // ---- Linear layer with softmax cross entropy ----
 
-// G of a piece takes at most this much memory.  A larger piece means fewer
-// launches and longer sums for dh.
-constexpr int64_t kPieceBytes = int64_t(256) << 20;
+// G of a piece takes at most this much memory.
+constexpr int64_t kPieceBytes = int64_t(320) << 20;
+constexpr int kMaxSplits = 16;
+
+// How the second pass is cut: pieces of the vocabulary, and parts of a piece's
+// columns that dh is summed over side by side.  Estimated microseconds decide,
+// from how many turns the 256 CUs take over a product's tiles (two tiles of 128 fit
+// a CU, one of 256), what a step of 64 columns of k costs a tile, and what adding
+// to dh's fp32 parts moves at 4 TB/s.
+void cut(dsm::CePlan* q, int64_t T, int64_t D, int64_t V) {
+    const int64_t tile = q->tile, width = q->f32 ? 2 : 1, tokens_pad = round_up(T, 64);
+    const double slots = tile == 256 ? 256 : 512, step = (tile == 256 ? 0.62 : 0.38) * (q->f32 ? 3.0 : 1.0);
+    const auto tiles = [&](int64_t n) { return (n + tile - 1) / tile; };
+    const auto turns = [&](int64_t n) { return std::ceil(static_cast<double>(n) / slots); };
+    const double dh_pass = 4e-6 * static_cast<double>(T * D) / 4.0;  // a read or write of one part
+    const int64_t most = std::max<int64_t>(kPieceBytes / (tokens_pad * 2 * width) / tile, 1);
+    double best = 0.0;
+    for (int64_t pieces = (tiles(V) + most - 1) / most; pieces <= tiles(V); ++pieces) {
+        const int64_t per = (tiles(V) + pieces - 1) / pieces, n = (tiles(V) + per - 1) / per;
+        const double logits = turns(tiles(T) * per) * (static_cast<double>(D) / 64 * step + 5.0);
+        const double dw = turns(per * tiles(D)) * (static_cast<double>(T) / 64 * step + 5.0);
+        for (int s = 1; s <= kMaxSplits && s * 256 <= std::max<int64_t>(per * tile, 256); ++s) {
+            const double dh = turns(tiles(T) * tiles(D) * s) * (static_cast<double>(per * tile) / 64 / s * step + 5.0) +
+                              s * dh_pass * (n > 1 ? 2 : 1);
+            const double cost = static_cast<double>(n) * (logits + dw + dh + 9.0) + s * dh_pass;
+            if (best == 0.0 || cost < best) {
+                best = cost;
+                q->piece = static_cast<int32_t>(per * tile);
+                q->dh_splits = s;
+            }
+        }
+        if (pieces > 64 && best > 0.0) break;
+    }
+    q->ld_p = q->piece * width;
+}
 
 dsm_status check_ce(const dsm_ce_problem* p) {
     if (!p) return invalid("problem is NULL");
@@ -93,26 +125,8 @@ dsm::CePlan make_plan(const dsm_ce_problem* p) {
     q.h = take(T * q.ld_h * 2);
     q.w = take(V * q.ld_w * 2);
     if (p->grads && T > 0) {
-        int64_t most = kPieceBytes / (tokens_pad * 2 * width) / q.tile * q.tile;
-        most = std::max<int64_t>(most, q.tile);
-        const int64_t pieces = (V + most - 1) / most;
-        q.piece = static_cast<int32_t>(round_up((V + pieces - 1) / pieces, q.tile));
-        q.ld_p = q.piece * width;
+        cut(&q, T, p->dim, V);
         q.p = take(tokens_pad * q.ld_p * 2);
-        // As many parts as fill the 256 CUs: the share of them that the last
-        // turn leaves idle is what counts, and each part costs a pass over dh.
-        const int64_t tiles = ((T + q.tile - 1) / q.tile) * ((p->dim + q.tile - 1) / q.tile);
-        const int64_t per_cu = q.tile == 256 ? 1 : 2, slots = 256 * per_cu;
-        double best = 0.0;
-        for (int s = 1; s <= 16 && s * 64 * 4 <= q.piece; ++s) {
-            const int64_t n = tiles * s, turns = (n + slots - 1) / slots;
-            const double score = static_cast<double>(n) / static_cast<double>(turns * slots) - 0.01 * s;
-            if (q.dh_splits == 0 || score > best) {
-                best = score;
-                q.dh_splits = s;
-            }
-        }
-        if (q.dh_splits == 0) q.dh_splits = 1;
         q.ld_dh = round_up(p->dim, 4);
         q.dh = take(q.dh_splits * T * q.ld_dh * 4);
     }
