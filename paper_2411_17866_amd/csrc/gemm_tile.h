@@ -39,6 +39,13 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 
 enum Kind { kContig, kStrided };  // how an operand lies in memory
 
+// What the operands hold: 16-bit numbers; two fp16 halves of each number; or fp32
+// itself, for tiles that wait for memory rather than for the matrix cores (fp32
+// products run at a sixteenth of the 16-bit ones' rate).  Sizes of operands count
+// 16-bit units, two for each number of the last two.
+enum Elem { kF16, kBF16, kSplit, kF32 };
+constexpr int units(Elem e) { return e == kSplit || e == kF32 ? 2 : 1; }
+
 // Zero-based 16-bit elements; `rows` is the number of rows that may be read
 // (rows past it are replaced by the last one: what they give is never used, or
 // meets zeros in the other operand), `cols` the same for the columns of a
@@ -50,9 +57,9 @@ struct Operand {
     int32_t cols;  // k-strided only: 16-bit elements that may be read in a row
 };
 
-template <bool BF16>
+template <Elem E>
 __device__ __forceinline__ f4 mfma(short8v a, short8v b, f4 c) {
-    if constexpr (BF16)
+    if constexpr (E == kBF16)
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bfloat8, a),
                                                        __builtin_bit_cast(bfloat8, b), c, 0, 0, 0);
     else
@@ -174,11 +181,27 @@ struct Side {
             return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
         }
     }
+    // fp32: steps part * 16 + lane / 16 * 4 and the next three, one for each of
+    // four matrix instructions.
+    static __device__ __forceinline__ f4 fragment32(const DSM_LDS char* lds, int f, int part, int lane) {
+        if constexpr (KIND == kContig) {
+            return __builtin_bit_cast(f4, fragment(lds, f, part, lane));
+        } else {
+            const int k = part * 16 + (lane >> 4) * 4, at = f * 64 + (lane & 15) * 4;
+            f4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] = *reinterpret_cast<const DSM_LDS float*>(lds + (k + e) * kRowBytes +
+                                                               (((at >> 5) ^ swz(k + e)) << 5) + (at & 31));
+            return v;
+        }
+    }
 };
 
 // BM x BN tile by WM x WN waves.
-template <bool BF16, int S, int BM, int BN, int WM, int WN_, Kind KI, Kind KJ>
+template <Elem E, int BM, int BN, int WM, int WN_, Kind KI, Kind KJ>
 struct Tile {
+    static constexpr int S = units(E), kBM = BM, kBN = BN;
     static constexpr int WN = WN_;
     static constexpr int kWaves = WM * WN;
     static constexpr int kThreads = kWaves * 64;
@@ -196,7 +219,23 @@ struct Tile {
     __device__ __forceinline__ void compute(const DSM_LDS char* st) {
         const DSM_LDS char* li = st;
         const DSM_LDS char* lj = st + SideI::kStageBytes;
-        if constexpr (S == 1) {
+        if constexpr (E == kF32) {
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                f4 fj[FJ];
+#pragma unroll
+                for (int j = 0; j < FJ; ++j) fj[j] = SideJ::fragment32(lj, wj * FJ + j, part, lane);
+#pragma unroll
+                for (int i = 0; i < FI; ++i) {
+                    const f4 fi = SideI::fragment32(li, wi * FI + i, part, lane);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int j = 0; j < FJ; ++j)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fj[j][e], fi[e], acc[i][j], 0, 0, 0);
+                }
+            }
+        } else if constexpr (S == 1) {
 #pragma unroll
             for (int part = 0; part < 2; ++part) {
                 short8v fj[FJ];
@@ -206,7 +245,7 @@ struct Tile {
                 for (int i = 0; i < FI; ++i) {
                     const short8v fi = SideI::fragment(li, wi * FI + i, part, lane);
 #pragma unroll
-                    for (int j = 0; j < FJ; ++j) acc[i][j] = mfma<BF16>(fj[j], fi, acc[i][j]);
+                    for (int j = 0; j < FJ; ++j) acc[i][j] = mfma<E>(fj[j], fi, acc[i][j]);
                 }
             }
         } else {
@@ -221,19 +260,16 @@ struct Tile {
                 const short8v hi = SideI::fragment(li, wi * FI + i, 0, lane);
                 const short8v li_ = SideI::fragment(li, wi * FI + i, 1, lane);
 #pragma unroll
-                for (int j = 0; j < FJ; ++j) acc[i][j] = mfma<BF16>(lo[j], hi, acc[i][j]);
+                for (int j = 0; j < FJ; ++j) acc[i][j] = mfma<E>(lo[j], hi, acc[i][j]);
 #pragma unroll
-                for (int j = 0; j < FJ; ++j) acc[i][j] = mfma<BF16>(hj[j], li_, acc[i][j]);
+                for (int j = 0; j < FJ; ++j) acc[i][j] = mfma<E>(hj[j], li_, acc[i][j]);
 #pragma unroll
-                for (int j = 0; j < FJ; ++j) acc[i][j] = mfma<BF16>(hj[j], hi, acc[i][j]);
+                for (int j = 0; j < FJ; ++j) acc[i][j] = mfma<E>(hj[j], hi, acc[i][j]);
             }
         }
     }
 
-    // The products of steps [k_begin, k_end); k_begin is a multiple of kSteps,
-    // and what lies between k_end and the next multiple is zero in one operand.
-    __device__ __forceinline__ void run(const Operand& oi, const Operand& oj, int64_t i0, int64_t j0,
-                                        int k_begin, int k_end, DSM_LDS char* lds) {
+    __device__ __forceinline__ void clear() {
         lane = threadIdx.x & 63;
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         wi = wave / WN;
@@ -242,6 +278,16 @@ struct Tile {
         for (int i = 0; i < FI; ++i)
 #pragma unroll
             for (int j = 0; j < FJ; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+    }
+    __device__ __forceinline__ void run(const Operand& oi, const Operand& oj, int64_t i0, int64_t j0,
+                                        int k_begin, int k_end, DSM_LDS char* lds) {
+        clear();
+        add(oi, oj, i0, j0, k_begin, k_end, lds);
+    }
+    // Adds the products of steps [k_begin, k_end); k_begin is a multiple of kSteps,
+    // and what lies between k_end and the next multiple is zero in one operand.
+    __device__ __forceinline__ void add(const Operand& oi, const Operand& oj, int64_t i0, int64_t j0,
+                                        int k_begin, int k_end, DSM_LDS char* lds) {
         SideI si;
         SideJ sj;
         si.init(oi, i0, lane, wave);
@@ -381,9 +427,11 @@ struct HalfSide {
 // Each load has two turns or more to arrive: before the barrier a wave waits
 // until at most 8 of its loads are in flight, which is all but those that the
 // next turn's reads need.
-template <bool BF16, int S, Kind KI, Kind KJ>
+template <Elem E, Kind KI, Kind KJ>
 struct BigTile {
-    static constexpr int kBM = 256, kThreads = 512;
+    static_assert(E != kF32, "fp32 products are for tiles that wait for memory");
+    static constexpr int S = units(E);
+    static constexpr int kBM = 256, kBN = 256, kThreads = 512;
     static constexpr int WN = 4, FI = 8, FJ = 4;
     using SideI = HalfSide<64, KI, S>;
     using SideJ = HalfSide<32, KJ, S>;
@@ -436,14 +484,13 @@ struct BigTile {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[H * 4 + i][j] = mfma<BF16>(fj[j][pj], fi[i][pi], acc[H * 4 + i][j]);
+                for (int j = 0; j < 4; ++j) acc[H * 4 + i][j] = mfma<E>(fj[j][pj], fi[i][pi], acc[H * 4 + i][j]);
         }
         __builtin_amdgcn_s_setprio(0);
         fence();
     }
 
-    __device__ __forceinline__ void run(const Operand& oi, const Operand& oj, int64_t i0, int64_t j0,
-                                        int k_begin, int k_end, DSM_LDS char* lds) {
+    __device__ __forceinline__ void clear() {
         lane = threadIdx.x & 63;
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         wi = wave / WN;
@@ -452,6 +499,14 @@ struct BigTile {
         for (int i = 0; i < FI; ++i)
 #pragma unroll
             for (int j = 0; j < FJ; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+    }
+    __device__ __forceinline__ void run(const Operand& oi, const Operand& oj, int64_t i0, int64_t j0,
+                                        int k_begin, int k_end, DSM_LDS char* lds) {
+        clear();
+        add(oi, oj, i0, j0, k_begin, k_end, lds);
+    }
+    __device__ __forceinline__ void add(const Operand& oi, const Operand& oj, int64_t i0, int64_t j0,
+                                        int k_begin, int k_end, DSM_LDS char* lds) {
         if (k_begin >= k_end) return;
         SideI si;
         SideJ sj;
@@ -538,18 +593,18 @@ struct Turned {
     }
 };
 
-template <bool BF16, int S, int BM, Kind KI, Kind KJ>
+template <Elem E, int BM, Kind KI, Kind KJ>
 struct Picked {
     static_assert(BM == 128, "tiles are 128 or 256 square");
-    using T = Tile<BF16, S, 128, 128, 2, 2, KI, KJ>;
+    using T = Tile<E, 128, 128, 2, 2, KI, KJ>;
 };
-template <bool BF16, int S, Kind KI, Kind KJ>
-struct Picked<BF16, S, 256, KI, KJ> {
-    using T = BigTile<BF16, S, KI, KJ>;
+template <Elem E, Kind KI, Kind KJ>
+struct Picked<E, 256, KI, KJ> {
+    using T = BigTile<E, KI, KJ>;
 };
 // The tile of BM x BM by BM * 2 threads.
-template <bool BF16, int S, int BM, Kind KI, Kind KJ>
-using Pick = typename Picked<BF16, S, BM, KI, KJ>::T;
+template <Elem E, int BM, Kind KI, Kind KJ>
+using Pick = typename Picked<E, BM, KI, KJ>::T;
 
 }  // namespace tile
 }  // namespace dsm

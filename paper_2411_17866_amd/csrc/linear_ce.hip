@@ -12,14 +12,22 @@
 // with gradients the matrix cores do 8 T V D operations where keeping all
 // logits would need 6.
 //
-// Types.  With gradients every operand is fp16, scaled by a power of two so that
-// its largest finite entry lies just under fp16's largest number.  A bf16 number
-// then keeps all its bits down to 2^-32 of the largest one, and G keeps 11 bits
-// where bf16 would leave it 8: a row of G is mostly its target's entry, whose
-// rounding no sum averages out, and in bf16 it alone would cost the gradients
-// what their own rounding to bf16 does.  fp32 buffers go as two fp16 halves each
-// (gemm_tile.h).  The losses alone of bf16 buffers take bf16 operands as they
-// are.  Logits, softmax statistics, losses and sums are fp32.
+// What the products take ("form", chosen by the host from type and tokens):
+//   fp16, scaled     bf16 buffers, many tokens.  A power of two brings an
+//                    operand's largest finite entry just under fp16's largest
+//                    number; a bf16 number then keeps all its bits down to 2^-32
+//                    of the largest, and G keeps 11 bits where bf16 would leave
+//                    it 8: a row of G is mostly its target's entry, whose
+//                    rounding no sum averages out, and in bf16 it alone would
+//                    cost the gradients what their own rounding to bf16 does.
+//   two fp16 halves  fp32 buffers, many tokens (gemm_tile.h)
+//   bf16             bf16 buffers, few tokens or no gradients: w is read where it
+//                    lies, which saves the passes over w that find its largest
+//                    entry and convert it, and G goes as two bf16 halves (twice
+//                    the matrix instructions in the products of G)
+//   fp32             fp32 buffers, few tokens: w is read where it lies
+// Few tokens are those for which reading w costs more than multiplying it.
+// Logits, softmax statistics, losses and sums are fp32.
 //
 // A token whose target lies outside [0, vocab) has no loss and no gradient, and
 // what its row of h holds, NaN included, reaches no output but its own zeros.
@@ -56,13 +64,16 @@ __device__ __forceinline__ float bf16_to_float(u16 v) {
     return __builtin_bit_cast(float, static_cast<uint32_t>(v) << 16);
 }
 
-// What the products take: bf16 as it is, scaled fp16, or two halves of it.
-enum Form { kBf16, kHalf, kHalves };
+constexpr bool is_f32(CeForm f) { return f == kCeHalves || f == kCeF32; }
+constexpr bool is_scaled(CeForm f) { return f == kCeHalf || f == kCeHalves; }
+constexpr tile::Elem elem(CeForm f) {
+    return f == kCeHalf ? tile::kF16 : f == kCeBf16 ? tile::kBF16 : f == kCeHalves ? tile::kSplit : tile::kF32;
+}
+constexpr int units(CeForm f) { return tile::units(elem(f)); }
 
 struct Scalars {
     uint32_t h_max, w_max;  // bits of the largest finite |h| and |w| (fp32 buffers)
     uint32_t c_max;         // bits of the largest finite |c_t|
-    int32_t valid;          // tokens whose target lies in the vocabulary
 };
 
 // The power of two that brings a largest magnitude into [2^14, 2^15).
@@ -80,8 +91,9 @@ __device__ __forceinline__ uint32_t finite_bits(float v) {
     return b < 0x7f800000u ? b : 0u;
 }
 
-// c_t of every token, their largest magnitude and the number of valid targets.
-__global__ __launch_bounds__(1024) void k_coef(CePlan p, CeBuffers b) {
+// c_t of every token, their largest magnitude and the number of valid targets;
+// by one work-group.
+__device__ void coefficients(const CePlan& p, const CeBuffers& b) {
     __shared__ int count;
     __shared__ uint32_t c_max;
     if (threadIdx.x == 0) {
@@ -90,14 +102,14 @@ __global__ __launch_bounds__(1024) void k_coef(CePlan p, CeBuffers b) {
     }
     __syncthreads();
     int mine = 0;
-    for (int t = threadIdx.x; t < p.tokens; t += 1024) mine += is_valid(b.target[t], p.vocab);
+    for (int t = threadIdx.x; t < p.tokens; t += blockDim.x) mine += is_valid(b.target[t], p.vocab);
     for (int w = 32; w > 0; w >>= 1) mine += __shfl_xor(mine, w);
     if ((threadIdx.x & 63) == 0) atomicAdd(&count, mine);
     __syncthreads();
     const float by = b.mean ? static_cast<float>(max(count, 1)) : 1.0f;
     float* coef = reinterpret_cast<float*>(b.workspace + p.coef);
     uint32_t top = 0;
-    for (int t = threadIdx.x; t < p.tokens; t += 1024) {
+    for (int t = threadIdx.x; t < p.tokens; t += blockDim.x) {
         float c = 0.f;
         if (is_valid(b.target[t], p.vocab)) c = (b.weight ? b.weight[t] : 1.0f) / by;
         coef[t] = c;
@@ -110,9 +122,10 @@ __global__ __launch_bounds__(1024) void k_coef(CePlan p, CeBuffers b) {
         s->h_max = 0;
         s->w_max = 0;
         s->c_max = c_max;
-        s->valid = count;
     }
 }
+
+__global__ __launch_bounds__(1024) void k_coef(CePlan p, CeBuffers b) { coefficients(p, b); }
 
 template <bool F32>
 __device__ __forceinline__ f4 load4(const void* base, int64_t at, int have, bool vec) {
@@ -168,33 +181,44 @@ __global__ __launch_bounds__(256) void k_largest(CePlan p, CeBuffers b) {
 }
 
 // h (blockIdx.y = 0) and w (1) as the products take them: rows of a multiple of
-// 64 columns, zeros in the padding and in h's rows without a valid target.
-template <Form FORM>
+// 64 columns, zeros in the padding and in h's rows without a valid target.  In the
+// forms without a scale the last work-group of h computes the coefficients, for
+// nothing else waits for them here.
+template <CeForm FORM>
 __global__ __launch_bounds__(256) void k_operands(CePlan p, CeBuffers b) {
     const bool of_w = blockIdx.y != 0;
+    const int groups = static_cast<int>(gridDim.x) - (is_scaled(FORM) ? 0 : 1);
+    if (static_cast<int>(blockIdx.x) >= groups) {
+        if (!of_w) coefficients(p, b);
+        return;
+    }
     const int rows = of_w ? p.vocab : p.tokens;
     const void* src = of_w ? b.w : b.h;
     const bool vec = of_w ? b.w_vector : b.h_vector;
     const int64_t stride = of_w ? b.w_stride : b.h_stride;
     const int64_t ld = of_w ? p.ld_w : p.ld_h;
-    const int cols = static_cast<int>(FORM == kHalves ? ld / 2 : ld);
+    const int cols = static_cast<int>(ld / units(FORM));
     u16* dst = reinterpret_cast<u16*>(b.workspace + (of_w ? p.w : p.h));
     float scale = 1.f;
-    if constexpr (FORM != kBf16) {
+    if constexpr (is_scaled(FORM)) {
         const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
         scale = ldexpf(1.f, exponent_for(of_w ? s->w_max : s->h_max));
     }
-    for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4) {
+    for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += groups * 4) {
         const bool keep = of_w || is_valid(b.target[r], p.vocab);
         u16* out = dst + r * ld;
 #pragma unroll 4
         for (int c = (threadIdx.x & 63) * 4; c < cols; c += 256) {
             f4 v = {0.f, 0.f, 0.f, 0.f};
-            if (keep && c < p.dim) v = load4<FORM == kHalves>(src, r * stride + c, p.dim - c, vec);
+            if (keep && c < p.dim) v = load4<is_f32(FORM)>(src, r * stride + c, p.dim - c, vec);
+            if constexpr (FORM == kCeF32) {
+                *reinterpret_cast<f4*>(out + 2 * c) = v;
+                continue;
+            }
             u16x4 hi, lo;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                if constexpr (FORM == kBf16) {
+                if constexpr (FORM == kCeBf16) {
                     hi[q] = float_to_bf16(v[q]);
                 } else {
                     const float x = v[q] * scale;
@@ -202,7 +226,7 @@ __global__ __launch_bounds__(256) void k_operands(CePlan p, CeBuffers b) {
                     lo[q] = float_to_half(x - half_to_float(hi[q]));
                 }
             }
-            if constexpr (FORM == kHalves) {
+            if constexpr (FORM == kCeHalves) {
                 u16* at = out + ((c >> 5) << 6) + (c & 31);
                 *reinterpret_cast<u16x4*>(at) = hi;
                 *reinterpret_cast<u16x4*>(at + 32) = lo;
@@ -220,8 +244,22 @@ __device__ __forceinline__ int xcd_run(int b, int total) {
     return x * q + min(x, r) + (b >> 3);
 }
 
-template <Form FORM, int BM, tile::Kind KI, tile::Kind KJ>
-using CeTile = tile::Pick<FORM == kBf16, FORM == kHalves ? 2 : 1, BM, KI, KJ>;
+// Tiles of TM tokens: with the vocabulary (or dim) side by side 256 or 128 of it,
+// and, for products summed over the tokens, squares of 256 or 128.
+template <CeForm FORM, int TM, tile::Kind KI, tile::Kind KJ>
+struct TokenTile {
+    using T = tile::Tile<elem(FORM), TM, 128, 1, 4, KI, KJ>;
+};
+template <CeForm FORM, tile::Kind KI, tile::Kind KJ>
+struct TokenTile<FORM, 128, KI, KJ> {
+    using T = tile::Pick<elem(FORM), 128, KI, KJ>;
+};
+template <CeForm FORM, tile::Kind KI, tile::Kind KJ>
+struct TokenTile<FORM, 256, KI, KJ> {
+    using T = tile::Pick<elem(FORM), 256, KI, KJ>;
+};
+constexpr int square_of(int tm) { return tm == 256 ? 256 : 128; }
+constexpr int threads_of(int tm) { return tm == 256 ? 512 : 256; }
 
 __device__ __forceinline__ Operand h_rows(const CePlan& p, const CeBuffers& b) {
     return Operand{reinterpret_cast<const u16*>(b.workspace + p.h), p.ld_h, p.tokens,
@@ -229,16 +267,16 @@ __device__ __forceinline__ Operand h_rows(const CePlan& p, const CeBuffers& b) {
 }
 __device__ __forceinline__ Operand w_rows(const CePlan& p, const CeBuffers& b, int first) {
     const u16* w = b.w_direct ? static_cast<const u16*>(b.w) : reinterpret_cast<const u16*>(b.workspace + p.w);
-    const int64_t ld = b.w_direct ? b.w_stride : p.ld_w;
+    const int64_t ld = !b.w_direct ? p.ld_w : p.form == kCeF32 ? 2 * b.w_stride : b.w_stride;
     return Operand{w + first * ld, ld, p.vocab - first, static_cast<int32_t>(p.ld_w)};
 }
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 
 // What brings a tile's accumulators to logits in units of log2.
-template <Form FORM>
+template <CeForm FORM>
 __device__ __forceinline__ float logit_unit(const CePlan& p, const CeBuffers& b) {
-    if constexpr (FORM == kBf16) return kLog2e;
+    if constexpr (!is_scaled(FORM)) return kLog2e;
     const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
     return ldexpf(kLog2e, -(exponent_for(s->h_max) + exponent_for(s->w_max)));
 }
@@ -252,39 +290,41 @@ __device__ __forceinline__ float2 joined(float2 a, float2 c) {
 
 // First pass: each row's largest logit and sum of exp(z - largest) in a tile,
 // and the target's logit.
-template <Form FORM, int BM>
-__global__ __launch_bounds__(BM * 2) void k_stats(CePlan p, CeBuffers b) {
-    using T = CeTile<FORM, BM, kContig, kContig>;
+template <CeForm FORM, int TM>
+__global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b) {
+    using T = typename TokenTile<FORM, TM, kContig, kContig>::T;
+    constexpr int TN = T::kBN;
     __shared__ __align__(1024) char lds[T::kLdsBytes];
-    const int tiles_t = (p.tokens + BM - 1) / BM, tiles_v = (p.vocab + BM - 1) / BM;
+    const int tiles_t = (p.tokens + TM - 1) / TM, tiles_v = (p.vocab + TN - 1) / TN;
     const int id = xcd_run(blockIdx.x, tiles_t * tiles_v);
     const int tv = id / tiles_t, tt = id - tv * tiles_t;
     T t;
-    t.run(h_rows(p, b), w_rows(p, b, 0), tt * BM, tv * BM, 0, static_cast<int>(p.ld_h / (FORM == kHalves ? 2 : 1)), (DSM_LDS char*)lds);
+    t.run(h_rows(p, b), w_rows(p, b, 0), tt * TM, tv * TN, 0, static_cast<int>(p.ld_h / units(FORM)),
+          (DSM_LDS char*)lds);
     // In units of log2: z2 = acc * unit, exp(z) = exp2(z2).
     const float unit = logit_unit<FORM>(p, b);
     float* hit = reinterpret_cast<float*>(b.workspace + p.hit);
-    float2* part = reinterpret_cast<float2*>(lds);  // [T::WN][BM]
+    float2* part = reinterpret_cast<float2*>(lds);  // [T::WN][TM]
     int rel[T::FI];  // the target's column in the tile, or -1
 #pragma unroll
     for (int fi = 0; fi < T::FI; ++fi) {
-        const int token = tt * BM + t.row(fi);
+        const int token = tt * TM + t.row(fi);
         const int64_t target = b.target[min(token, p.tokens - 1)];
-        rel[fi] = token < p.tokens && is_valid(target, p.vocab) ? static_cast<int>(target) - tv * BM : -1;
+        rel[fi] = token < p.tokens && is_valid(target, p.vocab) ? static_cast<int>(target) - tv * TN : -1;
     }
-    if (tv * BM + BM > p.vocab) {  // columns past the vocabulary
+    if (tv * TN + TN > p.vocab) {  // columns past the vocabulary
 #pragma unroll
         for (int fj = 0; fj < T::FJ; ++fj)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                if (tv * BM + t.col(fj) + r >= p.vocab)
+                if (tv * TN + t.col(fj) + r >= p.vocab)
 #pragma unroll
                     for (int fi = 0; fi < T::FI; ++fi) t.acc[fi][fj][r] = -__builtin_inff();
     }
     const int first_col = t.wj * T::FJ * 16;
 #pragma unroll
     for (int fi = 0; fi < T::FI; ++fi) {
-        const int token = tt * BM + t.row(fi);
+        const int token = tt * TM + t.row(fi);
         // Few waves hold a target's column.
         if (__any(rel[fi] >= first_col && rel[fi] < first_col + T::FJ * 16)) {
 #pragma unroll
@@ -311,21 +351,22 @@ __global__ __launch_bounds__(BM * 2) void k_stats(CePlan p, CeBuffers b) {
         }
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
-        if (t.lane < 16) part[t.wj * BM + t.row(fi)] = make_float2(top, sum);
+        if (t.lane < 16) part[t.wj * TM + t.row(fi)] = make_float2(top, sum);
     }
     __syncthreads();
     float2* stats = reinterpret_cast<float2*>(b.workspace + p.stats) + static_cast<int64_t>(tv) * p.tokens;
-    for (int r = threadIdx.x; r < BM; r += T::kThreads) {
-        if (tt * BM + r >= p.tokens) break;
+    for (int r = threadIdx.x; r < TM; r += T::kThreads) {
+        if (tt * TM + r >= p.tokens) break;
         float2 a = part[r];
 #pragma unroll
-        for (int w = 1; w < T::WN; ++w) a = joined(a, part[w * BM + r]);
-        stats[tt * BM + r] = a;
+        for (int w = 1; w < T::WN; ++w) a = joined(a, part[w * TM + r]);
+        stats[tt * TM + r] = a;
     }
 }
 
 // lse and loss of 64 tokens by a work-group: a lane a token, the waves share the
 // tiles.
+// With one work-group it sums the total as well.
 __global__ __launch_bounds__(1024) void k_join(CePlan p, CeBuffers b, int tiles) {
     __shared__ float2 part[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -336,15 +377,22 @@ __global__ __launch_bounds__(1024) void k_join(CePlan p, CeBuffers b, int tiles)
     for (int v = wave; v < tiles; v += 16) a = joined(a, stats[static_cast<int64_t>(v) * p.tokens]);
     part[wave][lane] = a;
     __syncthreads();
-    if (wave != 0 || token >= p.tokens) return;
+    if (wave != 0) return;
+#pragma unroll
     for (int w = 1; w < 16; ++w) a = joined(a, part[w][lane]);
     const float lse2 = a.x + __builtin_amdgcn_logf(a.y);  // v_log_f32: log2
-    reinterpret_cast<float*>(b.workspace + p.lse)[token] = lse2;
-    if (b.lse) b.lse[token] = lse2 * kLn2;
-    float loss = 0.f;
-    if (is_valid(b.target[token], p.vocab))
-        loss = (lse2 - reinterpret_cast<const float*>(b.workspace + p.hit)[token]) * kLn2;
-    b.loss[token] = loss;
+    const bool valid = token < p.tokens && is_valid(b.target[at], p.vocab);
+    const float loss =
+        valid ? (lse2 - reinterpret_cast<const float*>(b.workspace + p.hit)[at]) * kLn2 : 0.f;
+    if (token < p.tokens) {
+        reinterpret_cast<float*>(b.workspace + p.lse)[token] = lse2;
+        if (b.lse) b.lse[token] = lse2 * kLn2;
+        b.loss[token] = loss;
+    }
+    if (gridDim.x > 1) return;
+    double sum = valid ? static_cast<double>(reinterpret_cast<const float*>(b.workspace + p.coef)[at]) * loss : 0.0;
+    for (int w = 32; w > 0; w >>= 1) sum += __shfl_xor(sum, w);
+    if (lane == 0) b.total[0] = static_cast<float>(sum);
 }
 
 // The weighted total, in a fixed order.
@@ -364,18 +412,22 @@ __global__ __launch_bounds__(1024) void k_total(CePlan p, CeBuffers b) {
 }
 
 // G of one piece of the vocabulary, [first, first + cols).
-template <Form FORM, int BM>
-__global__ __launch_bounds__(BM * 2) void k_piece(CePlan p, CeBuffers b, int first, int cols) {
-    using T = CeTile<FORM, BM, kContig, kContig>;
+template <CeForm FORM, int TM>
+__global__ __launch_bounds__(threads_of(TM)) void k_piece(CePlan p, CeBuffers b, int first, int cols) {
+    using T = typename TokenTile<FORM, TM, kContig, kContig>::T;
+    constexpr int TN = T::kBN;
     __shared__ __align__(1024) char lds[T::kLdsBytes];
     const int rows_pad = (p.tokens + 63) / 64 * 64, cols_pad = (cols + 63) / 64 * 64;
-    const int tiles_t = (p.tokens + BM - 1) / BM, tiles_v = (cols + BM - 1) / BM;
+    const int tiles_t = (rows_pad + TM - 1) / TM, tiles_v = (cols + TN - 1) / TN;
     const int id = xcd_run(blockIdx.x, tiles_t * tiles_v);
     const int tv = id / tiles_t, tt = id - tv * tiles_t;
     T t;
-    t.run(h_rows(p, b), w_rows(p, b, first), tt * BM, tv * BM, 0, static_cast<int>(p.ld_h / (FORM == kHalves ? 2 : 1)), (DSM_LDS char*)lds);
+    t.clear();
+    if (tt * TM < p.tokens)  // (else the rows are padding)
+        t.add(h_rows(p, b), w_rows(p, b, first), tt * TM, tv * TN, 0, static_cast<int>(p.ld_h / units(FORM)),
+              (DSM_LDS char*)lds);
     const float unit = logit_unit<FORM>(p, b);
-    const int eg = exponent_for(reinterpret_cast<const Scalars*>(b.workspace + p.scalars)->c_max);
+    const int eg = !is_scaled(FORM) ? 0 : exponent_for(reinterpret_cast<const Scalars*>(b.workspace + p.scalars)->c_max);
     const float* lse = reinterpret_cast<const float*>(b.workspace + p.lse);
     const float* coef = reinterpret_cast<const float*>(b.workspace + p.coef);
     u16* g = reinterpret_cast<u16*>(b.workspace + p.p);
@@ -385,18 +437,18 @@ __global__ __launch_bounds__(BM * 2) void k_piece(CePlan p, CeBuffers b, int fir
     float l[T::FI], c[T::FI];
 #pragma unroll
     for (int fi = 0; fi < T::FI; ++fi) {
-        const int token = tt * BM + t.row(fi), at = min(token, p.tokens - 1);
+        const int token = tt * TM + t.row(fi), at = min(token, p.tokens - 1);
         const int64_t target = b.target[at];
         const bool valid = token < p.tokens && is_valid(target, p.vocab);
-        rel[fi] = valid ? static_cast<int>(target) - first - tv * BM : -1;
+        rel[fi] = valid ? static_cast<int>(target) - first - tv * TN : -1;
         l[fi] = valid ? lse[at] : __builtin_inff();
         c[fi] = valid ? ldexpf(coef[at], eg) : 0.f;
     }
-    const bool ragged = tv * BM + BM > cols;
+    const bool ragged = tv * TN + TN > cols;
     const int first_col = t.wj * T::FJ * 16;
 #pragma unroll
     for (int fi = 0; fi < T::FI; ++fi) {
-        const int token = tt * BM + t.row(fi);
+        const int token = tt * TM + t.row(fi);
         // Few waves hold a target's column.
         const bool hits = __any(rel[fi] >= first_col && rel[fi] < first_col + T::FJ * 16);
         if (token >= rows_pad) continue;
@@ -412,29 +464,53 @@ __global__ __launch_bounds__(BM * 2) void k_piece(CePlan p, CeBuffers b, int fir
                 for (int r = 0; r < 8; ++r)
                     if (rel[fi] == col + r) v[r] -= 1.0f;
             }
-            u16x8 hi, lo;
+            const int at = tv * TN + col;
 #pragma unroll
             for (int r = 0; r < 8; ++r) {
                 v[r] *= c[fi];
-                if (ragged && tv * BM + col + r >= cols) v[r] = 0.f;
-                hi[r] = float_to_half(v[r]);
-                lo[r] = float_to_half(v[r] - half_to_float(hi[r]));
+                if (ragged && at + r >= cols) v[r] = 0.f;
             }
-            const int at = tv * BM + col;
             if (at >= cols_pad) continue;
-            u16* out = g + token * p.ld_p + (FORM == kHalves ? ((at >> 5) << 6) + (at & 31) : at);
-            *reinterpret_cast<u16x8*>(out) = hi;
-            if constexpr (FORM == kHalves) *reinterpret_cast<u16x8*>(out + 32) = lo;
+            if constexpr (FORM == kCeF32) {
+                float* out = reinterpret_cast<float*>(g) + token * (p.ld_p / 2) + at;
+                *reinterpret_cast<f4*>(out) = f4{v[0], v[1], v[2], v[3]};
+                *reinterpret_cast<f4*>(out + 4) = f4{v[4], v[5], v[6], v[7]};
+            } else {
+                u16x8 hi, lo;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    if constexpr (FORM == kCeBf16) {
+                        hi[r] = float_to_bf16(v[r]);
+                        lo[r] = float_to_bf16(v[r] - bf16_to_float(hi[r]));
+                    } else {
+                        hi[r] = float_to_half(v[r]);
+                        lo[r] = float_to_half(v[r] - half_to_float(hi[r]));
+                    }
+                }
+                u16* out = g + token * p.ld_p + (FORM == kCeHalves ? ((at >> 5) << 6) + (at & 31) : at);
+                *reinterpret_cast<u16x8*>(out) = hi;
+                if constexpr (FORM == kCeHalves) *reinterpret_cast<u16x8*>(out + 32) = lo;
+                if constexpr (FORM == kCeBf16) *reinterpret_cast<u16x8*>(out + p.p_lo) = lo;
+            }
         }
     }
 }
 
+// G of the piece as an operand of its products; in the bf16 form its upper halves
+// or (LO) its lower ones.
+template <bool LO = false>
+__device__ __forceinline__ Operand g_rows(const CePlan& p, const CeBuffers& b, int rows) {
+    return Operand{reinterpret_cast<const u16*>(b.workspace + p.p) + (LO ? p.p_lo : 0), p.ld_p, rows,
+                   static_cast<int32_t>(p.ld_p)};
+}
+
 // dh's sums over one piece, each of dh_splits parts into its own fp32 buffer.
-template <Form FORM, int BM>
-__global__ __launch_bounds__(BM * 2) void k_dh(CePlan p, CeBuffers b, int first, int cols) {
-    using T = CeTile<FORM, BM, kContig, kStrided>;
+template <CeForm FORM, int TM>
+__global__ __launch_bounds__(threads_of(TM)) void k_dh(CePlan p, CeBuffers b, int first, int cols) {
+    using T = typename TokenTile<FORM, TM, kContig, kStrided>::T;
+    constexpr int TN = T::kBN;
     __shared__ __align__(1024) char lds[T::kLdsBytes];
-    const int tiles_t = (p.tokens + BM - 1) / BM, tiles_d = (p.dim + BM - 1) / BM;
+    const int tiles_t = (p.tokens + TM - 1) / TM, tiles_d = (p.dim + TN - 1) / TN;
     int id = xcd_run(blockIdx.x, tiles_t * tiles_d * p.dh_splits);
     const int part = id / (tiles_t * tiles_d);
     id -= part * tiles_t * tiles_d;
@@ -443,11 +519,13 @@ __global__ __launch_bounds__(BM * 2) void k_dh(CePlan p, CeBuffers b, int first,
     const int each = (cols_pad / 64 + p.dh_splits - 1) / p.dh_splits * 64;
     const int k0 = min(part * each, cols_pad), k1 = min(k0 + each, cols_pad);
     T t;
-    const Operand g{reinterpret_cast<const u16*>(b.workspace + p.p), p.ld_p, p.tokens, 0};
-    t.run(g, w_rows(p, b, first), tt * BM, td * BM, k0, k1, (DSM_LDS char*)lds);
+    t.clear();
+    t.add(g_rows(p, b, p.tokens), w_rows(p, b, first), tt * TM, td * TN, k0, k1, (DSM_LDS char*)lds);
+    if constexpr (FORM == kCeBf16)
+        t.add(g_rows<true>(p, b, p.tokens), w_rows(p, b, first), tt * TM, td * TN, k0, k1, (DSM_LDS char*)lds);
     float* out = reinterpret_cast<float*>(b.workspace + p.dh) + part * p.tokens * p.ld_dh;
     const int ld = static_cast<int>(p.ld_dh);
-    constexpr int kBatch = 4;
+    constexpr int kBatch = T::FI < 4 ? T::FI : 4;
 #pragma unroll
     for (int f0 = 0; f0 < T::FI; f0 += kBatch) {
         f4 old[kBatch][T::FJ];
@@ -455,16 +533,16 @@ __global__ __launch_bounds__(BM * 2) void k_dh(CePlan p, CeBuffers b, int first,
         for (int fi = 0; fi < kBatch; ++fi)
 #pragma unroll
             for (int fj = 0; fj < T::FJ; ++fj) {
-                const int64_t q = static_cast<int64_t>(min(tt * BM + t.row(f0 + fi), p.tokens - 1)) * ld +
-                                  min(td * BM + t.col(fj), ld - 4);
+                const int64_t q = static_cast<int64_t>(min(tt * TM + t.row(f0 + fi), p.tokens - 1)) * ld +
+                                  min(td * TN + t.col(fj), ld - 4);
                 old[fi][fj] = first == 0 ? f4{0.f, 0.f, 0.f, 0.f} : *reinterpret_cast<const f4*>(out + q);
             }
 #pragma unroll
         for (int fi = 0; fi < kBatch; ++fi) {
-            const int token = tt * BM + t.row(f0 + fi);
+            const int token = tt * TM + t.row(f0 + fi);
 #pragma unroll
             for (int fj = 0; fj < T::FJ; ++fj) {
-                const int d = td * BM + t.col(fj);
+                const int d = td * TN + t.col(fj);
                 if (token < p.tokens && d < ld)
                     *reinterpret_cast<f4*>(out + static_cast<int64_t>(token) * ld + d) = old[fi][fj] + t.acc[f0 + fi][fj];
             }
@@ -500,10 +578,10 @@ __device__ __forceinline__ void store_grad(void* base, int64_t at, f4 v, int hav
 }
 
 // dh from its parts, which are added in order; a wave takes a row.
-template <bool F32>
+template <CeForm FORM>
 __global__ __launch_bounds__(256) void k_dh_join(CePlan p, CeBuffers b) {
     const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
-    const int ex = -(exponent_for(s->c_max) + exponent_for(s->w_max));
+    const int ex = is_scaled(FORM) ? -(exponent_for(s->c_max) + exponent_for(s->w_max)) : 0;
     const int64_t each = p.tokens * p.ld_dh;
     const int row = blockIdx.x * 4 + (threadIdx.x >> 6);
     if (row >= p.tokens) return;
@@ -513,25 +591,30 @@ __global__ __launch_bounds__(256) void k_dh_join(CePlan p, CeBuffers b) {
         for (int q = 0; q < p.dh_splits; ++q) v += *reinterpret_cast<const f4*>(parts + q * each + d);
 #pragma unroll
         for (int r = 0; r < 4; ++r) v[r] = ldexpf(v[r], ex);
-        store_grad<F32>(b.dh, row * b.dh_stride + d, v, p.dim - d, b.dh_vector);
+        store_grad<is_f32(FORM)>(b.dh, row * b.dh_stride + d, v, p.dim - d, b.dh_vector);
     }
 }
 
 // dw of one piece.
-template <Form FORM, int BM>
-__global__ __launch_bounds__(BM * 2) void k_dw(CePlan p, CeBuffers b, int first, int cols) {
-    using T = CeTile<FORM, BM, kStrided, kStrided>;
+template <CeForm FORM, int TM>
+__global__ __launch_bounds__(threads_of(TM)) void k_dw(CePlan p, CeBuffers b, int first, int cols) {
+    constexpr int BM = square_of(TM);
+    using T = tile::Pick<elem(FORM), BM, kStrided, kStrided>;
     __shared__ __align__(1024) char lds[T::kLdsBytes];
     const int tiles_v = (cols + BM - 1) / BM, tiles_d = (p.dim + BM - 1) / BM;
     const int id = xcd_run(blockIdx.x, tiles_v * tiles_d);
     const int tv = id / tiles_d, td = id - tv * tiles_d;
     const int rows_pad = (p.tokens + 63) / 64 * 64;
     T t;
-    const Operand g{reinterpret_cast<const u16*>(b.workspace + p.p), p.ld_p, rows_pad,
-                    static_cast<int32_t>(p.ld_p)};
-    t.run(g, h_rows(p, b), tv * BM, td * BM, 0, rows_pad, (DSM_LDS char*)lds);
-    const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
-    const int ex = -(exponent_for(s->c_max) + exponent_for(s->h_max));
+    t.clear();
+    t.add(g_rows(p, b, rows_pad), h_rows(p, b), tv * BM, td * BM, 0, rows_pad, (DSM_LDS char*)lds);
+    if constexpr (FORM == kCeBf16)
+        t.add(g_rows<true>(p, b, rows_pad), h_rows(p, b), tv * BM, td * BM, 0, rows_pad, (DSM_LDS char*)lds);
+    int ex = 0;
+    if constexpr (is_scaled(FORM)) {
+        const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
+        ex = -(exponent_for(s->c_max) + exponent_for(s->h_max));
+    }
 #pragma unroll
     for (int fi = 0; fi < T::FI; ++fi) {
         const int v = tv * BM + t.row(fi);
@@ -547,65 +630,73 @@ __global__ __launch_bounds__(BM * 2) void k_dw(CePlan p, CeBuffers b, int first,
                 hi[r] = ldexpf(x.v[4 + r], ex);
             }
             const int64_t at = (first + v) * b.dw_stride + d;
-            if (d < p.dim) store_grad<FORM == kHalves>(b.dw, at, lo, p.dim - d, b.dw_vector);
-            if (d + 4 < p.dim) store_grad<FORM == kHalves>(b.dw, at + 4, hi, p.dim - d - 4, b.dw_vector);
+            if (d < p.dim) store_grad<is_f32(FORM)>(b.dw, at, lo, p.dim - d, b.dw_vector);
+            if (d + 4 < p.dim) store_grad<is_f32(FORM)>(b.dw, at + 4, hi, p.dim - d - 4, b.dw_vector);
         }
     }
 }
 
-template <Form FORM, int BM>
-void losses(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
-    const int tt = (p.tokens + BM - 1) / BM, tv = (p.vocab + BM - 1) / BM;
-    k_stats<FORM, BM><<<tt * tv, BM * 2, 0, stream>>>(p, b);
-    k_join<<<(p.tokens + 63) / 64, 1024, 0, stream>>>(p, b, tv);
-    k_total<<<1, 1024, 0, stream>>>(p, b);
-}
-
-template <Form FORM, int BM>
-void gradients(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
-    const int tt = (p.tokens + BM - 1) / BM, td = (p.dim + BM - 1) / BM;
-    for (int first = 0; first < p.vocab; first += p.piece) {
-        const int cols = p.vocab - first < p.piece ? p.vocab - first : p.piece;
-        const int tp = (cols + BM - 1) / BM;
-        k_piece<FORM, BM><<<tt * tp, BM * 2, 0, stream>>>(p, b, first, cols);
-        k_dh<FORM, BM><<<tt * td * p.dh_splits, BM * 2, 0, stream>>>(p, b, first, cols);
-        k_dw<FORM, BM><<<tp * td, BM * 2, 0, stream>>>(p, b, first, cols);
-    }
-    k_dh_join<FORM == kHalves><<<(p.tokens + 3) / 4, 256, 0, stream>>>(p, b);
-}
-
-template <int BM>
+template <CeForm FORM, int TM>
 void products(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
-    if (p.f32) {
-        losses<kHalves, BM>(p, b, stream);
-        if (p.grads) gradients<kHalves, BM>(p, b, stream);
-    } else if (p.grads) {
-        losses<kHalf, BM>(p, b, stream);
-        gradients<kHalf, BM>(p, b, stream);
-    } else {
-        losses<kBf16, BM>(p, b, stream);
+    constexpr int kThreads = threads_of(TM), TN = square_of(TM);
+    const int tt = (p.tokens + TM - 1) / TM, td = (p.dim + TN - 1) / TN, tv = (p.vocab + TN - 1) / TN;
+    k_stats<FORM, TM><<<tt * tv, kThreads, 0, stream>>>(p, b);
+    k_join<<<(p.tokens + 63) / 64, 1024, 0, stream>>>(p, b, tv);
+    if (p.tokens > 64) k_total<<<1, 1024, 0, stream>>>(p, b);
+    if constexpr (FORM != kCeBf16 || TM < 256) {  // (many tokens with gradients take fp16)
+        if (!p.grads) return;
+        const int tg = ((p.tokens + 63) / 64 * 64 + TM - 1) / TM;
+        for (int first = 0; first < p.vocab; first += p.piece) {
+            const int cols = p.vocab - first < p.piece ? p.vocab - first : p.piece;
+            const int tp = (cols + TN - 1) / TN;
+            k_piece<FORM, TM><<<tg * tp, kThreads, 0, stream>>>(p, b, first, cols);
+            k_dh<FORM, TM><<<tt * td * p.dh_splits, kThreads, 0, stream>>>(p, b, first, cols);
+            k_dw<FORM, TM><<<tp * td, kThreads, 0, stream>>>(p, b, first, cols);
+        }
+        k_dh_join<FORM><<<(p.tokens + 3) / 4, 256, 0, stream>>>(p, b);
     }
 }
 
 }  // namespace
 
 hipError_t launch_linear_ce(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
-    k_coef<<<1, 1024, 0, stream>>>(p, b);
-    const int most = p.tokens > p.vocab ? p.tokens : p.vocab;
-    const unsigned rows = static_cast<unsigned>(most < 8192 ? (most + 3) / 4 : 2048);
-    if (p.f32) {
-        k_largest<true><<<dim3(rows, 2), 256, 0, stream>>>(p, b);
-        k_operands<kHalves><<<dim3(rows, 2), 256, 0, stream>>>(p, b);
-    } else if (p.grads) {
-        k_largest<false><<<dim3(rows, 2), 256, 0, stream>>>(p, b);
-        k_operands<kHalf><<<dim3(rows, 2), 256, 0, stream>>>(p, b);
-    } else {
-        k_operands<kBf16><<<dim3(rows, b.w_direct ? 1 : 2), 256, 0, stream>>>(p, b);
+    const int most = b.w_direct || p.tokens > p.vocab ? p.tokens : p.vocab;
+    const unsigned groups = static_cast<unsigned>(most < 8192 ? (most + 3) / 4 : 2048);
+    switch (p.form) {
+        case kCeBf16:
+            k_operands<kCeBf16><<<dim3(groups + 1, b.w_direct ? 1 : 2), 256, 0, stream>>>(p, b);
+            if (p.tile == 32)
+                products<kCeBf16, 32>(p, b, stream);
+            else if (p.tile == 64)
+                products<kCeBf16, 64>(p, b, stream);
+            else if (p.tile == 128)
+                products<kCeBf16, 128>(p, b, stream);
+            else
+                products<kCeBf16, 256>(p, b, stream);
+            break;
+        case kCeF32:
+            k_operands<kCeF32><<<dim3(groups + 1, b.w_direct ? 1 : 2), 256, 0, stream>>>(p, b);
+            if (p.tile == 32)
+                products<kCeF32, 32>(p, b, stream);
+            else
+                products<kCeF32, 64>(p, b, stream);
+            break;
+        case kCeHalf:
+            k_coef<<<1, 1024, 0, stream>>>(p, b);
+            k_largest<false><<<dim3(groups, 2), 256, 0, stream>>>(p, b);
+            k_operands<kCeHalf><<<dim3(groups, 2), 256, 0, stream>>>(p, b);
+            products<kCeHalf, 256>(p, b, stream);
+            break;
+        case kCeHalves:
+            k_coef<<<1, 1024, 0, stream>>>(p, b);
+            k_largest<true><<<dim3(groups, 2), 256, 0, stream>>>(p, b);
+            k_operands<kCeHalves><<<dim3(groups, 2), 256, 0, stream>>>(p, b);
+            if (p.tile == 128)
+                products<kCeHalves, 128>(p, b, stream);
+            else
+                products<kCeHalves, 256>(p, b, stream);
+            break;
     }
-    if (p.tile == 256)
-        products<256>(p, b, stream);
-    else
-        products<128>(p, b, stream);
     return hipGetLastError();
 }
 

@@ -53,17 +53,21 @@ hipError_t launch_ortho(const OrthoGroup& g, const float* coeffs, const OrthoSca
 
 // ---- Linear layer with softmax cross entropy (linear_ce.hip) ----
 
+// What the products' operands hold (linear_ce.hip).
+enum CeForm { kCeBf16, kCeHalf, kCeHalves, kCeF32 };
+
 // Where the parts of the workspace lie (bytes from its start), and how the
 // vocabulary is cut.
 struct CePlan {
     int32_t tokens, dim, vocab;
-    int32_t f32;         // fp32 buffers, else bf16
+    CeForm form;
     int32_t grads;
-    int32_t tile;        // rows and columns of a work-group's tile
+    int32_t tile;        // tokens of a work-group's tile: 32, 64, 128 or 256
     int32_t piece;       // columns of the vocabulary whose gradients are in memory at once
     int32_t dh_splits;   // parts of a piece that dh is summed over side by side
     int64_t scalars, coef, lse, hit, stats, h, w, p, dh, bytes;
     int64_t ld_h, ld_w, ld_p;  // 16-bit elements of a row
+    int64_t p_lo;              // bf16 form: from G's upper halves to its lower ones
     int64_t ld_dh;             // floats of a row of dh's sums
 };
 
@@ -80,7 +84,7 @@ struct CeBuffers {
     int64_t h_stride, w_stride, dh_stride, dw_stride;
     char* workspace;
     int32_t mean;
-    int32_t w_direct;  // bf16 w is read where it lies
+    int32_t w_direct;  // w is read where it lies
     // Rows whose elements can be moved by four.
     int32_t h_vector, w_vector, dh_vector, dw_vector;
 };

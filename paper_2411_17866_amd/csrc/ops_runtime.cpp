@@ -56,7 +56,7 @@ dsm_status check_workspace(const void* ws, int64_t bytes, int64_t need) {
 
 // G of a piece takes at most this much memory.
 constexpr int64_t kPieceBytes = int64_t(320) << 20;
-constexpr int kMaxSplits = 16;
+constexpr int kMaxSplits = 128;
 
 // How the second pass is cut: pieces of the vocabulary, and parts of a piece's
 // columns that dh is summed over side by side.  Estimated microseconds decide,
@@ -64,30 +64,34 @@ constexpr int kMaxSplits = 16;
 // a CU, one of 256), what a step of 64 columns of k costs a tile, and what adding
 // to dh's fp32 parts moves at 4 TB/s.
 void cut(dsm::CePlan* q, int64_t T, int64_t D, int64_t V) {
-    const int64_t tile = q->tile, width = q->f32 ? 2 : 1, tokens_pad = round_up(T, 64);
-    const double slots = tile == 256 ? 256 : 512, step = (tile == 256 ? 0.62 : 0.38) * (q->f32 ? 3.0 : 1.0);
-    const auto tiles = [&](int64_t n) { return (n + tile - 1) / tile; };
+    const int64_t square = q->tile == 256 ? 256 : 128, width = q->form == dsm::kCeHalf ? 1 : 2;
+    const int64_t tokens_pad = round_up(T, 64);
+    const double slots = square == 256 ? 256 : 512;
+    double step = square == 256 ? 0.62 : 0.38;
+    if (q->form != dsm::kCeHalf) step *= q->form == dsm::kCeBf16 ? 2.0 : 3.0;
+    const auto tiles = [](int64_t n, int64_t of) { return (n + of - 1) / of; };
     const auto turns = [&](int64_t n) { return std::ceil(static_cast<double>(n) / slots); };
     const double dh_pass = 4e-6 * static_cast<double>(T * D) / 4.0;  // a read or write of one part
-    const int64_t most = std::max<int64_t>(kPieceBytes / (tokens_pad * 2 * width) / tile, 1);
+    const int64_t all = tiles(V, square), t = tiles(T, q->tile), d = tiles(D, square);
+    const int64_t most = std::max<int64_t>(kPieceBytes / (tokens_pad * 2 * width) / square, 1);
+    const int64_t fewest = tiles(all, most);
     double best = 0.0;
-    for (int64_t pieces = (tiles(V) + most - 1) / most; pieces <= tiles(V); ++pieces) {
-        const int64_t per = (tiles(V) + pieces - 1) / pieces, n = (tiles(V) + per - 1) / per;
-        const double logits = turns(tiles(T) * per) * (static_cast<double>(D) / 64 * step + 5.0);
-        const double dw = turns(per * tiles(D)) * (static_cast<double>(T) / 64 * step + 5.0);
-        for (int s = 1; s <= kMaxSplits && s * 256 <= std::max<int64_t>(per * tile, 256); ++s) {
-            const double dh = turns(tiles(T) * tiles(D) * s) * (static_cast<double>(per * tile) / 64 / s * step + 5.0) +
-                              s * dh_pass * (n > 1 ? 2 : 1);
+    for (int64_t pieces = fewest; pieces <= std::min(all, fewest + 16); ++pieces) {
+        const int64_t per = tiles(all, pieces), n = tiles(all, per);
+        const double logits = turns(t * per) * (static_cast<double>(D) / 64 * step + 5.0);
+        const double dw = turns(per * d) * (static_cast<double>(T) / 64 * step + 5.0);
+        for (int s = 1; s <= kMaxSplits && (s == 1 || s * 256 <= per * square); ++s) {
+            const double steps = std::ceil(static_cast<double>(per * square) / 64 / s);
+            const double dh = turns(t * d * s) * (steps * step + 5.0) + s * dh_pass * (n > 1 ? 2 : 1);
             const double cost = static_cast<double>(n) * (logits + dw + dh + 9.0) + s * dh_pass;
             if (best == 0.0 || cost < best) {
                 best = cost;
-                q->piece = static_cast<int32_t>(per * tile);
+                q->piece = static_cast<int32_t>(per * square);
                 q->dh_splits = s;
             }
         }
-        if (pieces > 64 && best > 0.0) break;
     }
-    q->ld_p = q->piece * width;
+    q->ld_p = q->piece * (q->form == dsm::kCeHalves || q->form == dsm::kCeF32 ? 2 : 1);
 }
 
 dsm_status check_ce(const dsm_ce_problem* p) {
@@ -105,11 +109,19 @@ dsm::CePlan make_plan(const dsm_ce_problem* p) {
     q.tokens = static_cast<int32_t>(p->tokens);
     q.dim = static_cast<int32_t>(p->dim);
     q.vocab = static_cast<int32_t>(p->vocab);
-    q.f32 = p->dtype == DSM_F32;
     q.grads = p->grads;
-    const int64_t T = p->tokens, V = p->vocab, width = q.f32 ? 2 : 1;
+    const int64_t T = p->tokens, V = p->vocab;
+    // Few tokens: the passes over w that make its fp16 form would cost more than
+    // the matrix cores lose without it (at 50257 x 768, bf16: 84 us against twice
+    // the products of G; fp32: 116 us against fp32 products).
+    if (p->dtype == DSM_F32)
+        q.form = T <= (p->grads ? 64 : 256) ? dsm::kCeF32 : dsm::kCeHalves;
+    else
+        q.form = p->grads && T > 512 ? dsm::kCeHalf : dsm::kCeBf16;
+    const int64_t width = p->dtype == DSM_F32 ? 2 : 1;
     const int64_t tokens_pad = round_up(T, 64);
-    q.tile = T > 512 ? 256 : 128;
+    q.tile = T <= 32 ? 32 : T <= 64 || q.form == dsm::kCeF32 ? 64 : T <= 512 ? 128 : 256;
+    const int64_t square = q.tile == 256 ? 256 : 128;
     q.ld_h = q.ld_w = round_up(p->dim, 64) * width;
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
@@ -121,12 +133,14 @@ dsm::CePlan make_plan(const dsm_ce_problem* p) {
     q.coef = take(T * 4);
     q.lse = take(T * 4);
     q.hit = take(T * 4);
-    q.stats = take((V + q.tile - 1) / q.tile * T * 8);
+    q.stats = take((V + square - 1) / square * T * 8);
     q.h = take(T * q.ld_h * 2);
     q.w = take(V * q.ld_w * 2);
     if (p->grads && T > 0) {
         cut(&q, T, p->dim, V);
-        q.p = take(tokens_pad * q.ld_p * 2);
+        // (In the bf16 form G is two arrays of halves.)
+        q.p_lo = tokens_pad * q.ld_p;
+        q.p = take(tokens_pad * q.ld_p * (q.form == dsm::kCeBf16 ? 4 : 2));
         q.ld_dh = round_up(p->dim, 4);
         q.dh = take(q.dh_splits * T * q.ld_dh * 4);
     }
@@ -315,9 +329,10 @@ dsm_status dsm_linear_ce(const dsm_ce_problem* problem, const dsm_ce_buffers* bu
     q.dw_stride = b.dw_stride;
     q.workspace = static_cast<char*>(b.workspace);
     q.mean = mean != 0;
-    // 16-byte loads of whole 64-column steps, with 32-bit offsets inside a tile.
-    q.w_direct = p.dtype == DSM_BF16 && !p.grads && p.dim % 64 == 0 && b.w_stride % 8 == 0 && aligned(b.w, 16) &&
-                 b.w_stride < (int64_t(1) << 22);
+    // 16-byte loads of whole steps of 64 columns (fp32: 32), with 32-bit offsets
+    // inside a tile.
+    q.w_direct = (plan.form == dsm::kCeBf16 || plan.form == dsm::kCeF32) && p.dim % 64 == 0 &&
+                 b.w_stride * elem % 16 == 0 && aligned(b.w, 16) && b.w_stride < (int64_t(1) << 22);
     const size_t four = 4 * elem;
     q.h_vector = p.dim % 4 == 0 && b.h_stride % 4 == 0 && aligned(b.h, four);
     q.w_vector = p.dim % 4 == 0 && b.w_stride % 4 == 0 && aligned(b.w, four);

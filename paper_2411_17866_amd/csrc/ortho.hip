@@ -284,7 +284,7 @@ __device__ __forceinline__ u16x8 lower(const Eight& e) {
 template <int S, int BM, Product P>
 __global__ __launch_bounds__(BM * 2) void k_product(OrthoGroup g, Parts parts, int from, float mul,
                                                          float add, OrthoScales sc) {
-    using T = tile::Pick<false, S, BM, kContig, P == kGram || P == kPoly ? kContig : kStrided>;
+    using T = tile::Pick<S == 1 ? tile::kF16 : tile::kSplit, BM, kContig, P == kGram || P == kPoly ? kContig : kStrided>;
     constexpr bool kSymmetric = P == kGram || P == kPoly;
     __shared__ __align__(1024) char lds[T::kLdsBytes];
     const int m = g.m, n = g.n, mp = pad(m), np = pad(n);
