@@ -33,6 +33,8 @@
 // what its row of h holds, NaN included, reaches no output but its own zeros.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "gemm_tile.h"
 #include "ops_internal.h"
 
@@ -160,13 +162,24 @@ __global__ __launch_bounds__(256) void k_largest(CePlan p, CeBuffers b) {
     const int64_t stride = of_w ? b.w_stride : b.h_stride;
     const int rows = of_w ? p.vocab : p.tokens;
     uint32_t top = 0;
-    for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4) {
-        if (!of_w && !is_valid(b.target[r], p.vocab)) continue;
-#pragma unroll 4
-        for (int c = (threadIdx.x & 63) * 4; c < p.dim; c += 256) {
-            const f4 v = load4<F32>(src, r * stride + c, p.dim - c, vec);
+    if (of_w && vec && stride == p.dim) {  // one run of elements
+        const int64_t all = static_cast<int64_t>(rows) * p.dim / 4;
+        const int64_t step = static_cast<int64_t>(gridDim.x) * 256;
+#pragma unroll 8
+        for (int64_t e = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; e < all; e += step) {
+            const f4 v = load4<F32>(src, e * 4, 4, true);
 #pragma unroll
             for (int q = 0; q < 4; ++q) top = max(top, finite_bits(v[q]));
+        }
+    } else {
+        for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4) {
+            if (!of_w && !is_valid(b.target[r], p.vocab)) continue;
+#pragma unroll 4
+            for (int c = (threadIdx.x & 63) * 4; c < p.dim; c += 256) {
+                const f4 v = load4<F32>(src, r * stride + c, p.dim - c, vec);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) top = max(top, finite_bits(v[q]));
+            }
         }
     }
     for (int w = 32; w > 0; w >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), w)));
@@ -181,7 +194,8 @@ __global__ __launch_bounds__(256) void k_largest(CePlan p, CeBuffers b) {
 }
 
 // h (blockIdx.y = 0) and w (1) as the products take them: rows of a multiple of
-// 64 columns, zeros in the padding and in h's rows without a valid target.  In the
+// 64 columns, h with a multiple of 64 rows; zeros in the padding and in h's rows
+// without a valid target.  In the
 // forms without a scale the last work-group of h computes the coefficients, for
 // nothing else waits for them here.
 template <CeForm FORM>
@@ -192,7 +206,7 @@ __global__ __launch_bounds__(256) void k_operands(CePlan p, CeBuffers b) {
         if (!of_w) coefficients(p, b);
         return;
     }
-    const int rows = of_w ? p.vocab : p.tokens;
+    const int rows = of_w ? p.vocab : (p.tokens + 63) / 64 * 64;
     const void* src = of_w ? b.w : b.h;
     const bool vec = of_w ? b.w_vector : b.h_vector;
     const int64_t stride = of_w ? b.w_stride : b.h_stride;
@@ -205,7 +219,7 @@ __global__ __launch_bounds__(256) void k_operands(CePlan p, CeBuffers b) {
         scale = ldexpf(1.f, exponent_for(of_w ? s->w_max : s->h_max));
     }
     for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += groups * 4) {
-        const bool keep = of_w || is_valid(b.target[r], p.vocab);
+        const bool keep = of_w || (r < p.tokens && is_valid(b.target[r], p.vocab));
         u16* out = dst + r * ld;
 #pragma unroll 4
         for (int c = (threadIdx.x & 63) * 4; c < cols; c += 256) {
@@ -248,7 +262,7 @@ __device__ __forceinline__ int xcd_run(int b, int total) {
 // and, for products summed over the tokens, squares of 256 or 128.
 template <CeForm FORM, int TM, tile::Kind KI, tile::Kind KJ>
 struct TokenTile {
-    using T = tile::Tile<elem(FORM), TM, 128, 1, 4, KI, KJ>;
+    using T = tile::Tile<elem(FORM), TM, 128, 1, 4, TM == 32 ? 4 : 3, KI, KJ>;
 };
 template <CeForm FORM, tile::Kind KI, tile::Kind KJ>
 struct TokenTile<FORM, 128, KI, KJ> {
@@ -259,10 +273,10 @@ struct TokenTile<FORM, 256, KI, KJ> {
     using T = tile::Pick<elem(FORM), 256, KI, KJ>;
 };
 constexpr int square_of(int tm) { return tm == 256 ? 256 : 128; }
-constexpr int threads_of(int tm) { return tm == 256 ? 512 : 256; }
+constexpr int threads_of(int tm) { return tm >= 128 ? 512 : 256; }
 
 __device__ __forceinline__ Operand h_rows(const CePlan& p, const CeBuffers& b) {
-    return Operand{reinterpret_cast<const u16*>(b.workspace + p.h), p.ld_h, p.tokens,
+    return Operand{reinterpret_cast<const u16*>(b.workspace + p.h), p.ld_h, (p.tokens + 63) / 64 * 64,
                    static_cast<int32_t>(p.ld_h)};
 }
 __device__ __forceinline__ Operand w_rows(const CePlan& p, const CeBuffers& b, int first) {
@@ -364,22 +378,25 @@ __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b)
     }
 }
 
-// lse and loss of 64 tokens by a work-group: a lane a token, the waves share the
-// tiles.
-// With one work-group it sums the total as well.
+// lse and loss of 16 tokens by a work-group: 64 lanes share a token's tiles.  With
+// one work-group it sums the total as well.
+constexpr int kJoinTokens = 16;
 __global__ __launch_bounds__(1024) void k_join(CePlan p, CeBuffers b, int tiles) {
-    __shared__ float2 part[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int token = blockIdx.x * 64 + lane, at = min(token, p.tokens - 1);
+    __shared__ float2 part[64][kJoinTokens];
+    const int lane = threadIdx.x % kJoinTokens, share = threadIdx.x / kJoinTokens;
+    const int token = blockIdx.x * kJoinTokens + lane, at = min(token, p.tokens - 1);
     const float2* stats = reinterpret_cast<const float2*>(b.workspace + p.stats) + at;
     float2 a = make_float2(-__builtin_inff(), 0.f);
 #pragma unroll 4
-    for (int v = wave; v < tiles; v += 16) a = joined(a, stats[static_cast<int64_t>(v) * p.tokens]);
-    part[wave][lane] = a;
+    for (int v = share; v < tiles; v += 64) a = joined(a, stats[static_cast<int64_t>(v) * p.tokens]);
+    part[share][lane] = a;
     __syncthreads();
-    if (wave != 0) return;
-#pragma unroll
-    for (int w = 1; w < 16; ++w) a = joined(a, part[w][lane]);
+    for (int w = 32; w > 0; w >>= 1) {
+        if (share < w) part[share][lane] = joined(part[share][lane], part[share + w][lane]);
+        __syncthreads();
+    }
+    if (share != 0) return;
+    a = part[0][lane];
     const float lse2 = a.x + __builtin_amdgcn_logf(a.y);  // v_log_f32: log2
     const bool valid = token < p.tokens && is_valid(b.target[at], p.vocab);
     const float loss =
@@ -391,7 +408,7 @@ __global__ __launch_bounds__(1024) void k_join(CePlan p, CeBuffers b, int tiles)
     }
     if (gridDim.x > 1) return;
     double sum = valid ? static_cast<double>(reinterpret_cast<const float*>(b.workspace + p.coef)[at]) * loss : 0.0;
-    for (int w = 32; w > 0; w >>= 1) sum += __shfl_xor(sum, w);
+    for (int w = kJoinTokens / 2; w > 0; w >>= 1) sum += __shfl_xor(sum, w);
     if (lane == 0) b.total[0] = static_cast<float>(sum);
 }
 
@@ -417,15 +434,13 @@ __global__ __launch_bounds__(threads_of(TM)) void k_piece(CePlan p, CeBuffers b,
     using T = typename TokenTile<FORM, TM, kContig, kContig>::T;
     constexpr int TN = T::kBN;
     __shared__ __align__(1024) char lds[T::kLdsBytes];
-    const int rows_pad = (p.tokens + 63) / 64 * 64, cols_pad = (cols + 63) / 64 * 64;
-    const int tiles_t = (rows_pad + TM - 1) / TM, tiles_v = (cols + TN - 1) / TN;
+    const int cols_pad = (cols + 63) / 64 * 64;
+    const int tiles_t = (p.tokens + TM - 1) / TM, tiles_v = (cols + TN - 1) / TN;
     const int id = xcd_run(blockIdx.x, tiles_t * tiles_v);
     const int tv = id / tiles_t, tt = id - tv * tiles_t;
     T t;
-    t.clear();
-    if (tt * TM < p.tokens)  // (else the rows are padding)
-        t.add(h_rows(p, b), w_rows(p, b, first), tt * TM, tv * TN, 0, static_cast<int>(p.ld_h / units(FORM)),
-              (DSM_LDS char*)lds);
+    t.run(h_rows(p, b), w_rows(p, b, first), tt * TM, tv * TN, 0, static_cast<int>(p.ld_h / units(FORM)),
+          (DSM_LDS char*)lds);
     const float unit = logit_unit<FORM>(p, b);
     const int eg = !is_scaled(FORM) ? 0 : exponent_for(reinterpret_cast<const Scalars*>(b.workspace + p.scalars)->c_max);
     const float* lse = reinterpret_cast<const float*>(b.workspace + p.lse);
@@ -451,7 +466,7 @@ __global__ __launch_bounds__(threads_of(TM)) void k_piece(CePlan p, CeBuffers b,
         const int token = tt * TM + t.row(fi);
         // Few waves hold a target's column.
         const bool hits = __any(rel[fi] >= first_col && rel[fi] < first_col + T::FJ * 16);
-        if (token >= rows_pad) continue;
+        if (token >= p.tokens) continue;
 #pragma unroll
         for (int q = 0; q < T::FJ / 2; ++q) {
             const int col = t.col8(q);
@@ -497,10 +512,11 @@ __global__ __launch_bounds__(threads_of(TM)) void k_piece(CePlan p, CeBuffers b,
 }
 
 // G of the piece as an operand of its products; in the bf16 form its upper halves
-// or (LO) its lower ones.
+// or (LO) its lower ones.  (Where a product runs over the tokens, those past the
+// last one meet h's rows of zeros.)
 template <bool LO = false>
-__device__ __forceinline__ Operand g_rows(const CePlan& p, const CeBuffers& b, int rows) {
-    return Operand{reinterpret_cast<const u16*>(b.workspace + p.p) + (LO ? p.p_lo : 0), p.ld_p, rows,
+__device__ __forceinline__ Operand g_rows(const CePlan& p, const CeBuffers& b) {
+    return Operand{reinterpret_cast<const u16*>(b.workspace + p.p) + (LO ? p.p_lo : 0), p.ld_p, p.tokens,
                    static_cast<int32_t>(p.ld_p)};
 }
 
@@ -520,9 +536,9 @@ __global__ __launch_bounds__(threads_of(TM)) void k_dh(CePlan p, CeBuffers b, in
     const int k0 = min(part * each, cols_pad), k1 = min(k0 + each, cols_pad);
     T t;
     t.clear();
-    t.add(g_rows(p, b, p.tokens), w_rows(p, b, first), tt * TM, td * TN, k0, k1, (DSM_LDS char*)lds);
+    t.add(g_rows(p, b), w_rows(p, b, first), tt * TM, td * TN, k0, k1, (DSM_LDS char*)lds);
     if constexpr (FORM == kCeBf16)
-        t.add(g_rows<true>(p, b, p.tokens), w_rows(p, b, first), tt * TM, td * TN, k0, k1, (DSM_LDS char*)lds);
+        t.add(g_rows<true>(p, b), w_rows(p, b, first), tt * TM, td * TN, k0, k1, (DSM_LDS char*)lds);
     float* out = reinterpret_cast<float*>(b.workspace + p.dh) + part * p.tokens * p.ld_dh;
     const int ld = static_cast<int>(p.ld_dh);
     constexpr int kBatch = T::FI < 4 ? T::FI : 4;
@@ -577,39 +593,48 @@ __device__ __forceinline__ void store_grad(void* base, int64_t at, f4 v, int hav
     }
 }
 
-// dh from its parts, which are added in order; a wave takes a row.
+// dh from its parts: 256 columns of a row by a work-group, whose four waves add a
+// quarter of the parts each; the order is fixed.
 template <CeForm FORM>
-__global__ __launch_bounds__(256) void k_dh_join(CePlan p, CeBuffers b) {
+__global__ __launch_bounds__(256) void k_dh_join(CePlan p, CeBuffers b, int first) {
+    __shared__ f4 sums[4][64];
     const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
     const int ex = is_scaled(FORM) ? -(exponent_for(s->c_max) + exponent_for(s->w_max)) : 0;
     const int64_t each = p.tokens * p.ld_dh;
-    const int row = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= p.tokens) return;
-    const float* parts = reinterpret_cast<const float*>(b.workspace + p.dh) + row * p.ld_dh;
-    for (int d = (threadIdx.x & 63) * 4; d < p.dim; d += 256) {
-        f4 v = {0.f, 0.f, 0.f, 0.f};
-        for (int q = 0; q < p.dh_splits; ++q) v += *reinterpret_cast<const f4*>(parts + q * each + d);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = ldexpf(v[r], ex);
-        store_grad<is_f32(FORM)>(b.dh, row * b.dh_stride + d, v, p.dim - d, b.dh_vector);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int row = first + blockIdx.y, d = blockIdx.x * 256 + lane * 4;
+    const int quarter = (p.dh_splits + 3) / 4, q1 = min((wave + 1) * quarter, p.dh_splits);
+    f4 v = {0.f, 0.f, 0.f, 0.f};
+    if (d < p.dim) {
+        const float* parts = reinterpret_cast<const float*>(b.workspace + p.dh) + row * p.ld_dh + d;
+#pragma unroll 8
+        for (int q = wave * quarter; q < q1; ++q) v += *reinterpret_cast<const f4*>(parts + q * each);
     }
+    sums[wave][lane] = v;
+    __syncthreads();
+    if (wave != 0 || d >= p.dim) return;
+    v = (v + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = ldexpf(v[r], ex);
+    store_grad<is_f32(FORM)>(b.dh, row * b.dh_stride + d, v, p.dim - d, b.dh_vector);
 }
 
 // dw of one piece.
 template <CeForm FORM, int TM>
-__global__ __launch_bounds__(threads_of(TM)) void k_dw(CePlan p, CeBuffers b, int first, int cols) {
+__global__ __launch_bounds__(tile::threads_of(square_of(TM))) void k_dw(CePlan p, CeBuffers b, int first, int cols) {
     constexpr int BM = square_of(TM);
     using T = tile::Pick<elem(FORM), BM, kStrided, kStrided>;
     __shared__ __align__(1024) char lds[T::kLdsBytes];
     const int tiles_v = (cols + BM - 1) / BM, tiles_d = (p.dim + BM - 1) / BM;
     const int id = xcd_run(blockIdx.x, tiles_v * tiles_d);
     const int tv = id / tiles_d, td = id - tv * tiles_d;
-    const int rows_pad = (p.tokens + 63) / 64 * 64;
+    constexpr int kSteps = T::kSteps;
+    const int rows_pad = (p.tokens + kSteps - 1) / kSteps * kSteps;
     T t;
     t.clear();
-    t.add(g_rows(p, b, rows_pad), h_rows(p, b), tv * BM, td * BM, 0, rows_pad, (DSM_LDS char*)lds);
+    t.add(g_rows(p, b), h_rows(p, b), tv * BM, td * BM, 0, rows_pad, (DSM_LDS char*)lds);
     if constexpr (FORM == kCeBf16)
-        t.add(g_rows<true>(p, b, rows_pad), h_rows(p, b), tv * BM, td * BM, 0, rows_pad, (DSM_LDS char*)lds);
+        t.add(g_rows<true>(p, b), h_rows(p, b), tv * BM, td * BM, 0, rows_pad, (DSM_LDS char*)lds);
     int ex = 0;
     if constexpr (is_scaled(FORM)) {
         const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
@@ -641,19 +666,19 @@ void products(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
     constexpr int kThreads = threads_of(TM), TN = square_of(TM);
     const int tt = (p.tokens + TM - 1) / TM, td = (p.dim + TN - 1) / TN, tv = (p.vocab + TN - 1) / TN;
     k_stats<FORM, TM><<<tt * tv, kThreads, 0, stream>>>(p, b);
-    k_join<<<(p.tokens + 63) / 64, 1024, 0, stream>>>(p, b, tv);
-    if (p.tokens > 64) k_total<<<1, 1024, 0, stream>>>(p, b);
+    k_join<<<(p.tokens + kJoinTokens - 1) / kJoinTokens, 1024, 0, stream>>>(p, b, tv);
+    if (p.tokens > kJoinTokens) k_total<<<1, 1024, 0, stream>>>(p, b);
     if constexpr (FORM != kCeBf16 || TM < 256) {  // (many tokens with gradients take fp16)
         if (!p.grads) return;
-        const int tg = ((p.tokens + 63) / 64 * 64 + TM - 1) / TM;
         for (int first = 0; first < p.vocab; first += p.piece) {
             const int cols = p.vocab - first < p.piece ? p.vocab - first : p.piece;
             const int tp = (cols + TN - 1) / TN;
-            k_piece<FORM, TM><<<tg * tp, kThreads, 0, stream>>>(p, b, first, cols);
+            k_piece<FORM, TM><<<tt * tp, kThreads, 0, stream>>>(p, b, first, cols);
             k_dh<FORM, TM><<<tt * td * p.dh_splits, kThreads, 0, stream>>>(p, b, first, cols);
-            k_dw<FORM, TM><<<tp * td, kThreads, 0, stream>>>(p, b, first, cols);
+            k_dw<FORM, TM><<<tp * td, tile::threads_of(TN), 0, stream>>>(p, b, first, cols);
         }
-        k_dh_join<FORM><<<(p.tokens + 3) / 4, 256, 0, stream>>>(p, b);
+        for (int row = 0; row < p.tokens; row += 32768)  // (a grid dimension holds 65535)
+            k_dh_join<FORM><<<dim3((p.dim + 255) / 256, std::min(p.tokens - row, 32768)), 256, 0, stream>>>(p, b, row);
     }
 }
 

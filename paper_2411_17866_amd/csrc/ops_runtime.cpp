@@ -65,7 +65,6 @@ constexpr int kMaxSplits = 128;
 // to dh's fp32 parts moves at 4 TB/s.
 void cut(dsm::CePlan* q, int64_t T, int64_t D, int64_t V) {
     const int64_t square = q->tile == 256 ? 256 : 128, width = q->form == dsm::kCeHalf ? 1 : 2;
-    const int64_t tokens_pad = round_up(T, 64);
     const double slots = square == 256 ? 256 : 512;
     double step = square == 256 ? 0.62 : 0.38;
     if (q->form != dsm::kCeHalf) step *= q->form == dsm::kCeBf16 ? 2.0 : 3.0;
@@ -73,7 +72,7 @@ void cut(dsm::CePlan* q, int64_t T, int64_t D, int64_t V) {
     const auto turns = [&](int64_t n) { return std::ceil(static_cast<double>(n) / slots); };
     const double dh_pass = 4e-6 * static_cast<double>(T * D) / 4.0;  // a read or write of one part
     const int64_t all = tiles(V, square), t = tiles(T, q->tile), d = tiles(D, square);
-    const int64_t most = std::max<int64_t>(kPieceBytes / (tokens_pad * 2 * width) / square, 1);
+    const int64_t most = std::max<int64_t>(kPieceBytes / (T * 2 * width) / square, 1);
     const int64_t fewest = tiles(all, most);
     double best = 0.0;
     for (int64_t pieces = fewest; pieces <= std::min(all, fewest + 16); ++pieces) {
@@ -134,13 +133,13 @@ dsm::CePlan make_plan(const dsm_ce_problem* p) {
     q.lse = take(T * 4);
     q.hit = take(T * 4);
     q.stats = take((V + square - 1) / square * T * 8);
-    q.h = take(T * q.ld_h * 2);
+    q.h = take(tokens_pad * q.ld_h * 2);
     q.w = take(V * q.ld_w * 2);
     if (p->grads && T > 0) {
         cut(&q, T, p->dim, V);
         // (In the bf16 form G is two arrays of halves.)
-        q.p_lo = tokens_pad * q.ld_p;
-        q.p = take(tokens_pad * q.ld_p * (q.form == dsm::kCeBf16 ? 4 : 2));
+        q.p_lo = T * q.ld_p;
+        q.p = take(T * q.ld_p * (q.form == dsm::kCeBf16 ? 4 : 2));
         q.ld_dh = round_up(p->dim, 4);
         q.dh = take(q.dh_splits * T * q.ld_dh * 4);
     }

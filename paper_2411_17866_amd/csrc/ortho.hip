@@ -282,8 +282,8 @@ __device__ __forceinline__ u16x8 lower(const Eight& e) {
 }
 
 template <int S, int BM, Product P>
-__global__ __launch_bounds__(BM * 2) void k_product(OrthoGroup g, Parts parts, int from, float mul,
-                                                         float add, OrthoScales sc) {
+__global__ __launch_bounds__(tile::threads_of(BM)) void k_product(OrthoGroup g, Parts parts, int from, float mul,
+                                                                    float add) {
     using T = tile::Pick<S == 1 ? tile::kF16 : tile::kSplit, BM, kContig, P == kGram || P == kPoly ? kContig : kStrided>;
     constexpr bool kSymmetric = P == kGram || P == kPoly;
     __shared__ __align__(1024) char lds[T::kLdsBytes];
@@ -315,7 +315,7 @@ __global__ __launch_bounds__(BM * 2) void k_product(OrthoGroup g, Parts parts, i
     // the stored A or X to the stored result.  What a batch of fragments needs of
     // them is loaded before the batch's first store, which the compiler must
     // assume to overlap it: one wait a batch, not one a fragment.
-    constexpr int kBatch = 4, kPairs = T::FJ / 2;
+    constexpr int kBatch = T::FI < 4 ? T::FI : 4, kPairs = T::FJ / 2;
     const int64_t lo_at = S == 2 ? 32 : parts.lo / 2;  // of an X
     const u16* old = P == kPoly ? A : X;
     const int64_t ld_old = P == kPoly ? lda : ldx, old_lo = P == kPoly ? 32 : lo_at;
@@ -436,7 +436,7 @@ __global__ __launch_bounds__(BM * 2) void k_product(OrthoGroup g, Parts parts, i
                 }
             __syncthreads();
             // 16 rows of the mirror image by 32 of its columns for each wave and turn.
-            for (int c = t.wave; c < BM / 16 * (BM / 32); c += BM * 2 / 64) {
+            for (int c = t.wave; c < BM / 16 * (BM / 32); c += tile::threads_of(BM) / 64) {
                 const int j0 = c / (BM / 32) * 16, i0 = c % (BM / 32) * 32;
                 const int j = tj * BM + j0 + (t.lane & 15), i = ti * BM + i0 + (t.lane >> 4) * 8;
                 const tile::short8v v = Turn::get(turned, i0, j0, t.lane);
@@ -450,24 +450,53 @@ __global__ __launch_bounds__(BM * 2) void k_product(OrthoGroup g, Parts parts, i
 
 float pow2(int e) { return __builtin_ldexpf(1.0f, e); }
 
-template <int S, int BM>
+// Work-groups of a product by tiles of bm.
+unsigned groups_of(const OrthoGroup& g, int bm, bool symmetric) {
+    const unsigned ti = (g.m + bm - 1) / bm, tj = (g.n + bm - 1) / bm;
+    return (symmetric ? ti * (ti + 1) / 2 : ti * tj) * g.count;
+}
+
+// The tile a product takes: the one whose turns over the CUs take least.  A CU
+// holds one work-group of 256, two of 128 or of 64; a turn of 128 takes 0.62, of 64
+// 0.40 (0.28 where a CU has one of them) of what a turn of 256 does, measured over
+// batches from 1 x 64 x 64 to 8 x 1600 x 6400.  One 512 x 1536 fp32 matrix: A in
+// 18 us by 36 tiles of 64, 41 us by 10 of 128; twelve of 768 x 2304: 68, 63 and
+// 124 us by 936, 252 and 72 tiles of 64, 128 and 256.
+int tile_of(const OrthoGroup& g, bool symmetric) {
+    const auto turns = [](unsigned groups, unsigned slots) { return (groups + slots - 1) / slots; };
+    const unsigned small = groups_of(g, 64, symmetric);
+    const float t64 = small <= 256 ? 0.28f : 0.40f * turns(small, 512);
+    const float t128 = 0.62f * turns(groups_of(g, 128, symmetric), 512);
+    const float t256 = 1.0f * turns(groups_of(g, 256, symmetric), 256);
+    return t64 <= t128 && t64 <= t256 ? 64 : t128 <= t256 ? 128 : 256;
+}
+
+template <int S, Product P>
+void product(const OrthoGroup& g, const Parts& parts, int from, float mul, float add, hipStream_t stream) {
+    constexpr bool kSymmetric = P == kGram || P == kPoly;
+    const int bm = tile_of(g, kSymmetric);
+    const unsigned groups = groups_of(g, bm, kSymmetric);
+    if (bm == 64)
+        k_product<S, 64, P><<<groups, tile::threads_of(64), 0, stream>>>(g, parts, from, mul, add);
+    else if (bm == 128)
+        k_product<S, 128, P><<<groups, tile::threads_of(128), 0, stream>>>(g, parts, from, mul, add);
+    else
+        k_product<S, 256, P><<<groups, tile::threads_of(256), 0, stream>>>(g, parts, from, mul, add);
+}
+
+template <int S>
 void iterate(const OrthoGroup& g, const Parts& parts, const float* coeffs, const OrthoScales* scales,
              int steps, hipStream_t stream) {
-    const int ti = (g.m + BM - 1) / BM, tj = (g.n + BM - 1) / BM;
-    const unsigned sym = static_cast<unsigned>(ti * (ti + 1) / 2) * g.count;
-    const unsigned full = static_cast<unsigned>(ti) * tj * g.count;
-    constexpr int kThreads = BM * 2;
     for (int s = 0; s < steps; ++s) {
         const OrthoScales sc = scales[s];
         const float a = coeffs[3 * s], b = coeffs[3 * s + 1], c = coeffs[3 * s + 2];
-        k_product<S, BM, kGram><<<sym, kThreads, 0, stream>>>(g, parts, s & 1, pow2(sc.a - 2 * sc.x), 0.f, sc);
-        k_product<S, BM, kPoly><<<sym, kThreads, 0, stream>>>(
-            g, parts, s & 1, c * pow2(sc.b - 2 * sc.a), b * pow2(sc.b - sc.a), sc);
+        product<S, kGram>(g, parts, s & 1, pow2(sc.a - 2 * sc.x), 0.f, stream);
+        product<S, kPoly>(g, parts, s & 1, c * pow2(sc.b - 2 * sc.a), b * pow2(sc.b - sc.a), stream);
         const float mul = pow2(sc.x_next - sc.b - sc.x), add = a * pow2(sc.x_next - sc.x);
         if (s + 1 < steps)
-            k_product<S, BM, kUpdate><<<full, kThreads, 0, stream>>>(g, parts, s & 1, mul, add, sc);
+            product<S, kUpdate>(g, parts, s & 1, mul, add, stream);
         else
-            k_product<S, BM, kLast><<<full, kThreads, 0, stream>>>(g, parts, s & 1, mul, add, sc);
+            product<S, kLast>(g, parts, s & 1, mul, add, stream);
     }
 }
 
@@ -496,18 +525,10 @@ hipError_t launch_ortho(const OrthoGroup& g, const float* coeffs, const OrthoSca
         start<2, true, false>(g, parts, scales[0].x, stream);
     else
         start<2, false, false>(g, parts, scales[0].x, stream);
-    const int64_t big = static_cast<int64_t>((g.m + 255) / 256) * ((g.n + 255) / 256) * g.count;
-    if (big >= 256) {
-        if (g.split)
-            iterate<2, 256>(g, parts, coeffs, scales, steps, stream);
-        else
-            iterate<1, 256>(g, parts, coeffs, scales, steps, stream);
-    } else {
-        if (g.split)
-            iterate<2, 128>(g, parts, coeffs, scales, steps, stream);
-        else
-            iterate<1, 128>(g, parts, coeffs, scales, steps, stream);
-    }
+    if (g.split)
+        iterate<2>(g, parts, coeffs, scales, steps, stream);
+    else
+        iterate<1>(g, parts, coeffs, scales, steps, stream);
     return hipGetLastError();
 }
 
