@@ -101,7 +101,7 @@ struct Side {
     static_assert(kStageBytes % (1024 * NW) == 0, "whole pieces for each wave");
     // k-strided: bytes of one k row of the tile.
     static constexpr int kRowBytes = R * 2 * S;
-    static_assert(kRowBytes <= 1024 && 1024 % kRowBytes == 0, "whole rows in a piece");
+    static_assert(KIND == kContig || (kRowBytes <= 1024 && 1024 % kRowBytes == 0), "whole rows in a piece");
 
     const char* base;        // of the tile at k = 0 (uniform)
     int64_t ld_bytes;
@@ -615,7 +615,7 @@ struct Picked {
 };
 template <Elem E, Kind KI, Kind KJ>
 struct Picked<E, 64, KI, KJ> {
-    using T = Tile<E, 64, 64, 2, 2, 4, KI, KJ>;
+    using T = Tile<E, 64, 64, 4, 2, 4, KI, KJ>;
 };
 template <Elem E, Kind KI, Kind KJ>
 struct Picked<E, 256, KI, KJ> {
@@ -625,7 +625,7 @@ struct Picked<E, 256, KI, KJ> {
 // LDS while the other multiplies where a CU has one work-group: 8-16% less time
 // than four waves there with split operands, 2-4% with fp16, and no more where two
 // work-groups share a CU.
-constexpr int threads_of(int bm) { return bm >= 128 ? 512 : 256; }
+constexpr int threads_of(int) { return 512; }
 template <Elem E, int BM, Kind KI, Kind KJ>
 using Pick = typename Picked<E, BM, KI, KJ>::T;
 
