@@ -522,12 +522,11 @@ __device__ __forceinline__ Operand g_rows(const CePlan& p, const CeBuffers& b) {
 
 // dh's sums over one piece, each of dh_splits parts into its own fp32 buffer.
 template <CeForm FORM, int TM>
-__global__ __launch_bounds__(threads_of(TM)) void k_dh(CePlan p, CeBuffers b, int first, int cols) {
+__device__ __forceinline__ void dh_tile(const CePlan& p, const CeBuffers& b, int first, int cols, int id,
+                                        DSM_LDS char* lds) {
     using T = typename TokenTile<FORM, TM, kContig, kStrided>::T;
     constexpr int TN = T::kBN;
-    __shared__ __align__(1024) char lds[T::kLdsBytes];
     const int tiles_t = (p.tokens + TM - 1) / TM, tiles_d = (p.dim + TN - 1) / TN;
-    int id = xcd_run(blockIdx.x, tiles_t * tiles_d * p.dh_splits);
     const int part = id / (tiles_t * tiles_d);
     id -= part * tiles_t * tiles_d;
     const int tt = id / tiles_d, td = id - tt * tiles_d;
@@ -536,9 +535,9 @@ __global__ __launch_bounds__(threads_of(TM)) void k_dh(CePlan p, CeBuffers b, in
     const int k0 = min(part * each, cols_pad), k1 = min(k0 + each, cols_pad);
     T t;
     t.clear();
-    t.add(g_rows(p, b), w_rows(p, b, first), tt * TM, td * TN, k0, k1, (DSM_LDS char*)lds);
+    t.add(g_rows(p, b), w_rows(p, b, first), tt * TM, td * TN, k0, k1, lds);
     if constexpr (FORM == kCeBf16)
-        t.add(g_rows<true>(p, b), w_rows(p, b, first), tt * TM, td * TN, k0, k1, (DSM_LDS char*)lds);
+        t.add(g_rows<true>(p, b), w_rows(p, b, first), tt * TM, td * TN, k0, k1, lds);
     float* out = reinterpret_cast<float*>(b.workspace + p.dh) + part * p.tokens * p.ld_dh;
     const int ld = static_cast<int>(p.ld_dh);
     constexpr int kBatch = T::FI < 4 ? T::FI : 4;
@@ -621,20 +620,22 @@ __global__ __launch_bounds__(256) void k_dh_join(CePlan p, CeBuffers b, int firs
 
 // dw of one piece.
 template <CeForm FORM, int TM>
-__global__ __launch_bounds__(tile::threads_of(square_of(TM))) void k_dw(CePlan p, CeBuffers b, int first, int cols) {
+using DwTile = tile::Pick<elem(FORM), square_of(TM), kStrided, kStrided>;
+
+template <CeForm FORM, int TM>
+__device__ __forceinline__ void dw_tile(const CePlan& p, const CeBuffers& b, int first, int cols, int id,
+                                        DSM_LDS char* lds) {
     constexpr int BM = square_of(TM);
-    using T = tile::Pick<elem(FORM), BM, kStrided, kStrided>;
-    __shared__ __align__(1024) char lds[T::kLdsBytes];
-    const int tiles_v = (cols + BM - 1) / BM, tiles_d = (p.dim + BM - 1) / BM;
-    const int id = xcd_run(blockIdx.x, tiles_v * tiles_d);
+    using T = DwTile<FORM, TM>;
+    const int tiles_d = (p.dim + BM - 1) / BM;
     const int tv = id / tiles_d, td = id - tv * tiles_d;
     constexpr int kSteps = T::kSteps;
     const int rows_pad = (p.tokens + kSteps - 1) / kSteps * kSteps;
     T t;
     t.clear();
-    t.add(g_rows(p, b), h_rows(p, b), tv * BM, td * BM, 0, rows_pad, (DSM_LDS char*)lds);
+    t.add(g_rows(p, b), h_rows(p, b), tv * BM, td * BM, 0, rows_pad, lds);
     if constexpr (FORM == kCeBf16)
-        t.add(g_rows<true>(p, b), h_rows(p, b), tv * BM, td * BM, 0, rows_pad, (DSM_LDS char*)lds);
+        t.add(g_rows<true>(p, b), h_rows(p, b), tv * BM, td * BM, 0, rows_pad, lds);
     int ex = 0;
     if constexpr (is_scaled(FORM)) {
         const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
@@ -661,6 +662,40 @@ __global__ __launch_bounds__(tile::threads_of(square_of(TM))) void k_dw(CePlan p
     }
 }
 
+// The two products of G in one launch: neither fills the CUs' last turn by itself,
+// and their tiles take different times.  Each XCD has its run of dh's tiles, the
+// longer ones, then its run of dw's.
+constexpr int kXcds = 8;
+__host__ __device__ inline int per_xcd(int tiles) { return (tiles + kXcds - 1) / kXcds; }
+
+template <CeForm FORM, int TM>
+__global__ __launch_bounds__(threads_of(TM)) void k_gradients(CePlan p, CeBuffers b, int first, int cols,
+                                                              int dh_tiles, int dw_tiles) {
+    using TD = typename TokenTile<FORM, TM, kContig, kStrided>::T;
+    constexpr int kLds = TD::kLdsBytes > DwTile<FORM, TM>::kLdsBytes ? TD::kLdsBytes : DwTile<FORM, TM>::kLdsBytes;
+    __shared__ __align__(1024) char lds[kLds];
+    const int x = blockIdx.x % kXcds, at = blockIdx.x / kXcds, front = per_xcd(dh_tiles);
+    if (at < front) {
+        const int id = x * front + at;
+        if (id < dh_tiles) dh_tile<FORM, TM>(p, b, first, cols, id, (DSM_LDS char*)lds);
+    } else {
+        const int id = x * per_xcd(dw_tiles) + at - front;
+        if (id < dw_tiles) dw_tile<FORM, TM>(p, b, first, cols, id, (DSM_LDS char*)lds);
+    }
+}
+
+// Few tokens: one by one, their tiles being of different shapes.
+template <CeForm FORM, int TM>
+__global__ __launch_bounds__(threads_of(TM)) void k_dh(CePlan p, CeBuffers b, int first, int cols) {
+    __shared__ __align__(1024) char lds[TokenTile<FORM, TM, kContig, kStrided>::T::kLdsBytes];
+    dh_tile<FORM, TM>(p, b, first, cols, xcd_run(blockIdx.x, gridDim.x), (DSM_LDS char*)lds);
+}
+template <CeForm FORM, int TM>
+__global__ __launch_bounds__(tile::threads_of(square_of(TM))) void k_dw(CePlan p, CeBuffers b, int first, int cols) {
+    __shared__ __align__(1024) char lds[DwTile<FORM, TM>::kLdsBytes];
+    dw_tile<FORM, TM>(p, b, first, cols, xcd_run(blockIdx.x, gridDim.x), (DSM_LDS char*)lds);
+}
+
 template <CeForm FORM, int TM>
 void products(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
     constexpr int kThreads = threads_of(TM), TN = square_of(TM);
@@ -674,8 +709,14 @@ void products(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
             const int cols = p.vocab - first < p.piece ? p.vocab - first : p.piece;
             const int tp = (cols + TN - 1) / TN;
             k_piece<FORM, TM><<<tt * tp, kThreads, 0, stream>>>(p, b, first, cols);
-            k_dh<FORM, TM><<<tt * td * p.dh_splits, kThreads, 0, stream>>>(p, b, first, cols);
-            k_dw<FORM, TM><<<tp * td, tile::threads_of(TN), 0, stream>>>(p, b, first, cols);
+            const int dh_tiles = tt * td * p.dh_splits, dw_tiles = tp * td;
+            if constexpr (TM >= 128) {
+                k_gradients<FORM, TM><<<kXcds * (per_xcd(dh_tiles) + per_xcd(dw_tiles)), kThreads, 0, stream>>>(
+                    p, b, first, cols, dh_tiles, dw_tiles);
+            } else {
+                k_dh<FORM, TM><<<dh_tiles, kThreads, 0, stream>>>(p, b, first, cols);
+                k_dw<FORM, TM><<<dw_tiles, tile::threads_of(TN), 0, stream>>>(p, b, first, cols);
+            }
         }
         for (int row = 0; row < p.tokens; row += 32768)  // (a grid dimension holds 65535)
             k_dh_join<FORM><<<dim3((p.dim + 255) / 256, std::min(p.tokens - row, 32768)), 256, 0, stream>>>(p, b, row);

@@ -55,7 +55,7 @@ dsm_status check_workspace(const void* ws, int64_t bytes, int64_t need) {
 // ---- Linear layer with softmax cross entropy ----
 
 // G of a piece takes at most this much memory.
-constexpr int64_t kPieceBytes = int64_t(320) << 20;
+constexpr int64_t kPieceBytes = int64_t(512) << 20;
 constexpr int kMaxSplits = 128;
 
 // How the second pass is cut: pieces of the vocabulary, and parts of a piece's
@@ -78,11 +78,15 @@ void cut(dsm::CePlan* q, int64_t T, int64_t D, int64_t V) {
     for (int64_t pieces = fewest; pieces <= std::min(all, fewest + 16); ++pieces) {
         const int64_t per = tiles(all, pieces), n = tiles(all, per);
         const double logits = turns(t * per) * (static_cast<double>(D) / 64 * step + 5.0);
-        const double dw = turns(per * d) * (static_cast<double>(T) / 64 * step + 5.0);
+        // dh and dw run side by side: the work over the CUs, and half a tile of the
+        // longer kind for the uneven end.
+        const double dw_tile = std::ceil(static_cast<double>(T) / 64) * step + 5.0;
         for (int s = 1; s <= kMaxSplits && (s == 1 || s * 256 <= per * square); ++s) {
-            const double steps = std::ceil(static_cast<double>(per * square) / 64 / s);
-            const double dh = turns(t * d * s) * (steps * step + 5.0) + s * dh_pass * (n > 1 ? 2 : 1);
-            const double cost = static_cast<double>(n) * (logits + dw + dh + 9.0) + s * dh_pass;
+            const double dh_tile = std::ceil(static_cast<double>(per * square) / 64 / s) * step + 5.0;
+            const double work = (static_cast<double>(t * d * s) * dh_tile + static_cast<double>(per * d) * dw_tile) / slots;
+            const double both = std::max(work, std::max(dh_tile, dw_tile)) + 0.5 * std::max(dh_tile, dw_tile) +
+                                s * dh_pass * (n > 1 ? 2 : 1);
+            const double cost = static_cast<double>(n) * (logits + both + 6.0) + s * dh_pass;
             if (best == 0.0 || cost < best) {
                 best = cost;
                 q->piece = static_cast<int32_t>(per * square);
