@@ -432,15 +432,23 @@ struct HalfSide {
 // barrier (waves 4-7 run one turn behind).  A stage of k has two such turns, one
 // for each half of the wave's rows:
 //
-//   turn  reads       multiplies      starts the loads of
-//   0     I0 J0 J1    I0 (J0 J1)      I1 one stage on
-//   1     I1          I1 (J0 J1)      I0 J0 J1 two stages on
+//   turn  reads          multiplies      starts the loads of
+//   0     I0 J1          I0 (J0 J1)      I1 one stage on, J0 two
+//   1     I1, next J0    I1 (J0 J1)      I0 J1 two stages on
 //
-// A turn's reads are waited for before the barrier that ends it, so the next
-// turn's loads may overwrite what was read, by the waves that run behind too.
-// Each load has two turns or more to arrive: before the barrier a wave waits
-// until at most 8 of its loads are in flight, which is all but those that the
-// next turn's reads need.
+// so that both turns read as much, about what LDS gives while the other wave
+// multiplies.  (Split operands multiply half as long again and need the registers:
+// there J0 is read in turn 0 of its own stage, and loaded in turn 1.)  A turn's
+// reads are waited for before the barrier that ends it, so the next turn's loads may
+// overwrite what was read, by the waves that run behind too.  Each load has two
+// turns or more to arrive: before the barrier a wave waits until at most 8 of its
+// loads are in flight, which is all but those that the next turn's reads need.
+//
+// 8192 x 8192 x 4096, bf16: 1260 TFLOP/s with both operands k-contiguous, 1150 with
+// one k-strided (1070 with J0 read in its own stage), 1060 with both; split operands
+// 1440-1500 TFLOP/s of matrix instructions.  What bounds it is the board's power:
+// the clock falls to 1.6-1.8 GHz, at which split operands keep the matrix cores
+// 90% busy and fp16 72%; the k-strided reads take the rest.
 template <Elem E, Kind KI, Kind KJ>
 struct BigTile {
     static_assert(E != kF32, "fp32 products are for tiles that wait for memory");
@@ -451,12 +459,13 @@ struct BigTile {
     using SideJ = HalfSide<32, KJ, S>;
     static constexpr int kSteps = SideI::kSteps;
     static constexpr int kHalf = SideI::kBytes;
+    static constexpr bool kAhead = S == 1;  // J0 is read a turn before its stage
     static constexpr int kStageBytes = 4 * kHalf;  // J0, I0, J1, I1
     static constexpr int kLdsBytes = 2 * kStageBytes;
 
     f4 acc[FI][FJ];
     int lane, wave, wi, wj;
-    short8v fi[4][2], fj[4][2];
+    short8v fi[4][2], j0[kAhead ? 2 : 1][2][2], j1[2][2];  // j0: this stage's and the next one's
 
     static __device__ __forceinline__ void fence() {
         __builtin_amdgcn_sched_barrier(0);
@@ -480,15 +489,14 @@ struct BigTile {
 #pragma unroll
             for (int f = 0; f < 4; ++f) fi[f][part] = SideI::fragment(half, wi * 4 + f, part, lane);
     }
-    template <int H>
-    __device__ __forceinline__ void read_j(const DSM_LDS char* half) {
+    __device__ __forceinline__ void read_j(const DSM_LDS char* half, short8v (&to)[2][2]) {
 #pragma unroll
         for (int part = 0; part < 2; ++part)
 #pragma unroll
-            for (int f = 0; f < 2; ++f) fj[H * 2 + f][part] = SideJ::fragment(half, wj * 2 + f, part, lane);
+            for (int f = 0; f < 2; ++f) to[f][part] = SideJ::fragment(half, wj * 2 + f, part, lane);
     }
     template <int H>
-    __device__ __forceinline__ void multiply() {
+    __device__ __forceinline__ void multiply(const short8v (&front)[2][2]) {
         fence();
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -498,7 +506,8 @@ struct BigTile {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[H * 4 + i][j] = mfma<E>(fj[j][pj], fi[i][pi], acc[H * 4 + i][j]);
+                for (int j = 0; j < 4; ++j)
+                    acc[H * 4 + i][j] = mfma<E>(j < 2 ? front[j][pj] : j1[j - 2][pj], fi[i][pi], acc[H * 4 + i][j]);
         }
         __builtin_amdgcn_s_setprio(0);
         fence();
@@ -514,27 +523,35 @@ struct BigTile {
 #pragma unroll
             for (int j = 0; j < FJ; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
     }
-    __device__ __forceinline__ void run(const Operand& oi, const Operand& oj, int64_t i0, int64_t j0,
+    __device__ __forceinline__ void run(const Operand& oi, const Operand& oj, int64_t first_i, int64_t first_j,
                                         int k_begin, int k_end, DSM_LDS char* lds) {
         clear();
-        add(oi, oj, i0, j0, k_begin, k_end, lds);
+        add(oi, oj, first_i, first_j, k_begin, k_end, lds);
     }
-    __device__ __forceinline__ void add(const Operand& oi, const Operand& oj, int64_t i0, int64_t j0,
+    __device__ __forceinline__ void add(const Operand& oi, const Operand& oj, int64_t first_i, int64_t first_j,
                                         int k_begin, int k_end, DSM_LDS char* lds) {
         if (k_begin >= k_end) return;
         SideI si;
         SideJ sj;
-        si.init(oi, i0, lane, wave);
-        sj.init(oj, j0, lane, wave);
-        load_front(si, sj, k_begin, lds);
+        si.init(oi, first_i, lane, wave);
+        sj.init(oj, first_j, lane, wave);
+        const bool second = k_begin + kSteps < k_end;
+        sj.template issue<0>(k_begin, lds, lane, wave);
+        load_middle(si, sj, k_begin, lds);
         si.template issue<1>(k_begin, lds + 3 * kHalf, lane, wave);
-        if (k_begin + kSteps < k_end) {
-            load_front(si, sj, k_begin + kSteps, lds + kStageBytes);
-            wait<8>();  // the front of the first stage is there
+        if (second) {
+            sj.template issue<0>(k_begin + kSteps, lds + kStageBytes, lane, wave);
+            load_middle(si, sj, k_begin + kSteps, lds + kStageBytes);
+            wait<8>();  // all of the first stage but I1 is there
         } else {
             wait<0>();
         }
         turn_over();
+        if constexpr (kAhead) {
+            read_j(lds, j0[0]);
+            wait<8>();
+            turn_over();  // J0 is read: its next load may start
+        }
         if (wave >= 4) turn_over();
         for (int k = k_begin;;) {
             stage<0>(si, sj, k, k_end, lds);
@@ -545,8 +562,7 @@ struct BigTile {
         if (wave < 4) turn_over();
         turn_over();  // every wave is done with LDS
     }
-    __device__ __forceinline__ void load_front(SideI& si, SideJ& sj, int k, DSM_LDS char* st) {
-        sj.template issue<0>(k, st, lane, wave);
+    __device__ __forceinline__ void load_middle(SideI& si, SideJ& sj, int k, DSM_LDS char* st) {
         si.template issue<0>(k, st + kHalf, lane, wave);
         sj.template issue<1>(k, st + 2 * kHalf, lane, wave);
     }
@@ -554,28 +570,35 @@ struct BigTile {
     template <int B>
     __device__ __forceinline__ void stage(SideI& si, SideJ& sj, int k, int k_end, DSM_LDS char* lds) {
         DSM_LDS char* st = lds + B * kStageBytes;
+        DSM_LDS char* other = lds + (B ^ 1) * kStageBytes;
         const bool next = k + kSteps < k_end, more = k + 2 * kSteps < k_end;
-        read_j<0>(st);
+        constexpr int kNow = kAhead ? B : 0;
+        if constexpr (!kAhead) read_j(st, j0[0]);
         read_i(st + kHalf);
-        read_j<1>(st + 2 * kHalf);
-        if (next) {
-            si.template issue<1>(k + kSteps, lds + (B ^ 1) * kStageBytes + 3 * kHalf, lane, wave);
+        read_j(st + 2 * kHalf, j1);
+        if (next) si.template issue<1>(k + kSteps, other + 3 * kHalf, lane, wave);
+        if (kAhead ? more : next) {
+            if constexpr (kAhead) sj.template issue<0>(k + 2 * kSteps, st, lane, wave);
             wait<8>();
         } else {
             wait<0>();
         }
         turn_over();
-        multiply<0>();
+        multiply<0>(j0[kNow]);
         turn_over();
         read_i(st + 3 * kHalf);
+        if constexpr (kAhead) {
+            if (next) read_j(other, j0[B ^ 1]);
+        }
         if (more) {
-            load_front(si, sj, k + 2 * kSteps, st);
+            if constexpr (!kAhead) sj.template issue<0>(k + 2 * kSteps, st, lane, wave);
+            load_middle(si, sj, k + 2 * kSteps, st);
             wait<8>();
         } else {
             wait<0>();
         }
         turn_over();
-        multiply<1>();
+        multiply<1>(j0[kNow]);
         turn_over();
     }
 
