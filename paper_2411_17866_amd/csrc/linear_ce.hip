@@ -302,6 +302,18 @@ __device__ __forceinline__ float2 joined(float2 a, float2 c) {
     return make_float2(top, a.y * __builtin_amdgcn_exp2f(a.x - top) + c.y * __builtin_amdgcn_exp2f(c.x - top));
 }
 
+// The logits' tiles in order: eight rows of tokens side by side, along the
+// vocabulary, so that the 32 tiles that an XCD has at once share 8 tiles of h and 4
+// of w.  (With every token's tile in turn, 8192 tokens, h went through each L2
+// again for every tile of w: 2.6 GB from beyond the L2s at 50257 x 768.)
+__device__ __forceinline__ void logit_tile(int id, int tiles_t, int tiles_v, int* tt, int* tv) {
+    constexpr int kRows = 8;
+    const int group = id / (kRows * tiles_v), rows = min(kRows, tiles_t - group * kRows);
+    id -= group * kRows * tiles_v;
+    *tv = id / rows;
+    *tt = group * kRows + id - *tv * rows;
+}
+
 // First pass: each row's largest logit and sum of exp(z - largest) in a tile,
 // and the target's logit.
 template <CeForm FORM, int TM>
@@ -310,8 +322,8 @@ __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b)
     constexpr int TN = T::kBN;
     __shared__ __align__(1024) char lds[T::kLdsBytes];
     const int tiles_t = (p.tokens + TM - 1) / TM, tiles_v = (p.vocab + TN - 1) / TN;
-    const int id = xcd_run(blockIdx.x, tiles_t * tiles_v);
-    const int tv = id / tiles_t, tt = id - tv * tiles_t;
+    int tt, tv;
+    logit_tile(xcd_run(blockIdx.x, tiles_t * tiles_v), tiles_t, tiles_v, &tt, &tv);
     T t;
     t.run(h_rows(p, b), w_rows(p, b, 0), tt * TM, tv * TN, 0, static_cast<int>(p.ld_h / units(FORM)),
           (DSM_LDS char*)lds);
@@ -436,8 +448,8 @@ __global__ __launch_bounds__(threads_of(TM)) void k_piece(CePlan p, CeBuffers b,
     __shared__ __align__(1024) char lds[T::kLdsBytes];
     const int cols_pad = (cols + 63) / 64 * 64;
     const int tiles_t = (p.tokens + TM - 1) / TM, tiles_v = (cols + TN - 1) / TN;
-    const int id = xcd_run(blockIdx.x, tiles_t * tiles_v);
-    const int tv = id / tiles_t, tt = id - tv * tiles_t;
+    int tt, tv;
+    logit_tile(xcd_run(blockIdx.x, tiles_t * tiles_v), tiles_t, tiles_v, &tt, &tv);
     T t;
     t.run(h_rows(p, b), w_rows(p, b, first), tt * TM, tv * TN, 0, static_cast<int>(p.ld_h / units(FORM)),
           (DSM_LDS char*)lds);
