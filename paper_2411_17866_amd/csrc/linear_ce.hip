@@ -93,8 +93,13 @@ __device__ __forceinline__ uint32_t finite_bits(float v) {
     return b < 0x7f800000u ? b : 0u;
 }
 
-// c_t of every token, their largest magnitude and the number of valid targets;
-// by one work-group.
+// c_t of a token with a valid target, of which there are `count`.
+__device__ __forceinline__ float coefficient(const CeBuffers& b, int t, int count) {
+    return (b.weight ? b.weight[t] : 1.0f) / (b.mean ? static_cast<float>(max(count, 1)) : 1.0f);
+}
+
+// c_t of every token and their largest magnitude, for the gradients; by one
+// work-group.
 __device__ void coefficients(const CePlan& p, const CeBuffers& b) {
     __shared__ int count;
     __shared__ uint32_t c_max;
@@ -108,12 +113,11 @@ __device__ void coefficients(const CePlan& p, const CeBuffers& b) {
     for (int w = 32; w > 0; w >>= 1) mine += __shfl_xor(mine, w);
     if ((threadIdx.x & 63) == 0) atomicAdd(&count, mine);
     __syncthreads();
-    const float by = b.mean ? static_cast<float>(max(count, 1)) : 1.0f;
     float* coef = reinterpret_cast<float*>(b.workspace + p.coef);
     uint32_t top = 0;
     for (int t = threadIdx.x; t < p.tokens; t += blockDim.x) {
         float c = 0.f;
-        if (is_valid(b.target[t], p.vocab)) c = (b.weight ? b.weight[t] : 1.0f) / by;
+        if (is_valid(b.target[t], p.vocab)) c = coefficient(b, t, count);
         coef[t] = c;
         top = max(top, finite_bits(c));
     }
@@ -203,7 +207,7 @@ __global__ __launch_bounds__(256) void k_operands(CePlan p, CeBuffers b) {
     const bool of_w = blockIdx.y != 0;
     const int groups = static_cast<int>(gridDim.x) - (is_scaled(FORM) ? 0 : 1);
     if (static_cast<int>(blockIdx.x) >= groups) {
-        if (!of_w) coefficients(p, b);
+        if (!of_w && p.grads) coefficients(p, b);
         return;
     }
     const int rows = of_w ? p.vocab : (p.tokens + 63) / 64 * 64;
@@ -276,6 +280,9 @@ constexpr int square_of(int tm) { return tm == 256 ? 256 : 128; }
 constexpr int threads_of(int tm) { return tm >= 128 ? 512 : 256; }
 
 __device__ __forceinline__ Operand h_rows(const CePlan& p, const CeBuffers& b) {
+    if (b.h_direct)
+        return Operand{static_cast<const u16*>(b.h), p.form == kCeF32 ? 2 * b.h_stride : b.h_stride, p.tokens,
+                       static_cast<int32_t>(p.ld_h)};
     return Operand{reinterpret_cast<const u16*>(b.workspace + p.h), p.ld_h, (p.tokens + 63) / 64 * 64,
                    static_cast<int32_t>(p.ld_h)};
 }
@@ -419,7 +426,8 @@ __global__ __launch_bounds__(1024) void k_join(CePlan p, CeBuffers b, int tiles)
         b.loss[token] = loss;
     }
     if (gridDim.x > 1) return;
-    double sum = valid ? static_cast<double>(reinterpret_cast<const float*>(b.workspace + p.coef)[at]) * loss : 0.0;
+    const int count = __popcll(__ballot(valid));
+    double sum = valid ? static_cast<double>(coefficient(b, at, count)) * loss : 0.0;
     for (int w = kJoinTokens / 2; w > 0; w >>= 1) sum += __shfl_xor(sum, w);
     if (lane == 0) b.total[0] = static_cast<float>(sum);
 }
@@ -427,10 +435,16 @@ __global__ __launch_bounds__(1024) void k_join(CePlan p, CeBuffers b, int tiles)
 // The weighted total, in a fixed order.
 __global__ __launch_bounds__(1024) void k_total(CePlan p, CeBuffers b) {
     __shared__ double s[1024];
-    const float* coef = reinterpret_cast<const float*>(b.workspace + p.coef);
+    __shared__ int count;
+    if (threadIdx.x == 0) count = 0;
+    __syncthreads();
+    int mine = 0;
+    for (int t = threadIdx.x; t < p.tokens; t += 1024) mine += is_valid(b.target[t], p.vocab);
+    atomicAdd(&count, mine);
+    __syncthreads();
     double sum = 0.0;
     for (int t = threadIdx.x; t < p.tokens; t += 1024)
-        if (is_valid(b.target[t], p.vocab)) sum += static_cast<double>(coef[t]) * b.loss[t];
+        if (is_valid(b.target[t], p.vocab)) sum += static_cast<double>(coefficient(b, t, count)) * b.loss[t];
     s[threadIdx.x] = sum;
     __syncthreads();
     for (int w = 512; w > 0; w >>= 1) {
@@ -742,7 +756,8 @@ hipError_t launch_linear_ce(const CePlan& p, const CeBuffers& b, hipStream_t str
     const unsigned groups = static_cast<unsigned>(most < 8192 ? (most + 3) / 4 : 2048);
     switch (p.form) {
         case kCeBf16:
-            k_operands<kCeBf16><<<dim3(groups + 1, b.w_direct ? 1 : 2), 256, 0, stream>>>(p, b);
+            if (!b.h_direct)
+                k_operands<kCeBf16><<<dim3(groups + 1, b.w_direct ? 1 : 2), 256, 0, stream>>>(p, b);
             if (p.tile == 32)
                 products<kCeBf16, 32>(p, b, stream);
             else if (p.tile == 64)
@@ -753,7 +768,8 @@ hipError_t launch_linear_ce(const CePlan& p, const CeBuffers& b, hipStream_t str
                 products<kCeBf16, 256>(p, b, stream);
             break;
         case kCeF32:
-            k_operands<kCeF32><<<dim3(groups + 1, b.w_direct ? 1 : 2), 256, 0, stream>>>(p, b);
+            if (!b.h_direct)
+                k_operands<kCeF32><<<dim3(groups + 1, b.w_direct ? 1 : 2), 256, 0, stream>>>(p, b);
             if (p.tile == 32)
                 products<kCeF32, 32>(p, b, stream);
             else
@@ -766,7 +782,7 @@ hipError_t launch_linear_ce(const CePlan& p, const CeBuffers& b, hipStream_t str
             products<kCeHalf, 256>(p, b, stream);
             break;
         case kCeHalves:
-            k_coef<<<1, 1024, 0, stream>>>(p, b);
+            k_coef<<<1, 1024, 0, stream>>>(p, b);  // (also clears the largest magnitudes)
             k_largest<true><<<dim3(groups, 2), 256, 0, stream>>>(p, b);
             k_operands<kCeHalves><<<dim3(groups, 2), 256, 0, stream>>>(p, b);
             if (p.tile == 128)

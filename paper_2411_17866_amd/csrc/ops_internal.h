@@ -11,7 +11,8 @@ namespace dsm {
 
 // ---- Orthogonalised updates (ortho.hip) ----
 
-constexpr int kOrthoGroup = 64;  // matrices that one set of launches takes
+constexpr int kOrthoGroup = 64;     // matrices that one set of launches takes
+constexpr int kOrthoMaxSteps = 32;  // iterations
 
 struct OrthoOffsets {
     int64_t at[kOrthoGroup];  // elements from the buffers' start to each matrix
@@ -29,7 +30,7 @@ struct OrthoGroup {
     int32_t count;
     int32_t m, n;
     int32_t tall;   // the matrix in memory is n x m
-    int32_t split;  // fp32 buffers, operands in two fp16 halves; else bf16 buffers, one fp16
+    int32_t bf16;   // bf16 buffers, operands as one fp16; else fp32 buffers, two fp16 halves
     int32_t vector;  // rows start where four elements can be moved at once (not for the
                      // transposed stores of a tall matrix)
     int64_t row_stride;
@@ -45,8 +46,9 @@ struct OrthoGroup {
     int32_t nesterov;
 };
 
-// Bytes of workspace that a group of `count` m x n matrices needs.
-int64_t ortho_group_bytes(int count, int m, int n, bool split);
+// Bytes of workspace that a group of `count` m x n matrices needs (0 for matrices
+// that are worked on in LDS).
+int64_t ortho_group_bytes(int count, int m, int n, bool bf16);
 
 hipError_t launch_ortho(const OrthoGroup& g, const float* coeffs, const OrthoScales* scales, int steps,
                         hipStream_t stream);
@@ -85,6 +87,7 @@ struct CeBuffers {
     char* workspace;
     int32_t mean;
     int32_t w_direct;  // w is read where it lies
+    int32_t h_direct;  // and h
     // Rows whose elements can be moved by four.
     int32_t h_vector, w_vector, dh_vector, dw_vector;
 };

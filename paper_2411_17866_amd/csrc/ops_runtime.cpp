@@ -14,7 +14,7 @@ namespace {
 
 constexpr int64_t kMaxTokens = int64_t(1) << 20, kMaxVocab = int64_t(1) << 20, kMaxDim = 1 << 16;
 constexpr int64_t kMaxSide = int64_t(1) << 20, kMaxShort = 1 << 14;
-constexpr int kMaxSteps = 32;
+constexpr int kMaxSteps = dsm::kOrthoMaxSteps;
 
 dsm_status bad(dsm_status st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 dsm_status bad(dsm_status st, const char* fmt, ...) {
@@ -233,15 +233,15 @@ bool is_empty(const dsm_ortho_problem* p) { return p->rows == 0 || p->cols == 0 
 
 int group_size(const dsm_ortho_problem* p) {
     const int m = static_cast<int>(std::min(p->rows, p->cols)), n = static_cast<int>(std::max(p->rows, p->cols));
-    const int64_t one = dsm::ortho_group_bytes(1, m, n, p->dtype == DSM_F32);
-    const int64_t fit = std::max<int64_t>(1, kGroupBytes / one);
+    const int64_t one = dsm::ortho_group_bytes(1, m, n, p->dtype == DSM_BF16);
+    const int64_t fit = one == 0 ? dsm::kOrthoGroup : std::max<int64_t>(1, kGroupBytes / one);
     return static_cast<int>(std::min<int64_t>(std::min<int64_t>(fit, p->count), dsm::kOrthoGroup));
 }
 
 int64_t ortho_bytes(const dsm_ortho_problem* p) {
     if (is_empty(p)) return 0;
     const int m = static_cast<int>(std::min(p->rows, p->cols)), n = static_cast<int>(std::max(p->rows, p->cols));
-    return dsm::ortho_group_bytes(group_size(p), m, n, p->dtype == DSM_F32);
+    return dsm::ortho_group_bytes(group_size(p), m, n, p->dtype == DSM_BF16);
 }
 
 dsm_status run_ortho(const dsm_ortho_problem* p, const dsm_ortho_buffers* b, const dsm_ortho_hparams* hp,
@@ -249,14 +249,16 @@ dsm_status run_ortho(const dsm_ortho_problem* p, const dsm_ortho_buffers* b, con
     if (!p->offsets) return invalid("offsets is NULL");
     for (int i = 0; i < p->count; ++i)
         if (p->offsets[i] < 0) return bad(DSM_ERR_INVALID_ARG, "offsets[%d] < 0", i);
-    if (dsm_status st = check_workspace(b->workspace, b->workspace_bytes, ortho_bytes(p))) return st;
+    const int64_t need = ortho_bytes(p);
+    if (need > 0)
+        if (dsm_status st = check_workspace(b->workspace, b->workspace_bytes, need)) return st;
     if (dsm_status st = check_device()) return st;
     const int group = group_size(p);
     dsm::OrthoGroup g{};
     g.m = static_cast<int32_t>(std::min(p->rows, p->cols));
     g.n = static_cast<int32_t>(std::max(p->rows, p->cols));
     g.tall = p->rows > p->cols;
-    g.split = p->dtype == DSM_F32;
+    g.bf16 = p->dtype == DSM_BF16;
     g.row_stride = p->row_stride;
     g.workspace = b->workspace;
     g.in = b->in;
@@ -336,6 +338,10 @@ dsm_status dsm_linear_ce(const dsm_ce_problem* problem, const dsm_ce_buffers* bu
     // inside a tile.
     q.w_direct = (plan.form == dsm::kCeBf16 || plan.form == dsm::kCeF32) && p.dim % 64 == 0 &&
                  b.w_stride * elem % 16 == 0 && aligned(b.w, 16) && b.w_stride < (int64_t(1) << 22);
+    // Without gradients nothing but a token's own loss meets its row of h, so rows
+    // without a valid target need no zeros.
+    q.h_direct = q.w_direct && !p.grads && b.h_stride * elem % 16 == 0 && aligned(b.h, 16) &&
+                 b.h_stride < (int64_t(1) << 22);
     const size_t four = 4 * elem;
     q.h_vector = p.dim % 4 == 0 && b.h_stride % 4 == 0 && aligned(b.h, four);
     q.w_vector = p.dim % 4 == 0 && b.w_stride % 4 == 0 && aligned(b.w, four);

@@ -17,8 +17,10 @@
 // them what rounding X, A or B to 8 bits put there).  Two rules keep 11 bits
 // enough: A is rounded once and that same A enters b A and c A A, and the term
 // a X takes X from 22 bits (hi + lo), the products hi alone.  Against 64 bits
-// this gives 0.02-0.2% (a strong low rank over noise, and noise alone), below
-// the 0.17% that rounding the result to bf16 costs; all of it in bf16, 1-5%.
+// this gives 0.02-0.2% (a strong low rank over noise, and noise alone), where
+// rounding the result to bf16 costs 0.17%; all of it in bf16, 1-5%.  The fewer the
+// singular values, the less their errors average: matrices small enough for LDS take
+// two halves (bf16 64 x 48: 0.28% so, with one half; 0.17% with two).
 //
 // Range.  ||X||_2 <= 1 at the start, and the polynomial bounds it after each
 // step, so the host picks for each stored operand the power of two that brings
@@ -448,6 +450,217 @@ __global__ __launch_bounds__(tile::threads_of(BM)) void k_product(OrthoGroup g, 
     }
 }
 
+// ---- Small matrices: the whole iteration in one work-group's LDS ----
+//
+// A matrix whose X and A fit LDS as split operands takes one launch: a work-group
+// of eight waves keeps X and A (then B in its place) and iterates between barriers.
+// With the products' kernels it would be 2 + 3 * steps launches of little work, each
+// 3-5 us on the host and on the device: one 64 x 48 matrix 57-67 us so, 29 us here.
+// Operands are stored as gemm_tile.h's stages are: for each 32 columns all rows of
+// 128 bytes (hi x 32, lo x 32), the 16-byte pieces of a row exchanged by its number.
+
+constexpr int kSmallLds = 144 << 10;
+constexpr int kSmallWaves = 8;
+constexpr int kSmallSquare = 5;   // fragments of A that a wave has, at most (96 x 96)
+constexpr int kSmallWide = 18;    // fragments of X
+
+__host__ __device__ inline int pad32(int v) { return (v + 31) / 32 * 32; }
+// It has to fit, and to be little: a wave's products of 16 x 16 x 32 in an iteration
+// take it about 0.2 us each here, five iterations 12 us + 1 us each: 64 x 64, 12 of
+// them, 30 us (68 us by the products' kernels); 128 x 128, 96, 107 us (70-85 us).
+inline bool is_small(int m, int n) {
+    const int64_t mp = pad32(m), np = pad32(n), mi = mp / 16;
+    const int64_t products = mi * mi * (np / 32 + mp / 32) + mi * (np / 16) * (mp / 32);
+    return mp * (mp + np) * 4 <= kSmallLds && mi * mi <= kSmallSquare * kSmallWaves &&
+           mi * (np / 16) <= kSmallWide * kSmallWaves && products <= 50 * kSmallWaves;
+}
+
+// Factors of the accumulators and of what is added to them, for each iteration.
+struct SmallSteps {
+    int steps;
+    struct {
+        float gram, poly, poly_add, update, update_add;
+    } f[kOrthoMaxSteps];
+};
+
+struct SmallOperand {
+    DSM_LDS char* p;
+    int rows;  // padded
+    __device__ __forceinline__ DSM_LDS char* piece(int row, int col, int half) const {
+        const int byte = (col & 31) * 2;
+        return p + ((col >> 5) * rows + row) * 128 + ((((byte >> 4) + half * 4) ^ (row & 7)) << 4) + (byte & 15);
+    }
+    // Rows 16 f .. of columns 32 kb .. : operand k-contiguous.
+    __device__ __forceinline__ tile::short8v along(int f, int kb, int half, int lane) const {
+        return *reinterpret_cast<const DSM_LDS tile::short8v*>(
+            piece(f * 16 + (lane & 15), kb * 32 + (lane >> 4) * 8, half));
+    }
+    // Columns 16 f .. of rows 32 kb .. : operand k-strided.
+    __device__ __forceinline__ tile::short8v across(int f, int kb, int half, int lane) const {
+        const int k = kb * 32 + (lane >> 4) * 8 + ((lane & 15) >> 2), c = f * 16 + (lane & 3) * 4;
+        const tile::short4v a =
+            __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<DSM_LDS tile::short4v*>(piece(k, c, half)));
+        const tile::short4v b =
+            __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<DSM_LDS tile::short4v*>(piece(k + 4, c, half)));
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    __device__ __forceinline__ f4 get(int row, int col) const {
+        const u16x4 h = *reinterpret_cast<const DSM_LDS u16x4*>(piece(row, col, 0));
+        const u16x4 l = *reinterpret_cast<const DSM_LDS u16x4*>(piece(row, col, 1));
+        f4 v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = from_bits(h[r]) + from_bits(l[r]);
+        return v;
+    }
+    __device__ __forceinline__ void put(int row, int col, f4 v) const {
+        u16x4 h, l;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            h[r] = to_bits(v[r]);
+            l[r] = to_bits(v[r] - from_bits(h[r]));
+        }
+        *reinterpret_cast<DSM_LDS u16x4*>(piece(row, col, 0)) = h;
+        *reinterpret_cast<DSM_LDS u16x4*>(piece(row, col, 1)) = l;
+    }
+};
+
+__device__ __forceinline__ f4 triple(tile::short8v ih, tile::short8v il, tile::short8v jh, tile::short8v jl, f4 c) {
+    c = tile::mfma<tile::kSplit>(jl, ih, c);
+    c = tile::mfma<tile::kSplit>(jh, il, c);
+    return tile::mfma<tile::kSplit>(jh, ih, c);
+}
+
+template <bool STEP, bool BF16>
+__global__ __launch_bounds__(kSmallWaves * 64) void k_small(OrthoGroup g, SmallSteps it, int x_exp) {
+    __shared__ __align__(1024) char lds[kSmallLds];
+    __shared__ double sums[kSmallWaves];
+    const int m = g.m, n = g.n, mp = pad32(m), np = pad32(n);
+    const SmallOperand X{(DSM_LDS char*)lds, mp}, A{(DSM_LDS char*)lds + mp * np * 4, mp};
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t base = g.off.at[blockIdx.x];
+    const int rows = g.tall ? n : m, cols = g.tall ? m : n, quads = (cols + 3) / 4;
+
+    // Momentum, norm, X_0.  A thread comes back to the elements it has written.
+    double sum = 0.0;
+    for (int q = threadIdx.x; q < rows * quads; q += kSmallWaves * 64) {
+        const int r = q / quads, c = (q - r * quads) * 4;
+        const f4 v = update_at<STEP, BF16, true>(g, base + r * g.row_stride + c, cols - c);
+        sum += static_cast<double>(v[0]) * v[0] + static_cast<double>(v[1]) * v[1] +
+               (static_cast<double>(v[2]) * v[2] + static_cast<double>(v[3]) * v[3]);
+    }
+    for (int w = 32; w > 0; w >>= 1) sum += __shfl_xor(sum, w);
+    if (lane == 0) sums[wave] = sum;
+    for (int e = threadIdx.x; e < mp * np / 4; e += kSmallWaves * 64)
+        reinterpret_cast<DSM_LDS f4*>((DSM_LDS char*)lds)[e] = f4{0.f, 0.f, 0.f, 0.f};
+    __syncthreads();
+    sum = 0.0;
+    for (int w = 0; w < kSmallWaves; ++w) sum += sums[w];
+    const double inv = ldexp(1.0 / (sqrt(sum) + static_cast<double>(g.eps)), x_exp);
+    for (int q = threadIdx.x; q < rows * quads; q += kSmallWaves * 64) {
+        const int r = q / quads, c = (q - r * quads) * 4;
+        const f4 v = update_at<STEP, BF16, false>(g, base + r * g.row_stride + c, cols - c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (c + e >= cols) break;
+            const float x = static_cast<float>(v[e] * inv);
+            const int i = g.tall ? c + e : r, j = g.tall ? r : c + e;
+            const u16 hi = to_bits(x);
+            *reinterpret_cast<DSM_LDS u16*>(X.piece(i, j, 0)) = hi;
+            *reinterpret_cast<DSM_LDS u16*>(X.piece(i, j, 1)) = to_bits(x - from_bits(hi));
+        }
+    }
+    __syncthreads();
+
+    const int mi = mp / 16, square = mi * mi, wide = mi * (np / 16);
+    for (int s = 0; s < it.steps; ++s) {
+        const auto f = it.f[s];
+        // Unknown to the compiler in each iteration, or it would keep the LDS
+        // addresses of every fragment in registers over all of them.
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        const int i0 = ln & 15, j0 = (ln >> 4) * 4;
+        for (int id = wave; id < square; id += kSmallWaves) {
+            const int fi = id / mi, fj = id - fi * mi;
+            f4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+            for (int kb = 0; kb < np / 32; ++kb)
+                acc = triple(X.along(fi, kb, 0, ln), X.along(fi, kb, 1, ln), X.along(fj, kb, 0, ln),
+                             X.along(fj, kb, 1, ln), acc);
+            A.put(fi * 16 + i0, fj * 16 + j0, acc * f.gram);
+        }
+        __syncthreads();
+        f4 b[kSmallSquare];
+#pragma unroll
+        for (int t = 0; t < kSmallSquare; ++t) {
+            const int id = t * kSmallWaves + wave;
+            if (id >= square) continue;
+            const int fi = id / mi, fj = id - fi * mi;
+            f4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+            for (int kb = 0; kb < mp / 32; ++kb)
+                acc = triple(A.along(fi, kb, 0, ln), A.along(fi, kb, 1, ln), A.along(fj, kb, 0, ln),
+                             A.along(fj, kb, 1, ln), acc);
+            const f4 a = A.get(fi * 16 + i0, fj * 16 + j0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) b[t][r] = __builtin_fmaf(f.poly_add, a[r], acc[r] * f.poly);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < kSmallSquare; ++t) {
+            const int id = t * kSmallWaves + wave;
+            if (id >= square) continue;
+            const int fi = id / mi;
+            A.put(fi * 16 + i0, (id - fi * mi) * 16 + j0, b[t]);
+        }
+        __syncthreads();
+        f4 x[kSmallWide];
+#pragma unroll
+        for (int t = 0; t < kSmallWide; ++t) {
+            const int id = t * kSmallWaves + wave;
+            if (id >= wide) continue;
+            const int fj = id / mi, fi = id - fj * mi;
+            f4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+            for (int kb = 0; kb < mp / 32; ++kb)
+                acc = triple(A.along(fi, kb, 0, ln), A.along(fi, kb, 1, ln), X.across(fj, kb, 0, ln),
+                             X.across(fj, kb, 1, ln), acc);
+            const f4 a = X.get(fi * 16 + i0, fj * 16 + j0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[t][r] = __builtin_fmaf(f.update_add, a[r], acc[r] * f.update);
+        }
+        __syncthreads();
+        const bool last = s + 1 == it.steps;
+#pragma unroll
+        for (int t = 0; t < kSmallWide; ++t) {
+            const int id = t * kSmallWaves + wave;
+            if (id >= wide) continue;
+            const int fj = id / mi, i = (id - fj * mi) * 16 + i0, j = fj * 16 + j0;
+            if (!last) {
+                X.put(i, j, x[t]);
+                continue;
+            }
+            if (i >= m) continue;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (j + r >= n) continue;
+                const int64_t e = base + (g.tall ? (j + r) * g.row_stride + i : i * g.row_stride + j + r);
+                if constexpr (BF16) {
+                    static_cast<u16*>(g.out)[e] = float_to_bf16(x[t][r]);
+                } else {
+                    const float d = g.scale * x[t][r];
+                    if (g.x) {
+                        const float p = g.x[e];
+                        g.x[e] = p - g.lr * (d + g.weight_decay * p);
+                    } else {
+                        static_cast<float*>(g.out)[e] = d;
+                    }
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
 float pow2(int e) { return __builtin_ldexpf(1.0f, e); }
 
 // Work-groups of a product by tiles of bm.
@@ -500,6 +713,18 @@ void iterate(const OrthoGroup& g, const Parts& parts, const float* coeffs, const
     }
 }
 
+template <bool STEP, bool BF16>
+void small(const OrthoGroup& g, const float* coeffs, const OrthoScales* scales, int steps, hipStream_t stream) {
+    SmallSteps it;
+    it.steps = steps;
+    for (int s = 0; s < steps; ++s) {
+        const OrthoScales sc = scales[s];
+        it.f[s] = {pow2(sc.a - 2 * sc.x), coeffs[3 * s + 2] * pow2(sc.b - 2 * sc.a), coeffs[3 * s + 1] * pow2(sc.b - sc.a),
+                   pow2(sc.x_next - sc.b - sc.x), coeffs[3 * s] * pow2(sc.x_next - sc.x)};
+    }
+    k_small<STEP, BF16><<<g.count, kSmallWaves * 64, 0, stream>>>(g, it, scales[0].x);
+}
+
 template <int S, bool STEP, bool BF16>
 void start(const OrthoGroup& g, const Parts& parts, int x_exp, hipStream_t stream) {
     // Some 4096 elements a work-group, and enough of them for all CUs.
@@ -512,23 +737,32 @@ void start(const OrthoGroup& g, const Parts& parts, int x_exp, hipStream_t strea
 
 }  // namespace
 
-int64_t ortho_group_bytes(int count, int m, int n, bool split) {
-    return Parts(m, n, split).bytes * count;
+int64_t ortho_group_bytes(int count, int m, int n, bool bf16) {
+    return is_small(m, n) ? 0 : Parts(m, n, !bf16).bytes * count;
 }
 
 hipError_t launch_ortho(const OrthoGroup& g, const float* coeffs, const OrthoScales* scales, int steps,
                         hipStream_t stream) {
-    const Parts parts(g.m, g.n, g.split != 0);
-    if (!g.split)
+    if (is_small(g.m, g.n)) {
+        if (g.bf16)
+            small<false, true>(g, coeffs, scales, steps, stream);
+        else if (g.mom || g.x)
+            small<true, false>(g, coeffs, scales, steps, stream);
+        else
+            small<false, false>(g, coeffs, scales, steps, stream);
+        return hipGetLastError();
+    }
+    const Parts parts(g.m, g.n, g.bf16 == 0);
+    if (g.bf16)
         start<1, false, true>(g, parts, scales[0].x, stream);
     else if (g.mom || g.x)
         start<2, true, false>(g, parts, scales[0].x, stream);
     else
         start<2, false, false>(g, parts, scales[0].x, stream);
-    if (g.split)
-        iterate<2>(g, parts, coeffs, scales, steps, stream);
-    else
+    if (g.bf16)
         iterate<1>(g, parts, coeffs, scales, steps, stream);
+    else
+        iterate<2>(g, parts, coeffs, scales, steps, stream);
     return hipGetLastError();
 }
 

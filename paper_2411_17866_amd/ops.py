@@ -7,6 +7,8 @@ problem: it checks tensors, keeps the workspace, and enqueues on torch's current
 stream.  Calls of one object on different streams are put one after another,
 since they share the workspace (under graph capture that is the caller's part).
 """
+import contextlib
+
 import torch
 
 from . import dsm
@@ -41,6 +43,11 @@ class _Plan:
                 self.workspace.record_stream(stream)
             self._stream = stream
         return stream.cuda_stream
+
+    def _on_device(self):
+        if torch.cuda.current_device() == self.device.index:
+            return contextlib.nullcontext()
+        return torch.cuda.device(self.device)
 
     def _check(self, name, t, dtype, shape):
         if t.device != self.device:
@@ -120,7 +127,7 @@ class LinearCE(_Plan):
         elif dh is not None or dw is not None:
             raise ValueError("dh or dw given to a plan without gradients")
         buf.workspace, buf.workspace_bytes = self.workspace.data_ptr(), self.workspace_bytes
-        with torch.cuda.device(self.device):
+        with self._on_device():
             buf.stream = self._enter()
             dsm.dsm_linear_ce(self.problem, buf, mean)
         return out
@@ -215,7 +222,7 @@ class Ortho(_Plan):
             out = torch.empty_strided(u.size(), u.stride(), dtype=u.dtype, device=u.device)
         problem = self._placed([("u", u), ("out", out)])
         buf = self._buffers(in_=u, out=out)
-        with torch.cuda.device(self.device):
+        with self._on_device():
             buf.stream = self._enter()
             dsm.dsm_orthogonalize(problem, buf)
         return out
@@ -225,7 +232,7 @@ class Ortho(_Plan):
         may be None for u = g."""
         problem = self._placed([(n, t) for n, t in (("x", x), ("m", m), ("g", g)) if t is not None])
         buf = self._buffers(in_=g, m=m, x=x)
-        with torch.cuda.device(self.device):
+        with self._on_device():
             buf.stream = self._enter()
             dsm.dsm_ortho_step(problem, buf, lr, mu, scale, wd, nesterov)
 
@@ -235,7 +242,7 @@ class Ortho(_Plan):
         problem = self._placed([(n, t) for n, t in (("m", m), ("g", g), ("out", out))
                                 if t is not None])
         buf = self._buffers(in_=g, m=m, out=out)
-        with torch.cuda.device(self.device):
+        with self._on_device():
             buf.stream = self._enter()
             dsm.dsm_ortho_step(problem, buf, 1.0, mu, scale, 0.0, nesterov)
         return out
