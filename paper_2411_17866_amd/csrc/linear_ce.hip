@@ -779,7 +779,10 @@ hipError_t launch_linear_ce(const CePlan& p, const CeBuffers& b, hipStream_t str
             k_coef<<<1, 1024, 0, stream>>>(p, b);
             k_largest<false><<<dim3(groups, 2), 256, 0, stream>>>(p, b);
             k_operands<kCeHalf><<<dim3(groups, 2), 256, 0, stream>>>(p, b);
-            products<kCeHalf, 256>(p, b, stream);
+            if (p.tile == 128)
+                products<kCeHalf, 128>(p, b, stream);
+            else
+                products<kCeHalf, 256>(p, b, stream);
             break;
         case kCeHalves:
             k_coef<<<1, 1024, 0, stream>>>(p, b);  // (also clears the largest magnitudes)

@@ -123,7 +123,17 @@ dsm::CePlan make_plan(const dsm_ce_problem* p) {
         q.form = p->grads && T > 512 ? dsm::kCeHalf : dsm::kCeBf16;
     const int64_t width = p->dtype == DSM_F32 ? 2 : 1;
     const int64_t tokens_pad = round_up(T, 64);
-    q.tile = T <= 32 ? 32 : T <= 64 || q.form == dsm::kCeF32 ? 64 : T <= 512 ? 128 : 256;
+    if (T <= 64 || q.form == dsm::kCeF32) {
+        q.tile = T <= 32 ? 32 : 64;
+    } else {
+        // 256 where it takes the CUs no longer over the logits (a turn of two tiles of
+        // 128 a CU takes 0.62 of a turn of one of 256): 1024 tokens of 4001 x 384 in
+        // bf16 with gradients 66 us by 128, 111 us by 256; 8192 of 50257 x 768 by 256.
+        const auto tiles = [&](int64_t of) { return ((T + of - 1) / of) * ((V + of - 1) / of); };
+        const double t128 = 0.62 * std::ceil(static_cast<double>(tiles(128)) / 512);
+        const double t256 = std::ceil(static_cast<double>(tiles(256)) / 256);
+        q.tile = T > 512 && t256 <= t128 ? 256 : 128;
+    }
     const int64_t square = q.tile == 256 ? 256 : 128;
     q.ld_h = q.ld_w = round_up(p->dim, 64) * width;
     int64_t at = 0;
