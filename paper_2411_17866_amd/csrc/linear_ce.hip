@@ -722,6 +722,16 @@ __global__ __launch_bounds__(tile::threads_of(square_of(TM))) void k_dw(CePlan p
     dw_tile<FORM, TM>(p, b, first, cols, xcd_run(blockIdx.x, gridDim.x), (DSM_LDS char*)lds);
 }
 
+// No tokens: the total and dw are zero.
+template <bool F32>
+__global__ __launch_bounds__(256) void k_nothing(CePlan p, CeBuffers b) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) b.total[0] = 0.f;
+    if (!p.grads) return;
+    for (int r = blockIdx.x; r < p.vocab; r += gridDim.x)
+        for (int c = threadIdx.x * 4; c < p.dim; c += 1024)
+            store_grad<F32>(b.dw, r * b.dw_stride + c, f4{0.f, 0.f, 0.f, 0.f}, p.dim - c, b.dw_vector);
+}
+
 template <CeForm FORM, int TM>
 void products(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
     constexpr int kThreads = threads_of(TM), TN = square_of(TM);
@@ -752,6 +762,14 @@ void products(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_linear_ce(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
+    if (p.tokens == 0) {
+        const unsigned rows = static_cast<unsigned>(p.grads ? std::min(p.vocab, 2048) : 1);
+        if (is_f32(p.form))
+            k_nothing<true><<<rows, 256, 0, stream>>>(p, b);
+        else
+            k_nothing<false><<<rows, 256, 0, stream>>>(p, b);
+        return hipGetLastError();
+    }
     const int most = b.w_direct || p.tokens > p.vocab ? p.tokens : p.vocab;
     const unsigned groups = static_cast<unsigned>(most < 8192 ? (most + 3) / 4 : 2048);
     switch (p.form) {

@@ -19,9 +19,9 @@ struct OrthoOffsets {
 };
 
 // Power-of-two exponents of one iteration's stored operands: X * 2^x, A * 2^a,
-// B * 2^b, and X * 2^x_next after it.
+// B * 2^b, and X * 2^x_next after it; an X below 1 grows by less than 2^growth.
 struct OrthoScales {
-    int x, a, b, x_next;
+    int x, a, b, x_next, growth;
 };
 
 // One group of matrices, all of one shape.  The iteration works on the wide

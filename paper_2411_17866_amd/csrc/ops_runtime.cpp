@@ -219,6 +219,7 @@ dsm_status plan_iteration(const dsm_ortho_problem* p, Iteration* it) {
         s.x = exponent_under(r);
         s.a = exponent_under(l);
         s.b = exponent_under(top_b * 1.01);
+        s.growth = std::max(0, static_cast<int>(std::ceil(std::log2(1.01 * (std::fabs(a) + std::fabs(b) + std::fabs(c)) + 1e-30))));
         if (k > 0) it->scales[k - 1].x_next = s.x;
         s.x_next = 0;  // the last result as it is
         r = next;
@@ -318,8 +319,8 @@ dsm_status dsm_linear_ce(const dsm_ce_problem* problem, const dsm_ce_buffers* bu
     if (!b.w || !b.total) return invalid("w or total is NULL");
     if (p.tokens > 0 && (!b.h || !b.target || !b.loss)) return invalid("h, target or loss is NULL");
     if (p.grads && (!b.dw || (p.tokens > 0 && !b.dh))) return invalid("dh or dw is NULL");
-    if (b.h_stride < p.dim || b.w_stride < p.dim) return invalid("h_stride or w_stride < dim");
-    if (p.grads && (b.dh_stride < p.dim || b.dw_stride < p.dim)) return invalid("dh_stride or dw_stride < dim");
+    if ((p.tokens > 0 && b.h_stride < p.dim) || b.w_stride < p.dim) return invalid("h_stride or w_stride < dim");
+    if (p.grads && ((p.tokens > 0 && b.dh_stride < p.dim) || b.dw_stride < p.dim)) return invalid("dh_stride or dw_stride < dim");
     if (!aligned(b.h, elem) || !aligned(b.w, elem) || !aligned(b.dh, elem) || !aligned(b.dw, elem))
         return invalid("h, w, dh or dw is not aligned to its elements");
     if (!aligned(b.target, 8) || !aligned(b.weight, 4) || !aligned(b.total, 4) || !aligned(b.loss, 4) ||

@@ -25,7 +25,9 @@
 // Range.  ||X||_2 <= 1 at the start, and the polynomial bounds it after each
 // step, so the host picks for each stored operand the power of two that brings
 // its bound just under fp16's largest number; entries then keep their bits down
-// to 2^-40 of that bound.
+// to 2^-40 of that bound.  Where eps outweighs the norm, X starts far below 1: it is
+// then stored times 2^e, e its own for each matrix, with which b A and c A A lose
+// 2^-2e and 2^-4e, and e falls with each iteration by what X can grow.
 #include <hip/hip_runtime.h>
 
 #include "gemm_tile.h"
@@ -63,7 +65,7 @@ struct Parts {
         const int64_t xb = up256(static_cast<int64_t>(m) * pad(n) * 2) * 2;
         const int64_t ab = up256(static_cast<int64_t>(m) * pad(m) * 2 * (split ? 2 : 1));
         lo = xb / 2;
-        x[0] = up256(kNormParts * 8);
+        x[0] = up256(kNormParts * 8 + 4);
         x[1] = x[0] + xb;
         a = x[1] + xb;
         b = a + ab;
@@ -180,6 +182,13 @@ __global__ __launch_bounds__(256) void k_norm(OrthoGroup g, Parts parts, int n_p
         reinterpret_cast<double*>(static_cast<char*>(g.workspace) + blockIdx.y * parts.bytes)[blockIdx.x] = s[0];
 }
 
+// The power of two that brings norm / (norm + eps) into (1/2, 1].
+__device__ __forceinline__ int lift_of(double norm, double eps) {
+    const double share = norm / (norm + eps);
+    return share > 0.0 && share < 0.5 ? -ilogb(share) - 1 : 0;
+}
+__host__ __device__ inline int64_t lift_at() { return kNormParts * 8; }  // bytes into a matrix's workspace
+
 // X_0 in the stored form, wide, its padding zero: 64 x 64 of it per work-group.
 template <int S, bool STEP, bool BF16>
 __global__ __launch_bounds__(256) void k_start(OrthoGroup g, Parts parts, int n_parts, int x_exp) {
@@ -207,7 +216,10 @@ __global__ __launch_bounds__(256) void k_start(OrthoGroup g, Parts parts, int n_
         if (static_cast<int>(threadIdx.x) < w) s[threadIdx.x] += s[threadIdx.x + w];
         __syncthreads();
     }
-    const double inv = ldexp(1.0 / (sqrt(s[0]) + static_cast<double>(g.eps)), x_exp);
+    const double norm = sqrt(s[0]);
+    const int lift = lift_of(norm, g.eps);
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *reinterpret_cast<int*>(ws + lift_at()) = lift;
+    const double inv = ldexp(1.0 / (norm + static_cast<double>(g.eps)), x_exp + lift);
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
@@ -285,7 +297,7 @@ __device__ __forceinline__ u16x8 lower(const Eight& e) {
 
 template <int S, int BM, Product P>
 __global__ __launch_bounds__(tile::threads_of(BM)) void k_product(OrthoGroup g, Parts parts, int from, float mul,
-                                                                    float add) {
+                                                                    float add, int fallen, int next) {
     using T = tile::Pick<S == 1 ? tile::kF16 : tile::kSplit, BM, kContig, P == kGram || P == kPoly ? kContig : kStrided>;
     constexpr bool kSymmetric = P == kGram || P == kPoly;
     __shared__ __align__(1024) char lds[T::kLdsBytes];
@@ -313,6 +325,16 @@ __global__ __launch_bounds__(tile::threads_of(BM)) void k_product(OrthoGroup g, 
     t.run(P == kGram ? ox : P == kPoly ? oa : ob, P == kPoly ? oa : ox, ti * BM, tj * BM, 0,
           P == kGram ? np : mp, (DSM_LDS char*)lds);
 
+    // X is stored times 2^lift more, and after this iteration 2^after.
+    const int lift = max(*reinterpret_cast<const int*>(ws + lift_at()) - fallen, 0);
+    if constexpr (P == kPoly) {
+        mul = ldexpf(mul, -4 * lift);
+        add = ldexpf(add, -2 * lift);
+    } else if constexpr (P == kUpdate || P == kLast) {
+        const int after = P == kLast ? 0 : max(lift - next, 0);
+        mul = ldexpf(mul, after - lift);
+        add = ldexpf(add, after - lift);
+    }
     // mul, add: powers of two and coefficients that bring the accumulator and
     // the stored A or X to the stored result.  What a batch of fragments needs of
     // them is loaded before the batch's first store, which the compiler must
@@ -480,6 +502,7 @@ struct SmallSteps {
     int steps;
     struct {
         float gram, poly, poly_add, update, update_add;
+        int growth;
     } f[kOrthoMaxSteps];
 };
 
@@ -555,7 +578,9 @@ __global__ __launch_bounds__(kSmallWaves * 64) void k_small(OrthoGroup g, SmallS
     __syncthreads();
     sum = 0.0;
     for (int w = 0; w < kSmallWaves; ++w) sum += sums[w];
-    const double inv = ldexp(1.0 / (sqrt(sum) + static_cast<double>(g.eps)), x_exp);
+    const double norm = sqrt(sum);
+    int lift = __builtin_amdgcn_readfirstlane(lift_of(norm, g.eps));
+    const double inv = ldexp(1.0 / (norm + static_cast<double>(g.eps)), x_exp + lift);
     for (int q = threadIdx.x; q < rows * quads; q += kSmallWaves * 64) {
         const int r = q / quads, c = (q - r * quads) * 4;
         const f4 v = update_at<STEP, BF16, false>(g, base + r * g.row_stride + c, cols - c);
@@ -573,7 +598,14 @@ __global__ __launch_bounds__(kSmallWaves * 64) void k_small(OrthoGroup g, SmallS
 
     const int mi = mp / 16, square = mi * mi, wide = mi * (np / 16);
     for (int s = 0; s < it.steps; ++s) {
-        const auto f = it.f[s];
+        auto f = it.f[s];
+        const bool last = s + 1 == it.steps;
+        const int after = last ? 0 : max(lift - f.growth, 0);
+        f.poly = ldexpf(f.poly, -4 * lift);
+        f.poly_add = ldexpf(f.poly_add, -2 * lift);
+        f.update = ldexpf(f.update, after - lift);
+        f.update_add = ldexpf(f.update_add, after - lift);
+        lift = after;
         // Unknown to the compiler in each iteration, or it would keep the LDS
         // addresses of every fragment in registers over all of them.
         int ln = lane;
@@ -629,7 +661,6 @@ __global__ __launch_bounds__(kSmallWaves * 64) void k_small(OrthoGroup g, SmallS
             for (int r = 0; r < 4; ++r) x[t][r] = __builtin_fmaf(f.update_add, a[r], acc[r] * f.update);
         }
         __syncthreads();
-        const bool last = s + 1 == it.steps;
 #pragma unroll
         for (int t = 0; t < kSmallWide; ++t) {
             const int id = t * kSmallWaves + wave;
@@ -685,31 +716,34 @@ int tile_of(const OrthoGroup& g, bool symmetric) {
 }
 
 template <int S, Product P>
-void product(const OrthoGroup& g, const Parts& parts, int from, float mul, float add, hipStream_t stream) {
+void product(const OrthoGroup& g, const Parts& parts, int from, float mul, float add, int fallen, int next,
+             hipStream_t stream) {
     constexpr bool kSymmetric = P == kGram || P == kPoly;
     const int bm = tile_of(g, kSymmetric);
     const unsigned groups = groups_of(g, bm, kSymmetric);
     if (bm == 64)
-        k_product<S, 64, P><<<groups, tile::threads_of(64), 0, stream>>>(g, parts, from, mul, add);
+        k_product<S, 64, P><<<groups, tile::threads_of(64), 0, stream>>>(g, parts, from, mul, add, fallen, next);
     else if (bm == 128)
-        k_product<S, 128, P><<<groups, tile::threads_of(128), 0, stream>>>(g, parts, from, mul, add);
+        k_product<S, 128, P><<<groups, tile::threads_of(128), 0, stream>>>(g, parts, from, mul, add, fallen, next);
     else
-        k_product<S, 256, P><<<groups, tile::threads_of(256), 0, stream>>>(g, parts, from, mul, add);
+        k_product<S, 256, P><<<groups, tile::threads_of(256), 0, stream>>>(g, parts, from, mul, add, fallen, next);
 }
 
 template <int S>
 void iterate(const OrthoGroup& g, const Parts& parts, const float* coeffs, const OrthoScales* scales,
              int steps, hipStream_t stream) {
+    int fallen = 0;  // by how much X's lift has fallen
     for (int s = 0; s < steps; ++s) {
         const OrthoScales sc = scales[s];
         const float a = coeffs[3 * s], b = coeffs[3 * s + 1], c = coeffs[3 * s + 2];
-        product<S, kGram>(g, parts, s & 1, pow2(sc.a - 2 * sc.x), 0.f, stream);
-        product<S, kPoly>(g, parts, s & 1, c * pow2(sc.b - 2 * sc.a), b * pow2(sc.b - sc.a), stream);
+        product<S, kGram>(g, parts, s & 1, pow2(sc.a - 2 * sc.x), 0.f, 0, 0, stream);
+        product<S, kPoly>(g, parts, s & 1, c * pow2(sc.b - 2 * sc.a), b * pow2(sc.b - sc.a), fallen, 0, stream);
         const float mul = pow2(sc.x_next - sc.b - sc.x), add = a * pow2(sc.x_next - sc.x);
         if (s + 1 < steps)
-            product<S, kUpdate>(g, parts, s & 1, mul, add, stream);
+            product<S, kUpdate>(g, parts, s & 1, mul, add, fallen, sc.growth, stream);
         else
-            product<S, kLast>(g, parts, s & 1, mul, add, stream);
+            product<S, kLast>(g, parts, s & 1, mul, add, fallen, 0, stream);
+        fallen += sc.growth;
     }
 }
 
@@ -720,7 +754,7 @@ void small(const OrthoGroup& g, const float* coeffs, const OrthoScales* scales, 
     for (int s = 0; s < steps; ++s) {
         const OrthoScales sc = scales[s];
         it.f[s] = {pow2(sc.a - 2 * sc.x), coeffs[3 * s + 2] * pow2(sc.b - 2 * sc.a), coeffs[3 * s + 1] * pow2(sc.b - sc.a),
-                   pow2(sc.x_next - sc.b - sc.x), coeffs[3 * s] * pow2(sc.x_next - sc.x)};
+                   pow2(sc.x_next - sc.b - sc.x), coeffs[3 * s] * pow2(sc.x_next - sc.x), sc.growth};
     }
     k_small<STEP, BF16><<<g.count, kSmallWaves * 64, 0, stream>>>(g, it, scales[0].x);
 }
