@@ -414,10 +414,11 @@ DSM_API dsm_status dsm_ce_workspace(const dsm_ce_problem* problem, int64_t* work
  * and, where the problem asks for gradients, those of total:
  *   G_tv = c_t (exp(z_tv - lse_t) - [v = y]);  dh = G w;  dw = G^T h
  * dh is 0 for the tokens left out; dh and dw are written, not added to.  The
- * vocabulary is taken in pieces and the logits are never in memory.  Products
- * of bf16 buffers take bf16 operands, with G rounded to bf16; those of fp32
- * buffers carry 22 bits.  Everything else is fp32.  Results do not depend on
- * the order in which the GPU runs: reruns give the same bits.
+ * logits are never in memory, and G is for a piece of the vocabulary at a time, at
+ * most 1 GiB (in 16 bits, or two halves).  Products of bf16 buffers take their bits
+ * and 11 or more of G; those of fp32 buffers carry 22 or more.  Everything else is
+ * fp32.  Results do not depend on the order in which the GPU runs: reruns give the
+ * same bits.
  * Non-finite values in h, w or weight reach every output that depends on them.
  * dh may not overlap h, nor dw w.
  * Errors: DSM_ERR_INVALID_ARG; DSM_ERR_HIP.

@@ -4,13 +4,18 @@
 //   z = h w^T;  lse_t = log sum_v exp z_tv;  loss_t = lse_t - z_t,target
 //   G_tv = c_t (exp(z_tv - lse_t) - [v = target_t]);  dh = G w;  dw = G^T h
 //
-// The logits are never in memory.  A first pass over the vocabulary computes
-// them tile by tile and keeps of each row of a tile its largest logit and the
-// sum of exp(z - largest); joined over the tiles they give lse.  A second pass
-// takes the vocabulary in pieces: it computes a piece's logits again, writes G
-// for the piece (16 bits, or two halves), and multiplies it by w and by h.  So
-// with gradients the matrix cores do 8 T V D operations where keeping all
-// logits would need 6.
+// A first pass over the vocabulary computes the logits tile by tile and keeps of
+// each row of a tile its largest logit and the sum of exp(z - largest); joined over
+// the tiles they give lse.  With gradients, G has to be in memory, for two products
+// read it: it is made for a piece of the vocabulary at a time, at most 1 GiB, in 16
+// bits or two halves an entry.  The logits themselves are never in memory.
+//   * For the first piece, which is most often the only one, the first pass leaves
+//     exp(z - largest of a wave's columns) in G's place, and a light pass multiplies
+//     it by c exp(largest - lse); the target's entry, where p - 1 cancels, it
+//     computes anew.  6 T V D operations of the matrix cores.
+//   * For the others the logits are computed again, 8 T V D in all.
+// 8192 tokens of 50257 x 768 in bf16, whose G is 0.8 GB: 2.87 ms by two pieces, both
+// computed again; 2.28 ms by one.
 //
 // What the products take ("form", chosen by the host from type and tokens):
 //   fp16, scaled     bf16 buffers, many tokens.  A power of two brings an
@@ -321,12 +326,67 @@ __device__ __forceinline__ void logit_tile(int id, int tiles_t, int tiles_v, int
     *tt = group * kRows + id - *tv * rows;
 }
 
-// First pass: each row's largest logit and sum of exp(z - largest) in a tile,
-// and the target's logit.
-template <CeForm FORM, int TM>
+// Four, or eight, neighbouring entries of G, or of what is kept in its place.
+template <CeForm FORM>
+__device__ __forceinline__ void store_g(const CePlan& p, u16* g, int token, int at, const float (&v)[8]) {
+    if constexpr (FORM == kCeF32) {
+        float* out = reinterpret_cast<float*>(g) + token * (p.ld_p / 2) + at;
+        *reinterpret_cast<f4*>(out) = f4{v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<f4*>(out + 4) = f4{v[4], v[5], v[6], v[7]};
+    } else {
+        u16x8 hi, lo;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            if constexpr (FORM == kCeBf16) {
+                hi[r] = float_to_bf16(v[r]);
+                lo[r] = float_to_bf16(v[r] - bf16_to_float(hi[r]));
+            } else {
+                hi[r] = float_to_half(v[r]);
+                lo[r] = float_to_half(v[r] - half_to_float(hi[r]));
+            }
+        }
+        u16* out = g + token * p.ld_p + (FORM == kCeHalves ? ((at >> 5) << 6) + (at & 31) : at);
+        *reinterpret_cast<u16x8*>(out) = hi;
+        if constexpr (FORM == kCeHalves) *reinterpret_cast<u16x8*>(out + 32) = lo;
+        if constexpr (FORM == kCeBf16) *reinterpret_cast<u16x8*>(out + p.p_lo) = lo;
+    }
+}
+template <CeForm FORM>
+__device__ __forceinline__ void load_g(const CePlan& p, const u16* g, int token, int at, float (&v)[8]) {
+    if constexpr (FORM == kCeF32) {
+        const float* in = reinterpret_cast<const float*>(g) + token * (p.ld_p / 2) + at;
+        const f4 a = *reinterpret_cast<const f4*>(in), b = *reinterpret_cast<const f4*>(in + 4);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            v[r] = a[r];
+            v[4 + r] = b[r];
+        }
+    } else {
+        const u16* in = g + token * p.ld_p + (FORM == kCeHalves ? ((at >> 5) << 6) + (at & 31) : at);
+        const u16x8 hi = *reinterpret_cast<const u16x8*>(in);
+        u16x8 lo = {};
+        if constexpr (FORM == kCeHalves) lo = *reinterpret_cast<const u16x8*>(in + 32);
+        if constexpr (FORM == kCeBf16) lo = *reinterpret_cast<const u16x8*>(in + p.p_lo);
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            v[r] = FORM == kCeBf16 ? bf16_to_float(hi[r]) : half_to_float(hi[r]);
+            if constexpr (FORM == kCeHalves) v[r] += half_to_float(lo[r]);
+            if constexpr (FORM == kCeBf16) v[r] += bf16_to_float(lo[r]);
+        }
+    }
+}
+
+// What exponentials are multiplied by where they are kept: fp16's upper range.
+template <CeForm FORM>
+constexpr float kKept = is_scaled(FORM) ? 16384.f : 1.f;
+
+// First pass: each row's largest logit and sum of exp(z - largest) in a tile, and
+// the target's logit.  KEEP also writes exp(z - largest) in G's place for the first
+// piece, the largest being that of a wave's columns (p.run_cols of them), and these.
+template <CeForm FORM, int TM, bool KEEP>
 __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b) {
     using T = typename TokenTile<FORM, TM, kContig, kContig>::T;
-    constexpr int TN = T::kBN;
+    constexpr int TN = T::kBN, kRun = T::FJ * 16;
     __shared__ __align__(1024) char lds[T::kLdsBytes];
     const int tiles_t = (p.tokens + TM - 1) / TM, tiles_v = (p.vocab + TN - 1) / TN;
     int tt, tv;
@@ -338,6 +398,9 @@ __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b)
     const float unit = logit_unit<FORM>(p, b);
     float* hit = reinterpret_cast<float*>(b.workspace + p.hit);
     float2* part = reinterpret_cast<float2*>(lds);  // [T::WN][TM]
+    u16* g = reinterpret_cast<u16*>(b.workspace + p.p);
+    float* tops = reinterpret_cast<float*>(b.workspace + p.tops);
+    const bool keep = KEEP && tv * TN < p.piece;
     int rel[T::FI];  // the target's column in the tile, or -1
 #pragma unroll
     for (int fi = 0; fi < T::FI; ++fi) {
@@ -354,12 +417,12 @@ __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b)
 #pragma unroll
                     for (int fi = 0; fi < T::FI; ++fi) t.acc[fi][fj][r] = -__builtin_inff();
     }
-    const int first_col = t.wj * T::FJ * 16;
+    const int first_col = t.wj * kRun;
 #pragma unroll
     for (int fi = 0; fi < T::FI; ++fi) {
         const int token = tt * TM + t.row(fi);
         // Few waves hold a target's column.
-        if (__any(rel[fi] >= first_col && rel[fi] < first_col + T::FJ * 16)) {
+        if (__any(rel[fi] >= first_col && rel[fi] < first_col + kRun)) {
 #pragma unroll
             for (int fj = 0; fj < T::FJ; ++fj)
 #pragma unroll
@@ -374,17 +437,36 @@ __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b)
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
         top *= unit;
+        // All logits -inf: no exponential counts (and -inf - -inf is none).
+        const float from = top == -__builtin_inff() ? 0.f : top;
         float sum = 0.f;
-        if (top != -__builtin_inff()) {
+        if (keep) {
+#pragma unroll
+            for (int q = 0; q < T::FJ / 2; ++q) {
+                const tile::Eight z = t.eight(fi, q);
+                float e[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(z.v[r], unit, -from));
+                    sum += e[r];
+                    e[r] *= kKept<FORM>;
+                }
+                if (token < p.tokens) store_g<FORM>(p, g, token, tv * TN + t.col8(q), e);
+            }
+        } else {
 #pragma unroll
             for (int fj = 0; fj < T::FJ; ++fj)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    sum += __builtin_amdgcn_exp2f(__builtin_fmaf(t.acc[fi][fj][r], unit, -top));
+                    sum += __builtin_amdgcn_exp2f(__builtin_fmaf(t.acc[fi][fj][r], unit, -from));
         }
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
-        if (t.lane < 16) part[t.wj * TM + t.row(fi)] = make_float2(top, sum);
+        if (t.lane < 16) {
+            part[t.wj * TM + t.row(fi)] = make_float2(top, sum);
+            if (keep && token < p.tokens)
+                tops[static_cast<int64_t>(token) * (p.piece / kRun) + (tv * TN + first_col) / kRun] = top;
+        }
     }
     __syncthreads();
     float2* stats = reinterpret_cast<float2*>(b.workspace + p.stats) + static_cast<int64_t>(tv) * p.tokens;
@@ -395,6 +477,35 @@ __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b)
         for (int w = 1; w < T::WN; ++w) a = joined(a, part[w * TM + r]);
         stats[tt * TM + r] = a;
     }
+}
+
+// The kept exponentials become G of the first piece: eight columns a lane, 2048 of a
+// row a work-group.
+template <CeForm FORM>
+__global__ __launch_bounds__(256) void k_settle(CePlan p, CeBuffers b) {
+    const int per_row = (p.piece + 2047) / 2048, token = blockIdx.x / per_row;
+    const int at = ((blockIdx.x - token * per_row) * 256 + threadIdx.x) * 8;
+    if (at >= p.piece) return;
+    const float lse = reinterpret_cast<const float*>(b.workspace + p.lse)[token];
+    const int eg = !is_scaled(FORM) ? 0 : exponent_for(reinterpret_cast<const Scalars*>(b.workspace + p.scalars)->c_max);
+    const float c = ldexpf(reinterpret_cast<const float*>(b.workspace + p.coef)[token], eg);
+    const int64_t target = b.target[token];
+    const bool valid = is_valid(target, p.vocab);
+    u16* g = reinterpret_cast<u16*>(b.workspace + p.p);
+    const int64_t run = static_cast<int64_t>(token) * (p.piece / p.run_cols) + at / p.run_cols;
+    const float top = reinterpret_cast<const float*>(b.workspace + p.tops)[run];
+    float v[8];
+    load_g<FORM>(p, g, token, at, v);
+    const float by = valid ? c * (1.f / kKept<FORM>) * __builtin_amdgcn_exp2f(top - lse) : 0.f;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) v[r] = valid ? v[r] * by : 0.f;
+    if (valid && target >= at && target < at + 8) {
+        const float p1 = __builtin_amdgcn_exp2f(reinterpret_cast<const float*>(b.workspace + p.hit)[token] - lse) - 1.f;
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+            if (target == at + r) v[r] = c * p1;
+    }
+    store_g<FORM>(p, g, token, at, v);
 }
 
 // lse and loss of 16 tokens by a work-group: 64 lanes share a token's tiles.  With
@@ -511,28 +622,7 @@ __global__ __launch_bounds__(threads_of(TM)) void k_piece(CePlan p, CeBuffers b,
                 v[r] *= c[fi];
                 if (ragged && at + r >= cols) v[r] = 0.f;
             }
-            if (at >= cols_pad) continue;
-            if constexpr (FORM == kCeF32) {
-                float* out = reinterpret_cast<float*>(g) + token * (p.ld_p / 2) + at;
-                *reinterpret_cast<f4*>(out) = f4{v[0], v[1], v[2], v[3]};
-                *reinterpret_cast<f4*>(out + 4) = f4{v[4], v[5], v[6], v[7]};
-            } else {
-                u16x8 hi, lo;
-#pragma unroll
-                for (int r = 0; r < 8; ++r) {
-                    if constexpr (FORM == kCeBf16) {
-                        hi[r] = float_to_bf16(v[r]);
-                        lo[r] = float_to_bf16(v[r] - bf16_to_float(hi[r]));
-                    } else {
-                        hi[r] = float_to_half(v[r]);
-                        lo[r] = float_to_half(v[r] - half_to_float(hi[r]));
-                    }
-                }
-                u16* out = g + token * p.ld_p + (FORM == kCeHalves ? ((at >> 5) << 6) + (at & 31) : at);
-                *reinterpret_cast<u16x8*>(out) = hi;
-                if constexpr (FORM == kCeHalves) *reinterpret_cast<u16x8*>(out + 32) = lo;
-                if constexpr (FORM == kCeBf16) *reinterpret_cast<u16x8*>(out + p.p_lo) = lo;
-            }
+            if (at < cols_pad) store_g<FORM>(p, g, token, at, v);
         }
     }
 }
@@ -736,15 +826,22 @@ template <CeForm FORM, int TM>
 void products(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
     constexpr int kThreads = threads_of(TM), TN = square_of(TM);
     const int tt = (p.tokens + TM - 1) / TM, td = (p.dim + TN - 1) / TN, tv = (p.vocab + TN - 1) / TN;
-    k_stats<FORM, TM><<<tt * tv, kThreads, 0, stream>>>(p, b);
+    if constexpr (FORM != kCeBf16 || TM < 256) {  // (many tokens with gradients take fp16)
+        if (p.grads) k_stats<FORM, TM, true><<<tt * tv, kThreads, 0, stream>>>(p, b);
+    }
+    if (!p.grads) k_stats<FORM, TM, false><<<tt * tv, kThreads, 0, stream>>>(p, b);
     k_join<<<(p.tokens + kJoinTokens - 1) / kJoinTokens, 1024, 0, stream>>>(p, b, tv);
     if (p.tokens > kJoinTokens) k_total<<<1, 1024, 0, stream>>>(p, b);
-    if constexpr (FORM != kCeBf16 || TM < 256) {  // (many tokens with gradients take fp16)
+    if constexpr (FORM != kCeBf16 || TM < 256) {
         if (!p.grads) return;
         for (int first = 0; first < p.vocab; first += p.piece) {
             const int cols = p.vocab - first < p.piece ? p.vocab - first : p.piece;
             const int tp = (cols + TN - 1) / TN;
-            k_piece<FORM, TM><<<tt * tp, kThreads, 0, stream>>>(p, b, first, cols);
+            if (first == 0) {
+                k_settle<FORM><<<p.tokens * ((p.piece + 2047) / 2048), 256, 0, stream>>>(p, b);
+            } else {
+                k_piece<FORM, TM><<<tt * tp, kThreads, 0, stream>>>(p, b, first, cols);
+            }
             const int dh_tiles = tt * td * p.dh_splits, dw_tiles = tp * td;
             if constexpr (TM >= 128) {
                 k_gradients<FORM, TM><<<kXcds * (per_xcd(dh_tiles) + per_xcd(dw_tiles)), kThreads, 0, stream>>>(

@@ -54,8 +54,9 @@ dsm_status check_workspace(const void* ws, int64_t bytes, int64_t need) {
 
 // ---- Linear layer with softmax cross entropy ----
 
-// G of a piece takes at most this much memory.
-constexpr int64_t kPieceBytes = int64_t(512) << 20;
+// G of a piece takes at most this much memory.  (8192 tokens of 50257 x 768 in bf16
+// take 0.8 GB for all of it; by two pieces half of the logits are computed twice.)
+constexpr int64_t kPieceBytes = int64_t(1) << 30;
 constexpr int kMaxSplits = 128;
 
 // How the second pass is cut: pieces of the vocabulary, and parts of a piece's
@@ -86,7 +87,8 @@ void cut(dsm::CePlan* q, int64_t T, int64_t D, int64_t V) {
             const double work = (static_cast<double>(t * d * s) * dh_tile + static_cast<double>(per * d) * dw_tile) / slots;
             const double both = std::max(work, std::max(dh_tile, dw_tile)) + 0.5 * std::max(dh_tile, dw_tile) +
                                 s * dh_pass * (n > 1 ? 2 : 1);
-            const double cost = static_cast<double>(n) * (logits + both + 6.0) + s * dh_pass;
+            // (The first piece's logits are there.)
+            const double cost = static_cast<double>(n - 1) * logits + static_cast<double>(n) * (both + 6.0) + s * dh_pass;
             if (best == 0.0 || cost < best) {
                 best = cost;
                 q->piece = static_cast<int32_t>(per * square);
@@ -151,6 +153,8 @@ dsm::CePlan make_plan(const dsm_ce_problem* p) {
     q.w = take(V * q.ld_w * 2);
     if (p->grads && T > 0) {
         cut(&q, T, p->dim, V);
+        q.run_cols = q.tile == 256 ? 64 : 32;
+        q.tops = take(T * (q.piece / q.run_cols) * 4);
         // (In the bf16 form G is two arrays of halves.)
         q.p_lo = T * q.ld_p;
         q.p = take(T * q.ld_p * (q.form == dsm::kCeBf16 ? 4 : 2));

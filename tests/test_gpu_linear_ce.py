@@ -83,9 +83,10 @@ def test_losses_alone(size, dtype):
     _run_and_check(h, w, t, weight, size[0] % 2 == 0, False)
 
 
+@pytest.mark.parametrize("times", [1, 2])  # G in one piece of at most 1 GiB, and in two
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
-def test_several_pieces_of_the_vocabulary(dtype):
-    tokens, dim, vocab = (4200 if dtype == BF16 else 2100), 64, 70001
+def test_several_pieces_of_the_vocabulary(dtype, times):
+    tokens, dim, vocab = times * (4200 if dtype == BF16 else 2100), 64, 70001
     h, w, t, weight = _problem(tokens, dim, vocab, dtype, seed=3)
     ops = _ops()
     out = ops.LinearCE(tokens, dim, vocab, dtype=dtype)(h, w, t, weight=weight)
