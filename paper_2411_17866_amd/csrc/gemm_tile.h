@@ -286,14 +286,14 @@ struct Tile {
             for (int j = 0; j < FJ; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
     }
     __device__ __forceinline__ void run(const Operand& oi, const Operand& oj, int64_t i0, int64_t j0,
-                                        int k_begin, int k_end, DSM_LDS char* lds) {
+                                        int k_begin, int k_end, DSM_LDS char* lds, int = 0, int = 0) {
         clear();
         add(oi, oj, i0, j0, k_begin, k_end, lds);
     }
     // Adds the products of steps [k_begin, k_end); k_begin is a multiple of kSteps,
     // and what lies between k_end and the next multiple is zero in one operand.
     __device__ __forceinline__ void add(const Operand& oi, const Operand& oj, int64_t i0, int64_t j0,
-                                        int k_begin, int k_end, DSM_LDS char* lds) {
+                                        int k_begin, int k_end, DSM_LDS char* lds, int = 0, int = 0) {
         SideI si;
         SideJ sj;
         si.init(oi, i0, lane, wave);
@@ -337,6 +337,8 @@ struct Tile {
     }
     static __device__ __forceinline__ void fence() { asm volatile("" ::: "memory"); }
 
+    // Whether no row of the fragments from fi on is wanted.
+    __device__ __forceinline__ bool idle(int) const { return false; }
     // i and j of acc[fi][fj][r] inside the tile.
     __device__ __forceinline__ int row(int fi) const { return (wi * FI + fi) * 16 + (lane & 15); }
     __device__ __forceinline__ int col(int fj) const { return (wj * FJ + fj) * 16 + (lane >> 4) * 4; }
@@ -346,9 +348,8 @@ struct Tile {
 };
 
 // One side of a big tile (BigTile below): two half tiles of 128 rows (or
-// columns), each a buffer of its own in LDS.  Half h holds, of every wave's
-// 2 * HW rows, the HW from h * HW on.
-template <int HW, Kind KIND, int S>
+// columns), each a buffer of its own in LDS.
+template <Kind KIND, int S>
 struct HalfSide {
     static constexpr int kRows = 128;
     static constexpr int kBytes = kRows * 128;
@@ -363,8 +364,6 @@ struct HalfSide {
     int32_t k_rows, last_col;
 
     static __device__ __forceinline__ int swz(int k) { return (k & 3) | ((k >> 1) & 4); }
-    // Row (or column) of the tile that row r of half h is.
-    static __device__ __forceinline__ int source(int r, int h) { return r / HW * (2 * HW) + h * HW + r % HW; }
 
     __device__ __forceinline__ void init(const Operand& o, int64_t first, int lane, int wave) {
         ld_bytes = o.ld * 2;
@@ -377,7 +376,7 @@ struct HalfSide {
                 for (int q = 0; q < kLoads; ++q) {
                     const int r = (q * kWaves + wave) * 8 + (lane >> 3);
                     const int chunk = (lane & 7) ^ (r & 7);
-                    off[h][q] = static_cast<uint32_t>(min(source(r, h), last)) * static_cast<uint32_t>(ld_bytes) +
+                    off[h][q] = static_cast<uint32_t>(min(h * kRows + r, last)) * static_cast<uint32_t>(ld_bytes) +
                                 chunk * 16;
                 }
         } else {
@@ -395,9 +394,7 @@ struct HalfSide {
         const int k = byte / kRowBytes;
         const int slot = (byte % kRowBytes) >> 4;
         const int at = (((slot >> 1) ^ swz(k)) << 1) | (slot & 1);  // 16-byte column of the half tile
-        // 16-byte columns come in runs of HW columns of the tile.
-        constexpr int kRun = HW * S / 8;
-        const int col = (at / kRun * (2 * kRun) + h * kRun + at % kRun) * 16;
+        const int col = h * kRowBytes + at * 16;
         return static_cast<uint32_t>(min(k, k_max)) * static_cast<uint32_t>(ld_bytes) + min(col, last_col);
     }
     // Starts this wave's loads of half h of the stage at step k0.
@@ -425,7 +422,9 @@ struct HalfSide {
     }
 };
 
-// A 256 x 256 tile by 8 waves (2 x 4, each 128 x 64), two waves on each SIMD.
+// A 256 x 256 tile by 8 waves, two on each SIMD.  A wave has 64 rows and 32 columns
+// of each 128 x 128 quarter, so that a quarter where nothing is wanted (past the
+// matrix's last row or column) costs no wave a matrix instruction.
 //
 // The two waves of a SIMD take turns: while one feeds the matrix core the other
 // reads fragments from LDS and starts global loads, then they change over at a
@@ -455,16 +454,20 @@ struct BigTile {
     static constexpr int S = units(E);
     static constexpr int kBM = 256, kBN = 256, kThreads = 512;
     static constexpr int WN = 4, FI = 8, FJ = 4;
-    using SideI = HalfSide<64, KI, S>;
-    using SideJ = HalfSide<32, KJ, S>;
+    using SideI = HalfSide<KI, S>;
+    using SideJ = HalfSide<KJ, S>;
     static constexpr int kSteps = SideI::kSteps;
     static constexpr int kHalf = SideI::kBytes;
     static constexpr bool kAhead = S == 1;  // J0 is read a turn before its stage
+    // Quarters without wanted rows or columns are left out by loops of their own.  (A
+    // branch in the loop, or these loops beside k-strided loads, spill registers.)
+    static constexpr bool kQuarters = KI == kContig && KJ == kContig;
     static constexpr int kStageBytes = 4 * kHalf;  // J0, I0, J1, I1
     static constexpr int kLdsBytes = 2 * kStageBytes;
 
     f4 acc[FI][FJ];
     int lane, wave, wi, wj;
+    bool tall, wide;  // more than 128 rows, columns are wanted
     short8v fi[4][2], j0[kAhead ? 2 : 1][2][2], j1[2][2];  // j0: this stage's and the next one's
 
     static __device__ __forceinline__ void fence() {
@@ -495,7 +498,8 @@ struct BigTile {
 #pragma unroll
             for (int f = 0; f < 2; ++f) to[f][part] = SideJ::fragment(half, wj * 2 + f, part, lane);
     }
-    template <int H>
+    // The first N fragments of columns by half H of the rows.
+    template <int H, int N>
     __device__ __forceinline__ void multiply(const short8v (&front)[2][2]) {
         fence();
         __builtin_amdgcn_s_setprio(1);
@@ -506,7 +510,7 @@ struct BigTile {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
+                for (int j = 0; j < N; ++j)
                     acc[H * 4 + i][j] = mfma<E>(j < 2 ? front[j][pj] : j1[j - 2][pj], fi[i][pi], acc[H * 4 + i][j]);
         }
         __builtin_amdgcn_s_setprio(0);
@@ -523,13 +527,16 @@ struct BigTile {
 #pragma unroll
             for (int j = 0; j < FJ; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
     }
+    // Of the tile rows x cols are wanted.
     __device__ __forceinline__ void run(const Operand& oi, const Operand& oj, int64_t first_i, int64_t first_j,
-                                        int k_begin, int k_end, DSM_LDS char* lds) {
+                                        int k_begin, int k_end, DSM_LDS char* lds, int rows, int cols) {
         clear();
-        add(oi, oj, first_i, first_j, k_begin, k_end, lds);
+        add(oi, oj, first_i, first_j, k_begin, k_end, lds, rows, cols);
     }
     __device__ __forceinline__ void add(const Operand& oi, const Operand& oj, int64_t first_i, int64_t first_j,
-                                        int k_begin, int k_end, DSM_LDS char* lds) {
+                                        int k_begin, int k_end, DSM_LDS char* lds, int rows, int cols) {
+        tall = rows > 128;
+        wide = cols > 128;
         if (k_begin >= k_end) return;
         SideI si;
         SideJ sj;
@@ -553,21 +560,33 @@ struct BigTile {
             turn_over();  // J0 is read: its next load may start
         }
         if (wave >= 4) turn_over();
-        for (int k = k_begin;;) {
-            stage<0>(si, sj, k, k_end, lds);
-            if ((k += kSteps) >= k_end) break;
-            stage<1>(si, sj, k, k_end, lds);
-            if ((k += kSteps) >= k_end) break;
-        }
+        if (!kQuarters || (tall && wide))
+            stages<2, 4>(si, sj, k_begin, k_end, lds);
+        else if (tall)
+            stages<2, 2>(si, sj, k_begin, k_end, lds);
+        else if (wide)
+            stages<1, 4>(si, sj, k_begin, k_end, lds);
+        else
+            stages<1, 2>(si, sj, k_begin, k_end, lds);
         if (wave < 4) turn_over();
         turn_over();  // every wave is done with LDS
+    }
+    // HALVES of the rows by N fragments of a wave's columns.
+    template <int HALVES, int N>
+    __device__ __forceinline__ void stages(SideI& si, SideJ& sj, int k, int k_end, DSM_LDS char* lds) {
+        for (;;) {
+            stage<0, HALVES, N>(si, sj, k, k_end, lds);
+            if ((k += kSteps) >= k_end) break;
+            stage<1, HALVES, N>(si, sj, k, k_end, lds);
+            if ((k += kSteps) >= k_end) break;
+        }
     }
     __device__ __forceinline__ void load_middle(SideI& si, SideJ& sj, int k, DSM_LDS char* st) {
         si.template issue<0>(k, st + kHalf, lane, wave);
         sj.template issue<1>(k, st + 2 * kHalf, lane, wave);
     }
     // The stage at step k, in buffer B.
-    template <int B>
+    template <int B, int HALVES, int N>
     __device__ __forceinline__ void stage(SideI& si, SideJ& sj, int k, int k_end, DSM_LDS char* lds) {
         DSM_LDS char* st = lds + B * kStageBytes;
         DSM_LDS char* other = lds + (B ^ 1) * kStageBytes;
@@ -575,7 +594,7 @@ struct BigTile {
         constexpr int kNow = kAhead ? B : 0;
         if constexpr (!kAhead) read_j(st, j0[0]);
         read_i(st + kHalf);
-        read_j(st + 2 * kHalf, j1);
+        if constexpr (N > 2) read_j(st + 2 * kHalf, j1);
         if (next) si.template issue<1>(k + kSteps, other + 3 * kHalf, lane, wave);
         if (kAhead ? more : next) {
             if constexpr (kAhead) sj.template issue<0>(k + 2 * kSteps, st, lane, wave);
@@ -584,9 +603,9 @@ struct BigTile {
             wait<0>();
         }
         turn_over();
-        multiply<0>(j0[kNow]);
+        multiply<0, N>(j0[kNow]);
         turn_over();
-        read_i(st + 3 * kHalf);
+        if constexpr (HALVES > 1) read_i(st + 3 * kHalf);
         if constexpr (kAhead) {
             if (next) read_j(other, j0[B ^ 1]);
         }
@@ -598,16 +617,17 @@ struct BigTile {
             wait<0>();
         }
         turn_over();
-        multiply<1>(j0[kNow]);
+        if constexpr (HALVES > 1) multiply<1, N>(j0[kNow]);
         turn_over();
     }
 
     // i and j of acc[fi][fj][r] inside the tile.
-    __device__ __forceinline__ int row(int f) const { return wi * 128 + f * 16 + (lane & 15); }
-    __device__ __forceinline__ int col(int f) const { return wj * 64 + f * 16 + (lane >> 4) * 4; }
+    __device__ __forceinline__ int row(int f) const { return (f >> 2) * 128 + wi * 64 + (f & 3) * 16 + (lane & 15); }
+    __device__ __forceinline__ int col(int f) const { return (f >> 1) * 128 + wj * 32 + (f & 1) * 16 + (lane >> 4) * 4; }
     // Fragments 2 p and 2 p + 1 of row(fi), and their first column.
     __device__ __forceinline__ Eight eight(int f, int p) const { return join(acc[f][2 * p], acc[f][2 * p + 1]); }
-    __device__ __forceinline__ int col8(int p) const { return wj * 64 + p * 32 + joined_col(lane); }
+    __device__ __forceinline__ int col8(int p) const { return p * 128 + wj * 32 + joined_col(lane); }
+    __device__ __forceinline__ bool idle(int f) const { return f >= 4 && !tall; }
 };
 
 // A BM x BM tile of 16-bit values in LDS (rows of BM * 2 bytes, their 32-byte

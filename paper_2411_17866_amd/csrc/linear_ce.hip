@@ -281,7 +281,7 @@ template <CeForm FORM, tile::Kind KI, tile::Kind KJ>
 struct TokenTile<FORM, 256, KI, KJ> {
     using T = tile::Pick<elem(FORM), 256, KI, KJ>;
 };
-constexpr int square_of(int tm) { return tm == 256 ? 256 : 128; }
+__host__ __device__ constexpr int square_of(int tm) { return tm == 256 ? 256 : 128; }
 constexpr int threads_of(int tm) { return tm >= 128 ? 512 : 256; }
 
 __device__ __forceinline__ Operand h_rows(const CePlan& p, const CeBuffers& b) {
@@ -376,24 +376,27 @@ __device__ __forceinline__ void load_g(const CePlan& p, const u16* g, int token,
     }
 }
 
+// Which of the four columns of waves has column j of a tile.
+__device__ __forceinline__ int wave_of(int j) { return (j >> 5) & 3; }
+
 // What exponentials are multiplied by where they are kept: fp16's upper range.
 template <CeForm FORM>
 constexpr float kKept = is_scaled(FORM) ? 16384.f : 1.f;
 
 // First pass: each row's largest logit and sum of exp(z - largest) in a tile, and
 // the target's logit.  KEEP also writes exp(z - largest) in G's place for the first
-// piece, the largest being that of a wave's columns (p.run_cols of them), and these.
+// piece, the largest being that of a wave's columns of the tile (wave_of), and these.
 template <CeForm FORM, int TM, bool KEEP>
 __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b) {
     using T = typename TokenTile<FORM, TM, kContig, kContig>::T;
-    constexpr int TN = T::kBN, kRun = T::FJ * 16;
+    constexpr int TN = T::kBN;
     __shared__ __align__(1024) char lds[T::kLdsBytes];
     const int tiles_t = (p.tokens + TM - 1) / TM, tiles_v = (p.vocab + TN - 1) / TN;
     int tt, tv;
     logit_tile(xcd_run(blockIdx.x, tiles_t * tiles_v), tiles_t, tiles_v, &tt, &tv);
     T t;
     t.run(h_rows(p, b), w_rows(p, b, 0), tt * TM, tv * TN, 0, static_cast<int>(p.ld_h / units(FORM)),
-          (DSM_LDS char*)lds);
+          (DSM_LDS char*)lds, p.tokens - tt * TM, p.vocab - tv * TN);
     // In units of log2: z2 = acc * unit, exp(z) = exp2(z2).
     const float unit = logit_unit<FORM>(p, b);
     float* hit = reinterpret_cast<float*>(b.workspace + p.hit);
@@ -417,12 +420,11 @@ __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b)
 #pragma unroll
                     for (int fi = 0; fi < T::FI; ++fi) t.acc[fi][fj][r] = -__builtin_inff();
     }
-    const int first_col = t.wj * kRun;
 #pragma unroll
     for (int fi = 0; fi < T::FI; ++fi) {
         const int token = tt * TM + t.row(fi);
         // Few waves hold a target's column.
-        if (__any(rel[fi] >= first_col && rel[fi] < first_col + kRun)) {
+        if (__any(rel[fi] >= 0 && rel[fi] < TN && wave_of(rel[fi]) == t.wj)) {
 #pragma unroll
             for (int fj = 0; fj < T::FJ; ++fj)
 #pragma unroll
@@ -465,7 +467,7 @@ __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b)
         if (t.lane < 16) {
             part[t.wj * TM + t.row(fi)] = make_float2(top, sum);
             if (keep && token < p.tokens)
-                tops[static_cast<int64_t>(token) * (p.piece / kRun) + (tv * TN + first_col) / kRun] = top;
+                tops[static_cast<int64_t>(token) * (p.piece / TN * 4) + tv * 4 + t.wj] = top;
         }
     }
     __syncthreads();
@@ -492,7 +494,8 @@ __global__ __launch_bounds__(256) void k_settle(CePlan p, CeBuffers b) {
     const int64_t target = b.target[token];
     const bool valid = is_valid(target, p.vocab);
     u16* g = reinterpret_cast<u16*>(b.workspace + p.p);
-    const int64_t run = static_cast<int64_t>(token) * (p.piece / p.run_cols) + at / p.run_cols;
+    const int square = square_of(p.tile);
+    const int64_t run = static_cast<int64_t>(token) * (p.piece / square * 4) + at / square * 4 + wave_of(at);
     const float top = reinterpret_cast<const float*>(b.workspace + p.tops)[run];
     float v[8];
     load_g<FORM>(p, g, token, at, v);
@@ -577,7 +580,7 @@ __global__ __launch_bounds__(threads_of(TM)) void k_piece(CePlan p, CeBuffers b,
     logit_tile(xcd_run(blockIdx.x, tiles_t * tiles_v), tiles_t, tiles_v, &tt, &tv);
     T t;
     t.run(h_rows(p, b), w_rows(p, b, first), tt * TM, tv * TN, 0, static_cast<int>(p.ld_h / units(FORM)),
-          (DSM_LDS char*)lds);
+          (DSM_LDS char*)lds, p.tokens - tt * TM, cols - tv * TN);
     const float unit = logit_unit<FORM>(p, b);
     const int eg = !is_scaled(FORM) ? 0 : exponent_for(reinterpret_cast<const Scalars*>(b.workspace + p.scalars)->c_max);
     const float* lse = reinterpret_cast<const float*>(b.workspace + p.lse);
@@ -597,12 +600,11 @@ __global__ __launch_bounds__(threads_of(TM)) void k_piece(CePlan p, CeBuffers b,
         c[fi] = valid ? ldexpf(coef[at], eg) : 0.f;
     }
     const bool ragged = tv * TN + TN > cols;
-    const int first_col = t.wj * T::FJ * 16;
 #pragma unroll
     for (int fi = 0; fi < T::FI; ++fi) {
         const int token = tt * TM + t.row(fi);
         // Few waves hold a target's column.
-        const bool hits = __any(rel[fi] >= first_col && rel[fi] < first_col + T::FJ * 16);
+        const bool hits = __any(rel[fi] >= 0 && rel[fi] < TN && wave_of(rel[fi]) == t.wj);
         if (token >= p.tokens) continue;
 #pragma unroll
         for (int q = 0; q < T::FJ / 2; ++q) {
@@ -651,9 +653,9 @@ __device__ __forceinline__ void dh_tile(const CePlan& p, const CeBuffers& b, int
     const int k0 = min(part * each, cols_pad), k1 = min(k0 + each, cols_pad);
     T t;
     t.clear();
-    t.add(g_rows(p, b), w_rows(p, b, first), tt * TM, td * TN, k0, k1, lds);
+    t.add(g_rows(p, b), w_rows(p, b, first), tt * TM, td * TN, k0, k1, lds, p.tokens - tt * TM, p.dim - td * TN);
     if constexpr (FORM == kCeBf16)
-        t.add(g_rows<true>(p, b), w_rows(p, b, first), tt * TM, td * TN, k0, k1, lds);
+        t.add(g_rows<true>(p, b), w_rows(p, b, first), tt * TM, td * TN, k0, k1, lds, p.tokens - tt * TM, p.dim - td * TN);
     float* out = reinterpret_cast<float*>(b.workspace + p.dh) + part * p.tokens * p.ld_dh;
     const int ld = static_cast<int>(p.ld_dh);
     constexpr int kBatch = T::FI < 4 ? T::FI : 4;
@@ -749,9 +751,9 @@ __device__ __forceinline__ void dw_tile(const CePlan& p, const CeBuffers& b, int
     const int rows_pad = (p.tokens + kSteps - 1) / kSteps * kSteps;
     T t;
     t.clear();
-    t.add(g_rows(p, b), h_rows(p, b), tv * BM, td * BM, 0, rows_pad, lds);
+    t.add(g_rows(p, b), h_rows(p, b), tv * BM, td * BM, 0, rows_pad, lds, cols - tv * BM, p.dim - td * BM);
     if constexpr (FORM == kCeBf16)
-        t.add(g_rows<true>(p, b), h_rows(p, b), tv * BM, td * BM, 0, rows_pad, lds);
+        t.add(g_rows<true>(p, b), h_rows(p, b), tv * BM, td * BM, 0, rows_pad, lds, cols - tv * BM, p.dim - td * BM);
     int ex = 0;
     if constexpr (is_scaled(FORM)) {
         const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);

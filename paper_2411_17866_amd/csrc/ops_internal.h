@@ -67,7 +67,6 @@ struct CePlan {
     int32_t tile;        // tokens of a work-group's tile: 32, 64, 128 or 256
     int32_t piece;       // columns of the vocabulary whose gradients are in memory at once
     int32_t dh_splits;   // parts of a piece that dh is summed over side by side
-    int32_t run_cols;    // columns of a wave of the first pass, which share a largest logit
     int64_t scalars, coef, lse, hit, stats, tops, h, w, p, dh, bytes;
     int64_t ld_h, ld_w, ld_p;  // 16-bit elements of a row
     int64_t p_lo;              // bf16 form: from G's upper halves to its lower ones

@@ -153,8 +153,7 @@ dsm::CePlan make_plan(const dsm_ce_problem* p) {
     q.w = take(V * q.ld_w * 2);
     if (p->grads && T > 0) {
         cut(&q, T, p->dim, V);
-        q.run_cols = q.tile == 256 ? 64 : 32;
-        q.tops = take(T * (q.piece / q.run_cols) * 4);
+        q.tops = take(T * (q.piece / square) * 4 * 4);  // four columns of waves a tile
         // (In the bf16 form G is two arrays of halves.)
         q.p_lo = T * q.ld_p;
         q.p = take(T * q.ld_p * (q.form == dsm::kCeBf16 ? 4 : 2));

@@ -323,7 +323,7 @@ __global__ __launch_bounds__(tile::threads_of(BM)) void k_product(OrthoGroup g, 
     const Operand ox{X, ldx, m, np * S}, oa{A, lda, m, mp * S}, ob{B, lda, m, mp * S};
     T t;
     t.run(P == kGram ? ox : P == kPoly ? oa : ob, P == kPoly ? oa : ox, ti * BM, tj * BM, 0,
-          P == kGram ? np : mp, (DSM_LDS char*)lds);
+          P == kGram ? np : mp, (DSM_LDS char*)lds, m - ti * BM, (kSymmetric ? m : n) - tj * BM);
 
     // X is stored times 2^lift more, and after this iteration 2^after.
     const int lift = max(*reinterpret_cast<const int*>(ws + lift_at()) - fallen, 0);
@@ -346,6 +346,7 @@ __global__ __launch_bounds__(tile::threads_of(BM)) void k_product(OrthoGroup g, 
     const int last_col = (P == kPoly ? mp : np) - 8;
 #pragma unroll
     for (int f0 = 0; f0 < T::FI; f0 += kBatch) {
+        if (!kSymmetric && t.idle(f0)) break;
         u16x8 oh[kBatch][kPairs], ol[kBatch][kPairs];
         if constexpr (P != kGram) {
 #pragma unroll

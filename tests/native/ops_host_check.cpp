@@ -119,12 +119,11 @@ static void check_plan(const dsm_ce_problem& p, const dsm::CePlan& q, int64_t ws
         CHECK(q.ld_p == q.piece * units && q.ld_dh >= D && q.ld_dh % 4 == 0);
         const int64_t g = T * q.ld_p * 2;
         if (q.form == dsm::kCeBf16) CHECK(q.p_lo == T * q.ld_p);
-        CHECK(q.run_cols == (q.tile == 256 ? 64 : 32));
         const int64_t all = q.form == dsm::kCeBf16 ? 2 * g : g;
         CHECK(all <= (int64_t(1) << 30) || q.piece == square);
         // A launch has a group for each 2048 columns of each row.
         CHECK(T * ((q.piece + 2047) / 2048) < (int64_t(1) << 31));
-        parts.push_back({q.tops, T * (q.piece / q.run_cols) * 4});
+        parts.push_back({q.tops, T * (q.piece / square) * 16});
         parts.push_back({q.p, all});
         parts.push_back({q.dh, q.dh_splits * T * q.ld_dh * 4});
     }
