@@ -17,6 +17,16 @@
 // 8192 tokens of 50257 x 768 in bf16, whose G is 0.8 GB: 2.87 ms by two pieces, both
 // computed again; 2.28 ms by one.
 //
+// The light pass itself is saved, with many tokens and a large vocabulary, by a
+// reference r_t for each row that is near lse_t and known before the first pass: the
+// logarithm of the sum over a few tiles of the vocabulary, a turn of the CUs, scaled
+// to all of it.  Exponentials are then kept relative to r_t and stay as they are:
+//   G_tv = s_t E_tv,  E_tv = exp(z_tv - x_t) - [v = target] exp(lse_t - x_t),
+//   s_t = c_t exp(x_t - lse_t),  x_t a constant below r_t
+// dh's sums are multiplied by s_t where they are joined, and dw is the product of E
+// with s_t h_t, which is written transposed on the way.  Only a row whose lse_t turns
+// out too far from r_t for fp16's range is passed over once more.
+//
 // What the products take ("form", chosen by the host from type and tokens):
 //   fp16, scaled     bf16 buffers, many tokens.  A power of two brings an
 //                    operand's largest finite entry just under fp16's largest
@@ -198,7 +208,9 @@ __global__ __launch_bounds__(256) void k_largest(CePlan p, CeBuffers b) {
     if (threadIdx.x == 0) {
         top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
         Scalars* s = reinterpret_cast<Scalars*>(b.workspace + p.scalars);
-        if (top) atomicMax(of_w ? &s->w_max : &s->h_max, top);
+        uint32_t* to = of_w ? &s->w_max : &s->h_max;
+        // (Atomics on one address take turns: most groups see that theirs is not needed.)
+        if (top > __hip_atomic_load(to, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(to, top);
     }
 }
 
@@ -326,11 +338,11 @@ __device__ __forceinline__ void logit_tile(int id, int tiles_t, int tiles_v, int
     *tt = group * kRows + id - *tv * rows;
 }
 
-// Four, or eight, neighbouring entries of G, or of what is kept in its place.
+// Eight neighbouring entries of a row of G, or of what is kept in its place.
 template <CeForm FORM>
-__device__ __forceinline__ void store_g(const CePlan& p, u16* g, int token, int at, const float (&v)[8]) {
+__device__ __forceinline__ void store_g(const CePlan& p, u16* row, int at, const float (&v)[8]) {
     if constexpr (FORM == kCeF32) {
-        float* out = reinterpret_cast<float*>(g) + token * (p.ld_p / 2) + at;
+        float* out = reinterpret_cast<float*>(row) + at;
         *reinterpret_cast<f4*>(out) = f4{v[0], v[1], v[2], v[3]};
         *reinterpret_cast<f4*>(out + 4) = f4{v[4], v[5], v[6], v[7]};
     } else {
@@ -345,16 +357,16 @@ __device__ __forceinline__ void store_g(const CePlan& p, u16* g, int token, int 
                 lo[r] = float_to_half(v[r] - half_to_float(hi[r]));
             }
         }
-        u16* out = g + token * p.ld_p + (FORM == kCeHalves ? ((at >> 5) << 6) + (at & 31) : at);
+        u16* out = row + (FORM == kCeHalves ? ((at >> 5) << 6) + (at & 31) : at);
         *reinterpret_cast<u16x8*>(out) = hi;
         if constexpr (FORM == kCeHalves) *reinterpret_cast<u16x8*>(out + 32) = lo;
         if constexpr (FORM == kCeBf16) *reinterpret_cast<u16x8*>(out + p.p_lo) = lo;
     }
 }
 template <CeForm FORM>
-__device__ __forceinline__ void load_g(const CePlan& p, const u16* g, int token, int at, float (&v)[8]) {
+__device__ __forceinline__ void load_g(const CePlan& p, const u16* row, int at, float (&v)[8]) {
     if constexpr (FORM == kCeF32) {
-        const float* in = reinterpret_cast<const float*>(g) + token * (p.ld_p / 2) + at;
+        const float* in = reinterpret_cast<const float*>(row) + at;
         const f4 a = *reinterpret_cast<const f4*>(in), b = *reinterpret_cast<const f4*>(in + 4);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
@@ -362,7 +374,7 @@ __device__ __forceinline__ void load_g(const CePlan& p, const u16* g, int token,
             v[4 + r] = b[r];
         }
     } else {
-        const u16* in = g + token * p.ld_p + (FORM == kCeHalves ? ((at >> 5) << 6) + (at & 31) : at);
+        const u16* in = row + (FORM == kCeHalves ? ((at >> 5) << 6) + (at & 31) : at);
         const u16x8 hi = *reinterpret_cast<const u16x8*>(in);
         u16x8 lo = {};
         if constexpr (FORM == kCeHalves) lo = *reinterpret_cast<const u16x8*>(in + 32);
@@ -379,37 +391,62 @@ __device__ __forceinline__ void load_g(const CePlan& p, const u16* g, int token,
 // Which of the four columns of waves has column j of a tile.
 __device__ __forceinline__ int wave_of(int j) { return (j >> 5) & 3; }
 
-// What exponentials are multiplied by where they are kept: fp16's upper range.
+// Exponentials relative to a largest one are kept times this power of two: fp16's
+// upper range.
 template <CeForm FORM>
-constexpr float kKept = is_scaled(FORM) ? 16384.f : 1.f;
+constexpr int kKept = is_scaled(FORM) ? 14 : 0;
+
+// References: lse_t may pass r_t by 2^room and lie 2^kLow below it, so exp(z - r_t) is
+// kept times 2^(15 - room): of c_t, entries of G keep what is above 2^-34 (one half:
+// rows whose sample misses a word of up to 15/16 of the sum stay in range) or 2^-36
+// (two halves; 3/4 of it).
+constexpr int kLow = 2;
+__host__ __device__ constexpr int room(CeForm f) { return f == kCeHalves ? 2 : 4; }
+__device__ __forceinline__ bool fits(CeForm f, float lse, float ref) {
+    return lse - ref <= room(f) && lse - ref >= -kLow;
+}
+// s_t is at most c_t 2^(kLow + room - 15), so s_t h_t is taken times this and the powers
+// of two that bring the largest c and h to 2^15: at most 2^15.
+constexpr int turned(CeForm f) { return -kLow - room(f); }
+// x_t of a row (all in units of log2).
+__device__ __forceinline__ float row_from(CeForm f, float lse, float ref) {
+    return fits(f, lse, ref) ? ref - (15 - room(f)) : lse - kKept<kCeHalf>;
+}
 
 // First pass: each row's largest logit and sum of exp(z - largest) in a tile, and
 // the target's logit.  KEEP also writes exp(z - largest) in G's place for the first
-// piece, the largest being that of a wave's columns of the tile (wave_of), and these.
+// piece, the largest being that of a wave's columns of the tile (wave_of), or
+// relative to the row's reference, and what they are relative to.  Of the tile
+// columns, tiles_v are taken, one of every `every`.
 template <CeForm FORM, int TM, bool KEEP>
-__global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b) {
+__global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b, int tiles_v, int every) {
     using T = typename TokenTile<FORM, TM, kContig, kContig>::T;
     constexpr int TN = T::kBN;
     __shared__ __align__(1024) char lds[T::kLdsBytes];
-    const int tiles_t = (p.tokens + TM - 1) / TM, tiles_v = (p.vocab + TN - 1) / TN;
-    int tt, tv;
-    logit_tile(xcd_run(blockIdx.x, tiles_t * tiles_v), tiles_t, tiles_v, &tt, &tv);
+    const int tiles_t = (p.tokens + TM - 1) / TM;
+    int tt, at;
+    logit_tile(xcd_run(blockIdx.x, tiles_t * tiles_v), tiles_t, tiles_v, &tt, &at);
+    const int tv = at * every;
     T t;
-    t.run(h_rows(p, b), w_rows(p, b, 0), tt * TM, tv * TN, 0, static_cast<int>(p.ld_h / units(FORM)),
+    t.clear();
+    t.add(h_rows(p, b), w_rows(p, b, 0), tt * TM, tv * TN, 0, static_cast<int>(p.ld_h / units(FORM)),
           (DSM_LDS char*)lds, p.tokens - tt * TM, p.vocab - tv * TN);
     // In units of log2: z2 = acc * unit, exp(z) = exp2(z2).
     const float unit = logit_unit<FORM>(p, b);
     float* hit = reinterpret_cast<float*>(b.workspace + p.hit);
     float2* part = reinterpret_cast<float2*>(lds);  // [T::WN][TM]
-    u16* g = reinterpret_cast<u16*>(b.workspace + p.p);
+    u16* g = reinterpret_cast<u16*>(b.workspace + p.p) + (tt * TM + t.row(0)) * p.ld_p;
     float* tops = reinterpret_cast<float*>(b.workspace + p.tops);
     const bool keep = KEEP && tv * TN < p.piece;
     int rel[T::FI];  // the target's column in the tile, or -1
+    float ref[T::FI];
 #pragma unroll
     for (int fi = 0; fi < T::FI; ++fi) {
         const int token = tt * TM + t.row(fi);
         const int64_t target = b.target[min(token, p.tokens - 1)];
         rel[fi] = token < p.tokens && is_valid(target, p.vocab) ? static_cast<int>(target) - tv * TN : -1;
+        ref[fi] = -__builtin_inff();
+        if (KEEP && p.sample > 0) ref[fi] = reinterpret_cast<const float*>(b.workspace + p.refs)[min(token, p.tokens - 1)];
     }
     if (tv * TN + TN > p.vocab) {  // columns past the vocabulary
 #pragma unroll
@@ -420,6 +457,21 @@ __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b)
 #pragma unroll
                     for (int fi = 0; fi < T::FI; ++fi) t.acc[fi][fj][r] = -__builtin_inff();
     }
+    // The rows' largest logits, all before the first store: one wait for the exchange.
+    float top[T::FI];
+#pragma unroll
+    for (int fi = 0; fi < T::FI; ++fi) {
+        top[fi] = t.acc[fi][0][0];
+#pragma unroll
+        for (int fj = 0; fj < T::FJ; ++fj)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) top[fi] = fmaxf(top[fi], t.acc[fi][fj][r]);
+    }
+#pragma unroll
+    for (int w = 16; w <= 32; w *= 2)
+#pragma unroll
+        for (int fi = 0; fi < T::FI; ++fi) top[fi] = fmaxf(top[fi], __shfl_xor(top[fi], w));
+    float sum[T::FI], kept[T::FI];
 #pragma unroll
     for (int fi = 0; fi < T::FI; ++fi) {
         const int token = tt * TM + t.row(fi);
@@ -431,17 +483,14 @@ __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b)
                 for (int r = 0; r < 4; ++r)
                     if (rel[fi] == t.col(fj) + r) hit[token] = t.acc[fi][fj][r] * unit;
         }
-        float top = t.acc[fi][0][0];
-#pragma unroll
-        for (int fj = 0; fj < T::FJ; ++fj)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) top = fmaxf(top, t.acc[fi][fj][r]);
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        top *= unit;
+        top[fi] *= unit;
         // All logits -inf: no exponential counts (and -inf - -inf is none).
-        const float from = top == -__builtin_inff() ? 0.f : top;
-        float sum = 0.f;
+        const bool none = top[fi] == -__builtin_inff();
+        float from = (none ? 0.f : top[fi]) - (KEEP ? kKept<FORM> : 0);
+        if (KEEP && top[fi] - ref[fi] <= room(FORM)) from = ref[fi] - (15 - room(FORM));
+        top[fi] = none ? top[fi] : from;
+        kept[fi] = from;
+        sum[fi] = 0.f;
         if (keep) {
 #pragma unroll
             for (int q = 0; q < T::FJ / 2; ++q) {
@@ -450,28 +499,34 @@ __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b)
 #pragma unroll
                 for (int r = 0; r < 8; ++r) {
                     e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(z.v[r], unit, -from));
-                    sum += e[r];
-                    e[r] *= kKept<FORM>;
+                    sum[fi] += e[r];
                 }
-                if (token < p.tokens) store_g<FORM>(p, g, token, tv * TN + t.col8(q), e);
+                if (token < p.tokens)
+                    store_g<FORM>(p, g + (t.row(fi) - t.row(0)) * p.ld_p, tv * TN + t.col8(q), e);
             }
         } else {
 #pragma unroll
             for (int fj = 0; fj < T::FJ; ++fj)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    sum += __builtin_amdgcn_exp2f(__builtin_fmaf(t.acc[fi][fj][r], unit, -from));
+                    sum[fi] += __builtin_amdgcn_exp2f(__builtin_fmaf(t.acc[fi][fj][r], unit, -from));
         }
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
-        if (t.lane < 16) {
-            part[t.wj * TM + t.row(fi)] = make_float2(top, sum);
+    }
+#pragma unroll
+    for (int w = 16; w <= 32; w *= 2)
+#pragma unroll
+        for (int fi = 0; fi < T::FI; ++fi) sum[fi] += __shfl_xor(sum[fi], w);
+    if (t.lane < 16) {
+#pragma unroll
+        for (int fi = 0; fi < T::FI; ++fi) {
+            const int token = tt * TM + t.row(fi);
+            part[t.wj * TM + t.row(fi)] = make_float2(top[fi], sum[fi]);
             if (keep && token < p.tokens)
-                tops[static_cast<int64_t>(token) * (p.piece / TN * 4) + tv * 4 + t.wj] = top;
+                tops[static_cast<int64_t>(token) * (p.piece / TN * 4) + tv * 4 + t.wj] = kept[fi];
         }
     }
     __syncthreads();
-    float2* stats = reinterpret_cast<float2*>(b.workspace + p.stats) + static_cast<int64_t>(tv) * p.tokens;
+    float2* stats = reinterpret_cast<float2*>(b.workspace + p.stats) + static_cast<int64_t>(at) * p.tokens;
     for (int r = threadIdx.x; r < TM; r += T::kThreads) {
         if (tt * TM + r >= p.tokens) break;
         float2 a = part[r];
@@ -481,34 +536,115 @@ __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b)
     }
 }
 
-// The kept exponentials become G of the first piece: eight columns a lane, 2048 of a
-// row a work-group.
+// The rows' references, from the sampled tiles.
+__global__ __launch_bounds__(64) void k_refs(CePlan p, CeBuffers b) {
+    const int token = blockIdx.x * 64 + threadIdx.x;
+    if (token >= p.tokens) return;
+    const float2* stats = reinterpret_cast<const float2*>(b.workspace + p.stats) + token;
+    float2 a = make_float2(-__builtin_inff(), 0.f);
+#pragma unroll 16
+    for (int v = 0; v < p.sample; ++v) a = joined(a, stats[static_cast<int64_t>(v) * p.tokens]);
+    const float all = static_cast<float>(p.vocab) / (p.sample * 256.f);
+    const float ref = a.x + __builtin_amdgcn_logf(a.y * all);
+    reinterpret_cast<float*>(b.workspace + p.refs)[token] = fabsf(ref) < __builtin_inff() ? ref : -__builtin_inff();
+}
+
+// The kept exponentials become G of the first piece, eight columns a lane; with
+// references, E: there only the target's entry changes, and rows that do not fit.
 template <CeForm FORM>
-__global__ __launch_bounds__(256) void k_settle(CePlan p, CeBuffers b) {
-    const int per_row = (p.piece + 2047) / 2048, token = blockIdx.x / per_row;
-    const int at = ((blockIdx.x - token * per_row) * 256 + threadIdx.x) * 8;
-    if (at >= p.piece) return;
+__global__ __launch_bounds__(256) void k_settle(CePlan p, CeBuffers b, int groups_of_row) {
+    const int token = blockIdx.x / groups_of_row, first = blockIdx.x - token * groups_of_row;
     const float lse = reinterpret_cast<const float*>(b.workspace + p.lse)[token];
-    const int eg = !is_scaled(FORM) ? 0 : exponent_for(reinterpret_cast<const Scalars*>(b.workspace + p.scalars)->c_max);
-    const float c = ldexpf(reinterpret_cast<const float*>(b.workspace + p.coef)[token], eg);
     const int64_t target = b.target[token];
     const bool valid = is_valid(target, p.vocab);
-    u16* g = reinterpret_cast<u16*>(b.workspace + p.p);
+    u16* g = reinterpret_cast<u16*>(b.workspace + p.p) + token * p.ld_p;
     const int square = square_of(p.tile);
-    const int64_t run = static_cast<int64_t>(token) * (p.piece / square * 4) + at / square * 4 + wave_of(at);
-    const float top = reinterpret_cast<const float*>(b.workspace + p.tops)[run];
-    float v[8];
-    load_g<FORM>(p, g, token, at, v);
-    const float by = valid ? c * (1.f / kKept<FORM>) * __builtin_amdgcn_exp2f(top - lse) : 0.f;
+    const float* tops = reinterpret_cast<const float*>(b.workspace + p.tops) + static_cast<int64_t>(token) * (p.piece / square * 4);
+    // G is exp(z - x) mul, the target's entry (p - 1) of it.
+    float x = lse, mul;
+    if (is_scaled(FORM) && p.sample > 0) {
+        const float ref = reinterpret_cast<const float*>(b.workspace + p.refs)[token];
+        x = row_from(FORM, lse, ref);
+        mul = valid ? 1.f : 0.f;
+        if (fits(FORM, lse, ref)) {
+            if (threadIdx.x != 0 || !valid || target >= p.piece) return;
+            const int at = static_cast<int>(target) & ~7;
+            float v[8];
+            load_g<FORM>(p, g, at, v);
+            const float hit = reinterpret_cast<const float*>(b.workspace + p.hit)[token];
+            const float e = __builtin_amdgcn_exp2f(lse - x) * (__builtin_amdgcn_exp2f(hit - lse) - 1.f);
 #pragma unroll
-    for (int r = 0; r < 8; ++r) v[r] = valid ? v[r] * by : 0.f;
-    if (valid && target >= at && target < at + 8) {
-        const float p1 = __builtin_amdgcn_exp2f(reinterpret_cast<const float*>(b.workspace + p.hit)[token] - lse) - 1.f;
-#pragma unroll
-        for (int r = 0; r < 8; ++r)
-            if (target == at + r) v[r] = c * p1;
+            for (int r = 0; r < 8; ++r)
+                if (target == at + r) v[r] = e;
+            store_g<FORM>(p, g, at, v);
+            return;
+        }
+    } else {
+        const int eg = !is_scaled(FORM) ? 0 : exponent_for(reinterpret_cast<const Scalars*>(b.workspace + p.scalars)->c_max);
+        mul = valid ? ldexpf(reinterpret_cast<const float*>(b.workspace + p.coef)[token], eg) : 0.f;
     }
-    store_g<FORM>(p, g, token, at, v);
+    for (int at = (first * 256 + threadIdx.x) * 8; at < p.piece; at += groups_of_row * 2048) {
+        float v[8];
+        load_g<FORM>(p, g, at, v);
+        const float by = valid ? mul * __builtin_amdgcn_exp2f(tops[at / square * 4 + wave_of(at)] - x) : 0.f;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) v[r] = valid ? v[r] * by : 0.f;
+        if (valid && target >= at && target < at + 8) {
+            const float hit = reinterpret_cast<const float*>(b.workspace + p.hit)[token];
+            const float e = mul * __builtin_amdgcn_exp2f(lse - x) * (__builtin_amdgcn_exp2f(hit - lse) - 1.f);
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+                if (target == at + r) v[r] = e;
+        }
+        store_g<FORM>(p, g, at, v);
+    }
+}
+
+// s_t h_t transposed, as dw takes it: 64 tokens by 64 columns a work-group, zeros for
+// tokens past the last one and those without a valid target.
+template <CeForm FORM>
+__global__ __launch_bounds__(256) void k_turn(CePlan p, CeBuffers b) {
+    __shared__ float tile[64][65];
+    const int t0 = blockIdx.x * 64, d0 = blockIdx.y * 64;
+    const Scalars* sc = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
+    const int es = exponent_for(sc->c_max) + turned(FORM);
+    const u16* h = reinterpret_cast<const u16*>(b.workspace + p.h);
+    const float2* rows = reinterpret_cast<const float2*>(b.workspace + p.rows);
+    const int four = (threadIdx.x & 15) * 4;  // of a row's columns, then of its tokens
+#pragma unroll
+    for (int r = threadIdx.x >> 4; r < 64; r += 16) {
+        const int token = t0 + r, d = d0 + four;
+        f4 v = {0.f, 0.f, 0.f, 0.f};
+        if (token < p.tokens && is_valid(b.target[token], p.vocab)) {
+            const u16* at = h + token * p.ld_h + (FORM == kCeHalves ? ((d >> 5) << 6) + (d & 31) : d);
+            const u16x4 hi = *reinterpret_cast<const u16x4*>(at);
+            u16x4 lo = {};
+            if constexpr (FORM == kCeHalves) lo = *reinterpret_cast<const u16x4*>(at + 32);
+            const float by = ldexpf(rows[token].y, es);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                v[q] = (FORM == kCeHalves ? half_to_float(hi[q]) + half_to_float(lo[q]) : half_to_float(hi[q])) * by;
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) tile[r][four + q] = v[q];
+    }
+    __syncthreads();
+    u16* ht = reinterpret_cast<u16*>(b.workspace + p.ht);
+#pragma unroll
+    for (int r = threadIdx.x >> 4; r < 64; r += 16) {
+        const int d = d0 + r, token = t0 + four;
+        if (d >= p.dim) break;
+        u16x4 hi, lo;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float v = tile[four + q][r];
+            hi[q] = float_to_half(v);
+            lo[q] = float_to_half(v - half_to_float(hi[q]));
+        }
+        u16* at = ht + d * p.ld_ht + (FORM == kCeHalves ? ((token >> 5) << 6) + (token & 31) : token);
+        *reinterpret_cast<u16x4*>(at) = hi;
+        if constexpr (FORM == kCeHalves) *reinterpret_cast<u16x4*>(at + 32) = lo;
+    }
 }
 
 // lse and loss of 16 tokens by a work-group: 64 lanes share a token's tiles.  With
@@ -538,6 +674,13 @@ __global__ __launch_bounds__(1024) void k_join(CePlan p, CeBuffers b, int tiles)
         reinterpret_cast<float*>(b.workspace + p.lse)[token] = lse2;
         if (b.lse) b.lse[token] = lse2 * kLn2;
         b.loss[token] = loss;
+        if (p.sample > 0) {
+            const float ref = reinterpret_cast<const float*>(b.workspace + p.refs)[token];
+            const float below = fits(p.form, lse2, ref) ? ref - lse2 - (15 - room(p.form)) : -static_cast<float>(kKept<kCeHalf>);
+            reinterpret_cast<float2*>(b.workspace + p.rows)[token] =
+                make_float2(row_from(p.form, lse2, ref),
+                            reinterpret_cast<const float*>(b.workspace + p.coef)[token] * __builtin_amdgcn_exp2f(below));
+        }
     }
     if (gridDim.x > 1) return;
     const int count = __popcll(__ballot(valid));
@@ -585,19 +728,23 @@ __global__ __launch_bounds__(threads_of(TM)) void k_piece(CePlan p, CeBuffers b,
     const int eg = !is_scaled(FORM) ? 0 : exponent_for(reinterpret_cast<const Scalars*>(b.workspace + p.scalars)->c_max);
     const float* lse = reinterpret_cast<const float*>(b.workspace + p.lse);
     const float* coef = reinterpret_cast<const float*>(b.workspace + p.coef);
-    u16* g = reinterpret_cast<u16*>(b.workspace + p.p);
+    u16* g = reinterpret_cast<u16*>(b.workspace + p.p) + (tt * TM + t.row(0)) * p.ld_p;
     // What the rows need, all loaded before the first store.  A row without a
-    // valid target gets exp2(z2 - inf) = 0 throughout.
+    // valid target gets exp2(z2 - inf) = 0 throughout.  With references, E.
+    const bool refs = is_scaled(FORM) && p.sample > 0;
+    const float2* rows = reinterpret_cast<const float2*>(b.workspace + p.rows);
     int rel[T::FI];
-    float l[T::FI], c[T::FI];
+    float l[T::FI], c[T::FI], one[T::FI];
 #pragma unroll
     for (int fi = 0; fi < T::FI; ++fi) {
         const int token = tt * TM + t.row(fi), at = min(token, p.tokens - 1);
         const int64_t target = b.target[at];
         const bool valid = token < p.tokens && is_valid(target, p.vocab);
         rel[fi] = valid ? static_cast<int>(target) - first - tv * TN : -1;
-        l[fi] = valid ? lse[at] : __builtin_inff();
-        c[fi] = valid ? ldexpf(coef[at], eg) : 0.f;
+        const float x = refs ? rows[at].x : lse[at];
+        l[fi] = valid ? x : __builtin_inff();
+        c[fi] = !valid ? 0.f : refs ? 1.f : ldexpf(coef[at], eg);
+        one[fi] = refs ? __builtin_amdgcn_exp2f(lse[at] - x) : 1.f;
     }
     const bool ragged = tv * TN + TN > cols;
 #pragma unroll
@@ -616,7 +763,7 @@ __global__ __launch_bounds__(threads_of(TM)) void k_piece(CePlan p, CeBuffers b,
             if (hits) {
 #pragma unroll
                 for (int r = 0; r < 8; ++r)
-                    if (rel[fi] == col + r) v[r] -= 1.0f;
+                    if (rel[fi] == col + r) v[r] -= one[fi];
             }
             const int at = tv * TN + col;
 #pragma unroll
@@ -624,7 +771,7 @@ __global__ __launch_bounds__(threads_of(TM)) void k_piece(CePlan p, CeBuffers b,
                 v[r] *= c[fi];
                 if (ragged && at + r >= cols) v[r] = 0.f;
             }
-            if (at < cols_pad) store_g<FORM>(p, g, token, at, v);
+            if (at < cols_pad) store_g<FORM>(p, g + (t.row(fi) - t.row(0)) * p.ld_p, at, v);
         }
     }
 }
@@ -716,7 +863,8 @@ template <CeForm FORM>
 __global__ __launch_bounds__(256) void k_dh_join(CePlan p, CeBuffers b, int first) {
     __shared__ f4 sums[4][64];
     const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
-    const int ex = is_scaled(FORM) ? -(exponent_for(s->c_max) + exponent_for(s->w_max)) : 0;
+    const bool refs = is_scaled(FORM) && p.sample > 0;
+    const int ex = is_scaled(FORM) ? -((refs ? 0 : exponent_for(s->c_max)) + exponent_for(s->w_max)) : 0;
     const int64_t each = p.tokens * p.ld_dh;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int row = first + blockIdx.y, d = blockIdx.x * 256 + lane * 4;
@@ -731,33 +879,37 @@ __global__ __launch_bounds__(256) void k_dh_join(CePlan p, CeBuffers b, int firs
     __syncthreads();
     if (wave != 0 || d >= p.dim) return;
     v = (v + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+    const float by = refs ? reinterpret_cast<const float2*>(b.workspace + p.rows)[row].y : 1.f;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = ldexpf(v[r], ex);
+    for (int r = 0; r < 4; ++r) v[r] = ldexpf(v[r], ex) * by;
     store_grad<is_f32(FORM)>(b.dh, row * b.dh_stride + d, v, p.dim - d, b.dh_vector);
 }
 
-// dw of one piece.
-template <CeForm FORM, int TM>
-using DwTile = tile::Pick<elem(FORM), square_of(TM), kStrided, kStrided>;
+// dw of one piece; REFS: of E by s_t h_t transposed.
+template <CeForm FORM, int TM, bool REFS>
+using DwTile = tile::Pick<elem(FORM), square_of(TM), kStrided, REFS ? kContig : kStrided>;
 
-template <CeForm FORM, int TM>
+template <CeForm FORM, int TM, bool REFS>
 __device__ __forceinline__ void dw_tile(const CePlan& p, const CeBuffers& b, int first, int cols, int id,
                                         DSM_LDS char* lds) {
     constexpr int BM = square_of(TM);
-    using T = DwTile<FORM, TM>;
+    using T = DwTile<FORM, TM, REFS>;
     const int tiles_d = (p.dim + BM - 1) / BM;
     const int tv = id / tiles_d, td = id - tv * tiles_d;
     constexpr int kSteps = T::kSteps;
     const int rows_pad = (p.tokens + kSteps - 1) / kSteps * kSteps;
+    const Operand h = REFS ? Operand{reinterpret_cast<const u16*>(b.workspace + p.ht), p.ld_ht, p.dim,
+                                     static_cast<int32_t>(p.ld_ht)}
+                           : h_rows(p, b);
     T t;
     t.clear();
-    t.add(g_rows(p, b), h_rows(p, b), tv * BM, td * BM, 0, rows_pad, lds, cols - tv * BM, p.dim - td * BM);
+    t.add(g_rows(p, b), h, tv * BM, td * BM, 0, rows_pad, lds, cols - tv * BM, p.dim - td * BM);
     if constexpr (FORM == kCeBf16)
-        t.add(g_rows<true>(p, b), h_rows(p, b), tv * BM, td * BM, 0, rows_pad, lds, cols - tv * BM, p.dim - td * BM);
+        t.add(g_rows<true>(p, b), h, tv * BM, td * BM, 0, rows_pad, lds, cols - tv * BM, p.dim - td * BM);
     int ex = 0;
     if constexpr (is_scaled(FORM)) {
         const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
-        ex = -(exponent_for(s->c_max) + exponent_for(s->h_max));
+        ex = -(exponent_for(s->c_max) + exponent_for(s->h_max) + (REFS ? turned(FORM) : 0));
     }
 #pragma unroll
     for (int fi = 0; fi < T::FI; ++fi) {
@@ -786,11 +938,12 @@ __device__ __forceinline__ void dw_tile(const CePlan& p, const CeBuffers& b, int
 constexpr int kXcds = 8;
 __host__ __device__ inline int per_xcd(int tiles) { return (tiles + kXcds - 1) / kXcds; }
 
-template <CeForm FORM, int TM>
+template <CeForm FORM, int TM, bool REFS>
 __global__ __launch_bounds__(threads_of(TM)) void k_gradients(CePlan p, CeBuffers b, int first, int cols,
                                                               int dh_tiles, int dw_tiles) {
     using TD = typename TokenTile<FORM, TM, kContig, kStrided>::T;
-    constexpr int kLds = TD::kLdsBytes > DwTile<FORM, TM>::kLdsBytes ? TD::kLdsBytes : DwTile<FORM, TM>::kLdsBytes;
+    using TW = DwTile<FORM, TM, REFS>;
+    constexpr int kLds = TD::kLdsBytes > TW::kLdsBytes ? TD::kLdsBytes : TW::kLdsBytes;
     __shared__ __align__(1024) char lds[kLds];
     const int x = blockIdx.x % kXcds, at = blockIdx.x / kXcds, front = per_xcd(dh_tiles);
     if (at < front) {
@@ -798,7 +951,7 @@ __global__ __launch_bounds__(threads_of(TM)) void k_gradients(CePlan p, CeBuffer
         if (id < dh_tiles) dh_tile<FORM, TM>(p, b, first, cols, id, (DSM_LDS char*)lds);
     } else {
         const int id = x * per_xcd(dw_tiles) + at - front;
-        if (id < dw_tiles) dw_tile<FORM, TM>(p, b, first, cols, id, (DSM_LDS char*)lds);
+        if (id < dw_tiles) dw_tile<FORM, TM, REFS>(p, b, first, cols, id, (DSM_LDS char*)lds);
     }
 }
 
@@ -810,8 +963,8 @@ __global__ __launch_bounds__(threads_of(TM)) void k_dh(CePlan p, CeBuffers b, in
 }
 template <CeForm FORM, int TM>
 __global__ __launch_bounds__(tile::threads_of(square_of(TM))) void k_dw(CePlan p, CeBuffers b, int first, int cols) {
-    __shared__ __align__(1024) char lds[DwTile<FORM, TM>::kLdsBytes];
-    dw_tile<FORM, TM>(p, b, first, cols, xcd_run(blockIdx.x, gridDim.x), (DSM_LDS char*)lds);
+    __shared__ __align__(1024) char lds[DwTile<FORM, TM, false>::kLdsBytes];
+    dw_tile<FORM, TM, false>(p, b, first, cols, xcd_run(blockIdx.x, gridDim.x), (DSM_LDS char*)lds);
 }
 
 // No tokens: the total and dw are zero.
@@ -827,11 +980,20 @@ __global__ __launch_bounds__(256) void k_nothing(CePlan p, CeBuffers b) {
 template <CeForm FORM, int TM>
 void products(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
     constexpr int kThreads = threads_of(TM), TN = square_of(TM);
+    constexpr bool kRefs = TM == 256 && is_scaled(FORM);  // rows may have references
     const int tt = (p.tokens + TM - 1) / TM, td = (p.dim + TN - 1) / TN, tv = (p.vocab + TN - 1) / TN;
     if constexpr (FORM != kCeBf16 || TM < 256) {  // (many tokens with gradients take fp16)
-        if (p.grads) k_stats<FORM, TM, true><<<tt * tv, kThreads, 0, stream>>>(p, b);
+        if (p.grads) {
+            if constexpr (kRefs) {
+                if (p.sample > 0) {
+                    k_stats<FORM, TM, false><<<tt * p.sample, kThreads, 0, stream>>>(p, b, p.sample, p.every);
+                    k_refs<<<(p.tokens + 63) / 64, 64, 0, stream>>>(p, b);
+                }
+            }
+            k_stats<FORM, TM, true><<<tt * tv, kThreads, 0, stream>>>(p, b, tv, 1);
+        }
     }
-    if (!p.grads) k_stats<FORM, TM, false><<<tt * tv, kThreads, 0, stream>>>(p, b);
+    if (!p.grads) k_stats<FORM, TM, false><<<tt * tv, kThreads, 0, stream>>>(p, b, tv, 1);
     k_join<<<(p.tokens + kJoinTokens - 1) / kJoinTokens, 1024, 0, stream>>>(p, b, tv);
     if (p.tokens > kJoinTokens) k_total<<<1, 1024, 0, stream>>>(p, b);
     if constexpr (FORM != kCeBf16 || TM < 256) {
@@ -840,14 +1002,23 @@ void products(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
             const int cols = p.vocab - first < p.piece ? p.vocab - first : p.piece;
             const int tp = (cols + TN - 1) / TN;
             if (first == 0) {
-                k_settle<FORM><<<p.tokens * ((p.piece + 2047) / 2048), 256, 0, stream>>>(p, b);
+                // With references few rows change: one group each.
+                const int groups = p.sample > 0 ? 1 : (p.piece + 2047) / 2048;
+                k_settle<FORM><<<p.tokens * groups, 256, 0, stream>>>(p, b, groups);
+                if constexpr (kRefs) {
+                    if (p.sample > 0)
+                        k_turn<FORM><<<dim3((p.tokens + 63) / 64, (p.dim + 63) / 64), 256, 0, stream>>>(p, b);
+                }
             } else {
                 k_piece<FORM, TM><<<tt * tp, kThreads, 0, stream>>>(p, b, first, cols);
             }
             const int dh_tiles = tt * td * p.dh_splits, dw_tiles = tp * td;
             if constexpr (TM >= 128) {
-                k_gradients<FORM, TM><<<kXcds * (per_xcd(dh_tiles) + per_xcd(dw_tiles)), kThreads, 0, stream>>>(
-                    p, b, first, cols, dh_tiles, dw_tiles);
+                const int groups = kXcds * (per_xcd(dh_tiles) + per_xcd(dw_tiles));
+                if (kRefs && p.sample > 0)
+                    k_gradients<FORM, TM, kRefs><<<groups, kThreads, 0, stream>>>(p, b, first, cols, dh_tiles, dw_tiles);
+                else
+                    k_gradients<FORM, TM, false><<<groups, kThreads, 0, stream>>>(p, b, first, cols, dh_tiles, dw_tiles);
             } else {
                 k_dh<FORM, TM><<<dh_tiles, kThreads, 0, stream>>>(p, b, first, cols);
                 k_dw<FORM, TM><<<dw_tiles, tile::threads_of(TN), 0, stream>>>(p, b, first, cols);
@@ -871,6 +1042,7 @@ hipError_t launch_linear_ce(const CePlan& p, const CeBuffers& b, hipStream_t str
     }
     const int most = b.w_direct || p.tokens > p.vocab ? p.tokens : p.vocab;
     const unsigned groups = static_cast<unsigned>(most < 8192 ? (most + 3) / 4 : 2048);
+    const unsigned few = std::min(groups, 512u);
     switch (p.form) {
         case kCeBf16:
             if (!b.h_direct)
@@ -894,7 +1066,7 @@ hipError_t launch_linear_ce(const CePlan& p, const CeBuffers& b, hipStream_t str
             break;
         case kCeHalf:
             k_coef<<<1, 1024, 0, stream>>>(p, b);
-            k_largest<false><<<dim3(groups, 2), 256, 0, stream>>>(p, b);
+            k_largest<false><<<dim3(few, 2), 256, 0, stream>>>(p, b);
             k_operands<kCeHalf><<<dim3(groups, 2), 256, 0, stream>>>(p, b);
             if (p.tile == 128)
                 products<kCeHalf, 128>(p, b, stream);
@@ -903,7 +1075,7 @@ hipError_t launch_linear_ce(const CePlan& p, const CeBuffers& b, hipStream_t str
             break;
         case kCeHalves:
             k_coef<<<1, 1024, 0, stream>>>(p, b);  // (also clears the largest magnitudes)
-            k_largest<true><<<dim3(groups, 2), 256, 0, stream>>>(p, b);
+            k_largest<true><<<dim3(few, 2), 256, 0, stream>>>(p, b);
             k_operands<kCeHalves><<<dim3(groups, 2), 256, 0, stream>>>(p, b);
             if (p.tile == 128)
                 products<kCeHalves, 128>(p, b, stream);

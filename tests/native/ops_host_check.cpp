@@ -124,6 +124,16 @@ static void check_plan(const dsm_ce_problem& p, const dsm::CePlan& q, int64_t ws
         // A launch has a group for each 2048 columns of each row.
         CHECK(T * ((q.piece + 2047) / 2048) < (int64_t(1) << 31));
         parts.push_back({q.tops, T * (q.piece / square) * 16});
+        if (q.sample > 0) {
+            CHECK(q.tile == 256 && (q.form == dsm::kCeHalf || q.form == dsm::kCeHalves));
+            // Sampled tile columns lie inside the vocabulary, and are a 64th of it.
+            CHECK(q.every >= 4 && int64_t(q.sample) * q.every <= (V + 255) / 256);
+            CHECK(int64_t(q.sample) * 64 * 256 >= V);
+            CHECK(q.ld_ht == high * units);
+            parts.push_back({q.refs, T * 4});
+            parts.push_back({q.rows, T * 8});
+            parts.push_back({q.ht, D * q.ld_ht * 2});
+        }
         parts.push_back({q.p, all});
         parts.push_back({q.dh, q.dh_splits * T * q.ld_dh * 4});
     }

@@ -300,3 +300,29 @@ def test_refusals_of_the_helper():
         with pytest.raises(dsm.DsmError) as e:
             ops.LinearCE(*sizes)
         assert e.value.status == dsm.DSM_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_rows_far_from_what_a_part_of_the_vocabulary_tells(dtype):
+    """Many tokens of a large vocabulary: single words that hold nearly all of a row's
+    sum, in every tile of the vocabulary in turn, beside even rows, tokens left out
+    and rows whose logits are all equal."""
+    tokens, dim, vocab = (4100 if dtype == BF16 else 2050), 64, 30011
+    h, w, t, weight = _problem(tokens, dim, vocab, dtype, seed=11)
+    peaked = torch.arange(0, tokens, 2, device="cuda")
+    word = (peaked * 251 + 13) % vocab
+    # The word's logit is 40 |w_v| above what its neighbours have.
+    unit = torch.nn.functional.normalize(w[word].float(), dim=1)
+    h[peaked] = (unit * 40.0).to(dtype)
+    t[peaked[::3]] = word[::3]
+    h[5::16] = 0
+    ops = _ops()
+    out = ops.LinearCE(tokens, dim, vocab, dtype=dtype)(h, w, t, weight=weight)
+    e = O.linear_ce(h, w, t, weight=weight, mean=True)
+    bounds = O.linear_ce_bounds(e, dtype, *_carried(dtype, tokens, True))
+    # Of c_t, an entry of G below 2^-34 may vanish; and G may be rounded twice.
+    u_g = _carried(dtype, tokens, True)[1]
+    bounds["dh"] += 2.0 ** -34 * e["c"][:, None] * e["w"].abs().sum(0) + u_g * (e["g"].abs() @ e["w"].abs())
+    c_h = e["c"][:, None] * e["h"].abs()
+    bounds["dw"] += 2.0 ** -34 * c_h.sum(0) + u_g * (e["g"].abs().t().contiguous() @ e["h"].abs())
+    _check(out, e, bounds, ("total", "loss", "dh", "dw"))
