@@ -5,13 +5,7 @@
 #include <hip/hip_runtime_api.h>
 #include <stdint.h>
 
-#include "dsm.h"
-
 namespace dsm {
-
-// Records the message that dsm_last_error(NULL) returns on this thread, and
-// returns the status (dsm_runtime.cpp).
-dsm_status set_thread_error(dsm_status st, const char* message);
 
 // Elements per chunk.  A chunk never crosses a tensor boundary, so the
 // per-tensor facts a kernel needs (decay flag, tensor index for the randomized

@@ -15,6 +15,7 @@
 #include <vector>
 
 #include "dsm_internal.h"
+#include "thread_error.h"
 
 struct dsm_ctx {
     int n = 0, H = 0, n_tensors = 0, base = 0;

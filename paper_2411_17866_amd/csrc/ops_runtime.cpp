@@ -7,8 +7,8 @@
 #include <cstdio>
 
 #include "dsm.h"
-#include "dsm_internal.h"
 #include "ops_internal.h"
+#include "thread_error.h"
 
 namespace {
 
