@@ -89,9 +89,11 @@ constexpr tile::Elem elem(CeForm f) {
 constexpr int units(CeForm f) { return tile::units(elem(f)); }
 
 struct Scalars {
-    uint32_t h_max, w_max;  // bits of the largest finite |h| and |w| (fp32 buffers)
+    uint32_t h_max, w_max;  // bits of the largest finite |h| and |w| (scaled forms)
     uint32_t c_max;         // bits of the largest finite |c_t|
+    uint32_t parts[2][kCeParts];  // of the work-groups that look for h_max and w_max
 };
+static_assert(sizeof(Scalars) <= kCeScalars, "the host's plan leaves room for this");
 
 // The power of two that brings a largest magnitude into [2^14, 2^15).
 __device__ __forceinline__ int exponent_for(uint32_t bits) {
@@ -124,29 +126,36 @@ __device__ void coefficients(const CePlan& p, const CeBuffers& b) {
     }
     __syncthreads();
     int mine = 0;
+#pragma unroll 8
     for (int t = threadIdx.x; t < p.tokens; t += blockDim.x) mine += is_valid(b.target[t], p.vocab);
     for (int w = 32; w > 0; w >>= 1) mine += __shfl_xor(mine, w);
     if ((threadIdx.x & 63) == 0) atomicAdd(&count, mine);
     __syncthreads();
     float* coef = reinterpret_cast<float*>(b.workspace + p.coef);
     uint32_t top = 0;
-    for (int t = threadIdx.x; t < p.tokens; t += blockDim.x) {
-        float c = 0.f;
-        if (is_valid(b.target[t], p.vocab)) c = coefficient(b, t, count);
-        coef[t] = c;
-        top = max(top, finite_bits(c));
+    // (Eight tokens' loads before their stores, which might overlap them.)
+    for (int first = threadIdx.x; first < p.tokens; first += 8 * blockDim.x) {
+        float c[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const int t = min(first + q * static_cast<int>(blockDim.x), p.tokens - 1);
+            const bool valid = is_valid(b.target[t], p.vocab);
+            c[q] = coefficient(b, t, count);
+            c[q] = valid ? c[q] : 0.f;
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const int t = first + q * static_cast<int>(blockDim.x);
+            if (t < p.tokens) coef[t] = c[q];
+            top = max(top, finite_bits(c[q]));
+        }
     }
     atomicMax(&c_max, top);
     __syncthreads();
     if (threadIdx.x == 0) {
-        Scalars* s = reinterpret_cast<Scalars*>(b.workspace + p.scalars);
-        s->h_max = 0;
-        s->w_max = 0;
-        s->c_max = c_max;
+        reinterpret_cast<Scalars*>(b.workspace + p.scalars)->c_max = c_max;
     }
 }
-
-__global__ __launch_bounds__(1024) void k_coef(CePlan p, CeBuffers b) { coefficients(p, b); }
 
 template <bool F32>
 __device__ __forceinline__ f4 load4(const void* base, int64_t at, int have, bool vec) {
@@ -172,7 +181,18 @@ __device__ __forceinline__ f4 load4(const void* base, int64_t at, int have, bool
     return v;
 }
 
-// The largest finite magnitude of h's valid rows (blockIdx.y = 0) and of w (1).
+// The largest of a work-group of 256.
+__device__ __forceinline__ uint32_t largest_of_group(uint32_t top) {
+    __shared__ uint32_t tops[4];
+    for (int w = 32; w > 0; w >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), w)));
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    __syncthreads();
+    return max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+}
+
+// The largest finite magnitude of h's valid rows (blockIdx.y = 0) and of w (1), one
+// of each work-group.  (Atomics on one address would take turns: 54 us where this
+// takes 19 for w of 50257 x 768 in bf16, 4.0 TB/s.)
 template <bool F32>
 __global__ __launch_bounds__(256) void k_largest(CePlan p, CeBuffers b) {
     const bool of_w = blockIdx.y != 0;
@@ -201,28 +221,19 @@ __global__ __launch_bounds__(256) void k_largest(CePlan p, CeBuffers b) {
             }
         }
     }
-    for (int w = 32; w > 0; w >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), w)));
-    __shared__ uint32_t tops[4];
-    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
-        Scalars* s = reinterpret_cast<Scalars*>(b.workspace + p.scalars);
-        uint32_t* to = of_w ? &s->w_max : &s->h_max;
-        // (Atomics on one address take turns: most groups see that theirs is not needed.)
-        if (top > __hip_atomic_load(to, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(to, top);
-    }
+    top = largest_of_group(top);
+    if (threadIdx.x == 0)
+        reinterpret_cast<Scalars*>(b.workspace + p.scalars)->parts[of_w][blockIdx.x] = top;
 }
 
 // h (blockIdx.y = 0) and w (1) as the products take them: rows of a multiple of
 // 64 columns, h with a multiple of 64 rows; zeros in the padding and in h's rows
-// without a valid target.  In the
-// forms without a scale the last work-group of h computes the coefficients, for
-// nothing else waits for them here.
+// without a valid target.  The last work-group of h computes the coefficients, for
+// nothing else waits for them here.  `parts`: of the largest magnitudes.
 template <CeForm FORM>
-__global__ __launch_bounds__(256) void k_operands(CePlan p, CeBuffers b) {
+__global__ __launch_bounds__(256) void k_operands(CePlan p, CeBuffers b, int parts) {
     const bool of_w = blockIdx.y != 0;
-    const int groups = static_cast<int>(gridDim.x) - (is_scaled(FORM) ? 0 : 1);
+    const int groups = static_cast<int>(gridDim.x) - 1;
     if (static_cast<int>(blockIdx.x) >= groups) {
         if (!of_w && p.grads) coefficients(p, b);
         return;
@@ -236,8 +247,12 @@ __global__ __launch_bounds__(256) void k_operands(CePlan p, CeBuffers b) {
     u16* dst = reinterpret_cast<u16*>(b.workspace + (of_w ? p.w : p.h));
     float scale = 1.f;
     if constexpr (is_scaled(FORM)) {
-        const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
-        scale = ldexpf(1.f, exponent_for(of_w ? s->w_max : s->h_max));
+        Scalars* s = reinterpret_cast<Scalars*>(b.workspace + p.scalars);
+        uint32_t top = 0;
+        for (int q = threadIdx.x; q < parts; q += 256) top = max(top, s->parts[of_w][q]);
+        top = largest_of_group(top);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *(of_w ? &s->w_max : &s->h_max) = top;
+        scale = ldexpf(1.f, exponent_for(top));
     }
     for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += groups * 4) {
         const bool keep = of_w || (r < p.tokens && is_valid(b.target[r], p.vocab));
@@ -536,24 +551,61 @@ __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b,
     }
 }
 
-// The rows' references, from the sampled tiles.
-__global__ __launch_bounds__(64) void k_refs(CePlan p, CeBuffers b) {
-    const int token = blockIdx.x * 64 + threadIdx.x;
-    if (token >= p.tokens) return;
-    const float2* stats = reinterpret_cast<const float2*>(b.workspace + p.stats) + token;
+// The rows' references, from the sampled tiles: 16 tokens a work-group, 16 lanes each.
+__global__ __launch_bounds__(256) void k_refs(CePlan p, CeBuffers b) {
+    __shared__ float2 part[16][16];
+    const int lane = threadIdx.x & 15, share = threadIdx.x >> 4;
+    const int token = blockIdx.x * 16 + lane;
+    const float2* stats = reinterpret_cast<const float2*>(b.workspace + p.stats) + min(token, p.tokens - 1);
     float2 a = make_float2(-__builtin_inff(), 0.f);
-#pragma unroll 16
-    for (int v = 0; v < p.sample; ++v) a = joined(a, stats[static_cast<int64_t>(v) * p.tokens]);
+#pragma unroll 4
+    for (int v = share; v < p.sample; v += 16) a = joined(a, stats[static_cast<int64_t>(v) * p.tokens]);
+    part[share][lane] = a;
+    __syncthreads();
+    if (share != 0 || token >= p.tokens) return;
+#pragma unroll
+    for (int q = 1; q < 16; ++q) a = joined(a, part[q][lane]);
     const float all = static_cast<float>(p.vocab) / (p.sample * 256.f);
     const float ref = a.x + __builtin_amdgcn_logf(a.y * all);
     reinterpret_cast<float*>(b.workspace + p.refs)[token] = fabsf(ref) < __builtin_inff() ? ref : -__builtin_inff();
 }
 
+// The weighted total, in a fixed order, by one work-group.
+template <int N>
+__device__ __forceinline__ void total_loss(const CePlan& p, const CeBuffers& b) {
+    __shared__ double s[N];
+    __shared__ int count;
+    if (threadIdx.x == 0) count = 0;
+    __syncthreads();
+    int mine = 0;
+#pragma unroll 8
+    for (int t = threadIdx.x; t < p.tokens; t += N) mine += is_valid(b.target[t], p.vocab);
+    atomicAdd(&count, mine);
+    __syncthreads();
+    double sum = 0.0;
+#pragma unroll 8
+    for (int t = threadIdx.x; t < p.tokens; t += N)
+        sum += is_valid(b.target[t], p.vocab) ? static_cast<double>(coefficient(b, t, count)) * b.loss[t] : 0.0;
+    s[threadIdx.x] = sum;
+    __syncthreads();
+    for (int w = N / 2; w > 0; w >>= 1) {
+        if (static_cast<int>(threadIdx.x) < w) s[threadIdx.x] += s[threadIdx.x + w];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) b.total[0] = static_cast<float>(s[0]);
+}
+__global__ __launch_bounds__(1024) void k_total(CePlan p, CeBuffers b) { total_loss<1024>(p, b); }
+
 // The kept exponentials become G of the first piece, eight columns a lane; with
-// references, E: there only the target's entry changes, and rows that do not fit.
+// references, E: there only the target's entry changes, and rows that do not fit.  A
+// work-group past the rows' sums the total, which would take a launch of its own.
 template <CeForm FORM>
 __global__ __launch_bounds__(256) void k_settle(CePlan p, CeBuffers b, int groups_of_row) {
     const int token = blockIdx.x / groups_of_row, first = blockIdx.x - token * groups_of_row;
+    if (token >= p.tokens) {
+        total_loss<256>(p, b);
+        return;
+    }
     const float lse = reinterpret_cast<const float*>(b.workspace + p.lse)[token];
     const int64_t target = b.target[token];
     const bool valid = is_valid(target, p.vocab);
@@ -687,28 +739,6 @@ __global__ __launch_bounds__(1024) void k_join(CePlan p, CeBuffers b, int tiles)
     double sum = valid ? static_cast<double>(coefficient(b, at, count)) * loss : 0.0;
     for (int w = kJoinTokens / 2; w > 0; w >>= 1) sum += __shfl_xor(sum, w);
     if (lane == 0) b.total[0] = static_cast<float>(sum);
-}
-
-// The weighted total, in a fixed order.
-__global__ __launch_bounds__(1024) void k_total(CePlan p, CeBuffers b) {
-    __shared__ double s[1024];
-    __shared__ int count;
-    if (threadIdx.x == 0) count = 0;
-    __syncthreads();
-    int mine = 0;
-    for (int t = threadIdx.x; t < p.tokens; t += 1024) mine += is_valid(b.target[t], p.vocab);
-    atomicAdd(&count, mine);
-    __syncthreads();
-    double sum = 0.0;
-    for (int t = threadIdx.x; t < p.tokens; t += 1024)
-        if (is_valid(b.target[t], p.vocab)) sum += static_cast<double>(coefficient(b, t, count)) * b.loss[t];
-    s[threadIdx.x] = sum;
-    __syncthreads();
-    for (int w = 512; w > 0; w >>= 1) {
-        if (static_cast<int>(threadIdx.x) < w) s[threadIdx.x] += s[threadIdx.x + w];
-        __syncthreads();
-    }
-    if (threadIdx.x == 0) b.total[0] = static_cast<float>(s[0]);
 }
 
 // G of one piece of the vocabulary, [first, first + cols).
@@ -987,7 +1017,7 @@ void products(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
             if constexpr (kRefs) {
                 if (p.sample > 0) {
                     k_stats<FORM, TM, false><<<tt * p.sample, kThreads, 0, stream>>>(p, b, p.sample, p.every);
-                    k_refs<<<(p.tokens + 63) / 64, 64, 0, stream>>>(p, b);
+                    k_refs<<<(p.tokens + 15) / 16, 256, 0, stream>>>(p, b);
                 }
             }
             k_stats<FORM, TM, true><<<tt * tv, kThreads, 0, stream>>>(p, b, tv, 1);
@@ -995,7 +1025,7 @@ void products(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
     }
     if (!p.grads) k_stats<FORM, TM, false><<<tt * tv, kThreads, 0, stream>>>(p, b, tv, 1);
     k_join<<<(p.tokens + kJoinTokens - 1) / kJoinTokens, 1024, 0, stream>>>(p, b, tv);
-    if (p.tokens > kJoinTokens) k_total<<<1, 1024, 0, stream>>>(p, b);
+    if (!p.grads && p.tokens > kJoinTokens) k_total<<<1, 1024, 0, stream>>>(p, b);
     if constexpr (FORM != kCeBf16 || TM < 256) {
         if (!p.grads) return;
         for (int first = 0; first < p.vocab; first += p.piece) {
@@ -1004,7 +1034,7 @@ void products(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
             if (first == 0) {
                 // With references few rows change: one group each.
                 const int groups = p.sample > 0 ? 1 : (p.piece + 2047) / 2048;
-                k_settle<FORM><<<p.tokens * groups, 256, 0, stream>>>(p, b, groups);
+                k_settle<FORM><<<p.tokens * groups + (p.tokens > kJoinTokens), 256, 0, stream>>>(p, b, groups);
                 if constexpr (kRefs) {
                     if (p.sample > 0)
                         k_turn<FORM><<<dim3((p.tokens + 63) / 64, (p.dim + 63) / 64), 256, 0, stream>>>(p, b);
@@ -1042,11 +1072,11 @@ hipError_t launch_linear_ce(const CePlan& p, const CeBuffers& b, hipStream_t str
     }
     const int most = b.w_direct || p.tokens > p.vocab ? p.tokens : p.vocab;
     const unsigned groups = static_cast<unsigned>(most < 8192 ? (most + 3) / 4 : 2048);
-    const unsigned few = std::min(groups, 512u);
+    const unsigned parts = std::min(groups, static_cast<unsigned>(kCeParts));
     switch (p.form) {
         case kCeBf16:
             if (!b.h_direct)
-                k_operands<kCeBf16><<<dim3(groups + 1, b.w_direct ? 1 : 2), 256, 0, stream>>>(p, b);
+                k_operands<kCeBf16><<<dim3(groups + 1, b.w_direct ? 1 : 2), 256, 0, stream>>>(p, b, 0);
             if (p.tile == 32)
                 products<kCeBf16, 32>(p, b, stream);
             else if (p.tile == 64)
@@ -1058,25 +1088,23 @@ hipError_t launch_linear_ce(const CePlan& p, const CeBuffers& b, hipStream_t str
             break;
         case kCeF32:
             if (!b.h_direct)
-                k_operands<kCeF32><<<dim3(groups + 1, b.w_direct ? 1 : 2), 256, 0, stream>>>(p, b);
+                k_operands<kCeF32><<<dim3(groups + 1, b.w_direct ? 1 : 2), 256, 0, stream>>>(p, b, 0);
             if (p.tile == 32)
                 products<kCeF32, 32>(p, b, stream);
             else
                 products<kCeF32, 64>(p, b, stream);
             break;
         case kCeHalf:
-            k_coef<<<1, 1024, 0, stream>>>(p, b);
-            k_largest<false><<<dim3(few, 2), 256, 0, stream>>>(p, b);
-            k_operands<kCeHalf><<<dim3(groups, 2), 256, 0, stream>>>(p, b);
+            k_largest<false><<<dim3(parts, 2), 256, 0, stream>>>(p, b);
+            k_operands<kCeHalf><<<dim3(groups + 1, 2), 256, 0, stream>>>(p, b, parts);
             if (p.tile == 128)
                 products<kCeHalf, 128>(p, b, stream);
             else
                 products<kCeHalf, 256>(p, b, stream);
             break;
         case kCeHalves:
-            k_coef<<<1, 1024, 0, stream>>>(p, b);  // (also clears the largest magnitudes)
-            k_largest<true><<<dim3(few, 2), 256, 0, stream>>>(p, b);
-            k_operands<kCeHalves><<<dim3(groups, 2), 256, 0, stream>>>(p, b);
+            k_largest<true><<<dim3(parts, 2), 256, 0, stream>>>(p, b);
+            k_operands<kCeHalves><<<dim3(groups + 1, 2), 256, 0, stream>>>(p, b, parts);
             if (p.tile == 128)
                 products<kCeHalves, 128>(p, b, stream);
             else

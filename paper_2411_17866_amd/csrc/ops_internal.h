@@ -58,6 +58,10 @@ hipError_t launch_ortho(const OrthoGroup& g, const float* coeffs, const OrthoSca
 // What the products' operands hold (linear_ce.hip).
 enum CeForm { kCeBf16, kCeHalf, kCeHalves, kCeF32 };
 
+// The plan's `scalars`: largest magnitudes, and those of kCeParts work-groups each.
+constexpr int kCeParts = 512;
+constexpr int64_t kCeScalars = 64 + 8 * kCeParts;
+
 // Where the parts of the workspace lie (bytes from its start), and how the
 // vocabulary is cut.
 struct CePlan {

@@ -157,7 +157,7 @@ dsm::CePlan make_plan(const dsm_ce_problem* p) {
         at = round_up(at + bytes, 256);
         return here;
     };
-    q.scalars = take(64);
+    q.scalars = take(dsm::kCeScalars);
     q.coef = take(T * 4);
     q.lse = take(T * 4);
     q.hit = take(T * 4);

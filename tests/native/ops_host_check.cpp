@@ -111,7 +111,7 @@ static void check_plan(const dsm_ce_problem& p, const dsm::CePlan& q, int64_t ws
     struct Part {
         int64_t at, bytes;
     };
-    std::vector<Part> parts = {{q.scalars, 16}, {q.coef, 4 * T}, {q.lse, 4 * T}, {q.hit, 4 * T},
+    std::vector<Part> parts = {{q.scalars, dsm::kCeScalars}, {q.coef, 4 * T}, {q.lse, 4 * T}, {q.hit, 4 * T},
                                {q.stats, (V + square - 1) / square * T * 8}, {q.h, high * wide * 2}, {q.w, V * wide * 2}};
     if (p.grads && T > 0) {
         CHECK(q.piece > 0 && q.piece % square == 0 && q.piece < V + square);
