@@ -192,10 +192,16 @@ __device__ __forceinline__ uint32_t largest_of_group(uint32_t top) {
 
 // The largest finite magnitude of h's valid rows (blockIdx.y = 0) and of w (1), one
 // of each work-group.  (Atomics on one address would take turns: 54 us where this
-// takes 19 for w of 50257 x 768 in bf16, 4.0 TB/s.)
+// takes 19 for w of 50257 x 768 in bf16, 4.0 TB/s.)  A work-group past those computes
+// the coefficients, for which nothing waits here.
 template <bool F32>
 __global__ __launch_bounds__(256) void k_largest(CePlan p, CeBuffers b) {
     const bool of_w = blockIdx.y != 0;
+    const int groups = static_cast<int>(gridDim.x) - 1;
+    if (static_cast<int>(blockIdx.x) >= groups) {
+        if (!of_w && p.grads) coefficients(p, b);
+        return;
+    }
     const void* src = of_w ? b.w : b.h;
     const bool vec = of_w ? b.w_vector : b.h_vector;
     const int64_t stride = of_w ? b.w_stride : b.h_stride;
@@ -203,7 +209,7 @@ __global__ __launch_bounds__(256) void k_largest(CePlan p, CeBuffers b) {
     uint32_t top = 0;
     if (of_w && vec && stride == p.dim) {  // one run of elements
         const int64_t all = static_cast<int64_t>(rows) * p.dim / 4;
-        const int64_t step = static_cast<int64_t>(gridDim.x) * 256;
+        const int64_t step = static_cast<int64_t>(groups) * 256;
 #pragma unroll 8
         for (int64_t e = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; e < all; e += step) {
             const f4 v = load4<F32>(src, e * 4, 4, true);
@@ -211,7 +217,7 @@ __global__ __launch_bounds__(256) void k_largest(CePlan p, CeBuffers b) {
             for (int q = 0; q < 4; ++q) top = max(top, finite_bits(v[q]));
         }
     } else {
-        for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4) {
+        for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += groups * 4) {
             if (!of_w && !is_valid(b.target[r], p.vocab)) continue;
 #pragma unroll 4
             for (int c = (threadIdx.x & 63) * 4; c < p.dim; c += 256) {
@@ -228,12 +234,12 @@ __global__ __launch_bounds__(256) void k_largest(CePlan p, CeBuffers b) {
 
 // h (blockIdx.y = 0) and w (1) as the products take them: rows of a multiple of
 // 64 columns, h with a multiple of 64 rows; zeros in the padding and in h's rows
-// without a valid target.  The last work-group of h computes the coefficients, for
-// nothing else waits for them here.  `parts`: of the largest magnitudes.
+// without a valid target.  In the forms without a scale the last work-group of h computes
+// the coefficients.  `parts`: of the largest magnitudes.
 template <CeForm FORM>
 __global__ __launch_bounds__(256) void k_operands(CePlan p, CeBuffers b, int parts) {
     const bool of_w = blockIdx.y != 0;
-    const int groups = static_cast<int>(gridDim.x) - 1;
+    const int groups = static_cast<int>(gridDim.x) - (is_scaled(FORM) ? 0 : 1);
     if (static_cast<int>(blockIdx.x) >= groups) {
         if (!of_w && p.grads) coefficients(p, b);
         return;
@@ -284,6 +290,51 @@ __global__ __launch_bounds__(256) void k_operands(CePlan p, CeBuffers b, int par
                 *reinterpret_cast<u16x4*>(out + c) = hi;
             }
         }
+    }
+}
+
+// w as the logits take it and transposed, as dh does (one half; a k-contiguous operand
+// gives the matrix cores 9% more than a k-strided one, and quarters past dim take
+// none): 64 words by up to 256 columns a work-group.  50257 x 768 bf16: 47 us, 4.9
+// TB/s; dh and dw of 8192 tokens 1.17 -> 1.09 ms by it.
+__global__ __launch_bounds__(256) void k_both(CePlan p, CeBuffers b, int parts) {
+    __shared__ u16 tile[64][64 + 4];
+    Scalars* s = reinterpret_cast<Scalars*>(b.workspace + p.scalars);
+    uint32_t top = 0;
+    for (int q = threadIdx.x; q < parts; q += 256) top = max(top, s->parts[1][q]);
+    top = largest_of_group(top);
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) s->w_max = top;
+    const float scale = ldexpf(1.f, exponent_for(top));
+    const int v0 = blockIdx.x * 64, four = (threadIdx.x & 15) * 4;
+    u16* w = reinterpret_cast<u16*>(b.workspace + p.w);
+    u16* wt = reinterpret_cast<u16*>(b.workspace + p.wt);
+    for (int d0 = blockIdx.y * 256; d0 < min(static_cast<int>(blockIdx.y + 1) * 256, static_cast<int>(p.ld_w)); d0 += 64) {
+        f4 in[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int v = v0 + k * 16 + (threadIdx.x >> 4), d = d0 + four;
+            in[k] = f4{0.f, 0.f, 0.f, 0.f};
+            if (v < p.vocab && d < p.dim) in[k] = load4<false>(b.w, v * b.w_stride + d, p.dim - d, b.w_vector);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int r = k * 16 + (threadIdx.x >> 4);
+            u16x4 x;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) x[q] = float_to_half(in[k][q] * scale);
+            if (v0 + r < p.vocab) *reinterpret_cast<u16x4*>(w + (v0 + r) * p.ld_w + d0 + four) = x;
+            *reinterpret_cast<u16x4*>(&tile[r][four]) = x;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int r = k * 16 + (threadIdx.x >> 4);
+            u16x4 x;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) x[q] = tile[four + q][r];
+            if (d0 + r < p.dim) *reinterpret_cast<u16x4*>(wt + (d0 + r) * p.ld_wt + v0 + four) = x;
+        }
+        __syncthreads();
     }
 }
 
@@ -826,10 +877,14 @@ __device__ __forceinline__ Operand g_rows(const CePlan& p, const CeBuffers& b) {
 
 // dh's sums over one piece, each of dh_splits parts into its own fp32 buffer: dh has few
 // tiles (96 of 256 x 256 for 8192 x 768), whose sums run over the whole vocabulary.
-template <CeForm FORM, int TM>
+template <CeForm FORM, int TM, bool TURNED>
+using DhTile = std::conditional_t<TURNED, tile::BigTile<elem(FORM), kContig, kContig, false>,
+                                  typename TokenTile<FORM, TM, kContig, kStrided>::T>;
+
+template <CeForm FORM, int TM, bool TURNED>
 __device__ __forceinline__ void dh_tile(const CePlan& p, const CeBuffers& b, int first, int cols, int id,
                                         DSM_LDS char* lds) {
-    using T = typename TokenTile<FORM, TM, kContig, kStrided>::T;
+    using T = DhTile<FORM, TM, TURNED>;
     constexpr int TN = T::kBN;
     const int tiles_t = (p.tokens + TM - 1) / TM, tiles_d = (p.dim + TN - 1) / TN;
     const int part = id / (tiles_t * tiles_d);
@@ -840,9 +895,12 @@ __device__ __forceinline__ void dh_tile(const CePlan& p, const CeBuffers& b, int
     const int k0 = min(part * each, cols_pad), k1 = min(k0 + each, cols_pad);
     T t;
     t.clear();
-    t.add(g_rows(p, b), w_rows(p, b, first), tt * TM, td * TN, k0, k1, lds, p.tokens - tt * TM, p.dim - td * TN);
+    const Operand w = TURNED ? Operand{reinterpret_cast<const u16*>(b.workspace + p.wt) + first, p.ld_wt, p.dim,
+                                       static_cast<int32_t>(p.ld_wt - first)}
+                             : w_rows(p, b, first);
+    t.add(g_rows(p, b), w, tt * TM, td * TN, k0, k1, lds, p.tokens - tt * TM, p.dim - td * TN);
     if constexpr (FORM == kCeBf16)
-        t.add(g_rows<true>(p, b), w_rows(p, b, first), tt * TM, td * TN, k0, k1, lds, p.tokens - tt * TM, p.dim - td * TN);
+        t.add(g_rows<true>(p, b), w, tt * TM, td * TN, k0, k1, lds, p.tokens - tt * TM, p.dim - td * TN);
     float* out = reinterpret_cast<float*>(b.workspace + p.dh) + part * p.tokens * p.ld_dh;
     const int ld = static_cast<int>(p.ld_dh);
     constexpr int kBatch = T::FI < 4 ? T::FI : 4;
@@ -974,7 +1032,7 @@ __device__ __forceinline__ void dw_tile(const CePlan& p, const CeBuffers& b, int
 
 // The two products of G in one launch: neither fills the CUs' last turn by itself,
 // and their tiles take different times.  Each XCD has its run of dh's tiles, the
-// longer ones, then its run of dw's.  8192 tokens of 50257 x 768 in bf16: 1.18 ms, 1.07
+// longer ones, then its run of dw's.  8192 tokens of 50257 x 768 in bf16: 1.09 ms, 1.16
 // PFLOP/s; what bounds it is LDS, whose transposing reads of k-strided operands give half
 // as much as plain ones, and the board's power: the clock falls to 1.7 GHz.
 constexpr int kXcds = 8;
@@ -983,14 +1041,15 @@ __host__ __device__ inline int per_xcd(int tiles) { return (tiles + kXcds - 1) /
 template <CeForm FORM, int TM, bool REFS>
 __global__ __launch_bounds__(threads_of(TM)) void k_gradients(CePlan p, CeBuffers b, int first, int cols,
                                                               int dh_tiles, int dw_tiles) {
-    using TD = typename TokenTile<FORM, TM, kContig, kStrided>::T;
+    constexpr bool kTurned = REFS && FORM == kCeHalf;
+    using TD = DhTile<FORM, TM, kTurned>;
     using TW = DwTile<FORM, TM, REFS>;
     constexpr int kLds = TD::kLdsBytes > TW::kLdsBytes ? TD::kLdsBytes : TW::kLdsBytes;
     __shared__ __align__(1024) char lds[kLds];
     const int x = blockIdx.x % kXcds, at = blockIdx.x / kXcds, front = per_xcd(dh_tiles);
     if (at < front) {
         const int id = x * front + at;
-        if (id < dh_tiles) dh_tile<FORM, TM>(p, b, first, cols, id, (DSM_LDS char*)lds);
+        if (id < dh_tiles) dh_tile<FORM, TM, kTurned>(p, b, first, cols, id, (DSM_LDS char*)lds);
     } else {
         const int id = x * per_xcd(dw_tiles) + at - front;
         if (id < dw_tiles) dw_tile<FORM, TM, REFS>(p, b, first, cols, id, (DSM_LDS char*)lds);
@@ -1000,8 +1059,8 @@ __global__ __launch_bounds__(threads_of(TM)) void k_gradients(CePlan p, CeBuffer
 // Few tokens: one by one, their tiles being of different shapes.
 template <CeForm FORM, int TM>
 __global__ __launch_bounds__(threads_of(TM)) void k_dh(CePlan p, CeBuffers b, int first, int cols) {
-    __shared__ __align__(1024) char lds[TokenTile<FORM, TM, kContig, kStrided>::T::kLdsBytes];
-    dh_tile<FORM, TM>(p, b, first, cols, xcd_run(blockIdx.x, gridDim.x), (DSM_LDS char*)lds);
+    __shared__ __align__(1024) char lds[DhTile<FORM, TM, false>::kLdsBytes];
+    dh_tile<FORM, TM, false>(p, b, first, cols, xcd_run(blockIdx.x, gridDim.x), (DSM_LDS char*)lds);
 }
 template <CeForm FORM, int TM>
 __global__ __launch_bounds__(tile::threads_of(square_of(TM))) void k_dw(CePlan p, CeBuffers b, int first, int cols) {
@@ -1107,16 +1166,18 @@ hipError_t launch_linear_ce(const CePlan& p, const CeBuffers& b, hipStream_t str
                 products<kCeF32, 64>(p, b, stream);
             break;
         case kCeHalf:
-            k_largest<false><<<dim3(parts, 2), 256, 0, stream>>>(p, b);
-            k_operands<kCeHalf><<<dim3(groups + 1, 2), 256, 0, stream>>>(p, b, parts);
+            k_largest<false><<<dim3(parts + 1, 2), 256, 0, stream>>>(p, b);
+            k_operands<kCeHalf><<<dim3(groups, p.ld_wt ? 1 : 2), 256, 0, stream>>>(p, b, parts);
+            if (p.ld_wt)
+                k_both<<<dim3((p.vocab + 63) / 64, (p.dim + 255) / 256), 256, 0, stream>>>(p, b, parts);
             if (p.tile == 128)
                 products<kCeHalf, 128>(p, b, stream);
             else
                 products<kCeHalf, 256>(p, b, stream);
             break;
         case kCeHalves:
-            k_largest<true><<<dim3(parts, 2), 256, 0, stream>>>(p, b);
-            k_operands<kCeHalves><<<dim3(groups + 1, 2), 256, 0, stream>>>(p, b, parts);
+            k_largest<true><<<dim3(parts + 1, 2), 256, 0, stream>>>(p, b);
+            k_operands<kCeHalves><<<dim3(groups, 2), 256, 0, stream>>>(p, b, parts);
             if (p.tile == 128)
                 products<kCeHalves, 128>(p, b, stream);
             else

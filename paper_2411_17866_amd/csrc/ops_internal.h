@@ -73,11 +73,12 @@ struct CePlan {
     int32_t dh_splits;   // parts of a piece that dh is summed over side by side
     int32_t sample;      // tile columns of the vocabulary that a row's reference is taken from (0: none)
     int32_t every;       // one of so many tile columns is
-    int64_t scalars, coef, lse, hit, stats, tops, refs, rows, h, ht, w, p, dh, bytes;
+    int64_t scalars, coef, lse, hit, stats, tops, refs, rows, h, ht, w, wt, p, dh, bytes;
     int64_t ld_h, ld_w, ld_p;  // 16-bit elements of a row
     int64_t p_lo;              // bf16 form: from G's upper halves to its lower ones
     int64_t ld_dh;             // floats of a row of dh's sums
     int64_t ld_ht;             // with references: of a row of h transposed
+    int64_t ld_wt;             // of a row of w transposed (0: there is none)
 };
 
 struct CeBuffers {

@@ -174,6 +174,10 @@ dsm::CePlan make_plan(const dsm_ce_problem* p) {
             q.rows = take(T * 8);
             q.ld_ht = tokens_pad * width;
             q.ht = take(p->dim * q.ld_ht * 2);
+            if (q.form == dsm::kCeHalf) {
+                q.ld_wt = round_up(V, 64);
+                q.wt = take(p->dim * q.ld_wt * 2);
+            }
         }
         // (In the bf16 form G is two arrays of halves.)
         q.p_lo = T * q.ld_p;

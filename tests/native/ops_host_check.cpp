@@ -133,6 +133,11 @@ static void check_plan(const dsm_ce_problem& p, const dsm::CePlan& q, int64_t ws
             parts.push_back({q.refs, T * 4});
             parts.push_back({q.rows, T * 8});
             parts.push_back({q.ht, D * q.ld_ht * 2});
+            CHECK((q.form == dsm::kCeHalf) == (q.ld_wt > 0));
+            if (q.ld_wt > 0) {
+                CHECK(q.ld_wt >= V && q.ld_wt % 64 == 0);
+                parts.push_back({q.wt, D * q.ld_wt * 2});
+            }
         }
         parts.push_back({q.p, all});
         parts.push_back({q.dh, q.dh_splits * T * q.ld_dh * 4});
