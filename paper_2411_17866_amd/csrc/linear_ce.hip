@@ -378,9 +378,8 @@ __device__ __forceinline__ Operand w_rows(const CePlan& p, const CeBuffers& b, i
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 
 // What brings a tile's accumulators to logits in units of log2.
-template <CeForm FORM>
-__device__ __forceinline__ float logit_unit(const CePlan& p, const CeBuffers& b) {
-    if constexpr (!is_scaled(FORM)) return kLog2e;
+__device__ __forceinline__ float logit_unit(CeForm form, const CePlan& p, const CeBuffers& b) {
+    if (!is_scaled(form)) return kLog2e;
     const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
     return ldexpf(kLog2e, -(exponent_for(s->h_max) + exponent_for(s->w_max)));
 }
@@ -504,7 +503,7 @@ __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b,
     t.add(h_rows(p, b), w_rows(p, b, 0), tt * TM, tv * TN, 0, static_cast<int>(p.ld_h / units(FORM)),
           (DSM_LDS char*)lds, p.tokens - tt * TM, p.vocab - tv * TN);
     // In units of log2: z2 = acc * unit, exp(z) = exp2(z2).
-    const float unit = logit_unit<FORM>(p, b);
+    const float unit = logit_unit(FORM, p, b);
     float* hit = reinterpret_cast<float*>(b.workspace + p.hit);
     float2* part = reinterpret_cast<float2*>(lds);  // [T::WN][TM]
     u16* g = reinterpret_cast<u16*>(b.workspace + p.p) + (tt * TM + t.row(0)) * p.ld_p;
@@ -553,7 +552,7 @@ __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b,
             for (int fj = 0; fj < T::FJ; ++fj)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    if (rel[fi] == t.col(fj) + r) hit[token] = t.acc[fi][fj][r] * unit;
+                    if (rel[fi] == t.col(fj) + r) hit[token] = t.acc[fi][fj][r];
         }
         top[fi] *= unit;
         // All logits -inf: no exponential counts (and -inf - -inf is none).
@@ -669,7 +668,7 @@ __global__ __launch_bounds__(256) void k_settle(CePlan p, CeBuffers b, int group
     u16* g = reinterpret_cast<u16*>(b.workspace + p.p) + token * p.ld_p;
     const int square = square_of(p.tile);
     const float* tops = reinterpret_cast<const float*>(b.workspace + p.tops) + static_cast<int64_t>(token) * (p.piece / square * 4);
-    // G is exp(z - x) mul, the target's entry (p - 1) of it.
+    // G is exp(z - x) mul, the target's entry p - 1 = expm1(-loss) of it.
     float x = lse, mul;
     if (is_scaled(FORM) && p.sample > 0) {
         const float ref = reinterpret_cast<const float*>(b.workspace + p.refs)[token];
@@ -680,8 +679,7 @@ __global__ __launch_bounds__(256) void k_settle(CePlan p, CeBuffers b, int group
             const int at = static_cast<int>(target) & ~7;
             float v[8];
             load_g<FORM>(p, g, at, v);
-            const float hit = reinterpret_cast<const float*>(b.workspace + p.hit)[token];
-            const float e = __builtin_amdgcn_exp2f(lse - x) * (__builtin_amdgcn_exp2f(hit - lse) - 1.f);
+            const float e = __builtin_amdgcn_exp2f(lse - x) * expm1f(-b.loss[token]);
 #pragma unroll
             for (int r = 0; r < 8; ++r)
                 if (target == at + r) v[r] = e;
@@ -699,8 +697,7 @@ __global__ __launch_bounds__(256) void k_settle(CePlan p, CeBuffers b, int group
 #pragma unroll
         for (int r = 0; r < 8; ++r) v[r] = valid ? v[r] * by : 0.f;
         if (valid && target >= at && target < at + 8) {
-            const float hit = reinterpret_cast<const float*>(b.workspace + p.hit)[token];
-            const float e = mul * __builtin_amdgcn_exp2f(lse - x) * (__builtin_amdgcn_exp2f(hit - lse) - 1.f);
+            const float e = mul * __builtin_amdgcn_exp2f(lse - x) * expm1f(-b.loss[token]);
 #pragma unroll
             for (int r = 0; r < 8; ++r)
                 if (target == at + r) v[r] = e;
@@ -777,10 +774,14 @@ __global__ __launch_bounds__(1024) void k_join(CePlan p, CeBuffers b, int tiles)
     }
     if (share != 0) return;
     a = part[0][lane];
-    const float lse2 = a.x + __builtin_amdgcn_logf(a.y);  // v_log_f32: log2
+    const float rest = log2f(a.y), lse2 = a.x + rest;
     const bool valid = token < p.tokens && is_valid(b.target[at], p.vocab);
-    const float loss =
-        valid ? (lse2 - reinterpret_cast<const float*>(b.workspace + p.hit)[at]) * kLn2 : 0.f;
+    // Of two logits of 30 and a loss of 0.01 the difference is what counts: the largest
+    // logit minus the target's in one rounding, not lse's rounding minus another.
+    const float hit = reinterpret_cast<const float*>(b.workspace + p.hit)[at];
+    float above = __builtin_fmaf(-hit, logit_unit(p.form, p, b), a.x);
+    if (!(fabsf(a.x) < __builtin_inff())) above = a.x - hit;
+    const float loss = valid ? (above + rest) * kLn2 : 0.f;
     if (token < p.tokens) {
         reinterpret_cast<float*>(b.workspace + p.lse)[token] = lse2;
         if (b.lse) b.lse[token] = lse2 * kLn2;
@@ -814,7 +815,7 @@ __global__ __launch_bounds__(threads_of(TM)) void k_piece(CePlan p, CeBuffers b,
     T t;
     t.run(h_rows(p, b), w_rows(p, b, first), tt * TM, tv * TN, 0, static_cast<int>(p.ld_h / units(FORM)),
           (DSM_LDS char*)lds, p.tokens - tt * TM, cols - tv * TN);
-    const float unit = logit_unit<FORM>(p, b);
+    const float unit = logit_unit(FORM, p, b);
     const int eg = !is_scaled(FORM) ? 0 : exponent_for(reinterpret_cast<const Scalars*>(b.workspace + p.scalars)->c_max);
     const float* lse = reinterpret_cast<const float*>(b.workspace + p.lse);
     const float* coef = reinterpret_cast<const float*>(b.workspace + p.coef);
@@ -824,7 +825,7 @@ __global__ __launch_bounds__(threads_of(TM)) void k_piece(CePlan p, CeBuffers b,
     const bool refs = is_scaled(FORM) && p.sample > 0;
     const float2* rows = reinterpret_cast<const float2*>(b.workspace + p.rows);
     int rel[T::FI];
-    float l[T::FI], c[T::FI], one[T::FI];
+    float l[T::FI], c[T::FI], less[T::FI];  // less: the target's entry, p - 1
 #pragma unroll
     for (int fi = 0; fi < T::FI; ++fi) {
         const int token = tt * TM + t.row(fi), at = min(token, p.tokens - 1);
@@ -834,7 +835,7 @@ __global__ __launch_bounds__(threads_of(TM)) void k_piece(CePlan p, CeBuffers b,
         const float x = refs ? rows[at].x : lse[at];
         l[fi] = valid ? x : __builtin_inff();
         c[fi] = !valid ? 0.f : refs ? 1.f : ldexpf(coef[at], eg);
-        one[fi] = refs ? __builtin_amdgcn_exp2f(lse[at] - x) : 1.f;
+        less[fi] = (refs ? __builtin_amdgcn_exp2f(lse[at] - x) : 1.f) * expm1f(-b.loss[at]);
     }
     const bool ragged = tv * TN + TN > cols;
 #pragma unroll
@@ -853,7 +854,7 @@ __global__ __launch_bounds__(threads_of(TM)) void k_piece(CePlan p, CeBuffers b,
             if (hits) {
 #pragma unroll
                 for (int r = 0; r < 8; ++r)
-                    if (rel[fi] == col + r) v[r] -= one[fi];
+                    if (rel[fi] == col + r) v[r] = less[fi];
             }
             const int at = tv * TN + col;
 #pragma unroll

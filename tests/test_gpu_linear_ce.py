@@ -326,3 +326,27 @@ def test_rows_far_from_what_a_part_of_the_vocabulary_tells(dtype):
     c_h = e["c"][:, None] * e["h"].abs()
     bounds["dw"] += 2.0 ** -34 * c_h.sum(0) + u_g * (e["g"].abs().t().contiguous() @ e["h"].abs())
     _check(out, e, bounds, ("total", "loss", "dh", "dw"))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_non_finite_among_many_tokens(dtype):
+    """NaN in a token that is left out reaches nothing; in a token that counts, its
+    dh and all of dw, and no other token's dh."""
+    tokens, dim, vocab = (4100 if dtype == BF16 else 2050), 64, 30011
+    h, w, t, weight = _problem(tokens, dim, vocab, dtype, seed=12, ignored=0.0)
+    ops = _ops()
+    plan = ops.LinearCE(tokens, dim, vocab, dtype=dtype)
+    t[777] = -1
+    clean = plan(h, w, t, weight=weight)
+    h[777, 5] = float("nan")
+    h[777, 6] = float("inf")
+    out = plan(h, w, t, weight=weight)
+    for name in ("total", "loss", "dh", "dw"):
+        assert torch.equal(clean[name], out[name]), name
+    h[1234, 7] = float("nan")
+    out = plan(h, w, t, weight=weight)
+    others = torch.arange(tokens, device="cuda") != 1234
+    assert torch.isnan(out["total"]) and torch.isnan(out["loss"][1234]) and torch.isnan(out["dh"][1234]).all()
+    assert torch.equal(out["dh"][others], clean["dh"][others])
+    assert torch.equal(out["loss"][others], clean["loss"][others])
+    assert torch.isnan(out["dw"]).all()
