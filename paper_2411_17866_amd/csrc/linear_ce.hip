@@ -482,7 +482,7 @@ __device__ __forceinline__ float row_from(CeForm f, float lse, float ref) {
 // the target's logit.  KEEP also writes exp(z - largest) in G's place for the first
 // piece, the largest being that of a wave's columns of the tile (wave_of), or
 // relative to the row's reference, and what they are relative to.  Of the tile
-// columns, tiles_v are taken, one of every `every`.
+// columns from `skip` on tiles_v are taken, one of every `every`, into slots from `slot`.
 //
 // Many tokens, bf16: 8192 of 50257 x 768 in 0.79 ms, 0.80 PFLOP/s.  Of a tile's 32 us
 // the products take 18 (1.44 PFLOP/s), the writes of exponentials 6 (at 5.7 TB/s; one
@@ -490,14 +490,15 @@ __device__ __forceinline__ float row_from(CeForm f, float lse, float ref) {
 // of the next tile 8.  One token reads w, 77 MB, in 15 us at 5.1 TB/s; tiles of 32 tokens
 // by 128 words with four stages on their way fill two work-groups a CU for that.
 template <CeForm FORM, int TM, bool KEEP>
-__global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b, int tiles_v, int every) {
+__global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b, int tiles_v, int every, int skip,
+                                                          int slot) {
     using T = typename TokenTile<FORM, TM, kContig, kContig>::T;
     constexpr int TN = T::kBN;
     __shared__ __align__(1024) char lds[T::kLdsBytes];
     const int tiles_t = (p.tokens + TM - 1) / TM;
     int tt, at;
     logit_tile(xcd_run(blockIdx.x, tiles_t * tiles_v), tiles_t, tiles_v, &tt, &at);
-    const int tv = at * every;
+    const int tv = skip + at * every;
     T t;
     t.clear();
     t.add(h_rows(p, b), w_rows(p, b, 0), tt * TM, tv * TN, 0, static_cast<int>(p.ld_h / units(FORM)),
@@ -597,7 +598,7 @@ __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b,
         }
     }
     __syncthreads();
-    float2* stats = reinterpret_cast<float2*>(b.workspace + p.stats) + static_cast<int64_t>(at) * p.tokens;
+    float2* stats = reinterpret_cast<float2*>(b.workspace + p.stats) + static_cast<int64_t>(slot + at) * p.tokens;
     for (int r = threadIdx.x; r < TM; r += T::kThreads) {
         if (tt * TM + r >= p.tokens) break;
         float2 a = part[r];
@@ -1088,15 +1089,27 @@ void products(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
         if (p.grads) {
             if constexpr (kRefs) {
                 if (p.sample > 0) {
-                    k_stats<FORM, TM, false><<<tt * p.sample, kThreads, 0, stream>>>(p, b, p.sample, p.every);
+                    k_stats<FORM, TM, false><<<tt * p.sample, kThreads, 0, stream>>>(p, b, p.sample, p.every, 0, 0);
                     k_refs<<<(p.tokens + 15) / 16, 256, 0, stream>>>(p, b);
                 }
             }
-            k_stats<FORM, TM, true><<<tt * tv, kThreads, 0, stream>>>(p, b, tv, 1);
+            k_stats<FORM, TM, true><<<tt * tv, kThreads, 0, stream>>>(p, b, tv, 1, 0, 0);
         }
     }
-    if (!p.grads) k_stats<FORM, TM, false><<<tt * tv, kThreads, 0, stream>>>(p, b, tv, 1);
-    k_join<<<(p.tokens + kJoinTokens - 1) / kJoinTokens, 1024, 0, stream>>>(p, b, tv);
+    int slots = tv;
+    if (!p.grads) {
+        int front = tv;
+        if constexpr (TM == 256) front = p.front;
+        k_stats<FORM, TM, false><<<tt * front, kThreads, 0, stream>>>(p, b, front, 1, 0, 0);
+        if constexpr (TM == 256) {
+            if (front < tv) {
+                const int rest = (p.vocab - front * 256 + 127) / 128;
+                k_stats<FORM, 128, false><<<(p.tokens + 127) / 128 * rest, kThreads, 0, stream>>>(p, b, rest, 1, front * 2, front);
+                slots = front + rest;
+            }
+        }
+    }
+    k_join<<<(p.tokens + kJoinTokens - 1) / kJoinTokens, 1024, 0, stream>>>(p, b, slots);
     if (!p.grads && p.tokens > kJoinTokens) k_total<<<1, 1024, 0, stream>>>(p, b);
     if constexpr (FORM != kCeBf16 || TM < 256) {
         if (!p.grads) return;

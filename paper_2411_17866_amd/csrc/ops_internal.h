@@ -69,6 +69,7 @@ struct CePlan {
     CeForm form;
     int32_t grads;
     int32_t tile;        // tokens of a work-group's tile: 32, 64, 128 or 256
+    int32_t front;       // losses alone: tile columns of 256 words; tiles of 128 take what follows
     int32_t piece;       // columns of the vocabulary whose gradients are in memory at once
     int32_t dh_splits;   // parts of a piece that dh is summed over side by side
     int32_t sample;      // tile columns of the vocabulary that a row's reference is taken from (0: none)

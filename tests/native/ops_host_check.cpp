@@ -107,12 +107,17 @@ static void check_plan(const dsm_ce_problem& p, const dsm::CePlan& q, int64_t ws
     const int64_t units = f32 ? 2 : 1, square = q.tile == 256 ? 256 : 128;
     const int64_t wide = (D + 63) / 64 * 64 * units, high = (T + 63) / 64 * 64;
     CHECK(q.ld_h == wide && q.ld_w == wide);
+    // Losses alone: columns by tiles of 256, then by 128.
+    const int64_t columns = (V + 255) / 256;
+    CHECK(q.front >= 1 && q.front <= columns && (q.front == columns || (q.tile == 256 && !p.grads)));
+    const int64_t slots = q.front == columns ? (V + square - 1) / square
+                                             : q.front + (V - 256 * int64_t(q.front) + 127) / 128;
     // Parts in order, at 256 bytes, each long enough for what the kernels write.
     struct Part {
         int64_t at, bytes;
     };
     std::vector<Part> parts = {{q.scalars, dsm::kCeScalars}, {q.coef, 4 * T}, {q.lse, 4 * T}, {q.hit, 4 * T},
-                               {q.stats, (V + square - 1) / square * T * 8}, {q.h, high * wide * 2}, {q.w, V * wide * 2}};
+                               {q.stats, slots * T * 8}, {q.h, high * wide * 2}, {q.w, V * wide * 2}};
     if (p.grads && T > 0) {
         CHECK(q.piece > 0 && q.piece % square == 0 && q.piece < V + square);
         CHECK(q.dh_splits >= 1 && q.dh_splits <= 128);
