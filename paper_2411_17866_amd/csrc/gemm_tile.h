@@ -468,7 +468,7 @@ struct HalfSide {
 // 1440-1500 TFLOP/s of matrix instructions.  What bounds it is the board's power:
 // the clock falls to 1.6-1.8 GHz, at which split operands keep the matrix cores
 // 90% busy and fp16 72%; the k-strided reads take the rest.
-template <Elem E, Kind KI, Kind KJ, bool QUARTERS = KI == kContig && KJ == kContig>
+template <Elem E, Kind KI, Kind KJ, bool QUARTERS = KI == kContig && KJ == kContig, bool NARROW = false>
 struct BigTile {
     static_assert(E != kF32, "fp32 products are for tiles that wait for memory");
     static constexpr int S = units(E);
@@ -481,6 +481,7 @@ struct BigTile {
     static constexpr bool kAhead = S == 1;  // J0 is read a turn before its stage
     // Quarters without wanted rows or columns are left out by loops of their own.  (A
     // branch in the loop, or these loops beside k-strided loads, spill registers.)
+    // NARROW: 128 columns at most are wanted, without asking.
     static constexpr bool kQuarters = QUARTERS;
     static constexpr int kStageBytes = 4 * kHalf;  // J0, I0, J1, I1
     static constexpr int kLdsBytes = 2 * kStageBytes;
@@ -581,7 +582,7 @@ struct BigTile {
         }
         if (wave >= 4) turn_over();
         if (!kQuarters || (tall && wide))
-            stages<2, 4>(si, sj, k_begin, k_end, lds);
+            stages<2, NARROW ? 2 : 4>(si, sj, k_begin, k_end, lds);
         else if (tall)
             stages<2, 2>(si, sj, k_begin, k_end, lds);
         else if (wide)
