@@ -15,7 +15,7 @@
 //     computes anew.  6 T V D operations of the matrix cores.
 //   * For the others the logits are computed again, 8 T V D in all.
 // 8192 tokens of 50257 x 768 in bf16, whose G is 0.8 GB: 2.87 ms by two pieces, both
-// computed again; 2.28 ms by one; 2.04 ms with what follows.
+// computed again; 2.28 ms by one; 1.89 ms with what follows.
 //
 // The light pass itself is saved, with many tokens and a large vocabulary, by a
 // reference r_t for each row that is near lse_t and known before the first pass: the
@@ -484,7 +484,7 @@ __device__ __forceinline__ float row_from(CeForm f, float lse, float ref) {
 // relative to the row's reference, and what they are relative to.  Of the tile
 // columns from `skip` on tiles_v are taken, one of every `every`, into slots from `slot`.
 //
-// Many tokens, bf16: 8192 of 50257 x 768 in 0.79 ms, 0.80 PFLOP/s.  Of a tile's 32 us
+// Many tokens, bf16: 8192 of 50257 x 768 in 0.81 ms, 0.78 PFLOP/s.  Of a tile's 32 us
 // the products take 18 (1.44 PFLOP/s), the writes of exponentials 6 (at 5.7 TB/s; one
 // work-group fills a CU, so nothing runs beside them), exponentials, sums and the start
 // of the next tile 8.  One token reads w, 77 MB, in 15 us at 5.1 TB/s; tiles of 32 tokens
