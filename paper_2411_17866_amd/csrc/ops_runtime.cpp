@@ -99,7 +99,8 @@ void cut(dsm::CePlan* q, int64_t T, int64_t D, int64_t V) {
     // Whether rows get a reference from a sample (linear_ce.hip), which takes a turn of
     // the logits' tiles (at least a 64th of the vocabulary) and saves reading and
     // writing G of the first piece at 5.8 TB/s.  8192 tokens of 50257 x 768 in bf16:
-    // 2.04 ms with references (2.30 where no row fits its own), 2.28 without, then.
+    // 1.96 ms with references and what they allow (dw, dh from operands transposed), 2.35
+    // without; rows that all miss their reference 2.19 and 2.26.
     if (square == 256) {
         const int64_t n = std::max(std::max<int64_t>(256 / t, 1), tiles(V, 64 * 256));
         const double sample = turns(n * t) * (static_cast<double>(D) / 64 * step + 5.0) + 12.0;
