@@ -32,6 +32,7 @@
 
 #include "gemm_tile.h"
 #include "ops_internal.h"
+#include "ortho_plan.h"
 
 #pragma clang fp contract(off)
 
@@ -527,21 +528,7 @@ __global__ __launch_bounds__(tile::threads_of(BM)) void k_product(OrthoGroup g, 
 // Operands are stored as gemm_tile.h's stages are: for each 32 columns all rows of
 // 128 bytes (hi x 32, lo x 32), the 16-byte pieces of a row exchanged by its number.
 
-constexpr int kSmallLds = 144 << 10;
-constexpr int kSmallWaves = 8;
-constexpr int kSmallSquare = 5;   // fragments of A that a wave has, at most (96 x 96)
-constexpr int kSmallWide = 18;    // fragments of X
-
 __host__ __device__ inline int pad32(int v) { return (v + 31) / 32 * 32; }
-// It has to fit, and to be little: a wave's products of 16 x 16 x 32 in an iteration
-// take it about 0.2 us each here, five iterations 12 us + 1 us each: 64 x 64, 12 of
-// them, 30 us (68 us by the products' kernels); 128 x 128, 96, 107 us (70-85 us).
-inline bool is_small(int m, int n) {
-    const int64_t mp = pad32(m), np = pad32(n), mi = mp / 16;
-    const int64_t products = mi * mi * (np / 32 + mp / 32) + mi * (np / 16) * (mp / 32);
-    return mp * (mp + np) * 4 <= kSmallLds && mi * mi <= kSmallSquare * kSmallWaves &&
-           mi * (np / 16) <= kSmallWide * kSmallWaves && products <= 50 * kSmallWaves;
-}
 
 // Factors of the accumulators and of what is added to them, for each iteration.
 struct SmallSteps {
@@ -740,33 +727,12 @@ __global__ __launch_bounds__(kSmallWaves * 64) void k_small(OrthoGroup g, SmallS
 
 float pow2(int e) { return __builtin_ldexpf(1.0f, e); }
 
-// Work-groups of a product by tiles of bm.
-unsigned groups_of(const OrthoGroup& g, int bm, bool symmetric) {
-    const unsigned ti = (g.m + bm - 1) / bm, tj = (g.n + bm - 1) / bm;
-    return (symmetric ? ti * (ti + 1) / 2 : ti * tj) * g.count;
-}
-
-// The tile a product takes: the one whose turns over the CUs take least.  A CU
-// holds one work-group of 256, two of 128 or of 64; a turn of 128 takes 0.62, of 64
-// 0.40 (0.28 where a CU has one of them) of what a turn of 256 does, measured over
-// batches from 1 x 64 x 64 to 8 x 1600 x 6400.  One 512 x 1536 fp32 matrix: A in
-// 18 us by 36 tiles of 64, 41 us by 10 of 128; twelve of 768 x 2304: 68, 63 and
-// 124 us by 936, 252 and 72 tiles of 64, 128 and 256.
-int tile_of(const OrthoGroup& g, bool symmetric) {
-    const auto turns = [](unsigned groups, unsigned slots) { return (groups + slots - 1) / slots; };
-    const unsigned small = groups_of(g, 64, symmetric);
-    const float t64 = small <= 256 ? 0.28f : 0.40f * turns(small, 512);
-    const float t128 = 0.62f * turns(groups_of(g, 128, symmetric), 512);
-    const float t256 = 1.0f * turns(groups_of(g, 256, symmetric), 256);
-    return t64 <= t128 && t64 <= t256 ? 64 : t128 <= t256 ? 128 : 256;
-}
-
 template <int S, Product P>
 void product(const OrthoGroup& g, const Parts& parts, int from, float mul, float add, int fallen, int next,
              hipStream_t stream) {
     constexpr bool kSymmetric = P == kGram || P == kPoly;
-    const int bm = tile_of(g, kSymmetric);
-    const unsigned groups = groups_of(g, bm, kSymmetric);
+    const int bm = ortho_tile(g.count, g.m, g.n, kSymmetric);
+    const unsigned groups = ortho_groups(g.count, g.m, g.n, bm, kSymmetric);
     if (bm == 64)
         k_product<S, 64, P><<<groups, tile::threads_of(64), 0, stream>>>(g, parts, from, mul, add, fallen, next);
     else if (bm == 128)
