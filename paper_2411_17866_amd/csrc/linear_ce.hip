@@ -377,11 +377,14 @@ __device__ __forceinline__ Operand w_rows(const CePlan& p, const CeBuffers& b, i
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 
-// What brings a tile's accumulators to logits in units of log2.
+// What brings a tile's accumulators to logits in units of log2: a positive normal
+// number, so that logits of -inf (the columns past the vocabulary) stay -inf, and 0 stays
+// 0, where h and w are both tiny or both huge.  (Accumulators stay below 2^46: times
+// 2^-126 nothing is left of them beside 1, as of the logits they stand for.)
 __device__ __forceinline__ float logit_unit(CeForm form, const CePlan& p, const CeBuffers& b) {
     if (!is_scaled(form)) return kLog2e;
     const Scalars* s = reinterpret_cast<const Scalars*>(b.workspace + p.scalars);
-    return ldexpf(kLog2e, -(exponent_for(s->h_max) + exponent_for(s->w_max)));
+    return ldexpf(kLog2e, max(-126, min(126, -(exponent_for(s->h_max) + exponent_for(s->w_max)))));
 }
 
 // Largest exponent and sum of exp2(z2 - largest) of two sets of logits.

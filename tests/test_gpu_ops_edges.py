@@ -1,0 +1,46 @@
+"""The operators where plain arithmetic would not notice anything: magnitudes at the
+ends of fp32, rows that are nearly sure of their target, launches past 2^32 threads,
+non-finite words, zeros without eps."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import ops_norms as N  # noqa: E402
+import ops_oracle as O  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+DTYPES = pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+# Through every form: w read in place, tiles of 128, of 256, and with references; vocabularies
+# that fit no tile.
+SIZES = pytest.mark.parametrize("size", [(5, 64, 1001), (100, 64, 1001), (600, 64, 1001), (200, 72, 50257),
+                                         (4100, 64, 30011)], ids=str)
+
+
+def _ops():
+    from paper_2411_17866_amd import ops
+    return ops
+
+
+def _normal(*shape, seed=0):
+    return torch.empty(shape, device="cuda").normal_(0, 1, generator=torch.Generator(device="cuda").manual_seed(seed))
+
+
+@DTYPES
+@SIZES
+def test_both_operands_tiny(size, dtype):
+    """Logits of 1e-38 are equal ones: the loss is log(vocab), and the gradients are
+    those of even rows."""
+    tokens, dim, vocab = size
+    h, w = (1e-20 * _normal(tokens, dim, seed=1)).to(dtype), (1e-18 * _normal(vocab, dim, seed=2)).to(dtype)
+    t = torch.arange(tokens, device="cuda") * 7 % vocab
+    for grads in (True, False):
+        out = _ops().LinearCE(*size, dtype=dtype, grads=grads)(h, w, t, mean=False)
+        assert (out["loss"] - math.log(vocab)).abs().max() <= 2.0 ** -21 * math.log(vocab)
+        assert abs(float(out["total"]) / tokens - math.log(vocab)) <= 2.0 ** -21 * math.log(vocab)
+        if grads:
+            e = N.linear_ce(h, w, t, mean=False)
+            assert N.off(out["dh"], e["dh"]) <= N.GRAD[dtype] and N.off(out["dw"], e["dw"]) <= N.GRAD[dtype]
