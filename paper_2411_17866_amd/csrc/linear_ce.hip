@@ -485,7 +485,8 @@ __device__ __forceinline__ float row_from(CeForm f, float lse, float ref) {
 // the target's logit.  KEEP also writes exp(z - largest) in G's place for the first
 // piece, the largest being that of a wave's columns of the tile (wave_of), or
 // relative to the row's reference, and what they are relative to.  Of the tile
-// columns from `skip` on tiles_v are taken, one of every `every`, into slots from `slot`.
+// columns from `skip` on tiles_v are taken, one of every `every`, into slots from `slot`;
+// `done` tiles were taken by launches before this one.
 //
 // Many tokens, bf16: 8192 of 50257 x 768 in 0.81 ms, 0.78 PFLOP/s.  Of a tile's 32 us
 // the products take 18 (1.44 PFLOP/s), the writes of exponentials 6 (at 5.7 TB/s; one
@@ -494,13 +495,13 @@ __device__ __forceinline__ float row_from(CeForm f, float lse, float ref) {
 // by 128 words with four stages on their way fill two work-groups a CU for that.
 template <CeForm FORM, int TM, bool KEEP>
 __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b, int tiles_v, int every, int skip,
-                                                          int slot) {
+                                                          int slot, int done) {
     using T = typename TokenTile<FORM, TM, kContig, kContig>::T;
     constexpr int TN = T::kBN;
     __shared__ __align__(1024) char lds[T::kLdsBytes];
     const int tiles_t = (p.tokens + TM - 1) / TM;
     int tt, at;
-    logit_tile(xcd_run(blockIdx.x, tiles_t * tiles_v), tiles_t, tiles_v, &tt, &at);
+    logit_tile(done + xcd_run(blockIdx.x, gridDim.x), tiles_t, tiles_v, &tt, &at);
     const int tv = skip + at * every;
     T t;
     t.clear();
@@ -1111,6 +1112,16 @@ __global__ __launch_bounds__(256) void k_nothing(CePlan p, CeBuffers b) {
             store_grad<F32>(b.dw, r * b.dw_stride + c, f4{0.f, 0.f, 0.f, 0.f}, p.dim - c, b.dw_vector);
 }
 
+// A launch holds fewer than 2^32 threads, which 2^20 tokens by 2^19 words have.
+constexpr int kMostGroups = 1 << 22;
+template <CeForm FORM, int TM, bool KEEP>
+void stats(const CePlan& p, const CeBuffers& b, int tiles_v, int every, int skip, int slot, hipStream_t stream) {
+    const int tiles = (p.tokens + TM - 1) / TM * tiles_v;
+    for (int done = 0; done < tiles; done += kMostGroups)
+        k_stats<FORM, TM, KEEP><<<std::min(tiles - done, kMostGroups), threads_of(TM), 0, stream>>>(p, b, tiles_v, every, skip,
+                                                                                                 slot, done);
+}
+
 template <CeForm FORM, int TM>
 void products(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
     constexpr int kThreads = threads_of(TM), TN = square_of(TM);
@@ -1120,22 +1131,22 @@ void products(const CePlan& p, const CeBuffers& b, hipStream_t stream) {
         if (p.grads) {
             if constexpr (kRefs) {
                 if (p.sample > 0) {
-                    k_stats<FORM, TM, false><<<tt * p.sample, kThreads, 0, stream>>>(p, b, p.sample, p.every, 0, 0);
+                    stats<FORM, TM, false>(p, b, p.sample, p.every, 0, 0, stream);
                     k_refs<<<(p.tokens + 15) / 16, 256, 0, stream>>>(p, b);
                 }
             }
-            k_stats<FORM, TM, true><<<tt * tv, kThreads, 0, stream>>>(p, b, tv, 1, 0, 0);
+            stats<FORM, TM, true>(p, b, tv, 1, 0, 0, stream);
         }
     }
     int slots = tv;
     if (!p.grads) {
         int front = tv;
         if constexpr (TM == 256) front = p.front;
-        k_stats<FORM, TM, false><<<tt * front, kThreads, 0, stream>>>(p, b, front, 1, 0, 0);
+        stats<FORM, TM, false>(p, b, front, 1, 0, 0, stream);
         if constexpr (TM == 256) {
             if (front < tv) {
                 const int rest = (p.vocab - front * 256 + 127) / 128;
-                k_stats<FORM, 128, false><<<(p.tokens + 127) / 128 * rest, kThreads, 0, stream>>>(p, b, rest, 1, front * 2, front);
+                stats<FORM, 128, false>(p, b, rest, 1, front * 2, front, stream);
                 slots = front + rest;
             }
         }

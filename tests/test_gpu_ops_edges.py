@@ -44,3 +44,15 @@ def test_both_operands_tiny(size, dtype):
         if grads:
             e = N.linear_ce(h, w, t, mean=False)
             assert N.off(out["dh"], e["dh"]) <= N.GRAD[dtype] and N.off(out["dw"], e["dw"]) <= N.GRAD[dtype]
+
+
+def test_more_threads_than_a_launch_takes():
+    """2^20 tokens by 2^19 words: 2^32 threads over the logits' tiles."""
+    tokens, dim, vocab = 1 << 20, 8, 1 << 19
+    h, w = _normal(tokens, dim, seed=5).to(BF16), _normal(vocab, dim, seed=6).to(BF16)
+    t = torch.randint(0, vocab, (tokens,), device="cuda")
+    out = _ops().LinearCE(tokens, dim, vocab, dtype=BF16, grads=False)(h, w, t)
+    rows = torch.cat([torch.arange(0, tokens, 16411, device="cuda"), torch.arange(tokens - 20, tokens, device="cuda")])
+    e = N.linear_ce(h[rows], w, t[rows], grads=False)
+    assert N.off(out["loss"][rows], e["loss"]) <= N.LOSS
+    assert abs(float(out["total"]) - float(out["loss"].double().mean())) <= 1e-6 * float(out["total"])
