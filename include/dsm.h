@@ -392,7 +392,7 @@ typedef struct dsm_ce_buffers {
     const float* weight;   /* [T] weight of each token's loss, or NULL for 1 */
     float* total;          /* [1] */
     float* loss;           /* [T] loss of each token, unweighted; 0 where left out */
-    float* lse;            /* [T] log of the sum of exp z, or NULL */
+    float* lse;            /* [T] log of the sum of exp z, 0 where left out; or NULL */
     void* dh;              /* [T, D], rows dh_stride apart; NULL without gradients */
     int64_t dh_stride;
     void* dw;              /* [V, D], rows dw_stride apart; NULL without gradients */

@@ -789,7 +789,7 @@ __global__ __launch_bounds__(1024) void k_join(CePlan p, CeBuffers b, int tiles)
     const float loss = valid ? (above + rest) * kLn2 : 0.f;
     if (token < p.tokens) {
         reinterpret_cast<float*>(b.workspace + p.lse)[token] = lse2;
-        if (b.lse) b.lse[token] = lse2 * kLn2;
+        if (b.lse) b.lse[token] = valid ? lse2 * kLn2 : 0.f;
         b.loss[token] = loss;
         if (p.sample > 0) {
             const float ref = reinterpret_cast<const float*>(b.workspace + p.refs)[token];

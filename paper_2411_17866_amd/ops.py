@@ -95,8 +95,9 @@ class LinearCE(_Plan):
                  total=None, lse=None):
         """{"total", "loss"} and, with gradients, {"dh", "dw"}: total (a scalar)
         is the sum of weight * loss, divided by the number of targets inside the
-        vocabulary when mean; loss (tokens,) is 0 where the target lies outside;
-        dh and dw are total's gradients.  Outputs are written into the tensors
+        vocabulary when mean; loss (tokens,) and lse (tokens,), which is written
+        where given, are 0 where the target lies outside; dh and dw are total's
+        gradients.  Outputs are written into the tensors
         given, or into new ones."""
         buf = dsm.dsm_ce_buffers()
         buf.h_stride = self._rows("h", h, self.h_shape)

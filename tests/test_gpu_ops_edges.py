@@ -56,3 +56,19 @@ def test_more_threads_than_a_launch_takes():
     e = N.linear_ce(h[rows], w, t[rows], grads=False)
     assert N.off(out["loss"][rows], e["loss"]) <= N.LOSS
     assert abs(float(out["total"]) - float(out["loss"].double().mean())) <= 1e-6 * float(out["total"])
+
+
+@DTYPES
+@pytest.mark.parametrize("dim", [64, 60])  # h read in place, and copied
+@pytest.mark.parametrize("grads", [True, False])
+@pytest.mark.parametrize("tokens", [5, 100, 600])
+def test_lse_of_tokens_without_a_target(tokens, grads, dim, dtype):
+    vocab = 300
+    h, w = _normal(tokens, dim, seed=9).to(dtype), (dim ** -0.5 * _normal(vocab, dim, seed=10)).to(dtype)
+    t = torch.randint(0, vocab, (tokens,), device="cuda")
+    t[::2] = -1
+    lse = torch.full((tokens,), float("nan"), device="cuda")
+    _ops().LinearCE(tokens, dim, vocab, dtype=dtype, grads=grads)(h, w, t, lse=lse)
+    assert (lse[::2] == 0).all()
+    want = torch.logsumexp(h[1::2].double() @ w.double().t().contiguous(), 1)
+    assert (lse[1::2].double() - want).abs().max() <= 2.0 ** -18
