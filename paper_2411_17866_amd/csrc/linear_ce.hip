@@ -826,10 +826,11 @@ __global__ __launch_bounds__(threads_of(TM)) void k_piece(CePlan p, CeBuffers b,
     const float* coef = reinterpret_cast<const float*>(b.workspace + p.coef);
     u16* g = reinterpret_cast<u16*>(b.workspace + p.p) + (tt * TM + t.row(0)) * p.ld_p;
     // What the rows need, all loaded before the first store.  A row without a
-    // valid target gets exp2(z2 - inf) = 0 throughout.  With references, E.
+    // valid target gets 0 throughout.  With references, E.
     const bool refs = is_scaled(FORM) && p.sample > 0;
     const float2* rows = reinterpret_cast<const float2*>(b.workspace + p.rows);
     int rel[T::FI];
+    bool counts[T::FI];
     float l[T::FI], c[T::FI], less[T::FI];  // less: the target's entry, p - 1
 #pragma unroll
     for (int fi = 0; fi < T::FI; ++fi) {
@@ -838,8 +839,9 @@ __global__ __launch_bounds__(threads_of(TM)) void k_piece(CePlan p, CeBuffers b,
         const bool valid = token < p.tokens && is_valid(target, p.vocab);
         rel[fi] = valid ? static_cast<int>(target) - first - tv * TN : -1;
         const float x = refs ? rows[at].x : lse[at];
-        l[fi] = valid ? x : __builtin_inff();
-        c[fi] = !valid ? 0.f : refs ? 1.f : ldexpf(coef[at], eg);
+        counts[fi] = valid;
+        l[fi] = x;
+        c[fi] = refs ? 1.f : ldexpf(coef[at], eg);
         less[fi] = (refs ? __builtin_amdgcn_exp2f(lse[at] - x) : 1.f) * expm1f(-b.loss[at]);
     }
     const bool ragged = tv * TN + TN > cols;
@@ -864,7 +866,7 @@ __global__ __launch_bounds__(threads_of(TM)) void k_piece(CePlan p, CeBuffers b,
             const int at = tv * TN + col;
 #pragma unroll
             for (int r = 0; r < 8; ++r) {
-                v[r] *= c[fi];
+                v[r] = counts[fi] ? v[r] * c[fi] : 0.f;
                 if (ragged && at + r >= cols) v[r] = 0.f;
             }
             if (at < cols_pad) store_g<FORM>(p, g + (t.row(fi) - t.row(0)) * p.ld_p, at, v);
@@ -1001,8 +1003,10 @@ __global__ __launch_bounds__(256) void k_dh_join(CePlan p, CeBuffers b, int firs
     if (wave != 0 || d >= p.dim) return;
     v = (v + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
     const float by = refs ? reinterpret_cast<const float2*>(b.workspace + p.rows)[row].y : 1.f;
+    // (A row of zeros in G meets what w holds, NaN included.)
+    const bool valid = is_valid(b.target[row], p.vocab);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = ldexpf(v[r], ex) * by;
+    for (int r = 0; r < 4; ++r) v[r] = valid ? ldexpf(v[r], ex) * by : 0.f;
     store_grad<is_f32(FORM)>(b.dh, row * b.dh_stride + d, v, p.dim - d, b.dh_vector);
 }
 

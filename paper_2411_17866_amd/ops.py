@@ -97,8 +97,7 @@ class LinearCE(_Plan):
         is the sum of weight * loss, divided by the number of targets inside the
         vocabulary when mean; loss (tokens,) and lse (tokens,), which is written
         where given, are 0 where the target lies outside; dh and dw are total's
-        gradients.  Outputs are written into the tensors
-        given, or into new ones."""
+        gradients.  Outputs are written into the tensors given, or into new ones."""
         buf = dsm.dsm_ce_buffers()
         buf.h_stride = self._rows("h", h, self.h_shape)
         buf.w_stride = self._rows("w", w, self.w_shape)

@@ -72,3 +72,44 @@ def test_lse_of_tokens_without_a_target(tokens, grads, dim, dtype):
     assert (lse[::2] == 0).all()
     want = torch.logsumexp(h[1::2].double() @ w.double().t().contiguous(), 1)
     assert (lse[1::2].double() - want).abs().max() <= 2.0 ** -18
+
+
+@DTYPES
+@SIZES
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_non_finite_words_leave_tokens_without_a_target_alone(size, dtype, value):
+    tokens, dim, vocab = size
+    h, w = _normal(tokens, dim, seed=7).to(dtype), (dim ** -0.5 * _normal(vocab, dim, seed=8)).to(dtype)
+    t = torch.randint(0, vocab, (tokens,), device="cuda")
+    out_of = torch.arange(tokens, device="cuda") % 3 == 1
+    t[out_of] = -1
+    w[vocab // 2, 3] = value
+    lse = torch.full((tokens,), float("nan"), device="cuda")
+    out = _ops().LinearCE(*size, dtype=dtype)(h, w, t, lse=lse)
+    for x in (out["dh"], out["loss"], lse):
+        assert (x[out_of] == 0).all()
+    # (A logit of -inf leaves its token a probability of 0 there: 0 * inf in one column.)
+    assert torch.isnan(out["dh"][~out_of][:, 3]).all()
+    if value != value:
+        assert torch.isnan(out["dh"][~out_of]).all() and torch.isnan(out["total"])
+    # No token that counts: nothing is left.
+    t.fill_(vocab)
+    out = _ops().LinearCE(*size, dtype=dtype)(h, w, t, lse=lse)
+    for x in (out["dh"], out["dw"], out["loss"], out["total"], lse):
+        assert (x == 0).all()
+
+
+@pytest.mark.parametrize("size,dtype", [((4500, 64, 65001), F32), ((9000, 64, 65001), BF16)], ids=str)
+def test_non_finite_words_of_a_later_piece(size, dtype):
+    """Two pieces of the vocabulary; no token counts, then some."""
+    tokens, dim, vocab = size
+    h, w = _normal(tokens, dim, seed=7).to(dtype), (dim ** -0.5 * _normal(vocab, dim, seed=8)).to(dtype)
+    w[vocab - 5, 3] = float("nan")
+    t = torch.full((tokens,), -1, device="cuda")
+    plan = _ops().LinearCE(*size, dtype=dtype)
+    out = plan(h, w, t)
+    for name, x in out.items():
+        assert (x == 0).all(), name
+    t[::2] = 11
+    out = plan(h, w, t)
+    assert (out["dh"][1::2] == 0).all() and torch.isnan(out["dh"][::2]).all()
