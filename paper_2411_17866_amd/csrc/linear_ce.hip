@@ -21,11 +21,19 @@
 // reference r_t for each row that is near lse_t and known before the first pass: the
 // logarithm of the sum over a few tiles of the vocabulary, a turn of the CUs, scaled
 // to all of it.  Exponentials are then kept relative to r_t and stay as they are:
-//   G_tv = s_t E_tv,  E_tv = exp(z_tv - x_t) - [v = target] exp(lse_t - x_t),
-//   s_t = c_t exp(x_t - lse_t),  x_t a constant below r_t
+//   G_tv = s_t E_tv,  E_tv = 2^k (exp(z_tv - x_t) - [v = target] exp(lse_t - x_t)),
+//   s_t = 2^-k c_t exp(x_t - lse_t),  x_t = r_t
 // dh's sums are multiplied by s_t where they are joined, and dw is the product of E
 // with s_t h_t, which is written transposed on the way.  Only a row whose lse_t turns
-// out too far from r_t for fp16's range is passed over once more.
+// out too far from r_t for fp16's range is passed over once more (x_t = lse_t).
+//
+// The target's exponential stays out of the sums: the first pass keeps the target's
+// logit and adds up the others, R = sum over v != target of exp(z_tv - x), so that a row
+// that is nearly sure of its target keeps the digits of what is left,
+//   loss_t = log(1 + R / exp(z_target - x)),  p_target - 1 = expm1(-loss_t)
+// Arguments of exponentials are near 0 where they count: powers of two that use fp16's
+// range are multiplied in afterwards.  (With those in the argument and the target among
+// the rest, losses were off by 4e-7, all of a loss of 1e-6.)
 //
 // What the products take ("form", chosen by the host from type and tokens):
 //   fp16, scaled     bf16 buffers, many tokens.  A power of two brings an
@@ -387,7 +395,8 @@ __device__ __forceinline__ float logit_unit(CeForm form, const CePlan& p, const 
     return ldexpf(kLog2e, max(-126, min(126, -(exponent_for(s->h_max) + exponent_for(s->w_max)))));
 }
 
-// Largest exponent and sum of exp2(z2 - largest) of two sets of logits.
+// What logits are taken relative to, at least the largest or a reference, and the sum
+// of exp2(z2 - that) over all but the targets, of two sets of logits.
 __device__ __forceinline__ float2 joined(float2 a, float2 c) {
     const float top = fmaxf(a.x, c.x);
     if (top == -__builtin_inff()) return make_float2(top, a.y + c.y);
@@ -459,32 +468,27 @@ __device__ __forceinline__ void load_g(const CePlan& p, const u16* row, int at, 
 // Which of the four columns of waves has column j of a tile.
 __device__ __forceinline__ int wave_of(int j) { return (j >> 5) & 3; }
 
-// Exponentials relative to a largest one are kept times this power of two: fp16's
-// upper range.
+// Exponentials relative to a largest one are kept times two to this: fp16's upper
+// range.
 template <CeForm FORM>
 constexpr int kKept = is_scaled(FORM) ? 14 : 0;
 
 // References: lse_t may pass r_t by 2^room and lie 2^kLow below it, so exp(z - r_t) is
-// kept times 2^(15 - room): of c_t, entries of G keep what is above 2^-34 (one half:
+// kept times 2^k, k = 15 - room: of c_t, entries of G keep what is above 2^-34 (one half:
 // rows whose sample misses a word of up to 15/16 of the sum stay in range) or 2^-36
 // (two halves; 3/4 of it).
 constexpr int kLow = 2;
 __host__ __device__ constexpr int room(CeForm f) { return f == kCeHalves ? 2 : 4; }
-__device__ __forceinline__ bool fits(CeForm f, float lse, float ref) {
-    return lse - ref <= room(f) && lse - ref >= -kLow;
-}
+__host__ __device__ constexpr int shift(CeForm f) { return 15 - room(f); }
+__host__ __device__ constexpr float pow2(int e) { return e < 0 ? 1.f / static_cast<float>(1 << -e) : static_cast<float>(1 << e); }
 // s_t is at most c_t 2^(kLow + room - 15), so s_t h_t is taken times this and the powers
 // of two that bring the largest c and h to 2^15: at most 2^15.
 constexpr int turned(CeForm f) { return -kLow - room(f); }
-// x_t of a row (all in units of log2).
-__device__ __forceinline__ float row_from(CeForm f, float lse, float ref) {
-    return fits(f, lse, ref) ? ref - (15 - room(f)) : lse - kKept<kCeHalf>;
-}
 
-// First pass: each row's largest logit and sum of exp(z - largest) in a tile, and
-// the target's logit.  KEEP also writes exp(z - largest) in G's place for the first
-// piece, the largest being that of a wave's columns of the tile (wave_of), or
-// relative to the row's reference, and what they are relative to.  Of the tile
+// First pass: each row's largest logit and sum of exp(z - largest) in a tile, without the
+// target's, and the target's logit.  KEEP also writes the exponentials in G's place for
+// the first piece, relative to the largest logit of a wave's columns of the tile
+// (wave_of), or to the row's reference, and what they are relative to.  Of the tile
 // columns from `skip` on tiles_v are taken, one of every `every`, into slots from `slot`;
 // `done` tiles were taken by launches before this one.
 //
@@ -557,13 +561,16 @@ __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b,
             for (int fj = 0; fj < T::FJ; ++fj)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    if (rel[fi] == t.col(fj) + r) hit[token] = t.acc[fi][fj][r];
+                    if (rel[fi] == t.col(fj) + r) {
+                        hit[token] = t.acc[fi][fj][r];
+                        t.acc[fi][fj][r] = -__builtin_inff();
+                    }
         }
         top[fi] *= unit;
         // All logits -inf: no exponential counts (and -inf - -inf is none).
         const bool none = top[fi] == -__builtin_inff();
-        float from = (none ? 0.f : top[fi]) - (KEEP ? kKept<FORM> : 0);
-        if (KEEP && top[fi] - ref[fi] <= room(FORM)) from = ref[fi] - (15 - room(FORM));
+        const bool near = KEEP && is_scaled(FORM) && top[fi] - ref[fi] <= room(FORM);
+        const float from = near ? ref[fi] : none ? 0.f : top[fi], by = near ? pow2(shift(FORM)) : pow2(kKept<FORM>);
         top[fi] = none ? top[fi] : from;
         kept[fi] = from;
         sum[fi] = 0.f;
@@ -576,6 +583,10 @@ __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b,
                 for (int r = 0; r < 8; ++r) {
                     e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(z.v[r], unit, -from));
                     sum[fi] += e[r];
+                }
+                if constexpr (is_scaled(FORM)) {
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) e[r] *= by;
                 }
                 if (token < p.tokens)
                     store_g<FORM>(p, g + (t.row(fi) - t.row(0)) * p.ld_p, tv * TN + t.col8(q), e);
@@ -613,6 +624,7 @@ __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b,
 }
 
 // The rows' references, from the sampled tiles: 16 tokens a work-group, 16 lanes each.
+// A target in the sample counts once, the other words for those that are not in it.
 __global__ __launch_bounds__(256) void k_refs(CePlan p, CeBuffers b) {
     __shared__ float2 part[16][16];
     const int lane = threadIdx.x & 15, share = threadIdx.x >> 4;
@@ -627,7 +639,12 @@ __global__ __launch_bounds__(256) void k_refs(CePlan p, CeBuffers b) {
 #pragma unroll
     for (int q = 1; q < 16; ++q) a = joined(a, part[q][lane]);
     const float all = static_cast<float>(p.vocab) / (p.sample * 256.f);
-    const float ref = a.x + __builtin_amdgcn_logf(a.y * all);
+    const int64_t target = b.target[token], column = target / 256;
+    float own = 0.f;
+    if (is_valid(target, p.vocab) && column % p.every == 0 && column / p.every < p.sample)
+        own = __builtin_amdgcn_exp2f(
+            __builtin_fmaf(reinterpret_cast<const float*>(b.workspace + p.hit)[token], logit_unit(p.form, p, b), -a.x));
+    const float ref = a.x + __builtin_amdgcn_logf(a.y * all + own);
     reinterpret_cast<float*>(b.workspace + p.refs)[token] = fabsf(ref) < __builtin_inff() ? ref : -__builtin_inff();
 }
 
@@ -673,18 +690,17 @@ __global__ __launch_bounds__(256) void k_settle(CePlan p, CeBuffers b, int group
     u16* g = reinterpret_cast<u16*>(b.workspace + p.p) + token * p.ld_p;
     const int square = square_of(p.tile);
     const float* tops = reinterpret_cast<const float*>(b.workspace + p.tops) + static_cast<int64_t>(token) * (p.piece / square * 4);
-    // G is exp(z - x) mul, the target's entry p - 1 = expm1(-loss) of it.
-    float x = lse, mul;
+    // G is exp(z - lse) mul, the target's entry p - 1 = expm1(-loss) of it.
+    float mul, ref = -__builtin_inff();
     if (is_scaled(FORM) && p.sample > 0) {
-        const float ref = reinterpret_cast<const float*>(b.workspace + p.refs)[token];
-        x = row_from(FORM, lse, ref);
-        mul = valid ? 1.f : 0.f;
-        if (fits(FORM, lse, ref)) {
+        ref = reinterpret_cast<const float*>(b.workspace + p.refs)[token];
+        mul = pow2(shift(FORM));
+        if (reinterpret_cast<const float2*>(b.workspace + p.rows)[token].x == ref) {
             if (threadIdx.x != 0 || !valid || target >= p.piece) return;
             const int at = static_cast<int>(target) & ~7;
             float v[8];
             load_g<FORM>(p, g, at, v);
-            const float e = __builtin_amdgcn_exp2f(lse - x) * expm1f(-b.loss[token]);
+            const float e = mul * __builtin_amdgcn_exp2f(lse - ref) * expm1f(-b.loss[token]);
 #pragma unroll
             for (int r = 0; r < 8; ++r)
                 if (target == at + r) v[r] = e;
@@ -693,16 +709,17 @@ __global__ __launch_bounds__(256) void k_settle(CePlan p, CeBuffers b, int group
         }
     } else {
         const int eg = !is_scaled(FORM) ? 0 : exponent_for(reinterpret_cast<const Scalars*>(b.workspace + p.scalars)->c_max);
-        mul = valid ? ldexpf(reinterpret_cast<const float*>(b.workspace + p.coef)[token], eg) : 0.f;
+        mul = ldexpf(reinterpret_cast<const float*>(b.workspace + p.coef)[token], eg);
     }
     for (int at = (first * 256 + threadIdx.x) * 8; at < p.piece; at += groups_of_row * 2048) {
         float v[8];
         load_g<FORM>(p, g, at, v);
-        const float by = valid ? mul * __builtin_amdgcn_exp2f(tops[at / square * 4 + wave_of(at)] - x) : 0.f;
+        const float from = tops[at / square * 4 + wave_of(at)];
+        const float by = mul * (from == ref ? pow2(-shift(FORM)) : pow2(-kKept<FORM>)) * __builtin_amdgcn_exp2f(from - lse);
 #pragma unroll
         for (int r = 0; r < 8; ++r) v[r] = valid ? v[r] * by : 0.f;
         if (valid && target >= at && target < at + 8) {
-            const float e = mul * __builtin_amdgcn_exp2f(lse - x) * expm1f(-b.loss[token]);
+            const float e = mul * expm1f(-b.loss[token]);
 #pragma unroll
             for (int r = 0; r < 8; ++r)
                 if (target == at + r) v[r] = e;
@@ -779,24 +796,28 @@ __global__ __launch_bounds__(1024) void k_join(CePlan p, CeBuffers b, int tiles)
     }
     if (share != 0) return;
     a = part[0][lane];
-    const float rest = log2f(a.y), lse2 = a.x + rest;
     const bool valid = token < p.tokens && is_valid(b.target[at], p.vocab);
-    // Of two logits of 30 and a loss of 0.01 the difference is what counts: the largest
-    // logit minus the target's in one rounding, not lse's rounding minus another.
+    // The target's logit over what the sum is relative to, in one rounding.  (-inf over
+    // -inf is NaN: a row without a logit has no loss, and its sum is 0.)
     const float hit = reinterpret_cast<const float*>(b.workspace + p.hit)[at];
-    float above = __builtin_fmaf(-hit, logit_unit(p.form, p, b), a.x);
-    if (!(fabsf(a.x) < __builtin_inff())) above = a.x - hit;
-    const float loss = valid ? (above + rest) * kLn2 : 0.f;
+    float over = __builtin_fmaf(hit, logit_unit(p.form, p, b), -a.x);
+    if (!(fabsf(a.x) < __builtin_inff())) over = hit - a.x;
+    const float own = valid && a.x != -__builtin_inff() ? exp2f(over) : 0.f;
+    const float sum2 = log2f(a.y + own), lse2 = a.x + sum2, odds = a.y * exp2f(-over);
+    const float loss = !valid ? 0.f : odds < 1.f ? log1pf(odds) : (sum2 - over) * kLn2;
     if (token < p.tokens) {
         reinterpret_cast<float*>(b.workspace + p.lse)[token] = lse2;
         if (b.lse) b.lse[token] = valid ? lse2 * kLn2 : 0.f;
         b.loss[token] = loss;
         if (p.sample > 0) {
+            // In range of its reference, and every wave kept exponentials relative to it
+            // (a larger logit elsewhere would be what the joined sum is relative to).
             const float ref = reinterpret_cast<const float*>(b.workspace + p.refs)[token];
-            const float below = fits(p.form, lse2, ref) ? ref - lse2 - (15 - room(p.form)) : -static_cast<float>(kKept<kCeHalf>);
-            reinterpret_cast<float2*>(b.workspace + p.rows)[token] =
-                make_float2(row_from(p.form, lse2, ref),
-                            reinterpret_cast<const float*>(b.workspace + p.coef)[token] * __builtin_amdgcn_exp2f(below));
+            const bool fits = a.x == ref && lse2 - ref <= room(p.form) && lse2 - ref >= -kLow;
+            const float below = fits ? ref - lse2 : 0.f;
+            reinterpret_cast<float2*>(b.workspace + p.rows)[token] = make_float2(
+                fits ? ref : lse2, reinterpret_cast<const float*>(b.workspace + p.coef)[token] *
+                                       __builtin_amdgcn_exp2f(below) * pow2(-shift(p.form)));
         }
     }
     if (gridDim.x > 1) return;
@@ -831,7 +852,7 @@ __global__ __launch_bounds__(threads_of(TM)) void k_piece(CePlan p, CeBuffers b,
     const float2* rows = reinterpret_cast<const float2*>(b.workspace + p.rows);
     int rel[T::FI];
     bool counts[T::FI];
-    float l[T::FI], c[T::FI], less[T::FI];  // less: the target's entry, p - 1
+    float l[T::FI], c[T::FI], less[T::FI];  // less: the target's entry, p - 1, before c
 #pragma unroll
     for (int fi = 0; fi < T::FI; ++fi) {
         const int token = tt * TM + t.row(fi), at = min(token, p.tokens - 1);
@@ -841,7 +862,7 @@ __global__ __launch_bounds__(threads_of(TM)) void k_piece(CePlan p, CeBuffers b,
         const float x = refs ? rows[at].x : lse[at];
         counts[fi] = valid;
         l[fi] = x;
-        c[fi] = refs ? 1.f : ldexpf(coef[at], eg);
+        c[fi] = refs ? pow2(shift(FORM)) : ldexpf(coef[at], eg);
         less[fi] = (refs ? __builtin_amdgcn_exp2f(lse[at] - x) : 1.f) * expm1f(-b.loss[at]);
     }
     const bool ragged = tv * TN + TN > cols;

@@ -114,3 +114,38 @@ def test_non_finite_words_of_a_later_piece(size, dtype):
     t[::2] = 11
     out = plan(h, w, t)
     assert (out["dh"][1::2] == 0).all() and torch.isnan(out["dh"][::2]).all()
+
+
+@DTYPES
+@SIZES
+def test_rows_nearly_sure_of_their_target(size, dtype):
+    """Losses from 1e-6 to 1e-2 keep their digits, and so do the gradients of such
+    rows: what bounds both is the logits' own rounding."""
+    tokens, dim, vocab = size
+    w = torch.nn.functional.normalize(_normal(vocab, dim, seed=3), dim=1).to(dtype)
+    # A third of the targets among the first words, which stand for frequent ones.
+    t = torch.randint(0, vocab, (tokens,), device="cuda", generator=torch.Generator(device="cuda").manual_seed(4))
+    t[::3] %= 200
+    # exp(others - target) sums to about vocab exp(a^2 / 2 dim - a).
+    want = 10.0 ** torch.linspace(-6, -2, tokens, device="cuda")
+    a = torch.full_like(want, 20.0)
+    for _ in range(30):
+        a = math.log(vocab) - want.log() + a * a / (2 * dim)
+        a.clamp_(max=45.0)
+    h = (a[:, None] * w[t].float()).to(dtype)
+    e = N.linear_ce(h, w, t, mean=False)
+    # Two logits of up to z (that of the target and those of the others that count), each a
+    # sum of dim terms and of operands of 22 bits; three more roundings of z; log1p and exp.
+    z = float(a.max())
+    tol = 2 * z * (2.0 ** -24 * dim ** 0.5 + 2.0 ** -22) + 4 * z * 2.0 ** -24 + 2.0 ** -20
+    for grads in (True, False):
+        out = _ops().LinearCE(*size, dtype=dtype, grads=grads)(h, w, t, mean=False)
+        rel = (out["loss"].double() - e["loss"]).abs() / e["loss"]
+        assert (rel <= tol).all(), f"{float(rel.max()):.3g} beyond {tol:.3g}"
+        if grads:
+            # G's entries by the same; dh's rounding; and what G's 16-bit storage leaves out,
+            # 2^-34 an entry, in random directions of w's unit rows.
+            norm = e["dh"].norm(dim=1)
+            dh = (out["dh"].double() - e["dh"]).norm(dim=1) / norm
+            far = dh - (tol + N.GRAD[dtype] + 2.0 ** -34 * vocab ** 0.5 / norm)
+            assert (far <= 0).all(), f"{int((far > 0).sum())} rows, by {float(far.max()):.3g}"
