@@ -205,6 +205,11 @@ __device__ __forceinline__ int lift_of(double norm, double eps) {
     const double share = norm / (norm + eps);
     return share > 0.0 && share < 0.5 ? -ilogb(share) - 1 : 0;
 }
+// 2^e / (norm + eps); zeros stay zeros where eps is 0 too.
+__device__ __forceinline__ double inverse_of(double norm, double eps, int e) {
+    const double size = norm + eps;
+    return size == 0.0 ? 0.0 : ldexp(1.0 / size, e);
+}
 __host__ __device__ inline int64_t lift_at() { return kNormParts * 8; }  // bytes into a matrix's workspace
 
 // X_0 in the stored form, wide, its padding zero: 64 x 64 of it per work-group, turned
@@ -239,7 +244,7 @@ __global__ __launch_bounds__(256) void k_start(OrthoGroup g, Parts parts, int n_
     const double norm = sqrt(s[0]);
     const int lift = lift_of(norm, g.eps);
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *reinterpret_cast<int*>(ws + lift_at()) = lift;
-    const double inv = ldexp(1.0 / (norm + static_cast<double>(g.eps)), x_exp + lift);
+    const double inv = inverse_of(norm, g.eps, x_exp + lift);
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
@@ -613,7 +618,7 @@ __global__ __launch_bounds__(kSmallWaves * 64) void k_small(OrthoGroup g, SmallS
     for (int w = 0; w < kSmallWaves; ++w) sum += sums[w];
     const double norm = sqrt(sum);
     int lift = __builtin_amdgcn_readfirstlane(lift_of(norm, g.eps));
-    const double inv = ldexp(1.0 / (norm + static_cast<double>(g.eps)), x_exp + lift);
+    const double inv = inverse_of(norm, g.eps, x_exp + lift);
     for (int q = threadIdx.x; q < rows * quads; q += kSmallWaves * 64) {
         const int r = q / quads, c = (q - r * quads) * 4;
         const f4 v = update_at<STEP, BF16, false>(g, base + r * g.row_stride + c, cols - c);

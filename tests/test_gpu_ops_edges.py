@@ -149,3 +149,20 @@ def test_rows_nearly_sure_of_their_target(size, dtype):
             dh = (out["dh"].double() - e["dh"]).norm(dim=1) / norm
             far = dh - (tol + N.GRAD[dtype] + 2.0 ** -34 * vocab ** 0.5 / norm)
             assert (far <= 0).all(), f"{int((far > 0).sum())} rows, by {float(far.max()):.3g}"
+
+
+@DTYPES
+@pytest.mark.parametrize("shape", [(3, 48, 64), (3, 200, 130), (3, 130, 200)], ids=str)
+def test_zeros_without_eps(shape, dtype):
+    u = (1e-3 * _normal(*shape, seed=11)).to(dtype)
+    u[1] = 0
+    plan = _ops().Ortho(*shape[1:], shape[0], dtype=dtype, eps=0.0)
+    out = plan.orthogonalize(u)
+    assert (out[1] == 0).all()
+    want = O.orthogonalize(u[::2], eps=0.0)
+    assert N.off(out[::2], want) <= (1e-5 if dtype == F32 else 4e-3)
+    if dtype == F32:
+        x = _normal(*shape, seed=12)
+        x0 = x.clone()
+        plan.step(x, None, u, lr=0.1, mu=0.0, wd=0.0)
+        assert torch.equal(x[1], x0[1]) and torch.isfinite(x).all()
