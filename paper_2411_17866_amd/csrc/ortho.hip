@@ -16,11 +16,11 @@
 // iteration multiplies small singular values by up to 3.4445^5 = 485, and with
 // them what rounding X, A or B to 8 bits put there).  Two rules keep 11 bits
 // enough: A is rounded once and that same A enters b A and c A A, and the term
-// a X takes X from 14 bits (hi and a byte of lo), the products hi alone.  Against 64 bits
-// this gives 0.02-0.2% (a strong low rank over noise, and noise alone), where
-// rounding the result to bf16 costs 0.17%; all of it in bf16, 1-5%.  The fewer the
-// singular values, the less their errors average: matrices small enough for LDS take
-// two halves (bf16 64 x 48: 0.28% so, with one half; 0.17% with two).
+// a X takes X from 22 bits (hi + lo), the products hi alone.  (With 14 bits there a
+// rank of 5 over noise of 1e-4 is off by 0.3-0.7%; rounding the result to bf16 costs
+// 0.17%, all of it in bf16 1-5%.)  The fewer the singular values, the less their errors
+// average: matrices small enough for LDS take two halves (bf16 64 x 48: 0.28% so, with
+// one half; 0.17% with two).
 //
 // Range.  ||X||_2 <= 1 at the start, and the polynomial bounds it after each
 // step, so the host picks for each stored operand the power of two that brings
@@ -61,11 +61,11 @@ __host__ __device__ inline int64_t up256(int64_t v) { return (v + 255) / 256 * 2
 // one half, X's lo lies apart, where only the epilogue reads it.
 struct Parts {
     int64_t x[2], a, b, bytes;
-    int64_t lo;  // from an X to its lo bytes (one half only)
+    int64_t lo;  // from an X to its lo half (one half only)
     __host__ __device__ Parts(int m, int n, bool split) {
-        lo = up256(static_cast<int64_t>(m) * pad(n) * 2);
-        const int64_t xb = split ? lo * 2 : lo + up256(static_cast<int64_t>(m) * pad(n));
+        const int64_t xb = up256(static_cast<int64_t>(m) * pad(n) * 2) * 2;
         const int64_t ab = up256(static_cast<int64_t>(m) * pad(m) * 2 * (split ? 2 : 1));
+        lo = xb / 2;
         x[0] = up256(kNormParts * 8 + 4);
         x[1] = x[0] + xb;
         a = x[1] + xb;
@@ -85,22 +85,6 @@ __device__ __forceinline__ float bf16_to_float(u16 v) {
 }
 __device__ __forceinline__ u16 float_to_bf16(float v) {
     return __builtin_bit_cast(u16, static_cast<__bf16>(v));
-}
-
-// The upper bytes of halves, to nearest, and halves of them: what X keeps below its
-// upper half where only a X takes it (3 bits of it, 14 with those above; NaN stays
-// NaN).  An update then moves 6 bytes an element for 8: eight 6400 x 1600 in 2.71 ms
-// for 2.80.
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ uint32_t bytes_of(u16x4 v) {
-    const u32x2 w = __builtin_bit_cast(u32x2, static_cast<u16x4>(v + static_cast<u16>(0x80)));
-    return __builtin_amdgcn_perm(w.y, w.x, 0x07050301);
-}
-__device__ __forceinline__ u16x8 halves_of(u32x2 b) {
-    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-    const u32x4 w = {__builtin_amdgcn_perm(b.x, 0, 0x050c040c), __builtin_amdgcn_perm(b.x, 0, 0x070c060c),
-                     __builtin_amdgcn_perm(b.y, 0, 0x050c040c), __builtin_amdgcn_perm(b.y, 0, 0x070c060c)};
-    return __builtin_bit_cast(u16x8, w);
 }
 
 // Where element (i, j) of a stored operand lies; the lo half is 32 further.
@@ -273,10 +257,7 @@ __global__ __launch_bounds__(256) void k_start(OrthoGroup g, Parts parts, int n_
         }
         u16* to = x + at<S>(i, j, static_cast<int64_t>(np) * S);
         *reinterpret_cast<u16x4*>(to) = hi;
-        if constexpr (S == 2)
-            *reinterpret_cast<u16x4*>(to + 32) = lo;
-        else
-            *reinterpret_cast<uint32_t*>(ws + parts.x[0] + parts.lo + at<S>(i, j, np)) = bytes_of(lo);
+        *reinterpret_cast<u16x4*>(to + (S == 2 ? 32 : parts.lo / 2)) = lo;
     }
 }
 
@@ -379,14 +360,14 @@ __global__ __launch_bounds__(tile::threads_of(BM)) void k_product(OrthoGroup g, 
     // them is loaded before the batch's first store, which the compiler must
     // assume to overlap it: one wait a batch, not one a fragment.
     constexpr int kBatch = T::FI < 4 ? T::FI : 4, kPairs = T::FJ / 2;
+    const int64_t lo_at = S == 2 ? 32 : parts.lo / 2;  // of an X
     const u16* old = P == kPoly ? A : X;
-    const int64_t ld_old = P == kPoly ? lda : ldx;
+    const int64_t ld_old = P == kPoly ? lda : ldx, old_lo = P == kPoly ? 32 : lo_at;
     const int last_col = (P == kPoly ? mp : np) - 8;
 #pragma unroll
     for (int f0 = 0; f0 < T::FI; f0 += kBatch) {
         if (!kSymmetric && t.idle(f0)) break;
-        u16x8 oh[kBatch][kPairs];
-        std::conditional_t<S == 2, u16x8, u32x2> ol[kBatch][kPairs];
+        u16x8 oh[kBatch][kPairs], ol[kBatch][kPairs];
         if constexpr (P != kGram) {
 #pragma unroll
             for (int fi = 0; fi < kBatch; ++fi)
@@ -395,10 +376,8 @@ __global__ __launch_bounds__(tile::threads_of(BM)) void k_product(OrthoGroup g, 
                     const int64_t q = at<S>(min(ti * BM + t.row(f0 + fi), m - 1),
                                             min(tj * BM + t.col8(p), last_col), ld_old);
                     oh[fi][p] = *reinterpret_cast<const u16x8*>(old + q);
-                    if constexpr (S == 2)
-                        ol[fi][p] = *reinterpret_cast<const u16x8*>(old + q + 32);
-                    else if constexpr (P != kPoly)
-                        ol[fi][p] = *reinterpret_cast<const u32x2*>(ws + parts.x[from] + parts.lo + q);
+                    if constexpr (P != kPoly || S == 2)
+                        ol[fi][p] = *reinterpret_cast<const u16x8*>(old + q + old_lo);
                 }
         }
 #pragma unroll
@@ -415,17 +394,12 @@ __global__ __launch_bounds__(tile::threads_of(BM)) void k_product(OrthoGroup g, 
             for (int p = 0; p < kPairs; ++p) {
                 const int j = tj * BM + t.col8(p);
                 Eight v = t.eight(f0 + fi, p);
-                u16x8 below;
-                if constexpr (S == 2)
-                    below = ol[fi][p];
-                else if constexpr (P == kUpdate || P == kLast)
-                    below = halves_of(ol[fi][p]);
 #pragma unroll
                 for (int r = 0; r < 8; ++r) {
                     v.v[r] *= mul;
                     if constexpr (P != kGram) {
                         float o = from_bits(oh[fi][p][r]);
-                        if constexpr (P != kPoly || S == 2) o += from_bits(below[r]);
+                        if constexpr (P != kPoly || S == 2) o += from_bits(ol[fi][p][r]);
                         v.v[r] = __builtin_fmaf(add, o, v.v[r]);
                     }
                 }
@@ -446,12 +420,7 @@ __global__ __launch_bounds__(tile::threads_of(BM)) void k_product(OrthoGroup g, 
                     if (i >= m || j >= np) continue;
                     u16* out = Y + at<S>(i, j, ldx);
                     *reinterpret_cast<u16x8*>(out) = upper(v);
-                    const u16x8 l = lower(v);
-                    if constexpr (S == 2)
-                        *reinterpret_cast<u16x8*>(out + 32) = l;
-                    else
-                        *reinterpret_cast<u32x2*>(ws + parts.x[from ^ 1] + parts.lo + at<S>(i, j, ldx)) =
-                            u32x2{bytes_of(l.lo), bytes_of(l.hi)};
+                    *reinterpret_cast<u16x8*>(out + lo_at) = lower(v);
                 } else {
                     if (i >= m || j >= n) continue;
                     const int64_t e = g.off.at[which] + (g.tall ? j * g.row_stride + i : i * g.row_stride + j);

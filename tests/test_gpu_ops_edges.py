@@ -166,3 +166,17 @@ def test_zeros_without_eps(shape, dtype):
         x0 = x.clone()
         plan.step(x, None, u, lr=0.1, mu=0.0, wd=0.0)
         assert torch.equal(x[1], x0[1]) and torch.isfinite(x).all()
+
+
+@pytest.mark.parametrize("shape", [(2, 200, 200), (2, 130, 70), (1, 400, 1600), (3, 900, 385), (12, 768, 768)], ids=str)
+@pytest.mark.parametrize("noise", [1e-2, 1e-4])
+def test_bf16_matrices_of_low_rank_cost_little_more_than_their_rounding(shape, noise):
+    """Against 64 bits a bf16 result cannot be nearer than its rounding; what the
+    iteration's own operands add has to stay below three quarters of that, which makes
+    1.25 of it together.  Small singular values under a few large ones are multiplied by
+    up to 485, and with them what storage puts there."""
+    u = _normal(*shape[:2], 5, seed=13) @ _normal(shape[0], 5, shape[2], seed=14) + noise * _normal(*shape, seed=15)
+    u = u.to(BF16)
+    want = O.orthogonalize(u)
+    out = _ops().Ortho(*shape[1:], shape[0], dtype=BF16).orthogonalize(u)
+    assert N.off(out, want) <= 1.25 * N.off(want.to(BF16), want)
