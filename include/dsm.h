@@ -475,7 +475,8 @@ DSM_API dsm_status dsm_ortho_workspace(const dsm_ortho_problem* problem, int64_t
  * with the customary coefficients the singular values of U are brought near 1.
  * A matrix of zeros gives zeros; one with a NaN or infinite entry gives NaN.
  * fp32 matrices are iterated with 22-bit operands, bf16 ones with 11-bit
- * operands; sums are fp32, norms fp64.
+ * operands whose products' diagonals stay in fp32 (results within about 1.1
+ * times the rounding to bf16); sums are fp32, norms fp64.
  * Errors: DSM_ERR_INVALID_ARG; DSM_ERR_UNSUPPORTED (as dsm_ortho_workspace);
  * DSM_ERR_HIP.
  */

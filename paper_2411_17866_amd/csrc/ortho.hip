@@ -18,9 +18,19 @@
 // enough: A is rounded once and that same A enters b A and c A A, and the term
 // a X takes X from 22 bits (hi + lo), the products hi alone.  (With 14 bits there a
 // rank of 5 over noise of 1e-4 is off by 0.3-0.7%; rounding the result to bf16 costs
-// 0.17%, all of it in bf16 1-5%.)  The fewer the singular values, the less their errors
-// average: matrices small enough for LDS take two halves (bf16 64 x 48: 0.28% so, with
-// one half; 0.17% with two).
+// 0.17%, all of it in bf16 1-5%.)
+//   Near the end all singular values are near 1, so A is near I and B near -2.5 I: their
+// diagonals are most of what is rounded, and a X + B X nearly cancels.  So the diagonals
+// D of A and E of B stay apart, in fp32, and with A' = A - D, B' = B - E
+//   A A = A' A' + D A' + A' D + D D,   a X + B X = (a + E) X + B' X
+// where the epilogues add what is not a product of matrices.  E X is part of a product
+// that takes hi alone, and in an early iteration it has to take hi too: B X is 0 where X
+// is small, and E X and B' X cancel there, with X's rounding on both sides or on neither.
+// When what is left multiplies small singular values little (late), (a + E) X takes hi
+// and lo.  Against 64 bits results are then off by 1.01-1.12 times what rounding them
+// to bf16 costs; by 1.2-1.6 times with the diagonals inside (noise, orthogonal rows).
+//   The fewer the singular values, the less their errors average: matrices small enough
+// for LDS take two halves (bf16 64 x 48: 0.28% so, with one half; 0.17% with two).
 //
 // Range.  ||X||_2 <= 1 at the start, and the polynomial bounds it after each
 // step, so the host picks for each stored operand the power of two that brings
@@ -29,6 +39,8 @@
 // then stored times 2^e, e its own for each matrix, with which b A and c A A lose
 // 2^-2e and 2^-4e, and e falls with each iteration by what X can grow.
 #include <hip/hip_runtime.h>
+
+#include <cmath>
 
 #include "gemm_tile.h"
 #include "ops_internal.h"
@@ -61,7 +73,8 @@ __host__ __device__ inline int64_t up256(int64_t v) { return (v + 255) / 256 * 2
 // one half, X's lo lies apart, where only the epilogue reads it.
 struct Parts {
     int64_t x[2], a, b, bytes;
-    int64_t lo;  // from an X to its lo half (one half only)
+    int64_t lo;           // from an X to its lo half (one half only)
+    int64_t diag_a, diag_b;  // diagonals of A and B in fp32 (one half only)
     __host__ __device__ Parts(int m, int n, bool split) {
         const int64_t xb = up256(static_cast<int64_t>(m) * pad(n) * 2) * 2;
         const int64_t ab = up256(static_cast<int64_t>(m) * pad(m) * 2 * (split ? 2 : 1));
@@ -70,7 +83,10 @@ struct Parts {
         x[1] = x[0] + xb;
         a = x[1] + xb;
         b = a + ab;
-        bytes = b + ab;
+        diag_a = b + ab;
+        const int64_t db = split ? 0 : up256(static_cast<int64_t>(pad(m)) * 4);
+        diag_b = diag_a + db;
+        bytes = diag_b + db;
     }
 };
 
@@ -317,7 +333,7 @@ __device__ __forceinline__ u16x8 lower(const Eight& e) {
 // of one turn or two, a launch's start and end for the most part.
 template <int S, int BM, Product P>
 __global__ __launch_bounds__(tile::threads_of(BM)) void k_product(OrthoGroup g, Parts parts, int from, float mul,
-                                                                    float add, int fallen, int next) {
+                                                                    float add, int fallen, int next, int late) {
     using T = tile::Pick<S == 1 ? tile::kF16 : tile::kSplit, BM, kContig, P == kGram || P == kPoly ? kContig : kStrided>;
     constexpr bool kSymmetric = P == kGram || P == kPoly;
     __shared__ __align__(1024) char lds[T::kLdsBytes];
@@ -364,10 +380,33 @@ __global__ __launch_bounds__(tile::threads_of(BM)) void k_product(OrthoGroup g, 
     const u16* old = P == kPoly ? A : X;
     const int64_t ld_old = P == kPoly ? lda : ldx, old_lo = P == kPoly ? 32 : lo_at;
     const int last_col = (P == kPoly ? mp : np) - 8;
+    // One half: A and B are stored without their diagonals.
+    constexpr bool kApart = S == 1;
+    float* diag_a = reinterpret_cast<float*>(ws + parts.diag_a);
+    float* diag_b = reinterpret_cast<float*>(ws + parts.diag_b);
+    Eight dj[kPairs];
+    if constexpr (kApart && P == kPoly) {
+#pragma unroll
+        for (int p = 0; p < kPairs; ++p) {
+            const float* d = diag_a + min(tj * BM + t.col8(p), last_col);
+            const f4 lo = *reinterpret_cast<const f4*>(d), hi = *reinterpret_cast<const f4*>(d + 4);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                dj[p].v[r] = lo[r];
+                dj[p].v[4 + r] = hi[r];
+            }
+        }
+    }
 #pragma unroll
     for (int f0 = 0; f0 < T::FI; f0 += kBatch) {
         if (!kSymmetric && t.idle(f0)) break;
         u16x8 oh[kBatch][kPairs], ol[kBatch][kPairs];
+        float di[kBatch];
+        if constexpr (kApart && P != kGram) {
+#pragma unroll
+            for (int fi = 0; fi < kBatch; ++fi)
+                di[fi] = (P == kPoly ? diag_a : diag_b)[min(ti * BM + t.row(f0 + fi), m - 1)];
+        }
         if constexpr (P != kGram) {
 #pragma unroll
             for (int fi = 0; fi < kBatch; ++fi)
@@ -383,6 +422,8 @@ __global__ __launch_bounds__(tile::threads_of(BM)) void k_product(OrthoGroup g, 
 #pragma unroll
         for (int fi = 0; fi < kBatch; ++fi) {
             const int i = ti * BM + t.row(f0 + fi);
+            // a X, with one half (a + E) X.
+            const float add_hi = kApart && !kSymmetric ? __builtin_fmaf(mul, di[fi], add) : add, add_lo = late ? add_hi : add;
             Eight px[kPairs];
             if constexpr (P == kLast && S == 2) {
                 if (g.x) {
@@ -397,10 +438,28 @@ __global__ __launch_bounds__(tile::threads_of(BM)) void k_product(OrthoGroup g, 
 #pragma unroll
                 for (int r = 0; r < 8; ++r) {
                     v.v[r] *= mul;
-                    if constexpr (P != kGram) {
-                        float o = from_bits(oh[fi][p][r]);
-                        if constexpr (P != kPoly || S == 2) o += from_bits(ol[fi][p][r]);
-                        v.v[r] = __builtin_fmaf(add, o, v.v[r]);
+                    if constexpr (P == kGram) {
+                        continue;
+                    } else if constexpr (S == 2) {
+                        v.v[r] = __builtin_fmaf(add, from_bits(oh[fi][p][r]) + from_bits(ol[fi][p][r]), v.v[r]);
+                    } else if constexpr (P == kPoly) {
+                        v.v[r] = __builtin_fmaf(__builtin_fmaf(mul, di[fi] + dj[p].v[r], add), from_bits(oh[fi][p][r]), v.v[r]);
+                    } else {
+                        v.v[r] = __builtin_fmaf(add_lo, from_bits(ol[fi][p][r]), v.v[r]);
+                        v.v[r] = __builtin_fmaf(add_hi, from_bits(oh[fi][p][r]), v.v[r]);
+                    }
+                }
+                if constexpr (kApart && kSymmetric) {
+                    if (ti == tj && i >= j && i < j + 8 && i < m) {
+                        float d = 0.f;
+#pragma unroll
+                        for (int r = 0; r < 8; ++r)
+                            if (i == j + r) {
+                                d = v.v[r];
+                                v.v[r] = 0.f;
+                            }
+                        if constexpr (P == kPoly) d = __builtin_fmaf(__builtin_fmaf(mul, di[fi], add), di[fi], d);
+                        (P == kGram ? diag_a : diag_b)[i] = d;
                     }
                 }
                 if constexpr (kSymmetric) {
@@ -703,17 +762,20 @@ float pow2(int e) { return __builtin_ldexpf(1.0f, e); }
 
 template <int S, Product P>
 void product(const OrthoGroup& g, const Parts& parts, int from, float mul, float add, int fallen, int next,
-             hipStream_t stream) {
+             bool late, hipStream_t stream) {
     constexpr bool kSymmetric = P == kGram || P == kPoly;
     const int bm = ortho_tile(g.count, g.m, g.n, kSymmetric);
     const unsigned groups = ortho_groups(g.count, g.m, g.n, bm, kSymmetric);
     if (bm == 64)
-        k_product<S, 64, P><<<groups, tile::threads_of(64), 0, stream>>>(g, parts, from, mul, add, fallen, next);
+        k_product<S, 64, P><<<groups, tile::threads_of(64), 0, stream>>>(g, parts, from, mul, add, fallen, next, late);
     else if (bm == 128)
-        k_product<S, 128, P><<<groups, tile::threads_of(128), 0, stream>>>(g, parts, from, mul, add, fallen, next);
+        k_product<S, 128, P><<<groups, tile::threads_of(128), 0, stream>>>(g, parts, from, mul, add, fallen, next, late);
     else
-        k_product<S, 256, P><<<groups, tile::threads_of(256), 0, stream>>>(g, parts, from, mul, add, fallen, next);
+        k_product<S, 256, P><<<groups, tile::threads_of(256), 0, stream>>>(g, parts, from, mul, add, fallen, next, late);
 }
+
+// From which growth on the iterations left are "late" (k_product).
+constexpr float kLate = 16.f;
 
 template <int S>
 void iterate(const OrthoGroup& g, const Parts& parts, const float* coeffs, const OrthoScales* scales,
@@ -722,13 +784,17 @@ void iterate(const OrthoGroup& g, const Parts& parts, const float* coeffs, const
     for (int s = 0; s < steps; ++s) {
         const OrthoScales sc = scales[s];
         const float a = coeffs[3 * s], b = coeffs[3 * s + 1], c = coeffs[3 * s + 2];
-        product<S, kGram>(g, parts, s & 1, pow2(sc.a - 2 * sc.x), 0.f, 0, 0, stream);
-        product<S, kPoly>(g, parts, s & 1, c * pow2(sc.b - 2 * sc.a), b * pow2(sc.b - sc.a), fallen, 0, stream);
+        // Small singular values grow by this much in the iterations that follow.
+        float growth = 1.f;
+        for (int k = s + 1; k < steps; ++k) growth *= std::fabs(coeffs[3 * k]);
+        const bool late = growth <= kLate;
+        product<S, kGram>(g, parts, s & 1, pow2(sc.a - 2 * sc.x), 0.f, 0, 0, late, stream);
+        product<S, kPoly>(g, parts, s & 1, c * pow2(sc.b - 2 * sc.a), b * pow2(sc.b - sc.a), fallen, 0, late, stream);
         const float mul = pow2(sc.x_next - sc.b - sc.x), add = a * pow2(sc.x_next - sc.x);
         if (s + 1 < steps)
-            product<S, kUpdate>(g, parts, s & 1, mul, add, fallen, sc.growth, stream);
+            product<S, kUpdate>(g, parts, s & 1, mul, add, fallen, sc.growth, late, stream);
         else
-            product<S, kLast>(g, parts, s & 1, mul, add, fallen, 0, stream);
+            product<S, kLast>(g, parts, s & 1, mul, add, fallen, 0, late, stream);
         fallen += sc.growth;
     }
 }

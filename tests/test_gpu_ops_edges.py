@@ -180,3 +180,18 @@ def test_bf16_matrices_of_low_rank_cost_little_more_than_their_rounding(shape, n
     want = O.orthogonalize(u)
     out = _ops().Ortho(*shape[1:], shape[0], dtype=BF16).orthogonalize(u)
     assert N.off(out, want) <= 1.25 * N.off(want.to(BF16), want)
+
+
+@pytest.mark.parametrize("shape", [(2, 200, 200), (2, 130, 70), (1, 400, 1600), (3, 900, 385), (12, 768, 768)], ids=str)
+@pytest.mark.parametrize("spectrum", ["noise", "orthogonal", "power"])
+def test_bf16_matrices_cost_little_more_than_their_rounding(shape, spectrum):
+    """The same where all singular values end near 1: there a X and B X nearly cancel."""
+    u = _normal(*shape, seed=16)
+    if spectrum != "noise":
+        left, _, right = torch.linalg.svd(u.double(), full_matrices=False)
+        s = torch.arange(1, left.shape[2] + 1, device="cuda").double() ** (-1.0 if spectrum == "power" else 0.0)
+        u = (left * s) @ right
+    u = u.to(BF16)
+    want = O.orthogonalize(u)
+    out = _ops().Ortho(*shape[1:], shape[0], dtype=BF16).orthogonalize(u)
+    assert N.off(out, want) <= 1.25 * N.off(want.to(BF16), want)
