@@ -4,10 +4,12 @@ with its gradients, and orthogonalised updates.
 PyTorch only allocates device memory and supplies the stream; the operators run
 in libdsm.so through the binding in ``dsm``.  An object here is the plan of one
 problem: it checks tensors, keeps the workspace, and enqueues on torch's current
-stream.  Calls of one object on different streams are put one after another,
-since they share the workspace (under graph capture that is the caller's part).
+stream.  Calls of one object share its workspace: on different streams they are put
+one after another (under graph capture that is the caller's part), and from several
+threads each call's launches are enqueued whole before the next call's.
 """
 import contextlib
+import threading
 
 import torch
 
@@ -23,6 +25,9 @@ def _dtype(dtype):
 
 
 class _Plan:
+    def __init__(self):
+        self._lock = threading.Lock()
+
     def _allocate(self, workspace_bytes, device):
         self.device = torch.device(device)
         if self.device.type != "cuda":
@@ -49,6 +54,12 @@ class _Plan:
             return contextlib.nullcontext()
         return torch.cuda.device(self.device)
 
+    @contextlib.contextmanager
+    def _enqueue(self):
+        """The stream for one call's launches, which no other call's come between."""
+        with self._lock, self._on_device():
+            yield self._enter()
+
     def _check(self, name, t, dtype, shape):
         if t.device != self.device:
             raise ValueError(f"{name} is on {t.device}, the plan on {self.device}")
@@ -67,6 +78,7 @@ class LinearCE(_Plan):
     """
 
     def __init__(self, tokens, dim, vocab, dtype=torch.float32, grads=True, device="cuda"):
+        super().__init__()
         self.problem = dsm.dsm_ce_problem(int(tokens), int(dim), int(vocab), _dtype(dtype),
                                           1 if grads else 0)
         self.dtype, self.grads = dtype, bool(grads)
@@ -127,8 +139,7 @@ class LinearCE(_Plan):
         elif dh is not None or dw is not None:
             raise ValueError("dh or dw given to a plan without gradients")
         buf.workspace, buf.workspace_bytes = self.workspace.data_ptr(), self.workspace_bytes
-        with self._on_device():
-            buf.stream = self._enter()
+        with self._enqueue() as buf.stream:
             dsm.dsm_linear_ce(self.problem, buf, mean)
         return out
 
@@ -147,6 +158,7 @@ class Ortho(_Plan):
 
     def __init__(self, rows, cols, count=1, dtype=torch.float32, steps=5, eps=1e-7, coeffs=None,
                  offsets=None, row_stride=None, device="cuda"):
+        super().__init__()
         self.rows, self.cols, self.count = int(rows), int(cols), int(count)
         self.dtype, self._given = dtype, offsets is not None
         self._args = dict(dtype=_dtype(dtype), steps=int(steps), eps=float(eps), coeffs=coeffs)
@@ -222,8 +234,7 @@ class Ortho(_Plan):
             out = torch.empty_strided(u.size(), u.stride(), dtype=u.dtype, device=u.device)
         problem = self._placed([("u", u), ("out", out)])
         buf = self._buffers(in_=u, out=out)
-        with self._on_device():
-            buf.stream = self._enter()
+        with self._enqueue() as buf.stream:
             dsm.dsm_orthogonalize(problem, buf)
         return out
 
@@ -232,8 +243,7 @@ class Ortho(_Plan):
         may be None for u = g."""
         problem = self._placed([(n, t) for n, t in (("x", x), ("m", m), ("g", g)) if t is not None])
         buf = self._buffers(in_=g, m=m, x=x)
-        with self._on_device():
-            buf.stream = self._enter()
+        with self._enqueue() as buf.stream:
             dsm.dsm_ortho_step(problem, buf, lr, mu, scale, wd, nesterov)
 
     def direction(self, m, g, out, mu, scale=1.0, nesterov=True):
@@ -242,7 +252,6 @@ class Ortho(_Plan):
         problem = self._placed([(n, t) for n, t in (("m", m), ("g", g), ("out", out))
                                 if t is not None])
         buf = self._buffers(in_=g, m=m, out=out)
-        with self._on_device():
-            buf.stream = self._enter()
+        with self._enqueue() as buf.stream:
             dsm.dsm_ortho_step(problem, buf, 1.0, mu, scale, 0.0, nesterov)
         return out

@@ -2,6 +2,7 @@
 ends of fp32, rows that are nearly sure of their target, launches past 2^32 threads,
 non-finite words, zeros without eps."""
 import math
+import threading
 
 import pytest
 
@@ -195,3 +196,40 @@ def test_bf16_matrices_cost_little_more_than_their_rounding(shape, spectrum):
     want = O.orthogonalize(u)
     out = _ops().Ortho(*shape[1:], shape[0], dtype=BF16).orthogonalize(u)
     assert N.off(out, want) <= 1.25 * N.off(want.to(BF16), want)
+
+
+@pytest.mark.parametrize("streams", [False, True], ids=["one stream", "a stream each"])
+def test_threads_share_a_plan(streams):
+    """Four threads, each with its own inputs: the bits that one thread alone gets."""
+    size = tokens, dim, vocab = 300, 128, 1500
+    ce, orth = _ops().LinearCE(*size, dtype=BF16), _ops().Ortho(130, 200, 2)
+
+    def inputs(k):
+        t = torch.randint(0, vocab, (tokens,), device="cuda", generator=torch.Generator(device="cuda").manual_seed(k))
+        return _normal(tokens, dim, seed=k).to(BF16), (0.1 * _normal(vocab, dim, seed=k + 9)).to(BF16), t
+
+    given = [inputs(k) for k in range(4)]
+    us = [_normal(2, 130, 200, seed=30 + k) for k in range(4)]
+    want = [{n: x.clone() for n, x in ce(*given[k]).items()} for k in range(4)]
+    want_o = [orth.orthogonalize(u).clone() for u in us]
+    torch.cuda.synchronize()
+    bad = []
+
+    def work(k):
+        try:
+            stream = torch.cuda.Stream() if streams else torch.cuda.current_stream()
+            with torch.cuda.stream(stream):
+                for _ in range(8):
+                    out, o = ce(*given[k]), orth.orthogonalize(us[k])
+                    stream.synchronize()
+                    if not all(torch.equal(out[n], want[k][n]) for n in out) or not torch.equal(o, want_o[k]):
+                        bad.append(k)
+        except Exception as e:  # noqa: BLE001
+            bad.append(e)
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad, bad
