@@ -447,7 +447,8 @@ typedef struct dsm_ortho_problem {
 typedef struct dsm_ortho_buffers {
     const void* in; /* the updates U (dsm_orthogonalize) or gradients g (dsm_ortho_step) */
     void* out;      /* results; may be `in` itself */
-    float* m;       /* dsm_ortho_step: momentum, updated; NULL for none (u = g) */
+    float* m;       /* dsm_ortho_step: momentum, updated, none of the others; NULL for
+                       none (u = g) */
     float* x;       /* dsm_ortho_step: parameters, updated; NULL to write out instead */
     void* workspace;
     int64_t workspace_bytes;
@@ -492,7 +493,7 @@ DSM_API dsm_status dsm_orthogonalize(const dsm_ortho_problem* problem,
  *             (lr and weight_decay are then not used)
  * The sums of m, u and x are fp32, one rounding per operation.
  * Errors: DSM_ERR_INVALID_ARG (dtype other than DSM_F32, both or neither of x
- * and out, hyperparameters); DSM_ERR_UNSUPPORTED (as dsm_ortho_workspace);
+ * and out, m one of the others, hyperparameters); DSM_ERR_UNSUPPORTED (as dsm_ortho_workspace);
  * DSM_ERR_HIP.
  */
 DSM_API dsm_status dsm_ortho_step(const dsm_ortho_problem* problem, const dsm_ortho_buffers* buffers,

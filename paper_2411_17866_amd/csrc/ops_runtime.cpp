@@ -441,6 +441,9 @@ dsm_status dsm_ortho_step(const dsm_ortho_problem* problem, const dsm_ortho_buff
         if (!std::isfinite(hp->weight_decay) || hp->weight_decay < 0)
             return invalid("weight_decay must be finite and >= 0");
     }
+    // The momentum is stored before the last read of `in`, and read after it.
+    if (buffers->m && (buffers->m == buffers->in || buffers->m == buffers->out || buffers->m == buffers->x))
+        return invalid("m is in, out or x");
     if (!aligned(buffers->in, 4) || !aligned(buffers->out, 4) || !aligned(buffers->m, 4) || !aligned(buffers->x, 4))
         return invalid("in, out, m or x is not aligned to its elements");
     return run_ortho(problem, buffers, hp, it);
