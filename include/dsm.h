@@ -413,12 +413,15 @@ DSM_API dsm_status dsm_ce_workspace(const dsm_ce_problem* problem, int64_t* work
  *           tokens (at least 1) when mean != 0
  * and, where the problem asks for gradients, those of total:
  *   G_tv = c_t (exp(z_tv - lse_t) - [v = y]);  dh = G w;  dw = G^T h
- * dh is 0 for the tokens left out; dh and dw are written, not added to.  The
- * logits are never in memory, and G is for a piece of the vocabulary at a time, at
- * most 1 GiB (in 16 bits, or two halves).  Products of bf16 buffers take their bits
- * and 11 or more of G; those of fp32 buffers carry 22 or more.  Everything else is
- * fp32.  Results do not depend on the order in which the GPU runs: reruns give the
- * same bits.
+ * dh is 0 for the tokens left out, whatever h and w hold; dh and dw are written, not
+ * added to.  The logits are never in memory, and G is for a piece of the vocabulary
+ * at a time, at most 1 GiB (in 16 bits, or two halves) or one tile's columns.
+ * Products of bf16 buffers take their bits and 11 or more of G; those of fp32 buffers
+ * carry 22 or more.  With many tokens that holds for entries of h and of w down to
+ * 2^-31 (bf16) or 2^-16 (fp32) of the buffer's largest finite magnitude: smaller ones
+ * lose bits, and vanish below 2^-39 of it; entries of G vanish below 2^-34 of their
+ * token's c or 2^-38 of the largest c.  Everything else is fp32.  Results do not depend
+ * on the order in which the GPU runs: reruns give the same bits.
  * Non-finite values in h, w or weight reach every output that depends on them.
  * dh may not overlap h, nor dw w.
  * Errors: DSM_ERR_INVALID_ARG; DSM_ERR_HIP.

@@ -329,7 +329,9 @@ struct Tile {
             if (s < n) load(s);
         for (int s = 0; s < n; ++s) {
             wait_loads_of(min(n - 1 - s, STAGES - 2));
-            __builtin_amdgcn_s_barrier();  // the stage is there, and the one before it read
+            // The stage is there, and the one before it read: its products come before the
+            // barrier in the compiled code (tests look), so its reads are over.
+            __builtin_amdgcn_s_barrier();
             fence();
             if (s + STAGES - 1 < n) load(s + STAGES - 1);
             compute(lds + s % STAGES * kStageBytes);
@@ -465,9 +467,10 @@ struct HalfSide {
 //
 // 8192 x 8192 x 4096, bf16: 1260 TFLOP/s with both operands k-contiguous, 1150 with
 // one k-strided (1070 with J0 read in its own stage), 1060 with both; split operands
-// 1440-1500 TFLOP/s of matrix instructions.  What bounds it is the board's power:
-// the clock falls to 1.6-1.8 GHz, at which split operands keep the matrix cores
-// 90% busy and fp16 72%; the k-strided reads take the rest.
+// 1440-1500 TFLOP/s of matrix instructions.  In the cross entropy's gradients the clock
+// is at 1.8 GHz (of 2.4) and the matrix cores are busy 69% of the time in which a CU has
+// work with one k-strided operand in fp16, 85% with split ones: the rest is the k-strided
+// reads, starts and epilogues.
 template <Elem E, Kind KI, Kind KJ, bool QUARTERS = KI == kContig && KJ == kContig, bool NARROW = false>
 struct BigTile {
     static_assert(E != kF32, "fp32 products are for tiles that wait for memory");

@@ -15,7 +15,7 @@
 //     computes anew.  6 T V D operations of the matrix cores.
 //   * For the others the logits are computed again, 8 T V D in all.
 // 8192 tokens of 50257 x 768 in bf16, whose G is 0.8 GB: 2.87 ms by two pieces, both
-// computed again; 2.28 ms by one; 1.89 ms with what follows.
+// computed again; 2.28 ms by one; 1.93 ms with what follows.
 //
 // The light pass itself is saved, with many tokens and a large vocabulary, by a
 // reference r_t for each row that is near lse_t and known before the first pass: the
@@ -405,8 +405,8 @@ __device__ __forceinline__ float2 joined(float2 a, float2 c) {
 
 // The logits' tiles in order: eight rows of tokens side by side, along the
 // vocabulary, so that the 32 tiles that an XCD has at once share 8 tiles of h and 4
-// of w.  (With every token's tile in turn, 8192 tokens, h went through each L2
-// again for every tile of w: 2.6 GB from beyond the L2s at 50257 x 768.)
+// of w.  (With every token's tile in turn, 8192 tokens, h went through each L2 again
+// for every tile of w; so, 1.0 GB come from beyond the L2s at 50257 x 768.)
 __device__ __forceinline__ void logit_tile(int id, int tiles_t, int tiles_v, int* tt, int* tv) {
     constexpr int kRows = 8;
     const int group = id / (kRows * tiles_v), rows = min(kRows, tiles_t - group * kRows);
@@ -495,7 +495,7 @@ constexpr int turned(CeForm f) { return -kLow - room(f); }
 // Many tokens, bf16: 8192 of 50257 x 768 in 0.81 ms, 0.78 PFLOP/s.  Of a tile's 32 us
 // the products take 18 (1.44 PFLOP/s), the writes of exponentials 6 (at 5.7 TB/s; one
 // work-group fills a CU, so nothing runs beside them), exponentials, sums and the start
-// of the next tile 8.  One token reads w, 77 MB, in 15 us at 5.1 TB/s; tiles of 32 tokens
+// of the next tile 8: the matrix cores are busy 42% of the time, at 2.0 GHz.  One token reads w, 77 MB, in 15 us at 5.1 TB/s; tiles of 32 tokens
 // by 128 words with four stages on their way fill two work-groups a CU for that.
 template <CeForm FORM, int TM, bool KEEP>
 __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b, int tiles_v, int every, int skip,
@@ -1082,8 +1082,8 @@ __device__ __forceinline__ void dw_tile(const CePlan& p, const CeBuffers& b, int
 // The two products of G in one launch: neither fills the CUs' last turn by itself,
 // and their tiles take different times.  Each XCD has its run of dh's tiles, the
 // longer ones, then its run of dw's.  8192 tokens of 50257 x 768 in bf16: 1.09 ms, 1.16
-// PFLOP/s; what bounds it is LDS, whose transposing reads of k-strided operands give half
-// as much as plain ones, and the board's power: the clock falls to 1.7 GHz.
+// PFLOP/s, the matrix cores busy 69% of the time at 1.8 GHz; what bounds it is LDS, whose
+// transposing reads of k-strided operands give half as much as plain ones, and the clock.
 constexpr int kXcds = 8;
 __host__ __device__ inline int per_xcd(int tiles) { return (tiles + kXcds - 1) / kXcds; }
 

@@ -324,13 +324,14 @@ __device__ __forceinline__ u16x8 lower(const Eight& e) {
 // BM x BM.  The symmetric two take the tiles on and below the diagonal, tile (i, j)
 // before (i, j + 1), and write each a second time, turned in LDS.
 //
-// Eight bf16 6400 x 1600: A in 142 us (224 tiles, 0.94 PFLOP/s of what the symmetry
-// leaves, the matrix cores at 1.36 while they run), B in 51 (of which 17 a launch, its
-// first loads and the turned stores), X in 365 (1400 tiles in six turns; their products
-// take 231 us, the epilogue's 491 MB the rest: one work-group fills a CU, so they do not
-// overlap).  Four fp32 5120 x 1280: A in 134 us, B 42, X 194 (two halves: three matrix
-// instructions for one, 1.3-1.5 PFLOP/s of them).  Twelve bf16 768 x 768: 14, 15 and 24 us
-// of one turn or two, a launch's start and end for the most part.
+// Eight bf16 6400 x 1600: A in 137-150 us (224 tiles, 0.9 PFLOP/s of what the symmetry
+// leaves; the matrix cores are busy 78% of the time in which a CU has work, 73% of all),
+// B in 50-55 (of which 17 a launch, its first loads and the turned stores), X in 374-403
+// (1400 tiles in six turns, matrix cores busy 41%: their products take 231 us, the
+// epilogue's 655 MB the rest: one work-group fills a CU, so they do not overlap).  Four fp32
+// 5120 x 1280: A in 127-135 us, B 40-42, X 184-194 (two halves: three matrix instructions
+// for one, 1.3-1.5 PFLOP/s of them).  Twelve bf16 768 x 768: 14, 16 and 26 us of one turn
+// or two, a launch's start and end for the most part.
 template <int S, int BM, Product P>
 __global__ __launch_bounds__(tile::threads_of(BM)) void k_product(OrthoGroup g, Parts parts, int from, float mul,
                                                                     float add, int fallen, int next, int late) {
