@@ -495,8 +495,9 @@ constexpr int turned(CeForm f) { return -kLow - room(f); }
 // Many tokens, bf16: 8192 of 50257 x 768 in 0.81 ms, 0.78 PFLOP/s.  Of a tile's 32 us
 // the products take 18 (1.44 PFLOP/s), the writes of exponentials 6 (at 5.7 TB/s; one
 // work-group fills a CU, so nothing runs beside them), exponentials, sums and the start
-// of the next tile 8: the matrix cores are busy 42% of the time, at 2.0 GHz.  One token reads w, 77 MB, in 15 us at 5.1 TB/s; tiles of 32 tokens
-// by 128 words with four stages on their way fill two work-groups a CU for that.
+// of the next tile 8: the matrix cores are busy 42% of the time, at 2.0 GHz.  One token
+// reads w, 77 MB, in 15 us at 5.1 TB/s; tiles of 32 tokens by 128 words with four stages
+// on their way fill two work-groups a CU for that.
 template <CeForm FORM, int TM, bool KEEP>
 __global__ __launch_bounds__(threads_of(TM)) void k_stats(CePlan p, CeBuffers b, int tiles_v, int every, int skip,
                                                           int slot, int done) {

@@ -5,8 +5,9 @@ PyTorch only allocates device memory and supplies the stream; the operators run
 in libdsm.so through the binding in ``dsm``.  An object here is the plan of one
 problem: it checks tensors, keeps the workspace, and enqueues on torch's current
 stream.  Calls of one object share its workspace: on different streams they are put
-one after another (under graph capture that is the caller's part), and from several
-threads each call's launches are enqueued whole before the next call's.
+one after another (under graph capture that is the caller's part, as is keeping the
+object while the graph is replayed), and from several threads each call's launches are
+enqueued whole before the next call's.
 """
 import contextlib
 import threading
