@@ -503,6 +503,203 @@ DSM_API dsm_status dsm_ortho_step(const dsm_ortho_problem* problem, const dsm_or
                                   const dsm_ortho_hparams* hp);
 
 /*
+ * The operators that a model's blocks and their gradients take, up to the gradients
+ * that dsm_local_step reads: the linear layer, the norms around a block, clipping.
+ * They are called as the operators above are: a problem, buffers, a workspace that
+ * holds nothing between calls, one for each of two calls that may overlap.
+ * Vectors (biases, gates, norms' weights) and their gradients are fp32, as in the
+ * arenas, whatever the type of the rows.
+ */
+
+/* Activations: relu max(z, 0); gelu z (1 + erf(z / sqrt 2)) / 2; gelu_tanh
+ * z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2; silu z / (1 + exp(-z)). */
+typedef enum dsm_act {
+    DSM_ACT_NONE = 0,
+    DSM_ACT_RELU = 1,
+    DSM_ACT_GELU = 2,
+    DSM_ACT_GELU_TANH = 3,
+    DSM_ACT_SILU = 4
+} dsm_act;
+
+typedef struct dsm_linear_problem {
+    int64_t tokens;   /* T in [0, 2^20] */
+    int64_t dim;      /* D in [1, 2^16], columns of x and w */
+    int64_t wide;     /* N in [1, 2^16], rows of w, columns of y */
+    int32_t dtype;    /* dsm_dtype of x, w, y, z, residual, dy and dx */
+    int32_t act;      /* dsm_act */
+    int32_t dw_dtype; /* dsm_dtype of dw: dtype, or DSM_F32 */
+    int32_t grads;    /* 1: dsm_linear_backward is called too (for the workspace) */
+} dsm_linear_problem;
+
+/* Matrices have contiguous rows, *_stride elements apart. */
+typedef struct dsm_linear_buffers {
+    const void* x;        /* [T, D] */
+    int64_t x_stride;
+    const void* w;        /* [N, D] */
+    int64_t w_stride;
+    const float* bias;    /* [N], or NULL */
+    const void* residual; /* [T, N], or NULL; may be y itself, with y's stride */
+    int64_t residual_stride;
+    void* y;              /* [T, N] */
+    int64_t y_stride;
+    void* z;              /* [T, N] x w^T + bias: dsm_linear writes it where given,
+                             dsm_linear_backward reads it unless act is none */
+    int64_t z_stride;
+    const void* dy;       /* [T, N], the gradient of y */
+    int64_t dy_stride;
+    void* dx;             /* [T, D], or NULL where not wanted */
+    int64_t dx_stride;
+    void* dw;             /* [N, D], or NULL */
+    int64_t dw_stride;
+    float* dbias;         /* [N], or NULL */
+    void* workspace;
+    int64_t workspace_bytes;
+    void* stream;
+} dsm_linear_buffers;
+
+/* dsm_linear_workspace - host only: the workspace of a problem in bytes (0 for up to
+ * 64 tokens without gradients).  Errors: DSM_ERR_INVALID_ARG. */
+DSM_API dsm_status dsm_linear_workspace(const dsm_linear_problem* problem, int64_t* workspace_bytes);
+
+/*
+ * dsm_linear - z = x w^T + bias;  y = act(z) + residual
+ * y takes z before its rounding.  Products of bf16 take their operands' bits; those of
+ * fp32 carry 22 bits or more of entries down to 2^-16 of their row's largest finite
+ * magnitude (smaller ones lose bits, and vanish below 2^-39 of it), all of them up to
+ * 64 tokens.  Sums, bias, activation and residual are fp32, rounded once.  Reruns give
+ * the same bits.  Non-finite values reach every output that depends on them.
+ * dsm_linear reads x, w, bias, residual and writes y and z; neither may overlap what is
+ * read, except y the residual.  Errors: DSM_ERR_INVALID_ARG; DSM_ERR_HIP.
+ */
+DSM_API dsm_status dsm_linear(const dsm_linear_problem* problem, const dsm_linear_buffers* buffers);
+
+/*
+ * dsm_linear_backward - the gradients of dsm_linear's y, given dy and z:
+ *   dz = dy act'(z);  dx = dz w;  dw = dz^T x;  dbias = the tokens' sum of dz
+ * (the residual's gradient is dy itself).  Outputs are written, not added to; any may be
+ * NULL.  Where there is an activation, bf16 takes dz rounded to bf16 into the products,
+ * and in fp32 into dbias.  Products of fp32 carry 22 bits or more of entries of dz
+ * down to 2^-16 of their token's largest, of w of its largest, and of x of the largest
+ * that a token's x and dz make together.
+ * dx, dw and dbias may not overlap what is read.  Errors: DSM_ERR_INVALID_ARG; DSM_ERR_HIP.
+ */
+DSM_API dsm_status dsm_linear_backward(const dsm_linear_problem* problem, const dsm_linear_buffers* buffers);
+
+/* A norm of a row v of `dim` columns, means over the row:
+ * layer (v - mean) / sqrt(mean of (v - mean)^2 + eps) weight + bias;
+ * rms v / sqrt(mean of v^2 + eps) weight + bias. */
+typedef enum dsm_norm_kind { DSM_NORM_NONE = 0, DSM_NORM_LAYER = 1, DSM_NORM_RMS = 2 } dsm_norm_kind;
+
+typedef struct dsm_norm_problem {
+    int64_t tokens; /* T in [0, 2^30] */
+    int64_t dim;    /* D in [1, 8192] */
+    int32_t dtype;  /* dsm_dtype of the rows */
+    int32_t norm;   /* dsm_norm_kind of y */
+    int32_t post;   /* dsm_norm_kind of the block's output f */
+    int32_t grads;  /* 1: dsm_residual_norm_backward is called too (for the workspace) */
+    float eps;      /* >= 0, of norm */
+    float post_eps; /* >= 0, of post */
+    float scale;    /* factor of the block's output */
+} dsm_norm_problem;
+
+/* Rows are contiguous, *_stride elements apart. */
+typedef struct dsm_norm_buffers {
+    const void* h;            /* [T, D] residual stream; for the gradients s, or h itself
+                                 where there is no f */
+    int64_t h_stride;
+    const void* f;            /* [T, D] the block's output, or NULL for none */
+    int64_t f_stride;
+    const float* weight;      /* [D], NULL for 1 */
+    const float* bias;        /* [D], NULL for 0 */
+    const float* gate;        /* [D], NULL for 1 */
+    const float* post_weight; /* [D], NULL for 1 */
+    const float* post_bias;   /* [D], NULL for 0 */
+    void* s;                  /* [T, D] or NULL */
+    int64_t s_stride;
+    void* y;                  /* [T, D], NULL without a norm */
+    int64_t y_stride;
+    const void* dy;           /* [T, D], NULL without a norm */
+    int64_t dy_stride;
+    const void* ds;           /* [T, D] the gradient that s has from elsewhere, or NULL */
+    int64_t ds_stride;
+    void* dh;                 /* [T, D], or NULL where not wanted, as all that follow */
+    int64_t dh_stride;
+    void* df;                 /* [T, D] */
+    int64_t df_stride;
+    float* dweight;           /* [D] */
+    float* dbias;
+    float* dgate;
+    float* dpost_weight;
+    float* dpost_bias;
+    void* workspace;
+    int64_t workspace_bytes;
+    void* stream;
+} dsm_norm_buffers;
+
+/* dsm_norm_workspace - host only: the workspace of a problem in bytes (0 without
+ * gradients).  Errors: DSM_ERR_INVALID_ARG. */
+DSM_API dsm_status dsm_norm_workspace(const dsm_norm_problem* problem, int64_t* workspace_bytes);
+
+/*
+ * dsm_residual_norm - p = post(f);  s = h + scale gate p;  y = norm(s)
+ * and without f, y = norm(h).  y takes s before its rounding.  Everything is fp32,
+ * rounded once.  s may be h or f, and y any of them, in place (the same pointer and
+ * stride); otherwise outputs may not overlap inputs.
+ * Errors: DSM_ERR_INVALID_ARG; DSM_ERR_HIP.
+ */
+DSM_API dsm_status dsm_residual_norm(const dsm_norm_problem* problem, const dsm_norm_buffers* buffers);
+
+/*
+ * dsm_residual_norm_backward - the gradients of s and y at s (in h) and f, whose
+ * statistics are computed anew:
+ *   d = ds + the gradient of norm at s times dy;  dh = d
+ *   df = the gradient of post at f times (scale gate d)
+ *   dweight, dbias, dgate, dpost_weight, dpost_bias: the tokens' sums
+ * Outputs are written, not added to.  f is read where post, gate's or post's gradients
+ * need it.  Rerunning gives the same bits.  dh may be dy or ds, and df dy, ds or f, in
+ * place.  Errors: DSM_ERR_INVALID_ARG; DSM_ERR_HIP.
+ */
+DSM_API dsm_status dsm_residual_norm_backward(const dsm_norm_problem* problem, const dsm_norm_buffers* buffers);
+
+/*
+ * A tensor of gradients: element e of its numel lies at
+ *   data + ((first + e) / block) * stride + (first + e) % block   (in elements)
+ * Contiguous: first 0, block = stride = numel.  Rows: block = columns, stride apart.
+ * Worker i's tensor in the arenas of dsm_layout: first = its offset; block = stride =
+ * d_pad and data = g_rep + i * d_pad, or with DSM_REPLICAS_STATE_BLOCKED block =
+ * DSM_STATE_BLOCK_ELEMS, stride = B * n * block and data = g_rep + i * block.
+ */
+typedef struct dsm_clip_tensor {
+    void* data;
+    int64_t first;  /* >= 0 */
+    int64_t numel;  /* >= 0 */
+    int64_t block;  /* >= 1 */
+    int64_t stride; /* >= block */
+    int32_t dtype;  /* dsm_dtype */
+    int32_t group;  /* whose norm it counts for: 0 .. n_groups - 1, not falling from
+                       one tensor to the next */
+} dsm_clip_tensor;
+
+/* dsm_clip_workspace - host only: the workspace in bytes (data is not read).
+ * Errors: DSM_ERR_INVALID_ARG. */
+DSM_API dsm_status dsm_clip_workspace(const dsm_clip_tensor* tensors, int32_t n_tensors, int32_t n_groups,
+                                      int64_t* workspace_bytes);
+
+/*
+ * dsm_grad_clip - for every group, norm = the 2-norm of all its tensors' elements and
+ *   g <- g min(1, max_norm / (norm + eps))
+ * in place.  Squares and sums are fp64, the factor is rounded to fp32, the product to
+ * the tensor's type.  norm[group] is written; a group without elements has norm 0.
+ * Gradients whose norm is NaN or infinite in fp64 stay as they are, and so do those
+ * that need no clipping.  max_norm = infinity: norms alone.  Tensors must not overlap.
+ * n_groups in [1, 256]; max_norm >= 0; eps >= 0, finite; 1e-6 is customary.
+ * Errors: DSM_ERR_INVALID_ARG; DSM_ERR_HIP.
+ */
+DSM_API dsm_status dsm_grad_clip(const dsm_clip_tensor* tensors, int32_t n_tensors, int32_t n_groups,
+                                 float max_norm, float eps, float* norm, void* workspace,
+                                 int64_t workspace_bytes, void* stream);
+
+/*
  * dsm_destroy - synchronises the context's stream and frees the context's
  * host memory.  The caller's device buffers are untouched.  NULL is a no-op.
  */

@@ -22,8 +22,8 @@ LIBPATH = os.path.join(LIBDIR, "libdsm.so")
 ARCH = "gfx950"
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 
-KERNELS = ["dsm_kernels.hip", "ortho.hip", "linear_ce.hip"]
-HOST = ["dsm_runtime.cpp", "ops_runtime.cpp"]
+KERNELS = ["dsm_kernels.hip", "ortho.hip", "linear_ce.hip", "linear.hip", "norm.hip", "clip.hip"]
+HOST = ["dsm_runtime.cpp", "ops_runtime.cpp", "block_runtime.cpp"]
 
 # Numerics: one IEEE fp32 rounding per written operation (no FMA contraction),
 # correctly rounded division and square root, denormals kept.  Packed fp32

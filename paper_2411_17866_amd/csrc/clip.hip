@@ -1,0 +1,183 @@
+// The global norm of many gradients, and clipping by it, on gfx950.
+//
+//   norm = sqrt(sum of g^2 over a group's tensors);  g <- g min(1, max / (norm + eps))
+//
+// A work-group takes a chunk of a tensor; squares are taken and summed in fp64, so
+// that no magnitude of fp32 overflows or vanishes in them and the order of the sums
+// does not show in the norm.  (A conversion and an fma an element, a fifth of what
+// the CUs can do while memory brings them.)  Sums of chunks go to the workspace and
+// are joined in a fixed order.
+//
+// It is bound by memory: all gradients are read, and where the norm exceeds the
+// maximum read again and written.  The second pass takes the chunks from the last to
+// the first: what was read last is still in the last-level cache.
+#include "block_internal.h"
+#include "elements.h"
+
+#pragma clang fp contract(off)
+
+namespace dsm {
+namespace {
+
+using rows::V8;
+
+struct Chunk {
+    ClipEntry e;
+    int64_t at;  // of the tensor's elements
+    int n;
+};
+
+__device__ __forceinline__ Chunk chunk_of(const ClipTable& t, int c) {
+    int lo = 0, hi = t.count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (t.e[mid].chunk <= c)
+            lo = mid;
+        else
+            hi = mid - 1;
+    }
+    Chunk k;
+    k.e = t.e[lo];
+    k.at = static_cast<int64_t>(c - k.e.chunk) * kClipChunk;
+    k.n = static_cast<int>(min(static_cast<int64_t>(kClipChunk), k.e.numel - k.at));
+    return k;
+}
+
+// Calls use(offset from data, elements) for runs of up to eight elements that lie side by side.
+template <class F>
+__device__ __forceinline__ void each_run(const Chunk& k, F use) {
+    const int64_t start = k.e.first + k.at;
+    if (k.e.block >= k.e.first + k.e.numel) {  // one run
+#pragma unroll 4
+        for (int u = threadIdx.x * 8; u < k.n; u += 2048) use(start + u, k.n - u);
+        return;
+    }
+    const int64_t row = start / k.e.block, col = start - row * k.e.block;
+    const int wide = start % 8 == 0 && k.e.block % 8 == 0 ? 8 : 1;
+    if (k.e.block >= kClipChunk) {  // at most one row ends inside
+        const int left = static_cast<int>(min(k.e.block - col, static_cast<int64_t>(kClipChunk)));
+#pragma unroll 4
+        for (int u = threadIdx.x * wide; u < k.n; u += 256 * wide) {
+            const int64_t at = u < left ? row * k.e.stride + col + u : (row + 1) * k.e.stride + u - left;
+            use(at, min(wide, k.n - u));
+        }
+    } else {
+        const unsigned block = static_cast<unsigned>(k.e.block), c0 = static_cast<unsigned>(col);
+#pragma unroll 4
+        for (int u = threadIdx.x * wide; u < k.n; u += 256 * wide) {
+            const unsigned c = c0 + u, r = c / block;
+            use((row + r) * k.e.stride + (c - r * block), min(wide, k.n - u));
+        }
+    }
+}
+
+// The sum of a work-group's values, in its first lane.
+__device__ __forceinline__ double group_sum(double v) {
+    __shared__ double waves[16];
+    for (int w = 32; w > 0; w >>= 1) v += __shfl_xor(v, w);
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = v;
+    __syncthreads();
+    double s = 0.0;
+    for (unsigned w = 0; w < blockDim.x / 64; ++w) s += waves[w];
+    return s;
+}
+
+template <bool F32>
+__device__ __forceinline__ double squares(const Chunk& k) {
+    double a = 0.0, b = 0.0;
+    each_run(k, [&](int64_t at, int have) {
+        const V8 x = rows::load8<F32>(k.e.data, at, have);
+#pragma unroll
+        for (int q = 0; q < 8; q += 2) {
+            const double u = x.v[q], v = x.v[q + 1];
+            a = __builtin_fma(u, u, a);
+            b = __builtin_fma(v, v, b);
+        }
+    });
+    return a + b;
+}
+
+__global__ __launch_bounds__(256) void k_clip_squares(ClipTable t, double* parts) {
+    const Chunk k = chunk_of(t, blockIdx.x);
+    const double s = group_sum(k.e.bf16 ? squares<false>(k) : squares<true>(k));
+    if (threadIdx.x == 0) parts[t.slot + blockIdx.x] = s;
+}
+
+// A group's norm from its chunks' sums.
+template <class Groups>
+__device__ __forceinline__ double group_norm(const Groups& g, int group, const double* parts) {
+    double s = 0.0;
+    for (int64_t c = g.start[group] + threadIdx.x; c < g.start[group + 1]; c += blockDim.x) s += parts[c];
+    return sqrt(group_sum(s));
+}
+// Gradients whose norm is not a finite number stay as they are: no factor mends them.
+template <class Groups>
+__device__ __forceinline__ float factor_of(const Groups& g, double norm) {
+    if (!(norm < __builtin_inf())) return 1.f;
+    return static_cast<float>(fmin(1.0, static_cast<double>(g.max_norm) / (norm + static_cast<double>(g.eps))));
+}
+
+__global__ __launch_bounds__(1024) void k_clip_norms(ClipGroups g, const double* parts, float* norm, float* factor) {
+    const double v = group_norm(g, blockIdx.x, parts);
+    if (threadIdx.x != 0) return;
+    norm[blockIdx.x] = static_cast<float>(v);
+    factor[blockIdx.x] = factor_of(g, v);
+}
+
+template <bool F32>
+__device__ __forceinline__ void scale(const Chunk& k, float by) {
+    each_run(k, [&](int64_t at, int have) {
+        V8 x = rows::load8<F32>(k.e.data, at, have);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) x.v[q] *= by;
+        rows::store8<F32>(k.e.data, at, x, have);
+    });
+}
+__device__ __forceinline__ void scale(const Chunk& k, float by) {
+    if (by == 1.f) return;
+    if (k.e.bf16)
+        scale<false>(k, by);
+    else
+        scale<true>(k, by);
+}
+
+__global__ __launch_bounds__(256) void k_clip_scale(ClipTable t, const float* factor) {
+    const Chunk k = chunk_of(t, t.chunks - 1 - blockIdx.x);
+    scale(k, factor[k.e.group]);
+}
+
+// Few chunks: a launch less.  The work-groups past the chunks write the norms.
+__global__ __launch_bounds__(256) void k_clip_rest(ClipTable t, ClipFew g, const double* parts, float* norm) {
+    const int c = blockIdx.x;
+    if (c >= t.chunks) {
+        const double v = group_norm(g, c - t.chunks, parts);
+        if (threadIdx.x == 0) norm[c - t.chunks] = static_cast<float>(v);
+        return;
+    }
+    const Chunk k = chunk_of(t, c);
+    scale(k, factor_of(g, group_norm(g, k.e.group, parts)));
+}
+
+}  // namespace
+
+hipError_t launch_clip_squares(const ClipTable& t, double* parts, hipStream_t stream) {
+    k_clip_squares<<<t.chunks, 256, 0, stream>>>(t, parts);
+    return hipGetLastError();
+}
+
+hipError_t launch_clip_norms(const ClipGroups& g, const double* parts, float* norm, float* factor, hipStream_t stream) {
+    k_clip_norms<<<g.count, 1024, 0, stream>>>(g, parts, norm, factor);
+    return hipGetLastError();
+}
+
+hipError_t launch_clip_scale(const ClipTable& t, const float* factor, hipStream_t stream) {
+    k_clip_scale<<<t.chunks, 256, 0, stream>>>(t, factor);
+    return hipGetLastError();
+}
+
+hipError_t launch_clip_rest(const ClipTable& t, const ClipFew& g, const double* parts, float* norm, hipStream_t stream) {
+    k_clip_rest<<<t.chunks + g.count, 256, 0, stream>>>(t, g, parts, norm);
+    return hipGetLastError();
+}
+
+}  // namespace dsm

@@ -1,0 +1,144 @@
+// Rows of fp32 or bf16 elements, eight to a lane, and sums over a wave or a
+// work-group, for the kernels that stream rows (clip.hip, norm.hip, linear.hip).
+//
+// Rows may start at any element: 16-byte accesses of global memory need no more than
+// the element's own alignment on gfx950, so odd widths and strides take the same path.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace dsm {
+namespace rows {
+
+typedef unsigned short u16;
+typedef u16 u16x8 __attribute__((ext_vector_type(8)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+// The same at any element's address.
+typedef u16x8 u16x8_at __attribute__((aligned(2)));
+typedef f4 f4_at __attribute__((aligned(4)));
+
+__device__ __forceinline__ u16 float_to_bf16(float v) { return __builtin_bit_cast(u16, static_cast<__bf16>(v)); }
+__device__ __forceinline__ float bf16_to_float(u16 v) {
+    return __builtin_bit_cast(float, static_cast<uint32_t>(v) << 16);
+}
+
+struct V8 {
+    float v[8];
+};
+
+// Eight elements from element `at` on, of which `have` exist (the others are 0).
+template <bool F32>
+__device__ __forceinline__ V8 load8(const void* base, int64_t at, int have) {
+    V8 o;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) o.v[q] = 0.f;
+    if constexpr (F32) {
+        const float* p = static_cast<const float*>(base) + at;
+        if (have >= 8) {
+            const f4 a = *reinterpret_cast<const f4_at*>(p), b = *reinterpret_cast<const f4_at*>(p + 4);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                o.v[q] = a[q];
+                o.v[4 + q] = b[q];
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < 7; ++q)
+                if (q < have) o.v[q] = p[q];
+        }
+    } else {
+        const u16* p = static_cast<const u16*>(base) + at;
+        if (have >= 8) {
+            const u16x8 a = *reinterpret_cast<const u16x8_at*>(p);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) o.v[q] = bf16_to_float(a[q]);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 7; ++q)
+                if (q < have) o.v[q] = bf16_to_float(p[q]);
+        }
+    }
+    return o;
+}
+
+template <bool F32>
+__device__ __forceinline__ void store8(void* base, int64_t at, const V8& x, int have) {
+    if constexpr (F32) {
+        float* p = static_cast<float*>(base) + at;
+        if (have >= 8) {
+            f4 a, b;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                a[q] = x.v[q];
+                b[q] = x.v[4 + q];
+            }
+            *reinterpret_cast<f4_at*>(p) = a;
+            *reinterpret_cast<f4_at*>(p + 4) = b;
+        } else {
+#pragma unroll
+            for (int q = 0; q < 7; ++q)
+                if (q < have) p[q] = x.v[q];
+        }
+    } else {
+        u16* p = static_cast<u16*>(base) + at;
+        if (have >= 8) {
+            u16x8 a;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) a[q] = float_to_bf16(x.v[q]);
+            *reinterpret_cast<u16x8_at*>(p) = a;
+        } else {
+#pragma unroll
+            for (int q = 0; q < 7; ++q)
+                if (q < have) p[q] = float_to_bf16(x.v[q]);
+        }
+    }
+}
+
+// x turned by N within every 16 lanes.
+template <int N>
+__device__ __forceinline__ float turned(float x) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x120 + N, 0xf, 0xf, true));
+}
+// The wave's sum, in every lane, in a fixed order: within 16 lanes by turns, then
+// rows of 16 change places.
+__device__ __forceinline__ float wave_sum(float x) {
+    x += turned<8>(x);
+    x += turned<4>(x);
+    x += turned<2>(x);
+    x += turned<1>(x);
+    unsigned u = __builtin_bit_cast(unsigned, x);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    unsigned p = a[0], q = a[1];
+    x = __builtin_bit_cast(float, p) + __builtin_bit_cast(float, q);
+    u = __builtin_bit_cast(unsigned, x);
+    const auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    p = b[0], q = b[1];
+    return __builtin_bit_cast(float, p) + __builtin_bit_cast(float, q);
+}
+
+// Sums of K values over a work-group of W waves, in every lane, through K * W floats
+// of LDS.  Two calls in a row take two buffers, so one barrier is enough: whoever
+// writes a buffer again has passed the barrier that follows everyone's reads of it.
+template <int W, int K>
+__device__ __forceinline__ void group_sums(float (&x)[K], float* lds) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) x[k] = wave_sum(x[k]);
+    if constexpr (W > 1) {
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) lds[k * W + (threadIdx.x >> 6)] = x[k];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            float s = lds[k * W];
+#pragma unroll
+            for (int w = 1; w < W; ++w) s += lds[k * W + w];
+            x[k] = s;
+        }
+    }
+}
+
+}  // namespace rows
+}  // namespace dsm

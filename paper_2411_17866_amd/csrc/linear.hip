@@ -1,0 +1,886 @@
+// The linear layer with bias, activation and residual, and its gradients, on gfx950.
+//
+//   z = x w^T + bias;  y = act(z) + residual
+//   dz = dy act'(z);  dx = dz w;  dw = dz^T x;  dbias = sum over the tokens of dz
+//
+// Up to kLinearFew tokens the forward pass is bound by reading w once: k_few does it
+// in one launch, without tiles in LDS and without copies.  More tokens go through the
+// tiles of gemm_tile.h with bias, activation and residual in their epilogue.  The
+// gradients are two products of dz in one launch, dz being made by a pass of its own,
+// which also sums dbias; where there is no activation, dy is taken where it lies.
+//
+// What the products take:
+//   bf16  the operands as they are, where rows of 64 columns (k-contiguous) or of 8
+//         (k-strided) are whole and aligned, else copies with zeros behind the rows.
+//         dz is rounded to bf16: an error of half a step for each term of a sum, which
+//         averages out to less than the rounding of the result.
+//   fp32  two fp16 halves of every number (gemm_tile.h).  Powers of two bring a row's
+//         largest magnitude just under fp16's, so rows of any size keep their bits:
+//         x's and w's rows forward, dz's for dx.  In dw the sum runs over the tokens,
+//         so there x_t is taken times 2^(c - e_t), e_t being dz_t's power: dz_t x_t
+//         comes out right up to one power, and c brings the largest of them to fp16's
+//         range.  w in dx, whose sum runs over w's rows, has one power for all.
+// Products accumulate in fp32.
+//
+// Sums over a long axis with few tiles are cut into parts that run side by side; they
+// are joined by a launch that then has the epilogue.
+#include <type_traits>
+
+#include "block_internal.h"
+#include "elements.h"
+#include "gemm_tile.h"
+
+#pragma clang fp contract(off)
+
+namespace dsm {
+namespace {
+
+using rows::f4;
+using rows::u16;
+using rows::u16x8;
+using rows::V8;
+using tile::kContig;
+using tile::kStrided;
+using tile::Operand;
+
+constexpr int kNoExponent = 10000;  // of a row of zeros: brings everything to 0
+
+// ---- Activations ----
+
+// 1 / (1 + exp(-v)) and one minus that, each to its own digits.  FAST, for results that
+// are rounded to bf16: the hardware's exp2 and reciprocal (2^-22).
+template <bool FAST>
+__device__ __forceinline__ void logistic(float v, float* share, float* rest) {
+    const float a = fabsf(v);
+    float e, one;
+    if constexpr (FAST) {
+        e = __builtin_amdgcn_exp2f(a * -1.44269504088896341f);
+        one = __builtin_amdgcn_rcpf(1.0f + e);
+    } else {
+        e = expf(-a);
+        one = 1.0f / (1.0f + e);
+    }
+    const float less = e * one;
+    *share = v < 0.f ? less : one;
+    *rest = v < 0.f ? one : less;
+}
+
+constexpr float kTanhA = 1.59576912160573071f;  // 2 sqrt(2 / pi): tanh(u) = 2 logistic(2 u) - 1
+constexpr float kTanhB = 0.044715f;
+
+template <bool FAST>
+__device__ __forceinline__ float activation(int act, float z) {
+    if (act == DSM_ACT_RELU) return z < 0.f ? 0.f : z;
+    if (act == DSM_ACT_GELU) return 0.5f * z * erfcf(z * -0.707106781186547524f);
+    if (act == DSM_ACT_NONE) return z;
+    float share, rest;
+    logistic<FAST>(act == DSM_ACT_SILU ? z : kTanhA * (z + kTanhB * (z * z * z)), &share, &rest);
+    return z * share;
+}
+
+template <bool FAST>
+__device__ __forceinline__ float slope(int act, float z) {
+    if (act == DSM_ACT_RELU) return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;
+    // (Beyond 50 the slopes are 0 and 1 in fp32, and their terms would overflow.)
+    const float v = z > 50.f ? 50.f : z < -50.f ? -50.f : z;
+    if (act == DSM_ACT_GELU) {
+        const float e = FAST ? __builtin_amdgcn_exp2f(v * v * -0.721347520444481703f) : expf(-0.5f * v * v);
+        return 0.5f * erfcf(v * -0.707106781186547524f) + v * 0.398942280401432678f * e;
+    }
+    float share, rest;
+    if (act == DSM_ACT_SILU) {
+        logistic<FAST>(v, &share, &rest);
+        return share + v * share * rest;
+    }
+    const float square = v * v;
+    logistic<FAST>(kTanhA * (v + kTanhB * (square * v)), &share, &rest);
+    return share + v * share * rest * (kTanhA * (1.f + 3.f * kTanhB * square));
+}
+
+// ---- Epilogue of the forward pass ----
+
+// Eight columns of a row of x w^T: bias, z, activation, residual, y.
+template <bool F32>
+__device__ __forceinline__ void finish(const LinearCall& c, int64_t row, int col, V8 v, const V8& bias) {
+    const int have = min(c.p.wide - col, 8);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v.v[q] += bias.v[q];
+    if (c.z) rows::store8<F32>(c.z, row * c.z_stride + col, v, have);
+    if (c.p.act != DSM_ACT_NONE) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v.v[q] = activation<!F32>(c.p.act, v.v[q]);
+    }
+    if (c.residual) {
+        const V8 r = rows::load8<F32>(c.residual, row * c.residual_stride + col, have);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v.v[q] += r.v[q];
+    }
+    rows::store8<F32>(c.y, row * c.y_stride + col, v, have);
+}
+
+__device__ __forceinline__ V8 bias8(const LinearCall& c, int col) {
+    V8 v;
+    if (c.bias) return rows::load8<true>(c.bias, col, c.p.wide - col);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v.v[q] = 0.f;
+    return v;
+}
+
+// ---- Few tokens ----
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bfloat8 __attribute__((ext_vector_type(8)));
+
+// 16 rows of w by G times 16 tokens a work-group, whose eight waves take every eighth
+// run of 128 bytes of k each, straight from memory into registers; their sums meet in
+// LDS.  Rows past the last one are the last one again, and not stored.
+constexpr int kFewWaves = 8;
+constexpr int kFewRuns = 4;  // of a wave on their way at once
+
+template <bool F32>
+struct Run {  // a lane's part of a row's run: 16 bytes of each 64
+    static constexpr int kSteps = F32 ? 32 : 64, kEach = F32 ? 4 : 8;
+    f4 v[2];
+    __device__ __forceinline__ void load(const char* row, int k, int lane) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            v[h] = *reinterpret_cast<const rows::f4_at*>(row + static_cast<int64_t>(k + h * (kSteps / 2)) * (F32 ? 4 : 2) +
+                                                         (lane >> 4) * 16);
+    }
+    // The row's last run, shorter than the others.
+    __device__ __forceinline__ void load_end(const char* row, int k, int dim, int lane) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int at = k + h * (kSteps / 2) + (lane >> 4) * kEach;
+            if constexpr (F32) {
+                v[h] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (at + e < dim) v[h][e] = reinterpret_cast<const float*>(row)[at + e];
+            } else {
+                u16x8 u = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (at + e < dim) u[e] = reinterpret_cast<const u16*>(row)[at + e];
+                v[h] = __builtin_bit_cast(f4, u);
+            }
+        }
+    }
+};
+
+template <bool F32>
+__device__ __forceinline__ f4 multiply(const Run<F32>& w, const Run<F32>& x, f4 acc) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        if constexpr (F32) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(w.v[h][e], x.v[h][e], acc, 0, 0, 0);
+        } else {
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bfloat8, w.v[h]),
+                                                          __builtin_bit_cast(bfloat8, x.v[h]), acc, 0, 0, 0);
+        }
+    }
+    return acc;
+}
+
+template <bool F32, int G>
+__global__ __launch_bounds__(kFewWaves * 64) void k_few(LinearCall c) {
+    using R = Run<F32>;
+    constexpr int kBytes = F32 ? 4 : 2;
+    __shared__ f4 sums[kFewWaves][G][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int n0 = blockIdx.x * 16, t0 = blockIdx.y * 16 * G;
+    const int dim = c.p.dim, whole = dim / R::kSteps;
+    const char* w = static_cast<const char*>(c.w) + static_cast<int64_t>(min(n0 + (lane & 15), c.p.wide - 1)) * c.w_stride * kBytes;
+    const char* x[G];
+    f4 acc[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        x[g] = static_cast<const char*>(c.x) +
+               static_cast<int64_t>(min(t0 + g * 16 + (lane & 15), c.p.tokens - 1)) * c.x_stride * kBytes;
+        acc[g] = f4{0.f, 0.f, 0.f, 0.f};
+    }
+    for (int first = wave; first < whole; first += kFewWaves * kFewRuns) {
+        R a[kFewRuns], b[kFewRuns][G];
+#pragma unroll
+        for (int u = 0; u < kFewRuns; ++u) {
+            const int r = min(first + u * kFewWaves, whole - 1);
+            a[u].load(w, r * R::kSteps, lane);
+#pragma unroll
+            for (int g = 0; g < G; ++g) b[u][g].load(x[g], r * R::kSteps, lane);
+        }
+#pragma unroll
+        for (int u = 0; u < kFewRuns; ++u)
+            if (first + u * kFewWaves < whole) {
+#pragma unroll
+                for (int g = 0; g < G; ++g) acc[g] = multiply(a[u], b[u][g], acc[g]);
+            }
+    }
+    if (whole * R::kSteps < dim && wave == whole % kFewWaves) {
+        R a, b;
+        a.load_end(w, whole * R::kSteps, dim, lane);
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            b.load_end(x[g], whole * R::kSteps, dim, lane);
+            acc[g] = multiply(a, b, acc[g]);
+        }
+    }
+#pragma unroll
+    for (int g = 0; g < G; ++g) sums[wave][g][lane] = acc[g];
+    __syncthreads();
+    // Lane l of a fragment has token l % 16, rows l / 16 * 4 .. + 3 of w: eight rows are
+    // those of lanes l and l + 16.
+    if (threadIdx.x >= G * 32) return;
+    const int g = threadIdx.x >> 5, l = (threadIdx.x & 15) + ((threadIdx.x >> 4) & 1) * 32;
+    const int token = t0 + g * 16 + (l & 15), col = n0 + (l >> 5) * 8;
+    if (token >= c.p.tokens || col >= c.p.wide) return;
+    f4 lo = sums[0][g][l], hi = sums[0][g][l + 16];
+#pragma unroll
+    for (int q = 1; q < kFewWaves; ++q) {
+        lo += sums[q][g][l];
+        hi += sums[q][g][l + 16];
+    }
+    V8 v;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        v.v[q] = lo[q];
+        v.v[4 + q] = hi[q];
+    }
+    finish<F32>(c, token, col, v, bias8(c, col));
+}
+
+// ---- Operands ----
+
+__device__ __forceinline__ u16 float_to_half(float v) { return __builtin_bit_cast(u16, static_cast<_Float16>(v)); }
+__device__ __forceinline__ float half_to_float(u16 v) { return static_cast<float>(__builtin_bit_cast(_Float16, v)); }
+
+__device__ __forceinline__ uint32_t finite_bits(float v) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, v) & 0x7fffffffu;
+    return b < 0x7f800000u ? b : 0u;
+}
+__device__ __forceinline__ uint32_t top_of(const V8& x, uint32_t top) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) top = max(top, finite_bits(x.v[q]));
+    return top;
+}
+__device__ __forceinline__ uint32_t wave_top(uint32_t top) {
+    for (int w = 32; w > 0; w >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), w)));
+    return top;
+}
+// The power of two that brings a largest magnitude into [2^14, 2^15).
+__device__ __forceinline__ int exponent_for(uint32_t bits) {
+    if (bits == 0) return kNoExponent;
+    int e;
+    frexpf(__builtin_bit_cast(float, bits), &e);
+    return 15 - e;
+}
+
+// Eight numbers times 2^e as two halves each, at column col of a row.
+__device__ __forceinline__ void store_halves(u16* row, int col, const V8& x, int e) {
+    u16x8 hi, lo;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        const float v = ldexpf(x.v[q], e);
+        hi[q] = float_to_half(v);
+        lo[q] = float_to_half(v - half_to_float(hi[q]));
+    }
+    u16* at = row + ((col >> 5) << 6) + (col & 31);
+    *reinterpret_cast<u16x8*>(at) = hi;
+    *reinterpret_cast<u16x8*>(at + 32) = lo;
+}
+
+// x and w (blockIdx.y) with zeros behind their rows, one wave a row.  bf16: a copy.
+// fp32, forward: halves, and the rows' exponents.
+template <bool F32>
+__global__ __launch_bounds__(256) void k_copies(LinearCall c, int from) {
+    const bool of_w = from + blockIdx.y != 0;
+    const int rows = of_w ? c.p.wide : c.p.tokens, lane = threadIdx.x & 63;
+    const void* src = of_w ? c.w : c.x;
+    const int64_t stride = of_w ? c.w_stride : c.x_stride, ld = c.p.ld_dim;
+    const int cols = static_cast<int>(ld / (F32 ? 2 : 1));
+    u16* dst = reinterpret_cast<u16*>(c.workspace + (of_w ? c.p.w : c.p.x));
+    for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4) {
+        int e = 0;
+        if constexpr (F32) {
+            uint32_t top = 0;
+#pragma unroll 4
+            for (int k = lane * 8; k < c.p.dim; k += 512) top = top_of(rows::load8<true>(src, r * stride + k, c.p.dim - k), top);
+            e = exponent_for(wave_top(top));
+            if (lane == 0) reinterpret_cast<int32_t*>(c.workspace + (of_w ? c.p.w_exp : c.p.x_exp))[r] = e;
+        }
+#pragma unroll 4
+        for (int k = lane * 8; k < cols; k += 512) {
+            const V8 v = rows::load8<F32>(src, r * stride + k, c.p.dim - k);
+            if constexpr (F32)
+                store_halves(dst + r * ld, k, v, e);
+            else
+                rows::store8<false>(dst + r * ld, k, v, 8);
+        }
+    }
+}
+
+// bf16: dz with zeros behind its rows (unless it is dy, read where it lies) and dbias's sums, 64
+// tokens by 512 columns a work-group.
+__global__ __launch_bounds__(256) void k_dz(LinearCall c) {
+    __shared__ V8 sums[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = (blockIdx.x * 64 + lane) * 8;
+    const int wide = c.p.wide, have = max(0, min(wide - col, 8));
+    u16* dz = reinterpret_cast<u16*>(c.workspace + c.p.dz);
+    V8 sum;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) sum.v[q] = 0.f;
+#pragma unroll 4
+    for (int k = wave; k < kDzRows; k += 4) {
+        const int64_t row = static_cast<int64_t>(blockIdx.y) * kDzRows + k;
+        const int here = row < c.p.tokens ? have : 0;
+        V8 d = rows::load8<false>(c.dy, row * c.dy_stride + col, here);
+        if (c.p.act != DSM_ACT_NONE) {
+            const V8 z = rows::load8<false>(c.z_in, row * c.z_stride + col, here);
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                if (q < here) d.v[q] *= slope<true>(c.p.act, z.v[q]);
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) sum.v[q] += d.v[q];
+        if (!c.dz_direct && row < c.p.pad_tokens && col < c.p.ld_wide) rows::store8<false>(dz, row * c.p.ld_wide + col, d, 8);
+    }
+    if (!c.dbias) return;
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave != 0) return;
+#pragma unroll
+    for (int w = 1; w < 4; ++w)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) sum.v[q] += sums[w][lane].v[q];
+    rows::store8<true>(c.workspace + c.p.bias_sums, static_cast<int64_t>(blockIdx.y) * wide + col, sum, have);
+}
+
+// fp32: dz as halves, its rows' exponents, dbias's sums, and the least exponent of x dz, kDzSplitRows
+// tokens a work-group; the work-groups before those look for w's largest magnitude.
+__global__ __launch_bounds__(256) void k_dz_split(LinearCall c, int top_groups) {
+    constexpr int R = kDzSplitRows;
+    __shared__ uint32_t tops[R][4];
+    __shared__ uint32_t x_tops[R];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (static_cast<int>(blockIdx.x) < top_groups) {
+        uint32_t top = 0;
+        for (int r = blockIdx.x * 4 + wave; r < c.p.wide; r += top_groups * 4)
+#pragma unroll 4
+            for (int k = lane * 8; k < c.p.dim; k += 512)
+                top = top_of(rows::load8<true>(c.w, r * c.w_stride + k, c.p.dim - k), top);
+        top = wave_top(top);
+        if (lane == 0) tops[0][wave] = top;
+        __syncthreads();
+        if (threadIdx.x == 0)
+            reinterpret_cast<uint32_t*>(c.workspace + c.p.w_tops)[blockIdx.x] =
+                max(max(tops[0][0], tops[0][1]), max(tops[0][2], tops[0][3]));
+        return;
+    }
+    const int group = blockIdx.x - top_groups, wide = c.p.wide;
+    const int64_t first = static_cast<int64_t>(group) * R;
+    u16* dz = reinterpret_cast<u16*>(c.workspace + c.p.dz);
+    const auto load = [&](int k, int col, int have) {
+        const int64_t row = first + k;
+        const int here = row < c.p.tokens ? have : 0;
+        V8 d = rows::load8<true>(c.dy, row * c.dy_stride + col, here);
+        if (c.p.act != DSM_ACT_NONE) {
+            const V8 z = rows::load8<true>(c.z_in, row * c.z_stride + col, here);
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                if (q < here) d.v[q] *= slope<false>(c.p.act, z.v[q]);
+        }
+        return d;
+    };
+    uint32_t top[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) top[k] = 0;
+    for (int col = threadIdx.x * 8; col < wide; col += 2048) {
+        const int have = min(wide - col, 8);
+        V8 sum;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) sum.v[q] = 0.f;
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const V8 d = load(k, col, have);
+            top[k] = top_of(d, top[k]);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) sum.v[q] += d.v[q];
+        }
+        if (c.dbias && first < c.p.tokens)
+            rows::store8<true>(c.workspace + c.p.bias_sums, static_cast<int64_t>(group) * wide + col, sum, have);
+    }
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        top[k] = wave_top(top[k]);
+        if (lane == 0) tops[k][wave] = top[k];
+    }
+    if (c.dw) {  // x's rows, two a wave
+#pragma unroll
+        for (int k = wave; k < R; k += 4) {
+            uint32_t t = 0;
+            const int64_t row = first + k;
+            if (row < c.p.tokens)
+                for (int col = lane * 8; col < c.p.dim; col += 512)
+                    t = top_of(rows::load8<true>(c.x, row * c.x_stride + col, c.p.dim - col), t);
+            t = wave_top(t);
+            if (lane == 0) x_tops[k] = t;
+        }
+    }
+    __syncthreads();
+    int e[R], least = kNoExponent;
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        e[k] = exponent_for(max(max(tops[k][0], tops[k][1]), max(tops[k][2], tops[k][3])));
+        if (c.dw) least = min(least, e[k] + exponent_for(x_tops[k]));
+    }
+    if (threadIdx.x == 0) {
+        if (c.dw) reinterpret_cast<int32_t*>(c.workspace + c.p.tops)[group] = least;
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+            if (first + k < c.p.tokens) reinterpret_cast<int32_t*>(c.workspace + c.p.z_exp)[first + k] = e[k];
+    }
+    const int cols = static_cast<int>(c.p.ld_wide / 2);
+    for (int col = threadIdx.x * 8; col < cols; col += 2048) {
+        const int have = max(0, min(wide - col, 8));
+#pragma unroll
+        for (int k = 0; k < R; ++k) store_halves(dz + (first + k) * c.p.ld_wide, col, load(k, col, have), e[k]);
+    }
+}
+
+// The largest of a work-group of 256.
+__device__ __forceinline__ int largest(int v) {
+    __shared__ int waves[4];
+    for (int w = 32; w > 0; w >>= 1) v = max(v, __shfl_xor(v, w));
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return max(max(waves[0], waves[1]), max(waves[2], waves[3]));
+}
+
+// fp32: w (blockIdx.y = 1) times one power of two, and x (0) times those that make its rows meet dz's.
+__global__ __launch_bounds__(256) void k_back_copies(LinearCall c, int from, int top_groups, int dz_groups) {
+    const bool of_w = from + blockIdx.y != 0;
+    int e;
+    if (of_w) {
+        int top = 0;  // (bits of a magnitude: at least 0)
+        const int* tops = reinterpret_cast<const int*>(c.workspace + c.p.w_tops);
+        for (int q = threadIdx.x; q < top_groups; q += 256) top = max(top, tops[q]);
+        e = exponent_for(static_cast<uint32_t>(largest(top)));
+    } else {
+        int least = -kNoExponent;
+        const int* tops = reinterpret_cast<const int*>(c.workspace + c.p.tops);
+        for (int q = threadIdx.x; q < dz_groups; q += 256) least = max(least, -tops[q]);
+        e = -largest(least);
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0)
+        *reinterpret_cast<int32_t*>(c.workspace + (of_w ? c.p.w_exp : c.p.x_exp)) = e;
+    const int rows = of_w ? c.p.wide : c.p.tokens, lane = threadIdx.x & 63;
+    const void* src = of_w ? c.w : c.x;
+    const int64_t stride = of_w ? c.w_stride : c.x_stride, ld = c.p.ld_dim;
+    const int cols = static_cast<int>(ld / 2);
+    u16* dst = reinterpret_cast<u16*>(c.workspace + (of_w ? c.p.w : c.p.x));
+    const int32_t* z_exp = reinterpret_cast<const int32_t*>(c.workspace + c.p.z_exp);
+    for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4) {
+        // (A row that dz has no entries for meets zeros alone.)
+        const int by = of_w ? e : z_exp[r] == kNoExponent ? -kNoExponent : e - z_exp[r];
+#pragma unroll 4
+        for (int k = lane * 8; k < cols; k += 512)
+            store_halves(dst + r * ld, k, rows::load8<true>(src, r * stride + k, c.p.dim - k), by);
+    }
+}
+
+// ---- Products ----
+
+template <bool F32>
+constexpr tile::Elem kElem = F32 ? tile::kSplit : tile::kBF16;
+
+template <bool F32>
+__device__ __forceinline__ Operand x_rows(const LinearCall& c) {
+    if (!F32 && c.x_direct) return Operand{static_cast<const u16*>(c.x), c.x_stride, c.p.tokens, c.p.dim};
+    return Operand{reinterpret_cast<const u16*>(c.workspace + c.p.x), c.p.ld_dim, c.p.tokens, static_cast<int32_t>(c.p.ld_dim)};
+}
+template <bool F32>
+__device__ __forceinline__ Operand w_rows(const LinearCall& c) {
+    if (!F32 && c.w_direct) return Operand{static_cast<const u16*>(c.w), c.w_stride, c.p.wide, c.p.dim};
+    return Operand{reinterpret_cast<const u16*>(c.workspace + c.p.w), c.p.ld_dim, c.p.wide, static_cast<int32_t>(c.p.ld_dim)};
+}
+template <bool F32>
+__device__ __forceinline__ Operand dz_rows(const LinearCall& c) {
+    if (!F32 && c.dz_direct) return Operand{static_cast<const u16*>(c.dy), c.dy_stride, c.p.tokens, c.p.wide};
+    return Operand{reinterpret_cast<const u16*>(c.workspace + c.p.dz), c.p.ld_wide, static_cast<int32_t>(c.p.pad_tokens),
+                   static_cast<int32_t>(c.p.ld_wide)};
+}
+
+// Work-groups go to the XCDs in turn; every XCD gets one run of the tiles in order.
+constexpr int kXcds = 8;
+__device__ __forceinline__ int xcd_run(int b, int total) {
+    const int x = b & 7, q = total >> 3, r = total & 7;
+    return x * q + min(x, r) + (b >> 3);
+}
+__host__ __device__ inline int per_xcd(int tiles) { return (tiles + kXcds - 1) / kXcds; }
+
+// Part `part` of `parts` of a sum of `all` steps: whole runs of 64.
+__device__ __forceinline__ void part_of(int all, int parts, int part, int* begin, int* end) {
+    const int each = ((all + 63) / 64 + parts - 1) / parts * 64;
+    *begin = min(part * each, all);
+    *end = min(*begin + each, all);
+}
+
+__device__ __forceinline__ V8 eight_of(const tile::Eight& x) {
+    V8 v;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v.v[q] = x.v[q];
+    return v;
+}
+
+// y, or a part of its sums, by tiles of BM.
+template <bool F32, int BM, bool PARTS>
+__global__ __launch_bounds__(tile::threads_of(BM)) void k_forward(LinearCall c, int tiles_t, int tiles_n) {
+    using T = tile::Pick<kElem<F32>, BM, kContig, kContig>;
+    __shared__ __align__(1024) char lds[T::kLdsBytes];
+    int id = xcd_run(blockIdx.x, gridDim.x);
+    const int part = PARTS ? id / (tiles_t * tiles_n) : 0;
+    id -= part * tiles_t * tiles_n;
+    // Eight rows of tiles side by side, so that the tiles an XCD has at once share rows
+    // of both operands.
+    constexpr int kRows = 8;
+    const int group = id / (kRows * tiles_n), rows = min(kRows, tiles_t - group * kRows);
+    id -= group * kRows * tiles_n;
+    const int tn = id / rows, tt = group * kRows + id - tn * rows;
+    int k0 = 0, k1 = static_cast<int>(c.p.ld_dim / (F32 ? 2 : 1));
+    if (PARTS) part_of(k1, c.p.splits, part, &k0, &k1);
+    T t;
+    t.clear();
+    t.add(x_rows<F32>(c), w_rows<F32>(c), tt * BM, tn * BM, k0, k1, (DSM_LDS char*)lds, c.p.tokens - tt * BM,
+          c.p.wide - tn * BM);
+    const int32_t* x_exp = reinterpret_cast<const int32_t*>(c.workspace + c.p.x_exp);
+    const int32_t* w_exp = reinterpret_cast<const int32_t*>(c.workspace + c.p.w_exp);
+#pragma unroll
+    for (int q = 0; q < T::FJ / 2; ++q) {
+        const int col = tn * BM + t.col8(q);
+        const V8 bias = PARTS ? V8{} : bias8(c, col);
+        int we[8];
+        if constexpr (F32) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) we[e] = w_exp[min(col + e, c.p.wide - 1)];
+        }
+#pragma unroll
+        for (int f = 0; f < T::FI; ++f) {
+            const int row = tt * BM + t.row(f);
+            V8 v = eight_of(t.eight(f, q));
+            if (row >= c.p.tokens || col >= c.p.wide) continue;
+            if constexpr (F32) {
+                const int xe = x_exp[row];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v.v[e] = ldexpf(v.v[e], -(xe + we[e]));
+            }
+            if constexpr (PARTS)
+                rows::store8<true>(c.workspace + c.p.y_parts,
+                                   (static_cast<int64_t>(part) * c.p.tokens + row) * c.p.ld_y + col, v, 8);
+            else
+                finish<F32>(c, row, col, v, bias);
+        }
+    }
+}
+
+// Eight columns of the sum of `parts` arrays of `rows` rows.
+__device__ __forceinline__ V8 joined(const char* at, int64_t row, int col, int64_t rows, int64_t ld, int parts) {
+    V8 v = rows::load8<true>(at, row * ld + col, 8);
+    for (int s = 1; s < parts; ++s) {
+        const V8 a = rows::load8<true>(at, (s * rows + row) * ld + col, 8);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v.v[q] += a.v[q];
+    }
+    return v;
+}
+
+template <bool F32>
+__global__ __launch_bounds__(256) void k_forward_join(LinearCall c) {
+    const int eights = (c.p.wide + 7) / 8;
+    const int64_t all = static_cast<int64_t>(c.p.tokens) * eights, step = static_cast<int64_t>(gridDim.x) * 256;
+    for (int64_t e = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; e < all; e += step) {
+        const int64_t row = e / eights;
+        const int col = static_cast<int>(e - row * eights) * 8;
+        finish<F32>(c, row, col, joined(c.workspace + c.p.y_parts, row, col, c.p.tokens, c.p.ld_y, c.p.splits), bias8(c, col));
+    }
+}
+
+__device__ __forceinline__ void store_dx(const LinearCall& c, int64_t row, int col, const V8& v) {
+    const int have = min(c.p.dim - col, 8);
+    if (c.p.f32)
+        rows::store8<true>(c.dx, row * c.dx_stride + col, v, have);
+    else
+        rows::store8<false>(c.dx, row * c.dx_stride + col, v, have);
+}
+__device__ __forceinline__ void store_dw(const LinearCall& c, int64_t row, int col, const V8& v) {
+    const int have = min(c.p.dim - col, 8);
+    if (c.p.f32 || c.p.dw_f32)
+        rows::store8<true>(c.dw, row * c.dw_stride + col, v, have);
+    else
+        rows::store8<false>(c.dw, row * c.dw_stride + col, v, have);
+}
+
+// Tiles of 256 whose last 128 columns lie past the row are a type of their own.
+template <bool F32, int BM, tile::Kind KI, tile::Kind KJ, bool NARROW>
+struct BackTile {
+    using T = tile::Pick<kElem<F32>, BM, KI, KJ>;
+};
+template <bool F32, tile::Kind KI, tile::Kind KJ, bool NARROW>
+struct BackTile<F32, 256, KI, KJ, NARROW> {
+    using T = tile::BigTile<kElem<F32>, KI, KJ, false, NARROW>;
+};
+
+template <bool F32, int BM, bool NARROW>
+__device__ __forceinline__ void dx_tile(const LinearCall& c, int id, DSM_LDS char* lds) {
+    using T = typename BackTile<F32, BM, kContig, kStrided, NARROW>::T;
+    const int tiles_t = (c.p.tokens + BM - 1) / BM, tiles_d = (c.p.dim + BM - 1) / BM;
+    const int part = id / (tiles_t * tiles_d);
+    id -= part * tiles_t * tiles_d;
+    const int tt = id / tiles_d, td = id - tt * tiles_d;
+    int k0, k1;
+    part_of(static_cast<int>(F32 || !c.dz_direct ? c.p.ld_wide / (F32 ? 2 : 1) : c.p.wide), c.p.dx_splits, part, &k0, &k1);
+    T t;
+    t.clear();
+    t.add(dz_rows<F32>(c), w_rows<F32>(c), tt * BM, td * BM, k0, k1, lds, c.p.tokens - tt * BM, c.p.dim - td * BM);
+    const int32_t* z_exp = reinterpret_cast<const int32_t*>(c.workspace + c.p.z_exp);
+    const int we = F32 ? *reinterpret_cast<const int32_t*>(c.workspace + c.p.w_exp) : 0;
+#pragma unroll
+    for (int f = 0; f < T::FI; ++f) {
+        const int row = tt * BM + t.row(f);
+        if (row >= c.p.tokens) continue;
+        const int e = F32 ? -(z_exp[row] + we) : 0;
+#pragma unroll
+        for (int q = 0; q < T::FJ / 2; ++q) {
+            const int col = td * BM + t.col8(q);
+            V8 v = eight_of(t.eight(f, q));
+            if (col >= c.p.dim) continue;
+            if constexpr (F32) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v.v[k] = ldexpf(v.v[k], e);
+            }
+            if (c.p.dx_splits > 1)
+                rows::store8<true>(c.workspace + c.p.dx_parts,
+                                   (static_cast<int64_t>(part) * c.p.tokens + row) * c.p.ld_dx + col, v, 8);
+            else
+                store_dx(c, row, col, v);
+        }
+    }
+}
+
+template <bool F32, int BM, bool NARROW>
+__device__ __forceinline__ void dw_tile(const LinearCall& c, int id, DSM_LDS char* lds) {
+    using T = typename BackTile<F32, BM, kStrided, kStrided, NARROW>::T;
+    const int tiles_n = (c.p.wide + BM - 1) / BM, tiles_d = (c.p.dim + BM - 1) / BM;
+    const int part = id / (tiles_n * tiles_d);
+    id -= part * tiles_n * tiles_d;
+    const int tn = id / tiles_d, td = id - tn * tiles_d;
+    int k0, k1;
+    part_of((c.p.tokens + T::kSteps - 1) / T::kSteps * T::kSteps, c.p.dw_splits, part, &k0, &k1);
+    T t;
+    t.clear();
+    t.add(dz_rows<F32>(c), x_rows<F32>(c), tn * BM, td * BM, k0, k1, lds, c.p.wide - tn * BM, c.p.dim - td * BM);
+    const int e = F32 ? -*reinterpret_cast<const int32_t*>(c.workspace + c.p.x_exp) : 0;
+#pragma unroll
+    for (int f = 0; f < T::FI; ++f) {
+        const int row = tn * BM + t.row(f);
+        if (row >= c.p.wide) continue;
+#pragma unroll
+        for (int q = 0; q < T::FJ / 2; ++q) {
+            const int col = td * BM + t.col8(q);
+            V8 v = eight_of(t.eight(f, q));
+            if (col >= c.p.dim) continue;
+            if constexpr (F32) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v.v[k] = ldexpf(v.v[k], e);
+            }
+            if (c.p.dw_splits > 1)
+                rows::store8<true>(c.workspace + c.p.dw_parts,
+                                   (static_cast<int64_t>(part) * c.p.wide + row) * c.p.ld_dx + col, v, 8);
+            else
+                store_dw(c, row, col, v);
+        }
+    }
+}
+
+// dx and dw in one launch: neither fills the CUs' last turn by itself.  Each XCD has its
+// run of one product's tiles, the longer ones, then its run of the other's.
+template <bool F32, int BM>
+__global__ __launch_bounds__(tile::threads_of(BM)) void k_backward(LinearCall c, int dx_tiles, int dw_tiles, int dw_first) {
+    using TX = typename BackTile<F32, BM, kContig, kStrided, false>::T;
+    using TW = typename BackTile<F32, BM, kStrided, kStrided, false>::T;
+    constexpr int kLds = TX::kLdsBytes > TW::kLdsBytes ? TX::kLdsBytes : TW::kLdsBytes;
+    __shared__ __align__(1024) char lds[kLds];
+    const int x = blockIdx.x % kXcds, at = blockIdx.x / kXcds;
+    const int front = per_xcd(dw_first ? dw_tiles : dx_tiles), tiles_d = (c.p.dim + BM - 1) / BM, full = (c.p.dim + 127) / 256;
+    const bool dw = (at < front) == (dw_first != 0);
+    const int id = at < front ? x * front + at : x * per_xcd(dw_first ? dx_tiles : dw_tiles) + at - front;
+    if (id >= (dw ? dw_tiles : dx_tiles)) return;
+    const bool narrow = BM == 256 && id % tiles_d >= full;
+    if (!dw) {
+        if (narrow)
+            dx_tile<F32, BM, BM == 256>(c, id, (DSM_LDS char*)lds);
+        else
+            dx_tile<F32, BM, false>(c, id, (DSM_LDS char*)lds);
+    } else {
+        if (narrow)
+            dw_tile<F32, BM, BM == 256>(c, id, (DSM_LDS char*)lds);
+        else
+            dw_tile<F32, BM, false>(c, id, (DSM_LDS char*)lds);
+    }
+}
+
+// What is left: dbias from its sums (the first work-groups, 64 columns each), and dx
+// and dw where their sums are in parts.
+__global__ __launch_bounds__(256) void k_backward_join(LinearCall c, int bias_groups) {
+    __shared__ float sums[4][64];
+    if (static_cast<int>(blockIdx.x) < bias_groups) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = blockIdx.x * 64 + lane;
+        float s = 0.f;
+        if (col < c.p.wide) {
+            const float* at = reinterpret_cast<const float*>(c.workspace + c.p.bias_sums) + col;
+#pragma unroll 8
+            for (int q = wave; q < c.p.bias_parts; q += 4) s += at[static_cast<int64_t>(q) * c.p.wide];
+        }
+        sums[wave][lane] = s;
+        __syncthreads();
+        if (wave == 0 && col < c.p.wide) c.dbias[col] = (s + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+        return;
+    }
+    const int eights = (c.p.dim + 7) / 8;
+    const int64_t of_dx = c.dx && c.p.dx_splits > 1 ? static_cast<int64_t>(c.p.tokens) * eights : 0;
+    const int64_t of_dw = c.dw && c.p.dw_splits > 1 ? static_cast<int64_t>(c.p.wide) * eights : 0;
+    const int64_t step = static_cast<int64_t>(gridDim.x - bias_groups) * 256;
+    for (int64_t e = static_cast<int64_t>(blockIdx.x - bias_groups) * 256 + threadIdx.x; e < of_dx + of_dw; e += step) {
+        const bool dw = e >= of_dx;
+        const int64_t at = dw ? e - of_dx : e, row = at / eights;
+        const int col = static_cast<int>(at - row * eights) * 8;
+        if (dw)
+            store_dw(c, row, col, joined(c.workspace + c.p.dw_parts, row, col, c.p.wide, c.p.ld_dx, c.p.dw_splits));
+        else
+            store_dx(c, row, col, joined(c.workspace + c.p.dx_parts, row, col, c.p.tokens, c.p.ld_dx, c.p.dx_splits));
+    }
+}
+
+// No tokens: dw and dbias are zero.
+__global__ __launch_bounds__(256) void k_no_tokens(LinearCall c) {
+    V8 zero;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) zero.v[q] = 0.f;
+    if (c.dbias)
+        for (int n = blockIdx.x * 256 + threadIdx.x; n < c.p.wide; n += gridDim.x * 256) c.dbias[n] = 0.f;
+    if (!c.dw) return;
+    for (int row = blockIdx.x; row < c.p.wide; row += gridDim.x)
+        for (int col = threadIdx.x * 8; col < c.p.dim; col += 2048) store_dw(c, row, col, zero);
+}
+
+// ---- Launches ----
+
+unsigned groups_for(int64_t wanted, int64_t most) { return static_cast<unsigned>(wanted < most ? wanted : most); }
+
+template <bool F32, int BM>
+void forward(const LinearCall& c, hipStream_t stream) {
+    const int tiles_t = (c.p.tokens + BM - 1) / BM, tiles_n = (c.p.wide + BM - 1) / BM;
+    const unsigned groups = static_cast<unsigned>(tiles_t) * tiles_n * c.p.splits;
+    if (c.p.splits > 1) {
+        k_forward<F32, BM, true><<<groups, tile::threads_of(BM), 0, stream>>>(c, tiles_t, tiles_n);
+        k_forward_join<F32><<<groups_for((static_cast<int64_t>(c.p.tokens) * ((c.p.wide + 7) / 8) + 255) / 256, 4096), 256, 0,
+                              stream>>>(c);
+    } else {
+        k_forward<F32, BM, false><<<groups, tile::threads_of(BM), 0, stream>>>(c, tiles_t, tiles_n);
+    }
+}
+
+template <bool F32>
+void forward(const LinearCall& c, hipStream_t stream) {
+    // x from 0, w from 1: whichever is not read where it lies.
+    const int from = c.x_direct ? 1 : 0, to = c.w_direct ? 1 : 2;
+    if (from < to) {
+        const int rows = c.p.tokens > c.p.wide ? c.p.tokens : c.p.wide;
+        k_copies<F32><<<dim3(groups_for((rows + 3) / 4, 4096), to - from), 256, 0, stream>>>(c, from);
+    }
+    if (c.p.tile == 64)
+        forward<F32, 64>(c, stream);
+    else if (c.p.tile == 128)
+        forward<F32, 128>(c, stream);
+    else
+        forward<F32, 256>(c, stream);
+}
+
+template <bool F32>
+void few(const LinearCall& c, hipStream_t stream) {
+    const unsigned n = (c.p.wide + 15) / 16;
+    if (c.p.tokens <= 16)
+        k_few<F32, 1><<<n, kFewWaves * 64, 0, stream>>>(c);
+    else if (c.p.tokens <= 32)
+        k_few<F32, 2><<<n, kFewWaves * 64, 0, stream>>>(c);
+    else
+        k_few<F32, 4><<<n, kFewWaves * 64, 0, stream>>>(c);
+}
+
+template <bool F32, int BM>
+void backward(const LinearCall& c, hipStream_t stream) {
+    const int tiles_t = (c.p.tokens + BM - 1) / BM, tiles_n = (c.p.wide + BM - 1) / BM, tiles_d = (c.p.dim + BM - 1) / BM;
+    const int dx = c.dx ? tiles_t * tiles_d * c.p.dx_splits : 0, dw = c.dw ? tiles_n * tiles_d * c.p.dw_splits : 0;
+    const int dw_first = static_cast<int64_t>(c.p.tokens) * c.p.dx_splits > static_cast<int64_t>(c.p.wide) * c.p.dw_splits;
+    k_backward<F32, BM><<<kXcds * (per_xcd(dx) + per_xcd(dw)), tile::threads_of(BM), 0, stream>>>(c, dx, dw, dw_first);
+}
+
+template <bool F32>
+void backward(const LinearCall& c, hipStream_t stream) {
+    const int copies_rows = c.p.tokens > c.p.wide ? c.p.tokens : c.p.wide;
+    // x is wanted for dw, w for dx.
+    const int from = c.dw && !c.x_direct ? 0 : 1, to = c.dx && !c.w_direct ? 2 : 1;
+    if constexpr (F32) {
+        const int top_groups = c.dx ? static_cast<int>(groups_for((c.p.wide + 3) / 4, kLinearTopParts)) : 0;
+        const int dz_groups = static_cast<int>(c.p.pad_tokens / kDzSplitRows);
+        k_dz_split<<<top_groups + dz_groups, 256, 0, stream>>>(c, top_groups);
+        if (from < to)
+            k_back_copies<<<dim3(groups_for((copies_rows + 3) / 4, 2048), to - from), 256, 0, stream>>>(c, from, top_groups,
+                                                                                                      dz_groups);
+    } else {
+        if (!c.dz_direct || c.dbias)
+            k_dz<<<dim3((c.p.ld_wide + 511) / 512, c.p.pad_tokens / kDzRows), 256, 0, stream>>>(c);
+        if (from < to)
+            k_copies<false><<<dim3(groups_for((copies_rows + 3) / 4, 4096), to - from), 256, 0, stream>>>(c, from);
+    }
+    if (c.dx || c.dw) {
+        if (c.p.back_tile == 64)
+            backward<F32, 64>(c, stream);
+        else if (c.p.back_tile == 128)
+            backward<F32, 128>(c, stream);
+        else
+            backward<F32, 256>(c, stream);
+    }
+    const int bias_groups = c.dbias ? (c.p.wide + 63) / 64 : 0;
+    const int64_t eights = (c.p.dim + 7) / 8;
+    const int64_t join = (c.dx && c.p.dx_splits > 1 ? c.p.tokens * eights : 0) + (c.dw && c.p.dw_splits > 1 ? c.p.wide * eights : 0);
+    const unsigned groups = bias_groups + groups_for((join + 255) / 256, 4096);
+    if (groups > 0) k_backward_join<<<groups, 256, 0, stream>>>(c, bias_groups);
+}
+
+}  // namespace
+
+hipError_t launch_linear(const LinearCall& c, hipStream_t stream) {
+    if (c.p.few) {
+        if (c.p.f32)
+            few<true>(c, stream);
+        else
+            few<false>(c, stream);
+    } else if (c.p.f32) {
+        forward<true>(c, stream);
+    } else {
+        forward<false>(c, stream);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_linear_backward(const LinearCall& c, hipStream_t stream) {
+    if (c.p.tokens == 0)
+        k_no_tokens<<<groups_for(c.p.wide, 2048), 256, 0, stream>>>(c);
+    else if (c.p.f32)
+        backward<true>(c, stream);
+    else
+        backward<false>(c, stream);
+    return hipGetLastError();
+}
+
+}  // namespace dsm

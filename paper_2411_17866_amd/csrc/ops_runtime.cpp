@@ -3,54 +3,24 @@
 // launches.  The runtime owns no memory of any kind; nothing here throws.
 #include <algorithm>
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 
 #include "dsm.h"
 #include "ops_internal.h"
-#include "thread_error.h"
+#include "runtime_checks.h"
 
 namespace {
+
+using dsm::aligned;
+using dsm::bad;
+using dsm::check_device;
+using dsm::check_workspace;
+using dsm::invalid;
+using dsm::launched;
+using dsm::round_up;
 
 constexpr int64_t kMaxTokens = int64_t(1) << 20, kMaxVocab = int64_t(1) << 20, kMaxDim = 1 << 16;
 constexpr int64_t kMaxSide = int64_t(1) << 20, kMaxShort = 1 << 14;
 constexpr int kMaxSteps = dsm::kOrthoMaxSteps;
-
-dsm_status bad(dsm_status st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
-dsm_status bad(dsm_status st, const char* fmt, ...) {
-    char msg[512];
-    va_list ap;
-    va_start(ap, fmt);
-    std::vsnprintf(msg, sizeof msg, fmt, ap);
-    va_end(ap);
-    return dsm::set_thread_error(st, msg);
-}
-
-dsm_status invalid(const char* what) { return bad(DSM_ERR_INVALID_ARG, "%s", what); }
-
-bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
-
-int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
-
-dsm_status check_device() {
-    int n = 0;
-    if (hipGetDeviceCount(&n) != hipSuccess || n < 1) return bad(DSM_ERR_HIP, "no HIP device");
-    return DSM_OK;
-}
-
-dsm_status launched(const char* what, hipError_t e) {
-    if (e == hipSuccess) return DSM_OK;
-    return bad(DSM_ERR_HIP, "%s: %s (%d)", what, hipGetErrorString(e), static_cast<int>(e));
-}
-
-dsm_status check_workspace(const void* ws, int64_t bytes, int64_t need) {
-    if (!ws) return invalid("workspace is NULL");
-    if (!aligned(ws, 256)) return invalid("workspace is not 256-byte aligned");
-    if (bytes < need)
-        return bad(DSM_ERR_INVALID_ARG, "workspace_bytes %lld < %lld", static_cast<long long>(bytes),
-                   static_cast<long long>(need));
-    return DSM_OK;
-}
 
 // ---- Linear layer with softmax cross entropy ----
 

@@ -45,7 +45,9 @@ EXPORTED = ("dsm_layout", "dsm_init", "dsm_init_static", "dsm_local_step", "dsm_
             "dsm_round_end", "dsm_sync",
             "dsm_read_bounds", "dsm_test_philox", "dsm_test_stream", "dsm_destroy",
             "dsm_last_error", "dsm_ce_workspace", "dsm_linear_ce", "dsm_ortho_workspace",
-            "dsm_orthogonalize", "dsm_ortho_step")
+            "dsm_orthogonalize", "dsm_ortho_step",
+            "dsm_linear_workspace", "dsm_linear", "dsm_linear_backward", "dsm_norm_workspace", "dsm_residual_norm",
+            "dsm_residual_norm_backward", "dsm_clip_workspace", "dsm_grad_clip")
 
 DSM_F32, DSM_BF16 = 0, 1
 
@@ -118,6 +120,50 @@ class dsm_ortho_hparams(ctypes.Structure):
                 ("weight_decay", ctypes.c_float), ("nesterov", ctypes.c_int32)]
 
 
+DSM_ACT_NONE = 0
+DSM_ACT_RELU = 1
+DSM_ACT_GELU = 2
+DSM_ACT_GELU_TANH = 3
+DSM_ACT_SILU = 4
+
+DSM_NORM_NONE = 0
+DSM_NORM_LAYER = 1
+DSM_NORM_RMS = 2
+
+
+def _fields(types):
+    """[(name, ctype)] from "i64: a b; ptr: c"."""
+    kinds = {"i64": ctypes.c_int64, "i32": ctypes.c_int32, "f32": ctypes.c_float, "ptr": ctypes.c_void_p}
+    return [(name, kinds[kind.strip()]) for part in types.split(";") for kind, names in [part.split(":")]
+            for name in names.split()]
+
+
+class dsm_linear_problem(ctypes.Structure):
+    _fields_ = _fields("i64: tokens dim wide; i32: dtype act dw_dtype grads")
+
+
+class dsm_linear_buffers(ctypes.Structure):
+    _fields_ = _fields("ptr: x; i64: x_stride; ptr: w; i64: w_stride; ptr: bias residual; i64: residual_stride; "
+                       "ptr: y; i64: y_stride; ptr: z; i64: z_stride; ptr: dy; i64: dy_stride; ptr: dx; "
+                       "i64: dx_stride; ptr: dw; i64: dw_stride; ptr: dbias workspace; i64: workspace_bytes; "
+                       "ptr: stream")
+
+
+class dsm_norm_problem(ctypes.Structure):
+    _fields_ = _fields("i64: tokens dim; i32: dtype norm post grads; f32: eps post_eps scale")
+
+
+class dsm_norm_buffers(ctypes.Structure):
+    _fields_ = _fields("ptr: h; i64: h_stride; ptr: f; i64: f_stride; ptr: weight bias gate post_weight post_bias s; "
+                       "i64: s_stride; ptr: y; i64: y_stride; ptr: dy; i64: dy_stride; ptr: ds; i64: ds_stride; "
+                       "ptr: dh; i64: dh_stride; ptr: df; i64: df_stride; ptr: dweight dbias dgate dpost_weight "
+                       "dpost_bias workspace; i64: workspace_bytes; ptr: stream")
+
+
+class dsm_clip_tensor(ctypes.Structure):
+    _fields_ = _fields("ptr: data; i64: first numel block stride; i32: dtype group")
+
+
 _lib = None
 
 
@@ -160,6 +206,16 @@ def load_library(path=LIBPATH):
     lib.dsm_ortho_step.argtypes = [ctypes.POINTER(dsm_ortho_problem),
                                    ctypes.POINTER(dsm_ortho_buffers),
                                    ctypes.POINTER(dsm_ortho_hparams)]
+    lib.dsm_linear_workspace.argtypes = [ctypes.POINTER(dsm_linear_problem), c_int64_p]
+    for name in ("dsm_linear", "dsm_linear_backward"):
+        getattr(lib, name).argtypes = [ctypes.POINTER(dsm_linear_problem),
+                                       ctypes.POINTER(dsm_linear_buffers)]
+    lib.dsm_norm_workspace.argtypes = [ctypes.POINTER(dsm_norm_problem), c_int64_p]
+    for name in ("dsm_residual_norm", "dsm_residual_norm_backward"):
+        getattr(lib, name).argtypes = [ctypes.POINTER(dsm_norm_problem), ctypes.POINTER(dsm_norm_buffers)]
+    lib.dsm_clip_workspace.argtypes = [ctypes.POINTER(dsm_clip_tensor), ctypes.c_int32, ctypes.c_int32, c_int64_p]
+    lib.dsm_grad_clip.argtypes = [ctypes.POINTER(dsm_clip_tensor), ctypes.c_int32, ctypes.c_int32, ctypes.c_float,
+                                  ctypes.c_float, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]
     lib.dsm_destroy.argtypes = [ctypes.c_void_p]
     lib.dsm_last_error.argtypes = [ctypes.c_void_p]
     lib.dsm_last_error.restype = ctypes.c_char_p
@@ -315,3 +371,47 @@ def dsm_ortho_step(problem, buffers, lr, mu, scale=1.0, weight_decay=0.0, nester
     hp = dsm_ortho_hparams(lr, mu, scale, weight_decay, 1 if nesterov else 0)
     _check(load_library().dsm_ortho_step(ctypes.byref(problem), ctypes.byref(buffers),
                                          ctypes.byref(hp)))
+
+
+def _workspace(entry, problem):
+    ws = ctypes.c_int64()
+    _check(entry(ctypes.byref(problem), ctypes.byref(ws)))
+    return ws.value
+
+
+def dsm_linear_workspace(problem):
+    """Workspace of a dsm_linear_problem in bytes."""
+    return _workspace(load_library().dsm_linear_workspace, problem)
+
+
+def dsm_linear(problem, buffers):
+    _check(load_library().dsm_linear(ctypes.byref(problem), ctypes.byref(buffers)))
+
+
+def dsm_linear_backward(problem, buffers):
+    _check(load_library().dsm_linear_backward(ctypes.byref(problem), ctypes.byref(buffers)))
+
+
+def dsm_norm_workspace(problem):
+    """Workspace of a dsm_norm_problem in bytes."""
+    return _workspace(load_library().dsm_norm_workspace, problem)
+
+
+def dsm_residual_norm(problem, buffers):
+    _check(load_library().dsm_residual_norm(ctypes.byref(problem), ctypes.byref(buffers)))
+
+
+def dsm_residual_norm_backward(problem, buffers):
+    _check(load_library().dsm_residual_norm_backward(ctypes.byref(problem), ctypes.byref(buffers)))
+
+
+def dsm_clip_workspace(tensors, n_groups):
+    """Workspace in bytes; tensors: a ctypes array of dsm_clip_tensor."""
+    ws = ctypes.c_int64()
+    _check(load_library().dsm_clip_workspace(tensors, len(tensors), n_groups, ctypes.byref(ws)))
+    return ws.value
+
+
+def dsm_grad_clip(tensors, n_groups, max_norm, norm_ptr, workspace_ptr, workspace_bytes, eps=1e-6, stream_ptr=None):
+    _check(load_library().dsm_grad_clip(tensors, len(tensors), n_groups, max_norm, eps, norm_ptr, workspace_ptr,
+                                        workspace_bytes, stream_ptr))

@@ -1,5 +1,6 @@
 """Language-model operators on torch tensors: the output layer's cross entropy
-with its gradients, and orthogonalised updates.
+with its gradients, orthogonalised updates, and what a model's blocks take up to the
+gradients of a local step: the linear layer, the norms around a block, clipping.
 
 PyTorch only allocates device memory and supplies the stream; the operators run
 in libdsm.so through the binding in ``dsm``.  An object here is the plan of one
@@ -69,6 +70,23 @@ class _Plan:
         if t.shape != shape:
             raise ValueError(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
 
+    def _rows(self, name, t, shape, dtype=None):
+        """The stride of a matrix with contiguous rows."""
+        self._check(name, t, self.dtype if dtype is None else dtype, shape)
+        if shape[1] > 1 and t.stride(1) != 1:
+            raise ValueError(f"{name}'s rows must be contiguous, got strides {t.stride()}")
+        if shape[0] <= 1:
+            return shape[1]
+        if t.stride(0) < shape[1]:
+            raise ValueError(f"{name}'s rows overlap: strides {t.stride()}")
+        return t.stride(0)
+
+    def _vector(self, name, t, dtype, shape):
+        self._check(name, t, dtype, shape)
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        return t.data_ptr()
+
 
 class LinearCE(_Plan):
     """Softmax cross entropy of the logits h w^T (dsm_linear_ce).
@@ -87,22 +105,6 @@ class LinearCE(_Plan):
         self.w_shape = torch.Size((int(vocab), int(dim)))
         self.t_shape = self.h_shape[:1]
         self._allocate(dsm.dsm_ce_workspace(self.problem), device)
-
-    def _rows(self, name, t, shape):
-        self._check(name, t, self.dtype, shape)
-        if shape[1] > 1 and t.stride(1) != 1:
-            raise ValueError(f"{name}'s rows must be contiguous, got strides {t.stride()}")
-        if shape[0] <= 1:
-            return shape[1]
-        if t.stride(0) < shape[1]:
-            raise ValueError(f"{name}'s rows overlap: strides {t.stride()}")
-        return t.stride(0)
-
-    def _vector(self, name, t, dtype, shape):
-        self._check(name, t, dtype, shape)
-        if not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous")
-        return t.data_ptr()
 
     def __call__(self, h, w, target, weight=None, mean=True, dh=None, dw=None, loss=None,
                  total=None, lse=None):
@@ -256,3 +258,323 @@ class Ortho(_Plan):
         with self._enqueue() as buf.stream:
             dsm.dsm_ortho_step(problem, buf, 1.0, mu, scale, 0.0, nesterov)
         return out
+
+
+ACTS = {"none": dsm.DSM_ACT_NONE, "relu": dsm.DSM_ACT_RELU, "gelu": dsm.DSM_ACT_GELU,
+        "gelu_tanh": dsm.DSM_ACT_GELU_TANH, "silu": dsm.DSM_ACT_SILU}
+NORMS = {"none": dsm.DSM_NORM_NONE, "layer": dsm.DSM_NORM_LAYER, "rms": dsm.DSM_NORM_RMS}
+
+
+def _named(table, what, name):
+    if name not in table:
+        raise ValueError(f"{what} must be one of {', '.join(table)}, got {name!r}")
+    return table[name]
+
+
+class Linear(_Plan):
+    """A linear layer with bias, activation and residual, and its gradients (dsm_linear,
+    dsm_linear_backward).
+
+    tokens, dim, wide: the sizes of x (tokens, dim), w (wide, dim) and y (tokens, wide);
+    dtype: of all of them, torch.float32 or torch.bfloat16; act: "none", "relu", "gelu",
+    "gelu_tanh" or "silu"; grads: whether backward is called too; dw_dtype: of dw, dtype
+    or torch.float32, as the arenas keep gradients.  Biases and their gradients are fp32.
+    """
+
+    def __init__(self, tokens, dim, wide, dtype=torch.float32, act="none", grads=True, dw_dtype=None, device="cuda"):
+        super().__init__()
+        self.dtype, self.dw_dtype = dtype, dtype if dw_dtype is None else dw_dtype
+        self.act, self.grads = act, bool(grads)
+        self.problem = dsm.dsm_linear_problem(int(tokens), int(dim), int(wide), _dtype(dtype), _named(ACTS, "act", act),
+                                              _dtype(self.dw_dtype), 1 if grads else 0)
+        self.x_shape = torch.Size((int(tokens), int(dim)))
+        self.w_shape = torch.Size((int(wide), int(dim)))
+        self.y_shape = torch.Size((int(tokens), int(wide)))
+        self.bias_shape = self.w_shape[:1]
+        self._allocate(dsm.dsm_linear_workspace(self.problem), device)
+
+    def _operands(self, x, w):
+        buf = dsm.dsm_linear_buffers()
+        if x is not None:
+            buf.x_stride, buf.x = self._rows("x", x, self.x_shape), x.data_ptr()
+        if w is not None:
+            buf.w_stride, buf.w = self._rows("w", w, self.w_shape), w.data_ptr()
+        buf.workspace, buf.workspace_bytes = self.workspace.data_ptr(), self.workspace_bytes
+        return buf
+
+    def _empty(self, shape, dtype=None):
+        return torch.empty(shape, dtype=self.dtype if dtype is None else dtype, device=self.device)
+
+    def __call__(self, x, w, bias=None, residual=None, y=None, z=None):
+        """{"y"}: act(x w^T + bias) + residual; and, for a plan with gradients and an
+        activation or where z is given, {"z"}: x w^T + bias, which backward takes.  Outputs
+        are written into the tensors given (y may be the residual), or into new ones."""
+        buf = self._operands(x, w)
+        if bias is not None:
+            buf.bias = self._vector("bias", bias, torch.float32, self.bias_shape)
+        if residual is not None:
+            buf.residual_stride, buf.residual = self._rows("residual", residual, self.y_shape), residual.data_ptr()
+        if y is None:
+            y = self._empty(self.y_shape)
+        if z is None and self.grads and self.act != "none":
+            z = self._empty(self.y_shape)
+        buf.y_stride, buf.y = self._rows("y", y, self.y_shape), y.data_ptr()
+        out = {"y": y}
+        if z is not None:
+            buf.z_stride, buf.z = self._rows("z", z, self.y_shape), z.data_ptr()
+            out["z"] = z
+        with self._enqueue() as buf.stream:
+            dsm.dsm_linear(self.problem, buf)
+        return out
+
+    def backward(self, dy, x=None, w=None, z=None, dx=None, dw=None, dbias=None, wanted=("dx", "dw", "dbias")):
+        """The gradients named in `wanted`, {"dx", "dw", "dbias"}, from y's gradient dy and
+        what the forward pass had: x (for dw), w (for dx), and z unless there is no
+        activation.  (The residual's gradient is dy.)  Outputs are written into the tensors
+        given, or into new ones."""
+        if not self.grads:
+            raise ValueError("the plan is without gradients")
+        for name, t in (("dx", dx), ("dw", dw), ("dbias", dbias)):
+            if t is not None and name not in wanted:
+                raise ValueError(f"{name} is given but not wanted")
+        for name in wanted:
+            if name not in ("dx", "dw", "dbias"):
+                raise ValueError(f"wanted holds {name!r}")
+        for name, t, needed in (("x", x, "dw" in wanted), ("w", w, "dx" in wanted), ("z", z, self.act != "none")):
+            if t is None and needed:
+                raise ValueError(f"{name} is wanted for these gradients")
+        buf = self._operands(x, w)
+        buf.dy_stride, buf.dy = self._rows("dy", dy, self.y_shape), dy.data_ptr()
+        if self.act != "none":
+            buf.z_stride, buf.z = self._rows("z", z, self.y_shape), z.data_ptr()
+        out = {}
+        if "dx" in wanted:
+            out["dx"] = dx = self._empty(self.x_shape) if dx is None else dx
+            buf.dx_stride, buf.dx = self._rows("dx", dx, self.x_shape), dx.data_ptr()
+        if "dw" in wanted:
+            out["dw"] = dw = self._empty(self.w_shape, self.dw_dtype) if dw is None else dw
+            buf.dw_stride, buf.dw = self._rows("dw", dw, self.w_shape, self.dw_dtype), dw.data_ptr()
+        if "dbias" in wanted:
+            out["dbias"] = dbias = self._empty(self.bias_shape, torch.float32) if dbias is None else dbias
+            buf.dbias = self._vector("dbias", dbias, torch.float32, self.bias_shape)
+        with self._enqueue() as buf.stream:
+            dsm.dsm_linear_backward(self.problem, buf)
+        return out
+
+
+class ResidualNorm(_Plan):
+    """The norms before and after a block, fused with its gate and residual scale, and
+    their gradients (dsm_residual_norm, dsm_residual_norm_backward):
+
+        p = post(f);  s = h + scale gate p;  y = norm(s)
+
+    tokens, dim, dtype: of the rows h, f, s, y and their gradients; norm, post: "layer",
+    "rms" or "none"; eps, post_eps (eps where None): of them; grads: whether backward is
+    called too.  Vectors and their gradients are fp32.
+    """
+
+    VECTORS = ("weight", "bias", "gate", "post_weight", "post_bias")
+
+    def __init__(self, tokens, dim, dtype=torch.float32, norm="layer", post="none", eps=1e-5, post_eps=None, grads=True,
+                 device="cuda"):
+        super().__init__()
+        self.dtype, self.norm, self.post, self.grads = dtype, norm, post, bool(grads)
+        self.shape = torch.Size((int(tokens), int(dim)))
+        self._args = (int(tokens), int(dim), _dtype(dtype), _named(NORMS, "norm", norm), _named(NORMS, "post", post),
+                      1 if grads else 0, float(eps), float(eps if post_eps is None else post_eps))
+        self._allocate(dsm.dsm_norm_workspace(self._problem(1.0)), device)
+
+    def _problem(self, scale):
+        return dsm.dsm_norm_problem(*self._args, float(scale))
+
+    def _fill(self, buf, rows, vectors):
+        for name, t in rows:
+            if t is not None:
+                setattr(buf, name + "_stride", self._rows(name, t, self.shape))
+                setattr(buf, name, t.data_ptr())
+        for name, t in vectors:
+            if t is not None:
+                setattr(buf, name, self._vector(name, t, torch.float32, self.shape[1:]))
+        buf.workspace, buf.workspace_bytes = self.workspace.data_ptr(), self.workspace_bytes
+        return buf
+
+    def _vectors(self, given):
+        for name, t in given:
+            if t is None:
+                continue
+            if name in ("weight", "bias") and self.norm == "none":
+                raise ValueError(f"{name} is given without a norm")
+            if name in ("post_weight", "post_bias") and self.post == "none":
+                raise ValueError(f"{name} is given without a post norm")
+
+    def __call__(self, h, f=None, weight=None, bias=None, gate=None, scale=1.0, post_weight=None, post_bias=None, s=None,
+                 y=None):
+        """{"s", "y"}: s where there is f, y where there is a norm; written into the tensors
+        given (s may be h or f, y h or f), or into new ones.  Absent weights and gate are 1, absent
+        biases 0."""
+        vectors = [("weight", weight), ("bias", bias), ("gate", gate), ("post_weight", post_weight),
+                   ("post_bias", post_bias)]
+        self._vectors(vectors)
+        if f is None and (self.post != "none" or gate is not None or s is not None):
+            raise ValueError("f is None: there is no block's output for post, gate or s")
+        if y is not None and self.norm == "none":
+            raise ValueError("y is given without a norm")
+        out = {}
+        if f is not None:
+            out["s"] = s = torch.empty(self.shape, dtype=self.dtype, device=self.device) if s is None else s
+        if self.norm != "none":
+            out["y"] = y = torch.empty(self.shape, dtype=self.dtype, device=self.device) if y is None else y
+        buf = self._fill(dsm.dsm_norm_buffers(), [("h", h), ("f", f), ("s", s), ("y", y)], vectors)
+        with self._enqueue() as buf.stream:
+            dsm.dsm_residual_norm(self._problem(scale), buf)
+        return out
+
+    def backward(self, dy, s, f=None, ds=None, weight=None, bias=None, gate=None, scale=1.0, post_weight=None,
+                 post_bias=None, dh=None, df=None, dweight=None, dbias=None, dgate=None, dpost_weight=None,
+                 dpost_bias=None):
+        """The gradients of what the forward pass was given: {"dh"}, {"df"} where there is f,
+        and those of the vectors given.  dy: y's gradient (None without a norm); s: the
+        forward pass's s, or h where there was no f; ds: the gradient that s has from
+        elsewhere, or None.  Outputs are written into the tensors given (dh may be dy or ds,
+        df dy, ds or f), or into new ones."""
+        if not self.grads:
+            raise ValueError("the plan is without gradients")
+        vectors = [("weight", weight), ("bias", bias), ("gate", gate), ("post_weight", post_weight),
+                   ("post_bias", post_bias)]
+        self._vectors(vectors)
+        if f is None and (self.post != "none" or gate is not None or df is not None):
+            raise ValueError("f is None: there is no block's output for post, gate or df")
+        if (dy is None) != (self.norm == "none"):
+            raise ValueError("dy is wanted where there is a norm, and only there")
+        if dy is None and ds is None:
+            raise ValueError("ds is wanted where there is no norm")
+
+        def new():
+            return torch.empty(self.shape, dtype=self.dtype, device=self.device)
+
+        out = {"dh": new() if dh is None else dh}
+        if f is not None:
+            out["df"] = new() if df is None else df
+        grads = {"weight": dweight, "bias": dbias, "gate": dgate, "post_weight": dpost_weight, "post_bias": dpost_bias}
+        for name, t in vectors:
+            if t is not None:
+                given = grads[name]
+                out["d" + name] = torch.empty_like(t) if given is None else given
+            elif grads[name] is not None:
+                raise ValueError(f"d{name} is given without {name}")
+        rows = [("h", s), ("f", f), ("dy", dy), ("ds", ds), ("dh", out["dh"]), ("df", out.get("df"))]
+        if self.norm == "none":
+            rows = [r for r in rows if r[0] != "h"]
+        buf = self._fill(dsm.dsm_norm_buffers(), rows, vectors + [("d" + n, out.get("d" + n)) for n in self.VECTORS])
+        with self._enqueue() as buf.stream:
+            dsm.dsm_residual_norm_backward(self._problem(scale), buf)
+        return out
+
+
+class _Clip(_Plan):
+    def __init__(self):
+        super().__init__()
+        self._table_lock = threading.Lock()
+
+    def _table(self, sizes, groups, n_groups, eps, device):
+        """sizes: [(numel, dtype)]; the tensors' table, whose addresses each call fills."""
+        self._entries = (dsm.dsm_clip_tensor * len(sizes))()
+        for e, (numel, dtype), group in zip(self._entries, sizes, groups):
+            e.numel, e.block, e.stride, e.dtype, e.group = numel, max(numel, 1), max(numel, 1), _dtype(dtype), group
+        self.n_groups, self.eps = int(n_groups), float(eps)
+        self._allocate(dsm.dsm_clip_workspace(self._entries, self.n_groups), device)
+
+    def _norm(self, norm):
+        if norm is None:
+            return torch.empty(self.n_groups, dtype=torch.float32, device=self.device)
+        self._vector("norm", norm, torch.float32, torch.Size((self.n_groups,)))
+        return norm
+
+    def _run(self, max_norm, norm):
+        with self._enqueue() as stream:
+            dsm.dsm_grad_clip(self._entries, self.n_groups, float("inf") if max_norm is None else float(max_norm),
+                              norm.data_ptr(), self.workspace.data_ptr(), self.workspace_bytes, self.eps, stream)
+        return norm
+
+
+class GradClip(_Clip):
+    """Clipping of gradients by the global norm of a list of tensors, or of each group of
+    them (dsm_grad_clip).
+
+    tensors: tensors (or anything with their shape and dtype) of the sizes that calls
+    take; groups: the group of each, 0 .. n - 1 (None: one group); eps: added to the norm.
+    """
+
+    def __init__(self, tensors, groups=None, eps=1e-6, device="cuda"):
+        super().__init__()
+        tensors = list(tensors)
+        groups = [0] * len(tensors) if groups is None else [int(g) for g in groups]
+        if len(groups) != len(tensors):
+            raise ValueError(f"{len(groups)} groups for {len(tensors)} tensors")
+        if any(g < 0 for g in groups):
+            raise ValueError("a group is negative")
+        self._like = [(t.shape, t.dtype) for t in tensors]
+        # Groups in order: the order of a call's tensors is the caller's.
+        self._order = sorted(range(len(tensors)), key=groups.__getitem__)
+        self._table([(self._like[i][0].numel(), self._like[i][1]) for i in self._order], [groups[i] for i in self._order],
+                    max(groups, default=0) + 1, eps, device)
+
+    def __call__(self, tensors, max_norm=None, norm=None):
+        """norm (n_groups,): the groups' norms, before clipping.  Where one exceeds max_norm its
+        tensors are scaled to it in place (None: norms alone).  Tensors have contiguous elements,
+        or are matrices with contiguous rows.  They may not overlap."""
+        if len(tensors) != len(self._like):
+            raise ValueError(f"{len(tensors)} tensors for a plan of {len(self._like)}")
+        norm = self._norm(norm)
+        places = []
+        for i, e in zip(self._order, self._entries):
+            t, (shape, dtype) = tensors[i], self._like[i]
+            if t.shape != shape or t.dtype != dtype or t.device != self.device:
+                raise ValueError(f"tensors[{i}] must be {dtype} of shape {tuple(shape)} on {self.device}, "
+                                 f"got {t.dtype}, {tuple(t.shape)}, {t.device}")
+            if t.is_contiguous():
+                block = stride = max(t.numel(), 1)
+            elif t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1) and t.stride(0) >= t.shape[1]:
+                block, stride = t.shape[1], t.stride(0)
+            else:
+                raise ValueError(f"tensors[{i}] has neither contiguous elements nor contiguous rows: strides {t.stride()}")
+            places.append((t.data_ptr(), block, stride))
+        with self._table_lock:
+            for e, place in zip(self._entries, places):
+                e.data, e.block, e.stride = place
+            return self._run(max_norm, norm)
+
+
+class ArenaClip(_Clip):
+    """Clipping of the workers' gradients in an ``arena.Arenas`` by the global norm of each
+    worker's tensors, or of all workers' together; padding between tensors does not count."""
+
+    def __init__(self, arenas, together=False, eps=1e-6):
+        super().__init__()
+        self._n, self._numel = arenas.n, list(arenas.numel)
+        self._offsets = [int(o) for o in arenas.offsets]
+        self._layout = (arenas.replica_layout, arenas.n_state_buffers, arenas.arena_elems)
+        count = len(self._numel)
+        self._table([(n, torch.float32) for n in self._numel] * self._n,
+                    [0 if together else i for i in range(self._n) for _ in range(count)], 1 if together else self._n, eps,
+                    arenas.x.device)
+
+    def __call__(self, arenas, max_norm=None, norm=None):
+        """norm: (n_workers,), or (1,) together; as GradClip's."""
+        if (arenas.n, list(arenas.numel), (arenas.replica_layout, arenas.n_state_buffers, arenas.arena_elems)) != (
+                self._n, self._numel, self._layout):
+            raise ValueError("the plan is for arenas of another problem")
+        norm = self._norm(norm)
+        if arenas.g_rep.device != self.device:
+            raise ValueError(f"the arenas are on {arenas.g_rep.device}, the plan on {self.device}")
+        layout, buffers, elems = self._layout
+        with self._table_lock:
+            for k, e in enumerate(self._entries):
+                worker, tensor = divmod(k, len(self._numel))
+                e.first, e.block, e.stride = self._offsets[tensor], max(elems, 1), max(elems, 1)
+                e.data = arenas.g_rep.data_ptr() + 4 * worker * elems
+                if layout == dsm.DSM_REPLICAS_STATE_BLOCKED:
+                    e.block = dsm.DSM_STATE_BLOCK_ELEMS
+                    e.stride = buffers * self._n * e.block
+                    e.data = arenas.g_rep.data_ptr() + 4 * worker * e.block
+            return self._run(max_norm, norm)
