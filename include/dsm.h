@@ -688,8 +688,8 @@ DSM_API dsm_status dsm_clip_workspace(const dsm_clip_tensor* tensors, int32_t n_
 /*
  * dsm_grad_clip - for every group, norm = the 2-norm of all its tensors' elements and
  *   g <- g min(1, max_norm / (norm + eps))
- * in place.  Squares and sums are fp64, the factor is rounded to fp32, the product to
- * the tensor's type.  norm[group] is written; a group without elements has norm 0.
+ * in place.  Squares, sums, the factor and products are fp64, rounded once to the tensor's
+ * type.  norm[group] is written; a group without elements has norm 0.
  * Gradients whose norm is NaN or infinite in fp64 stay as they are, and so do those
  * that need no clipping.  max_norm = infinity: norms alone.  Tensors must not overlap.
  * n_groups in [1, 256]; max_norm >= 0; eps >= 0, finite; 1e-6 is customary.

@@ -39,8 +39,8 @@ using ClipGroups = ClipStarts<int64_t, kClipGroups>;
 using ClipFew = ClipStarts<int32_t, kClipFewGroups>;
 
 hipError_t launch_clip_squares(const ClipTable& t, double* parts, hipStream_t stream);
-hipError_t launch_clip_norms(const ClipGroups& g, const double* parts, float* norm, float* factor, hipStream_t stream);
-hipError_t launch_clip_scale(const ClipTable& t, const float* factor, hipStream_t stream);
+hipError_t launch_clip_norms(const ClipGroups& g, const double* parts, float* norm, double* factor, hipStream_t stream);
+hipError_t launch_clip_scale(const ClipTable& t, const double* factor, hipStream_t stream);
 // The last two in one, where every work-group sums its group's parts itself.
 hipError_t launch_clip_rest(const ClipTable& t, const ClipFew& g, const double* parts, float* norm, hipStream_t stream);
 

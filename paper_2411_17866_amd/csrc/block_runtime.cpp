@@ -248,7 +248,7 @@ dsm_status check_clip(const dsm_clip_tensor* t, int32_t n, int32_t groups, int64
     return DSM_OK;
 }
 
-int64_t clip_bytes(int64_t chunks) { return round_up(chunks * 8, 256) + dsm::kClipGroups * 4; }
+int64_t clip_bytes(int64_t chunks) { return round_up(chunks * 8, 256) + dsm::kClipGroups * 8; }
 
 bool contiguous(const dsm::ClipEntry& e) { return e.block >= e.first + e.numel; }
 
@@ -490,7 +490,7 @@ dsm_status dsm_grad_clip(const dsm_clip_tensor* tensors, int32_t n_tensors, int3
     if (dsm_status st = check_device()) return st;
     const auto s = static_cast<hipStream_t>(stream);
     double* parts = static_cast<double*>(workspace);
-    float* factor = reinterpret_cast<float*>(static_cast<char*>(workspace) + round_up(chunks * 8, 256));
+    double* factor = reinterpret_cast<double*>(static_cast<char*>(workspace) + round_up(chunks * 8, 256));
     dsm::ClipGroups groups;
     groups.count = n_groups;
     groups.max_norm = max_norm;

@@ -111,13 +111,15 @@ __device__ __forceinline__ double group_norm(const Groups& g, int group, const d
     return sqrt(group_sum(s));
 }
 // Gradients whose norm is not a finite number stay as they are: no factor mends them.
+// (In fp64, as the products: a norm near fp32's largest number has a factor below its
+// smallest.)
 template <class Groups>
-__device__ __forceinline__ float factor_of(const Groups& g, double norm) {
-    if (!(norm < __builtin_inf())) return 1.f;
-    return static_cast<float>(fmin(1.0, static_cast<double>(g.max_norm) / (norm + static_cast<double>(g.eps))));
+__device__ __forceinline__ double factor_of(const Groups& g, double norm) {
+    if (!(norm < __builtin_inf())) return 1.0;
+    return fmin(1.0, static_cast<double>(g.max_norm) / (norm + static_cast<double>(g.eps)));
 }
 
-__global__ __launch_bounds__(1024) void k_clip_norms(ClipGroups g, const double* parts, float* norm, float* factor) {
+__global__ __launch_bounds__(1024) void k_clip_norms(ClipGroups g, const double* parts, float* norm, double* factor) {
     const double v = group_norm(g, blockIdx.x, parts);
     if (threadIdx.x != 0) return;
     norm[blockIdx.x] = static_cast<float>(v);
@@ -125,23 +127,23 @@ __global__ __launch_bounds__(1024) void k_clip_norms(ClipGroups g, const double*
 }
 
 template <bool F32>
-__device__ __forceinline__ void scale(const Chunk& k, float by) {
+__device__ __forceinline__ void scale(const Chunk& k, double by) {
     each_run(k, [&](int64_t at, int have) {
         V8 x = rows::load8<F32>(k.e.data, at, have);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) x.v[q] *= by;
+        for (int q = 0; q < 8; ++q) x.v[q] = static_cast<float>(x.v[q] * by);
         rows::store8<F32>(k.e.data, at, x, have);
     });
 }
-__device__ __forceinline__ void scale(const Chunk& k, float by) {
-    if (by == 1.f) return;
+__device__ __forceinline__ void scale(const Chunk& k, double by) {
+    if (by == 1.0) return;
     if (k.e.bf16)
         scale<false>(k, by);
     else
         scale<true>(k, by);
 }
 
-__global__ __launch_bounds__(256) void k_clip_scale(ClipTable t, const float* factor) {
+__global__ __launch_bounds__(256) void k_clip_scale(ClipTable t, const double* factor) {
     const Chunk k = chunk_of(t, t.chunks - 1 - blockIdx.x);
     scale(k, factor[k.e.group]);
 }
@@ -165,12 +167,12 @@ hipError_t launch_clip_squares(const ClipTable& t, double* parts, hipStream_t st
     return hipGetLastError();
 }
 
-hipError_t launch_clip_norms(const ClipGroups& g, const double* parts, float* norm, float* factor, hipStream_t stream) {
+hipError_t launch_clip_norms(const ClipGroups& g, const double* parts, float* norm, double* factor, hipStream_t stream) {
     k_clip_norms<<<g.count, 1024, 0, stream>>>(g, parts, norm, factor);
     return hipGetLastError();
 }
 
-hipError_t launch_clip_scale(const ClipTable& t, const float* factor, hipStream_t stream) {
+hipError_t launch_clip_scale(const ClipTable& t, const double* factor, hipStream_t stream) {
     k_clip_scale<<<t.chunks, 256, 0, stream>>>(t, factor);
     return hipGetLastError();
 }
