@@ -81,6 +81,7 @@ struct LinearPlan {
     int32_t f32, dw_f32;
     int32_t few;                 // forward: no tiles
     int32_t tile, splits;        // forward: tile, and parts that its sums run over side by side
+    int32_t front;               // tile columns of 256; tiles of 128 take what follows
     int32_t back_tile, dx_splits, dw_splits;
     int32_t bias_parts;          // rows of sums that dbias is joined from
     int64_t ld_dim, ld_wide;     // 16-bit elements of a row of x's and w's copies, of dz

@@ -28,18 +28,25 @@ bool known_dtype(int32_t dtype) { return dtype == DSM_F32 || dtype == DSM_BF16; 
 
 int64_t tiles(int64_t n, int64_t of) { return (n + of - 1) / of; }
 
-// A turn of the CUs over tiles of 64, 128 (two on a CU) and 256 (one): microseconds of
-// a step of 64 of k, bf16.
+// How products are cut is decided by estimated microseconds, of a turn of the CUs over
+// tiles of 64 and 128 (two on a CU) and of 256 (one).  Measured over 14 shapes from 64 x 1600 x 6400
+// to 8192 x 1600 x 6400 and every combination of tile and parts, the rules' choices take the least time
+// or within 5% of it (fp32 4096 x 1600 x 6400).
 constexpr int kTiles[3] = {64, 128, 256};
-constexpr double kStep[3] = {0.70, 1.09, 1.75};
 constexpr double kSlots[3] = {512, 512, 256};
 constexpr int kMaxSplits = 16;
 
-// What joining `parts` parts of n numbers moves, at 4 TB/s, and a launch.
-double join_time(int parts, int64_t n) { return parts > 1 ? 4.0 + 4e-6 * static_cast<double>(n) * (2 * parts) / 4.0 : 0.0; }
-
-// fp32 takes three matrix instructions for one.
-double step_of(int i, bool f32) { return kStep[i] * (f32 ? 2.6 : 1.0); }
+// A step of 64 of k for a turn that fills the CUs and for tiles that have one each, and what a turn takes
+// besides: forward (bf16; both operands k-contiguous), and the gradients' products.
+struct Turn {
+    double full[3], alone[3], end[3], f32;
+};
+constexpr Turn kForward = {{0.43, 0.97, 1.45}, {0.28, 0.55, 1.45}, {2.2, 5.0, 8.0}, 2.0};
+constexpr Turn kBackward = {{0.50, 1.04, 1.66}, {0.58, 0.88, 1.26}, {3.0, 5.0, 10.0}, 2.42};
+// Joining `parts` parts of n numbers: a launch, and what is moved.
+double join_time(int parts, int64_t n, double each) {
+    return parts > 1 ? 4.4 + each * 2e-6 * static_cast<double>(n * parts) : 0.0;
+}
 
 // Tile columns: the last of 256 takes half as long where 128 columns of it lie past the end.
 double columns(int64_t n, int of) {
@@ -47,36 +54,78 @@ double columns(int64_t n, int of) {
     return static_cast<double>(all) - (of == 256 && n <= (all - 1) * 256 + 128 ? 0.45 : 0.0);
 }
 
+// Forward: tiles, parts of k, and for tiles of 256 without parts how many of its columns
+// they take (a tile of 128 that follows them has a CU for itself).  8192 x 1600 x 6400 in bf16: 159 us
+// by 24 columns of 256 and 128 tiles of 128; 176 by 256 or 128 alone.
 void cut_forward(dsm::LinearPlan* q) {
     const int64_t T = q->tokens, D = q->dim, N = q->wide, steps = tiles(D, 64);
+    const double f32 = q->f32 ? kForward.f32 : 1.0;
     double best = 0.0;
+    const auto take = [&](double cost, int tile, int splits, int64_t front) {
+        if (best != 0.0 && cost >= best) return;
+        best = cost;
+        q->tile = tile;
+        q->splits = splits;
+        q->front = static_cast<int32_t>(front);
+    };
+    // Turns of n tiles of `i`, the last of which may leave CUs half filled.
+    const auto turns = [&](int64_t n, int i, int64_t k) {
+        const int64_t slots = static_cast<int64_t>(kSlots[i]), whole = n / slots, rest = n % slots;
+        const double full = static_cast<double>(k) * kForward.full[i] * f32 + kForward.end[i];
+        const double last = rest == 0 ? 0.0 : rest <= 256 ? static_cast<double>(k) * kForward.alone[i] * f32 + kForward.end[i] : full;
+        return static_cast<double>(whole) * full + last;
+    };
     for (int i = 0; i < 3; ++i) {
-        const int64_t all = tiles(T, kTiles[i]) * tiles(N, kTiles[i]);
+        const int64_t rows = tiles(T, kTiles[i]), all = tiles(N, kTiles[i]);
         for (int s = 1; s <= kMaxSplits && (s == 1 || s * 4 <= steps); ++s) {
-            const double turns = std::ceil(static_cast<double>(all * s) / kSlots[i]);
-            const double cost = turns * (static_cast<double>(tiles(steps, s)) * step_of(i, q->f32) + 4.0) + join_time(s, T * N);
-            if (best == 0.0 || cost < best) {
-                best = cost;
-                q->tile = kTiles[i];
-                q->splits = s;
+            take(turns(rows * all * s, i, tiles(steps, s)) + join_time(s, T * N, 1.0), kTiles[i], s, all);
+            if (kTiles[i] != 256 || s > 1) continue;
+            const double turn = turns(1, 2, steps), alone = turns(1, 1, steps);
+            for (int64_t front = all - 1; front >= std::max<int64_t>(all - 32, 1); --front) {
+                // CUs that the last turn of 256 leaves idle take the first of the others.
+                const int64_t last = rows * front % 256, idle = last > 0 ? 256 - last : 0;
+                const int64_t rest = tiles(T, 128) * tiles(N - front * 256, 128) - idle * static_cast<int64_t>(turn / alone);
+                take(turns(rows * front, 2, steps) + static_cast<double>(tiles(std::max<int64_t>(rest, 0), 256)) * alone, 256, 1, front);
             }
         }
     }
 }
 
+// Few tokens: parts of k, where few rows of w leave CUs idle.  A work-group reads its rows of
+// w and x at some 75 GB/s, and joining the parts takes a launch.  One token of 6400 -> 256 in fp32: 15.2 us
+// in one part, 8.7 in 4; 24 tokens of 6400 -> 1600 in bf16: 9.6, and 9.4 in 2.
+int few_splits(const dsm::LinearPlan& q) {
+    const int64_t groups = tiles(q.wide, 16), size = q.f32 ? 4 : 2, rows = 16 + round_up(q.tokens, 16);
+    const double whole = static_cast<double>(q.dim * size * rows) / 75e3;
+    int best = 1;
+    double least = whole - 1.5;
+    for (int s = 2; s <= kMaxSplits && groups * s <= 256 && s * 1024 <= q.dim * size; ++s) {
+        const double cost = whole / s + 3.4 + 0.5 * s;
+        if (cost < least) {
+            least = cost;
+            best = s;
+        }
+    }
+    return best;
+}
+
+// The gradients: dx and dw run side by side.  The work over the CUs, and a part of the longest tile
+// for the uneven end.
 void cut_backward(dsm::LinearPlan* q) {
     const int64_t T = q->tokens, D = q->dim, N = q->wide;
+    const double f32 = q->f32 ? kBackward.f32 : 1.0;
     double best = 0.0;
     for (int i = 0; i < 3; ++i) {
         const int of = kTiles[i];
         const double dx = static_cast<double>(tiles(T, of)) * columns(D, of), dw = static_cast<double>(tiles(N, of)) * columns(D, of);
+        const auto time = [&](int64_t k, const double* step) { return static_cast<double>(k) * step[i] * f32 + kBackward.end[i]; };
         for (int sx = 1; sx <= kMaxSplits && (sx == 1 || sx * 256 <= N); ++sx)
             for (int sw = 1; sw <= kMaxSplits && (sw == 1 || sw * 256 <= T); ++sw) {
-                const double tx = static_cast<double>(tiles(tiles(N, 64), sx)) * step_of(i, q->f32) + 4.0;
-                const double tw = static_cast<double>(tiles(tiles(T, 64), sw)) * step_of(i, q->f32) + 4.0;
-                // The work over the CUs, and half a tile for the uneven end.
-                const double work = (dx * sx * tx + dw * sw * tw) / kSlots[i], longest = std::max(tx, tw);
-                const double cost = std::max(work + 0.3 * longest, longest) + join_time(sx, T * D) + join_time(sw, N * D);
+                const int64_t kx = tiles(tiles(N, 64), sx), kw = tiles(tiles(T, 64), sw);
+                const double work = (dx * sx * time(kx, kBackward.full) + dw * sw * time(kw, kBackward.full)) / kSlots[i];
+                const double longest = time(std::max(kx, kw), kBackward.alone);
+                const double joins = join_time(sx, T * D, 0.25) + join_time(sw, N * D, 0.25) - (sx > 1 && sw > 1 ? 4.4 : 0.0);
+                const double cost = std::max(work + 0.40 * longest, longest) + joins;
                 if (best == 0.0 || cost < best) {
                     best = cost;
                     q->back_tile = of;
@@ -127,11 +176,12 @@ dsm::LinearPlan plan_linear(const dsm_linear_problem* p) {
     q.x_exp = take(T * 4);
     q.w_exp = take(N * 4);
     const int64_t common = at;
-    if (!q.few) {
+    if (q.few)
+        q.splits = few_splits(q);
+    else
         cut_forward(&q);
-        q.y_parts = take(q.splits > 1 ? q.splits * T * q.ld_y * 4 : 0);
-        q.forward_bytes = at;
-    }
+    q.y_parts = take(q.splits > 1 ? q.splits * T * q.ld_y * 4 : 0);
+    q.forward_bytes = q.few && q.splits == 1 ? 0 : at;
     if (!p->grads || T == 0) return q;
     at = common;
     cut_backward(&q);

@@ -27,39 +27,61 @@ struct V8 {
     float v[8];
 };
 
+// Eight elements as they lie in memory.
+template <bool F32>
+struct Raw8 {
+    u16x8 v;
+};
+template <>
+struct Raw8<true> {
+    f4 a, b;
+};
+
 // Eight elements from element `at` on, of which `have` exist (the others are 0).
 template <bool F32>
-__device__ __forceinline__ V8 load8(const void* base, int64_t at, int have) {
-    V8 o;
-#pragma unroll
-    for (int q = 0; q < 8; ++q) o.v[q] = 0.f;
+__device__ __forceinline__ Raw8<F32> raw8(const void* base, int64_t at, int have) {
+    Raw8<F32> o;
     if constexpr (F32) {
         const float* p = static_cast<const float*>(base) + at;
+        o.a = o.b = f4{0.f, 0.f, 0.f, 0.f};
         if (have >= 8) {
-            const f4 a = *reinterpret_cast<const f4_at*>(p), b = *reinterpret_cast<const f4_at*>(p + 4);
+            o.a = *reinterpret_cast<const f4_at*>(p);
+            o.b = *reinterpret_cast<const f4_at*>(p + 4);
+        } else {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                o.v[q] = a[q];
-                o.v[4 + q] = b[q];
+                if (q < have) o.a[q] = p[q];
+                if (q < 3 && 4 + q < have) o.b[q] = p[4 + q];
             }
+        }
+    } else {
+        const u16* p = static_cast<const u16*>(base) + at;
+        o.v = u16x8{0, 0, 0, 0, 0, 0, 0, 0};
+        if (have >= 8) {
+            o.v = *reinterpret_cast<const u16x8_at*>(p);
         } else {
 #pragma unroll
             for (int q = 0; q < 7; ++q)
                 if (q < have) o.v[q] = p[q];
         }
-    } else {
-        const u16* p = static_cast<const u16*>(base) + at;
-        if (have >= 8) {
-            const u16x8 a = *reinterpret_cast<const u16x8_at*>(p);
-#pragma unroll
-            for (int q = 0; q < 8; ++q) o.v[q] = bf16_to_float(a[q]);
-        } else {
-#pragma unroll
-            for (int q = 0; q < 7; ++q)
-                if (q < have) o.v[q] = bf16_to_float(p[q]);
-        }
     }
     return o;
+}
+template <bool F32>
+__device__ __forceinline__ V8 wide8(const Raw8<F32>& x) {
+    V8 o;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        if constexpr (F32)
+            o.v[q] = q < 4 ? x.a[q & 3] : x.b[q & 3];
+        else
+            o.v[q] = bf16_to_float(x.v[q]);
+    }
+    return o;
+}
+template <bool F32>
+__device__ __forceinline__ V8 load8(const void* base, int64_t at, int have) {
+    return wide8(raw8<F32>(base, at, have));
 }
 
 template <bool F32>

@@ -46,55 +46,105 @@ using tile::Operand;
 constexpr int kNoExponent = 10000;  // of a row of zeros: brings everything to 0
 
 // ---- Activations ----
+//
+// FAST, for results that are rounded to bf16: the hardware's exp2 and reciprocal
+// (2^-22).  The epilogue's arithmetic does not overlap the next tile's products, so
+// every instruction of it counts.
 
-// 1 / (1 + exp(-v)) and one minus that, each to its own digits.  FAST, for results that
-// are rounded to bf16: the hardware's exp2 and reciprocal (2^-22).
-template <bool FAST>
-__device__ __forceinline__ void logistic(float v, float* share, float* rest) {
-    const float a = fabsf(v);
-    float e, one;
-    if constexpr (FAST) {
-        e = __builtin_amdgcn_exp2f(a * -1.44269504088896341f);
-        one = __builtin_amdgcn_rcpf(1.0f + e);
-    } else {
-        e = expf(-a);
-        one = 1.0f / (1.0f + e);
-    }
-    const float less = e * one;
-    *share = v < 0.f ? less : one;
-    *rest = v < 0.f ? one : less;
-}
-
-constexpr float kTanhA = 1.59576912160573071f;  // 2 sqrt(2 / pi): tanh(u) = 2 logistic(2 u) - 1
+constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kTanhA = 1.59576912160573071f;  // 2 sqrt(2 / pi): (1 + tanh(u)) / 2 = logistic(2 u)
 constexpr float kTanhB = 0.044715f;
 
 template <bool FAST>
-__device__ __forceinline__ float activation(int act, float z) {
-    if (act == DSM_ACT_RELU) return z < 0.f ? 0.f : z;
-    if (act == DSM_ACT_GELU) return 0.5f * z * erfcf(z * -0.707106781186547524f);
-    if (act == DSM_ACT_NONE) return z;
-    float share, rest;
-    logistic<FAST>(act == DSM_ACT_SILU ? z : kTanhA * (z + kTanhB * (z * z * z)), &share, &rest);
-    return z * share;
+__device__ __forceinline__ float one_over(float v) {
+    return FAST ? __builtin_amdgcn_rcpf(v) : 1.0f / v;
+}
+// exp(-v), of the logistic 1 / (1 + exp(-v)).
+template <bool FAST>
+__device__ __forceinline__ float exp_minus(float v) {
+    return FAST ? __builtin_amdgcn_exp2f(v * -kLog2e) : expf(-v);
 }
 
+// The normal distribution's share below z, and exp(-z^2 / 2).  FAST: erfc(x) exp(x^2) is
+// t Q(t) with t = 1 / (1 + 0.35 x) and Q a polynomial of degree 7, a least-squares fit of
+// its relative error in Chebyshev's basis over x in [0, 40] (1.3e-6 in fp32 arithmetic).
 template <bool FAST>
-__device__ __forceinline__ float slope(int act, float z) {
-    if (act == DSM_ACT_RELU) return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;
+__device__ __forceinline__ float normal_share(float z, float* bell) {
+    if constexpr (!FAST) {
+        *bell = expf(-0.5f * z * z);
+        return 0.5f * erfcf(z * -0.707106781186547524f);
+    }
+    constexpr float kQ[8] = {0.19746625423431396f, 0.1974421590566635f,     0.18609043955802917f, 0.1536107361316681f,
+                             0.16591569781303406f, -0.018850743770599365f, 0.20431290566921234f, -0.08598839491605759f};
+    *bell = __builtin_amdgcn_exp2f(z * z * (-0.5f * kLog2e));
+    const float u = __builtin_amdgcn_rcpf(__builtin_fmaf(fabsf(z), 0.35f * 0.707106781186547524f, 1.0f));
+    float q = kQ[7];
+#pragma unroll
+    for (int k = 6; k >= 0; --k) q = __builtin_fmaf(q, u, kQ[k]);
+    const float less = 0.5f * u * q * *bell;
+    return z < 0.f ? less : 1.0f - less;
+}
+
+template <int ACT, bool FAST>
+__device__ __forceinline__ float activation(float z) {
+    if constexpr (ACT == DSM_ACT_RELU) {
+        return z < 0.f ? 0.f : z;
+    } else if constexpr (ACT == DSM_ACT_GELU) {
+        float bell;
+        return z * normal_share<FAST>(z, &bell);
+    } else {
+        const float v = ACT == DSM_ACT_SILU ? z : z * __builtin_fmaf(z * z, kTanhA * kTanhB, kTanhA);
+        return z * one_over<FAST>(1.0f + exp_minus<FAST>(v));
+    }
+}
+
+template <int ACT, bool FAST>
+__device__ __forceinline__ float slope(float z) {
+    if constexpr (ACT == DSM_ACT_RELU) return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;
     // (Beyond 50 the slopes are 0 and 1 in fp32, and their terms would overflow.)
     const float v = z > 50.f ? 50.f : z < -50.f ? -50.f : z;
-    if (act == DSM_ACT_GELU) {
-        const float e = FAST ? __builtin_amdgcn_exp2f(v * v * -0.721347520444481703f) : expf(-0.5f * v * v);
-        return 0.5f * erfcf(v * -0.707106781186547524f) + v * 0.398942280401432678f * e;
+    if constexpr (ACT == DSM_ACT_GELU) {
+        float bell;
+        const float share = normal_share<FAST>(v, &bell);
+        return __builtin_fmaf(v * 0.398942280401432678f, bell, share);
     }
-    float share, rest;
-    if (act == DSM_ACT_SILU) {
-        logistic<FAST>(v, &share, &rest);
-        return share + v * share * rest;
+    float u = v, rate = 1.f;
+    if constexpr (ACT == DSM_ACT_GELU_TANH) {
+        const float square = v * v;
+        u = v * __builtin_fmaf(square, kTanhA * kTanhB, kTanhA);
+        rate = __builtin_fmaf(square, 3.f * kTanhA * kTanhB, kTanhA);
     }
-    const float square = v * v;
-    logistic<FAST>(kTanhA * (v + kTanhB * (square * v)), &share, &rest);
-    return share + v * share * rest * (kTanhA * (1.f + 3.f * kTanhB * square));
+    // share (1 - share) without a difference; exp stays a number.
+    const float e = exp_minus<FAST>(u < -80.f ? -80.f : u), share = one_over<FAST>(1.0f + e);
+    return __builtin_fmaf(v * rate, share * (e * share), share);
+}
+
+// use(an activation's number as a type): one branch for eight entries.
+template <class F>
+__device__ __forceinline__ void with_act(int act, F use) {
+    switch (act) {
+        case DSM_ACT_RELU: return use(std::integral_constant<int, DSM_ACT_RELU>());
+        case DSM_ACT_GELU: return use(std::integral_constant<int, DSM_ACT_GELU>());
+        case DSM_ACT_GELU_TANH: return use(std::integral_constant<int, DSM_ACT_GELU_TANH>());
+        case DSM_ACT_SILU: return use(std::integral_constant<int, DSM_ACT_SILU>());
+        default: return;
+    }
+}
+template <bool FAST>
+__device__ __forceinline__ void activate(int act, V8& v) {
+    with_act(act, [&](auto a) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v.v[q] = activation<decltype(a)::value, FAST>(v.v[q]);
+    });
+}
+// d times the slopes at z, of the columns that there are.
+template <bool FAST>
+__device__ __forceinline__ void times_slope(int act, V8& d, const V8& z, int have) {
+    with_act(act, [&](auto a) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (q < have) d.v[q] *= slope<decltype(a)::value, FAST>(z.v[q]);
+    });
 }
 
 // ---- Epilogue of the forward pass ----
@@ -106,10 +156,7 @@ __device__ __forceinline__ void finish(const LinearCall& c, int64_t row, int col
 #pragma unroll
     for (int q = 0; q < 8; ++q) v.v[q] += bias.v[q];
     if (c.z) rows::store8<F32>(c.z, row * c.z_stride + col, v, have);
-    if (c.p.act != DSM_ACT_NONE) {
-#pragma unroll
-        for (int q = 0; q < 8; ++q) v.v[q] = activation<!F32>(c.p.act, v.v[q]);
-    }
+    activate<!F32>(c.p.act, v);
     if (c.residual) {
         const V8 r = rows::load8<F32>(c.residual, row * c.residual_stride + col, have);
 #pragma unroll
@@ -131,40 +178,56 @@ __device__ __forceinline__ V8 bias8(const LinearCall& c, int col) {
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bfloat8 __attribute__((ext_vector_type(8)));
 
-// 16 rows of w by G times 16 tokens a work-group, whose eight waves take every eighth
-// run of 128 bytes of k each, straight from memory into registers; their sums meet in
-// LDS.  Rows past the last one are the last one again, and not stored.
+// 16 rows of w by G times 16 tokens a work-group, whose waves take every eighth run of
+// 128 bytes of k each (of their part of k: few rows of w leave CUs idle otherwise).  Four
+// neighbouring lanes load 64 bytes of a row; lanes that are neighbours in a fragment hold
+// neighbouring rows instead, and loads in that order take the L1 a turn for each lane
+// (24 tokens of 6400 -> 1600: 19 us).  So runs go through LDS on their way, in a corner of each
+// wave's own, without barriers.  The waves' sums meet in LDS.
+// Rows past the last one are the last one again, and not stored.
 constexpr int kFewWaves = 8;
-constexpr int kFewRuns = 4;  // of a wave on their way at once
+constexpr int few_runs(int g) { return g < 4 ? 2 : 1; }  // of a wave on their way at once
 
 template <bool F32>
-struct Run {  // a lane's part of a row's run: 16 bytes of each 64
+struct Run {  // a lane's part of 16 rows' runs
     static constexpr int kSteps = F32 ? 32 : 64, kEach = F32 ? 4 : 8;
     f4 v[2];
-    __device__ __forceinline__ void load(const char* row, int k, int lane) {
+    // `row`: of the lane, from its 16 bytes of each 64 on.
+    __device__ __forceinline__ void load(const char* row, int k) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-            v[h] = *reinterpret_cast<const rows::f4_at*>(row + static_cast<int64_t>(k + h * (kSteps / 2)) * (F32 ? 4 : 2) +
-                                                         (lane >> 4) * 16);
+            v[h] = *reinterpret_cast<const rows::f4_at*>(row + static_cast<int64_t>(k) * (F32 ? 4 : 2) + h * 64);
     }
-    // The row's last run, shorter than the others.
-    __device__ __forceinline__ void load_end(const char* row, int k, int dim, int lane) {
+    // The row's last run, shorter than the others: `left` from the lane's bytes on.
+    __device__ __forceinline__ void load_end(const char* row, int k, int left) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int at = k + h * (kSteps / 2) + (lane >> 4) * kEach;
+            const char* at = row + static_cast<int64_t>(k) * (F32 ? 4 : 2) + h * 64;
+            const int have = left - h * (kSteps / 2);
             if constexpr (F32) {
                 v[h] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (at + e < dim) v[h][e] = reinterpret_cast<const float*>(row)[at + e];
+                    if (e < have) v[h][e] = reinterpret_cast<const float*>(at)[e];
             } else {
                 u16x8 u = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (at + e < dim) u[e] = reinterpret_cast<const u16*>(row)[at + e];
+                    if (e < have) u[e] = reinterpret_cast<const u16*>(at)[e];
                 v[h] = __builtin_bit_cast(f4, u);
             }
         }
+    }
+    // From lane (row, 16 bytes) = (l / 4, l % 4) to (l % 16, l / 16); the 16 bytes of a row change places
+    // so that neither side meets a bank twice.
+    __device__ __forceinline__ void turn(f4* lds, int lane) {
+        const int r = lane >> 2, l = lane & 15;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) lds[h * 64 + r * 4 + ((lane & 3) ^ (r >> 2))] = v[h];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) v[h] = lds[h * 64 + l * 4 + ((lane >> 4) ^ (l >> 2))];
+        __builtin_amdgcn_wave_barrier();
     }
 };
 
@@ -186,59 +249,73 @@ __device__ __forceinline__ f4 multiply(const Run<F32>& w, const Run<F32>& x, f4 
 template <bool F32, int G>
 __global__ __launch_bounds__(kFewWaves * 64) void k_few(LinearCall c) {
     using R = Run<F32>;
-    constexpr int kBytes = F32 ? 4 : 2;
-    __shared__ f4 sums[kFewWaves][G][64];
+    constexpr int kBytes = F32 ? 4 : 2, kFewRuns = few_runs(G);
+    __shared__ f4 lds[kFewWaves][G < 2 ? 2 : G][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int n0 = blockIdx.x * 16, t0 = blockIdx.y * 16 * G;
-    const int dim = c.p.dim, whole = dim / R::kSteps;
-    const char* w = static_cast<const char*>(c.w) + static_cast<int64_t>(min(n0 + (lane & 15), c.p.wide - 1)) * c.w_stride * kBytes;
+    const int n0 = blockIdx.x * 16, parts = c.p.splits;
+    const int dim = c.p.dim, runs = (dim + R::kSteps - 1) / R::kSteps, whole = dim / R::kSteps;
+    const int each = (runs + parts - 1) / parts, begin = min(static_cast<int>(blockIdx.y) * each, runs);
+    const int end = min(begin + each, runs), full = min(end, whole);
+    // Lane l of a fragment has token l % 16, rows l / 16 * 4 .. + 3 of w: eight rows are
+    // those of lanes l and l + 16.  What a lane that ends with them adds is on its way early.
+    const int g = (threadIdx.x >> 5) % G, l = (threadIdx.x & 15) + ((threadIdx.x >> 4) & 1) * 32;
+    const int token = g * 16 + (l & 15), col = n0 + (l >> 5) * 8;
+    const bool ends = threadIdx.x < G * 32 && token < c.p.tokens && col < c.p.wide;
+    const V8 bias = ends && parts == 1 ? bias8(c, col) : V8{};
+    const char* w = static_cast<const char*>(c.w) +
+                    static_cast<int64_t>(min(n0 + (lane >> 2), c.p.wide - 1)) * c.w_stride * kBytes + (lane & 3) * 16;
     const char* x[G];
     f4 acc[G];
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-        x[g] = static_cast<const char*>(c.x) +
-               static_cast<int64_t>(min(t0 + g * 16 + (lane & 15), c.p.tokens - 1)) * c.x_stride * kBytes;
-        acc[g] = f4{0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < G; ++k) {
+        x[k] = static_cast<const char*>(c.x) +
+               static_cast<int64_t>(min(k * 16 + (lane >> 2), c.p.tokens - 1)) * c.x_stride * kBytes + (lane & 3) * 16;
+        acc[k] = f4{0.f, 0.f, 0.f, 0.f};
     }
-    for (int first = wave; first < whole; first += kFewWaves * kFewRuns) {
+    f4* corner = &lds[wave][0][0];
+    for (int first = begin + wave; first < full; first += kFewWaves * kFewRuns) {
         R a[kFewRuns], b[kFewRuns][G];
 #pragma unroll
         for (int u = 0; u < kFewRuns; ++u) {
-            const int r = min(first + u * kFewWaves, whole - 1);
-            a[u].load(w, r * R::kSteps, lane);
+            const int r = first + u * kFewWaves;
+            if (r < full) {
+                a[u].load(w, r * R::kSteps);
 #pragma unroll
-            for (int g = 0; g < G; ++g) b[u][g].load(x[g], r * R::kSteps, lane);
+                for (int k = 0; k < G; ++k) b[u][k].load(x[k], r * R::kSteps);
+            }
         }
 #pragma unroll
         for (int u = 0; u < kFewRuns; ++u)
-            if (first + u * kFewWaves < whole) {
+            if (first + u * kFewWaves < full) {
+                a[u].turn(corner, lane);
 #pragma unroll
-                for (int g = 0; g < G; ++g) acc[g] = multiply(a[u], b[u][g], acc[g]);
+                for (int k = 0; k < G; ++k) {
+                    b[u][k].turn(corner, lane);
+                    acc[k] = multiply(a[u], b[u][k], acc[k]);
+                }
             }
     }
-    if (whole * R::kSteps < dim && wave == whole % kFewWaves) {
+    if (full < end && wave == (full - begin) % kFewWaves) {
         R a, b;
-        a.load_end(w, whole * R::kSteps, dim, lane);
+        const int left = dim - full * R::kSteps - (lane & 3) * R::kEach;
+        a.load_end(w, full * R::kSteps, left);
+        a.turn(corner, lane);
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-            b.load_end(x[g], whole * R::kSteps, dim, lane);
-            acc[g] = multiply(a, b, acc[g]);
+        for (int k = 0; k < G; ++k) {
+            b.load_end(x[k], full * R::kSteps, left);
+            b.turn(corner, lane);
+            acc[k] = multiply(a, b, acc[k]);
         }
     }
 #pragma unroll
-    for (int g = 0; g < G; ++g) sums[wave][g][lane] = acc[g];
+    for (int k = 0; k < G; ++k) lds[wave][k][lane] = acc[k];
     __syncthreads();
-    // Lane l of a fragment has token l % 16, rows l / 16 * 4 .. + 3 of w: eight rows are
-    // those of lanes l and l + 16.
-    if (threadIdx.x >= G * 32) return;
-    const int g = threadIdx.x >> 5, l = (threadIdx.x & 15) + ((threadIdx.x >> 4) & 1) * 32;
-    const int token = t0 + g * 16 + (l & 15), col = n0 + (l >> 5) * 8;
-    if (token >= c.p.tokens || col >= c.p.wide) return;
-    f4 lo = sums[0][g][l], hi = sums[0][g][l + 16];
+    if (!ends) return;
+    f4 lo = lds[0][g][l], hi = lds[0][g][l + 16];
 #pragma unroll
     for (int q = 1; q < kFewWaves; ++q) {
-        lo += sums[q][g][l];
-        hi += sums[q][g][l + 16];
+        lo += lds[q][g][l];
+        hi += lds[q][g][l + 16];
     }
     V8 v;
 #pragma unroll
@@ -246,7 +323,10 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_few(LinearCall c) {
         v.v[q] = lo[q];
         v.v[4 + q] = hi[q];
     }
-    finish<F32>(c, token, col, v, bias8(c, col));
+    if (parts > 1)
+        rows::store8<true>(c.workspace + c.p.y_parts, (static_cast<int64_t>(blockIdx.y) * c.p.tokens + token) * c.p.ld_y + col, v, 8);
+    else
+        finish<F32>(c, token, col, v, bias);
 }
 
 // ---- Operands ----
@@ -335,10 +415,7 @@ __global__ __launch_bounds__(256) void k_dz(LinearCall c) {
         const int here = row < c.p.tokens ? have : 0;
         V8 d = rows::load8<false>(c.dy, row * c.dy_stride + col, here);
         if (c.p.act != DSM_ACT_NONE) {
-            const V8 z = rows::load8<false>(c.z_in, row * c.z_stride + col, here);
-#pragma unroll
-            for (int q = 0; q < 8; ++q)
-                if (q < here) d.v[q] *= slope<true>(c.p.act, z.v[q]);
+            times_slope<true>(c.p.act, d, rows::load8<false>(c.z_in, row * c.z_stride + col, here), here);
         }
 #pragma unroll
         for (int q = 0; q < 8; ++q) sum.v[q] += d.v[q];
@@ -384,10 +461,7 @@ __global__ __launch_bounds__(256) void k_dz_split(LinearCall c, int top_groups) 
         const int here = row < c.p.tokens ? have : 0;
         V8 d = rows::load8<true>(c.dy, row * c.dy_stride + col, here);
         if (c.p.act != DSM_ACT_NONE) {
-            const V8 z = rows::load8<true>(c.z_in, row * c.z_stride + col, here);
-#pragma unroll
-            for (int q = 0; q < 8; ++q)
-                if (q < here) d.v[q] *= slope<false>(c.p.act, z.v[q]);
+            times_slope<false>(c.p.act, d, rows::load8<true>(c.z_in, row * c.z_stride + col, here), here);
         }
         return d;
     };
@@ -532,31 +606,19 @@ __device__ __forceinline__ V8 eight_of(const tile::Eight& x) {
     return v;
 }
 
-// y, or a part of its sums, by tiles of BM.
-template <bool F32, int BM, bool PARTS>
-__global__ __launch_bounds__(tile::threads_of(BM)) void k_forward(LinearCall c, int tiles_t, int tiles_n) {
-    using T = tile::Pick<kElem<F32>, BM, kContig, kContig>;
-    __shared__ __align__(1024) char lds[T::kLdsBytes];
-    int id = xcd_run(blockIdx.x, gridDim.x);
-    const int part = PARTS ? id / (tiles_t * tiles_n) : 0;
-    id -= part * tiles_t * tiles_n;
-    // Eight rows of tiles side by side, so that the tiles an XCD has at once share rows
-    // of both operands.
-    constexpr int kRows = 8;
-    const int group = id / (kRows * tiles_n), rows = min(kRows, tiles_t - group * kRows);
-    id -= group * kRows * tiles_n;
-    const int tn = id / rows, tt = group * kRows + id - tn * rows;
+// y, or a part of its sums: the tile of rows from row0 on, columns from col0 on.
+template <bool F32, class T, bool PARTS>
+__device__ __forceinline__ void forward_tile(const LinearCall& c, int row0, int col0, int part, DSM_LDS char* lds) {
     int k0 = 0, k1 = static_cast<int>(c.p.ld_dim / (F32 ? 2 : 1));
     if (PARTS) part_of(k1, c.p.splits, part, &k0, &k1);
     T t;
     t.clear();
-    t.add(x_rows<F32>(c), w_rows<F32>(c), tt * BM, tn * BM, k0, k1, (DSM_LDS char*)lds, c.p.tokens - tt * BM,
-          c.p.wide - tn * BM);
+    t.add(x_rows<F32>(c), w_rows<F32>(c), row0, col0, k0, k1, lds, c.p.tokens - row0, c.p.wide - col0);
     const int32_t* x_exp = reinterpret_cast<const int32_t*>(c.workspace + c.p.x_exp);
     const int32_t* w_exp = reinterpret_cast<const int32_t*>(c.workspace + c.p.w_exp);
 #pragma unroll
     for (int q = 0; q < T::FJ / 2; ++q) {
-        const int col = tn * BM + t.col8(q);
+        const int col = col0 + t.col8(q);
         const V8 bias = PARTS ? V8{} : bias8(c, col);
         int we[8];
         if constexpr (F32) {
@@ -565,7 +627,7 @@ __global__ __launch_bounds__(tile::threads_of(BM)) void k_forward(LinearCall c, 
         }
 #pragma unroll
         for (int f = 0; f < T::FI; ++f) {
-            const int row = tt * BM + t.row(f);
+            const int row = row0 + t.row(f);
             V8 v = eight_of(t.eight(f, q));
             if (row >= c.p.tokens || col >= c.p.wide) continue;
             if constexpr (F32) {
@@ -580,6 +642,38 @@ __global__ __launch_bounds__(tile::threads_of(BM)) void k_forward(LinearCall c, 
                 finish<F32>(c, row, col, v, bias);
         }
     }
+}
+
+// Tile `id` of tiles_t x tiles_n: eight rows of tiles side by side, so that the tiles an
+// XCD has at once share rows of both operands.
+__device__ __forceinline__ void place_tile(int id, int tiles_t, int tiles_n, int* tt, int* tn) {
+    constexpr int kRows = 8;
+    const int group = id / (kRows * tiles_n), rows = min(kRows, tiles_t - group * kRows);
+    id -= group * kRows * tiles_n;
+    *tn = id / rows;
+    *tt = group * kRows + id - *tn * rows;
+}
+
+// By tiles of BM.  Tiles of 256 take the first `tiles_n` columns of tiles alone; what a
+// last turn that leaves most CUs idle would take goes by tiles of 128.
+template <bool F32, int BM, bool PARTS>
+__global__ __launch_bounds__(tile::threads_of(BM)) void k_forward(LinearCall c, int tiles_t, int tiles_n, int groups) {
+    using T = tile::Pick<kElem<F32>, BM, kContig, kContig>;
+    __shared__ __align__(1024) char lds[T::kLdsBytes];
+    int tt, tn;
+    if constexpr (BM == 256 && !PARTS) {
+        if (static_cast<int>(blockIdx.x) >= groups) {
+            const int col0 = tiles_n * 256, rest_t = (c.p.tokens + 127) / 128, rest_n = (c.p.wide - col0 + 127) / 128;
+            place_tile(xcd_run(blockIdx.x - groups, gridDim.x - groups), rest_t, rest_n, &tt, &tn);
+            forward_tile<F32, tile::Pick<kElem<F32>, 128, kContig, kContig>, false>(c, tt * 128, col0 + tn * 128, 0,
+                                                                                    (DSM_LDS char*)lds);
+            return;
+        }
+    }
+    int id = xcd_run(blockIdx.x, groups);
+    const int part = PARTS ? id / (tiles_t * tiles_n) : 0;
+    place_tile(id - part * tiles_t * tiles_n, tiles_t, tiles_n, &tt, &tn);
+    forward_tile<F32, T, PARTS>(c, tt * BM, tn * BM, part, (DSM_LDS char*)lds);
 }
 
 // Eight columns of the sum of `parts` arrays of `rows` rows.
@@ -776,16 +870,22 @@ __global__ __launch_bounds__(256) void k_no_tokens(LinearCall c) {
 
 unsigned groups_for(int64_t wanted, int64_t most) { return static_cast<unsigned>(wanted < most ? wanted : most); }
 
+template <bool F32>
+void forward_join(const LinearCall& c, hipStream_t stream) {
+    const int64_t eights = static_cast<int64_t>(c.p.tokens) * ((c.p.wide + 7) / 8);
+    k_forward_join<F32><<<groups_for((eights + 255) / 256, 4096), 256, 0, stream>>>(c);
+}
+
 template <bool F32, int BM>
 void forward(const LinearCall& c, hipStream_t stream) {
-    const int tiles_t = (c.p.tokens + BM - 1) / BM, tiles_n = (c.p.wide + BM - 1) / BM;
-    const unsigned groups = static_cast<unsigned>(tiles_t) * tiles_n * c.p.splits;
+    const int tiles_t = (c.p.tokens + BM - 1) / BM, all = (c.p.wide + BM - 1) / BM;
+    const int tiles_n = BM == 256 && c.p.splits == 1 ? c.p.front : all, groups = tiles_t * tiles_n * c.p.splits;
     if (c.p.splits > 1) {
-        k_forward<F32, BM, true><<<groups, tile::threads_of(BM), 0, stream>>>(c, tiles_t, tiles_n);
-        k_forward_join<F32><<<groups_for((static_cast<int64_t>(c.p.tokens) * ((c.p.wide + 7) / 8) + 255) / 256, 4096), 256, 0,
-                              stream>>>(c);
+        k_forward<F32, BM, true><<<groups, tile::threads_of(BM), 0, stream>>>(c, tiles_t, tiles_n, groups);
+        forward_join<F32>(c, stream);
     } else {
-        k_forward<F32, BM, false><<<groups, tile::threads_of(BM), 0, stream>>>(c, tiles_t, tiles_n);
+        const int rest = tiles_n < all ? (c.p.tokens + 127) / 128 * ((c.p.wide - tiles_n * 256 + 127) / 128) : 0;
+        k_forward<F32, BM, false><<<groups + rest, tile::threads_of(BM), 0, stream>>>(c, tiles_t, tiles_n, groups);
     }
 }
 
@@ -807,13 +907,14 @@ void forward(const LinearCall& c, hipStream_t stream) {
 
 template <bool F32>
 void few(const LinearCall& c, hipStream_t stream) {
-    const unsigned n = (c.p.wide + 15) / 16;
+    const dim3 n((c.p.wide + 15) / 16, c.p.splits);
     if (c.p.tokens <= 16)
         k_few<F32, 1><<<n, kFewWaves * 64, 0, stream>>>(c);
     else if (c.p.tokens <= 32)
         k_few<F32, 2><<<n, kFewWaves * 64, 0, stream>>>(c);
     else
         k_few<F32, 4><<<n, kFewWaves * 64, 0, stream>>>(c);
+    if (c.p.splits > 1) forward_join<F32>(c, stream);
 }
 
 template <bool F32, int BM>

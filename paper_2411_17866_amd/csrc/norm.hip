@@ -188,20 +188,41 @@ __global__ __launch_bounds__(W * 64) void k_norm_backward(NormCall p) {
     for (int s = 0; s < kNormSums; ++s)
 #pragma unroll
         for (int q = 0; q < 8; ++q) sums[s].v[q] = 0.f;
-    for (int64_t row = static_cast<int64_t>(blockIdx.x) * R; row < p.tokens; row += static_cast<int64_t>(gridDim.x) * R) {
+    // The rows after these are on their way while these are worked on (sixteen waves have
+    // no registers for that).
+    constexpr bool kAhead = W < 16;
+    struct {
+        rows::Raw8<F32> dy[R], h[R], ds[R], f[R];
+    } next;
+    const auto load = [&](int64_t row) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const int have = row + k < p.tokens ? c.have : 0;
+            if (normed) {
+                next.dy[k] = rows::raw8<F32>(p.dy, (row + k) * p.dy_stride + c.col, have);
+                next.h[k] = rows::raw8<F32>(p.h, (row + k) * p.h_stride + c.col, have);
+            }
+            if (p.ds) next.ds[k] = rows::raw8<F32>(p.ds, (row + k) * p.ds_stride + c.col, have);
+            if (reads_f) next.f[k] = rows::raw8<F32>(p.f, (row + k) * p.f_stride + c.col, have);
+        }
+    };
+    const int64_t step = static_cast<int64_t>(gridDim.x) * R;
+    if (kAhead) load(static_cast<int64_t>(blockIdx.x) * R);
+    for (int64_t row = static_cast<int64_t>(blockIdx.x) * R; row < p.tokens; row += step) {
         const int count = static_cast<int>(min(static_cast<int64_t>(R), p.tokens - row));
         V8 d[R], hat[R], f[R], ds[R];
         float r[R];
+        if (!kAhead) load(row);
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            const int have = k < count ? c.have : 0;
             if (normed) {
-                d[k] = rows::load8<F32>(p.dy, (row + k) * p.dy_stride + c.col, have);
-                hat[k] = rows::load8<F32>(p.h, (row + k) * p.h_stride + c.col, have);
+                d[k] = rows::wide8(next.dy[k]);
+                hat[k] = rows::wide8(next.h[k]);
             }
-            if (p.ds) ds[k] = rows::load8<F32>(p.ds, (row + k) * p.ds_stride + c.col, have);
-            if (reads_f) f[k] = rows::load8<F32>(p.f, (row + k) * p.f_stride + c.col, have);
+            if (p.ds) ds[k] = rows::wide8(next.ds[k]);
+            if (reads_f) f[k] = rows::wide8(next.f[k]);
         }
+        if (kAhead) load(row + step);
         if (normed) {
             standardise<W, R>(hat, r, c, count, p.norm == DSM_NORM_LAYER, p.eps, dim, sum);
 #pragma unroll

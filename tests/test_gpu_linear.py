@@ -56,7 +56,7 @@ def _backward(i, name="none", dw_dtype=None, **given):
 
 # One, odd sizes, and around runs of k (32, 64), fragments (16), few tokens (64), tiles (64, 128, 256).
 SIZES = [(1, 1, 1), (1, 7, 3), (1, 768, 1000), (2, 64, 17), (3, 65, 16), (7, 31, 129), (15, 128, 33), (16, 100, 48), (17, 63, 64),
-         (31, 257, 100), (33, 96, 255), (48, 1000, 15), (63, 64, 65), (64, 192, 31), (65, 64, 64), (66, 1, 9), (80, 72, 136),
+         (31, 257, 100), (33, 96, 255), (48, 1000, 15), (63, 64, 65), (50, 6400, 40), (3, 4097, 20), (64, 192, 31), (65, 64, 64), (66, 1, 9), (80, 72, 136),
          (127, 129, 130), (128, 128, 128), (129, 320, 384), (192, 64, 257), (255, 33, 65), (256, 256, 256), (257, 264, 520),
          (300, 1600, 48), (500, 24, 2000), (513, 512, 513), (1025, 40, 72)]
 
