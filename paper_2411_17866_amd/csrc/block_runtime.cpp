@@ -148,7 +148,7 @@ dsm_status check_linear(const dsm_linear_problem* p) {
     return DSM_OK;
 }
 
-dsm::LinearPlan plan_linear(const dsm_linear_problem* p) {
+dsm::LinearPlan make_linear_plan(const dsm_linear_problem* p) {
     dsm::LinearPlan q{};
     const int64_t T = p->tokens, D = p->dim, N = p->wide;
     q.tokens = static_cast<int32_t>(T);
@@ -195,6 +195,30 @@ dsm::LinearPlan plan_linear(const dsm_linear_problem* p) {
     q.bias_sums = take(q.bias_parts * N * 4);
     q.backward_bytes = at;
     return q;
+}
+
+// A plan follows from the problem alone and takes some microseconds to weigh: each thread keeps
+// the plans of the sizes that it asked for last.
+const dsm::LinearPlan& plan_linear(const dsm_linear_problem* p) {
+    constexpr int kKept = 16;
+    static thread_local struct {
+        dsm_linear_problem problem;
+        dsm::LinearPlan plan;
+        bool there;
+    } kept[kKept];
+    static thread_local int next = 0;
+    const auto same = [&](const dsm_linear_problem& o) {
+        return o.tokens == p->tokens && o.dim == p->dim && o.wide == p->wide && o.dtype == p->dtype && o.act == p->act &&
+               o.dw_dtype == p->dw_dtype && o.grads == p->grads;
+    };
+    for (const auto& k : kept)
+        if (k.there && same(k.problem)) return k.plan;
+    auto& k = kept[next];
+    next = (next + 1) % kKept;
+    k.problem = *p;
+    k.plan = make_linear_plan(p);
+    k.there = true;
+    return k.plan;
 }
 
 // Whether products can take a matrix's rows of `cols` bf16 elements where they lie: 16-byte
@@ -353,7 +377,7 @@ extern "C" {
 dsm_status dsm_linear_workspace(const dsm_linear_problem* problem, int64_t* workspace_bytes) {
     if (dsm_status st = check_linear(problem)) return st;
     if (!workspace_bytes) return invalid("workspace_bytes is NULL");
-    const dsm::LinearPlan q = plan_linear(problem);
+    const dsm::LinearPlan& q = plan_linear(problem);
     *workspace_bytes = std::max(q.forward_bytes, q.backward_bytes);
     return DSM_OK;
 }

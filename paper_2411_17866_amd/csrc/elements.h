@@ -47,11 +47,16 @@ __device__ __forceinline__ Raw8<F32> raw8(const void* base, int64_t at, int have
         if (have >= 8) {
             o.a = *reinterpret_cast<const f4_at*>(p);
             o.b = *reinterpret_cast<const f4_at*>(p + 4);
-        } else {
+        } else if (have > 0) {
+            // The last one again for those that are missing: loads side by side, no branches.
+            // (Their places are not kept in registers from one row to the next.)
+            int last = have - 1;
+            asm volatile("" : "+v"(last));
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                if (q < have) o.a[q] = p[q];
-                if (q < 3 && 4 + q < have) o.b[q] = p[4 + q];
+                const float a = p[min(q, last)], b = p[min(4 + q, last)];
+                o.a[q] = q < have ? a : 0.f;
+                o.b[q] = 4 + q < have ? b : 0.f;
             }
         }
     } else {
@@ -59,10 +64,14 @@ __device__ __forceinline__ Raw8<F32> raw8(const void* base, int64_t at, int have
         o.v = u16x8{0, 0, 0, 0, 0, 0, 0, 0};
         if (have >= 8) {
             o.v = *reinterpret_cast<const u16x8_at*>(p);
-        } else {
+        } else if (have > 0) {
+            int last = have - 1;
+            asm volatile("" : "+v"(last));
 #pragma unroll
-            for (int q = 0; q < 7; ++q)
-                if (q < have) o.v[q] = p[q];
+            for (int q = 0; q < 7; ++q) {
+                const u16 a = p[min(q, last)];
+                o.v[q] = q < have ? a : static_cast<u16>(0);
+            }
         }
     }
     return o;
@@ -78,6 +87,13 @@ __device__ __forceinline__ V8 wide8(const Raw8<F32>& x) {
             o.v[q] = bf16_to_float(x.v[q]);
     }
     return o;
+}
+// Moves elements `back` places to the front, zeros behind them.
+__device__ __forceinline__ void shift(V8& v, int back) {
+#pragma unroll
+    for (int by = 4; by > 0; by /= 2)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v.v[q] = (back & by) ? (q + by < 8 ? v.v[q + by] : 0.f) : v.v[q];
 }
 template <bool F32>
 __device__ __forceinline__ V8 load8(const void* base, int64_t at, int have) {
@@ -97,7 +113,7 @@ __device__ __forceinline__ void store8(void* base, int64_t at, const V8& x, int 
             }
             *reinterpret_cast<f4_at*>(p) = a;
             *reinterpret_cast<f4_at*>(p + 4) = b;
-        } else {
+        } else if (have > 0) {
 #pragma unroll
             for (int q = 0; q < 7; ++q)
                 if (q < have) p[q] = x.v[q];
@@ -109,7 +125,7 @@ __device__ __forceinline__ void store8(void* base, int64_t at, const V8& x, int 
 #pragma unroll
             for (int q = 0; q < 8; ++q) a[q] = float_to_bf16(x.v[q]);
             *reinterpret_cast<u16x8_at*>(p) = a;
-        } else {
+        } else if (have > 0) {
 #pragma unroll
             for (int q = 0; q < 7; ++q)
                 if (q < have) p[q] = float_to_bf16(x.v[q]);
@@ -117,26 +133,39 @@ __device__ __forceinline__ void store8(void* base, int64_t at, const V8& x, int 
     }
 }
 
-// x turned by N within every 16 lanes.
-template <int N>
-__device__ __forceinline__ float turned(float x) {
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x120 + N, 0xf, 0xf, true));
+// x of the lane that a DPP control names.
+template <int CTRL>
+__device__ __forceinline__ float from_lane(float x) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
 }
-// The wave's sum, in every lane, in a fixed order: within 16 lanes by turns, then
-// rows of 16 change places.
-__device__ __forceinline__ float wave_sum(float x) {
-    x += turned<8>(x);
-    x += turned<4>(x);
-    x += turned<2>(x);
-    x += turned<1>(x);
-    unsigned u = __builtin_bit_cast(unsigned, x);
-    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-    unsigned p = a[0], q = a[1];
-    x = __builtin_bit_cast(float, p) + __builtin_bit_cast(float, q);
-    u = __builtin_bit_cast(unsigned, x);
-    const auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    p = b[0], q = b[1];
-    return __builtin_bit_cast(float, p) + __builtin_bit_cast(float, q);
+// The sum over every L lanes that lie together, in each of them, in a fixed order: within
+// 16 lanes by turns, then rows of 16 change places.
+template <int L>
+__device__ __forceinline__ float lanes_sum(float x) {
+    static_assert(L == 8 || L == 16 || L == 32 || L == 64, "parts of a wave");
+    if constexpr (L == 8) {
+        x += from_lane<0xb1>(x);   // quad_perm: lane ^ 1
+        x += from_lane<0x4e>(x);   // quad_perm: lane ^ 2
+        x += from_lane<0x141>(x);  // half of a row mirrored: the other quad
+        return x;
+    }
+    x += from_lane<0x128>(x);  // turned by 8, 4, 2, 1 in a row of 16
+    x += from_lane<0x124>(x);
+    x += from_lane<0x122>(x);
+    x += from_lane<0x121>(x);
+    if constexpr (L >= 32) {
+        const unsigned u = __builtin_bit_cast(unsigned, x);
+        const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        const unsigned p = a[0], q = a[1];
+        x = __builtin_bit_cast(float, p) + __builtin_bit_cast(float, q);
+    }
+    if constexpr (L == 64) {
+        const unsigned u = __builtin_bit_cast(unsigned, x);
+        const auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        const unsigned p = b[0], q = b[1];
+        x = __builtin_bit_cast(float, p) + __builtin_bit_cast(float, q);
+    }
+    return x;
 }
 
 // Sums of K values over a work-group of W waves, in every lane, through K * W floats
@@ -145,7 +174,7 @@ __device__ __forceinline__ float wave_sum(float x) {
 template <int W, int K>
 __device__ __forceinline__ void group_sums(float (&x)[K], float* lds) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) x[k] = wave_sum(x[k]);
+    for (int k = 0; k < K; ++k) x[k] = lanes_sum<64>(x[k]);
     if constexpr (W > 1) {
         if ((threadIdx.x & 63) == 0) {
 #pragma unroll

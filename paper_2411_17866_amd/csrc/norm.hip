@@ -5,21 +5,22 @@
 //   a norm of a row v:  "layer"  (v - mean) r weight + bias,  r = 1 / sqrt(var + eps)
 //                       "rms"    v r weight + bias,           r = 1 / sqrt(mean of v^2 + eps)
 //
-// Backward, with e = dy weight and v' = v - mean (or v):
-//   d = ds + r e - v' r^3 mean(e v') [- r mean(e)]      (dh = d)
-//   the same formula again takes scale gate d post_weight back through post, to df;
+// Backward, with v^ = (v - mean) r (or v r) and e = dy weight:
+//   dh = d = ds + r (e - v^ mean(e v^) [- mean(e)])
+//   the same formula takes g = scale gate d post_weight back through post, to df;
 //   the vectors' gradients are sums over the tokens.
 // Statistics are computed anew from s and f, which have to be read anyway: they are in
 // registers, and nothing but s is kept from the forward pass.
 //
-// Everything is bound by memory: each tensor is read or written once.  A work-group of
-// W waves takes R rows at a time, eight columns a lane in registers, and sums over them
-// by turns of lanes and one exchange through LDS; variances are those of v - mean, not
-// differences of sums.  In the backward kernel a lane keeps its columns of the
-// vectors' gradients in registers over all of its work-group's rows; the work-groups'
-// sums are joined by a second launch, in a fixed order.
-#include <type_traits>
-
+// Everything is bound by memory: each tensor is read or written once.  A row is worked
+// on by L lanes of a wave (several rows a wave) or by W waves, with 8 columns a lane
+// in registers; sums over it go by turns of lanes and one exchange through LDS.
+// Variances are those of v - mean, not differences of sums.  In the backward kernel a
+// lane keeps its columns of the vectors' gradients in registers over all of its
+// work-group's rows; the work-groups' sums are joined by a second launch, in a fixed
+// order.  Few registers and many waves hide the rows' latency better than rows ahead
+// of their turn: two rows at a time, or loads of the next ones, took 8192 x 1600 in fp32
+// from 74 us to 103, 85 and with both 135 us.
 #include "block_internal.h"
 #include "elements.h"
 
@@ -30,253 +31,272 @@ namespace {
 
 using rows::V8;
 
-// Rows that a work-group takes at a time (sixteen waves have 128 registers).
-constexpr int rows_of(int waves) { return waves == 16 ? 1 : 2; }
+// Who works on a row: L lanes, or all 64 of W waves, with 8 columns each.
+template <int W_, int L_>
+struct Team {
+    static constexpr int W = W_, L = L_;
+    static constexpr int kRows = 64 / L;  // of a work-group at a time
+    static constexpr int kFloats = 2 * 4 * W;
+    static_assert(L == 64 || W == 1, "parts of a wave");
 
-// This lane's columns: 8 from `col` on, of which `have` exist.
-struct Cols {
-    int col, have;
-};
-__device__ __forceinline__ Cols cols_of(int dim) {
-    const int c = static_cast<int>(threadIdx.x) * 8;
-    return {c, max(0, min(dim - c, 8))};
-}
-
-// Columns past the row count as 0 in every sum.
-__device__ __forceinline__ V8 vector8(const float* p, const Cols& c, float otherwise) {
-    if (p) return rows::load8<true>(p, c.col, c.have);
-    V8 v;
-#pragma unroll
-    for (int q = 0; q < 8; ++q) v.v[q] = q < c.have ? otherwise : 0.f;
-    return v;
-}
-
-// What a kernel's sums over a row share.
-template <int W, int R>
-struct Sums {
-    static constexpr int kFloats = 4 * R * W;  // two buffers of up to 2 R sums
     float* lds;
-    int turn;
+    int turn, col, have;  // this lane's columns: 8 from col on, of which `have` exist
+    int row;              // of the work-group's rows
+    int back;             // where a row ends among them: how far before col eight columns are whole
+    bool ragged;          // there are such lanes
+
+    __device__ __forceinline__ Team(float* lds_, int dim) : lds(lds_), turn(0) {
+        col = (static_cast<int>(threadIdx.x) % (W * L)) * 8;
+        row = W == 1 ? static_cast<int>(threadIdx.x) / L : 0;
+        have = max(0, min(dim - col, 8));
+        ragged = dim % 8 != 0;
+        // (Columns of another wave may be written in place before they are read here.)
+        back = have > 0 && have < 8 && col > 0 && (threadIdx.x & 63) != 0 ? 8 - have : 0;
+    }
+    // Eight columns, on their way: a row's end takes the eight before it and moves them to
+    // their places when they are there (taken one by one they would be waited for at once).
+    template <bool F32>
+    __device__ __forceinline__ rows::Raw8<F32> raw(const void* base, int64_t r, int64_t stride, bool there = true) const {
+        return rows::raw8<F32>(base, r * stride + col - back, there ? have + back : 0);
+    }
+    template <bool F32>
+    __device__ __forceinline__ V8 wide(const rows::Raw8<F32>& x) const {
+        V8 v = rows::wide8(x);
+        if (ragged) rows::shift(v, back);
+        return v;
+    }
+    // Sums over the row; two buffers of LDS take turns.
     template <int K>
-    __device__ __forceinline__ void operator()(float (&x)[K]) {
-        static_assert(K <= 2 * R, "a buffer's sums");
-        rows::group_sums<W, K>(x, lds + turn * 2 * R * W);
-        turn ^= 1;
+    __device__ __forceinline__ void sum(float (&x)[K]) {
+        static_assert(K <= 4, "a buffer's sums");
+        if constexpr (L < 64) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) x[k] = rows::lanes_sum<L>(x[k]);
+        } else {
+            rows::group_sums<W, K>(x, lds + turn * 4 * W);
+            turn ^= 1;
+        }
+    }
+    // A vector, or `otherwise`; columns past the row count as 0 in every sum.
+    __device__ __forceinline__ rows::Raw8<true> vector(const float* p) const {
+        return p ? raw<true>(p, 0, 0) : rows::Raw8<true>{};
+    }
+    __device__ __forceinline__ V8 vector(const float* p, const rows::Raw8<true>& x, float otherwise) const {
+        if (p) return wide(x);
+        V8 v;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v.v[q] = q < have ? otherwise : 0.f;
+        return v;
+    }
+    __device__ __forceinline__ float total(const V8& v) const {
+        float s = 0.f;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) s += v.v[q];
+        return s;
+    }
+    __device__ __forceinline__ float squares(const V8& v) const {
+        float s = 0.f;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) s = __builtin_fmaf(v.v[q], v.v[q], s);
+        return s;
+    }
+    __device__ __forceinline__ void subtract(V8& v, float mean) const {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v.v[q] = q < have ? v.v[q] - mean : 0.f;
+    }
+    template <bool F32>
+    __device__ __forceinline__ void store(const V8& v, void* base, int64_t r, int64_t stride, bool there) const {
+        rows::store8<F32>(base, r * stride + col, v, there ? have : 0);
     }
 };
 
-// R rows -> (v - mean) r (layer) or v r, and r; 0 for rows from `count` on and in the
-// columns past the row.
-template <int W, int R>
-__device__ __forceinline__ void standardise(V8 (&v)[R], float (&r)[R], const Cols& c, int count, bool layer, float eps,
-                                            float dim, Sums<W, R>& sum) {
-    float s[R];
+// A row standardised in place.
+template <class T>
+__device__ __forceinline__ void standardise(T& t, V8& v, bool layer, float eps, float dim) {
     if (layer) {
-#pragma unroll
-        for (int k = 0; k < R; ++k) {
-            s[k] = 0.f;
-#pragma unroll
-            for (int q = 0; q < 8; ++q) s[k] += v[k].v[q];
-        }
-        sum(s);
-#pragma unroll
-        for (int k = 0; k < R; ++k) {
-            const float mean = s[k] / dim;
-#pragma unroll
-            for (int q = 0; q < 8; ++q) v[k].v[q] = q < c.have ? v[k].v[q] - mean : 0.f;
-        }
+        float s[1] = {t.total(v)};
+        t.sum(s);
+        t.subtract(v, s[0] / dim);
     }
+    float s[1] = {t.squares(v)};
+    t.sum(s);
+    const float r = 1.0f / sqrtf(s[0] / dim + eps);
 #pragma unroll
-    for (int k = 0; k < R; ++k) {
-        s[k] = 0.f;
-#pragma unroll
-        for (int q = 0; q < 8; ++q) s[k] = __builtin_fmaf(v[k].v[q], v[k].v[q], s[k]);
-    }
-    sum(s);
-#pragma unroll
-    for (int k = 0; k < R; ++k) {
-        r[k] = k < count ? 1.0f / sqrtf(s[k] / dim + eps) : 0.f;
-#pragma unroll
-        for (int q = 0; q < 8; ++q) v[k].v[q] *= r[k];
-    }
+    for (int q = 0; q < 8; ++q) v.v[q] *= r;
 }
 
-// 8192 rows of 1600 in bf16 onto the residual, layer: 26 us, 4.1 TB/s.
-template <bool F32, int W, int R>
-__global__ __launch_bounds__(W * 64) void k_norm(NormCall p) {
-    __shared__ float lds[Sums<W, R>::kFloats];
-    Sums<W, R> sum{lds, 0};
+// 8192 rows of 1600 in bf16 onto the residual, layer: 23 us, 4.5 TB/s.
+template <bool F32, class T>
+__global__ __launch_bounds__(T::W * 64) void k_norm(NormCall p) {
+    __shared__ float lds[T::kFloats];
+    T t(lds, p.dim);
     const float dim = static_cast<float>(p.dim);
-    const Cols c = cols_of(p.dim);
-    const V8 weight = vector8(p.weight, c, 1.f), bias = vector8(p.bias, c, 0.f);
-    const V8 post_weight = vector8(p.post_weight, c, 1.f), post_bias = vector8(p.post_bias, c, 0.f);
-    V8 share = vector8(p.gate, c, 1.f);
+    const auto raw_weight = t.vector(p.weight), raw_bias = t.vector(p.bias), raw_gate = t.vector(p.gate);
+    const auto raw_post_weight = t.vector(p.post_weight), raw_post_bias = t.vector(p.post_bias);
+    // The first row is on its way before the vectors are there.
+    rows::Raw8<F32> h{}, x{};
+    const auto load = [&](int64_t row) {
+        h = t.template raw<F32>(p.h, row, p.h_stride, row < p.tokens);
+        if (p.f) x = t.template raw<F32>(p.f, row, p.f_stride, row < p.tokens);
+    };
+    load(static_cast<int64_t>(blockIdx.x) * T::kRows + t.row);
+    const V8 weight = t.vector(p.weight, raw_weight, 1.f), bias = t.vector(p.bias, raw_bias, 0.f);
+    const V8 post_weight = t.vector(p.post_weight, raw_post_weight, 1.f), post_bias = t.vector(p.post_bias, raw_post_bias, 0.f);
+    V8 share = t.vector(p.gate, raw_gate, 1.f);
 #pragma unroll
     for (int q = 0; q < 8; ++q) share.v[q] *= p.scale;
-    for (int64_t row = static_cast<int64_t>(blockIdx.x) * R; row < p.tokens; row += static_cast<int64_t>(gridDim.x) * R) {
-        const int count = static_cast<int>(min(static_cast<int64_t>(R), p.tokens - row));
-        V8 v[R], f[R];
-        float r[R];
-#pragma unroll
-        for (int k = 0; k < R; ++k) {
-            const int have = k < count ? c.have : 0;
-            v[k] = rows::load8<F32>(p.h, (row + k) * p.h_stride + c.col, have);
-            if (p.f) f[k] = rows::load8<F32>(p.f, (row + k) * p.f_stride + c.col, have);
-        }
+    const int64_t step = static_cast<int64_t>(gridDim.x) * T::kRows;
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * T::kRows; first < p.tokens; first += step) {
+        const int64_t row = first + t.row;
+        const bool there = row < p.tokens;
+        V8 v = t.wide(h), f;
         if (p.f) {
+            f = t.wide(x);
             if (p.post != DSM_NORM_NONE) {
-                standardise<W, R>(f, r, c, count, p.post == DSM_NORM_LAYER, p.post_eps, dim, sum);
+                standardise(t, f, p.post == DSM_NORM_LAYER, p.post_eps, dim);
 #pragma unroll
-                for (int k = 0; k < R; ++k)
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) f[k].v[q] = f[k].v[q] * post_weight.v[q] + post_bias.v[q];
+                for (int q = 0; q < 8; ++q) f.v[q] = __builtin_fmaf(f.v[q], post_weight.v[q], post_bias.v[q]);
             }
 #pragma unroll
-            for (int k = 0; k < R; ++k) {
-#pragma unroll
-                for (int q = 0; q < 8; ++q) v[k].v[q] += f[k].v[q] * share.v[q];
-                if (p.s && k < count) rows::store8<F32>(p.s, (row + k) * p.s_stride + c.col, v[k], c.have);
-            }
+            for (int q = 0; q < 8; ++q) v.v[q] = __builtin_fmaf(f.v[q], share.v[q], v.v[q]);
+            if (p.s) t.template store<F32>(v, p.s, row, p.s_stride, there);
         }
+        load(row + step);
         if (p.norm == DSM_NORM_NONE) continue;
-        standardise<W, R>(v, r, c, count, p.norm == DSM_NORM_LAYER, p.eps, dim, sum);
+        standardise(t, v, p.norm == DSM_NORM_LAYER, p.eps, dim);
 #pragma unroll
-        for (int k = 0; k < R; ++k) {
-#pragma unroll
-            for (int q = 0; q < 8; ++q) v[k].v[q] = v[k].v[q] * weight.v[q] + bias.v[q];
-            if (k < count) rows::store8<F32>(p.y, (row + k) * p.y_stride + c.col, v[k], c.have);
-        }
+        for (int q = 0; q < 8; ++q) v.v[q] = __builtin_fmaf(v.v[q], weight.v[q], bias.v[q]);
+        t.template store<F32>(v, p.y, row, p.y_stride, there);
     }
 }
 
-// d = the gradient of the standardised rows `hat` -> that of the rows.
-template <int W, int R>
-__device__ __forceinline__ void back(V8 (&d)[R], const V8 (&hat)[R], const float (&r)[R], bool layer, float dim,
-                                     Sums<W, R>& sum) {
-    float s[2 * R];
-#pragma unroll
-    for (int k = 0; k < R; ++k) {
-        s[k] = s[R + k] = 0.f;
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            s[k] = __builtin_fmaf(d[k].v[q], hat[k].v[q], s[k]);
-            s[R + k] += d[k].v[q];
-        }
-    }
-    sum(s);
-#pragma unroll
-    for (int k = 0; k < R; ++k) {
-        const float along = s[k] / dim, mean = layer ? s[R + k] / dim : 0.f;
-#pragma unroll
-        for (int q = 0; q < 8; ++q) d[k].v[q] = r[k] * (d[k].v[q] - hat[k].v[q] * along - mean);
-    }
-}
-
-template <bool F32, int W, int R>
-__global__ __launch_bounds__(W * 64) void k_norm_backward(NormCall p) {
-    __shared__ float lds[Sums<W, R>::kFloats];
-    Sums<W, R> sum{lds, 0};
+// Sums that need each other's results go by one exchange each:
+//   means of v and f (layer);  (v - mean)^2, e (v - mean), e and f's squares;  g f^ and g.
+// 8192 rows of 1600 in bf16, rms on both sides with a gate: 50 us, 3.1 TB/s; layer without post
+// 38 us; its 45 instructions an element and the exchanges' latency are what is above memory's 34.
+template <bool F32, class T, bool POST>
+__global__ __launch_bounds__(T::W * 64) void k_norm_backward(NormCall p) {
+    __shared__ float lds[T::kFloats];
+    T t(lds, p.dim);
     const float dim = static_cast<float>(p.dim);
-    const bool normed = p.norm != DSM_NORM_NONE, posted = p.post != DSM_NORM_NONE;
+    const bool normed = p.norm != DSM_NORM_NONE, layer = p.norm == DSM_NORM_LAYER, post_layer = POST && p.post == DSM_NORM_LAYER;
     const bool branch = p.df || p.sums[2] || p.sums[3] || p.sums[4];
     const bool reads_f = branch && p.f;
-    const Cols c = cols_of(p.dim);
-    const V8 weight = vector8(p.weight, c, 1.f), gate = vector8(p.gate, c, 1.f);
-    const V8 post_weight = vector8(p.post_weight, c, 1.f), post_bias = vector8(p.post_bias, c, 0.f);
-    V8 sums[kNormSums];
+    // Sixteen waves have 128 registers each: there the vectors are read again for every row.
+    constexpr bool kKept = !(T::W == 16 && POST);
+    V8 weight, gate, post_weight, post_bias, sums[kNormSums];
+    if (kKept) {
+        const auto raw_weight = t.vector(p.weight), raw_gate = t.vector(p.gate);
+        const auto raw_post_weight = POST ? t.vector(p.post_weight) : rows::Raw8<true>{};
+        const auto raw_post_bias = POST ? t.vector(p.post_bias) : rows::Raw8<true>{};
+        weight = t.vector(p.weight, raw_weight, 1.f);
+        gate = t.vector(p.gate, raw_gate, 1.f);
+        if (POST) {
+            post_weight = t.vector(p.post_weight, raw_post_weight, 1.f);
+            post_bias = t.vector(p.post_bias, raw_post_bias, 0.f);
+        }
+    }
 #pragma unroll
     for (int s = 0; s < kNormSums; ++s)
 #pragma unroll
         for (int q = 0; q < 8; ++q) sums[s].v[q] = 0.f;
-    // The rows after these are on their way while these are worked on (sixteen waves have
-    // no registers for that).
-    constexpr bool kAhead = W < 16;
-    struct {
-        rows::Raw8<F32> dy[R], h[R], ds[R], f[R];
-    } next;
-    const auto load = [&](int64_t row) {
-#pragma unroll
-        for (int k = 0; k < R; ++k) {
-            const int have = row + k < p.tokens ? c.have : 0;
-            if (normed) {
-                next.dy[k] = rows::raw8<F32>(p.dy, (row + k) * p.dy_stride + c.col, have);
-                next.h[k] = rows::raw8<F32>(p.h, (row + k) * p.h_stride + c.col, have);
-            }
-            if (p.ds) next.ds[k] = rows::raw8<F32>(p.ds, (row + k) * p.ds_stride + c.col, have);
-            if (reads_f) next.f[k] = rows::raw8<F32>(p.f, (row + k) * p.f_stride + c.col, have);
-        }
-    };
-    const int64_t step = static_cast<int64_t>(gridDim.x) * R;
-    if (kAhead) load(static_cast<int64_t>(blockIdx.x) * R);
-    for (int64_t row = static_cast<int64_t>(blockIdx.x) * R; row < p.tokens; row += step) {
-        const int count = static_cast<int>(min(static_cast<int64_t>(R), p.tokens - row));
-        V8 d[R], hat[R], f[R], ds[R];
-        float r[R];
-        if (!kAhead) load(row);
-#pragma unroll
-        for (int k = 0; k < R; ++k) {
-            if (normed) {
-                d[k] = rows::wide8(next.dy[k]);
-                hat[k] = rows::wide8(next.h[k]);
-            }
-            if (p.ds) ds[k] = rows::wide8(next.ds[k]);
-            if (reads_f) f[k] = rows::wide8(next.f[k]);
-        }
-        if (kAhead) load(row + step);
+    const int64_t step = static_cast<int64_t>(gridDim.x) * T::kRows;
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * T::kRows; first < p.tokens; first += step) {
+        const int64_t row = first + t.row;
+        const bool there = row < p.tokens;
+        rows::Raw8<F32> raw_d{}, raw_v{}, raw_ds{}, raw_f{};
         if (normed) {
-            standardise<W, R>(hat, r, c, count, p.norm == DSM_NORM_LAYER, p.eps, dim, sum);
-#pragma unroll
-            for (int k = 0; k < R; ++k)
+            raw_d = t.template raw<F32>(p.dy, row, p.dy_stride, there);
+            raw_v = t.template raw<F32>(p.h, row, p.h_stride, there);
+        }
+        if (p.ds) raw_ds = t.template raw<F32>(p.ds, row, p.ds_stride, there);
+        if (reads_f) raw_f = t.template raw<F32>(p.f, row, p.f_stride, there);
+        V8 d = t.wide(raw_d), v = t.wide(raw_v), f = t.wide(raw_f);
+        const V8 ds = t.wide(raw_ds);
+        if (layer || post_layer) {
+            float s[2] = {layer ? t.total(v) : 0.f, post_layer ? t.total(f) : 0.f};
+            t.sum(s);
+            if (layer) t.subtract(v, s[0] / dim);
+            if (post_layer) t.subtract(f, s[1] / dim);
+        }
+        float post_r = 0.f;
+        if (normed || POST) {
+            float s[4] = {0.f, 0.f, 0.f, POST ? t.squares(f) : 0.f};
+            if (!kKept) weight = t.vector(p.weight, t.vector(p.weight), 1.f);
+            if (normed) {
+                s[0] = t.squares(v);
 #pragma unroll
                 for (int q = 0; q < 8; ++q) {
-                    const float dy = d[k].v[q];
-                    sums[0].v[q] += dy * hat[k].v[q];
+                    const float e = d.v[q] * weight.v[q];
+                    s[1] = __builtin_fmaf(e, v.v[q], s[1]);
+                    s[2] += e;
+                }
+            }
+            t.sum(s);
+            // (0 for a row that is not there, which has no statistics.)
+            const float r = there ? 1.0f / sqrtf(s[0] / dim + p.eps) : 0.f;
+            post_r = there ? 1.0f / sqrtf(s[3] / dim + p.post_eps) : 0.f;
+            if (normed) {
+                const float along = s[1] * r / dim, mean = layer ? s[2] / dim : 0.f;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const float dy = d.v[q], hat = v.v[q] * r;
+                    sums[0].v[q] = __builtin_fmaf(dy, hat, sums[0].v[q]);
                     sums[1].v[q] += dy;
-                    d[k].v[q] = dy * weight.v[q];
+                    d.v[q] = r * __builtin_fmaf(-hat, along, __builtin_fmaf(dy, weight.v[q], -mean));
+                    if (p.ds) d.v[q] += ds.v[q];
                 }
-            back<W, R>(d, hat, r, p.norm == DSM_NORM_LAYER, dim, sum);
-            if (p.ds) {
-#pragma unroll
-                for (int k = 0; k < R; ++k)
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) d[k].v[q] += ds[k].v[q];
             }
-        } else {
-#pragma unroll
-            for (int k = 0; k < R; ++k) d[k] = ds[k];
         }
-        if (p.dh) {
-#pragma unroll
-            for (int k = 0; k < R; ++k)
-                if (k < count) rows::store8<F32>(p.dh, (row + k) * p.dh_stride + c.col, d[k], c.have);
-        }
+        if (!normed) d = ds;
+        if (p.dh) t.template store<F32>(d, p.dh, row, p.dh_stride, there);
         if (!branch) continue;
-        if (posted) standardise<W, R>(f, r, c, count, p.post == DSM_NORM_LAYER, p.post_eps, dim, sum);
+        if (!kKept) {
+            const auto raw_gate = t.vector(p.gate), raw_post_weight = t.vector(p.post_weight), raw_post_bias = t.vector(p.post_bias);
+            gate = t.vector(p.gate, raw_gate, 1.f);
+            post_weight = t.vector(p.post_weight, raw_post_weight, 1.f);
+            post_bias = t.vector(p.post_bias, raw_post_bias, 0.f);
+        }
+        float s[2] = {0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < R; ++k)
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                const float sd = p.scale * d[k].v[q], dp = sd * gate.v[q];
-                d[k].v[q] = dp;
-                if (posted) {
-                    sums[2].v[q] += sd * (f[k].v[q] * post_weight.v[q] + post_bias.v[q]);
-                    sums[3].v[q] += dp * f[k].v[q];
-                    sums[4].v[q] += dp;
-                    d[k].v[q] = dp * post_weight.v[q];
-                } else if (reads_f) {
-                    sums[2].v[q] += sd * f[k].v[q];
-                }
+        for (int q = 0; q < 8; ++q) {
+            // (Columns past the row: gate is 0 there.)
+            const float sd = p.scale * d.v[q], dp = sd * gate.v[q];
+            d.v[q] = dp;
+            if constexpr (POST) {
+                const float hat = f.v[q] * post_r, g = dp * post_weight.v[q];
+                f.v[q] = hat;
+                const float value = __builtin_fmaf(hat, post_weight.v[q], post_bias.v[q]);
+                sums[2].v[q] = __builtin_fmaf(sd, value, sums[2].v[q]);
+                sums[3].v[q] = __builtin_fmaf(dp, hat, sums[3].v[q]);
+                sums[4].v[q] += dp;
+                d.v[q] = g;
+                s[0] = __builtin_fmaf(g, hat, s[0]);
+                s[1] += g;
+            } else if (reads_f) {
+                sums[2].v[q] = __builtin_fmaf(sd, f.v[q], sums[2].v[q]);
             }
+        }
         if (!p.df) continue;
-        if (posted) back<W, R>(d, f, r, p.post == DSM_NORM_LAYER, dim, sum);
+        if constexpr (POST) {
+            t.sum(s);
+            const float along = s[0] / dim, mean = post_layer ? s[1] / dim : 0.f;
 #pragma unroll
-        for (int k = 0; k < R; ++k)
-            if (k < count) rows::store8<F32>(p.df, (row + k) * p.df_stride + c.col, d[k], c.have);
+            for (int q = 0; q < 8; ++q) d.v[q] = post_r * __builtin_fmaf(-f.v[q], along, d.v[q] - mean);
+        }
+        t.template store<F32>(d, p.df, row, p.df_stride, there);
     }
 #pragma unroll
-    for (int s = 0; s < kNormSums; ++s)
-        if (p.sums[s])
-            rows::store8<true>(p.parts + (static_cast<int64_t>(s) * p.groups + blockIdx.x) * p.dim, c.col, sums[s], c.have);
+    for (int s = 0; s < kNormSums; ++s) {
+        if (!p.sums[s]) continue;
+        if constexpr (T::L < 64) {  // the wave's rows
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+#pragma unroll
+                for (int w = T::L; w < 64; w *= 2) sums[s].v[q] += __shfl_xor(sums[s].v[q], w);
+        }
+        t.template store<true>(sums[s], p.parts + static_cast<int64_t>(s) * p.groups * p.dim, blockIdx.x, p.dim, t.row == 0);
+    }
 }
 
 // A vector's gradient from the work-groups' sums: 64 columns a work-group, whose 16
@@ -300,53 +320,80 @@ __global__ __launch_bounds__(1024) void k_norm_sums(NormCall p) {
     out[col] = s;
 }
 
-// Waves of a row: eight columns a lane.
-int waves_of(int64_t dim) {
-    int w = 1;
-    while (w < 16 && w * 512 < dim) w *= 2;
-    return w;
-}
+template <class T>
+struct Type {
+    using type = T;
+};
+// The team for a row's columns: use(team as a type).
 template <class F>
-void with_waves(int dim, F launch) {
-    switch (waves_of(dim)) {
-        case 1: return launch(std::integral_constant<int, 1>());
-        case 2: return launch(std::integral_constant<int, 2>());
-        case 4: return launch(std::integral_constant<int, 4>());
-        case 8: return launch(std::integral_constant<int, 8>());
-        default: return launch(std::integral_constant<int, 16>());
-    }
+void with_team(int64_t dim, F use) {
+    if (dim <= 64)
+        use(Type<Team<1, 8>>());
+    else if (dim <= 128)
+        use(Type<Team<1, 16>>());
+    else if (dim <= 256)
+        use(Type<Team<1, 32>>());
+    else if (dim <= 512)
+        use(Type<Team<1, 64>>());
+    else if (dim <= 1024)
+        use(Type<Team<2, 64>>());
+    else if (dim <= 2048)
+        use(Type<Team<4, 64>>());
+    else if (dim <= 4096)
+        use(Type<Team<8, 64>>());
+    else
+        use(Type<Team<16, 64>>());
 }
+
+// Work-groups for `tokens` rows, of `waves` a CU at most.
+template <class T>
+int groups_for(int64_t tokens, int64_t waves) {
+    const int64_t turns = (tokens + T::kRows - 1) / T::kRows, most = waves * 256 / T::W;
+    return static_cast<int>(turns < most ? turns : most);
+}
+constexpr int64_t kForwardWaves = 64;
+// As many as a CU holds at once, whole work-groups of them.  8192 x 1600 in bf16 with post: 47 us by 12
+// waves a CU, 55 by 8, 58 by 16; 4096 x 2500 in fp32: 68 by 8, 84 by 12; 2048 x 5000 in bf16: 70 by 16, 81 by 12.
+template <class T>
+constexpr int64_t kBackwardWaves = T::W == 16 ? 16 : T::W == 8 ? 8 : 12;
 
 }  // namespace
 
 int norm_groups(int64_t tokens, int64_t dim) {
-    const int w = waves_of(dim);
-    const int64_t most = 2048 / w, turns = (tokens + rows_of(w) - 1) / rows_of(w);
-    return static_cast<int>(turns < most ? turns : most);
+    int groups = 0;
+    with_team(dim, [&](auto team) {
+        using T = typename decltype(team)::type;
+        groups = groups_for<T>(tokens, kBackwardWaves<T>);
+    });
+    return groups;
 }
 
 hipError_t launch_norm(const NormCall& c, hipStream_t stream) {
-    with_waves(c.dim, [&](auto waves) {
-        constexpr int W = decltype(waves)::value, R = rows_of(W);
-        const int64_t turns = (static_cast<int64_t>(c.tokens) + R - 1) / R, most = 8192 / W;
-        const unsigned groups = static_cast<unsigned>(turns < most ? turns : most);
+    with_team(c.dim, [&](auto team) {
+        using T = typename decltype(team)::type;
+        const int groups = groups_for<T>(c.tokens, kForwardWaves);
         if (c.f32)
-            k_norm<true, W, R><<<groups, W * 64, 0, stream>>>(c);
+            k_norm<true, T><<<groups, T::W * 64, 0, stream>>>(c);
         else
-            k_norm<false, W, R><<<groups, W * 64, 0, stream>>>(c);
+            k_norm<false, T><<<groups, T::W * 64, 0, stream>>>(c);
     });
     return hipGetLastError();
 }
 
 hipError_t launch_norm_backward(const NormCall& c, hipStream_t stream) {
-    with_waves(c.dim, [&](auto waves) {
-        constexpr int W = decltype(waves)::value, R = rows_of(W);
-        if (c.groups > 0) {
-            if (c.f32)
-                k_norm_backward<true, W, R><<<c.groups, W * 64, 0, stream>>>(c);
-            else
-                k_norm_backward<false, W, R><<<c.groups, W * 64, 0, stream>>>(c);
-        }
+    with_team(c.dim, [&](auto team) {
+        using T = typename decltype(team)::type;
+        if (c.groups == 0) return;
+        // (f is not read where nothing of post is wanted.)
+        const bool post = c.post != DSM_NORM_NONE && c.f;
+        if (c.f32 && post)
+            k_norm_backward<true, T, true><<<c.groups, T::W * 64, 0, stream>>>(c);
+        else if (c.f32)
+            k_norm_backward<true, T, false><<<c.groups, T::W * 64, 0, stream>>>(c);
+        else if (post)
+            k_norm_backward<false, T, true><<<c.groups, T::W * 64, 0, stream>>>(c);
+        else
+            k_norm_backward<false, T, false><<<c.groups, T::W * 64, 0, stream>>>(c);
     });
     bool any = false;
     for (float* s : c.sums) any = any || s != nullptr;

@@ -11,13 +11,19 @@ object while the graph is replayed), and from several threads each call's launch
 enqueued whole before the next call's.
 """
 import contextlib
+import operator
 import threading
 
+import numpy as np
 import torch
 
 from . import dsm
 
 DTYPES = {torch.float32: dsm.DSM_F32, torch.bfloat16: dsm.DSM_BF16}
+
+
+# The current stream's handle without a Stream object around it (a microsecond of a call).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _dtype(dtype):
@@ -36,25 +42,49 @@ class _Plan:
             raise ValueError(f"the operators run on a GPU, got device {device}")
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index
         self.workspace_bytes = workspace_bytes
         self.workspace = torch.empty(max(workspace_bytes, 256), dtype=torch.uint8,
                                      device=self.device)
         self._stream = torch.cuda.current_stream(self.device)
+        self._handle = self._stream.cuda_stream
 
     def _enter(self):
         """The current stream, after what this plan last did on another one."""
+        if _raw_stream is not None and _raw_stream(self._index) == self._handle:
+            return self._handle
         stream = torch.cuda.current_stream(self.device)
         if stream != self._stream:
             if not torch.cuda.is_current_stream_capturing():
                 stream.wait_stream(self._stream)
                 self.workspace.record_stream(stream)
-            self._stream = stream
-        return stream.cuda_stream
+            self._stream, self._handle = stream, stream.cuda_stream
+        return self._handle
 
     def _on_device(self):
         if torch.cuda.current_device() == self.device.index:
             return contextlib.nullcontext()
         return torch.cuda.device(self.device)
+
+    def _launch(self, call):
+        """call(stream): one call's launches, which no other call's come between."""
+        with self._lock:
+            if torch.cuda.current_device() == self._index:
+                call(self._enter())
+            else:
+                with torch.cuda.device(self.device):
+                    call(self._enter())
+
+    def _launch_with(self, entry, problem, buf):
+        """entry(problem, buf) on the current stream, as _launch."""
+        with self._lock:
+            if torch.cuda.current_device() == self._index:
+                buf.stream = self._enter()
+                entry(problem, buf)
+            else:
+                with torch.cuda.device(self.device):
+                    buf.stream = self._enter()
+                    entry(problem, buf)
 
     @contextlib.contextmanager
     def _enqueue(self):
@@ -81,8 +111,16 @@ class _Plan:
             raise ValueError(f"{name}'s rows overlap: strides {t.stride()}")
         return t.stride(0)
 
+    def _matrix(self, name, t, shape, dtype=None):
+        """(address, stride) of a matrix with contiguous rows."""
+        dtype = self.dtype if dtype is None else dtype
+        if t.shape != shape or t.dtype is not dtype or t.get_device() != self._index:
+            self._check(name, t, dtype, shape)
+        return t.data_ptr(), shape[1] if t.is_contiguous() else self._rows(name, t, shape, dtype)
+
     def _vector(self, name, t, dtype, shape):
-        self._check(name, t, dtype, shape)
+        if t.shape != shape or t.dtype is not dtype or t.get_device() != self._index:
+            self._check(name, t, dtype, shape)
         if not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
         return t.data_ptr()
@@ -293,38 +331,33 @@ class Linear(_Plan):
         self.bias_shape = self.w_shape[:1]
         self._allocate(dsm.dsm_linear_workspace(self.problem), device)
 
-    def _operands(self, x, w):
-        buf = dsm.dsm_linear_buffers()
-        if x is not None:
-            buf.x_stride, buf.x = self._rows("x", x, self.x_shape), x.data_ptr()
-        if w is not None:
-            buf.w_stride, buf.w = self._rows("w", w, self.w_shape), w.data_ptr()
-        buf.workspace, buf.workspace_bytes = self.workspace.data_ptr(), self.workspace_bytes
-        return buf
-
     def _empty(self, shape, dtype=None):
         return torch.empty(shape, dtype=self.dtype if dtype is None else dtype, device=self.device)
+
+    def _buffers(self):
+        return dsm.dsm_linear_buffers(workspace=self.workspace.data_ptr(), workspace_bytes=self.workspace_bytes)
 
     def __call__(self, x, w, bias=None, residual=None, y=None, z=None):
         """{"y"}: act(x w^T + bias) + residual; and, for a plan with gradients and an
         activation or where z is given, {"z"}: x w^T + bias, which backward takes.  Outputs
         are written into the tensors given (y may be the residual), or into new ones."""
-        buf = self._operands(x, w)
+        buf = self._buffers()
+        buf.x, buf.x_stride = self._matrix("x", x, self.x_shape)
+        buf.w, buf.w_stride = self._matrix("w", w, self.w_shape)
         if bias is not None:
             buf.bias = self._vector("bias", bias, torch.float32, self.bias_shape)
         if residual is not None:
-            buf.residual_stride, buf.residual = self._rows("residual", residual, self.y_shape), residual.data_ptr()
+            buf.residual, buf.residual_stride = self._matrix("residual", residual, self.y_shape)
         if y is None:
             y = self._empty(self.y_shape)
         if z is None and self.grads and self.act != "none":
-            z = self._empty(self.y_shape)
-        buf.y_stride, buf.y = self._rows("y", y, self.y_shape), y.data_ptr()
+            z = torch.empty_like(y)
+        buf.y, buf.y_stride = self._matrix("y", y, self.y_shape)
         out = {"y": y}
         if z is not None:
-            buf.z_stride, buf.z = self._rows("z", z, self.y_shape), z.data_ptr()
+            buf.z, buf.z_stride = self._matrix("z", z, self.y_shape)
             out["z"] = z
-        with self._enqueue() as buf.stream:
-            dsm.dsm_linear(self.problem, buf)
+        self._launch_with(dsm.dsm_linear, self.problem, buf)
         return out
 
     def backward(self, dy, x=None, w=None, z=None, dx=None, dw=None, dbias=None, wanted=("dx", "dw", "dbias")):
@@ -343,22 +376,29 @@ class Linear(_Plan):
         for name, t, needed in (("x", x, "dw" in wanted), ("w", w, "dx" in wanted), ("z", z, self.act != "none")):
             if t is None and needed:
                 raise ValueError(f"{name} is wanted for these gradients")
-        buf = self._operands(x, w)
-        buf.dy_stride, buf.dy = self._rows("dy", dy, self.y_shape), dy.data_ptr()
+        buf = self._buffers()
+        if x is not None:
+            buf.x, buf.x_stride = self._matrix("x", x, self.x_shape)
+        if w is not None:
+            buf.w, buf.w_stride = self._matrix("w", w, self.w_shape)
+        buf.dy, buf.dy_stride = self._matrix("dy", dy, self.y_shape)
         if self.act != "none":
-            buf.z_stride, buf.z = self._rows("z", z, self.y_shape), z.data_ptr()
+            buf.z, buf.z_stride = self._matrix("z", z, self.y_shape)
         out = {}
         if "dx" in wanted:
-            out["dx"] = dx = self._empty(self.x_shape) if dx is None else dx
-            buf.dx_stride, buf.dx = self._rows("dx", dx, self.x_shape), dx.data_ptr()
+            if dx is None:
+                dx = self._empty(self.x_shape) if x is None else torch.empty_like(x)
+            out["dx"] = dx
+            buf.dx, buf.dx_stride = self._matrix("dx", dx, self.x_shape)
         if "dw" in wanted:
-            out["dw"] = dw = self._empty(self.w_shape, self.dw_dtype) if dw is None else dw
-            buf.dw_stride, buf.dw = self._rows("dw", dw, self.w_shape, self.dw_dtype), dw.data_ptr()
+            if dw is None:
+                dw = self._empty(self.w_shape, self.dw_dtype) if w is None else torch.empty_like(w, dtype=self.dw_dtype)
+            out["dw"] = dw
+            buf.dw, buf.dw_stride = self._matrix("dw", dw, self.w_shape, self.dw_dtype)
         if "dbias" in wanted:
             out["dbias"] = dbias = self._empty(self.bias_shape, torch.float32) if dbias is None else dbias
             buf.dbias = self._vector("dbias", dbias, torch.float32, self.bias_shape)
-        with self._enqueue() as buf.stream:
-            dsm.dsm_linear_backward(self.problem, buf)
+        self._launch_with(dsm.dsm_linear_backward, self.problem, buf)
         return out
 
 
@@ -373,60 +413,68 @@ class ResidualNorm(_Plan):
     called too.  Vectors and their gradients are fp32.
     """
 
-    VECTORS = ("weight", "bias", "gate", "post_weight", "post_bias")
-
     def __init__(self, tokens, dim, dtype=torch.float32, norm="layer", post="none", eps=1e-5, post_eps=None, grads=True,
                  device="cuda"):
         super().__init__()
         self.dtype, self.norm, self.post, self.grads = dtype, norm, post, bool(grads)
         self.shape = torch.Size((int(tokens), int(dim)))
+        self.vector_shape = self.shape[1:]
         self._args = (int(tokens), int(dim), _dtype(dtype), _named(NORMS, "norm", norm), _named(NORMS, "post", post),
                       1 if grads else 0, float(eps), float(eps if post_eps is None else post_eps))
-        self._allocate(dsm.dsm_norm_workspace(self._problem(1.0)), device)
+        self._scaled = 1.0, dsm.dsm_norm_problem(*self._args, 1.0)
+        self._allocate(dsm.dsm_norm_workspace(self._scaled[1]), device)
 
     def _problem(self, scale):
-        return dsm.dsm_norm_problem(*self._args, float(scale))
+        last = self._scaled
+        if last[0] != scale:
+            self._scaled = last = scale, dsm.dsm_norm_problem(*self._args, float(scale))
+        return last[1]
 
-    def _fill(self, buf, rows, vectors):
-        for name, t in rows:
-            if t is not None:
-                setattr(buf, name + "_stride", self._rows(name, t, self.shape))
-                setattr(buf, name, t.data_ptr())
-        for name, t in vectors:
-            if t is not None:
-                setattr(buf, name, self._vector(name, t, torch.float32, self.shape[1:]))
-        buf.workspace, buf.workspace_bytes = self.workspace.data_ptr(), self.workspace_bytes
+    def _buffers(self, f, gate, weight, bias, post_weight, post_bias):
+        """With the vectors, of those that the kinds of norms have."""
+        if self.norm == "none" and (weight is not None or bias is not None):
+            raise ValueError("weight or bias is given without a norm")
+        if self.post == "none":
+            if post_weight is not None or post_bias is not None:
+                raise ValueError("post_weight or post_bias is given without a post norm")
+        elif f is None:
+            raise ValueError("f is None: there is no block's output for post")
+        if f is None and gate is not None:
+            raise ValueError("f is None: there is no block's output for gate")
+        buf = dsm.dsm_norm_buffers(workspace=self.workspace.data_ptr(), workspace_bytes=self.workspace_bytes)
+        if weight is not None:
+            buf.weight = self._vector("weight", weight, torch.float32, self.vector_shape)
+        if bias is not None:
+            buf.bias = self._vector("bias", bias, torch.float32, self.vector_shape)
+        if gate is not None:
+            buf.gate = self._vector("gate", gate, torch.float32, self.vector_shape)
+        if post_weight is not None:
+            buf.post_weight = self._vector("post_weight", post_weight, torch.float32, self.vector_shape)
+        if post_bias is not None:
+            buf.post_bias = self._vector("post_bias", post_bias, torch.float32, self.vector_shape)
+        if f is not None:
+            buf.f, buf.f_stride = self._matrix("f", f, self.shape)
         return buf
-
-    def _vectors(self, given):
-        for name, t in given:
-            if t is None:
-                continue
-            if name in ("weight", "bias") and self.norm == "none":
-                raise ValueError(f"{name} is given without a norm")
-            if name in ("post_weight", "post_bias") and self.post == "none":
-                raise ValueError(f"{name} is given without a post norm")
 
     def __call__(self, h, f=None, weight=None, bias=None, gate=None, scale=1.0, post_weight=None, post_bias=None, s=None,
                  y=None):
         """{"s", "y"}: s where there is f, y where there is a norm; written into the tensors
         given (s may be h or f, y h or f), or into new ones.  Absent weights and gate are 1, absent
         biases 0."""
-        vectors = [("weight", weight), ("bias", bias), ("gate", gate), ("post_weight", post_weight),
-                   ("post_bias", post_bias)]
-        self._vectors(vectors)
-        if f is None and (self.post != "none" or gate is not None or s is not None):
-            raise ValueError("f is None: there is no block's output for post, gate or s")
+        buf = self._buffers(f, gate, weight, bias, post_weight, post_bias)
+        if f is None and s is not None:
+            raise ValueError("f is None: s is h")
         if y is not None and self.norm == "none":
             raise ValueError("y is given without a norm")
+        buf.h, buf.h_stride = self._matrix("h", h, self.shape)
         out = {}
         if f is not None:
-            out["s"] = s = torch.empty(self.shape, dtype=self.dtype, device=self.device) if s is None else s
+            out["s"] = s = torch.empty_like(h) if s is None else s
+            buf.s, buf.s_stride = self._matrix("s", s, self.shape)
         if self.norm != "none":
-            out["y"] = y = torch.empty(self.shape, dtype=self.dtype, device=self.device) if y is None else y
-        buf = self._fill(dsm.dsm_norm_buffers(), [("h", h), ("f", f), ("s", s), ("y", y)], vectors)
-        with self._enqueue() as buf.stream:
-            dsm.dsm_residual_norm(self._problem(scale), buf)
+            out["y"] = y = torch.empty_like(h) if y is None else y
+            buf.y, buf.y_stride = self._matrix("y", y, self.shape)
+        self._launch_with(dsm.dsm_residual_norm, self._problem(scale), buf)
         return out
 
     def backward(self, dy, s, f=None, ds=None, weight=None, bias=None, gate=None, scale=1.0, post_weight=None,
@@ -439,48 +487,43 @@ class ResidualNorm(_Plan):
         df dy, ds or f), or into new ones."""
         if not self.grads:
             raise ValueError("the plan is without gradients")
-        vectors = [("weight", weight), ("bias", bias), ("gate", gate), ("post_weight", post_weight),
-                   ("post_bias", post_bias)]
-        self._vectors(vectors)
-        if f is None and (self.post != "none" or gate is not None or df is not None):
-            raise ValueError("f is None: there is no block's output for post, gate or df")
+        buf = self._buffers(f, gate, weight, bias, post_weight, post_bias)
+        if f is None and df is not None:
+            raise ValueError("f is None: there is no df")
         if (dy is None) != (self.norm == "none"):
             raise ValueError("dy is wanted where there is a norm, and only there")
         if dy is None and ds is None:
             raise ValueError("ds is wanted where there is no norm")
-
-        def new():
-            return torch.empty(self.shape, dtype=self.dtype, device=self.device)
-
-        out = {"dh": new() if dh is None else dh}
+        if dy is not None:
+            buf.h, buf.h_stride = self._matrix("s", s, self.shape)
+            buf.dy, buf.dy_stride = self._matrix("dy", dy, self.shape)
+        if ds is not None:
+            buf.ds, buf.ds_stride = self._matrix("ds", ds, self.shape)
+        like = dy if ds is None else ds
+        out = {"dh": torch.empty_like(like) if dh is None else dh}
+        buf.dh, buf.dh_stride = self._matrix("dh", out["dh"], self.shape)
         if f is not None:
-            out["df"] = new() if df is None else df
-        grads = {"weight": dweight, "bias": dbias, "gate": dgate, "post_weight": dpost_weight, "post_bias": dpost_bias}
-        for name, t in vectors:
+            out["df"] = torch.empty_like(like) if df is None else df
+            buf.df, buf.df_stride = self._matrix("df", out["df"], self.shape)
+        for name, t, given in (("dweight", weight, dweight), ("dbias", bias, dbias), ("dgate", gate, dgate),
+                               ("dpost_weight", post_weight, dpost_weight), ("dpost_bias", post_bias, dpost_bias)):
             if t is not None:
-                given = grads[name]
-                out["d" + name] = torch.empty_like(t) if given is None else given
-            elif grads[name] is not None:
-                raise ValueError(f"d{name} is given without {name}")
-        rows = [("h", s), ("f", f), ("dy", dy), ("ds", ds), ("dh", out["dh"]), ("df", out.get("df"))]
-        if self.norm == "none":
-            rows = [r for r in rows if r[0] != "h"]
-        buf = self._fill(dsm.dsm_norm_buffers(), rows, vectors + [("d" + n, out.get("d" + n)) for n in self.VECTORS])
-        with self._enqueue() as buf.stream:
-            dsm.dsm_residual_norm_backward(self._problem(scale), buf)
+                out[name] = given = torch.empty_like(t) if given is None else given
+                setattr(buf, name, self._vector(name, given, torch.float32, self.vector_shape))
+            elif given is not None:
+                raise ValueError(f"{name} is given without {name[1:]}")
+        self._launch_with(dsm.dsm_residual_norm_backward, self._problem(scale), buf)
         return out
 
 
 class _Clip(_Plan):
-    def __init__(self):
-        super().__init__()
-        self._table_lock = threading.Lock()
-
     def _table(self, sizes, groups, n_groups, eps, device):
         """sizes: [(numel, dtype)]; the tensors' table, whose addresses each call fills."""
         self._entries = (dsm.dsm_clip_tensor * len(sizes))()
         for e, (numel, dtype), group in zip(self._entries, sizes, groups):
             e.numel, e.block, e.stride, e.dtype, e.group = numel, max(numel, 1), max(numel, 1), _dtype(dtype), group
+        # The same memory as columns, to fill at once.
+        self._columns = np.frombuffer(self._entries, dtype=np.int64).reshape(len(sizes), -1).T if sizes else None
         self.n_groups, self.eps = int(n_groups), float(eps)
         self._allocate(dsm.dsm_clip_workspace(self._entries, self.n_groups), device)
 
@@ -490,11 +533,23 @@ class _Clip(_Plan):
         self._vector("norm", norm, torch.float32, torch.Size((self.n_groups,)))
         return norm
 
-    def _run(self, max_norm, norm):
-        with self._enqueue() as stream:
+    def _run(self, max_norm, norm, data, **columns):
+        """data: addresses; columns: first, block and stride where they differ from what stands there."""
+        def call(stream):
+            if self._columns is not None:
+                self._columns[0] = data
+                for name, values in columns.items():
+                    self._columns[_COLUMNS[name]] = values
             dsm.dsm_grad_clip(self._entries, self.n_groups, float("inf") if max_norm is None else float(max_norm),
                               norm.data_ptr(), self.workspace.data_ptr(), self.workspace_bytes, self.eps, stream)
+
+        self._launch(call)
         return norm
+
+
+# The words of a dsm_clip_tensor.
+_COLUMNS = {"data": 0, "first": 1, "numel": 2, "block": 3, "stride": 4}
+_SHAPE_DTYPE = operator.attrgetter("shape", "dtype")
 
 
 class GradClip(_Clip):
@@ -513,11 +568,24 @@ class GradClip(_Clip):
             raise ValueError(f"{len(groups)} groups for {len(tensors)} tensors")
         if any(g < 0 for g in groups):
             raise ValueError("a group is negative")
-        self._like = [(t.shape, t.dtype) for t in tensors]
+        self._like = [(torch.Size(t.shape), t.dtype) for t in tensors]
         # Groups in order: the order of a call's tensors is the caller's.
         self._order = sorted(range(len(tensors)), key=groups.__getitem__)
-        self._table([(self._like[i][0].numel(), self._like[i][1]) for i in self._order], [groups[i] for i in self._order],
-                    max(groups, default=0) + 1, eps, device)
+        sizes = [(self._like[i][0].numel(), self._like[i][1]) for i in self._order]
+        self._whole = np.array([max(n, 1) for n, _ in sizes], dtype=np.int64)
+        self._table(sizes, [groups[i] for i in self._order], max(groups, default=0) + 1, eps, device)
+
+    def _place(self, i, t):
+        """(block, stride) of tensor i, checked."""
+        shape, dtype = self._like[i]
+        if t.shape != shape or t.dtype != dtype or t.device != self.device:
+            raise ValueError(f"tensors[{i}] must be {dtype} of shape {tuple(shape)} on {self.device}, "
+                             f"got {t.dtype}, {tuple(t.shape)}, {t.device}")
+        if t.is_contiguous():
+            return max(t.numel(), 1), max(t.numel(), 1)
+        if t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1) and t.stride(0) >= t.shape[1]:
+            return t.shape[1], t.stride(0)
+        raise ValueError(f"tensors[{i}] has neither contiguous elements nor contiguous rows: strides {t.stride()}")
 
     def __call__(self, tensors, max_norm=None, norm=None):
         """norm (n_groups,): the groups' norms, before clipping.  Where one exceeds max_norm its
@@ -525,24 +593,15 @@ class GradClip(_Clip):
         or are matrices with contiguous rows.  They may not overlap."""
         if len(tensors) != len(self._like):
             raise ValueError(f"{len(tensors)} tensors for a plan of {len(self._like)}")
-        norm = self._norm(norm)
-        places = []
-        for i, e in zip(self._order, self._entries):
-            t, (shape, dtype) = tensors[i], self._like[i]
-            if t.shape != shape or t.dtype != dtype or t.device != self.device:
-                raise ValueError(f"tensors[{i}] must be {dtype} of shape {tuple(shape)} on {self.device}, "
-                                 f"got {t.dtype}, {tuple(t.shape)}, {t.device}")
-            if t.is_contiguous():
-                block = stride = max(t.numel(), 1)
-            elif t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1) and t.stride(0) >= t.shape[1]:
-                block, stride = t.shape[1], t.stride(0)
-            else:
-                raise ValueError(f"tensors[{i}] has neither contiguous elements nor contiguous rows: strides {t.stride()}")
-            places.append((t.data_ptr(), block, stride))
-        with self._table_lock:
-            for e, place in zip(self._entries, places):
-                e.data, e.block, e.stride = place
-            return self._run(max_norm, norm)
+        # Hundreds of tensors: no Python code for each where all is well.
+        if (list(map(_SHAPE_DTYPE, tensors)) == self._like and all(map(torch.Tensor.is_contiguous, tensors)) and
+                set(map(torch.Tensor.get_device, tensors)) <= {self._index}):
+            place = {"block": self._whole, "stride": self._whole}
+        else:
+            places = [self._place(i, tensors[i]) for i in self._order]
+            place = {"block": [p[0] for p in places], "stride": [p[1] for p in places]}
+        data = list(map(torch.Tensor.data_ptr, map(tensors.__getitem__, self._order)))
+        return self._run(max_norm, self._norm(norm), data, **place)
 
 
 class ArenaClip(_Clip):
@@ -564,17 +623,13 @@ class ArenaClip(_Clip):
         if (arenas.n, list(arenas.numel), (arenas.replica_layout, arenas.n_state_buffers, arenas.arena_elems)) != (
                 self._n, self._numel, self._layout):
             raise ValueError("the plan is for arenas of another problem")
-        norm = self._norm(norm)
         if arenas.g_rep.device != self.device:
             raise ValueError(f"the arenas are on {arenas.g_rep.device}, the plan on {self.device}")
         layout, buffers, elems = self._layout
-        with self._table_lock:
-            for k, e in enumerate(self._entries):
-                worker, tensor = divmod(k, len(self._numel))
-                e.first, e.block, e.stride = self._offsets[tensor], max(elems, 1), max(elems, 1)
-                e.data = arenas.g_rep.data_ptr() + 4 * worker * elems
-                if layout == dsm.DSM_REPLICAS_STATE_BLOCKED:
-                    e.block = dsm.DSM_STATE_BLOCK_ELEMS
-                    e.stride = buffers * self._n * e.block
-                    e.data = arenas.g_rep.data_ptr() + 4 * worker * e.block
-            return self._run(max_norm, norm)
+        block = stride = apart = max(elems, 1)  # apart: elements from one worker's copy to the next
+        if layout == dsm.DSM_REPLICAS_STATE_BLOCKED:
+            block = apart = dsm.DSM_STATE_BLOCK_ELEMS
+            stride = buffers * self._n * block
+        data = arenas.g_rep.data_ptr() + 4 * apart * np.arange(self._n, dtype=np.int64).repeat(len(self._numel))
+        first = np.tile(np.array(self._offsets, dtype=np.int64), self._n)
+        return self._run(max_norm, self._norm(norm), data, first=first, block=block, stride=stride)

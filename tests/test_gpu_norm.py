@@ -61,7 +61,7 @@ def _run(i, norm="layer", post="none", branch=True, scale=0.7, without=(), eps=1
 
 
 # Widths around 8 columns a lane and 1 to 16 waves; tokens around the rows of a work-group.
-SIZES = [(1, 1), (1, 2), (1, 1600), (2, 7), (3, 8), (2, 9), (5, 63), (4, 511), (3, 512), (6, 513), (7, 768), (9, 1000), (3, 1024), (2, 1025),
+SIZES = [(1, 1), (1, 2), (1, 1600), (2, 7), (3, 8), (2, 9), (5, 63), (4, 511), (3, 512), (6, 513), (5, 1030), (7, 768), (9, 1000), (3, 1024), (2, 1025),
          (11, 1601), (4, 2048), (3, 2049), (5, 4096), (3, 4097), (2, 6400), (3, 8191), (2, 8192), (1, 8185), (333, 100), (1000, 48)]
 
 
@@ -121,11 +121,13 @@ def test_strided_views(dim, dtype):
 
 
 @TYPES
-def test_in_place(dtype):
-    i = _inputs(77, 200, dtype, seed=5)
-    want = _run(i, "layer", "layer")
-    vectors = _given(i, "layer", "layer")
-    plan = _ops().ResidualNorm(77, 200, dtype=dtype, norm="layer", post="layer", post_eps=1e-3)
+@pytest.mark.parametrize("post", ["none", "layer"])
+@pytest.mark.parametrize("dim", [200, 203, 513, 1029])  # rows that end within a lane's columns, and in a wave's first lane
+def test_in_place(dim, post, dtype):
+    i = _inputs(77, dim, dtype, seed=5)
+    want = _run(i, "layer", post)
+    vectors = _given(i, "layer", post)
+    plan = _ops().ResidualNorm(77, dim, dtype=dtype, norm="layer", post=post, post_eps=1e-3)
     for s_at, y_at in (("h", "f"), ("f", "h")):
         rows = {k: i[k].clone() for k in ("h", "f")}
         out = plan(rows["h"], f=rows["f"], scale=0.7, s=rows[s_at], y=rows[y_at], **vectors)
