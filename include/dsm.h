@@ -577,8 +577,8 @@ DSM_API dsm_status dsm_linear(const dsm_linear_problem* problem, const dsm_linea
  * dsm_linear_backward - the gradients of dsm_linear's y, given dy and z:
  *   dz = dy act'(z);  dx = dz w;  dw = dz^T x;  dbias = the tokens' sum of dz
  * (the residual's gradient is dy itself).  Outputs are written, not added to; any may be
- * NULL.  Where there is an activation, bf16 takes dz rounded to bf16 into the products,
- * and in fp32 into dbias.  Products of fp32 carry 22 bits or more of entries of dz
+ * NULL.  Where there is an activation, bf16 takes dz rounded to bf16 into dx and a bf16
+ * dw, as two bf16 halves (16 bits) into an fp32 dw, and in fp32 into dbias.  Products of fp32 carry 22 bits or more of entries of dz
  * down to 2^-16 of their token's largest, of w of its largest, and of x of the largest
  * that a token's x and dz make together.
  * dx, dw and dbias may not overlap what is read.  Errors: DSM_ERR_INVALID_ARG; DSM_ERR_HIP.

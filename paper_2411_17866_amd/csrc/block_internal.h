@@ -72,13 +72,17 @@ hipError_t launch_norm_backward(const NormCall& c, hipStream_t stream);
 
 constexpr int kLinearFew = 64;       // tokens that are answered by one launch without tiles
 constexpr int kLinearTopParts = 512; // work-groups that look for w's largest magnitude
-constexpr int kDzRows = 64;          // tokens of a work-group that makes dz (bf16)
-constexpr int kDzSplitRows = 8;      // (fp32)
+constexpr int kDzRows = 64;          // tokens of a work-group that makes dz
+constexpr int kDzSplitRows = 8;      // (as halves)
+
+enum LinearForm { kLinearBf16, kLinearHalves, kLinearSingle };  // what the products' operands hold (linear.hip)
 
 // How a problem is cut and where the parts of the workspace lie (bytes from its start).
 struct LinearPlan {
     int32_t tokens, dim, wide, act;
     int32_t f32, dw_f32;
+    int32_t dz_halves;           // dz is two bf16 arrays, for dw
+    LinearForm form, back_form;
     int32_t few;                 // forward: no tiles
     int32_t tile, splits;        // forward: tile, and parts that its sums run over side by side
     int32_t front;               // tile columns of 256; tiles of 128 take what follows
@@ -88,8 +92,8 @@ struct LinearPlan {
     int64_t pad_tokens;          // rows of dz
     int64_t ld_y, ld_dx;         // floats of a row of the parts of y; of dx and dw
     int64_t x, w, dz;            // operands, where they are not read in place
-    int64_t x_exp, w_exp, z_exp; // fp32: powers of two of the rows of x, w and dz
-    int64_t w_tops, tops;        // fp32, backward: largest magnitudes of w by work-group; least exponents of x dz
+    int64_t x_exp, w_exp, z_exp; // halves: powers of two of the rows of x, w and dz
+    int64_t w_tops, tops;        // halves, backward: largest magnitudes of w by work-group; least exponents of x dz
     int64_t y_parts, dx_parts, dw_parts, bias_sums;
     int64_t forward_bytes, backward_bytes;
 };

@@ -41,12 +41,16 @@ constexpr int kMaxSplits = 16;
 struct Turn {
     double full[3], alone[3], end[3], f32;
 };
+constexpr Turn kSingle = {{1.7, 0.0, 0.0}, {0.95, 0.0, 0.0}, {2.5, 0.0, 0.0}, 1.0};
 constexpr Turn kForward = {{0.43, 0.97, 1.45}, {0.28, 0.55, 1.45}, {2.2, 5.0, 8.0}, 2.0};
 constexpr Turn kBackward = {{0.50, 1.04, 1.66}, {0.58, 0.88, 1.26}, {3.0, 5.0, 10.0}, 2.42};
 // Joining `parts` parts of n numbers: a launch, and what is moved.
 double join_time(int parts, int64_t n, double each) {
     return parts > 1 ? 4.4 + each * 2e-6 * static_cast<double>(n * parts) : 0.0;
 }
+
+// fp32 products as they are up to this many tokens.
+constexpr int64_t kSingleForward = 128, kSingleBackward = 64;
 
 // Tile columns: the last of 256 takes half as long where 128 columns of it lie past the end.
 double columns(int64_t n, int of) {
@@ -59,7 +63,9 @@ double columns(int64_t n, int of) {
 // by 24 columns of 256 and 128 tiles of 128; 176 by 256 or 128 alone.
 void cut_forward(dsm::LinearPlan* q) {
     const int64_t T = q->tokens, D = q->dim, N = q->wide, steps = tiles(D, 64);
-    const double f32 = q->f32 ? kForward.f32 : 1.0;
+    const bool single = q->form == dsm::kLinearSingle;
+    const Turn& of = single ? kSingle : kForward;
+    const double f32 = q->f32 ? of.f32 : 1.0;
     double best = 0.0;
     const auto take = [&](double cost, int tile, int splits, int64_t front) {
         if (best != 0.0 && cost >= best) return;
@@ -71,11 +77,11 @@ void cut_forward(dsm::LinearPlan* q) {
     // Turns of n tiles of `i`, the last of which may leave CUs half filled.
     const auto turns = [&](int64_t n, int i, int64_t k) {
         const int64_t slots = static_cast<int64_t>(kSlots[i]), whole = n / slots, rest = n % slots;
-        const double full = static_cast<double>(k) * kForward.full[i] * f32 + kForward.end[i];
-        const double last = rest == 0 ? 0.0 : rest <= 256 ? static_cast<double>(k) * kForward.alone[i] * f32 + kForward.end[i] : full;
+        const double full = static_cast<double>(k) * of.full[i] * f32 + of.end[i];
+        const double last = rest == 0 ? 0.0 : rest <= 256 ? static_cast<double>(k) * of.alone[i] * f32 + of.end[i] : full;
         return static_cast<double>(whole) * full + last;
     };
-    for (int i = 0; i < 3; ++i) {
+    for (int i = 0; i < (single ? 1 : 3); ++i) {
         const int64_t rows = tiles(T, kTiles[i]), all = tiles(N, kTiles[i]);
         for (int s = 1; s <= kMaxSplits && (s == 1 || s * 4 <= steps); ++s) {
             take(turns(rows * all * s, i, tiles(steps, s)) + join_time(s, T * N, 1.0), kTiles[i], s, all);
@@ -111,21 +117,40 @@ int few_splits(const dsm::LinearPlan& q) {
 
 // The gradients: dx and dw run side by side.  The work over the CUs, and a part of the longest tile
 // for the uneven end.
+// (Rows of one product by tiles of 128 behind tiles of 256, as forward, gained at most 2%: 4093 x 1600 x 6400.)
 void cut_backward(dsm::LinearPlan* q) {
     const int64_t T = q->tokens, D = q->dim, N = q->wide;
     const double f32 = q->f32 ? kBackward.f32 : 1.0;
     double best = 0.0;
+    if (q->back_form == dsm::kLinearSingle) {
+        // One row of tiles of 64 for dx; dw's tiles have a step or two and run beside them.
+        q->back_tile = 64;
+        const int64_t steps = tiles(N, 64), cols = tiles(T, 64) * tiles(D, 64);
+        for (int s = 1; s <= kMaxSplits && (s == 1 || s * 256 <= N); ++s) {
+            const double turns = std::ceil(static_cast<double>(cols * s) / 512);
+            const double cost = turns * (static_cast<double>(tiles(steps, s)) * (cols * s > 256 ? kSingle.full[0] : kSingle.alone[0]) + 2.5) +
+                                join_time(s, T * D, 0.25);
+            if (best == 0.0 || cost < best) {
+                best = cost;
+                q->dx_splits = s;
+            }
+        }
+        return;
+    }
     for (int i = 0; i < 3; ++i) {
         const int of = kTiles[i];
         const double dx = static_cast<double>(tiles(T, of)) * columns(D, of), dw = static_cast<double>(tiles(N, of)) * columns(D, of);
         const auto time = [&](int64_t k, const double* step) { return static_cast<double>(k) * step[i] * f32 + kBackward.end[i]; };
+        const auto cost_of = [&](int sx, int sw) {
+            const int64_t kx = tiles(tiles(N, 64), sx), kw = tiles(tiles(T, 64), sw) * (q->dz_halves ? 2 : 1);
+            const double work = (dx * sx * time(kx, kBackward.full) + dw * sw * time(kw, kBackward.full)) / kSlots[i];
+            const double longest = time(std::max(kx, kw), kBackward.alone);
+            const double joins = join_time(sx, T * D, 0.25) + join_time(sw, N * D, 0.25) - (sx > 1 && sw > 1 ? 4.4 : 0.0);
+            return std::max(work + 0.40 * longest, longest) + joins;
+        };
         for (int sx = 1; sx <= kMaxSplits && (sx == 1 || sx * 256 <= N); ++sx)
             for (int sw = 1; sw <= kMaxSplits && (sw == 1 || sw * 256 <= T); ++sw) {
-                const int64_t kx = tiles(tiles(N, 64), sx), kw = tiles(tiles(T, 64), sw);
-                const double work = (dx * sx * time(kx, kBackward.full) + dw * sw * time(kw, kBackward.full)) / kSlots[i];
-                const double longest = time(std::max(kx, kw), kBackward.alone);
-                const double joins = join_time(sx, T * D, 0.25) + join_time(sw, N * D, 0.25) - (sx > 1 && sw > 1 ? 4.4 : 0.0);
-                const double cost = std::max(work + 0.40 * longest, longest) + joins;
+                const double cost = cost_of(sx, sw);
                 if (best == 0.0 || cost < best) {
                     best = cost;
                     q->back_tile = of;
@@ -157,6 +182,10 @@ dsm::LinearPlan make_linear_plan(const dsm_linear_problem* p) {
     q.act = p->act;
     q.f32 = p->dtype == DSM_F32;
     q.dw_f32 = p->dw_dtype == DSM_F32;
+    q.dz_halves = !q.f32 && q.dw_f32 && p->act != DSM_ACT_NONE;
+    // fp32: halves take a pass over w that reads and writes it, fp32 products six times as long.
+    q.form = !q.f32 ? dsm::kLinearBf16 : T <= kSingleForward ? dsm::kLinearSingle : dsm::kLinearHalves;
+    q.back_form = !q.f32 ? dsm::kLinearBf16 : T <= kSingleBackward ? dsm::kLinearSingle : dsm::kLinearHalves;
     q.few = T <= dsm::kLinearFew;
     q.splits = q.dx_splits = q.dw_splits = 1;
     const int64_t width = q.f32 ? 2 : 1;  // 16-bit elements of a number
@@ -171,7 +200,7 @@ dsm::LinearPlan make_linear_plan(const dsm_linear_problem* p) {
         at = round_up(at + bytes, 256);
         return here;
     };
-    q.x = take(T * q.ld_dim * 2);
+    q.x = take((p->grads && q.dz_halves ? 2 * q.pad_tokens : T) * q.ld_dim * 2);
     q.w = take(N * q.ld_dim * 2);
     q.x_exp = take(T * 4);
     q.w_exp = take(N * 4);
@@ -185,8 +214,8 @@ dsm::LinearPlan make_linear_plan(const dsm_linear_problem* p) {
     if (!p->grads || T == 0) return q;
     at = common;
     cut_backward(&q);
-    q.bias_parts = static_cast<int32_t>(q.f32 ? tiles(T, dsm::kDzSplitRows) : q.pad_tokens / dsm::kDzRows);
-    q.dz = take(q.pad_tokens * q.ld_wide * 2);
+    q.bias_parts = static_cast<int32_t>(q.back_form == dsm::kLinearHalves ? tiles(T, dsm::kDzSplitRows) : q.pad_tokens / dsm::kDzRows);
+    q.dz = take(q.pad_tokens * q.ld_wide * (q.dz_halves ? 4 : 2));
     q.z_exp = take(T * 4);
     q.w_tops = take(dsm::kLinearTopParts * 4);
     q.tops = take(q.pad_tokens / dsm::kDzSplitRows * 4);
@@ -221,10 +250,12 @@ const dsm::LinearPlan& plan_linear(const dsm_linear_problem* p) {
     return k.plan;
 }
 
-// Whether products can take a matrix's rows of `cols` bf16 elements where they lie: 16-byte
-// loads of whole runs of `run` elements.
-bool direct(const void* p, int64_t stride, int64_t cols, int64_t run) {
-    return cols % run == 0 && stride % 8 == 0 && stride < kMaxStride && aligned(p, 16);
+// Whether products can take a matrix's rows of `cols` elements where they lie: 16-byte
+// loads of whole runs of `run` 16-bit elements.
+bool direct(dsm::LinearForm form, const void* p, int64_t stride, int64_t cols, int64_t run) {
+    if (form == dsm::kLinearHalves) return false;
+    const int64_t size = form == dsm::kLinearSingle ? 4 : 2;
+    return cols * size % (run * 2) == 0 && stride * size % 16 == 0 && stride * size < kMaxStride * 2 && aligned(p, 16);
 }
 
 dsm_status check_rows(const char* name, const void* p, int64_t rows, int64_t stride, int64_t cols, size_t elem, bool wanted) {
@@ -409,8 +440,8 @@ dsm_status dsm_linear(const dsm_linear_problem* problem, const dsm_linear_buffer
     c.y = b.y;
     c.y_stride = b.y_stride;
     c.z = b.z;
-    c.x_direct = !c.p.f32 && direct(b.x, b.x_stride, p.dim, 64);
-    c.w_direct = !c.p.f32 && direct(b.w, b.w_stride, p.dim, 64);
+    c.x_direct = direct(c.p.form, b.x, b.x_stride, p.dim, 64);
+    c.w_direct = direct(c.p.form, b.w, b.w_stride, p.dim, 64);
     return launched("launching the linear layer", dsm::launch_linear(c, static_cast<hipStream_t>(b.stream)));
 }
 
@@ -447,9 +478,9 @@ dsm_status dsm_linear_backward(const dsm_linear_problem* problem, const dsm_line
     c.dbias = b.dbias;
     // k-strided operands: whole runs of 8.  dz is k-contiguous in dx, and its rows from
     // the last token on meet x's, so they have to be zeros.
-    c.x_direct = !c.p.f32 && direct(b.x, b.x_stride, p.dim, 8);
-    c.w_direct = !c.p.f32 && direct(b.w, b.w_stride, p.dim, 8);
-    c.dz_direct = !c.p.f32 && !act && direct(b.dy, b.dy_stride, p.wide, 64) && p.tokens % 64 == 0;
+    c.x_direct = !c.p.dz_halves && direct(c.p.back_form, b.x, b.x_stride, p.dim, 8);
+    c.w_direct = direct(c.p.back_form, b.w, b.w_stride, p.dim, 8);
+    c.dz_direct = !act && direct(c.p.back_form, b.dy, b.dy_stride, p.wide, 64) && p.tokens % 64 == 0;
     return launched("launching the linear layer's gradients", dsm::launch_linear_backward(c, static_cast<hipStream_t>(b.stream)));
 }
 

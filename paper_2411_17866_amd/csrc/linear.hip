@@ -12,14 +12,18 @@
 // What the products take:
 //   bf16  the operands as they are, where rows of 64 columns (k-contiguous) or of 8
 //         (k-strided) are whole and aligned, else copies with zeros behind the rows.
-//         dz is rounded to bf16: an error of half a step for each term of a sum, which
-//         averages out to less than the rounding of the result.
+//         dz is rounded to bf16: an error of half a step for each term of a sum, which is
+//         about what the rounding of a bf16 result costs (0.0024 of its norm with both,
+//         0.0017 with one).  A dw in fp32 takes dz as two bf16 halves, 16 bits, with twice
+//         the matrix instructions.
 //   fp32  two fp16 halves of every number (gemm_tile.h).  Powers of two bring a row's
 //         largest magnitude just under fp16's, so rows of any size keep their bits:
 //         x's and w's rows forward, dz's for dx.  In dw the sum runs over the tokens,
 //         so there x_t is taken times 2^(c - e_t), e_t being dz_t's power: dz_t x_t
 //         comes out right up to one power, and c brings the largest of them to fp16's
 //         range.  w in dx, whose sum runs over w's rows, has one power for all.
+//   fp32 itself, for few tokens, where reading w costs more than multiplying it: w is
+//         read where it lies, and the matrix cores multiply fp32 at a 16th of the rate.
 // Products accumulate in fp32.
 //
 // Sums over a long axis with few tiles are cut into parts that run side by side; they
@@ -42,6 +46,18 @@ using rows::V8;
 using tile::kContig;
 using tile::kStrided;
 using tile::Operand;
+
+template <class T_>
+struct Type {
+    using type = T_;
+};
+
+// What the products' operands hold (the plan's `form`).
+constexpr bool is_f32(LinearForm f) { return f != kLinearBf16; }
+constexpr tile::Elem elem(LinearForm f) {
+    return f == kLinearBf16 ? tile::kBF16 : f == kLinearHalves ? tile::kSplit : tile::kF32;
+}
+constexpr int units(LinearForm f) { return tile::units(elem(f)); }
 
 constexpr int kNoExponent = 10000;  // of a row of zeros: brings everything to 0
 
@@ -369,19 +385,20 @@ __device__ __forceinline__ void store_halves(u16* row, int col, const V8& x, int
     *reinterpret_cast<u16x8*>(at + 32) = lo;
 }
 
-// x and w (blockIdx.y) with zeros behind their rows, one wave a row.  bf16: a copy.
-// fp32, forward: halves, and the rows' exponents.
-template <bool F32>
-__global__ __launch_bounds__(256) void k_copies(LinearCall c, int from) {
+// x and w (blockIdx.y) with zeros behind their rows, one wave a row: copies, or, forward, halves
+// and the rows' exponents.
+template <LinearForm FORM>
+__global__ __launch_bounds__(256) void k_copies(LinearCall c, int from, bool twice) {
     const bool of_w = from + blockIdx.y != 0;
-    const int rows = of_w ? c.p.wide : c.p.tokens, lane = threadIdx.x & 63;
+    // (x twice, for dz as two halves: its rows from the last token on are zeros then.)
+    const int rows = of_w ? c.p.wide : twice ? static_cast<int>(c.p.pad_tokens) : c.p.tokens, lane = threadIdx.x & 63;
     const void* src = of_w ? c.w : c.x;
     const int64_t stride = of_w ? c.w_stride : c.x_stride, ld = c.p.ld_dim;
-    const int cols = static_cast<int>(ld / (F32 ? 2 : 1));
+    const int cols = static_cast<int>(ld / units(FORM));
     u16* dst = reinterpret_cast<u16*>(c.workspace + (of_w ? c.p.w : c.p.x));
     for (int r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4) {
         int e = 0;
-        if constexpr (F32) {
+        if constexpr (FORM == kLinearHalves) {
             uint32_t top = 0;
 #pragma unroll 4
             for (int k = lane * 8; k < c.p.dim; k += 512) top = top_of(rows::load8<true>(src, r * stride + k, c.p.dim - k), top);
@@ -390,49 +407,62 @@ __global__ __launch_bounds__(256) void k_copies(LinearCall c, int from) {
         }
 #pragma unroll 4
         for (int k = lane * 8; k < cols; k += 512) {
-            const V8 v = rows::load8<F32>(src, r * stride + k, c.p.dim - k);
-            if constexpr (F32)
+            const V8 v = rows::load8<is_f32(FORM)>(src, r * stride + k, of_w || r < c.p.tokens ? c.p.dim - k : 0);
+            if constexpr (FORM == kLinearHalves) {
                 store_halves(dst + r * ld, k, v, e);
-            else
-                rows::store8<false>(dst + r * ld, k, v, 8);
+            } else {
+                const int64_t at = r * (ld / units(FORM)) + k;
+                rows::store8<is_f32(FORM)>(dst, at, v, 8);
+                if (twice && !of_w) rows::store8<is_f32(FORM)>(dst, at + c.p.pad_tokens * (ld / units(FORM)), v, 8);
+            }
         }
     }
 }
 
-// bf16: dz with zeros behind its rows (unless it is dy, read where it lies) and dbias's sums, 64
-// tokens by 512 columns a work-group.
-__global__ __launch_bounds__(256) void k_dz(LinearCall c) {
-    __shared__ V8 sums[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = (blockIdx.x * 64 + lane) * 8;
+// dz with zeros behind its rows (unless it is dy, read where it lies) and dbias's sums:
+// kDzRows tokens from row0 on by 512 columns from col0 on, by a work-group of WAVES.
+template <bool F32, int WAVES>
+__device__ __forceinline__ void dz_block(const LinearCall& c, int64_t row0, int col0, V8 (*sums)[64]) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = col0 + lane * 8;
     const int wide = c.p.wide, have = max(0, min(wide - col, 8));
-    u16* dz = reinterpret_cast<u16*>(c.workspace + c.p.dz);
+    const int64_t ld = c.p.ld_wide / (F32 ? 2 : 1);
     V8 sum;
 #pragma unroll
     for (int q = 0; q < 8; ++q) sum.v[q] = 0.f;
-#pragma unroll 4
-    for (int k = wave; k < kDzRows; k += 4) {
-        const int64_t row = static_cast<int64_t>(blockIdx.y) * kDzRows + k;
+#pragma unroll 8
+    for (int k = wave; k < kDzRows; k += WAVES) {
+        const int64_t row = row0 + k;
         const int here = row < c.p.tokens ? have : 0;
-        V8 d = rows::load8<false>(c.dy, row * c.dy_stride + col, here);
-        if (c.p.act != DSM_ACT_NONE) {
-            times_slope<true>(c.p.act, d, rows::load8<false>(c.z_in, row * c.z_stride + col, here), here);
-        }
+        V8 d = rows::load8<F32>(c.dy, row * c.dy_stride + col, here);
+        if (c.p.act != DSM_ACT_NONE)
+            times_slope<!F32>(c.p.act, d, rows::load8<F32>(c.z_in, row * c.z_stride + col, here), here);
 #pragma unroll
         for (int q = 0; q < 8; ++q) sum.v[q] += d.v[q];
-        if (!c.dz_direct && row < c.p.pad_tokens && col < c.p.ld_wide) rows::store8<false>(dz, row * c.p.ld_wide + col, d, 8);
+        if (c.dz_direct || row >= c.p.pad_tokens || col >= ld) continue;
+        rows::store8<F32>(c.workspace + c.p.dz, row * ld + col, d, 8);
+        if (!F32 && c.p.dz_halves) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) d.v[q] -= rows::bf16_to_float(rows::float_to_bf16(d.v[q]));
+            rows::store8<false>(c.workspace + c.p.dz, (c.p.pad_tokens + row) * ld + col, d, 8);
+        }
     }
     if (!c.dbias) return;
     sums[wave][lane] = sum;
     __syncthreads();
     if (wave != 0) return;
 #pragma unroll
-    for (int w = 1; w < 4; ++w)
+    for (int w = 1; w < WAVES; ++w)
 #pragma unroll
         for (int q = 0; q < 8; ++q) sum.v[q] += sums[w][lane].v[q];
-    rows::store8<true>(c.workspace + c.p.bias_sums, static_cast<int64_t>(blockIdx.y) * wide + col, sum, have);
+    rows::store8<true>(c.workspace + c.p.bias_sums, row0 / kDzRows * wide + col, sum, have);
+}
+template <bool F32>
+__global__ __launch_bounds__(256) void k_dz(LinearCall c) {
+    __shared__ V8 sums[4][64];
+    dz_block<F32, 4>(c, static_cast<int64_t>(blockIdx.y) * kDzRows, blockIdx.x * 512, sums);
 }
 
-// fp32: dz as halves, its rows' exponents, dbias's sums, and the least exponent of x dz, kDzSplitRows
+// Halves: dz, its rows' exponents, dbias's sums, and the least exponent of x dz, kDzSplitRows
 // tokens a work-group; the work-groups before those look for w's largest magnitude.  A
 // work-group's threads have a row's columns between them, eight each, so that the rows stay in
 // registers until their exponents are known (HOLD: up to 8192 columns; wider rows are read
@@ -537,7 +567,7 @@ __device__ __forceinline__ int largest(int v) {
     return max(max(waves[0], waves[1]), max(waves[2], waves[3]));
 }
 
-// fp32: w (blockIdx.y = 1) times one power of two, and x (0) times those that make its rows meet dz's.
+// Halves: w (blockIdx.y = 1) times one power of two, and x (0) times those that make its rows meet dz's.
 __global__ __launch_bounds__(256) void k_back_copies(LinearCall c, int from, int top_groups, int dz_groups) {
     const bool of_w = from + blockIdx.y != 0;
     int e;
@@ -571,24 +601,27 @@ __global__ __launch_bounds__(256) void k_back_copies(LinearCall c, int from, int
 
 // ---- Products ----
 
-template <bool F32>
-constexpr tile::Elem kElem = F32 ? tile::kSplit : tile::kBF16;
-
-template <bool F32>
-__device__ __forceinline__ Operand x_rows(const LinearCall& c) {
-    if (!F32 && c.x_direct) return Operand{static_cast<const u16*>(c.x), c.x_stride, c.p.tokens, c.p.dim};
-    return Operand{reinterpret_cast<const u16*>(c.workspace + c.p.x), c.p.ld_dim, c.p.tokens, static_cast<int32_t>(c.p.ld_dim)};
+// 16-bit elements of a row that lies where the caller has it.
+template <LinearForm FORM>
+__device__ __forceinline__ Operand rows_at(const void* p, int64_t stride, int rows, int cols) {
+    return Operand{static_cast<const u16*>(p), stride * units(FORM), rows, cols * units(FORM)};
 }
-template <bool F32>
+template <LinearForm FORM, bool BACK = false>
+__device__ __forceinline__ Operand x_rows(const LinearCall& c) {
+    if (FORM != kLinearHalves && c.x_direct) return rows_at<FORM>(c.x, c.x_stride, c.p.tokens, c.p.dim);
+    const int rows = BACK && c.p.dz_halves ? static_cast<int>(2 * c.p.pad_tokens) : c.p.tokens;
+    return Operand{reinterpret_cast<const u16*>(c.workspace + c.p.x), c.p.ld_dim, rows, static_cast<int32_t>(c.p.ld_dim)};
+}
+template <LinearForm FORM>
 __device__ __forceinline__ Operand w_rows(const LinearCall& c) {
-    if (!F32 && c.w_direct) return Operand{static_cast<const u16*>(c.w), c.w_stride, c.p.wide, c.p.dim};
+    if (FORM != kLinearHalves && c.w_direct) return rows_at<FORM>(c.w, c.w_stride, c.p.wide, c.p.dim);
     return Operand{reinterpret_cast<const u16*>(c.workspace + c.p.w), c.p.ld_dim, c.p.wide, static_cast<int32_t>(c.p.ld_dim)};
 }
-template <bool F32>
+template <LinearForm FORM>
 __device__ __forceinline__ Operand dz_rows(const LinearCall& c) {
-    if (!F32 && c.dz_direct) return Operand{static_cast<const u16*>(c.dy), c.dy_stride, c.p.tokens, c.p.wide};
-    return Operand{reinterpret_cast<const u16*>(c.workspace + c.p.dz), c.p.ld_wide, static_cast<int32_t>(c.p.pad_tokens),
-                   static_cast<int32_t>(c.p.ld_wide)};
+    if (FORM != kLinearHalves && c.dz_direct) return rows_at<FORM>(c.dy, c.dy_stride, c.p.tokens, c.p.wide);
+    return Operand{reinterpret_cast<const u16*>(c.workspace + c.p.dz), c.p.ld_wide,
+                   static_cast<int32_t>(c.p.pad_tokens * (c.p.dz_halves ? 2 : 1)), static_cast<int32_t>(c.p.ld_wide)};
 }
 
 // Work-groups go to the XCDs in turn; every XCD gets one run of the tiles in order.
@@ -614,13 +647,13 @@ __device__ __forceinline__ V8 eight_of(const tile::Eight& x) {
 }
 
 // y, or a part of its sums: the tile of rows from row0 on, columns from col0 on.
-template <bool F32, class T, bool PARTS>
+template <LinearForm FORM, class T, bool PARTS>
 __device__ __forceinline__ void forward_tile(const LinearCall& c, int row0, int col0, int part, DSM_LDS char* lds) {
-    int k0 = 0, k1 = static_cast<int>(c.p.ld_dim / (F32 ? 2 : 1));
+    int k0 = 0, k1 = static_cast<int>(c.p.ld_dim / units(FORM));
     if (PARTS) part_of(k1, c.p.splits, part, &k0, &k1);
     T t;
     t.clear();
-    t.add(x_rows<F32>(c), w_rows<F32>(c), row0, col0, k0, k1, lds, c.p.tokens - row0, c.p.wide - col0);
+    t.add(x_rows<FORM>(c), w_rows<FORM>(c), row0, col0, k0, k1, lds, c.p.tokens - row0, c.p.wide - col0);
     const int32_t* x_exp = reinterpret_cast<const int32_t*>(c.workspace + c.p.x_exp);
     const int32_t* w_exp = reinterpret_cast<const int32_t*>(c.workspace + c.p.w_exp);
 #pragma unroll
@@ -628,7 +661,7 @@ __device__ __forceinline__ void forward_tile(const LinearCall& c, int row0, int 
         const int col = col0 + t.col8(q);
         const V8 bias = PARTS ? V8{} : bias8(c, col);
         int we[8];
-        if constexpr (F32) {
+        if constexpr (FORM == kLinearHalves) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) we[e] = w_exp[min(col + e, c.p.wide - 1)];
         }
@@ -637,7 +670,7 @@ __device__ __forceinline__ void forward_tile(const LinearCall& c, int row0, int 
             const int row = row0 + t.row(f);
             V8 v = eight_of(t.eight(f, q));
             if (row >= c.p.tokens || col >= c.p.wide) continue;
-            if constexpr (F32) {
+            if constexpr (FORM == kLinearHalves) {
                 const int xe = x_exp[row];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v.v[e] = ldexpf(v.v[e], -(xe + we[e]));
@@ -646,7 +679,7 @@ __device__ __forceinline__ void forward_tile(const LinearCall& c, int row0, int 
                 rows::store8<true>(c.workspace + c.p.y_parts,
                                    (static_cast<int64_t>(part) * c.p.tokens + row) * c.p.ld_y + col, v, 8);
             else
-                finish<F32>(c, row, col, v, bias);
+                finish<is_f32(FORM)>(c, row, col, v, bias);
         }
     }
 }
@@ -663,16 +696,16 @@ __device__ __forceinline__ void place_tile(int id, int tiles_t, int tiles_n, int
 
 // By tiles of BM.  Tiles of 256 take the first `tiles_n` columns of tiles alone; what a
 // last turn that leaves most CUs idle would take goes by tiles of 128.
-template <bool F32, int BM, bool PARTS>
+template <LinearForm FORM, int BM, bool PARTS>
 __global__ __launch_bounds__(tile::threads_of(BM)) void k_forward(LinearCall c, int tiles_t, int tiles_n, int groups) {
-    using T = tile::Pick<kElem<F32>, BM, kContig, kContig>;
+    using T = tile::Pick<elem(FORM), BM, kContig, kContig>;
     __shared__ __align__(1024) char lds[T::kLdsBytes];
     int tt, tn;
     if constexpr (BM == 256 && !PARTS) {
         if (static_cast<int>(blockIdx.x) >= groups) {
             const int col0 = tiles_n * 256, rest_t = (c.p.tokens + 127) / 128, rest_n = (c.p.wide - col0 + 127) / 128;
             place_tile(xcd_run(blockIdx.x - groups, gridDim.x - groups), rest_t, rest_n, &tt, &tn);
-            forward_tile<F32, tile::Pick<kElem<F32>, 128, kContig, kContig>, false>(c, tt * 128, col0 + tn * 128, 0,
+            forward_tile<FORM, tile::Pick<elem(FORM), 128, kContig, kContig>, false>(c, tt * 128, col0 + tn * 128, 0,
                                                                                     (DSM_LDS char*)lds);
             return;
         }
@@ -680,7 +713,7 @@ __global__ __launch_bounds__(tile::threads_of(BM)) void k_forward(LinearCall c, 
     int id = xcd_run(blockIdx.x, groups);
     const int part = PARTS ? id / (tiles_t * tiles_n) : 0;
     place_tile(id - part * tiles_t * tiles_n, tiles_t, tiles_n, &tt, &tn);
-    forward_tile<F32, T, PARTS>(c, tt * BM, tn * BM, part, (DSM_LDS char*)lds);
+    forward_tile<FORM, T, PARTS>(c, tt * BM, tn * BM, part, (DSM_LDS char*)lds);
 }
 
 // Eight columns of the sum of `parts` arrays of `rows` rows.
@@ -720,45 +753,31 @@ __device__ __forceinline__ void store_dw(const LinearCall& c, int64_t row, int c
         rows::store8<false>(c.dw, row * c.dw_stride + col, v, have);
 }
 
-// Tiles of 256 whose last 128 columns lie past the row are a type of their own.
-template <bool F32, int BM, tile::Kind KI, tile::Kind KJ, bool NARROW>
-struct BackTile {
-    using T = tile::Pick<kElem<F32>, BM, KI, KJ>;
-};
-template <bool F32, tile::Kind KI, tile::Kind KJ, bool NARROW>
-struct BackTile<F32, 256, KI, KJ, NARROW> {
-    using T = tile::BigTile<kElem<F32>, KI, KJ, false, NARROW>;
-};
-
-template <bool F32, int BM, bool NARROW>
-__device__ __forceinline__ void dx_tile(const LinearCall& c, int id, DSM_LDS char* lds) {
-    using T = typename BackTile<F32, BM, kContig, kStrided, NARROW>::T;
-    const int tiles_t = (c.p.tokens + BM - 1) / BM, tiles_d = (c.p.dim + BM - 1) / BM;
-    const int part = id / (tiles_t * tiles_d);
-    id -= part * tiles_t * tiles_d;
-    const int tt = id / tiles_d, td = id - tt * tiles_d;
+// dx: the tile of tokens from row0 on, columns from col0 on; a part of its sums, or all.
+template <LinearForm FORM, class T>
+__device__ __forceinline__ void dx_tile(const LinearCall& c, int row0, int col0, int part, int parts, DSM_LDS char* lds) {
     int k0, k1;
-    part_of(static_cast<int>(F32 || !c.dz_direct ? c.p.ld_wide / (F32 ? 2 : 1) : c.p.wide), c.p.dx_splits, part, &k0, &k1);
+    part_of(FORM == kLinearHalves || !c.dz_direct ? static_cast<int>(c.p.ld_wide / units(FORM)) : c.p.wide, parts, part, &k0, &k1);
     T t;
     t.clear();
-    t.add(dz_rows<F32>(c), w_rows<F32>(c), tt * BM, td * BM, k0, k1, lds, c.p.tokens - tt * BM, c.p.dim - td * BM);
+    t.add(dz_rows<FORM>(c), w_rows<FORM>(c), row0, col0, k0, k1, lds, c.p.tokens - row0, c.p.dim - col0);
     const int32_t* z_exp = reinterpret_cast<const int32_t*>(c.workspace + c.p.z_exp);
-    const int we = F32 ? *reinterpret_cast<const int32_t*>(c.workspace + c.p.w_exp) : 0;
+    const int we = FORM == kLinearHalves ? *reinterpret_cast<const int32_t*>(c.workspace + c.p.w_exp) : 0;
 #pragma unroll
     for (int f = 0; f < T::FI; ++f) {
-        const int row = tt * BM + t.row(f);
+        const int row = row0 + t.row(f);
         if (row >= c.p.tokens) continue;
-        const int e = F32 ? -(z_exp[row] + we) : 0;
+        const int e = FORM == kLinearHalves ? -(z_exp[row] + we) : 0;
 #pragma unroll
         for (int q = 0; q < T::FJ / 2; ++q) {
-            const int col = td * BM + t.col8(q);
+            const int col = col0 + t.col8(q);
             V8 v = eight_of(t.eight(f, q));
             if (col >= c.p.dim) continue;
-            if constexpr (F32) {
+            if constexpr (FORM == kLinearHalves) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) v.v[k] = ldexpf(v.v[k], e);
             }
-            if (c.p.dx_splits > 1)
+            if (parts > 1)
                 rows::store8<true>(c.workspace + c.p.dx_parts,
                                    (static_cast<int64_t>(part) * c.p.tokens + row) * c.p.ld_dx + col, v, 8);
             else
@@ -767,33 +786,31 @@ __device__ __forceinline__ void dx_tile(const LinearCall& c, int id, DSM_LDS cha
     }
 }
 
-template <bool F32, int BM, bool NARROW>
-__device__ __forceinline__ void dw_tile(const LinearCall& c, int id, DSM_LDS char* lds) {
-    using T = typename BackTile<F32, BM, kStrided, kStrided, NARROW>::T;
-    const int tiles_n = (c.p.wide + BM - 1) / BM, tiles_d = (c.p.dim + BM - 1) / BM;
-    const int part = id / (tiles_n * tiles_d);
-    id -= part * tiles_n * tiles_d;
-    const int tn = id / tiles_d, td = id - tn * tiles_d;
+// dw: rows of w from row0 on, columns from col0 on.
+template <LinearForm FORM, class T>
+__device__ __forceinline__ void dw_tile(const LinearCall& c, int row0, int col0, int part, int parts, DSM_LDS char* lds) {
     int k0, k1;
-    part_of((c.p.tokens + T::kSteps - 1) / T::kSteps * T::kSteps, c.p.dw_splits, part, &k0, &k1);
+    // (dz as two halves: one behind the other, and x twice.)
+    const int steps = c.p.dz_halves ? static_cast<int>(2 * c.p.pad_tokens) : (c.p.tokens + T::kSteps - 1) / T::kSteps * T::kSteps;
+    part_of(steps, parts, part, &k0, &k1);
     T t;
     t.clear();
-    t.add(dz_rows<F32>(c), x_rows<F32>(c), tn * BM, td * BM, k0, k1, lds, c.p.wide - tn * BM, c.p.dim - td * BM);
-    const int e = F32 ? -*reinterpret_cast<const int32_t*>(c.workspace + c.p.x_exp) : 0;
+    t.add(dz_rows<FORM>(c), x_rows<FORM, true>(c), row0, col0, k0, k1, lds, c.p.wide - row0, c.p.dim - col0);
+    const int e = FORM == kLinearHalves ? -*reinterpret_cast<const int32_t*>(c.workspace + c.p.x_exp) : 0;
 #pragma unroll
     for (int f = 0; f < T::FI; ++f) {
-        const int row = tn * BM + t.row(f);
+        const int row = row0 + t.row(f);
         if (row >= c.p.wide) continue;
 #pragma unroll
         for (int q = 0; q < T::FJ / 2; ++q) {
-            const int col = td * BM + t.col8(q);
+            const int col = col0 + t.col8(q);
             V8 v = eight_of(t.eight(f, q));
             if (col >= c.p.dim) continue;
-            if constexpr (F32) {
+            if constexpr (FORM == kLinearHalves) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) v.v[k] = ldexpf(v.v[k], e);
             }
-            if (c.p.dw_splits > 1)
+            if (parts > 1)
                 rows::store8<true>(c.workspace + c.p.dw_parts,
                                    (static_cast<int64_t>(part) * c.p.wide + row) * c.p.ld_dx + col, v, 8);
             else
@@ -802,30 +819,64 @@ __device__ __forceinline__ void dw_tile(const LinearCall& c, int id, DSM_LDS cha
     }
 }
 
-// dx and dw in one launch: neither fills the CUs' last turn by itself.  Each XCD has its
-// run of one product's tiles, the longer ones, then its run of the other's.
-template <bool F32, int BM>
-__global__ __launch_bounds__(tile::threads_of(BM)) void k_backward(LinearCall c, int dx_tiles, int dw_tiles, int dw_first) {
-    using TX = typename BackTile<F32, BM, kContig, kStrided, false>::T;
-    using TW = typename BackTile<F32, BM, kStrided, kStrided, false>::T;
+// Tile `id` of one of the products, by BM.
+template <LinearForm FORM, int BM, bool DW>
+__device__ __forceinline__ void back_tile(const LinearCall& c, int id, DSM_LDS char* lds) {
+    constexpr tile::Kind KI = DW ? kStrided : kContig;
+    const int rows = ((DW ? c.p.wide : c.p.tokens) + BM - 1) / BM, tiles_d = (c.p.dim + BM - 1) / BM;
+    const int part = id / (rows * tiles_d), parts = DW ? c.p.dw_splits : c.p.dx_splits;
+    id -= part * rows * tiles_d;
+    const int tt = id / tiles_d, td = id - tt * tiles_d;
+    const auto run = [&](auto as) {
+        using T = typename decltype(as)::type;
+        if constexpr (DW)
+            dw_tile<FORM, T>(c, tt * BM, td * BM, part, parts, lds);
+        else
+            dx_tile<FORM, T>(c, tt * BM, td * BM, part, parts, lds);
+    };
+    // Tiles of 256 whose last 128 columns lie past the row are a type of their own.
+    if constexpr (BM == 256) {
+        if (c.p.dim - td * 256 <= 128)
+            run(Type<tile::BigTile<elem(FORM), KI, kStrided, false, true>>());
+        else
+            run(Type<tile::BigTile<elem(FORM), KI, kStrided, false, false>>());
+    } else {
+        run(Type<tile::Pick<elem(FORM), BM, KI, kStrided>>());
+    }
+}
+
+// dx, dw and, where dz is dy, dbias's sums in one launch: neither product fills the CUs'
+// last turn by itself.  Each XCD has its run of the product's tiles that have more steps,
+// then its run of the other's, then of the sums.  4093 x 1600 x 6400 in bf16: 0.86 PFLOP/s; the CUs'
+// clock falls to 1.8 GHz when all of them multiply, and k-strided operands take LDS twice as long.
+struct BackJobs {
+    int32_t count[3];
+    int32_t dw_first;
+};
+// Few tokens: dx is as narrow as one tile of 64, and dw's sums have one or two steps.
+constexpr int dw_tile_of(LinearForm form, int bm) { return form == kLinearSingle ? 128 : bm; }
+template <LinearForm FORM, int BM>
+__global__ __launch_bounds__(tile::threads_of(BM)) void k_backward(LinearCall c, BackJobs jobs) {
+    constexpr int BW = dw_tile_of(FORM, BM);
+    using TX = tile::Pick<elem(FORM), BM, kContig, kStrided>;
+    using TW = tile::Pick<elem(FORM), BW, kStrided, kStrided>;
     constexpr int kLds = TX::kLdsBytes > TW::kLdsBytes ? TX::kLdsBytes : TW::kLdsBytes;
     __shared__ __align__(1024) char lds[kLds];
-    const int x = blockIdx.x % kXcds, at = blockIdx.x / kXcds;
-    const int front = per_xcd(dw_first ? dw_tiles : dx_tiles), tiles_d = (c.p.dim + BM - 1) / BM, full = (c.p.dim + 127) / 256;
-    const bool dw = (at < front) == (dw_first != 0);
-    const int id = at < front ? x * front + at : x * per_xcd(dw_first ? dx_tiles : dw_tiles) + at - front;
-    if (id >= (dw ? dw_tiles : dx_tiles)) return;
-    const bool narrow = BM == 256 && id % tiles_d >= full;
-    if (!dw) {
-        if (narrow)
-            dx_tile<F32, BM, BM == 256>(c, id, (DSM_LDS char*)lds);
-        else
-            dx_tile<F32, BM, false>(c, id, (DSM_LDS char*)lds);
+    const int x = blockIdx.x % kXcds;
+    int at = blockIdx.x / kXcds, kind = 0;
+    while (kind < 2 && at >= per_xcd(jobs.count[kind])) at -= per_xcd(jobs.count[kind++]);
+    const int id = x * per_xcd(jobs.count[kind]) + at;
+    if (id >= jobs.count[kind]) return;
+    if (kind == 2) {
+        if constexpr (FORM != kLinearHalves) {
+            const int across = (c.p.wide + 511) / 512, down = id / across;
+            dz_block<is_f32(FORM), tile::threads_of(BM) / 64>(c, static_cast<int64_t>(down) * kDzRows, (id - down * across) * 512,
+                                                              reinterpret_cast<V8(*)[64]>(lds));
+        }
+    } else if ((kind == 0) == (jobs.dw_first != 0)) {
+        back_tile<FORM, BW, true>(c, id, (DSM_LDS char*)lds);
     } else {
-        if (narrow)
-            dw_tile<F32, BM, BM == 256>(c, id, (DSM_LDS char*)lds);
-        else
-            dw_tile<F32, BM, false>(c, id, (DSM_LDS char*)lds);
+        back_tile<FORM, BM, false>(c, id, (DSM_LDS char*)lds);
     }
 }
 
@@ -883,33 +934,32 @@ void forward_join(const LinearCall& c, hipStream_t stream) {
     k_forward_join<F32><<<groups_for((eights + 255) / 256, 4096), 256, 0, stream>>>(c);
 }
 
-template <bool F32, int BM>
+template <LinearForm FORM, int BM>
 void forward(const LinearCall& c, hipStream_t stream) {
     const int tiles_t = (c.p.tokens + BM - 1) / BM, all = (c.p.wide + BM - 1) / BM;
     const int tiles_n = BM == 256 && c.p.splits == 1 ? c.p.front : all, groups = tiles_t * tiles_n * c.p.splits;
     if (c.p.splits > 1) {
-        k_forward<F32, BM, true><<<groups, tile::threads_of(BM), 0, stream>>>(c, tiles_t, tiles_n, groups);
-        forward_join<F32>(c, stream);
+        k_forward<FORM, BM, true><<<groups, tile::threads_of(BM), 0, stream>>>(c, tiles_t, tiles_n, groups);
+        forward_join<is_f32(FORM)>(c, stream);
     } else {
         const int rest = tiles_n < all ? (c.p.tokens + 127) / 128 * ((c.p.wide - tiles_n * 256 + 127) / 128) : 0;
-        k_forward<F32, BM, false><<<groups + rest, tile::threads_of(BM), 0, stream>>>(c, tiles_t, tiles_n, groups);
+        k_forward<FORM, BM, false><<<groups + rest, tile::threads_of(BM), 0, stream>>>(c, tiles_t, tiles_n, groups);
     }
 }
 
-template <bool F32>
+template <LinearForm FORM>
 void forward(const LinearCall& c, hipStream_t stream) {
     // x from 0, w from 1: whichever is not read where it lies.
     const int from = c.x_direct ? 1 : 0, to = c.w_direct ? 1 : 2;
     if (from < to) {
         const int rows = c.p.tokens > c.p.wide ? c.p.tokens : c.p.wide;
-        k_copies<F32><<<dim3(groups_for((rows + 3) / 4, 4096), to - from), 256, 0, stream>>>(c, from);
+        k_copies<FORM><<<dim3(groups_for((rows + 3) / 4, 4096), to - from), 256, 0, stream>>>(c, from, false);
     }
-    if (c.p.tile == 64)
-        forward<F32, 64>(c, stream);
-    else if (c.p.tile == 128)
-        forward<F32, 128>(c, stream);
-    else
-        forward<F32, 256>(c, stream);
+    if constexpr (FORM != kLinearSingle) {
+        if (c.p.tile == 128) return forward<FORM, 128>(c, stream);
+        if (c.p.tile == 256) return forward<FORM, 256>(c, stream);
+    }
+    forward<FORM, 64>(c, stream);
 }
 
 template <bool F32>
@@ -924,20 +974,27 @@ void few(const LinearCall& c, hipStream_t stream) {
     if (c.p.splits > 1) forward_join<F32>(c, stream);
 }
 
-template <bool F32, int BM>
-void backward(const LinearCall& c, hipStream_t stream) {
-    const int tiles_t = (c.p.tokens + BM - 1) / BM, tiles_n = (c.p.wide + BM - 1) / BM, tiles_d = (c.p.dim + BM - 1) / BM;
-    const int dx = c.dx ? tiles_t * tiles_d * c.p.dx_splits : 0, dw = c.dw ? tiles_n * tiles_d * c.p.dw_splits : 0;
-    const int dw_first = static_cast<int64_t>(c.p.tokens) * c.p.dx_splits > static_cast<int64_t>(c.p.wide) * c.p.dw_splits;
-    k_backward<F32, BM><<<kXcds * (per_xcd(dx) + per_xcd(dw)), tile::threads_of(BM), 0, stream>>>(c, dx, dw, dw_first);
+template <LinearForm FORM, int BM>
+void backward(const LinearCall& c, bool with_bias, hipStream_t stream) {
+    const auto tiles = [](int n, int of) { return (n + of - 1) / of; };
+    constexpr int BW = dw_tile_of(FORM, BM);
+    const int dx = c.dx ? tiles(c.p.tokens, BM) * tiles(c.p.dim, BM) * c.p.dx_splits : 0;
+    const int dw = c.dw ? tiles(c.p.wide, BW) * tiles(c.p.dim, BW) * c.p.dw_splits : 0;
+    BackJobs jobs;
+    jobs.dw_first = static_cast<int64_t>(c.p.tokens) * c.p.dx_splits > static_cast<int64_t>(c.p.wide) * c.p.dw_splits;
+    jobs.count[0] = jobs.dw_first ? dw : dx;
+    jobs.count[1] = jobs.dw_first ? dx : dw;
+    jobs.count[2] = with_bias ? static_cast<int>((c.p.wide + 511) / 512 * (c.p.pad_tokens / kDzRows)) : 0;
+    const int groups = per_xcd(jobs.count[0]) + per_xcd(jobs.count[1]) + per_xcd(jobs.count[2]);
+    k_backward<FORM, BM><<<kXcds * groups, tile::threads_of(BM), 0, stream>>>(c, jobs);
 }
 
-template <bool F32>
+template <LinearForm FORM>
 void backward(const LinearCall& c, hipStream_t stream) {
     const int copies_rows = c.p.tokens > c.p.wide ? c.p.tokens : c.p.wide;
     // x is wanted for dw, w for dx.
     const int from = c.dw && !c.x_direct ? 0 : 1, to = c.dx && !c.w_direct ? 2 : 1;
-    if constexpr (F32) {
+    if constexpr (FORM == kLinearHalves) {
         const int top_groups = c.dx ? static_cast<int>(groups_for((c.p.wide + 3) / 4, kLinearTopParts)) : 0;
         const int dz_groups = static_cast<int>(c.p.pad_tokens / kDzSplitRows);
         // (ld_wide counts halves: its columns, eight a thread, are a multiple of 64.)
@@ -950,18 +1007,23 @@ void backward(const LinearCall& c, hipStream_t stream) {
             k_back_copies<<<dim3(groups_for((copies_rows + 3) / 4, 2048), to - from), 256, 0, stream>>>(c, from, top_groups,
                                                                                                       dz_groups);
     } else {
-        if (!c.dz_direct || c.dbias)
-            k_dz<<<dim3((c.p.ld_wide + 511) / 512, c.p.pad_tokens / kDzRows), 256, 0, stream>>>(c);
+        // (Where dz is dy, dbias's sums run beside the products.)
+        if (!c.dz_direct || (c.dbias && !c.dx && !c.dw))
+            k_dz<is_f32(FORM)><<<dim3((c.p.ld_wide / units(FORM) + 511) / 512, c.p.pad_tokens / kDzRows), 256, 0, stream>>>(c);
         if (from < to)
-            k_copies<false><<<dim3(groups_for((copies_rows + 3) / 4, 4096), to - from), 256, 0, stream>>>(c, from);
+            k_copies<FORM><<<dim3(groups_for((copies_rows + 3) / 4, 4096), to - from), 256, 0, stream>>>(c, from, c.p.dz_halves);
     }
     if (c.dx || c.dw) {
-        if (c.p.back_tile == 64)
-            backward<F32, 64>(c, stream);
-        else if (c.p.back_tile == 128)
-            backward<F32, 128>(c, stream);
-        else
-            backward<F32, 256>(c, stream);
+        const bool with_bias = FORM != kLinearHalves && c.dz_direct && c.dbias;
+        bool done = false;
+        if constexpr (FORM != kLinearSingle) {
+            if (c.p.back_tile == 128)
+                backward<FORM, 128>(c, with_bias, stream);
+            else if (c.p.back_tile == 256)
+                backward<FORM, 256>(c, with_bias, stream);
+            done = c.p.back_tile != 64;
+        }
+        if (!done) backward<FORM, 64>(c, with_bias, stream);
     }
     const int bias_groups = c.dbias ? (c.p.wide + 63) / 64 : 0;
     const int64_t eights = (c.p.dim + 7) / 8;
@@ -978,10 +1040,12 @@ hipError_t launch_linear(const LinearCall& c, hipStream_t stream) {
             few<true>(c, stream);
         else
             few<false>(c, stream);
-    } else if (c.p.f32) {
-        forward<true>(c, stream);
+    } else if (c.p.form == kLinearSingle) {
+        forward<kLinearSingle>(c, stream);
+    } else if (c.p.form == kLinearHalves) {
+        forward<kLinearHalves>(c, stream);
     } else {
-        forward<false>(c, stream);
+        forward<kLinearBf16>(c, stream);
     }
     return hipGetLastError();
 }
@@ -989,10 +1053,12 @@ hipError_t launch_linear(const LinearCall& c, hipStream_t stream) {
 hipError_t launch_linear_backward(const LinearCall& c, hipStream_t stream) {
     if (c.p.tokens == 0)
         k_no_tokens<<<groups_for(c.p.wide, 2048), 256, 0, stream>>>(c);
-    else if (c.p.f32)
-        backward<true>(c, stream);
+    else if (c.p.back_form == kLinearSingle)
+        backward<kLinearSingle>(c, stream);
+    else if (c.p.back_form == kLinearHalves)
+        backward<kLinearHalves>(c, stream);
     else
-        backward<false>(c, stream);
+        backward<kLinearBf16>(c, stream);
     return hipGetLastError();
 }
 

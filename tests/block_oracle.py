@@ -87,9 +87,11 @@ def linear_backward_bounds(e, dy, x, w, name, dw_dtype):
     x, w, dz, dy = x.double().abs(), w.double().abs(), e["dz"].abs(), dy.double().abs()
     u = 0.0 if dtype == torch.bfloat16 else HALVES
     d = torch.zeros_like(dz) if name == "none" else (0.0 if name == "relu" else ACT) * dy + 2 * U * dz
-    taken = d + (HALF[dtype] * (dz + d) if name != "none" and dtype == torch.bfloat16 else 0.0)
-    dx = taken @ w + (2 * u + (w.shape[0] + 2) * 2 * U) * (dz @ w)
-    dw = taken.t().contiguous() @ x + (2 * u + (x.shape[0] + 2) * 2 * U) * (dz.t().contiguous() @ x)
+    rounded = name != "none" and dtype == torch.bfloat16
+    halves = HALF[dtype] ** 2 if dw_dtype == torch.float32 else HALF[dtype]  # of a bf16 dz in dw: two of them
+    dx = (d + (HALF[dtype] * (dz + d) if rounded else 0.0)) @ w + (2 * u + (w.shape[0] + 2) * 2 * U) * (dz @ w)
+    dw = (d + (halves * (dz + d) if rounded else 0.0)).t().contiguous() @ x
+    dw = dw + (2 * u + (x.shape[0] * (2 if rounded else 1) + 2) * 2 * U) * (dz.t().contiguous() @ x)
     if u:
         dx = dx + VANISH * (dz.amax(1)[:, None] * w.sum(0) + dz.sum(1)[:, None] * w.max())
         each = dz.amax(1) * x.amax(1)  # what a token's rows make together

@@ -108,6 +108,10 @@ def test_long_sums(size, dtype):
     for name, terms in (("dx", wide), ("dw", tokens)):
         O.check_norm(out[name], e[name], O.norm_bound(terms, dtype, 2), name)
     O.check_norm(out["dbias"], e["dbias"], O.norm_bound(tokens, F32), "dbias")
+    if dtype == BF16:  # dz as two halves: of 16 bits
+        plan = _ops().Linear(*size, dtype=dtype, act="gelu", dw_dtype=F32)
+        dw = plan.backward(i["dy"], i["x"], i["w"], z=i["z"], wanted=("dw",))["dw"]
+        O.check_norm(dw, e["dw"], O.norm_bound(2 * tokens, F32) + 2.0 ** -16, "dw in fp32")
 
 
 @TYPES
