@@ -73,7 +73,6 @@ hipError_t launch_norm_backward(const NormCall& c, hipStream_t stream);
 constexpr int kLinearFew = 64;       // tokens that are answered by one launch without tiles
 constexpr int kLinearTopParts = 512; // work-groups that look for w's largest magnitude
 constexpr int kDzRows = 64;          // tokens of a work-group that makes dz
-constexpr int kDzSplitRows = 8;      // (as halves)
 
 enum LinearForm { kLinearBf16, kLinearHalves, kLinearSingle };  // what the products' operands hold (linear.hip)
 
@@ -87,6 +86,7 @@ struct LinearPlan {
     int32_t tile, splits;        // forward: tile, and parts that its sums run over side by side
     int32_t front;               // tile columns of 256; tiles of 128 take what follows
     int32_t back_tile, dx_splits, dw_splits;
+    int32_t split_rows;          // tokens of a work-group that makes dz as halves
     int32_t bias_parts;          // rows of sums that dbias is joined from
     int64_t ld_dim, ld_wide;     // 16-bit elements of a row of x's and w's copies, of dz
     int64_t pad_tokens;          // rows of dz

@@ -49,7 +49,8 @@ double join_time(int parts, int64_t n, double each) {
     return parts > 1 ? 4.4 + each * 2e-6 * static_cast<double>(n * parts) : 0.0;
 }
 
-// fp32 products as they are up to this many tokens.
+// fp32 products as they are up to this many tokens.  128 tokens of 4096 -> 4800 forward: 58 us by tiles of fp32, 67 as
+// halves; 13 tokens of 6400 -> 4800 backward: 72 and 165; 74 of 1024 -> 6400 backward as halves: 46.
 constexpr int64_t kSingleForward = 128, kSingleBackward = 64;
 
 // Tile columns: the last of 256 takes half as long where 128 columns of it lie past the end.
@@ -123,18 +124,9 @@ void cut_backward(dsm::LinearPlan* q) {
     const double f32 = q->f32 ? kBackward.f32 : 1.0;
     double best = 0.0;
     if (q->back_form == dsm::kLinearSingle) {
-        // One row of tiles of 64 for dx; dw's tiles have a step or two and run beside them.
-        q->back_tile = 64;
-        const int64_t steps = tiles(N, 64), cols = tiles(T, 64) * tiles(D, 64);
-        for (int s = 1; s <= kMaxSplits && (s == 1 || s * 256 <= N); ++s) {
-            const double turns = std::ceil(static_cast<double>(cols * s) / 512);
-            const double cost = turns * (static_cast<double>(tiles(steps, s)) * (cols * s > 256 ? kSingle.full[0] : kSingle.alone[0]) + 2.5) +
-                                join_time(s, T * D, 0.25);
-            if (best == 0.0 || cost < best) {
-                best = cost;
-                q->dx_splits = s;
-            }
-        }
+        // dx by slabs of 64 columns, of 256 work-groups or more; parts of 256 rows of w at least.
+        const int64_t slabs = tiles(D, 64);
+        q->dx_splits = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>({kMaxSplits, tiles(512, slabs), N / 256})));
         return;
     }
     for (int i = 0; i < 3; ++i) {
@@ -214,11 +206,12 @@ dsm::LinearPlan make_linear_plan(const dsm_linear_problem* p) {
     if (!p->grads || T == 0) return q;
     at = common;
     cut_backward(&q);
-    q.bias_parts = static_cast<int32_t>(q.back_form == dsm::kLinearHalves ? tiles(T, dsm::kDzSplitRows) : q.pad_tokens / dsm::kDzRows);
+    q.split_rows = T >= 1536 || N > 8192 ? 8 : 2;
+    q.bias_parts = static_cast<int32_t>(q.back_form == dsm::kLinearHalves ? tiles(T, q.split_rows) : q.pad_tokens / dsm::kDzRows);
     q.dz = take(q.pad_tokens * q.ld_wide * (q.dz_halves ? 4 : 2));
     q.z_exp = take(T * 4);
     q.w_tops = take(dsm::kLinearTopParts * 4);
-    q.tops = take(q.pad_tokens / dsm::kDzSplitRows * 4);
+    q.tops = take(q.pad_tokens / q.split_rows * 4);
     q.dx_parts = take(q.dx_splits > 1 ? q.dx_splits * T * q.ld_dx * 4 : 0);
     q.dw_parts = take(q.dw_splits > 1 ? q.dw_splits * N * q.ld_dx * 4 : 0);
     q.bias_sums = take(q.bias_parts * N * 4);
@@ -480,7 +473,9 @@ dsm_status dsm_linear_backward(const dsm_linear_problem* problem, const dsm_line
     // the last token on meet x's, so they have to be zeros.
     c.x_direct = !c.p.dz_halves && direct(c.p.back_form, b.x, b.x_stride, p.dim, 8);
     c.w_direct = direct(c.p.back_form, b.w, b.w_stride, p.dim, 8);
-    c.dz_direct = !act && direct(c.p.back_form, b.dy, b.dy_stride, p.wide, 64) && p.tokens % 64 == 0;
+    // (Few tokens in fp32 take dz from its copy, which has zeros behind it.)
+    c.dz_direct = !act && c.p.back_form == dsm::kLinearBf16 && direct(c.p.back_form, b.dy, b.dy_stride, p.wide, 64) &&
+                  p.tokens % 64 == 0;
     return launched("launching the linear layer's gradients", dsm::launch_linear_backward(c, static_cast<hipStream_t>(b.stream)));
 }
 

@@ -420,56 +420,60 @@ __global__ __launch_bounds__(256) void k_copies(LinearCall c, int from, bool twi
 }
 
 // dz with zeros behind its rows (unless it is dy, read where it lies) and dbias's sums:
-// kDzRows tokens from row0 on by 512 columns from col0 on, by a work-group of WAVES.
-template <bool F32, int WAVES>
-__device__ __forceinline__ void dz_block(const LinearCall& c, int64_t row0, int col0, V8 (*sums)[64]) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = col0 + lane * 8;
+// kDzRows tokens from row0 on by kDzCols columns from col0 on, by a work-group of THREADS;
+// 16 lanes have a row's columns, eight each.  (64 lanes for 512 columns: few tokens then
+// have few work-groups, whose rows wait for each other; 64 x 1600 in fp32 27 us.)
+constexpr int kDzCols = 128;
+template <bool F32, int THREADS>
+__device__ __forceinline__ void dz_block(const LinearCall& c, int64_t row0, int col0, V8 (*sums)[16]) {
+    constexpr int kLanes = THREADS / 16;
+    const int lane = threadIdx.x & 15, first = threadIdx.x >> 4, col = col0 + lane * 8;
     const int wide = c.p.wide, have = max(0, min(wide - col, 8));
     const int64_t ld = c.p.ld_wide / (F32 ? 2 : 1);
     V8 sum;
 #pragma unroll
     for (int q = 0; q < 8; ++q) sum.v[q] = 0.f;
-#pragma unroll 8
-    for (int k = wave; k < kDzRows; k += WAVES) {
-        const int64_t row = row0 + k;
+#pragma unroll
+    for (int k = 0; k < kDzRows / kLanes; ++k) {
+        const int64_t row = row0 + first + k * kLanes;
         const int here = row < c.p.tokens ? have : 0;
         V8 d = rows::load8<F32>(c.dy, row * c.dy_stride + col, here);
         if (c.p.act != DSM_ACT_NONE)
             times_slope<!F32>(c.p.act, d, rows::load8<F32>(c.z_in, row * c.z_stride + col, here), here);
 #pragma unroll
         for (int q = 0; q < 8; ++q) sum.v[q] += d.v[q];
-        if (c.dz_direct || row >= c.p.pad_tokens || col >= ld) continue;
-        rows::store8<F32>(c.workspace + c.p.dz, row * ld + col, d, 8);
-        if (!F32 && c.p.dz_halves) {
+        if (!c.dz_direct && row < c.p.pad_tokens && col < ld) {
+            rows::store8<F32>(c.workspace + c.p.dz, row * ld + col, d, 8);
+            if (!F32 && c.p.dz_halves) {
 #pragma unroll
-            for (int q = 0; q < 8; ++q) d.v[q] -= rows::bf16_to_float(rows::float_to_bf16(d.v[q]));
-            rows::store8<false>(c.workspace + c.p.dz, (c.p.pad_tokens + row) * ld + col, d, 8);
+                for (int q = 0; q < 8; ++q) d.v[q] -= rows::bf16_to_float(rows::float_to_bf16(d.v[q]));
+                rows::store8<false>(c.workspace + c.p.dz, (c.p.pad_tokens + row) * ld + col, d, 8);
+            }
         }
     }
     if (!c.dbias) return;
-    sums[wave][lane] = sum;
+    sums[first][lane] = sum;
     __syncthreads();
-    if (wave != 0) return;
+    if (first != 0) return;
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w)
+    for (int w = 1; w < kLanes; ++w)
 #pragma unroll
         for (int q = 0; q < 8; ++q) sum.v[q] += sums[w][lane].v[q];
     rows::store8<true>(c.workspace + c.p.bias_sums, row0 / kDzRows * wide + col, sum, have);
 }
 template <bool F32>
 __global__ __launch_bounds__(256) void k_dz(LinearCall c) {
-    __shared__ V8 sums[4][64];
-    dz_block<F32, 4>(c, static_cast<int64_t>(blockIdx.y) * kDzRows, blockIdx.x * 512, sums);
+    __shared__ V8 sums[16][16];
+    dz_block<F32, 256>(c, static_cast<int64_t>(blockIdx.y) * kDzRows, blockIdx.x * kDzCols, sums);
 }
 
-// Halves: dz, its rows' exponents, dbias's sums, and the least exponent of x dz, kDzSplitRows
-// tokens a work-group; the work-groups before those look for w's largest magnitude.  A
+// Halves: dz, its rows' exponents, dbias's sums, and the least exponent of x dz, R tokens a
+// work-group (two, where there are too few of them for every CU); the work-groups before those look for w's largest magnitude.  A
 // work-group's threads have a row's columns between them, eight each, so that the rows stay in
 // registers until their exponents are known (HOLD: up to 8192 columns; wider rows are read
 // again).  2045 x 4096 with an activation: 39 us by 256 threads that read twice.
-template <bool HOLD>
+template <bool HOLD, int R>
 __global__ __launch_bounds__(1024) void k_dz_split(LinearCall c, int top_groups) {
-    constexpr int R = kDzSplitRows;
     __shared__ uint32_t tops[R][16];
     __shared__ uint32_t x_tops[R];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, span = blockDim.x * 8;
@@ -853,13 +857,10 @@ struct BackJobs {
     int32_t count[3];
     int32_t dw_first;
 };
-// Few tokens: dx is as narrow as one tile of 64, and dw's sums have one or two steps.
-constexpr int dw_tile_of(LinearForm form, int bm) { return form == kLinearSingle ? 128 : bm; }
 template <LinearForm FORM, int BM>
 __global__ __launch_bounds__(tile::threads_of(BM)) void k_backward(LinearCall c, BackJobs jobs) {
-    constexpr int BW = dw_tile_of(FORM, BM);
     using TX = tile::Pick<elem(FORM), BM, kContig, kStrided>;
-    using TW = tile::Pick<elem(FORM), BW, kStrided, kStrided>;
+    using TW = tile::Pick<elem(FORM), BM, kStrided, kStrided>;
     constexpr int kLds = TX::kLdsBytes > TW::kLdsBytes ? TX::kLdsBytes : TW::kLdsBytes;
     __shared__ __align__(1024) char lds[kLds];
     const int x = blockIdx.x % kXcds;
@@ -869,32 +870,180 @@ __global__ __launch_bounds__(tile::threads_of(BM)) void k_backward(LinearCall c,
     if (id >= jobs.count[kind]) return;
     if (kind == 2) {
         if constexpr (FORM != kLinearHalves) {
-            const int across = (c.p.wide + 511) / 512, down = id / across;
-            dz_block<is_f32(FORM), tile::threads_of(BM) / 64>(c, static_cast<int64_t>(down) * kDzRows, (id - down * across) * 512,
-                                                              reinterpret_cast<V8(*)[64]>(lds));
+            const int across = (c.p.wide + kDzCols - 1) / kDzCols, down = id / across;
+            dz_block<is_f32(FORM), tile::threads_of(BM)>(c, static_cast<int64_t>(down) * kDzRows, (id - down * across) * kDzCols,
+                                                         reinterpret_cast<V8(*)[16]>(lds));
         }
     } else if ((kind == 0) == (jobs.dw_first != 0)) {
-        back_tile<FORM, BW, true>(c, id, (DSM_LDS char*)lds);
+        back_tile<FORM, BM, true>(c, id, (DSM_LDS char*)lds);
     } else {
         back_tile<FORM, BM, false>(c, id, (DSM_LDS char*)lds);
     }
 }
 
-// What is left: dbias from its sums (the first work-groups, 64 columns each), and dx
+// ---- Few tokens in fp32: gradients ----
+//
+// Both products straight from memory, four columns a lane: a matrix instruction takes 16
+// rows of its first operand across the lanes, and element e of what lane i loaded stands
+// for column 4 i + e, so that four instructions take four times 16 columns and their sums
+// lie side by side again.  No LDS on the way.
+//   dx  4 x 16 columns of d and a part of n to a wave: w is read once, dz from the caches.
+//   dw  4 x 16 columns of d by kFewRows rows of n to a wave: x is kept in registers, and
+//       every step writes 16 rows of 256 bytes.
+// 13 tokens of 6400 -> 4800, both products: 63 us, 3.9 TB/s (by tiles of fp32 102).
+
+constexpr int kFewBackWaves = 4, kFewRows = 64;
+
+struct FewJobs {
+    int32_t slabs, dx, dw;  // slabs of 64 columns of d; work-groups
+};
+
+// Four columns from `col` on, of which `have` exist.
+__device__ __forceinline__ f4 four(const float* row, int col, int have) {
+    if (have >= 4) return *reinterpret_cast<const rows::f4_at*>(row + col);
+    f4 v = {0.f, 0.f, 0.f, 0.f};
+    if (have > 0) {
+#pragma unroll
+        for (int e = 0; e < 3; ++e) {
+            const float a = row[col + min(e, have - 1)];
+            v[e] = e < have ? a : 0.f;
+        }
+    }
+    return v;
+}
+__device__ __forceinline__ void store_four(float* row, int col, int have, f4 v) {
+    if (have >= 4) {
+        *reinterpret_cast<rows::f4_at*>(row + col) = v;
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+        if (e < have) row[col + e] = v[e];
+}
+
+template <int G>
+__global__ __launch_bounds__(kFewBackWaves * 64) void k_few_backward(LinearCall c, FewJobs jobs) {
+    __shared__ f4 sums[kFewBackWaves][4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, k = lane >> 4;
+    const int dim = c.p.dim, wide = c.p.wide;
+    const int64_t ld = c.p.ld_wide / 2;
+    const float* dz = reinterpret_cast<const float*>(c.workspace + c.p.dz);
+    if (static_cast<int>(blockIdx.x) < jobs.dx) {
+        const int part = blockIdx.x / jobs.slabs, d0 = (blockIdx.x - part * jobs.slabs) * 64, col = d0 + 4 * i, have = dim - col;
+        const float* w = static_cast<const float*>(c.w);
+        // Runs of 16 rows of w, every fourth one to a wave.
+        const int runs = (wide + 15) / 16, each = (runs + c.p.dx_splits - 1) / c.p.dx_splits;
+        const int begin = part * each, end = min(begin + each, runs);
+        f4 acc[G][4];
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[g][e] = f4{0.f, 0.f, 0.f, 0.f};
+        constexpr int kAhead = G < 4 ? 4 : 2;
+        for (int first = begin + wave; first < end; first += kFewBackWaves * kAhead) {
+            f4 a[kAhead][4], b[kAhead][G];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int n0 = (first + u * kFewBackWaves) * 16;
+                if (first + u * kFewBackWaves < end) {
+                    // (Rows past the last one meet zeros in dz.)
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) a[u][s] = four(w + min(n0 + 4 * k + s, wide - 1) * c.w_stride, col, have);
+#pragma unroll
+                    for (int g = 0; g < G; ++g) b[u][g] = *reinterpret_cast<const f4*>(dz + (g * 16 + i) * ld + n0 + 4 * k);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (first + u * kFewBackWaves < end) {
+#pragma unroll
+                    for (int s = 0; s < 4; ++s)
+#pragma unroll
+                        for (int g = 0; g < G; ++g)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                acc[g][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[u][s][e], b[u][g][s], acc[g][e], 0, 0, 0);
+                }
+        }
+        // Lane l's acc[g][e][r] is token 16 g + l % 16, column d0 + 16 (l / 16) + 4 r + e; wave r sums it.
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            if (g > 0) __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sums[wave][e][lane] = acc[g][e];
+            __syncthreads();
+            f4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float* at = reinterpret_cast<const float*>(&sums[0][e][lane]) + wave;
+                v[e] = at[0];
+#pragma unroll
+                for (int o = 1; o < kFewBackWaves; ++o) v[e] += at[o * 4 * 64 * 4];
+            }
+            const int token = g * 16 + i, at = d0 + 16 * k + 4 * wave;
+            if (token >= c.p.tokens) continue;
+            if (c.p.dx_splits > 1)
+                store_four(reinterpret_cast<float*>(c.workspace + c.p.dx_parts) + (static_cast<int64_t>(part) * c.p.tokens + token) * c.p.ld_dx,
+                           at, static_cast<int>(c.p.ld_dx) - at, v);
+            else
+                store_four(static_cast<float*>(c.dx) + token * c.dx_stride, at, dim - at, v);
+        }
+        return;
+    }
+    const int id = blockIdx.x - jobs.dx, down = id / jobs.slabs, d0 = (id - down * jobs.slabs) * 64, col = d0 + 4 * i, have = dim - col;
+    const int first = (down * kFewBackWaves + wave) * kFewRows;
+    const float* x = static_cast<const float*>(c.x);
+    f4 a[4 * G];
+#pragma unroll
+    for (int s = 0; s < 4 * G; ++s) a[s] = four(x + min(4 * s + k, c.p.tokens - 1) * c.x_stride, col, have);
+    // (dz has zeros for the tokens that x does not have, and 64 columns a run.)
+    const int last = min(first + kFewRows, wide);
+    float next[4 * G];
+    const auto load = [&](int n0) {
+#pragma unroll
+        for (int s = 0; s < 4 * G; ++s) next[s] = dz[(4 * s + k) * ld + min(n0, static_cast<int>(ld) - 16) + i];
+    };
+    load(first);
+    for (int n0 = first; n0 < last; n0 += 16) {
+        float b[4 * G];
+#pragma unroll
+        for (int s = 0; s < 4 * G; ++s) b[s] = next[s];
+        load(n0 + 16);
+        f4 acc[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < 4 * G; ++s)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[s][e], b[s], acc[e], 0, 0, 0);
+        if (n0 + i >= wide) continue;
+        float* row = static_cast<float*>(c.dw) + (n0 + i) * c.dw_stride;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int at = d0 + 16 * k + 4 * q;
+            store_four(row, at, dim - at, f4{acc[0][q], acc[1][q], acc[2][q], acc[3][q]});
+        }
+    }
+}
+
+// What is left: dbias from its sums (the first work-groups, 16 columns each), and dx
 // and dw where their sums are in parts.
 __global__ __launch_bounds__(256) void k_backward_join(LinearCall c, int bias_groups) {
-    __shared__ float sums[4][64];
+    __shared__ float sums[16][16];
     if (static_cast<int>(blockIdx.x) < bias_groups) {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = blockIdx.x * 64 + lane;
+        const int lane = threadIdx.x & 15, first = threadIdx.x >> 4, col = blockIdx.x * 16 + lane;
         float s = 0.f;
         if (col < c.p.wide) {
             const float* at = reinterpret_cast<const float*>(c.workspace + c.p.bias_sums) + col;
 #pragma unroll 8
-            for (int q = wave; q < c.p.bias_parts; q += 4) s += at[static_cast<int64_t>(q) * c.p.wide];
+            for (int q = first; q < c.p.bias_parts; q += 16) s += at[static_cast<int64_t>(q) * c.p.wide];
         }
-        sums[wave][lane] = s;
+        sums[first][lane] = s;
         __syncthreads();
-        if (wave == 0 && col < c.p.wide) c.dbias[col] = (s + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+        if (first != 0 || col >= c.p.wide) return;
+#pragma unroll
+        for (int w = 1; w < 16; ++w) s += sums[w][lane];
+        c.dbias[col] = s;
         return;
     }
     const int eights = (c.p.dim + 7) / 8;
@@ -977,16 +1126,28 @@ void few(const LinearCall& c, hipStream_t stream) {
 template <LinearForm FORM, int BM>
 void backward(const LinearCall& c, bool with_bias, hipStream_t stream) {
     const auto tiles = [](int n, int of) { return (n + of - 1) / of; };
-    constexpr int BW = dw_tile_of(FORM, BM);
     const int dx = c.dx ? tiles(c.p.tokens, BM) * tiles(c.p.dim, BM) * c.p.dx_splits : 0;
-    const int dw = c.dw ? tiles(c.p.wide, BW) * tiles(c.p.dim, BW) * c.p.dw_splits : 0;
+    const int dw = c.dw ? tiles(c.p.wide, BM) * tiles(c.p.dim, BM) * c.p.dw_splits : 0;
     BackJobs jobs;
     jobs.dw_first = static_cast<int64_t>(c.p.tokens) * c.p.dx_splits > static_cast<int64_t>(c.p.wide) * c.p.dw_splits;
     jobs.count[0] = jobs.dw_first ? dw : dx;
     jobs.count[1] = jobs.dw_first ? dx : dw;
-    jobs.count[2] = with_bias ? static_cast<int>((c.p.wide + 511) / 512 * (c.p.pad_tokens / kDzRows)) : 0;
+    jobs.count[2] = with_bias ? static_cast<int>((c.p.wide + kDzCols - 1) / kDzCols * (c.p.pad_tokens / kDzRows)) : 0;
     const int groups = per_xcd(jobs.count[0]) + per_xcd(jobs.count[1]) + per_xcd(jobs.count[2]);
     k_backward<FORM, BM><<<kXcds * groups, tile::threads_of(BM), 0, stream>>>(c, jobs);
+}
+
+void few_backward(const LinearCall& c, hipStream_t stream) {
+    FewJobs jobs;
+    jobs.slabs = (c.p.dim + 63) / 64;
+    jobs.dx = c.dx ? jobs.slabs * c.p.dx_splits : 0;
+    jobs.dw = c.dw ? jobs.slabs * ((c.p.wide + kFewBackWaves * kFewRows - 1) / (kFewBackWaves * kFewRows)) : 0;
+    if (c.p.tokens <= 16)
+        k_few_backward<1><<<jobs.dx + jobs.dw, kFewBackWaves * 64, 0, stream>>>(c, jobs);
+    else if (c.p.tokens <= 32)
+        k_few_backward<2><<<jobs.dx + jobs.dw, kFewBackWaves * 64, 0, stream>>>(c, jobs);
+    else
+        k_few_backward<4><<<jobs.dx + jobs.dw, kFewBackWaves * 64, 0, stream>>>(c, jobs);
 }
 
 template <LinearForm FORM>
@@ -996,36 +1157,37 @@ void backward(const LinearCall& c, hipStream_t stream) {
     const int from = c.dw && !c.x_direct ? 0 : 1, to = c.dx && !c.w_direct ? 2 : 1;
     if constexpr (FORM == kLinearHalves) {
         const int top_groups = c.dx ? static_cast<int>(groups_for((c.p.wide + 3) / 4, kLinearTopParts)) : 0;
-        const int dz_groups = static_cast<int>(c.p.pad_tokens / kDzSplitRows);
-        // (ld_wide counts halves: its columns, eight a thread, are a multiple of 64.)
-        const int threads = static_cast<int>((c.p.ld_wide / 16 + 63) / 64 * 64);
-        if (threads <= 1024)
-            k_dz_split<true><<<top_groups + dz_groups, threads, 0, stream>>>(c, top_groups);
+        const int dz_groups = static_cast<int>(c.p.pad_tokens / c.p.split_rows);
+        // (ld_wide counts halves: its columns, eight a thread, are a multiple of 64.  Four waves or more, for x's rows.)
+        const int threads = static_cast<int>((c.p.ld_wide / 16 + 63) / 64 * 64), groups = top_groups + dz_groups;
+        if (threads > 1024)
+            k_dz_split<false, 8><<<groups, 1024, 0, stream>>>(c, top_groups);
+        else if (c.p.split_rows == 8)
+            k_dz_split<true, 8><<<groups, threads < 256 ? 256 : threads, 0, stream>>>(c, top_groups);
         else
-            k_dz_split<false><<<top_groups + dz_groups, 1024, 0, stream>>>(c, top_groups);
+            k_dz_split<true, 2><<<groups, threads < 256 ? 256 : threads, 0, stream>>>(c, top_groups);
         if (from < to)
             k_back_copies<<<dim3(groups_for((copies_rows + 3) / 4, 2048), to - from), 256, 0, stream>>>(c, from, top_groups,
                                                                                                       dz_groups);
     } else {
         // (Where dz is dy, dbias's sums run beside the products.)
         if (!c.dz_direct || (c.dbias && !c.dx && !c.dw))
-            k_dz<is_f32(FORM)><<<dim3((c.p.ld_wide / units(FORM) + 511) / 512, c.p.pad_tokens / kDzRows), 256, 0, stream>>>(c);
-        if (from < to)
+            k_dz<is_f32(FORM)><<<dim3((c.p.ld_wide / units(FORM) + kDzCols - 1) / kDzCols, c.p.pad_tokens / kDzRows), 256, 0, stream>>>(c);
+        if (FORM == kLinearBf16 && from < to)
             k_copies<FORM><<<dim3(groups_for((copies_rows + 3) / 4, 4096), to - from), 256, 0, stream>>>(c, from, c.p.dz_halves);
     }
     if (c.dx || c.dw) {
         const bool with_bias = FORM != kLinearHalves && c.dz_direct && c.dbias;
-        bool done = false;
-        if constexpr (FORM != kLinearSingle) {
-            if (c.p.back_tile == 128)
-                backward<FORM, 128>(c, with_bias, stream);
-            else if (c.p.back_tile == 256)
-                backward<FORM, 256>(c, with_bias, stream);
-            done = c.p.back_tile != 64;
-        }
-        if (!done) backward<FORM, 64>(c, with_bias, stream);
+        if constexpr (FORM == kLinearSingle)
+            few_backward(c, stream);
+        else if (c.p.back_tile == 64)
+            backward<FORM, 64>(c, with_bias, stream);
+        else if (c.p.back_tile == 128)
+            backward<FORM, 128>(c, with_bias, stream);
+        else
+            backward<FORM, 256>(c, with_bias, stream);
     }
-    const int bias_groups = c.dbias ? (c.p.wide + 63) / 64 : 0;
+    const int bias_groups = c.dbias ? (c.p.wide + 15) / 16 : 0;
     const int64_t eights = (c.p.dim + 7) / 8;
     const int64_t join = (c.dx && c.p.dx_splits > 1 ? c.p.tokens * eights : 0) + (c.dw && c.p.dw_splits > 1 ? c.p.wide * eights : 0);
     const unsigned groups = bias_groups + groups_for((join + 255) / 256, 4096);
