@@ -557,16 +557,16 @@ typedef struct dsm_linear_buffers {
     void* stream;
 } dsm_linear_buffers;
 
-/* dsm_linear_workspace - host only: the workspace of a problem in bytes (0 for up to
- * 64 tokens without gradients).  Errors: DSM_ERR_INVALID_ARG. */
+/* dsm_linear_workspace - host only: the workspace of a problem in bytes (for up to 64
+ * tokens without gradients 0, or the parts of its sums).  Errors: DSM_ERR_INVALID_ARG. */
 DSM_API dsm_status dsm_linear_workspace(const dsm_linear_problem* problem, int64_t* workspace_bytes);
 
 /*
  * dsm_linear - z = x w^T + bias;  y = act(z) + residual
- * y takes z before its rounding.  Products of bf16 take their operands' bits; those of
- * fp32 carry 22 bits or more of entries down to 2^-16 of their row's largest finite
- * magnitude (smaller ones lose bits, and vanish below 2^-39 of it), all of them up to
- * 64 tokens.  Sums, bias, activation and residual are fp32, rounded once.  Reruns give
+ * y takes z before its rounding.  Products of bf16 take their operands' bits, and so do
+ * those of fp32 up to 128 tokens; of more they carry 22 bits or more of entries down to
+ * 2^-16 of their row's largest finite magnitude (smaller ones lose bits, and vanish below
+ * 2^-39 of it).  Sums, bias, activation and residual are fp32, rounded once.  Reruns give
  * the same bits.  Non-finite values reach every output that depends on them.
  * dsm_linear reads x, w, bias, residual and writes y and z; neither may overlap what is
  * read, except y the residual.  Errors: DSM_ERR_INVALID_ARG; DSM_ERR_HIP.
@@ -578,9 +578,10 @@ DSM_API dsm_status dsm_linear(const dsm_linear_problem* problem, const dsm_linea
  *   dz = dy act'(z);  dx = dz w;  dw = dz^T x;  dbias = the tokens' sum of dz
  * (the residual's gradient is dy itself).  Outputs are written, not added to; any may be
  * NULL.  Where there is an activation, bf16 takes dz rounded to bf16 into dx and a bf16
- * dw, as two bf16 halves (16 bits) into an fp32 dw, and in fp32 into dbias.  Products of fp32 carry 22 bits or more of entries of dz
- * down to 2^-16 of their token's largest, of w of its largest, and of x of the largest
- * that a token's x and dz make together.
+ * dw, as two bf16 halves (16 bits) into an fp32 dw, and in fp32 into dbias.  Products of
+ * fp32 take their operands' bits up to 64 tokens; of more they carry 22 bits or more of
+ * entries of dz down to 2^-16 of their token's largest, of w of its largest, and of x of
+ * the largest that a token's x and dz make together.
  * dx, dw and dbias may not overlap what is read.  Errors: DSM_ERR_INVALID_ARG; DSM_ERR_HIP.
  */
 DSM_API dsm_status dsm_linear_backward(const dsm_linear_problem* problem, const dsm_linear_buffers* buffers);

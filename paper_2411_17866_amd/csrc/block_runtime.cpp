@@ -542,7 +542,11 @@ dsm_status dsm_residual_norm_backward(const dsm_norm_problem* problem, const dsm
                 return invalid("an output in place of an input has another stride");
     float* const sums[dsm::kNormSums] = {b.dweight, b.dbias, b.dgate, b.dpost_weight, b.dpost_bias};
     bool any = false;
-    for (float* s : sums) any = any || s;
+    for (int i = 0; i < dsm::kNormSums; ++i) {
+        any = any || sums[i];
+        for (int k = 0; k < i; ++k)
+            if (sums[i] && sums[i] == sums[k]) return invalid("two vectors' gradients are one array");
+    }
     if (!any && (p.tokens == 0 || (!b.dh && !b.df))) return DSM_OK;
     dsm::NormCall c = norm_call(p, b);
     if (any && norm_bytes(problem) > 0)
@@ -605,7 +609,7 @@ dsm_status dsm_grad_clip(const dsm_clip_tensor* tensors, int32_t n_tensors, int3
     };
     int64_t counts[dsm::kClipGroups] = {};
     int launches = 0;
-    each([&] {
+    (void)each([&] {
         for (int k = 0; k < table.count; ++k) counts[table.e[k].group] += tiles(table.e[k].numel, dsm::kClipChunk);
         ++launches;
         return hipSuccess;

@@ -601,6 +601,10 @@ class GradClip(_Clip):
             places = [self._place(i, tensors[i]) for i in self._order]
             place = {"block": [p[0] for p in places], "stride": [p[1] for p in places]}
         data = list(map(torch.Tensor.data_ptr, map(tensors.__getitem__, self._order)))
+        if len(set(data)) < len(data):  # (tensors without elements may share an address)
+            given = [a for a, i in zip(data, self._order) if tensors[i].numel()]
+            if len(set(given)) < len(given):
+                raise ValueError("a tensor is given twice")
         return self._run(max_norm, self._norm(norm), data, **place)
 
 

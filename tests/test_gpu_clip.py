@@ -211,6 +211,11 @@ def test_refusals():
                  lambda: ops.GradClip([t], eps=-1.0)([t], 1.0)):
         with pytest.raises((ValueError, dsm.DsmError)):
             call()
+    twice = ops.GradClip([t, t[:0], t[:0], t])
+    with pytest.raises(ValueError, match="twice"):
+        twice([t, t[:0], t[:0], t], 1.0)
+    u = torch.ones(6, 8, device="cuda")
+    assert twice([t, t[:0], t[:0], u], 1.0).tolist() == [pytest.approx(96 ** 0.5)] and torch.equal(t, u)
     ar = arena.Arenas([100], 2, 2, dsm.DSM_BASE_SGD_MOMENTUM)
     with pytest.raises(ValueError):
         ops.ArenaClip(ar)(arena.Arenas([101], 2, 2, dsm.DSM_BASE_SGD_MOMENTUM), 1.0)
