@@ -14,6 +14,7 @@ namespace dsm {
 constexpr int kClipChunk = 16384;  // elements that a work-group takes
 constexpr int kClipEntries = 48;   // tensors of a launch
 constexpr int kClipGroups = 256;   // groups of a call
+constexpr int64_t kClipOnce = int64_t(256) << 20;  // bytes of a call that the last-level cache does not hold
 constexpr int kClipFewGroups = 64, kClipFewChunks = 2048;  // of a call whose norms take no launch of their own
 
 struct ClipEntry {
@@ -38,7 +39,8 @@ struct ClipStarts {
 using ClipGroups = ClipStarts<int64_t, kClipGroups>;
 using ClipFew = ClipStarts<int32_t, kClipFewGroups>;
 
-hipError_t launch_clip_squares(const ClipTable& t, double* parts, hipStream_t stream);
+// `bytes`: of all the call's tensors.
+hipError_t launch_clip_squares(const ClipTable& t, int64_t bytes, double* parts, hipStream_t stream);
 hipError_t launch_clip_norms(const ClipGroups& g, const double* parts, float* norm, double* factor, hipStream_t stream);
 hipError_t launch_clip_scale(const ClipTable& t, const double* factor, hipStream_t stream);
 // The last two in one, where every work-group sums its group's parts itself.

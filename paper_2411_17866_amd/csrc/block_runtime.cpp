@@ -607,16 +607,19 @@ dsm_status dsm_grad_clip(const dsm_clip_tensor* tensors, int32_t n_tensors, int3
             if (const hipError_t e = use()) return e;
         return hipSuccess;
     };
-    int64_t counts[dsm::kClipGroups] = {};
+    int64_t counts[dsm::kClipGroups] = {}, bytes = 0;
     int launches = 0;
     (void)each([&] {
-        for (int k = 0; k < table.count; ++k) counts[table.e[k].group] += tiles(table.e[k].numel, dsm::kClipChunk);
+        for (int k = 0; k < table.count; ++k) {
+            counts[table.e[k].group] += tiles(table.e[k].numel, dsm::kClipChunk);
+            bytes += table.e[k].numel * (table.e[k].bf16 ? 2 : 4);
+        }
         ++launches;
         return hipSuccess;
     });
     groups.start[0] = 0;
     for (int g = 0; g < n_groups; ++g) groups.start[g + 1] = groups.start[g] + counts[g];
-    if (const hipError_t e = each([&] { return dsm::launch_clip_squares(table, parts, s); })) return launched("launching the norms", e);
+    if (const hipError_t e = each([&] { return dsm::launch_clip_squares(table, bytes, parts, s); })) return launched("launching the norms", e);
     const bool scales = max_norm < INFINITY;
     if (scales && launches == 1 && n_groups <= dsm::kClipFewGroups && groups.start[n_groups] <= dsm::kClipFewChunks) {
         dsm::ClipFew few;

@@ -37,16 +37,26 @@ struct Raw8<true> {
     f4 a, b;
 };
 
-// Eight elements from element `at` on, of which `have` exist (the others are 0).
-template <bool F32>
-__device__ __forceinline__ Raw8<F32> raw8(const void* base, int64_t at, int have) {
+// Loads that leave the caches to what is read again (ONCE), or not.
+template <bool ONCE, class T>
+__device__ __forceinline__ T from(const T* p) {
+    if constexpr (ONCE)
+        return __builtin_nontemporal_load(p);
+    else
+        return *p;
+}
+
+// Eight elements from element `at` on, of which `have` exist (the others are 0); in fp32 all
+// eight may also be two fours, `apart` from each other.
+template <bool F32, bool ONCE = false>
+__device__ __forceinline__ Raw8<F32> raw8(const void* base, int64_t at, int have, int apart = 4) {
     Raw8<F32> o;
     if constexpr (F32) {
         const float* p = static_cast<const float*>(base) + at;
         o.a = o.b = f4{0.f, 0.f, 0.f, 0.f};
         if (have >= 8) {
-            o.a = *reinterpret_cast<const f4_at*>(p);
-            o.b = *reinterpret_cast<const f4_at*>(p + 4);
+            o.a = from<ONCE>(reinterpret_cast<const f4_at*>(p));
+            o.b = from<ONCE>(reinterpret_cast<const f4_at*>(p + apart));
         } else if (have > 0) {
             // The last one again for those that are missing: loads side by side, no branches.
             // (Their places are not kept in registers from one row to the next.)
@@ -63,7 +73,7 @@ __device__ __forceinline__ Raw8<F32> raw8(const void* base, int64_t at, int have
         const u16* p = static_cast<const u16*>(base) + at;
         o.v = u16x8{0, 0, 0, 0, 0, 0, 0, 0};
         if (have >= 8) {
-            o.v = *reinterpret_cast<const u16x8_at*>(p);
+            o.v = from<ONCE>(reinterpret_cast<const u16x8_at*>(p));
         } else if (have > 0) {
             int last = have - 1;
             asm volatile("" : "+v"(last));
@@ -95,13 +105,13 @@ __device__ __forceinline__ void shift(V8& v, int back) {
 #pragma unroll
         for (int q = 0; q < 8; ++q) v.v[q] = (back & by) ? (q + by < 8 ? v.v[q + by] : 0.f) : v.v[q];
 }
-template <bool F32>
-__device__ __forceinline__ V8 load8(const void* base, int64_t at, int have) {
-    return wide8(raw8<F32>(base, at, have));
+template <bool F32, bool ONCE = false>
+__device__ __forceinline__ V8 load8(const void* base, int64_t at, int have, int apart = 4) {
+    return wide8(raw8<F32, ONCE>(base, at, have, apart));
 }
 
 template <bool F32>
-__device__ __forceinline__ void store8(void* base, int64_t at, const V8& x, int have) {
+__device__ __forceinline__ void store8(void* base, int64_t at, const V8& x, int have, int apart = 4) {
     if constexpr (F32) {
         float* p = static_cast<float*>(base) + at;
         if (have >= 8) {
@@ -112,7 +122,7 @@ __device__ __forceinline__ void store8(void* base, int64_t at, const V8& x, int 
                 b[q] = x.v[4 + q];
             }
             *reinterpret_cast<f4_at*>(p) = a;
-            *reinterpret_cast<f4_at*>(p + 4) = b;
+            *reinterpret_cast<f4_at*>(p + apart) = b;
         } else if (have > 0) {
 #pragma unroll
             for (int q = 0; q < 7; ++q)

@@ -38,6 +38,7 @@ struct ClipCall {
     const double *parts, *factor;
 };
 static std::vector<ClipCall> clip_calls;
+static int64_t clip_bytes = 0;
 
 template <class Groups>
 static std::vector<int64_t> starts_of(const Groups& g) {
@@ -55,7 +56,8 @@ hipError_t launch_norm(const NormCall& c, hipStream_t) { return norm_calls.push_
 hipError_t launch_norm_backward(const NormCall& c, hipStream_t) { return norm_calls.push_back(c), launch_result; }
 // The kernels' own rule is not compiled here.
 int norm_groups(int64_t tokens, int64_t) { return static_cast<int>(std::min<int64_t>(tokens, 700)); }
-hipError_t launch_clip_squares(const ClipTable& t, double* parts, hipStream_t) {
+hipError_t launch_clip_squares(const ClipTable& t, int64_t bytes, double* parts, hipStream_t) {
+    clip_bytes = bytes;
     return clip_calls.push_back({kSquares, t, {}, parts, nullptr}), launch_result;
 }
 hipError_t launch_clip_norms(const ClipGroups& g, const double* parts, float*, double* factor, hipStream_t) {
@@ -572,6 +574,9 @@ static void clipping() {
             ++tables[pass];
         }
         CHECK(got[0] == want);
+        int64_t bytes = 0;
+        for (const Stretch& r : want) bytes += r.bytes;
+        CHECK(want.empty() || clip_bytes == bytes);
         CHECK(got[1] == (max_norm < INFINITY ? want : std::vector<Stretch>()));
         CHECK(static_cast<int>(starts.size()) == groups + 1 && starts[0] == 0);
         for (int g = 0; g < groups; ++g) CHECK(starts[g + 1] - starts[g] == chunks[g]);

@@ -20,7 +20,7 @@ hipError_t launch_linear(const LinearCall& c, hipStream_t) {
 hipError_t launch_linear_backward(const LinearCall&, hipStream_t) { return hipSuccess; }
 hipError_t launch_norm(const NormCall&, hipStream_t) { return hipSuccess; }
 hipError_t launch_norm_backward(const NormCall&, hipStream_t) { return hipSuccess; }
-hipError_t launch_clip_squares(const ClipTable&, double*, hipStream_t) { return hipSuccess; }
+hipError_t launch_clip_squares(const ClipTable&, int64_t, double*, hipStream_t) { return hipSuccess; }
 hipError_t launch_clip_norms(const ClipGroups&, const double*, float*, double*, hipStream_t) { return hipSuccess; }
 hipError_t launch_clip_scale(const ClipTable&, const double*, hipStream_t) { return hipSuccess; }
 hipError_t launch_clip_rest(const ClipTable&, const ClipFew&, const double*, float*, hipStream_t) { return hipSuccess; }
