@@ -84,7 +84,7 @@ struct LinearPlan {
     int32_t f32, dw_f32;
     int32_t dz_halves;           // dz is two bf16 arrays, for dw
     LinearForm form, back_form;
-    int32_t few;                 // forward: no tiles
+    int32_t few, back_few;       // no tiles
     int32_t tile, splits;        // forward: tile, and parts that its sums run over side by side
     int32_t front;               // tile columns of 256; tiles of 128 take what follows
     int32_t back_tile, dx_splits, dw_splits;

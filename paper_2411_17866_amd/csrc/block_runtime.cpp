@@ -52,6 +52,9 @@ double join_time(int parts, int64_t n, double each) {
 // fp32 products as they are up to this many tokens.  128 tokens of 4096 -> 4800 forward: 58 us by tiles of fp32, 67 as
 // halves; 13 tokens of 6400 -> 4800 backward: 72 and 165; 74 of 1024 -> 6400 backward as halves: 46.
 constexpr int64_t kSingleForward = 128, kSingleBackward = 64;
+// bf16 gradients without tiles up to this many tokens: 1600 -> 6400 of 17 tokens 20.3 us and 25.4 by tiles, of 33
+// 24.7 and 26.4, of 64 25.5 and 20.9; 768 -> 2304 of 32 10.1 and 13.8, of 64 12.3 and 11.4.
+constexpr int64_t kFewBackward = 32;
 
 // Tile columns: the last of 256 takes half as long where 128 columns of it lie past the end.
 double columns(int64_t n, int of) {
@@ -123,7 +126,7 @@ void cut_backward(dsm::LinearPlan* q) {
     const int64_t T = q->tokens, D = q->dim, N = q->wide;
     const double f32 = q->f32 ? kBackward.f32 : 1.0;
     double best = 0.0;
-    if (q->back_form == dsm::kLinearSingle) {
+    if (q->back_few) {
         // dx by slabs of 64 columns, of 256 work-groups or more; parts of 256 rows of w at least.
         const int64_t slabs = tiles(D, 64);
         q->dx_splits = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>({kMaxSplits, tiles(512, slabs), N / 256})));
@@ -179,6 +182,7 @@ dsm::LinearPlan make_linear_plan(const dsm_linear_problem* p) {
     q.form = !q.f32 ? dsm::kLinearBf16 : T <= kSingleForward ? dsm::kLinearSingle : dsm::kLinearHalves;
     q.back_form = !q.f32 ? dsm::kLinearBf16 : T <= kSingleBackward ? dsm::kLinearSingle : dsm::kLinearHalves;
     q.few = T <= dsm::kLinearFew;
+    q.back_few = T <= (q.f32 ? kSingleBackward : kFewBackward);
     q.splits = q.dx_splits = q.dw_splits = 1;
     const int64_t width = q.f32 ? 2 : 1;  // 16-bit elements of a number
     q.ld_dim = round_up(D, 64) * width;
@@ -473,9 +477,9 @@ dsm_status dsm_linear_backward(const dsm_linear_problem* problem, const dsm_line
     // the last token on meet x's, so they have to be zeros.
     c.x_direct = !c.p.dz_halves && direct(c.p.back_form, b.x, b.x_stride, p.dim, 8);
     c.w_direct = direct(c.p.back_form, b.w, b.w_stride, p.dim, 8);
-    // (Few tokens in fp32 take dz from its copy, which has zeros behind it.)
-    c.dz_direct = !act && c.p.back_form == dsm::kLinearBf16 && direct(c.p.back_form, b.dy, b.dy_stride, p.wide, 64) &&
-                  p.tokens % 64 == 0;
+    // (Few tokens look for the ends of dz's rows themselves; in fp32 they take its copy.)
+    c.dz_direct = !act && c.p.back_form == dsm::kLinearBf16 &&
+                  (c.p.back_few || (direct(c.p.back_form, b.dy, b.dy_stride, p.wide, 64) && p.tokens % 64 == 0));
     return launched("launching the linear layer's gradients", dsm::launch_linear_backward(c, static_cast<hipStream_t>(b.stream)));
 }
 

@@ -459,7 +459,10 @@ __device__ __forceinline__ void dz_block(const LinearCall& c, int64_t row0, int 
     for (int w = 1; w < kLanes; ++w)
 #pragma unroll
         for (int q = 0; q < 8; ++q) sum.v[q] += sums[w][lane].v[q];
-    rows::store8<true>(c.workspace + c.p.bias_sums, row0 / kDzRows * wide + col, sum, have);
+    if (c.p.bias_parts == 1)
+        rows::store8<true>(c.dbias, col, sum, have);
+    else
+        rows::store8<true>(c.workspace + c.p.bias_sums, row0 / kDzRows * wide + col, sum, have);
 }
 template <bool F32>
 __global__ __launch_bounds__(256) void k_dz(LinearCall c) {
@@ -881,21 +884,23 @@ __global__ __launch_bounds__(tile::threads_of(BM)) void k_backward(LinearCall c,
     }
 }
 
-// ---- Few tokens in fp32: gradients ----
+// ---- Few tokens: gradients ----
 //
-// Both products straight from memory, four columns a lane: a matrix instruction takes 16
-// rows of its first operand across the lanes, and element e of what lane i loaded stands
-// for column 4 i + e, so that four instructions take four times 16 columns and their sums
-// lie side by side again.  No LDS on the way.
+// Both products straight from memory, four columns a lane, without tiles in LDS and without
+// copies of w and x.  A matrix instruction takes 16 of its first operand's rows across the
+// lanes; element e of what lane i loaded stands for column 4 i + e, so that four instructions
+// take four times 16 columns and their sums lie side by side again.  bf16 multiplies eight
+// steps of k a lane: its eight rows of four change places in registers first.
 //   dx  4 x 16 columns of d and a part of n to a wave: w is read once, dz from the caches.
-//   dw  4 x 16 columns of d by kFewRows rows of n to a wave: x is kept in registers, and
-//       every step writes 16 rows of 256 bytes.
-// 13 tokens of 6400 -> 4800, both products: 63 us, 3.9 TB/s (by tiles of fp32 102).
+//   dw  4 x 16 columns of d by kFewRows rows of n to a wave, whose x stays in registers:
+//       every row is written in pieces of 128 or 256 bytes.
+// 13 tokens of 6400 -> 4800, both products: in fp32 63 us, 3.9 TB/s (by tiles of fp32 102); in
+// bf16 28.6, dz's and dx's launches included, 4.3 TB/s.
 
 constexpr int kFewBackWaves = 4, kFewRows = 64;
 
 struct FewJobs {
-    int32_t slabs, dx, dw;  // slabs of 64 columns of d; work-groups
+    int32_t slabs, dx, dw, bias;  // slabs of 64 columns of d; work-groups
 };
 
 // Four columns from `col` on, of which `have` exist.
@@ -919,6 +924,76 @@ __device__ __forceinline__ void store_four(float* row, int col, int have, f4 v) 
 #pragma unroll
     for (int e = 0; e < 3; ++e)
         if (e < have) row[col + e] = v[e];
+}
+
+typedef u16 u16x4 __attribute__((ext_vector_type(4)));
+typedef u16x4 u16x4_at __attribute__((aligned(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+struct Two {  // four columns in bf16
+    uint32_t v[2];
+};
+__device__ __forceinline__ Two four(const u16* row, int col, int have) {
+    u16x4 v = {0, 0, 0, 0};
+    if (have >= 4) {
+        v = *reinterpret_cast<const u16x4_at*>(row + col);
+    } else if (have > 0) {
+#pragma unroll
+        for (int e = 0; e < 3; ++e) {
+            const u16 a = row[col + min(e, have - 1)];
+            v[e] = e < have ? a : static_cast<u16>(0);
+        }
+    }
+    return __builtin_bit_cast(Two, v);
+}
+// Eight rows of four columns: four columns of eight.
+__device__ __forceinline__ void turn(const Two (&rows)[8], bfloat8 (&cols)[4]) {
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        u32x4 even, odd;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            even[q] = __builtin_amdgcn_perm(rows[2 * q + 1].v[p], rows[2 * q].v[p], 0x05040100u);
+            odd[q] = __builtin_amdgcn_perm(rows[2 * q + 1].v[p], rows[2 * q].v[p], 0x07060302u);
+        }
+        cols[2 * p] = __builtin_bit_cast(bfloat8, even);
+        cols[2 * p + 1] = __builtin_bit_cast(bfloat8, odd);
+    }
+}
+
+// The waves' sums of dx.  Lane l's acc[g][e][r] is token 16 g + l % 16, column
+// d0 + 16 (l / 16) + 4 r + e; wave r sums it.
+template <bool F32, int G>
+__device__ __forceinline__ void few_dx_end(const LinearCall& c, const f4 (&acc)[G][4], int part, int d0, f4 (*sums)[4][64]) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = d0 + 16 * (lane >> 4) + 4 * wave;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        if (g > 0) __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sums[wave][e][lane] = acc[g][e];
+        __syncthreads();
+        f4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float* from = reinterpret_cast<const float*>(&sums[0][e][lane]) + wave;
+            v[e] = from[0];
+#pragma unroll
+            for (int o = 1; o < kFewBackWaves; ++o) v[e] += from[o * 4 * 64 * 4];
+        }
+        const int token = g * 16 + (lane & 15);
+        if (token >= c.p.tokens) continue;
+        if (c.p.dx_splits > 1) {
+            store_four(reinterpret_cast<float*>(c.workspace + c.p.dx_parts) + (static_cast<int64_t>(part) * c.p.tokens + token) * c.p.ld_dx,
+                       at, static_cast<int>(c.p.ld_dx) - at, v);
+        } else if constexpr (F32) {
+            store_four(static_cast<float*>(c.dx) + token * c.dx_stride, at, c.p.dim - at, v);
+        } else {
+            u16* row = static_cast<u16*>(c.dx) + token * c.dx_stride;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (at + e < c.p.dim) row[at + e] = rows::float_to_bf16(v[e]);
+        }
+    }
 }
 
 template <int G>
@@ -965,29 +1040,7 @@ __global__ __launch_bounds__(kFewBackWaves * 64) void k_few_backward(LinearCall 
                                 acc[g][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[u][s][e], b[u][g][s], acc[g][e], 0, 0, 0);
                 }
         }
-        // Lane l's acc[g][e][r] is token 16 g + l % 16, column d0 + 16 (l / 16) + 4 r + e; wave r sums it.
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-            if (g > 0) __syncthreads();
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sums[wave][e][lane] = acc[g][e];
-            __syncthreads();
-            f4 v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float* at = reinterpret_cast<const float*>(&sums[0][e][lane]) + wave;
-                v[e] = at[0];
-#pragma unroll
-                for (int o = 1; o < kFewBackWaves; ++o) v[e] += at[o * 4 * 64 * 4];
-            }
-            const int token = g * 16 + i, at = d0 + 16 * k + 4 * wave;
-            if (token >= c.p.tokens) continue;
-            if (c.p.dx_splits > 1)
-                store_four(reinterpret_cast<float*>(c.workspace + c.p.dx_parts) + (static_cast<int64_t>(part) * c.p.tokens + token) * c.p.ld_dx,
-                           at, static_cast<int>(c.p.ld_dx) - at, v);
-            else
-                store_four(static_cast<float*>(c.dx) + token * c.dx_stride, at, dim - at, v);
-        }
+        few_dx_end<true, G>(c, acc, part, d0, sums);
         return;
     }
     const int id = blockIdx.x - jobs.dx, down = id / jobs.slabs, d0 = (id - down * jobs.slabs) * 64, col = d0 + 4 * i, have = dim - col;
@@ -1022,6 +1075,103 @@ __global__ __launch_bounds__(kFewBackWaves * 64) void k_few_backward(LinearCall 
         for (int q = 0; q < 4; ++q) {
             const int at = d0 + 16 * k + 4 * q;
             store_four(row, at, dim - at, f4{acc[0][q], acc[1][q], acc[2][q], acc[3][q]});
+        }
+    }
+}
+
+// bf16: dz is dy where it lies, or its copy, in HALVES for dw.
+template <int G, int HALVES>
+__global__ __launch_bounds__(kFewBackWaves * 64) void k_few_backward_bf16(LinearCall c, FewJobs jobs) {
+    __shared__ f4 sums[kFewBackWaves][4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, k = lane >> 4;
+    const int dim = c.p.dim, wide = c.p.wide, tokens = c.p.tokens;
+    const u16* dz = c.dz_direct ? static_cast<const u16*>(c.dy) : reinterpret_cast<const u16*>(c.workspace + c.p.dz);
+    const int64_t ld = c.dz_direct ? c.dy_stride : c.p.ld_wide;
+    int id = blockIdx.x;
+    if (id < jobs.dx) {
+        const int part = id / jobs.slabs, d0 = (id - part * jobs.slabs) * 64, col = d0 + 4 * i, have = dim - col;
+        const u16* w = static_cast<const u16*>(c.w);
+        // Runs of 32 rows of w, every fourth one to a wave.
+        const int runs = (wide + 31) / 32, each = (runs + c.p.dx_splits - 1) / c.p.dx_splits;
+        const int begin = part * each, end = min(begin + each, runs);
+        f4 acc[G][4];
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[g][e] = f4{0.f, 0.f, 0.f, 0.f};
+        constexpr int kAhead = 2;
+        for (int first = begin + wave; first < end; first += kFewBackWaves * kAhead) {
+            Two a[kAhead][8];
+            rows::Raw8<false> b[kAhead][G];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int n0 = (first + u * kFewBackWaves) * 32 + 8 * k;
+                if (first + u * kFewBackWaves < end) {
+                    // (Rows past the last one meet zeros in dz; tokens past the last one are not stored.)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) a[u][j] = four(w + min(n0 + j, wide - 1) * c.w_stride, col, have);
+#pragma unroll
+                    for (int g = 0; g < G; ++g) b[u][g] = rows::raw8<false>(dz, min(g * 16 + i, tokens - 1) * ld + n0, wide - n0);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (first + u * kFewBackWaves < end) {
+                    bfloat8 f[4];
+                    turn(a[u], f);
+#pragma unroll
+                    for (int g = 0; g < G; ++g)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            acc[g][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[e], __builtin_bit_cast(bfloat8, b[u][g].v), acc[g][e], 0, 0, 0);
+                }
+        }
+        few_dx_end<false, G>(c, acc, part, d0, sums);
+        return;
+    }
+    id -= jobs.dx;
+    if (id >= jobs.dw) {  // dbias, where dz is dy
+        dz_block<false, kFewBackWaves * 64>(c, 0, (id - jobs.dw) * kDzCols, reinterpret_cast<V8(*)[16]>(&sums[0][0][0]));
+        return;
+    }
+    const int down = id / jobs.slabs, d0 = (id - down * jobs.slabs) * 64, col = d0 + 4 * i, have = dim - col;
+    const int n = (down * kFewBackWaves + wave) * kFewRows + 4 * i;
+    static_assert(G <= 2, "one step of 32 tokens");
+    bfloat8 a[4], b[HALVES][4];
+    Two r[8], d[HALVES][8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        // (Tokens past the last one: x's last row, and zeros in dz.)
+        const int token = 8 * k + j, row = min(token, tokens - 1);
+        r[j] = four(static_cast<const u16*>(c.x) + row * c.x_stride, col, have);
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) d[h][j] = four(dz + (row + h * c.p.pad_tokens) * ld, n, token < tokens ? wide - n : 0);
+    }
+    turn(r, a);
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h) turn(d[h], b[h]);
+    // Lane l's acc[e][r] is row n + q, column d0 + 16 (l / 16) + 4 r + e.
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        f4 acc[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[e], b[h][q], acc[e], 0, 0, 0);
+        if (n + q >= wide) continue;
+#pragma unroll
+        for (int o = 0; o < 2; ++o) {
+            const int at = d0 + 16 * k + 8 * o;
+            if (at >= dim) continue;
+            V8 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v.v[e] = acc[e][2 * o];
+                v.v[4 + e] = acc[e][2 * o + 1];
+            }
+            store_dw(c, n + q, at, v);
         }
     }
 }
@@ -1111,15 +1261,21 @@ void forward(const LinearCall& c, hipStream_t stream) {
     forward<FORM, 64>(c, stream);
 }
 
+// use(groups of 16 tokens as a type)
+template <class F>
+void with_groups(int tokens, F use) {
+    if (tokens <= 16)
+        use(std::integral_constant<int, 1>());
+    else if (tokens <= 32)
+        use(std::integral_constant<int, 2>());
+    else
+        use(std::integral_constant<int, 4>());
+}
+
 template <bool F32>
 void few(const LinearCall& c, hipStream_t stream) {
     const dim3 n((c.p.wide + 15) / 16, c.p.splits);
-    if (c.p.tokens <= 16)
-        k_few<F32, 1><<<n, kFewWaves * 64, 0, stream>>>(c);
-    else if (c.p.tokens <= 32)
-        k_few<F32, 2><<<n, kFewWaves * 64, 0, stream>>>(c);
-    else
-        k_few<F32, 4><<<n, kFewWaves * 64, 0, stream>>>(c);
+    with_groups(c.p.tokens, [&](auto g) { k_few<F32, decltype(g)::value><<<n, kFewWaves * 64, 0, stream>>>(c); });
     if (c.p.splits > 1) forward_join<F32>(c, stream);
 }
 
@@ -1142,12 +1298,19 @@ void few_backward(const LinearCall& c, hipStream_t stream) {
     jobs.slabs = (c.p.dim + 63) / 64;
     jobs.dx = c.dx ? jobs.slabs * c.p.dx_splits : 0;
     jobs.dw = c.dw ? jobs.slabs * ((c.p.wide + kFewBackWaves * kFewRows - 1) / (kFewBackWaves * kFewRows)) : 0;
-    if (c.p.tokens <= 16)
-        k_few_backward<1><<<jobs.dx + jobs.dw, kFewBackWaves * 64, 0, stream>>>(c, jobs);
-    else if (c.p.tokens <= 32)
-        k_few_backward<2><<<jobs.dx + jobs.dw, kFewBackWaves * 64, 0, stream>>>(c, jobs);
-    else
-        k_few_backward<4><<<jobs.dx + jobs.dw, kFewBackWaves * 64, 0, stream>>>(c, jobs);
+    jobs.bias = c.dz_direct && c.dbias ? (c.p.wide + kDzCols - 1) / kDzCols : 0;
+    const int groups = jobs.dx + jobs.dw + jobs.bias;
+    with_groups(c.p.tokens, [&](auto g) {
+        constexpr int G = decltype(g)::value;
+        if (c.p.f32) {
+            k_few_backward<G><<<groups, kFewBackWaves * 64, 0, stream>>>(c, jobs);
+        } else if constexpr (G <= 2) {
+            if (c.p.dz_halves)
+                k_few_backward_bf16<G, 2><<<groups, kFewBackWaves * 64, 0, stream>>>(c, jobs);
+            else
+                k_few_backward_bf16<G, 1><<<groups, kFewBackWaves * 64, 0, stream>>>(c, jobs);
+        }
+    });
 }
 
 template <LinearForm FORM>
@@ -1173,21 +1336,23 @@ void backward(const LinearCall& c, hipStream_t stream) {
         // (Where dz is dy, dbias's sums run beside the products.)
         if (!c.dz_direct || (c.dbias && !c.dx && !c.dw))
             k_dz<is_f32(FORM)><<<dim3((c.p.ld_wide / units(FORM) + kDzCols - 1) / kDzCols, c.p.pad_tokens / kDzRows), 256, 0, stream>>>(c);
-        if (FORM == kLinearBf16 && from < to)
+        if (!c.p.back_few && from < to)
             k_copies<FORM><<<dim3(groups_for((copies_rows + 3) / 4, 4096), to - from), 256, 0, stream>>>(c, from, c.p.dz_halves);
     }
     if (c.dx || c.dw) {
         const bool with_bias = FORM != kLinearHalves && c.dz_direct && c.dbias;
-        if constexpr (FORM == kLinearSingle)
+        if (c.p.back_few)
             few_backward(c, stream);
-        else if (c.p.back_tile == 64)
-            backward<FORM, 64>(c, with_bias, stream);
-        else if (c.p.back_tile == 128)
-            backward<FORM, 128>(c, with_bias, stream);
-        else
-            backward<FORM, 256>(c, with_bias, stream);
+        else if constexpr (FORM != kLinearSingle) {
+            if (c.p.back_tile == 64)
+                backward<FORM, 64>(c, with_bias, stream);
+            else if (c.p.back_tile == 128)
+                backward<FORM, 128>(c, with_bias, stream);
+            else
+                backward<FORM, 256>(c, with_bias, stream);
+        }
     }
-    const int bias_groups = c.dbias ? (c.p.wide + 15) / 16 : 0;
+    const int bias_groups = c.dbias && c.p.bias_parts > 1 ? (c.p.wide + 15) / 16 : 0;
     const int64_t eights = (c.p.dim + 7) / 8;
     const int64_t join = (c.dx && c.p.dx_splits > 1 ? c.p.tokens * eights : 0) + (c.dw && c.p.dw_splits > 1 ? c.p.wide * eights : 0);
     const unsigned groups = bias_groups + groups_for((join + 255) / 256, 4096);

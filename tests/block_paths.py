@@ -18,10 +18,16 @@ FORWARD = [
     ((8192, 832, 6400), "halves 256 front", "bf16 256 front"),
 ]
 
-# The products of the gradients: the tile, and which of dx and dw are in parts; of fp32 up to 64
-# tokens groups of 16 tokens.  fp32, bf16, and bf16 with dw in fp32.
+# The products of the gradients: the tile, and which of dx and dw are in parts; of few tokens
+# groups of 16.  fp32, bf16, and bf16 with dw in fp32.
 BACKWARD = [
-    ((21, 9, 690), "single 2 dx", "64", "64"),
+    ((1, 4800, 1600), "few 1 dx", "few 1 dx", "few 1 dx"),
+    ((16, 700, 100), "few 1", "few 1", "few 1"),
+    ((21, 9, 690), "few 2 dx", "few 2 dx", "few 2 dx"),
+    ((30, 1917, 513), "few 2 dx", "few 2 dx", "few 2 dx"),
+    ((33, 1601, 255), "few 4", "64", "64"),
+    ((63, 130, 5123), "few 4 dx", "64 dx", "64 dx"),
+    ((64, 1024, 4096), "few 4 dx", "128 dx", "128 dx"),
     ((827, 8, 545), "64 dx dw", "64 dx dw", "64 dw"),
     ((573, 9, 839), "64 dx dw", "64 dx dw", "64 dx dw"),
     ((4115, 71, 836), "128 dx dw", "128 dx dw", "64 dw"),
@@ -55,8 +61,8 @@ def forward_way(size, plan):
 
 
 def backward_way(size, plan):
-    if plan["back_form"] == "single":
-        way = f"single {1 if size[0] <= 16 else 2 if size[0] <= 32 else 4}"
+    if plan["back_few"] == "1":
+        way = f"few {1 if size[0] <= 16 else 2 if size[0] <= 32 else 4}"
     else:
         way = plan["back_tile"]
     return way + " dx" * (plan["dx_splits"] != "1") + " dw" * (plan["dw_splits"] != "1")

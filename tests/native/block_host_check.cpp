@@ -172,26 +172,27 @@ static void check_backward(const dsm_linear_problem& p, const dsm_linear_buffers
     CHECK(q.dz_halves == (!q.f32 && p.dw_dtype == DSM_F32 && p.act != 0));
     CHECK(q.pad_tokens % 64 == 0 && q.pad_tokens >= T);
     CHECK(q.ld_wide >= up(N, 64) * units && q.ld_wide % (64 * units) == 0 && q.ld_dx >= D && q.ld_dx % 8 == 0);
-    const bool single = q.back_form == dsm::kLinearSingle, halves = q.back_form == dsm::kLinearHalves;
-    if (single) CHECK(T <= 64 && q.dw_splits == 1);
-    if (!single) CHECK(q.back_tile == 64 || q.back_tile == 128 || q.back_tile == 256);
+    const bool few = q.back_few, halves = q.back_form == dsm::kLinearHalves;
+    if (few) CHECK(T <= (q.f32 ? 64 : 32) && q.dw_splits == 1 && q.bias_parts == 1);
+    CHECK(few || q.back_form != dsm::kLinearSingle);
+    if (!few) CHECK(q.back_tile == 64 || q.back_tile == 128 || q.back_tile == 256);
     if (halves) CHECK(q.split_rows == 8 || (q.split_rows == 2 && N <= 8192));
     // dbias's parts: of the kernels that make dz.
     CHECK(q.bias_parts == (halves ? (T + q.split_rows - 1) / q.split_rows : q.pad_tokens / dsm::kDzRows));
     // dz's rows past the tokens meet x's last one, and have to be zeros.
-    CHECK(c.dz_direct == (!p.act && q.back_form == dsm::kLinearBf16 && T % 64 == 0 &&
-                          reads_whole(reinterpret_cast<int64_t>(b.dy), b.dy_stride, N, size, 64)));
+    CHECK(c.dz_direct == (!p.act && q.back_form == dsm::kLinearBf16 &&
+                          (few || (T % 64 == 0 && reads_whole(reinterpret_cast<int64_t>(b.dy), b.dy_stride, N, size, 64)))));
     CHECK(c.x_direct == (!halves && !q.dz_halves && reads_whole(reinterpret_cast<int64_t>(b.x), b.x_stride, D, size, 8)));
     CHECK(c.w_direct == (!halves && reads_whole(reinterpret_cast<int64_t>(b.w), b.w_stride, D, size, 8)));
     const int64_t twice = q.dz_halves ? 2 : 1;
-    check_regions({{q.x, c.x_direct || single ? 0 : (q.dz_halves ? 2 * q.pad_tokens : T) * q.ld_dim * 2},
-                   {q.w, c.w_direct || single ? 0 : N * q.ld_dim * 2}, {q.x_exp, halves ? 4 : 0}, {q.w_exp, halves ? 4 : 0},
+    check_regions({{q.x, c.x_direct || few ? 0 : (q.dz_halves ? 2 * q.pad_tokens : T) * q.ld_dim * 2},
+                   {q.w, c.w_direct || few ? 0 : N * q.ld_dim * 2}, {q.x_exp, halves ? 4 : 0}, {q.w_exp, halves ? 4 : 0},
                    {q.dz, c.dz_direct ? 0 : q.pad_tokens * q.ld_wide * 2 * twice}, {q.z_exp, halves ? T * 4 : 0},
                    {q.w_tops, halves ? dsm::kLinearTopParts * 4 : 0}, {q.tops, halves ? q.pad_tokens / q.split_rows * 4 : 0},
                    {q.dx_parts, q.dx_splits > 1 ? q.dx_splits * T * q.ld_dx * 4 : 0},
                    {q.dw_parts, q.dw_splits > 1 ? q.dw_splits * N * q.ld_dx * 4 : 0}, {q.bias_sums, q.bias_parts * N * 4}},
                   q.backward_bytes);
-    if (single) return;
+    if (few) return;
     const int64_t of = q.back_tile, across = (D + of - 1) / of;
     CHECK(((T + of - 1) / of * q.dx_splits + (N + of - 1) / of * q.dw_splits) * across + (N + 127) / 128 * (q.pad_tokens / 64) <
           (int64_t(1) << 24));

@@ -50,9 +50,9 @@ int main(int argc, char** argv) {
         if (dsm_linear_workspace(&p, &b.workspace_bytes) != DSM_OK || dsm_linear(&p, &b) != DSM_OK) return 1;
         static const char* const forms[] = {"bf16", "halves", "single"};
         std::printf("form %s back_form %s few %d tile %d splits %d front %d back_tile %d dx_splits %d dw_splits %d "
-                    "split_rows %d dz_halves %d\n",
+                    "split_rows %d dz_halves %d back_few %d\n",
                     forms[seen.form], forms[seen.back_form], seen.few, seen.tile, seen.splits, seen.front, seen.back_tile,
-                    seen.dx_splits, seen.dw_splits, seen.split_rows, seen.dz_halves);
+                    seen.dx_splits, seen.dw_splits, seen.split_rows, seen.dz_halves, seen.back_few);
     }
     return 0;
 }

@@ -27,6 +27,6 @@ def test_backward(size, kind):
 # Without an activation dz is dy, read where it lies where its rows are whole; dbias's sums run
 # beside the products.
 @TYPES
-@pytest.mark.parametrize("size", [(64, 128, 192), (192, 1000, 128), (1536, 1601, 704), (3200, 1504, 1216)], ids=str)
+@pytest.mark.parametrize("size", [(1, 70, 900), (5, 1917, 515), (20, 1600, 2304), (47, 65, 1030), (64, 128, 192), (192, 1000, 128), (1536, 1601, 704), (3200, 1504, 1216)], ids=str)
 def test_backward_without_an_activation(size, dtype):
     _backward(_inputs(*size, dtype, seed=sum(size)), "none")
