@@ -1044,37 +1044,32 @@ __global__ __launch_bounds__(kFewBackWaves * 64) void k_few_backward(LinearCall 
         return;
     }
     const int id = blockIdx.x - jobs.dx, down = id / jobs.slabs, d0 = (id - down * jobs.slabs) * 64, col = d0 + 4 * i, have = dim - col;
-    const int first = (down * kFewBackWaves + wave) * kFewRows;
+    const int n = (down * kFewBackWaves + wave) * kFewRows + 4 * i;
+    if (n >= c.p.ld_wide / 2) return;
     const float* x = static_cast<const float*>(c.x);
-    f4 a[4 * G];
-#pragma unroll
-    for (int s = 0; s < 4 * G; ++s) a[s] = four(x + min(4 * s + k, c.p.tokens - 1) * c.x_stride, col, have);
+    f4 a[4 * G], b[4 * G];
     // (dz has zeros for the tokens that x does not have, and 64 columns a run.)
-    const int last = min(first + kFewRows, wide);
-    float next[4 * G];
-    const auto load = [&](int n0) {
 #pragma unroll
-        for (int s = 0; s < 4 * G; ++s) next[s] = dz[(4 * s + k) * ld + min(n0, static_cast<int>(ld) - 16) + i];
-    };
-    load(first);
-    for (int n0 = first; n0 < last; n0 += 16) {
-        float b[4 * G];
+    for (int s = 0; s < 4 * G; ++s) {
+        a[s] = four(x + min(4 * s + k, c.p.tokens - 1) * c.x_stride, col, have);
+        b[s] = *reinterpret_cast<const f4*>(dz + (4 * s + k) * ld + n);
+    }
+    // Lane l's acc[e][r] is row n + q, column d0 + 16 (l / 16) + 4 r + e.
 #pragma unroll
-        for (int s = 0; s < 4 * G; ++s) b[s] = next[s];
-        load(n0 + 16);
+    for (int q = 0; q < 4; ++q) {
         f4 acc[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < 4 * G; ++s)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[s][e], b[s], acc[e], 0, 0, 0);
-        if (n0 + i >= wide) continue;
-        float* row = static_cast<float*>(c.dw) + (n0 + i) * c.dw_stride;
+            for (int e = 0; e < 4; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[s][e], b[s][q], acc[e], 0, 0, 0);
+        if (n + q >= wide) continue;
+        float* row = static_cast<float*>(c.dw) + (n + q) * c.dw_stride;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int at = d0 + 16 * k + 4 * q;
-            store_four(row, at, dim - at, f4{acc[0][q], acc[1][q], acc[2][q], acc[3][q]});
+        for (int r = 0; r < 4; ++r) {
+            const int at = d0 + 16 * k + 4 * r;
+            store_four(row, at, dim - at, f4{acc[0][r], acc[1][r], acc[2][r], acc[3][r]});
         }
     }
 }
