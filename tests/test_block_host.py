@@ -55,7 +55,9 @@ def test_runtime_under_sanitizers(tmp_path):
     ("q.dw_splits * N * q.ld_dx * 4", "q.dw_splits * N * D * 4"),
     ("q.tops = take(q.pad_tokens / q.split_rows * 4);", "q.tops = take(q.pad_tokens / 8 * 4);"),
     ("T >= 1536 || N > 8192 ? 8 : 2", "T >= 1536 ? 8 : 2"),
-    ("p.tokens % 64 == 0;", "true;"),
+    ("p.tokens % 64 == 0));", "true));"),
+    ("(c.p.back_few || (direct", "((direct"),
+    ("q.back_few = T <= (q.f32 ? kSingleBackward : kFewBackward);", "q.back_few = T <= kSingleBackward;"),
     ("!c.p.dz_halves && direct", "direct"),
     ("stride * size < kMaxStride * 2 && ", ""),
     ("if (form == dsm::kLinearHalves) return false;", ""),
