@@ -33,6 +33,8 @@ def _dtype(dtype):
 
 
 class _Plan:
+    _index = -1  # of the device, as Tensor.get_device gives it
+
     def __init__(self):
         self._lock = threading.Lock()
 
@@ -51,14 +53,15 @@ class _Plan:
 
     def _enter(self):
         """The current stream, after what this plan last did on another one."""
-        if _raw_stream is not None and _raw_stream(self._index) == self._handle:
+        if _raw_stream is not None and self._index >= 0 and _raw_stream(self._index) == self._handle:
             return self._handle
         stream = torch.cuda.current_stream(self.device)
         if stream != self._stream:
             if not torch.cuda.is_current_stream_capturing():
                 stream.wait_stream(self._stream)
                 self.workspace.record_stream(stream)
-            self._stream, self._handle = stream, stream.cuda_stream
+            self._stream = stream
+        self._handle = stream.cuda_stream
         return self._handle
 
     def _on_device(self):

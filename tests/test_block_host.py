@@ -35,13 +35,13 @@ def _build(folder, check, runtime, *flags):
     return exe
 
 
-def _check(folder, runtime):
-    exe = _build(folder, "block_host_check", runtime, *SANITIZED)
+def _check(folder, runtime, *flags):
+    exe = _build(folder, "block_host_check", runtime, *flags)
     return subprocess.run([exe], capture_output=True, text=True, timeout=600)
 
 
 def test_runtime_under_sanitizers(tmp_path):
-    r = _check(tmp_path, RUNTIME)
+    r = _check(tmp_path, RUNTIME, *SANITIZED)
     assert r.returncode == 0, (r.stdout + r.stderr)[-4000:]
     assert "all checks passed" in r.stdout
 
