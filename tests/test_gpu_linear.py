@@ -216,6 +216,27 @@ def test_zeros(tokens, dtype):
 
 
 @TYPES
+@pytest.mark.parametrize("tokens", [5, 40, 100, 200])
+def test_operands_below_the_normal_numbers(tokens, dtype):
+    """Operands of 2^-130 and large ones make ordinary products: none of them is taken as 0."""
+    i = _inputs(tokens, 70, 90, dtype, seed=11)
+    i["x"] = (i["x"].double() * 2.0 ** -130).to(dtype)
+    i["w"] = (i["w"].double() * 2.0 ** 60).to(dtype)
+    plan = _ops().Linear(tokens, 70, 90, dtype=dtype)
+    y = plan(i["x"], i["w"])["y"]
+    e = O.linear(i["x"], i["w"], None, None)
+    O.check_norm(y, e["y"], O.norm_bound(70, dtype), "y")
+    i["dy"] = (i["dy"].double() * 2.0 ** 80).to(dtype)
+    dw = plan.backward(i["dy"], i["x"], i["w"], wanted=("dw",))["dw"]
+    e = O.linear_backward(i["dy"], i["x"], i["w"])
+    O.check_norm(dw, e["dw"], O.norm_bound(tokens, dtype), "dw")
+    i["dy"] = (i["dy"].double() * 2.0 ** -210).to(dtype)
+    dx = plan.backward(i["dy"], i["x"], i["w"], wanted=("dx",))["dx"]
+    e = O.linear_backward(i["dy"], i["x"], i["w"])
+    O.check_norm(dx, e["dx"], O.norm_bound(90, dtype), "dx")
+
+
+@TYPES
 @pytest.mark.parametrize("tokens", [20, 150])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 def test_non_finite_values_reach_what_depends_on_them_alone(tokens, bad, dtype):
