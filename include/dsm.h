@@ -644,7 +644,8 @@ DSM_API dsm_status dsm_norm_workspace(const dsm_norm_problem* problem, int64_t* 
 /*
  * dsm_residual_norm - p = post(f);  s = h + scale gate p;  y = norm(s)
  * and without f, y = norm(h).  y takes s before its rounding.  Everything is fp32,
- * rounded once.  s may be h or f, and y any of them, in place (the same pointer and
+ * rounded once (squares too: a row whose squares pass fp32's range has no finite size).
+ * s may be h or f, and y any of them, in place (the same pointer and
  * stride); otherwise outputs may not overlap inputs.
  * Errors: DSM_ERR_INVALID_ARG; DSM_ERR_HIP.
  */

@@ -527,6 +527,7 @@ class _Clip(_Plan):
             e.numel, e.block, e.stride, e.dtype, e.group = numel, max(numel, 1), max(numel, 1), _dtype(dtype), group
         # The same memory as columns, to fill at once.
         self._columns = np.frombuffer(self._entries, dtype=np.int64).reshape(len(sizes), -1).T if sizes else None
+        self._placed = None
         self.n_groups, self.eps = int(n_groups), float(eps)
         self._allocate(dsm.dsm_clip_workspace(self._entries, self.n_groups), device)
 
@@ -536,13 +537,16 @@ class _Clip(_Plan):
         self._vector("norm", norm, torch.float32, torch.Size((self.n_groups,)))
         return norm
 
-    def _run(self, max_norm, norm, data, **columns):
-        """data: addresses; columns: first, block and stride where they differ from what stands there."""
+    def _run(self, max_norm, norm, data, columns):
+        """data: addresses; columns: first, block and stride where they differ from what stands there (a
+        dictionary that the last call gave stands there)."""
         def call(stream):
             if self._columns is not None:
                 self._columns[0] = data
-                for name, values in columns.items():
-                    self._columns[_COLUMNS[name]] = values
+                if columns is not self._placed:
+                    self._placed = columns
+                    for name, values in columns.items():
+                        self._columns[_COLUMNS[name]] = values
             dsm.dsm_grad_clip(self._entries, self.n_groups, float("inf") if max_norm is None else float(max_norm),
                               norm.data_ptr(), self.workspace.data_ptr(), self.workspace_bytes, self.eps, stream)
 
@@ -575,7 +579,8 @@ class GradClip(_Clip):
         # Groups in order: the order of a call's tensors is the caller's.
         self._order = sorted(range(len(tensors)), key=groups.__getitem__)
         sizes = [(self._like[i][0].numel(), self._like[i][1]) for i in self._order]
-        self._whole = np.array([max(n, 1) for n, _ in sizes], dtype=np.int64)
+        whole = np.array([max(n, 1) for n, _ in sizes], dtype=np.int64)
+        self._whole = {"block": whole, "stride": whole}
         self._table(sizes, [groups[i] for i in self._order], max(groups, default=0) + 1, eps, device)
 
     def _place(self, i, t):
@@ -599,7 +604,7 @@ class GradClip(_Clip):
         # Hundreds of tensors: no Python code for each where all is well.
         if (list(map(_SHAPE_DTYPE, tensors)) == self._like and all(map(torch.Tensor.is_contiguous, tensors)) and
                 set(map(torch.Tensor.get_device, tensors)) <= {self._index}):
-            place = {"block": self._whole, "stride": self._whole}
+            place = self._whole
         else:
             places = [self._place(i, tensors[i]) for i in self._order]
             place = {"block": [p[0] for p in places], "stride": [p[1] for p in places]}
@@ -608,7 +613,7 @@ class GradClip(_Clip):
             given = [a for a, i in zip(data, self._order) if tensors[i].numel()]
             if len(set(given)) < len(given):
                 raise ValueError("a tensor is given twice")
-        return self._run(max_norm, self._norm(norm), data, **place)
+        return self._run(max_norm, self._norm(norm), data, place)
 
 
 class ArenaClip(_Clip):
@@ -639,4 +644,4 @@ class ArenaClip(_Clip):
             stride = buffers * self._n * block
         data = arenas.g_rep.data_ptr() + 4 * apart * np.arange(self._n, dtype=np.int64).repeat(len(self._numel))
         first = np.tile(np.array(self._offsets, dtype=np.int64), self._n)
-        return self._run(max_norm, self._norm(norm), data, first=first, block=block, stride=stride)
+        return self._run(max_norm, self._norm(norm), data, {"first": first, "block": block, "stride": stride})
