@@ -127,9 +127,10 @@ void cut_backward(dsm::LinearPlan* q) {
     const double f32 = q->f32 ? kBackward.f32 : 1.0;
     double best = 0.0;
     if (q->back_few) {
-        // dx by slabs of 64 columns, of 256 work-groups or more; parts of 256 rows of w at least.
-        const int64_t slabs = tiles(D, 64);
-        q->dx_splits = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>({kMaxSplits, tiles(512, slabs), N / 256})));
+        // dx by slabs of 64 columns, some 512 work-groups; parts of 256 rows of w at least.  (Past 32 tokens the CUs hold
+        // no more at once: 64 of 6400 -> 6400 in fp32 dx 86 us by 500, 126 by 600; of 8 tokens 47 and 46.)
+        const int64_t slabs = tiles(D, 64), parts = T > 32 ? 512 / slabs : tiles(512, slabs);
+        q->dx_splits = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>({kMaxSplits, parts, N / 256})));
         return;
     }
     for (int i = 0; i < 3; ++i) {

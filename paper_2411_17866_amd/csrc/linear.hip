@@ -1043,7 +1043,10 @@ __global__ __launch_bounds__(kFewBackWaves * 64) void k_few_backward(LinearCall 
         few_dx_end<true, G>(c, acc, part, d0, sums);
         return;
     }
-    const int id = blockIdx.x - jobs.dx, down = id / jobs.slabs, d0 = (id - down * jobs.slabs) * 64, col = d0 + 4 * i, have = dim - col;
+    // (Columns go to lanes so that a store's four lanes of a row have 64 bytes of it side by side: 13 tokens
+    // of 6400 -> 4800 28 us for dw, dz's launch included; 46 by pieces of 16 bytes.)
+    const int id = blockIdx.x - jobs.dx, down = id / jobs.slabs, d0 = (id - down * jobs.slabs) * 64;
+    const int col = d0 + 4 * (4 * (i & 3) + (i >> 2)), have = dim - col;
     const int n = (down * kFewBackWaves + wave) * kFewRows + 4 * i;
     if (n >= c.p.ld_wide / 2) return;
     const float* x = static_cast<const float*>(c.x);
@@ -1054,7 +1057,7 @@ __global__ __launch_bounds__(kFewBackWaves * 64) void k_few_backward(LinearCall 
         a[s] = four(x + min(4 * s + k, c.p.tokens - 1) * c.x_stride, col, have);
         b[s] = *reinterpret_cast<const f4*>(dz + (4 * s + k) * ld + n);
     }
-    // Lane l's acc[e][r] is row n + q, column d0 + 16 (l / 16) + 4 r + e.
+    // Lane l's acc[e][r] is row n + q, column d0 + 16 r + 4 (l / 16) + e.
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         f4 acc[4];
@@ -1068,7 +1071,7 @@ __global__ __launch_bounds__(kFewBackWaves * 64) void k_few_backward(LinearCall 
         float* row = static_cast<float*>(c.dw) + (n + q) * c.dw_stride;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int at = d0 + 16 * k + 4 * r;
+            const int at = d0 + 16 * r + 4 * k;
             store_four(row, at, dim - at, f4{acc[0][r], acc[1][r], acc[2][r], acc[3][r]});
         }
     }
@@ -1129,7 +1132,9 @@ __global__ __launch_bounds__(kFewBackWaves * 64) void k_few_backward_bf16(Linear
         dz_block<false, kFewBackWaves * 64>(c, 0, (id - jobs.dw) * kDzCols, reinterpret_cast<V8(*)[16]>(&sums[0][0][0]));
         return;
     }
-    const int down = id / jobs.slabs, d0 = (id - down * jobs.slabs) * 64, col = d0 + 4 * i, have = dim - col;
+    // (As above, of two columns' fours a store.)
+    const int down = id / jobs.slabs, d0 = (id - down * jobs.slabs) * 64;
+    const int col = d0 + 4 * (8 * ((i >> 1) & 1) + 2 * (i >> 2) + (i & 1)), have = dim - col;
     const int n = (down * kFewBackWaves + wave) * kFewRows + 4 * i;
     static_assert(G <= 2, "one step of 32 tokens");
     bfloat8 a[4], b[HALVES][4];
@@ -1145,7 +1150,7 @@ __global__ __launch_bounds__(kFewBackWaves * 64) void k_few_backward_bf16(Linear
     turn(r, a);
 #pragma unroll
     for (int h = 0; h < HALVES; ++h) turn(d[h], b[h]);
-    // Lane l's acc[e][r] is row n + q, column d0 + 16 (l / 16) + 4 r + e.
+    // Lane l's acc[e][r] is row n + q, column d0 + 32 (r / 2) + 8 (l / 16) + 4 (r % 2) + e.
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         f4 acc[4];
@@ -1158,7 +1163,7 @@ __global__ __launch_bounds__(kFewBackWaves * 64) void k_few_backward_bf16(Linear
         if (n + q >= wide) continue;
 #pragma unroll
         for (int o = 0; o < 2; ++o) {
-            const int at = d0 + 16 * k + 8 * o;
+            const int at = d0 + 32 * o + 8 * k;
             if (at >= dim) continue;
             V8 v;
 #pragma unroll
