@@ -103,13 +103,15 @@ void cut_forward(dsm::LinearPlan* q) {
 
 // Few tokens: parts of k, where few rows of w leave CUs idle.  A work-group reads its rows of
 // w and x at some 75 GB/s, and joining the parts takes a launch.  One token of 6400 -> 256 in fp32: 15.2 us
-// in one part, 8.7 in 4; 24 tokens of 6400 -> 1600 in bf16: 9.6, and 9.4 in 2.
+// in one part, 8.7 in 4; 24 tokens of 6400 -> 1600 in bf16: 9.6, and 9.4 in 2.  In fp32 up to 32 tokens two
+// work-groups a CU still gain: 1 token of 6400 -> 1600 17.1 us in 2 parts, 13.3 in 5; 55 tokens of 4096 -> 4096 28.1 and 37.1.
 int few_splits(const dsm::LinearPlan& q) {
     const int64_t groups = tiles(q.wide, 16), size = q.f32 ? 4 : 2, rows = 16 + round_up(q.tokens, 16);
+    const int64_t most = q.f32 && q.tokens <= 32 ? 512 : 256;
     const double whole = static_cast<double>(q.dim * size * rows) / 75e3;
     int best = 1;
     double least = whole - 1.5;
-    for (int s = 2; s <= kMaxSplits && groups * s <= 256 && s * 1024 <= q.dim * size; ++s) {
+    for (int s = 2; s <= kMaxSplits && groups * s <= most && s * 1024 <= q.dim * size; ++s) {
         const double cost = whole / s + 3.4 + 0.5 * s;
         if (cost < least) {
             least = cost;

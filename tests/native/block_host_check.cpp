@@ -141,7 +141,7 @@ static void check_forward(const dsm_linear_problem& p, const dsm_linear_buffers&
     CHECK((q.form == dsm::kLinearBf16) == !q.f32);
     CHECK(q.ld_y >= N && q.ld_y % 8 == 0);
     if (q.few) {
-        CHECK(T <= 64 && (q.splits == 1 || (N + 15) / 16 * q.splits <= 256));
+        CHECK(T <= 64 && (q.splits == 1 || (N + 15) / 16 * q.splits <= (q.f32 && T <= 32 ? 512 : 256)));
         check_regions({{q.y_parts, q.splits > 1 ? q.splits * T * q.ld_y * 4 : 0}}, q.forward_bytes);
         return;
     }
