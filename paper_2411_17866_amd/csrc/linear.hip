@@ -653,6 +653,19 @@ __device__ __forceinline__ V8 eight_of(const tile::Eight& x) {
     return v;
 }
 
+// Four columns from `col` on, of which `have` exist.  (fp32 results go to memory as they lie in a
+// tile's fragments, four columns a lane and 64 bytes of a row side by side; eight columns a lane would be
+// pieces of 16 bytes: 2045 x 1024 x 4096 in fp32, both gradients 126.8 us instead of 124.1.)
+__device__ __forceinline__ void store_four(float* row, int col, int have, f4 v) {
+    if (have >= 4) {
+        *reinterpret_cast<rows::f4_at*>(row + col) = v;
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+        if (e < have) row[col + e] = v[e];
+}
+
 // y, or a part of its sums: the tile of rows from row0 on, columns from col0 on.
 template <LinearForm FORM, class T, bool PARTS>
 __device__ __forceinline__ void forward_tile(const LinearCall& c, int row0, int col0, int part, DSM_LDS char* lds) {
@@ -760,6 +773,40 @@ __device__ __forceinline__ void store_dw(const LinearCall& c, int64_t row, int c
         rows::store8<false>(c.dw, row * c.dw_stride + col, v, have);
 }
 
+// A tile's rows from row0 on, columns from col0 on, of `rows` x `cols`: in fp32, times 2^exponent(row), or in bf16.
+template <LinearForm FORM, class T, class E>
+__device__ __forceinline__ void store_tile(T& t, int row0, int col0, int rows, int cols, float* to, int64_t stride, E exponent) {
+#pragma unroll
+    for (int f = 0; f < T::FI; ++f) {
+        const int row = row0 + t.row(f);
+        if (row >= rows) continue;
+        const int e = exponent(row);
+#pragma unroll
+        for (int q = 0; q < T::FJ; ++q) {
+            const int col = col0 + t.col(q);
+            f4 v = t.acc[f][q];
+            if constexpr (FORM == kLinearHalves) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] = ldexpf(v[k], e);
+            }
+            store_four(to + row * stride, col, cols - col, v);
+        }
+    }
+}
+template <class T>
+__device__ __forceinline__ void store_tile(T& t, int row0, int col0, int high, int cols, u16* to, int64_t stride) {
+#pragma unroll
+    for (int f = 0; f < T::FI; ++f) {
+        const int row = row0 + t.row(f);
+#pragma unroll
+        for (int q = 0; q < T::FJ / 2; ++q) {
+            const int col = col0 + t.col8(q);
+            const V8 v = eight_of(t.eight(f, q));
+            if (row < high && col < cols) rows::store8<false>(to, row * stride + col, v, min(cols - col, 8));
+        }
+    }
+}
+
 // dx: the tile of tokens from row0 on, columns from col0 on; a part of its sums, or all.
 template <LinearForm FORM, class T>
 __device__ __forceinline__ void dx_tile(const LinearCall& c, int row0, int col0, int part, int parts, DSM_LDS char* lds) {
@@ -770,27 +817,14 @@ __device__ __forceinline__ void dx_tile(const LinearCall& c, int row0, int col0,
     t.add(dz_rows<FORM>(c), w_rows<FORM>(c), row0, col0, k0, k1, lds, c.p.tokens - row0, c.p.dim - col0);
     const int32_t* z_exp = reinterpret_cast<const int32_t*>(c.workspace + c.p.z_exp);
     const int we = FORM == kLinearHalves ? *reinterpret_cast<const int32_t*>(c.workspace + c.p.w_exp) : 0;
-#pragma unroll
-    for (int f = 0; f < T::FI; ++f) {
-        const int row = row0 + t.row(f);
-        if (row >= c.p.tokens) continue;
-        const int e = FORM == kLinearHalves ? -(z_exp[row] + we) : 0;
-#pragma unroll
-        for (int q = 0; q < T::FJ / 2; ++q) {
-            const int col = col0 + t.col8(q);
-            V8 v = eight_of(t.eight(f, q));
-            if (col >= c.p.dim) continue;
-            if constexpr (FORM == kLinearHalves) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v.v[k] = ldexpf(v.v[k], e);
-            }
-            if (parts > 1)
-                rows::store8<true>(c.workspace + c.p.dx_parts,
-                                   (static_cast<int64_t>(part) * c.p.tokens + row) * c.p.ld_dx + col, v, 8);
-            else
-                store_dx(c, row, col, v);
-        }
-    }
+    const auto exponent = [&](int row) { return FORM == kLinearHalves ? -(z_exp[row] + we) : 0; };
+    float* to = reinterpret_cast<float*>(c.workspace + c.p.dx_parts) + static_cast<int64_t>(part) * c.p.tokens * c.p.ld_dx;
+    if (is_f32(FORM) && parts == 1) to = static_cast<float*>(c.dx);
+    if (is_f32(FORM) || parts > 1)
+        store_tile<FORM>(t, row0, col0, c.p.tokens, parts > 1 ? static_cast<int>(c.p.ld_dx) : c.p.dim, to,
+                         parts > 1 ? c.p.ld_dx : c.dx_stride, exponent);
+    else
+        store_tile(t, row0, col0, c.p.tokens, c.p.dim, static_cast<u16*>(c.dx), c.dx_stride);
 }
 
 // dw: rows of w from row0 on, columns from col0 on.
@@ -804,26 +838,14 @@ __device__ __forceinline__ void dw_tile(const LinearCall& c, int row0, int col0,
     t.clear();
     t.add(dz_rows<FORM>(c), x_rows<FORM, true>(c), row0, col0, k0, k1, lds, c.p.wide - row0, c.p.dim - col0);
     const int e = FORM == kLinearHalves ? -*reinterpret_cast<const int32_t*>(c.workspace + c.p.x_exp) : 0;
-#pragma unroll
-    for (int f = 0; f < T::FI; ++f) {
-        const int row = row0 + t.row(f);
-        if (row >= c.p.wide) continue;
-#pragma unroll
-        for (int q = 0; q < T::FJ / 2; ++q) {
-            const int col = col0 + t.col8(q);
-            V8 v = eight_of(t.eight(f, q));
-            if (col >= c.p.dim) continue;
-            if constexpr (FORM == kLinearHalves) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v.v[k] = ldexpf(v.v[k], e);
-            }
-            if (parts > 1)
-                rows::store8<true>(c.workspace + c.p.dw_parts,
-                                   (static_cast<int64_t>(part) * c.p.wide + row) * c.p.ld_dx + col, v, 8);
-            else
-                store_dw(c, row, col, v);
-        }
-    }
+    const auto exponent = [&](int) { return e; };
+    float* to = reinterpret_cast<float*>(c.workspace + c.p.dw_parts) + static_cast<int64_t>(part) * c.p.wide * c.p.ld_dx;
+    if (parts == 1) to = static_cast<float*>(c.dw);
+    if (is_f32(FORM) || parts > 1 || c.p.dw_f32)
+        store_tile<FORM>(t, row0, col0, c.p.wide, parts > 1 ? static_cast<int>(c.p.ld_dx) : c.p.dim, to,
+                         parts > 1 ? c.p.ld_dx : c.dw_stride, exponent);
+    else
+        store_tile(t, row0, col0, c.p.wide, c.p.dim, static_cast<u16*>(c.dw), c.dw_stride);
 }
 
 // Tile `id` of one of the products, by BM.
@@ -894,8 +916,8 @@ __global__ __launch_bounds__(tile::threads_of(BM)) void k_backward(LinearCall c,
 //   dx  4 x 16 columns of d and a part of n to a wave: w is read once, dz from the caches.
 //   dw  4 x 16 columns of d by kFewRows rows of n to a wave, whose x stays in registers:
 //       every row is written in pieces of 128 or 256 bytes.
-// 13 tokens of 6400 -> 4800, both products: in fp32 63 us, 3.9 TB/s (by tiles of fp32 102); in
-// bf16 28.6, dz's and dx's launches included, 4.3 TB/s.
+// 13 tokens of 6400 -> 4800, both products, with dz's and the join's launches: in fp32 56 us, 4.4 TB/s;
+// in bf16 28.6, 4.3 TB/s.
 
 constexpr int kFewBackWaves = 4, kFewRows = 64;
 
@@ -916,16 +938,6 @@ __device__ __forceinline__ f4 four(const float* row, int col, int have) {
     }
     return v;
 }
-__device__ __forceinline__ void store_four(float* row, int col, int have, f4 v) {
-    if (have >= 4) {
-        *reinterpret_cast<rows::f4_at*>(row + col) = v;
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 3; ++e)
-        if (e < have) row[col + e] = v[e];
-}
-
 typedef u16 u16x4 __attribute__((ext_vector_type(4)));
 typedef u16x4 u16x4_at __attribute__((aligned(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
