@@ -385,11 +385,11 @@ def dsm_linear_workspace(problem):
 
 
 def dsm_linear(problem, buffers):
-    _check(load_library().dsm_linear(ctypes.byref(problem), ctypes.byref(buffers)))
+    _check(load_library().dsm_linear(problem, buffers))  # (by reference, as argtypes say)
 
 
 def dsm_linear_backward(problem, buffers):
-    _check(load_library().dsm_linear_backward(ctypes.byref(problem), ctypes.byref(buffers)))
+    _check(load_library().dsm_linear_backward(problem, buffers))
 
 
 def dsm_norm_workspace(problem):
@@ -398,11 +398,11 @@ def dsm_norm_workspace(problem):
 
 
 def dsm_residual_norm(problem, buffers):
-    _check(load_library().dsm_residual_norm(ctypes.byref(problem), ctypes.byref(buffers)))
+    _check(load_library().dsm_residual_norm(problem, buffers))
 
 
 def dsm_residual_norm_backward(problem, buffers):
-    _check(load_library().dsm_residual_norm_backward(ctypes.byref(problem), ctypes.byref(buffers)))
+    _check(load_library().dsm_residual_norm_backward(problem, buffers))
 
 
 def dsm_clip_workspace(tensors, n_groups):

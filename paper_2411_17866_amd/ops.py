@@ -22,8 +22,10 @@ from . import dsm
 DTYPES = {torch.float32: dsm.DSM_F32, torch.bfloat16: dsm.DSM_BF16}
 
 
-# The current stream's handle without a Stream object around it (a microsecond of a call).
+# The current stream's handle without a Stream object around it (a microsecond of a call), and the
+# current device without looking whether the GPU has been initialised: the plan has done that.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _dtype(dtype):
@@ -72,7 +74,7 @@ class _Plan:
     def _launch(self, call):
         """call(stream): one call's launches, which no other call's come between."""
         with self._lock:
-            if torch.cuda.current_device() == self._index:
+            if _device() == self._index:
                 call(self._enter())
             else:
                 with torch.cuda.device(self.device):
@@ -81,7 +83,7 @@ class _Plan:
     def _launch_with(self, entry, problem, buf):
         """entry(problem, buf) on the current stream, as _launch."""
         with self._lock:
-            if torch.cuda.current_device() == self._index:
+            if _device() == self._index:
                 buf.stream = self._enter()
                 entry(problem, buf)
             else:
