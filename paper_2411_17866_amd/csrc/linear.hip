@@ -669,7 +669,8 @@ __device__ __forceinline__ void store_four(float* row, int col, int have, f4 v) 
 // y, or a part of its sums: the tile of rows from row0 on, columns from col0 on.
 template <LinearForm FORM, class T, bool PARTS>
 __device__ __forceinline__ void forward_tile(const LinearCall& c, int row0, int col0, int part, DSM_LDS char* lds) {
-    int k0 = 0, k1 = static_cast<int>(c.p.ld_dim / units(FORM));
+    // (Rows that are read where they lie end with a whole stage, copies have zeros up to one at least.)
+    int k0 = 0, k1 = (c.p.dim + T::kSteps - 1) / T::kSteps * T::kSteps;
     if (PARTS) part_of(k1, c.p.splits, part, &k0, &k1);
     T t;
     t.clear();

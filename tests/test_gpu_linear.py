@@ -139,6 +139,21 @@ def test_strided_and_misaligned_views(tokens, dtype):
 
 
 @TYPES
+@pytest.mark.parametrize("tokens,dim,wide", [(66, 32, 40), (100, 96, 130), (114, 352, 17), (128, 160, 64), (100, 2528, 200), (40, 96, 64), (200, 96, 64)])
+def test_rows_that_end_with_half_a_step(tokens, dim, wide, dtype):
+    """Rows of 32 columns past the steps of 64, with nothing but NaN behind them."""
+    i = _inputs(tokens, dim, wide, dtype, seed=6)
+    big = {k: torch.full((i[k].shape[0], dim + 32), float("nan"), device="cuda", dtype=dtype) for k in "xw"}
+    for k, t in big.items():
+        t[:, :dim] = i[k]
+        i[k] = t[:, :dim]
+    _forward(i, "relu")
+    _backward(i, "relu")
+    _forward(dict(i, w=i["w"].contiguous()), bias=False)
+    _forward(dict(i, x=i["x"].contiguous()), residual=False)
+
+
+@TYPES
 @pytest.mark.parametrize("tokens", [4, 200])
 def test_onto_the_residual_in_place(tokens, dtype):
     i = _inputs(tokens, 96, 136, dtype, seed=6)
