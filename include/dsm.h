@@ -557,8 +557,9 @@ typedef struct dsm_linear_buffers {
     void* stream;
 } dsm_linear_buffers;
 
-/* dsm_linear_workspace - host only: the workspace of a problem in bytes (for up to 64
- * tokens without gradients 0, or the parts of its sums).  Errors: DSM_ERR_INVALID_ARG. */
+/* dsm_linear_workspace - host only: the workspace of a problem in bytes.  For up to 64
+ * tokens without gradients it is 0, or the parts of sums; for more it has room for copies of
+ * x and w, whose rows may lie so that they cannot be read in place.  Errors: DSM_ERR_INVALID_ARG. */
 DSM_API dsm_status dsm_linear_workspace(const dsm_linear_problem* problem, int64_t* workspace_bytes);
 
 /*

@@ -93,7 +93,7 @@ struct LinearPlan {
     int64_t ld_dim, ld_wide;     // 16-bit elements of a row of x's and w's copies, of dz
     int64_t pad_tokens;          // rows of dz
     int64_t ld_y, ld_dx;         // floats of a row of the parts of y; of dx and dw
-    int64_t x, w, dz;            // operands, where they are not read in place
+    int64_t x, w, dz;            // operands, where they are not read in place (of few tokens x and w always are)
     int64_t x_exp, w_exp, z_exp; // halves: powers of two of the rows of x, w and dz
     int64_t w_tops, tops;        // halves, backward: largest magnitudes of w by work-group; least exponents of x dz
     int64_t y_parts, dx_parts, dw_parts, bias_sums;

@@ -199,26 +199,38 @@ dsm::LinearPlan make_linear_plan(const dsm_linear_problem* p) {
         at = round_up(at + bytes, 256);
         return here;
     };
-    q.x = take((p->grads && q.dz_halves ? 2 * q.pad_tokens : T) * q.ld_dim * 2);
-    q.w = take(N * q.ld_dim * 2);
-    q.x_exp = take(T * 4);
-    q.w_exp = take(N * 4);
-    const int64_t common = at;
-    if (q.few)
+    // Few tokens are read where they lie; of more, x and w may lie so that the tiles cannot.
+    if (!q.few || (p->grads && !q.back_few)) {
+        q.x = take((p->grads && q.dz_halves ? 2 * q.pad_tokens : T) * q.ld_dim * 2);
+        q.w = take(N * q.ld_dim * 2);
+    }
+    const int64_t copies = at;
+    const auto powers = [&] {
+        q.x_exp = take(T * 4);
+        q.w_exp = take(N * 4);
+    };
+    if (q.few) {
+        at = 0;
         q.splits = few_splits(q);
-    else
+    } else {
         cut_forward(&q);
+    }
+    if (q.form == dsm::kLinearHalves) powers();
     q.y_parts = take(q.splits > 1 ? q.splits * T * q.ld_y * 4 : 0);
-    q.forward_bytes = q.few && q.splits == 1 ? 0 : at;
+    q.forward_bytes = at;
     if (!p->grads || T == 0) return q;
-    at = common;
+    at = q.back_few ? 0 : copies;
     cut_backward(&q);
     q.split_rows = T >= 1536 || N > 8192 ? 8 : 2;
     q.bias_parts = static_cast<int32_t>(q.back_form == dsm::kLinearHalves ? tiles(T, q.split_rows) : q.pad_tokens / dsm::kDzRows);
-    q.dz = take(q.pad_tokens * q.ld_wide * (q.dz_halves ? 4 : 2));
-    q.z_exp = take(T * 4);
-    q.w_tops = take(dsm::kLinearTopParts * 4);
-    q.tops = take(q.pad_tokens / q.split_rows * 4);
+    if (q.back_form == dsm::kLinearHalves) {
+        powers();
+        q.z_exp = take(T * 4);
+        q.w_tops = take(dsm::kLinearTopParts * 4);
+        q.tops = take(q.pad_tokens / q.split_rows * 4);
+    }
+    // (Few tokens of bf16 without an activation: dz is dy, however it lies.)
+    if (!q.back_few || q.f32 || p->act != DSM_ACT_NONE) q.dz = take(q.pad_tokens * q.ld_wide * (q.dz_halves ? 4 : 2));
     q.dx_parts = take(q.dx_splits > 1 ? q.dx_splits * T * q.ld_dx * 4 : 0);
     q.dw_parts = take(q.dw_splits > 1 ? q.dw_splits * N * q.ld_dx * 4 : 0);
     q.bias_sums = take(q.bias_parts * N * 4);
