@@ -117,8 +117,8 @@ __device__ __forceinline__ float activation(float z) {
 template <int ACT, bool FAST>
 __device__ __forceinline__ float slope(float z) {
     if constexpr (ACT == DSM_ACT_RELU) return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;
-    // (Beyond 50 the slopes are 0 and 1 in fp32, and their terms would overflow.)
-    const float v = z > 50.f ? 50.f : z < -50.f ? -50.f : z;
+    // (Beyond 200 every slope is 0 or 1 in fp32, and its terms would overflow.)
+    const float v = z > 200.f ? 200.f : z < -200.f ? -200.f : z;
     if constexpr (ACT == DSM_ACT_GELU) {
         float bell;
         const float share = normal_share<FAST>(v, &bell);
@@ -130,9 +130,10 @@ __device__ __forceinline__ float slope(float z) {
         u = v * __builtin_fmaf(square, kTanhA * kTanhB, kTanhA);
         rate = __builtin_fmaf(square, 3.f * kTanhA * kTanhB, kTanhA);
     }
-    // share (1 - share) without a difference; exp stays a number.
-    const float e = exp_minus<FAST>(u < -80.f ? -80.f : u), share = one_over<FAST>(1.0f + e);
-    return __builtin_fmaf(v * rate, share * (e * share), share);
+    // With t = exp(-|u|) the logistic of u is 1 / (1 + t) or t / (1 + t), and its slope their product: no
+    // difference, no overflow, and the slopes far below 0 keep their size (the hardware's exp2 takes t to 0 below 2^-126).
+    const float t = exp_minus<FAST>(fabsf(u)), near = one_over<FAST>(1.0f + t), far = t * near;
+    return __builtin_fmaf(v * rate, far * near, u < 0.f ? far : near);
 }
 
 // use(an activation's number as a type): one branch for eight entries.
