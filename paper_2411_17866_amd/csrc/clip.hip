@@ -134,12 +134,38 @@ __global__ __launch_bounds__(1024) void k_clip_norms(ClipGroups g, const double*
     factor[blockIdx.x] = factor_of(g, v);
 }
 
+// v in fp32, on v's side of a middle between two numbers of bf16 that it is rounded to.
+__device__ __forceinline__ float beside_middle(double v) {
+    const float f = static_cast<float>(v);
+    uint32_t bits = __builtin_bit_cast(uint32_t, f);
+    if ((bits & 0xffffu) == 0x8000u && f != v) bits += fabs(static_cast<double>(f)) < fabs(v) ? 1u : ~0u;
+    return __builtin_bit_cast(float, bits);
+}
+
+// x times `by` in fp64, in fp32 for the store.  bf16 is rounded twice then, which comes to one rounding of the
+// product but where fp32's falls on a middle, as one in 2^16 does by chance: only those are looked at.  (50257 x 768
+// with rows apart, 77 MB: 43 us; 45 with every product looked at, 42 with none.)
+template <bool F32>
+__device__ __forceinline__ void times(V8& x, double by) {
+    V8 f;
+    bool middle = false;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        f.v[q] = static_cast<float>(x.v[q] * by);
+        middle |= static_cast<uint16_t>(__builtin_bit_cast(uint32_t, f.v[q])) == 0x8000u;
+    }
+    if (!F32 && middle) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) f.v[q] = beside_middle(x.v[q] * by);
+    }
+    x = f;
+}
+
 template <bool F32>
 __device__ __forceinline__ void scale(const Chunk& k, double by) {
     each_run<F32>(k, [&](int64_t at, int have, int apart) {
         V8 x = rows::load8<F32>(k.e.data, at, have, apart);
-#pragma unroll
-        for (int q = 0; q < 8; ++q) x.v[q] = static_cast<float>(x.v[q] * by);
+        times<F32>(x, by);
         rows::store8<F32>(k.e.data, at, x, have, apart);
     });
 }
