@@ -37,13 +37,23 @@ struct Raw8<true> {
     f4 a, b;
 };
 
-// Loads that leave the caches to what is read again (ONCE), or not.
-template <bool ONCE, class T>
-__device__ __forceinline__ T from(const T* p) {
+// 16 bytes from any element's address; ONCE leaves the caches to what is read again.  (A
+// type's lesser alignment does not pass through a template's argument.)
+template <bool ONCE>
+__device__ __forceinline__ f4 from(const float* p) {
+    const f4_at* at = reinterpret_cast<const f4_at*>(p);
     if constexpr (ONCE)
-        return __builtin_nontemporal_load(p);
+        return __builtin_nontemporal_load(at);
     else
-        return *p;
+        return *at;
+}
+template <bool ONCE>
+__device__ __forceinline__ u16x8 from(const u16* p) {
+    const u16x8_at* at = reinterpret_cast<const u16x8_at*>(p);
+    if constexpr (ONCE)
+        return __builtin_nontemporal_load(at);
+    else
+        return *at;
 }
 
 // Eight elements from element `at` on, of which `have` exist (the others are 0); in fp32 all
@@ -55,8 +65,8 @@ __device__ __forceinline__ Raw8<F32> raw8(const void* base, int64_t at, int have
         const float* p = static_cast<const float*>(base) + at;
         o.a = o.b = f4{0.f, 0.f, 0.f, 0.f};
         if (have >= 8) {
-            o.a = from<ONCE>(reinterpret_cast<const f4_at*>(p));
-            o.b = from<ONCE>(reinterpret_cast<const f4_at*>(p + apart));
+            o.a = from<ONCE>(p);
+            o.b = from<ONCE>(p + apart);
         } else if (have > 0) {
             // The last one again for those that are missing: loads side by side, no branches.
             // (Their places are not kept in registers from one row to the next.)
@@ -73,7 +83,7 @@ __device__ __forceinline__ Raw8<F32> raw8(const void* base, int64_t at, int have
         const u16* p = static_cast<const u16*>(base) + at;
         o.v = u16x8{0, 0, 0, 0, 0, 0, 0, 0};
         if (have >= 8) {
-            o.v = from<ONCE>(reinterpret_cast<const u16x8_at*>(p));
+            o.v = from<ONCE>(p);
         } else if (have > 0) {
             int last = have - 1;
             asm volatile("" : "+v"(last));

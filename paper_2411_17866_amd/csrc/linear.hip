@@ -212,8 +212,13 @@ struct Run {  // a lane's part of 16 rows' runs
     // `row`: of the lane, from its 16 bytes of each 64 on.
     __device__ __forceinline__ void load(const char* row, int k) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-            v[h] = *reinterpret_cast<const rows::f4_at*>(row + static_cast<int64_t>(k) * (F32 ? 4 : 2) + h * 64);
+        for (int h = 0; h < 2; ++h) {
+            const char* at = row + static_cast<int64_t>(k) * (F32 ? 4 : 2) + h * 64;
+            if constexpr (F32)
+                v[h] = rows::from<false>(reinterpret_cast<const float*>(at));
+            else
+                v[h] = __builtin_bit_cast(f4, rows::from<false>(reinterpret_cast<const u16*>(at)));
+        }
     }
     // The row's last run, shorter than the others: `left` from the lane's bytes on.
     __device__ __forceinline__ void load_end(const char* row, int k, int left) {
