@@ -512,7 +512,8 @@ DSM_API dsm_status dsm_ortho_step(const dsm_ortho_problem* problem, const dsm_or
  */
 
 /* Activations: relu max(z, 0); gelu z (1 + erf(z / sqrt 2)) / 2; gelu_tanh
- * z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2; silu z / (1 + exp(-z)). */
+ * z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2; silu z / (1 + exp(-z)).
+ * (In fp32: results of the last two under 2^-119 may be 0.) */
 typedef enum dsm_act {
     DSM_ACT_NONE = 0,
     DSM_ACT_RELU = 1,

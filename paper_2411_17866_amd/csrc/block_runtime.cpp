@@ -49,8 +49,11 @@ double join_time(int parts, int64_t n, double each) {
     return parts > 1 ? 4.4 + each * 2e-6 * static_cast<double>(n * parts) : 0.0;
 }
 
-// fp32 products as they are up to this many tokens.  128 tokens of 4096 -> 4800 forward: 58 us by tiles of fp32, 67 as
-// halves; 13 tokens of 6400 -> 4800 backward: 72 and 165; 74 of 1024 -> 6400 backward as halves: 46.
+// fp32 products as they are up to this many tokens; microseconds as they are, and as halves.  Forward, 128 tokens:
+// 4096 -> 4800 60 and 67, 1600 -> 6400 38.4 and 39.5, 768 -> 2304 13.5 and 18.5; 129, a third row of tiles: 90 and 75, 53
+// and 43, 15.5 and 18.2; 192: 90 and 76, 63 and 44, 20 and 19.  Gradients, 33 tokens: 6400 -> 4800 124 and 137, 6400 -> 1600 58
+// and 56, 768 -> 2304 21 and 26; 64: 126 and 152, 60 and 58, 21 and 27 (6400 -> 6400 173, library products 133).  More
+// than 64 have no kernel of their own: 65 as halves 154, 59 and 30.
 constexpr int64_t kSingleForward = 128, kSingleBackward = 64;
 // bf16 gradients without tiles up to this many tokens: 1600 -> 6400 of 17 tokens 20.3 us and 25.4 by tiles, of 33
 // 24.7 and 26.4, of 64 25.5 and 20.9; 768 -> 2304 of 32 10.1 and 13.8, of 64 12.3 and 11.4.

@@ -10,7 +10,9 @@
 //
 // It is bound by memory: all gradients are read, and where the norm exceeds the
 // maximum read again and written.  The second pass takes the chunks from the last to
-// the first: what was read last is still in the last-level cache.
+// the first: what was read last is still in the last-level cache.  Rows apart whose width or
+// first element is no multiple of eight go an element a lane, eight times the instructions: 16384 x 1601
+// in bf16 198 us (norm alone 86), x 1600 and x 1608 34 (14); in fp32 170 (76) and 54 (20).
 #include "block_internal.h"
 #include "elements.h"
 

@@ -4,8 +4,9 @@
 //   dz = dy act'(z);  dx = dz w;  dw = dz^T x;  dbias = sum over the tokens of dz
 //
 // Up to kLinearFew tokens the forward pass is bound by reading w once: k_few does it
-// in one launch, without tiles in LDS and without copies.  More tokens go through the
-// tiles of gemm_tile.h with bias, activation and residual in their epilogue.  The
+// without tiles in LDS and without copies, in one launch, or where few rows of w leave
+// CUs idle in parts of k that a second one joins.  More tokens go through the tiles of
+// gemm_tile.h with bias, activation and residual in their epilogue.  The
 // gradients are two products of dz in one launch, dz being made by a pass of its own,
 // which also sums dbias; where there is no activation, dy is taken where it lies.
 //
@@ -65,7 +66,8 @@ constexpr int kNoExponent = 10000;  // of a row of zeros: brings everything to 0
 //
 // FAST, for results that are rounded to bf16: the hardware's exp2 and reciprocal
 // (2^-22).  The epilogue's arithmetic does not overlap the next tile's products, so
-// every instruction of it counts.
+// every instruction of it counts.  (silu and gelu_tanh are 0 where 1 + exp(-v) passes
+// fp32's range, or its reciprocal falls below the normal numbers: results under 2^-119.)
 
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr float kTanhA = 1.59576912160573071f;  // 2 sqrt(2 / pi): (1 + tanh(u)) / 2 = logistic(2 u)
@@ -192,7 +194,6 @@ __device__ __forceinline__ V8 bias8(const LinearCall& c, int col) {
 
 // ---- Few tokens ----
 
-typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bfloat8 __attribute__((ext_vector_type(8)));
 
 // 16 rows of w by G times 16 tokens a work-group, whose waves take every eighth run of
