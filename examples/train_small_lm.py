@@ -1,14 +1,17 @@
-"""Trains a small language model with the library's operators end to end: the output
-layer's cross entropy and its gradients (ops.LinearCE), orthogonalised momentum as the
-direction of the hidden matrices (ops.Ortho), and distributed sign momentum with local
-steps over the whole parameter arena.
+"""Trains a small language model with the library's operators end to end: the hidden
+layer and its gradients (ops.Linear), the output layer's cross entropy and its gradients
+(ops.LinearCE), clipping by each worker's global norm (ops.ArenaClip), orthogonalised
+momentum as the direction of the hidden matrices (ops.Ortho), and distributed sign
+momentum with local steps over the whole parameter arena.
 
 The model predicts a token from the two before it:  a = E[t-1] + F[t-2],
 h = a + relu(a U^T) V^T, logits = h W^T.  Its data is a synthetic second-order Markov
 chain.  Every worker has its own replica and stream of tokens; each local step takes
 
+  * the hidden layer through two Linear plans, the second onto the residual a;
   * h and W through LinearCE, whose dw is written into the worker's gradient arena;
-  * dh back through the hidden layer into the arena (plain torch products);
+  * dh back through the hidden layer, whose dw are written into the arena too;
+  * every worker's gradients through the clip, in the arena;
   * the hidden matrices' gradients through momentum and orthogonalisation, in the arena
     (every worker's in one call);
   * the local step of the arena with that direction (SGD, beta1 = 0);
@@ -29,7 +32,7 @@ from paper_2411_17866_amd import arena, dsm, ops  # noqa: E402
 VOCAB, DIM, HIDDEN = 1009, 96, 200
 WORKERS, LOCAL_STEPS, TOKENS = 2, 4, 700
 SHAPES = {"E": (VOCAB, DIM), "F": (VOCAB, DIM), "U": (HIDDEN, DIM), "V": (DIM, HIDDEN), "W": (VOCAB, DIM)}
-LR, MU, GAMMA = 0.3, 0.9, 2e-3
+LR, MU, GAMMA, CLIP = 0.3, 0.9, 2e-3, 30.0
 GLOBAL = dict(eta=0.8, beta1=0.95, beta2=0.98, lam=0.0)
 
 
@@ -55,7 +58,10 @@ class Model:
         self.ar.x.normal_(0.0, 0.05, generator=self.generator)
         self.ar.init()
         self.batch = chain(self.generator)
+        self.up = ops.Linear(TOKENS, DIM, HIDDEN, act="relu")
+        self.down = ops.Linear(TOKENS, HIDDEN, DIM)
         self.loss = ops.LinearCE(TOKENS, DIM, VOCAB)
+        self.clip = ops.ArenaClip(self.ar)
         # The hidden matrices of every worker, by their places in the gradient arena.
         self.momentum = torch.zeros_like(self.ar.g_rep)
         self.ortho = []
@@ -76,13 +82,13 @@ class Model:
         p, g = self.views(source, worker), self.views(self.ar.g_rep, worker)
         last, before, target = self.batch(TOKENS)
         a = p["E"][last] + p["F"][before]
-        z = a @ p["U"].t()
-        h = a + z.relu() @ p["V"].t()
+        inner = self.up(a, p["U"])
+        h = self.down(inner["y"], p["V"], residual=a)["y"]
         out = self.loss(h, p["W"], target, dw=g["W"])
-        dz = (out["dh"] @ p["V"]) * (z > 0)
-        da = out["dh"] + dz @ p["U"]
-        torch.mm(out["dh"].t(), z.relu(), out=g["V"])
-        torch.mm(dz.t(), a, out=g["U"])
+        weights = ("dx", "dw")
+        back = self.down.backward(out["dh"], inner["y"], p["V"], dw=g["V"], wanted=weights)
+        back = self.up.backward(back["dx"], a, p["U"], z=inner["z"], dw=g["U"], wanted=weights)
+        da = out["dh"] + back["dx"]
         for name, tokens in (("E", last), ("F", before)):
             g[name].zero_().index_add_(0, tokens, da)
             g[name].mul_(30.0)
@@ -96,6 +102,7 @@ class Model:
             # After a global step without broadcast the replicas are x.
             losses = [self.gradients(i, stale=k == 0 and t > 0) for i in range(WORKERS)]
             total = total + torch.stack(losses).mean()
+            self.clip(self.ar, max_norm=CLIP)
             for plan, scale in self.ortho:
                 plan.direction(self.momentum, self.ar.g_rep, self.ar.g_rep, mu=MU, scale=scale)
             self.step += 1
