@@ -10,9 +10,7 @@
 //
 // It is bound by memory: all gradients are read, and where the norm exceeds the
 // maximum read again and written.  The second pass takes the chunks from the last to
-// the first: what was read last is still in the last-level cache.  Rows apart whose width or
-// first element is no multiple of eight go an element a lane, eight times the instructions: 16384 x 1601
-// in bf16 198 us (norm alone 86), x 1600 and x 1608 34 (14); in fp32 170 (76) and 54 (20).
+// the first: what was read last is still in the last-level cache.
 #include "block_internal.h"
 #include "elements.h"
 
@@ -45,9 +43,54 @@ __device__ __forceinline__ Chunk chunk_of(const ClipTable& t, int c) {
     return k;
 }
 
-// Calls use(offset from data, elements, 4) for runs of up to eight elements that lie side by
-// side; in fp32 also use(offset, 8, apart) for two runs of four: neighbouring lanes then
-// load whole lines (496 MB clipped in 261 us instead of 272).
+// Where up to eight elements lie, as offsets from data.
+struct Run {  // side by side; in fp32 also two fours, `apart` from each other
+    int64_t at;
+    int have, apart;
+};
+struct Spread {  // each by itself
+    int64_t at[8];
+    int have;
+};
+template <bool F32, bool ONCE = false>
+__device__ __forceinline__ V8 load(const void* data, const Run& r) {
+    return rows::load8<F32, ONCE>(data, r.at, r.have, r.apart);
+}
+template <bool F32>
+__device__ __forceinline__ void store(void* data, const Run& r, const V8& x) {
+    rows::store8<F32>(data, r.at, x, r.have, r.apart);
+}
+template <bool F32, bool ONCE = false>
+__device__ __forceinline__ V8 load(const void* data, const Spread& s) {
+    V8 x;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        x.v[q] = 0.f;
+        if (q >= s.have) continue;
+        if constexpr (F32)
+            x.v[q] = static_cast<const float*>(data)[s.at[q]];
+        else
+            x.v[q] = rows::bf16_to_float(static_cast<const rows::u16*>(data)[s.at[q]]);
+    }
+    return x;
+}
+template <bool F32>
+__device__ __forceinline__ void store(void* data, const Spread& s, const V8& x) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        if (q >= s.have) continue;
+        if constexpr (F32)
+            static_cast<float*>(data)[s.at[q]] = x.v[q];
+        else
+            static_cast<rows::u16*>(data)[s.at[q]] = rows::float_to_bf16(x.v[q]);
+    }
+}
+
+// Calls use(Run or Spread) for all elements of a chunk.  In fp32 neighbouring lanes load whole
+// lines as two fours (496 MB clipped in 261 us instead of 272).  Rows apart whose width or first element is no
+// multiple of eight have no eights in common with the chunk's: there a lane takes eight elements 256 from
+// each other, and its neighbours those beside them (16384 x 1601 in bf16 88 us, the norm alone 37, where one
+// element at a time took 198 and 86; x 1600 34 and 14).
 template <bool F32, class F>
 __device__ __forceinline__ void each_run(const Chunk& k, F use) {
     const int64_t start = k.e.first + k.at;
@@ -55,27 +98,36 @@ __device__ __forceinline__ void each_run(const Chunk& k, F use) {
         const int whole = k.n & ~2047;
 #pragma unroll 4
         for (int u = 0; u < whole; u += 2048)
-            use(start + u + threadIdx.x * (F32 ? 4 : 8), 8, F32 ? 1024 : 4);
+            use(Run{static_cast<int64_t>(start + u + threadIdx.x * (F32 ? 4 : 8)), 8, F32 ? 1024 : 4});
         const int u = whole + static_cast<int>(threadIdx.x) * 8;
-        if (u < k.n) use(start + u, k.n - u, 4);
+        if (u < k.n) use(Run{start + u, k.n - u, 4});
         return;
     }
     const int64_t row = start / k.e.block, col = start - row * k.e.block;
-    const int wide = start % 8 == 0 && k.e.block % 8 == 0 ? 8 : 1;
+    const bool eights = start % 8 == 0 && k.e.block % 8 == 0;
+    const auto elements = [&](auto place) {
+        if (eights) {
+#pragma unroll 4
+            for (int u = threadIdx.x * 8; u < k.n; u += 2048) use(Run{place(u), min(8, k.n - u), 4});
+            return;
+        }
+        for (int u = threadIdx.x; u < k.n; u += 2048) {
+            Spread s;
+            s.have = min(8, (k.n - u + 255) / 256);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) s.at[q] = place(u + q * 256);
+            use(s);
+        }
+    };
     if (k.e.block >= kClipChunk) {  // at most one row ends inside
         const int left = static_cast<int>(min(k.e.block - col, static_cast<int64_t>(kClipChunk)));
-#pragma unroll 4
-        for (int u = threadIdx.x * wide; u < k.n; u += 256 * wide) {
-            const int64_t at = u < left ? row * k.e.stride + col + u : (row + 1) * k.e.stride + u - left;
-            use(at, min(wide, k.n - u), 4);
-        }
+        elements([&](int u) { return u < left ? row * k.e.stride + col + u : (row + 1) * k.e.stride + u - left; });
     } else {
         const unsigned block = static_cast<unsigned>(k.e.block), c0 = static_cast<unsigned>(col);
-#pragma unroll 4
-        for (int u = threadIdx.x * wide; u < k.n; u += 256 * wide) {
+        elements([&](int u) {
             const unsigned c = c0 + u, r = c / block;
-            use((row + r) * k.e.stride + (c - r * block), min(wide, k.n - u), 4);
-        }
+            return static_cast<int64_t>((row + r) * k.e.stride + (c - r * block));
+        });
     }
 }
 
@@ -93,8 +145,8 @@ __device__ __forceinline__ double group_sum(double v) {
 template <bool F32, bool ONCE>
 __device__ __forceinline__ double squares(const Chunk& k) {
     double a = 0.0, b = 0.0;
-    each_run<F32>(k, [&](int64_t at, int have, int apart) {
-        const V8 x = rows::load8<F32, ONCE>(k.e.data, at, have, apart);
+    each_run<F32>(k, [&](const auto& at) {
+        const V8 x = load<F32, ONCE>(k.e.data, at);
 #pragma unroll
         for (int q = 0; q < 8; q += 2) {
             const double u = x.v[q], v = x.v[q + 1];
@@ -165,10 +217,10 @@ __device__ __forceinline__ void times(V8& x, double by) {
 
 template <bool F32>
 __device__ __forceinline__ void scale(const Chunk& k, double by) {
-    each_run<F32>(k, [&](int64_t at, int have, int apart) {
-        V8 x = rows::load8<F32>(k.e.data, at, have, apart);
+    each_run<F32>(k, [&](const auto& at) {
+        V8 x = load<F32>(k.e.data, at);
         times<F32>(x, by);
-        rows::store8<F32>(k.e.data, at, x, have, apart);
+        store<F32>(k.e.data, at, x);
     });
 }
 __device__ __forceinline__ void scale(const Chunk& k, double by) {
