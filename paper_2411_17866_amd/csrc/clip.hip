@@ -86,36 +86,50 @@ __device__ __forceinline__ void store(void* data, const Spread& s, const V8& x) 
     }
 }
 
-// Calls use(Run or Spread) for all elements of a chunk.  In fp32 neighbouring lanes load whole
+// Calls use(array of Runs or Spreads, whose loads go side by side) for all elements of a chunk.  In fp32 neighbouring lanes load whole
 // lines as two fours (496 MB clipped in 261 us instead of 272).  Rows apart whose width or first element is no
 // multiple of eight have no eights in common with the chunk's: there a lane takes eight elements 256 from
-// each other, and its neighbours those beside them (16384 x 1601 in bf16 88 us, the norm alone 37, where one
-// element at a time took 198 and 86; x 1600 34 and 14).
+// each other, and its neighbours those beside them (16384 x 1601 in fp32 99 us, where an element at a time
+// took 171; x 1600 55).
 template <bool F32, class F>
 __device__ __forceinline__ void each_run(const Chunk& k, F use) {
     const int64_t start = k.e.first + k.at;
     if (k.e.block >= k.e.first + k.e.numel) {  // one run
-        const int whole = k.n & ~2047;
-#pragma unroll 4
-        for (int u = 0; u < whole; u += 2048)
-            use(Run{static_cast<int64_t>(start + u + threadIdx.x * (F32 ? 4 : 8)), 8, F32 ? 1024 : 4});
-        const int u = whole + static_cast<int>(threadIdx.x) * 8;
-        if (u < k.n) use(Run{start + u, k.n - u, 4});
+        const auto whole = [&](int u) { return Run{static_cast<int64_t>(start + u + threadIdx.x * (F32 ? 4 : 8)), 8, F32 ? 1024 : 4}; };
+        int u = 0;
+        for (; u + 8192 <= k.n; u += 8192) {
+            const Run runs[4] = {whole(u), whole(u + 2048), whole(u + 4096), whole(u + 6144)};
+            use(runs);
+        }
+        for (; u + 2048 <= k.n; u += 2048) {
+            const Run runs[1] = {whole(u)};
+            use(runs);
+        }
+        u += static_cast<int>(threadIdx.x) * 8;
+        const Run runs[1] = {Run{start + u, k.n - u, 4}};
+        if (u < k.n) use(runs);
         return;
     }
     const int64_t row = start / k.e.block, col = start - row * k.e.block;
     const bool eights = start % 8 == 0 && k.e.block % 8 == 0;
     const auto elements = [&](auto place) {
         if (eights) {
-#pragma unroll 4
-            for (int u = threadIdx.x * 8; u < k.n; u += 2048) use(Run{place(u), min(8, k.n - u), 4});
+            int u = threadIdx.x * 8;
+            for (; u + 6144 + 8 <= k.n; u += 8192) {
+                const Run runs[4] = {{place(u), 8, 4}, {place(u + 2048), 8, 4}, {place(u + 4096), 8, 4}, {place(u + 6144), 8, 4}};
+                use(runs);
+            }
+            for (; u < k.n; u += 2048) {
+                const Run runs[1] = {{place(u), min(8, k.n - u), 4}};
+                use(runs);
+            }
             return;
         }
         for (int u = threadIdx.x; u < k.n; u += 2048) {
-            Spread s;
-            s.have = min(8, (k.n - u + 255) / 256);
+            Spread s[1];
+            s[0].have = min(8, (k.n - u + 255) / 256);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) s.at[q] = place(u + q * 256);
+            for (int q = 0; q < 8; ++q) s[0].at[q] = place(u + q * 256);
             use(s);
         }
     };
@@ -146,13 +160,18 @@ template <bool F32, bool ONCE>
 __device__ __forceinline__ double squares(const Chunk& k) {
     double a = 0.0, b = 0.0;
     each_run<F32>(k, [&](const auto& at) {
-        const V8 x = load<F32, ONCE>(k.e.data, at);
+        constexpr int N = sizeof(at) / sizeof(at[0]);
+        V8 x[N];
 #pragma unroll
-        for (int q = 0; q < 8; q += 2) {
-            const double u = x.v[q], v = x.v[q + 1];
-            a = __builtin_fma(u, u, a);
-            b = __builtin_fma(v, v, b);
-        }
+        for (int i = 0; i < N; ++i) x[i] = load<F32, ONCE>(k.e.data, at[i]);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int q = 0; q < 8; q += 2) {
+                const double u = x[i].v[q], v = x[i].v[q + 1];
+                a = __builtin_fma(u, u, a);
+                b = __builtin_fma(v, v, b);
+            }
     });
     return a + b;
 }
@@ -188,39 +207,47 @@ __global__ __launch_bounds__(1024) void k_clip_norms(ClipGroups g, const double*
     factor[blockIdx.x] = factor_of(g, v);
 }
 
-// v in fp32, on v's side of a middle between two numbers of bf16 that it is rounded to.
-__device__ __forceinline__ float beside_middle(double v) {
-    const float f = static_cast<float>(v);
-    uint32_t bits = __builtin_bit_cast(uint32_t, f);
-    if ((bits & 0xffffu) == 0x8000u && f != v) bits += fabs(static_cast<double>(f)) < fabs(v) ? 1u : ~0u;
-    return __builtin_bit_cast(float, bits);
+// Ten of v's bits, the last of them set where anything follows: exact in fp32 down to where bf16 is 0, and rounded
+// to bf16 as v itself.
+__device__ __forceinline__ float ten_bits(double v) {
+    const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+    const uint32_t high = static_cast<uint32_t>(bits >> 32), low = static_cast<uint32_t>(bits);
+    const uint32_t rest = ((high & 0x3ffu) | low) != 0 ? 0x400u : 0u;
+    return static_cast<float>(__builtin_bit_cast(double, static_cast<uint64_t>((high & ~0x3ffu) | rest) << 32));
 }
 
-// x times `by` in fp64, in fp32 for the store.  bf16 is rounded twice then, which comes to one rounding of the
-// product but where fp32's falls on a middle, as one in 2^16 does by chance: only those are looked at.  (50257 x 768
-// with rows apart, 77 MB: 43 us; 45 with every product looked at, 42 with none.)
-template <bool F32>
-__device__ __forceinline__ void times(V8& x, double by) {
-    V8 f;
-    bool middle = false;
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-        f.v[q] = static_cast<float>(x.v[q] * by);
-        middle |= static_cast<uint16_t>(__builtin_bit_cast(uint32_t, f.v[q])) == 0x8000u;
-    }
-    if (!F32 && middle) {
-#pragma unroll
-        for (int q = 0; q < 8; ++q) f.v[q] = beside_middle(x.v[q] * by);
-    }
-    x = f;
-}
-
+// Products in fp64.  bf16 is rounded by way of fp32, which comes to one rounding of the product but where fp32's falls
+// on a middle of bf16's (its lower half is 0x8000, the least of 16 signed bits), as one in 2^16 does by chance: where one of
+// a lane's eight does, they go by their first ten bits.  (Nine tensors of 100 x 201 and less, both launches: 6.63 us,
+// 6.92 with every product's ten bits, 6.48 with neither; loads of four runs go before their first store.)
 template <bool F32>
 __device__ __forceinline__ void scale(const Chunk& k, double by) {
+    typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
     each_run<F32>(k, [&](const auto& at) {
-        V8 x = load<F32>(k.e.data, at);
-        times<F32>(x, by);
-        store<F32>(k.e.data, at, x);
+        constexpr int N = sizeof(at) / sizeof(at[0]);
+        V8 x[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = load<F32>(k.e.data, at[i]);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            V8 f;
+            i16x2 least = {0, 0};
+#pragma unroll
+            for (int q = 0; q < 8; ++q) f.v[q] = static_cast<float>(x[i].v[q] * by);
+            if constexpr (!F32) {
+#pragma unroll
+                for (int q = 0; q < 8; q += 2) {
+                    const i16x2 halves = {static_cast<int16_t>(__builtin_bit_cast(uint32_t, f.v[q])),
+                                          static_cast<int16_t>(__builtin_bit_cast(uint32_t, f.v[q + 1]))};
+                    least = __builtin_elementwise_min(least, halves);
+                }
+                if (__builtin_expect(min(least[0], least[1]) == INT16_MIN, 0)) {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) f.v[q] = ten_bits(x[i].v[q] * by);
+                }
+            }
+            store<F32>(k.e.data, at[i], f);
+        }
     });
 }
 __device__ __forceinline__ void scale(const Chunk& k, double by) {
